@@ -44,6 +44,7 @@ extern "C" {
 
 #define UNITY_MAX_MODELS 16
 #define UNITY_MAX_ROLES 64
+#define UNITY_MAX_TOP 128            /* listed teacher entries per token                         */
 #define UNITY_N_METRICS 8            /* per class: n_valid, mean pg loss, mean KL, mean entropy,
                                         clip fraction, mean ratio, mean logp, mean advantage     */
 
@@ -402,6 +403,65 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
                            const float* old_logp, const float* ref_logp, const float* adv_tok, float* loss,
                            float* metrics, float* logp, float* entropy, float* tok_loss, void* dHidden,
                            void* const* dW);
+
+/* ------------------------------------------------------------------------------------------------
+ * Token losses on the same rows (no counterpart in the paper): what a role model learns from before and beside the policy
+ * update - recorded answers (cross entropy) or a teacher's listed logits (distillation).  Rows, routing, masks and
+ * limits are those of stages 2 and 3; with z = inv_temperature * W_{model(i)} h_i, p = softmax(z), lse = log sum exp z:
+ *   loss[k] = (1/M_k) sum_{valid i of model k} tok_weight[i] * l_i ,  M_k = norm[k] if given else max(#valid rows, 1)
+ * Forms: evaluation (dHidden and dW NULL: one sweep over the vocabulary), frozen head (dW NULL), training.  The logits
+ * exist only in tensor memory; the backward works on bounded blocks of dL/dz.
+ *   tok_weight : f32 [n_tok] or NULL (= all 1), any sign; not read where tok_mask is 0
+ *   loss       : out f32 [K];  tok_loss (l_i, without its weight), lse : out f32 [n_tok] or NULL, 0 on masked rows
+ *   dHidden    : out bf16 [n_tok, H] or NULL (zeros on masked rows)
+ *   dW         : (host) K device pointers or NULL, each f32 or bf16 [V, H] (dW_type).  bf16 is rounded once, from the fp32
+ *                sum over all rows (plus the old value with accumulate_dW)
+ * dL/dz is held in bf16 between the products, as in stage 3: a gradient entry is off by up to 2^-8 of the terms it sums.
+ * Deterministic: no floating-point atomics anywhere. */
+#define UNITY_F32 0
+#define UNITY_BF16 1
+#define UNITY_TEACHER_LOGITS 0   /* q = softmax over the row's listed entries of inv_temperature * top_vals           */
+#define UNITY_TEACHER_LOGPROBS 1 /* q = exp(top_vals) as given; what the list leaves out is left out of the loss      */
+
+/* Scratch bytes with which the calls below run with full-size blocks (n_top = 0 for the cross entropy, backward = 0
+ * for evaluation only). */
+size_t unity_token_loss_workspace_bytes(int64_t n_tok, int32_t H, int32_t V, int32_t K, int32_t n_top, int32_t backward);
+
+/* Cross entropy of the targets:
+ *   l_i = (1 - eps) (lse - z_target) + eps (lse - mean_v z_v) + z_loss * lse^2
+ *   dl_i/dz_v = (1 + 2 z_loss lse) p_v - (1 - eps) [v = target] - eps/V */
+typedef struct {
+    float label_smoothing; /* eps in [0, 1) */
+    float z_loss;          /* >= 0 */
+    const float* norm;     /* (host) f32 [K] or NULL */
+    int accumulate_dW;     /* 0: overwrite dW, 1: add to it */
+    int dW_type;           /* UNITY_F32 or UNITY_BF16 */
+} unity_ce_params;
+int unity_cross_entropy_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_ce_params* params,
+                                const float* tok_weight, float* loss, float* tok_loss, float* lse, void* dHidden,
+                                void* const* dW);
+
+/* Distillation from a teacher's listed entries, optionally mixed with the cross entropy of the targets:
+ *   l_i = kd_coef * sum_v q_v (log q_v - z_v + lse) + hard_coef (lse - z_target)      (v over the listed entries)
+ *   dl_i/dz_v = (kd_coef sum q + hard_coef) p_v - kd_coef q_v - hard_coef [v = target]
+ *   top_ids  : int32 [n_tok, n_top], any order; a negative id is an empty place, equal ids add up their q; an id >= V
+ *              flags UNITY_ERR_BAD_INDEX and counts as empty.  A row without entries has no distillation loss
+ *   top_vals : f32 [n_tok, n_top], logits or log-probabilities (teacher_mode); -inf is a probability of 0; not read in
+ *              empty places
+ * rows->target is read only when hard_coef > 0 and may be NULL otherwise.  The temperature is inv_temperature; a factor
+ * of its square, where it is wanted, belongs into kd_coef. */
+typedef struct {
+    int32_t n_top;         /* 1 .. UNITY_MAX_TOP */
+    int teacher_mode;      /* UNITY_TEACHER_* */
+    float kd_coef;         /* >= 0 */
+    float hard_coef;       /* >= 0 */
+    const float* norm;     /* (host) f32 [K] or NULL */
+    int accumulate_dW;
+    int dW_type;
+} unity_distill_params;
+int unity_distill_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_distill_params* params,
+                          const int32_t* top_ids, const float* top_vals, const float* tok_weight, float* loss,
+                          float* tok_loss, float* lse, void* dHidden, void* const* dW);
 
 #ifdef __cplusplus
 }

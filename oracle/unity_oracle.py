@@ -30,8 +30,10 @@ What each function follows:
   reflector of round i being paid the improvement of round i+1); an agent that ended the loop gets 0.
 * ``gae``             - the generalized-advantage equation printed in the same section
   (A_t = sum_l (gamma lambda)^l delta_{t+l}), evaluated as the literal double sum.
+* ``token_loss_fwd_bwd`` - cross entropy with label smoothing and z-loss, and distillation from a teacher's listed
+  entries (no counterpart in the paper), on the rows and heads of the update.
 
-Pins: tests/test_oracle_pins.py (closed forms, invariants, library special cases, finite
+Pins: tests/test_oracle_pins.py and tests/test_token_loss_oracle.py (closed forms, invariants, library special cases, finite
 differences, autograd third opinion, brute force).  No function here is unpinned.
 """
 from __future__ import annotations
@@ -529,3 +531,74 @@ def align_rewards(r_inv, cu_seqlens, tok_mask=None):
                 out[t] = r[s]
                 break
     return out
+
+
+# ----------------------------------------------------------------------------------------------
+# token losses: cross entropy and distillation from a teacher's listed entries
+# ----------------------------------------------------------------------------------------------
+
+def teacher_rows(top_ids, top_vals, V, logits, inv_temperature=1.0) -> np.ndarray:
+    """Dense teacher probabilities [n, V]: softmax over the row's listed entries, or exp of listed log-probabilities.
+    Negative ids and ids >= V are empty places; equal ids add up; a row without entries is zero."""
+    ids = np.asarray(top_ids, dtype=np.int64)
+    q = np.zeros((ids.shape[0], V), F64)
+    for i in range(ids.shape[0]):
+        on = (ids[i] >= 0) & (ids[i] < V)
+        t = to_f64(top_vals)[i][on]
+        if logits:
+            t = t * inv_temperature
+            if t.size and t.max() == -np.inf:
+                t = t[:0]
+                on[:] = False
+            e = np.exp(t - t.max()) if t.size else t
+            w = e / e.sum() if t.size else e
+        else:
+            w = np.exp(t)
+        np.add.at(q[i], ids[i][on], w)
+    return q
+
+
+def token_loss_fwd_bwd(hidden, W, cu_seqlens, inv_role, role_model, target, tok_mask=None, tok_weight=None, norm=None,
+                       inv_temperature=1.0, label_smoothing=0.0, z_loss=0.0, teacher=None, kd_coef=1.0, hard_coef=0.0):
+    """Loss per model, per-token l and lse, dHidden, dW and the logit gradients G [N, V] (all float64).
+
+    ``teacher`` None: cross entropy of ``target`` with label smoothing and z-loss.  Otherwise dense teacher
+    probabilities [N, V] (teacher_rows): distillation, mixed with the targets' cross entropy by ``hard_coef``.
+    """
+    cu = np.asarray(cu_seqlens, dtype=np.int64)
+    n_tok, H, V, tau = int(cu[-1]), hidden.shape[1], W[0].shape[0], float(inv_temperature)
+    tok_model = token_role_model(cu, inv_role, role_model)[1]
+    on = np.ones(n_tok, bool) if tok_mask is None else np.asarray(tok_mask) != 0
+    w = np.ones(n_tok, F64) if tok_weight is None else to_f64(tok_weight)
+    loss, l, lse = np.zeros(len(W), F64), np.zeros(n_tok, F64), np.zeros(n_tok, F64)
+    G, dH, dW, M = np.zeros((n_tok, V), F64), np.zeros((n_tok, H), F64), [], []
+    for k in range(len(W)):
+        i = np.nonzero(on & (tok_model == k))[0]
+        M.append(float(norm[k]) if norm is not None else max(float(i.size), 1.0))
+        Wk, h = to_f64(W[k]), to_f64(hidden[i])
+        if i.size:
+            Z = tau * (h @ Wk.T)
+            lse[i], _, P = _row_stats(Z)
+            logP = Z - lse[i][:, None]
+            soft = np.zeros_like(P)
+            if teacher is None:
+                soft += label_smoothing / V
+                soft[np.arange(i.size), np.asarray(target)[i]] += 1.0 - label_smoothing
+                l[i] = -(soft * logP).sum(1) + z_loss * lse[i] ** 2
+                g = (1.0 + 2.0 * z_loss * lse[i])[:, None] * P - soft
+            else:
+                q = teacher[i]
+                with np.errstate(divide="ignore", invalid="ignore"):
+                    l[i] = kd_coef * (np.where(q > 0, q * np.log(q), 0.0) - q * logP).sum(1)
+                soft += kd_coef * q
+                mass = kd_coef * q.sum(1)
+                if hard_coef > 0:
+                    soft[np.arange(i.size), np.asarray(target)[i]] += hard_coef
+                    l[i] -= hard_coef * logP[np.arange(i.size), np.asarray(target)[i]]
+                    mass = mass + hard_coef
+                g = mass[:, None] * P - soft
+            G[i] = tau * (w[i] / M[k])[:, None] * g
+            dH[i] = G[i] @ Wk
+            loss[k] = (w[i] * l[i]).sum() / M[k]
+        dW.append(G[i].T @ h)
+    return dict(loss=loss, tok_loss=l, lse=lse, dHidden=dH, dW=dW, G=G, M=np.array(M), tok_model=tok_model, on=on)

@@ -29,7 +29,8 @@ EXPORTS = ["unity_create", "unity_destroy", "unity_workspace_hint", "unity_works
            "unity_get_profile", "unity_set_option", "unity_advantage_workspace_bytes", "unity_role_advantage", "unity_reward_assembly", "unity_gae", "unity_value_loss_fwd_bwd",
            "unity_ready_batch_plan", "unity_ready_batch_gather", "unity_align_rewards",
            "unity_role_advantage_noalloc",
-           "unity_logprob_fwd", "unity_ppo_loss_fwd_bwd"]
+           "unity_logprob_fwd", "unity_ppo_loss_fwd_bwd",
+           "unity_token_loss_workspace_bytes", "unity_cross_entropy_fwd_bwd", "unity_distill_fwd_bwd"]
 
 
 class UnityError(RuntimeError):
@@ -62,6 +63,16 @@ class unity_ppo_params(C.Structure):
     _fields_ = [("clip_lo", C.c_float), ("clip_hi", C.c_float), ("kl_coef", C.c_float), ("kl_mode", C.c_int),
                 ("ent_coef", C.c_float), ("norm", C.POINTER(C.c_float)), ("accumulate_dW", C.c_int),
                 ("logp_in", C.c_void_p), ("entropy_in", C.c_void_p), ("lse_in", C.c_void_p)]
+
+
+class unity_ce_params(C.Structure):
+    _fields_ = [("label_smoothing", C.c_float), ("z_loss", C.c_float), ("norm", C.POINTER(C.c_float)),
+                ("accumulate_dW", C.c_int), ("dW_type", C.c_int)]
+
+
+class unity_distill_params(C.Structure):
+    _fields_ = [("n_top", C.c_int32), ("teacher_mode", C.c_int), ("kd_coef", C.c_float), ("hard_coef", C.c_float),
+                ("norm", C.POINTER(C.c_float)), ("accumulate_dW", C.c_int), ("dW_type", C.c_int)]
 
 
 _LIB = None
@@ -130,6 +141,14 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.unity_ppo_loss_fwd_bwd.argtypes = [vp, C.POINTER(unity_rows), C.POINTER(unity_ppo_params), vp, vp, vp,
                                            vp, vp, vp, vp, vp, vp, C.POINTER(vp)]
     lib.unity_ppo_loss_fwd_bwd.restype = C.c_int
+    lib.unity_token_loss_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+    lib.unity_token_loss_workspace_bytes.restype = C.c_size_t
+    lib.unity_cross_entropy_fwd_bwd.argtypes = [vp, C.POINTER(unity_rows), C.POINTER(unity_ce_params), vp, vp, vp, vp, vp,
+                                                C.POINTER(vp)]
+    lib.unity_cross_entropy_fwd_bwd.restype = C.c_int
+    lib.unity_distill_fwd_bwd.argtypes = [vp, C.POINTER(unity_rows), C.POINTER(unity_distill_params), vp, vp, vp, vp, vp,
+                                          vp, vp, C.POINTER(vp)]
+    lib.unity_distill_fwd_bwd.restype = C.c_int
     if path == _build.LIB_PATH:
         _LIB = lib
     return lib
@@ -408,6 +427,103 @@ def unity_ppo_loss_fwd_bwd(ctx, hidden, W, cu_seqlens, inv_role, role_model, tar
 
 
 # ------------------------------------------------------------------------------------------------
+# token losses: cross entropy and distillation from a teacher's listed entries
+# ------------------------------------------------------------------------------------------------
+UNITY_F32, UNITY_BF16 = 0, 1
+TEACHER_LOGITS, TEACHER_LOGPROBS = 0, 1
+UNITY_MAX_TOP = 128
+
+
+def unity_token_loss_workspace_bytes(n_tok: int, H: int, V: int, K: int, n_top: int = 0, backward: bool = True) -> int:
+    return int(load_library().unity_token_loss_workspace_bytes(n_tok, H, V, K, n_top, 1 if backward else 0))
+
+
+def _sized(t: Optional[torch.Tensor], shape, dtype, device, name) -> Optional[int]:
+    """data_ptr of an optional tensor that must have exactly this shape, type and device."""
+    if t is None:
+        return None
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, hidden on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _token_loss_args(hidden, W, cu_seqlens, inv_role, role_model, target, tok_mask, inv_temperature, norm, tok_weight,
+                     loss, tok_loss, lse, dHidden, dW, top=None):
+    """What both losses take: (rows, norm array, pointers of the per-token arrays and outputs, dW array, dW type, pointers
+    of the teacher's lists).  `top` = (top_ids, top_vals)."""
+    if hidden.dim() != 2 or not W or W[0].dim() != 2 or inv_role.dim() != 1 or loss is None:
+        raise ValueError("hidden must be [n_tok, H], W a non-empty sequence of [V, H], inv_role [n_inv] and loss a tensor")
+    n_tok, H = hidden.shape
+    K, V, n_inv, dev = len(W), W[0].shape[0], inv_role.shape[0], hidden.device
+    f32, i32, b16 = torch.float32, torch.int32, torch.bfloat16
+    per_tok = (n_tok,)
+    h = _sized(hidden, (n_tok, H), b16, dev, "hidden")
+    Wp = (C.c_void_p * K)(*[_sized(w, (V, H), b16, dev, "W") for w in W])
+    rm = (C.c_int32 * len(role_model))(*[int(x) for x in role_model])
+    rows = unity_rows(n_tok, H, V, K, n_inv, len(role_model), h, Wp,
+                      _sized(cu_seqlens, (n_inv + 1,), torch.int64, dev, "cu_seqlens"),
+                      _sized(inv_role, (n_inv,), i32, dev, "inv_role"), rm, _sized(target, per_tok, i32, dev, "target"),
+                      _sized(tok_mask, per_tok, torch.uint8, dev, "tok_mask"), float(inv_temperature))
+    norm_arr = None
+    if norm is not None:
+        if len(norm) != K:
+            raise ValueError(f"norm: expected {K} values, got {len(norm)}")
+        norm_arr = (C.c_float * K)(*[float(x) for x in norm])
+    per = (_sized(tok_weight, per_tok, f32, dev, "tok_weight"), _sized(loss, (K,), f32, dev, "loss"),
+           _sized(tok_loss, per_tok, f32, dev, "tok_loss"), _sized(lse, per_tok, f32, dev, "lse"),
+           _sized(dHidden, (n_tok, H), b16, dev, "dHidden"))
+    dWp, dw_type = None, UNITY_F32
+    if dW is not None:
+        if len(dW) != K:
+            raise ValueError(f"dW: expected {K} tensors, got {len(dW)}")
+        dtype = dW[0].dtype
+        if dtype not in (f32, b16):
+            raise TypeError(f"dW: expected float32 or bfloat16, got {dtype}")
+        dw_type = UNITY_BF16 if dtype == b16 else UNITY_F32
+        dWp = (C.c_void_p * K)(*[_sized(g, (V, H), dtype, dev, "dW") for g in dW])
+    lists = ()
+    if top is not None:
+        if top[0].dim() != 2:
+            raise ValueError("top_ids must be [n_tok, n_top]")
+        shape = (n_tok, top[0].shape[1])
+        lists = (_sized(top[0], shape, i32, dev, "top_ids"), _sized(top[1], shape, f32, dev, "top_vals"))
+    if not hidden.is_cuda:
+        raise ValueError("hidden must be a CUDA tensor")
+    return rows, norm_arr, per, dWp, dw_type, lists
+
+
+def unity_cross_entropy_fwd_bwd(ctx, hidden, W, cu_seqlens, inv_role, role_model, target, tok_mask, inv_temperature,
+                                label_smoothing: float, z_loss: float, norm: Optional[Sequence[float]],
+                                accumulate_dW: bool, tok_weight, loss, tok_loss=None, lse=None, dHidden=None,
+                                dW=None) -> None:
+    """dHidden / dW None: that gradient is not computed; dW: K tensors [V, H], all f32 or all bf16."""
+    rows, norm_arr, per, dWp, dw_type, _ = _token_loss_args(hidden, W, cu_seqlens, inv_role, role_model, target, tok_mask,
+                                                            inv_temperature, norm, tok_weight, loss, tok_loss, lse,
+                                                            dHidden, dW)
+    p = unity_ce_params(float(label_smoothing), float(z_loss), norm_arr, 1 if accumulate_dW else 0, dw_type)
+    _raise(ctx, load_library().unity_cross_entropy_fwd_bwd(ctx, C.byref(rows), C.byref(p), *per, dWp))
+
+
+def unity_distill_fwd_bwd(ctx, hidden, W, cu_seqlens, inv_role, role_model, target, tok_mask, inv_temperature, top_ids,
+                          top_vals, teacher_mode: int, kd_coef: float, hard_coef: float,
+                          norm: Optional[Sequence[float]], accumulate_dW: bool, tok_weight, loss, tok_loss=None,
+                          lse=None, dHidden=None, dW=None) -> None:
+    """top_ids int32 / top_vals f32: CUDA tensors [n_tok, n_top]; target may be None when hard_coef is 0."""
+    rows, norm_arr, per, dWp, dw_type, lists = _token_loss_args(hidden, W, cu_seqlens, inv_role, role_model, target,
+                                                                tok_mask, inv_temperature, norm, tok_weight, loss,
+                                                                tok_loss, lse, dHidden, dW, (top_ids, top_vals))
+    p = unity_distill_params(top_ids.shape[1], int(teacher_mode), float(kd_coef), float(hard_coef), norm_arr,
+                             1 if accumulate_dW else 0, dw_type)
+    _raise(ctx, load_library().unity_distill_fwd_bwd(ctx, C.byref(rows), C.byref(p), *lists, *per, dWp))
+
+
+# ------------------------------------------------------------------------------------------------
 class Context:
     """Owns a workspace tensor and a unity_ctx bound to a torch stream."""
 
@@ -472,3 +588,9 @@ class Context:
 
     def ppo_loss_fwd_bwd(self, *a, **kw):
         return unity_ppo_loss_fwd_bwd(self.ctx, *a, **kw)
+
+    def cross_entropy_fwd_bwd(self, *a, **kw):
+        return unity_cross_entropy_fwd_bwd(self.ctx, *a, **kw)
+
+    def distill_fwd_bwd(self, *a, **kw):
+        return unity_distill_fwd_bwd(self.ctx, *a, **kw)

@@ -60,6 +60,10 @@ struct Cfg {
     static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kBarBytes;
 };
 
+// The token losses' epilogues run on the schedules of the policy update's.
+__host__ __device__ constexpr bool is_stats(int epi) { return epi == kEpiSoftmaxStats || epi == kEpiLossStats; }
+__host__ __device__ constexpr bool is_grad(int epi) { return epi == kEpiLogitGrad || epi == kEpiLossGrad; }
+
 struct Unit {
     int m_tile, n_begin, n_end, split;
     bool rev;     // walk the unit's column tiles from n_end - 1 down to n_begin
@@ -68,13 +72,13 @@ struct Unit {
 // Column tiles per unit of the striding schedule (below): one, or a run of GemmArgs::unit_tiles (logit gradient only).
 template <int EPI>
 __device__ __forceinline__ int stride_unit_tiles(const GemmArgs& g) {
-    return EPI == kEpiLogitGrad && g.unit_tiles > 1 ? g.unit_tiles : 1;
+    return is_grad(EPI) && g.unit_tiles > 1 ? g.unit_tiles : 1;
 }
 // The logit-gradient epilogue can run on the softmax epilogue's schedule of rounds: the launch says so by carrying a
 // split count.
 template <int EPI>
 __device__ __forceinline__ bool in_rounds(const GemmArgs& g) {
-    return EPI == kEpiSoftmaxStats || (EPI == kEpiLogitGrad && g.n_splits > 0);
+    return is_stats(EPI) || (is_grad(EPI) && g.n_splits > 0);
 }
 
 // Work decomposition over workers (CTAs or CTA pairs); `it` counts the iterations of a worker's persistent loop.
@@ -102,7 +106,7 @@ __device__ __forceinline__ bool next_unit(const GemmArgs& g, int it, int pair, i
         t.n_end = min(t.n_begin + tps, g.n_tiles);
         // logit gradient: odd rounds sweep their split backwards, so a round starts on the W tiles the round before it
         // ended with (the statistics of the softmax epilogue depend on the order of the sweep and keep it)
-        t.rev = EPI == kEpiLogitGrad && (it & 1);
+        t.rev = is_grad(EPI) && (it & 1);
         return true;
     } else {
         // a unit is one output tile, or (logit gradient, GemmArgs::unit_tiles > 1) a run of that many column tiles of one
@@ -403,7 +407,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
             uint64_t run_s2 = 0ull, run_t2 = 0ull;           // (even, odd) partial sums of e and e*v
             int tgt = -1;
             float ca = 0.f, cb = 0.f, lse = 0.f, ent = 0.f;
-            if (EPI == kEpiSoftmaxStats || EPI == kEpiLogitGrad) {
+            if (EPI != kEpiAccumF32) {
                 if (row_ok) tgt = g.target_p[g.a_row0 + row] - g.vocab0;     // column index relative to b_row0
             }
             if (EPI == kEpiLogitGrad && row_ok) {
@@ -425,6 +429,30 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     gA = -fmaf(cb, ent - lse, ca);
                     gB = -cb * g.scale;
                 }
+            }
+
+            // token losses: dL/dz = lp * p - lu, and lt at the target
+            float lshift = 0.f, lp = 0.f, lu = 0.f, lt = 0.f;
+            if (EPI == kEpiLossGrad && row_ok) {
+                lshift = -g.row_lse[g.a_row0 + row] * kLog2e;
+                lp = g.coef_p[g.a_row0 + row];
+                lu = g.coef_g[g.a_row0 + row] * g.uniform;
+                lt = g.target_g[g.a_row0 + row];
+            }
+            // ... the row's listed entries: the next one at or after this unit's first column
+            int top_next = 0x7fffffff, top_pos = 0, top_cnt = 0;
+            long long top_base = 0;
+            if (EPI == kEpiLossStats && g.top_ids != nullptr && row_ok) {
+                top_base = static_cast<long long>(g.a_row0 + row) * g.top_n;
+                top_cnt = g.top_cnt[g.a_row0 + row];
+                const int first = t.n_begin * kTileN;
+                int lo = 0, hi = top_cnt;
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (g.top_ids[top_base + mid] < first) lo = mid + 1; else hi = mid;
+                }
+                top_pos = lo;
+                if (top_pos < top_cnt) top_next = g.top_ids[top_base + top_pos];
             }
 
             for (int ni = t.n_begin; ni < t.n_end && ok; ++ni) {
@@ -499,6 +527,83 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                                     if (q * 8 < n_here)
                                         *reinterpret_cast<uint4*>(dst + q * 8) =
                                             make_uint4(zp[4 * q], zp[4 * q + 1], zp[4 * q + 2], zp[4 * q + 3]);
+                                }
+                            }
+                        }
+                    } else if (EPI == kEpiLossStats) {
+                        // the same online sums without the entropy's; sum z (label smoothing) in its place.  V is a multiple
+                        // of 8, so the last columns end on a pair.
+                        if (n_here < 32) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (j >= n_here) v[j] = kNegBig;
+                        }
+                        float cm = ptx::max3(v[0], v[1], v[2]);
+#pragma unroll
+                        for (int j = 3; j < 31; j += 2) cm = ptx::max3(cm, v[j], v[j + 1]);
+                        cm = fmaxf(cm, v[31]);
+                        const float new_m = fmaxf(run_m, cm);
+                        const float resc = ptx::ex2((run_m - new_m) * c2);
+                        run_s2 = ptx::mul2(run_s2, ptx::pack2(resc, resc));
+                        run_m = new_m;
+                        const float shift = -new_m * c2;
+                        const uint64_t shift2 = ptx::pack2(shift, shift), c22 = ptx::pack2(c2, c2);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            if (j < n_here) {
+                                const uint64_t x = ptx::pack2(v[j], v[j + 1]);
+                                float a0, a1;
+                                ptx::unpack2(ptx::fma2(x, c22, shift2), a0, a1);
+                                run_s2 = ptx::add2(run_s2, ptx::pack2(ptx::ex2(a0), ptx::ex2(a1)));
+                                run_t2 = ptx::add2(run_t2, x);
+                            }
+                        }
+                        const int jt = tgt - cbase;
+                        if (jt >= 0 && jt < 32) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (j == jt) z_tgt = v[j];
+                        }
+                        while (top_next < cbase + 32) {           // listed entries among these columns
+                            const int jn = top_next - cbase;
+                            float z = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) if (j == jn) z = v[j];
+                            g.top_z[top_base + top_pos] = z;
+                            ++top_pos;
+                            top_next = top_pos < top_cnt ? g.top_ids[top_base + top_pos] : 0x7fffffff;
+                        }
+                    } else if (EPI == kEpiLossGrad) {
+                        unsigned packed[16];
+                        const uint64_t c22 = ptx::pack2(c2, c2), sh2 = ptx::pack2(lshift, lshift);
+                        const uint64_t lp2 = ptx::pack2(lp, lp), lu2 = ptx::pack2(-lu, -lu);
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            float a0, a1, o0, o1;
+                            ptx::unpack2(ptx::fma2(ptx::pack2(v[j], v[j + 1]), c22, sh2), a0, a1);
+                            ptx::unpack2(ptx::fma2(ptx::pack2(ptx::ex2(a0), ptx::ex2(a1)), lp2, lu2), o0, o1);
+                            packed[j >> 1] = pack_bf16(o0, o1);
+                        }
+                        const int jt = tgt - cbase;
+                        if (jt >= 0 && jt < 32) {
+                            const unsigned bits = static_cast<unsigned>(__bfloat16_as_ushort(__float2bfloat16_rn(lt)));
+                            const unsigned keep = (jt & 1) ? 0x0000ffffu : 0xffff0000u;
+                            const unsigned put = (jt & 1) ? (bits << 16) : bits;
+                            const int jp = jt >> 1;
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) packed[j] = (j == jp) ? ((packed[j] & keep) | put) : packed[j];
+                        }
+                        if (row_ok) {
+                            __nv_bfloat16* dst = g.G + static_cast<long long>(row) * g.ldg + cbase;
+                            if (n_here == 32 && g.g_wide_store) {
+                                ptx::st_global_v8_hint(dst, packed[0], packed[1], packed[2], packed[3], packed[4], packed[5],
+                                                       packed[6], packed[7], pol_st);
+                                ptx::st_global_v8_hint(dst + 16, packed[8], packed[9], packed[10], packed[11], packed[12],
+                                                       packed[13], packed[14], packed[15], pol_st);
+                            } else {
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    if (q * 8 < n_here)
+                                        *reinterpret_cast<uint4*>(dst + q * 8) =
+                                            make_uint4(packed[4 * q], packed[4 * q + 1], packed[4 * q + 2], packed[4 * q + 3]);
                                 }
                             }
                         }
@@ -593,7 +698,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 }
                 if (++acc == kAccStages) { acc = 0; acc_phase ^= 1; }
             }
-            if (EPI == kEpiSoftmaxStats && ok && row_ok) {
+            if (is_stats(EPI) && ok && row_ok) {
                 float s0, s1, t0, t1;
                 ptx::unpack2(run_s2, s0, s1);
                 ptx::unpack2(run_t2, t0, t1);
@@ -656,6 +761,10 @@ cudaError_t gemm_set_attributes() {
     if ((e = set_attr<kEpiSoftmaxStats, false, false, 2>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiLogitGrad, false, false, 1>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiLogitGrad, false, false, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr<kEpiLossStats, false, false, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr<kEpiLossStats, false, false, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr<kEpiLossGrad, false, false, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr<kEpiLossGrad, false, false, 2>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiAccumF32, false, true, 1>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiAccumF32, false, true, 2>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiAccumF32, true, true, 1>()) != cudaSuccess) return e;
@@ -678,7 +787,7 @@ cudaError_t launch_gemm(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap
     const int max_workers = sm_count / ctas;                                   // one CTA per SM
     int workers = workers_known > 0 && workers_known < max_workers ? workers_known : max_workers;
     if (args.span.plan == nullptr) {
-        const long long units = epi == kEpiSoftmaxStats
+        const long long units = is_stats(epi)
                                     ? static_cast<long long>(args.group_m < args.m_tiles ? args.group_m : args.m_tiles) * args.n_splits
                                     : static_cast<long long>(args.m_tiles) * args.n_tiles;
         if (units <= 0 || args.m_tiles <= 0 || args.k_iters <= 0) return cudaSuccess;
@@ -693,6 +802,12 @@ cudaError_t launch_gemm(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap
         case kEpiLogitGrad:
             return two ? launch<kEpiLogitGrad, false, false, 2>(tmA, tmB, args, workers, stream)
                        : launch<kEpiLogitGrad, false, false, 1>(tmA, tmB, args, workers, stream);
+        case kEpiLossStats:
+            return two ? launch<kEpiLossStats, false, false, 2>(tmA, tmB, args, workers, stream)
+                       : launch<kEpiLossStats, false, false, 1>(tmA, tmB, args, workers, stream);
+        case kEpiLossGrad:
+            return two ? launch<kEpiLossGrad, false, false, 2>(tmA, tmB, args, workers, stream)
+                       : launch<kEpiLossGrad, false, false, 1>(tmA, tmB, args, workers, stream);
         default:   // fp32 accumulate: B is always MN-major (W or hidden read in place), A is G either way round
             if (wide && two)
                 return a_mn ? launch<kEpiAccumF32, true, true, 2, 2>(tmA, tmB, args, workers, stream)

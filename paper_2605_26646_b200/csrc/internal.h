@@ -61,6 +61,7 @@ struct FwdPlanParams {
     int gmax;        // largest round, in row tiles
     int tile_rows;   // rows of a row tile (128 or 256)
     int n_tiles;     // vocabulary tiles of 256
+    int max_splits;  // most vocabulary splits of a round (32 for stages 2 and 3; the token losses let few rows use all workers)
 };
 __host__ __device__ inline FwdShape forward_shape(const FwdPlanParams& p, int rows) {
     const int m_tiles = rows / p.tile_rows;
@@ -75,7 +76,7 @@ __host__ __device__ inline FwdShape forward_shape(const FwdPlanParams& p, int ro
     for (int cand = p.gmax; cand >= cand_min; --cand) {
         const int c = cand < m_tiles ? cand : (m_tiles > 0 ? m_tiles : 1);
         int sp = p.n_pairs / c;
-        sp = sp > 32 ? 32 : sp;
+        sp = sp > p.max_splits ? p.max_splits : sp;
         sp = sp > p.n_tiles ? p.n_tiles : sp;
         sp = sp < 1 ? 1 : sp;
         // several rounds: at most 4 splits, which bounds the statistics a launch writes by 4 per row (plus the short last
@@ -85,7 +86,7 @@ __host__ __device__ inline FwdShape forward_shape(const FwdPlanParams& p, int ro
         int sp_last = sp;
         if (rest > 0) {
             sp_last = p.n_pairs / rest;
-            sp_last = sp_last > 32 ? 32 : sp_last;
+            sp_last = sp_last > p.max_splits ? p.max_splits : sp_last;
             sp_last = sp_last > p.n_tiles ? p.n_tiles : sp_last;
             sp_last = sp_last < 1 ? 1 : sp_last;
         }
@@ -113,7 +114,9 @@ enum : int { kSpanNone = 0, kSpanForward = 1, kSpanRowsA = 2, kSpanRowsM = 3, kS
 enum GemmEpilogue : int {
     kEpiSoftmaxStats = 0,   // online (max, sum exp, sum exp*z, target logit) per row; nothing of size M x N stored
     kEpiLogitGrad = 1,      // dL/dz in bf16 for a bounded (rows x vocab) chunk
-    kEpiAccumF32 = 2        // C (+)= acc, fp32, row-major
+    kEpiAccumF32 = 2,       // C (+)= acc, fp32, row-major
+    kEpiLossStats = 3,      // token losses: online (max, sum exp, sum z, target logit) per row, the logits of listed entries
+    kEpiLossGrad = 4        // token losses: dL/dz in bf16 for a bounded (rows x vocab) chunk
 };
 
 struct GemmArgs {
@@ -155,6 +158,17 @@ struct GemmArgs {
     __nv_bfloat16* G;         // [m_rows, ldg] chunk-local
     long long ldg;
     int g_wide_store;         // G and ldg allow 32-byte aligned row segments: 256-bit stores
+    // kEpiLossStats: the listed entries of a row (ascending, distinct vocabulary indexes, top_cnt of them) and the place of
+    // their logits (accumulator units); null = none
+    const int* top_ids;       // [rows, top_n], indexed from a_row0 + row
+    const int* top_cnt;       // [rows]
+    float* top_z;             // out [rows, top_n]
+    int top_n;
+    // kEpiLossGrad: G = coef_p * p - coef_g * uniform, and target_g at the target (row_lse as above)
+    const float* coef_p;      // [rows] dL/dz_v per unit of p_v, times scale
+    const float* coef_g;      // [rows] scale * weight / M
+    const float* target_g;    // [rows] the whole gradient at the target
+    float uniform;            // label smoothing's share of every entry: eps / V
     // kEpiAccumF32
     float* C;
     long long ldc;
@@ -334,6 +348,63 @@ struct ValueArgs {
 constexpr int kValueSlices = 32;      // slices of the invocations in the last pass of the value loss
 size_t value_counters_bytes();
 cudaError_t launch_value_loss(const ValueArgs& a, cudaStream_t stream, int* n_launches);
+
+// ----------------------------------------------------------------------------------------------
+// token losses (token_loss.cu)
+// ----------------------------------------------------------------------------------------------
+struct TeacherArgs {
+    const DevPlan* plan;
+    const int* slot_tok;
+    int K, V, n_top;
+    int logits;                // 1: softmax of the listed logits (times scale); 0: exp of listed log-probabilities
+    float scale;
+    const int* top_ids;        // caller order [n_tok, n_top]
+    const float* top_vals;
+    int *ids_p, *cnt_p;        // packed [slots, n_top], [slots]
+    float* q_p;                // packed [slots, n_top]
+    int* status;
+};
+cudaError_t launch_teacher_lists(const TeacherArgs& a, long long max_slots, cudaStream_t stream);
+
+struct LossRowArgs {
+    RowSpan block;             // as in TokenArgs: one block of one model's rows, or (block.model < 0) every packed row
+    const DevPlan* plan;
+    FwdPlanParams fwd;
+    long long max_slots;
+    int K, V;
+    const float4* stats;       // (max, sum exp, sum z, target logit) per split, accumulator units
+    const int* slot_tok;
+    const int8_t* tok_model;
+    float scale;
+    const float* tok_weight;   // caller order, nullable
+    int has_norm;
+    float norm[UNITY_MAX_MODELS];
+    float smoothing, z_loss;   // cross entropy (n_top == 0)
+    int n_top;                 // distillation
+    float kd, hard;
+    const int *ids_p, *cnt_p, *target_p;
+    const float* q_p;
+    float* top_z;              // packed [slots, n_top]: logits in, gradients out (with_grad)
+    int with_grad;
+    float *row_lse, *coef_p, *coef_g, *target_g;   // packed [slots]
+    float *tok_loss, *lse;     // caller order, nullable
+    float* partial;            // [slots / 8]
+    float* loss;               // [K]
+};
+cudaError_t launch_loss_rows(const LossRowArgs& a, cudaStream_t stream);
+cudaError_t launch_loss_sum(const LossRowArgs& a, cudaStream_t stream);
+
+struct TeacherScatterArgs {
+    RowSpan span;
+    const int *ids_p, *cnt_p;
+    const float* top_g;
+    int n_top, v0, cols;
+    __nv_bfloat16* G;          // first row of the span, first column v0
+    long long ld;
+};
+cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream);
+// dst[0, n) = bf16(src) (+ dst when add); n a multiple of 8
+cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream);
 
 // ----------------------------------------------------------------------------------------------
 // ready-batch construction (batch_kernels.cu)

@@ -288,7 +288,7 @@ __global__ void k_route_count(RouteArgs a) {
         if (on) {
             const int s = find_invocation(a.cu_seqlens, a.n_inv, i);
             const int role = a.inv_role[s];
-            const int tgt = a.target[i];
+            const int tgt = a.target ? a.target[i] : 0;
             if (role >= 0 && role < a.n_roles && tgt >= 0 && tgt < a.V) {
                 model = a.role_model[role];
                 if (model < 0 || model >= a.K) model = -1;
@@ -377,7 +377,7 @@ __global__ void k_gather_rows(const __nv_bfloat16* __restrict__ hidden, const in
     } else {
         for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
     }
-    if (lane == 0) target_p[slot] = tok >= 0 ? target[tok] : 0;
+    if (lane == 0) target_p[slot] = tok >= 0 ? (target ? target[tok] : -1) : 0;
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -235,7 +235,7 @@ int make_tmap(unity_ctx* ctx, CUtensorMap* tm, const void* ptr, uint64_t inner, 
     return UNITY_OK;
 }
 
-int validate_rows(unity_ctx* ctx, const unity_rows* r) {
+int validate_rows(unity_ctx* ctx, const unity_rows* r, bool need_target = true) {
     if (!ctx) return UNITY_ERR_INVALID_ARG;
     if (!r) return fail(ctx, UNITY_ERR_INVALID_ARG, "rows is NULL");
     if (r->n_tok < 0 || r->n_inv < 0) return fail(ctx, UNITY_ERR_INVALID_ARG, "negative size");
@@ -247,7 +247,7 @@ int validate_rows(unity_ctx* ctx, const unity_rows* r) {
     if (r->V < 8 || r->V % 8 != 0) return fail(ctx, UNITY_ERR_SHAPE, "V=%d must be a positive multiple of 8", r->V);
     if (!(r->inv_temperature > 0.f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "inv_temperature must be > 0");
     if (!r->W || !r->role_model) return fail(ctx, UNITY_ERR_INVALID_ARG, "W / role_model is NULL");
-    if (r->n_tok > 0 && (!r->hidden || !r->cu_seqlens || !r->inv_role || !r->target || r->n_inv < 1))
+    if (r->n_tok > 0 && (!r->hidden || !r->cu_seqlens || !r->inv_role || (need_target && !r->target) || r->n_inv < 1))
         return fail(ctx, UNITY_ERR_INVALID_ARG, "hidden / cu_seqlens / inv_role / target is NULL or n_inv < 1");
     if (reinterpret_cast<uintptr_t>(r->hidden) & 15) return fail(ctx, UNITY_ERR_ALIGNMENT, "hidden not 16-byte aligned");
     for (int k = 0; k < r->K; ++k) {
@@ -286,6 +286,7 @@ FwdPlanParams fwd_params(const unity_ctx* ctx, int V, int H) {
     p.n_pairs = ctx->sm_count / ctas;
     p.tile_rows = gemm_tile_rows(ctas);
     p.n_tiles = (V + kTileN - 1) / kTileN;
+    p.max_splits = 32;
     const int group = ctx->fwd_group >= 0 ? ctx->fwd_group : (large_rounds_fit(ctx, H) ? ctx->sm_count / 2 : 48);
     int gmax = group > 0 ? group / ctas : p.n_pairs / 4;
     if (gmax < 1) gmax = 1;
@@ -399,6 +400,278 @@ void fill_token_args(TokenArgs& t, const unity_rows* r, const RowPlan& P) {
     t.row_lse = L.row_lse; t.row_ent = L.row_ent; t.row_logp = L.row_logp;
     t.cu_seqlens = r->cu_seqlens; t.inv_role = r->inv_role;
     for (int v = 0; v < r->n_roles; ++v) t.role_model[v] = r->role_model[v];
+}
+
+
+// ------------------------------------------------------------------------------------------------
+// Token losses: cross entropy and distillation on the rows of stages 2 and 3
+// ------------------------------------------------------------------------------------------------
+// The caller's current device comes back when a call returns.
+struct DeviceGuard {
+    int prev;
+    bool ok;
+    explicit DeviceGuard(int device) : prev(-1), ok(false) {
+        if (cudaGetDevice(&prev) != cudaSuccess) { cudaGetLastError(); prev = -1; }
+        ok = prev == device || cudaSetDevice(device) == cudaSuccess;
+        if (prev == device) prev = -1;
+    }
+    ~DeviceGuard() { if (prev >= 0) cudaSetDevice(prev); }
+};
+
+// What the two losses differ in, and what both take beside the rows.
+struct LossCall {
+    float smoothing, z_loss;                        // cross entropy
+    int n_top, logits;                              // distillation (n_top > 0)
+    float kd, hard;
+    const int32_t* top_ids;
+    const float* top_vals;
+    const float *norm, *tok_weight;
+    int accumulate, bf16_dw;
+    float *loss, *tok_loss, *lse;
+    void* dHidden;
+    void* const* dW;
+};
+
+struct LossLayout {
+    int* tok_slot; int* slot_tok; int8_t* tok_model; int* blk_cnt; DevPlan* plan; unsigned* sync_counters;
+    __nv_bfloat16* hp; int* target_p; float4* stats; float* partial;
+    int *ids_p, *cnt_p; float *q_p, *top_z;
+    float *row_lse, *coef_p, *coef_g, *target_g;
+    __nv_bfloat16* G; float *dHc, *dWc;
+    long long max_slots;
+    int n_blocks, chunk_rows, chunk_vocab;
+    size_t bytes;
+};
+
+// chunk_rows = 0: no gradient.  dw_scratch: fp32 copy of one dW, for sums over several row blocks rounded to bf16 once.
+LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int K, int n_top, int chunk_rows,
+                      int chunk_vocab, bool dw_scratch, bool* fits) {
+    LossLayout L;
+    memset(&L, 0, sizeof(L));
+    Bump b{base, 0, cap, true};
+    L.max_slots = max_slots_of(n_tok, K);
+    L.n_blocks = static_cast<int>((n_tok + kRouteBlock - 1) / kRouteBlock);
+    L.chunk_rows = chunk_rows; L.chunk_vocab = chunk_vocab;
+    const size_t ms = static_cast<size_t>(L.max_slots);
+    L.tok_slot = b.take<int>(n_tok);
+    L.slot_tok = b.take<int>(ms);
+    L.tok_model = b.take<int8_t>(n_tok);
+    L.blk_cnt = b.take<int>(static_cast<size_t>(L.n_blocks) * K + 1);
+    L.plan = b.take<DevPlan>(1);
+    L.sync_counters = b.take<unsigned>(kSyncCounters);
+    L.hp = b.take<__nv_bfloat16>(ms * H);
+    L.target_p = b.take<int>(ms);
+    L.stats = b.take<float4>(4 * ms + 94720ull * K);
+    L.partial = b.take<float>(ms / 8);
+    if (n_top > 0) {
+        L.ids_p = b.take<int>(ms * n_top);
+        L.cnt_p = b.take<int>(ms);
+        L.q_p = b.take<float>(ms * n_top);
+        L.top_z = b.take<float>(ms * n_top);
+    }
+    if (chunk_rows > 0) {
+        L.row_lse = b.take<float>(ms);
+        L.coef_p = b.take<float>(ms);
+        L.coef_g = b.take<float>(ms);
+        L.target_g = b.take<float>(ms);
+        L.G = b.take<__nv_bfloat16>(static_cast<size_t>(chunk_rows) * chunk_vocab);
+        L.dHc = b.take<float>(static_cast<size_t>(chunk_rows) * H);
+        if (dw_scratch) L.dWc = b.take<float>(static_cast<size_t>(V) * H);
+    }
+    L.bytes = up(b.off, kAlign);
+    if (fits) *fits = b.ok;
+    return L;
+}
+
+int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
+    const int K = r->K, H = r->H, V = r->V;
+    const bool want_h = c.dHidden != nullptr, want_w = c.dW != nullptr, want = want_h || want_w;
+    if (!c.loss) return fail(ctx, UNITY_ERR_INVALID_ARG, "loss is NULL");
+    for (int k = 0; k < K; ++k) {
+        if (want_w && !c.dW[k]) return fail(ctx, UNITY_ERR_INVALID_ARG, "dW[%d] is NULL", k);
+        if (want_w && (reinterpret_cast<uintptr_t>(c.dW[k]) & 15)) return fail(ctx, UNITY_ERR_ALIGNMENT, "dW[%d] not 16-byte aligned", k);
+        if (c.norm && !(c.norm[k] > 0.f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "norm[%d] must be > 0", k);
+    }
+    if (reinterpret_cast<uintptr_t>(c.dHidden) & 15) return fail(ctx, UNITY_ERR_ALIGNMENT, "dHidden not 16-byte aligned");
+    const DeviceGuard dev(ctx->device);
+    if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+    cudaStream_t st = ctx->stream;
+    const size_t dw_bytes = static_cast<size_t>(V) * H * (c.bf16_dw ? 2 : 4);
+    if (r->n_tok == 0) {
+        CUDA_TRY(ctx, cudaMemsetAsync(c.loss, 0, sizeof(float) * K, st));
+        for (int k = 0; want_w && !c.accumulate && k < K; ++k) CUDA_TRY(ctx, cudaMemsetAsync(c.dW[k], 0, dw_bytes, st));
+        return UNITY_OK;
+    }
+
+    int cr = want ? wanted_chunk_rows(r->n_tok, K, ctx->chunk_rows_mult) : 0;
+    int cv = want ? wanted_chunk_vocab(V, ctx->chunk_vocab_mult) : 0;
+    LossLayout L;
+    for (;;) {
+        bool fits = false;
+        L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, cr, cv, want_w && c.bf16_dw, &fits);
+        if (fits) break;
+        if (cr > kMinChunkRows && cr >= cv) cr = static_cast<int>(up(cr / 2, kTileM));
+        else if (cv > kMinChunkVocab) cv = static_cast<int>(up(cv / 2, kTileN));
+        else if (cr > kMinChunkRows) cr = static_cast<int>(up(cr / 2, kTileM));
+        else return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: need at least %zu bytes, have %zu", L.bytes, ctx->ws_bytes);
+    }
+    if (c.tok_loss) CUDA_TRY(ctx, cudaMemsetAsync(c.tok_loss, 0, sizeof(float) * r->n_tok, st));
+    if (c.lse) CUDA_TRY(ctx, cudaMemsetAsync(c.lse, 0, sizeof(float) * r->n_tok, st));
+
+    int nl = 0, rc;
+    FwdPlanParams fwd = fwd_params(ctx, V, H);
+    fwd.max_splits = fwd.n_pairs;
+    SyncCounters counters{L.sync_counters, 0, kSyncCounters};
+    const long long rows_bound = static_cast<long long>(up(r->n_tok, kTileM));
+    CUDA_TRY(ctx, cudaMemsetAsync(L.slot_tok, 0xff, sizeof(int) * L.max_slots, st));
+    CUDA_TRY(ctx, cudaMemsetAsync(L.sync_counters, 0, sizeof(unsigned) * kSyncCounters, st));
+    RouteArgs ra;
+    memset(&ra, 0, sizeof(ra));
+    ra.n_tok = r->n_tok; ra.n_inv = r->n_inv; ra.n_roles = r->n_roles; ra.K = K; ra.V = V;
+    ra.cu_seqlens = r->cu_seqlens; ra.inv_role = r->inv_role; ra.target = r->target; ra.tok_mask = r->tok_mask;
+    for (int v = 0; v < r->n_roles; ++v) ra.role_model[v] = r->role_model[v];
+    ra.n_blocks = L.n_blocks; ra.blk_cnt = L.blk_cnt; ra.plan = L.plan; ra.fwd = fwd;
+    ra.tok_slot = L.tok_slot; ra.slot_tok = L.slot_tok; ra.tok_model = L.tok_model; ra.status = ctx->d_status;
+    CUDA_TRY(ctx, launch_route(ra, st, &nl));
+    CUDA_TRY(ctx, launch_gather_rows(static_cast<const __nv_bfloat16*>(r->hidden), r->target, L.slot_tok, L.plan, K,
+                                     L.max_slots, H, L.hp, L.target_p, st));
+    nl += 1;
+    if (c.n_top > 0) {
+        const TeacherArgs ta{L.plan, L.slot_tok, K, V, c.n_top, c.logits, r->inv_temperature, c.top_ids, c.top_vals,
+                             L.ids_p, L.cnt_p, L.q_p, ctx->d_status};
+        CUDA_TRY(ctx, launch_teacher_lists(ta, L.max_slots, st));
+        nl += 1;
+    }
+
+    // forward: statistics of every row of every model
+    CUtensorMap tm_hp_k, tm_hp_mn;
+    if ((rc = make_tmap(ctx, &tm_hp_k, L.hp, H, L.max_slots, static_cast<uint64_t>(H) * 2, kBoxRows))) return rc;
+    if ((rc = make_tmap(ctx, &tm_hp_mn, L.hp, H, L.max_slots, static_cast<uint64_t>(H) * 2, kTileK))) return rc;
+    for (int k = 0; k < K; ++k) {
+        const int ctas = ctx->ctas[UNITY_PROF_FWD_GEMM];
+        CUtensorMap tmB;
+        if ((rc = make_tmap(ctx, &tmB, r->W[k], H, V, static_cast<uint64_t>(H) * 2, kTileN / ctas))) return rc;
+        GemmArgs g;
+        memset(&g, 0, sizeof(g));
+        g.span = RowSpan{L.plan, k, 0, 0x7fffff00}; g.span_mode = kSpanForward; g.stats_from_plan = 1; g.fwd = fwd;
+        g.m_tiles = 1;                                   // set by the kernel
+        g.n_tiles = (V + kTileN - 1) / kTileN; g.k_iters = H / kTileK; g.n_cols = V;
+        g.stats = L.stats; g.target_p = L.target_p; g.scale = r->inv_temperature;
+        g.top_ids = L.ids_p; g.top_cnt = L.cnt_p; g.top_z = L.top_z; g.top_n = c.n_top;
+        gemm_common(ctx, g, UNITY_PROF_FWD_GEMM, &counters, ctx->fwd_sync != 0);
+        ProfScope ps(ctx, UNITY_PROF_FWD_GEMM);
+        CUDA_TRY(ctx, launch_gemm(kEpiLossStats, false, ctas, tm_hp_k, tmB, g, ctx->sm_count, st));
+        nl += 1;
+    }
+    LossRowArgs la;
+    memset(&la, 0, sizeof(la));
+    la.block = RowSpan{L.plan, -1, 0, 0}; la.plan = L.plan; la.fwd = fwd; la.max_slots = L.max_slots; la.K = K; la.V = V;
+    la.stats = L.stats; la.slot_tok = L.slot_tok; la.tok_model = L.tok_model; la.scale = r->inv_temperature;
+    la.tok_weight = c.tok_weight; la.has_norm = c.norm != nullptr;
+    for (int k = 0; k < K && c.norm; ++k) la.norm[k] = c.norm[k];
+    la.smoothing = c.smoothing; la.z_loss = c.z_loss; la.n_top = c.n_top; la.kd = c.kd; la.hard = c.hard;
+    la.ids_p = L.ids_p; la.cnt_p = L.cnt_p; la.q_p = L.q_p; la.top_z = L.top_z; la.target_p = L.target_p;
+    la.with_grad = want; la.row_lse = L.row_lse; la.coef_p = L.coef_p; la.coef_g = L.coef_g; la.target_g = L.target_g;
+    la.tok_loss = c.tok_loss; la.lse = c.lse; la.partial = L.partial; la.loss = c.loss;
+    CUDA_TRY(ctx, launch_loss_rows(la, st));
+    CUDA_TRY(ctx, launch_loss_sum(la, st));
+    nl += 2;
+    if (!want) { ctx->launches += nl; return UNITY_OK; }
+
+    // backward: per model, block of rows and piece of the vocabulary: G = dL/dz in bf16, dHidden += G W, dW += G^T hidden
+    __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
+    if (want_h) { CUDA_TRY(ctx, launch_zero_masked_rows(L.tok_slot, r->n_tok, H, dH, st)); nl += 1; }
+    const int c_grad = ctx->ctas[UNITY_PROF_GRAD_GEMM], c_dh = ctx->ctas[UNITY_PROF_DH_GEMM], c_dw = ctx->ctas[UNITY_PROF_DW_GEMM];
+    const int mma_n = gemm_mma_n(H);
+    for (int k = 0; k < K; ++k) {
+        const __nv_bfloat16* Wk = static_cast<const __nv_bfloat16*>(r->W[k]);
+        float* dWk = want_w ? (c.bf16_dw ? L.dWc : static_cast<float*>(c.dW[k])) : nullptr;
+        const bool add_dw = c.accumulate && !c.bf16_dw;
+        if (want_w && !add_dw) {   // a model without rows: its dW reads zero
+            CUDA_TRY(ctx, launch_zero_if_empty(dWk, static_cast<long long>(V) * H, L.plan, k, st));
+            nl += 1;
+        }
+        CUtensorMap tm_W_k, tm_W_mn;
+        if ((rc = make_tmap(ctx, &tm_W_k, Wk, H, V, static_cast<uint64_t>(H) * 2, kTileN / c_grad))) return rc;
+        if ((rc = make_tmap(ctx, &tm_W_mn, Wk, H, V, static_cast<uint64_t>(H) * 2, kTileK))) return rc;
+        for (long long c0 = 0; c0 < rows_bound; c0 += cr) {
+            const int nc = static_cast<int>(rows_bound - c0 < cr ? rows_bound - c0 : cr);
+            const RowSpan chunk{L.plan, k, static_cast<int>(c0), nc};
+            int base, n_pieces;
+            vocab_chunks(V, cv, &base, &n_pieces);
+            for (int ci = 0; ci < n_pieces; ++ci) {
+                const int v0 = ci * base, vc = ci + 1 == n_pieces ? V - v0 : base;
+                GemmArgs g;
+                memset(&g, 0, sizeof(g));
+                g.span = chunk; g.span_mode = kSpanRowsA;
+                g.m_tiles = 1;                                   // set by the kernel
+                g.n_tiles = (vc + kTileN - 1) / kTileN; g.k_iters = H / kTileK; g.group_m = 1;
+                g.fwd.n_pairs = ctx->sm_count / c_grad; g.fwd.tile_rows = gemm_tile_rows(c_grad); g.fwd.n_tiles = g.n_tiles;
+                g.fwd.max_splits = g.fwd.n_pairs;
+                if (large_rounds_fit(ctx, H)) {
+                    g.fwd.gmax = ctx->sm_count / 2 / c_grad;
+                } else {   // runs of column tiles, as many row tiles in flight as a 45 MB share of L2 holds
+                    int runs = static_cast<int>((45ll << 20) / (128ll * H * 2));
+                    runs = runs < 8 ? 8 : (runs > ctx->sm_count / 2 ? ctx->sm_count / 2 : runs);
+                    g.plan_runs = 1;
+                    g.fwd.gmax = runs / c_grad > 0 ? runs / c_grad : 1;
+                }
+                g.b_row0 = v0; g.n_cols = vc; g.target_p = L.target_p; g.vocab0 = v0; g.scale = r->inv_temperature;
+                g.row_lse = L.row_lse; g.coef_p = L.coef_p; g.coef_g = L.coef_g; g.target_g = L.target_g;
+                g.uniform = c.smoothing / static_cast<float>(V);
+                g.G = L.G; g.ldg = cv; g.g_wide_store = (reinterpret_cast<uintptr_t>(L.G) % 32 == 0) && cv % 16 == 0;
+                gemm_common(ctx, g, UNITY_PROF_GRAD_GEMM, &counters, (ctx->chunk_sync & 1) != 0);
+                {
+                    ProfScope ps(ctx, UNITY_PROF_GRAD_GEMM);
+                    CUDA_TRY(ctx, launch_gemm(kEpiLossGrad, false, c_grad, tm_hp_k, tm_W_k, g, ctx->sm_count, st));
+                    nl += 1;
+                }
+                if (c.n_top > 0) {
+                    const TeacherScatterArgs ts{chunk, L.ids_p, L.cnt_p, L.top_z, c.n_top, v0, vc, L.G, cv};
+                    CUDA_TRY(ctx, launch_teacher_scatter(ts, st));
+                    nl += 1;
+                }
+                CUtensorMap tm_G_k, tm_G_mn;
+                if ((rc = make_tmap(ctx, &tm_G_k, L.G, vc, nc, static_cast<uint64_t>(cv) * 2, kBoxRows))) return rc;
+                if ((rc = make_tmap(ctx, &tm_G_mn, L.G, vc, nc, static_cast<uint64_t>(cv) * 2, kTileK))) return rc;
+                if (want_h) {
+                    GemmArgs h;
+                    memset(&h, 0, sizeof(h));
+                    h.mma_n = mma_n;
+                    h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1;
+                    h.n_tiles = (H + mma_n - 1) / mma_n; h.k_iters = (vc + kTileK - 1) / kTileK;
+                    h.group_m = ctx->chunk_group[1] / c_dh > 0 ? ctx->chunk_group[1] / c_dh : 1;
+                    h.b_k0 = v0; h.n_cols = H; h.C = L.dHc; h.ldc = H; h.beta = v0 > 0;
+                    gemm_common(ctx, h, UNITY_PROF_DH_GEMM, &counters, (ctx->chunk_sync & 2) != 0);
+                    ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
+                    CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, false, c_dh, tm_G_k, tm_W_mn, h, ctx->sm_count, st));
+                    nl += 1;
+                }
+                if (want_w) {
+                    GemmArgs w;
+                    memset(&w, 0, sizeof(w));
+                    const int tile_v = gemm_tile_rows(c_dw);
+                    w.mma_n = mma_n;
+                    w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = (vc + tile_v - 1) / tile_v;
+                    w.n_tiles = (H + mma_n - 1) / mma_n; w.k_iters = 1;
+                    w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
+                    w.m_rows = vc; w.n_cols = H; w.C = dWk + static_cast<long long>(v0) * H; w.ldc = H;
+                    w.beta = (add_dw || c0 > 0) ? 1 : 0;
+                    gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0);
+                    ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
+                    CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st));
+                    nl += 1;
+                }
+            }
+            if (want_h) { CUDA_TRY(ctx, launch_store_dhidden(L.dHc, L.slot_tok, chunk, H, dH, st)); nl += 1; }
+        }
+        if (want_w && c.bf16_dw) {
+            CUDA_TRY(ctx, launch_cast_dw(dWk, static_cast<__nv_bfloat16*>(c.dW[k]), static_cast<long long>(V) * H, c.accumulate != 0, st));
+            nl += 1;
+        }
+    }
+    ctx->launches += nl;
+    return UNITY_OK;
 }
 
 }  // namespace
@@ -1047,6 +1320,7 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
                                 g.fwd.n_pairs = ctx->sm_count / c_grad;
                                 g.fwd.tile_rows = gemm_tile_rows(c_grad);
                                 g.fwd.n_tiles = g.n_tiles;
+                                g.fwd.max_splits = 32;
                                 g.fwd.gmax = rounds / c_grad > 0 ? rounds / c_grad : 1;
                                 if (g.fwd.gmax > g.fwd.n_pairs) g.fwd.gmax = g.fwd.n_pairs;
                             }
@@ -1133,6 +1407,58 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
     if (stash) CUDA_TRY(ctx, launch_loss_reduce(t, st, &nl));
     ctx->launches += nl;
     return UNITY_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+size_t unity_token_loss_workspace_bytes(int64_t n_tok, int32_t H, int32_t V, int32_t K, int32_t n_top, int32_t backward) {
+    if (n_tok < 0 || n_tok > 0x7fffff00LL || H <= 0 || V <= 0 || K <= 0 || n_top < 0 || n_top > UNITY_MAX_TOP) return 0;
+    return carve_loss(nullptr, ~size_t(0), n_tok, H, V, K, n_top, backward ? wanted_chunk_rows(n_tok, K, kDefaultChunkMult) : 0,
+                      wanted_chunk_vocab(V, kDefaultChunkMult), backward != 0, nullptr).bytes;
+}
+
+int unity_cross_entropy_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_ce_params* params,
+                                const float* tok_weight, float* loss, float* tok_loss, float* lse, void* dHidden,
+                                void* const* dW) {
+    int rc = validate_rows(ctx, rows);
+    if (rc) return rc;
+    if (!params) return fail(ctx, UNITY_ERR_INVALID_ARG, "params is NULL");
+    if (!(params->label_smoothing >= 0.f && params->label_smoothing < 1.f))
+        return fail(ctx, UNITY_ERR_INVALID_ARG, "label_smoothing must lie in [0, 1)");
+    if (!(params->z_loss >= 0.f && params->z_loss <= 3.0e38f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "z_loss must be >= 0 and finite");
+    if (params->dW_type != UNITY_F32 && params->dW_type != UNITY_BF16) return fail(ctx, UNITY_ERR_INVALID_ARG, "dW_type must be UNITY_F32 or UNITY_BF16");
+    LossCall c;
+    memset(&c, 0, sizeof(c));
+    c.smoothing = params->label_smoothing; c.z_loss = params->z_loss;
+    c.norm = params->norm; c.tok_weight = tok_weight;
+    c.accumulate = params->accumulate_dW != 0; c.bf16_dw = params->dW_type == UNITY_BF16;
+    c.loss = loss; c.tok_loss = tok_loss; c.lse = lse; c.dHidden = dHidden; c.dW = dW;
+    return token_loss(ctx, rows, c);
+}
+
+int unity_distill_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_distill_params* params,
+                          const int32_t* top_ids, const float* top_vals, const float* tok_weight, float* loss,
+                          float* tok_loss, float* lse, void* dHidden, void* const* dW) {
+    if (!ctx) return UNITY_ERR_INVALID_ARG;
+    if (!params) return fail(ctx, UNITY_ERR_INVALID_ARG, "params is NULL");
+    if (!(params->kd_coef >= 0.f && params->kd_coef <= 3.0e38f) || !(params->hard_coef >= 0.f && params->hard_coef <= 3.0e38f))
+        return fail(ctx, UNITY_ERR_INVALID_ARG, "kd_coef and hard_coef must be >= 0 and finite");
+    int rc = validate_rows(ctx, rows, params->hard_coef > 0.f);
+    if (rc) return rc;
+    if (params->n_top < 1 || params->n_top > UNITY_MAX_TOP) return fail(ctx, UNITY_ERR_SHAPE, "n_top=%d outside [1,%d]", params->n_top, UNITY_MAX_TOP);
+    if (params->teacher_mode != UNITY_TEACHER_LOGITS && params->teacher_mode != UNITY_TEACHER_LOGPROBS)
+        return fail(ctx, UNITY_ERR_INVALID_ARG, "teacher_mode must be UNITY_TEACHER_LOGITS or UNITY_TEACHER_LOGPROBS");
+    if (params->dW_type != UNITY_F32 && params->dW_type != UNITY_BF16) return fail(ctx, UNITY_ERR_INVALID_ARG, "dW_type must be UNITY_F32 or UNITY_BF16");
+    if (rows->n_tok > 0 && (!top_ids || !top_vals)) return fail(ctx, UNITY_ERR_INVALID_ARG, "top_ids / top_vals is NULL");
+    unity_rows r = *rows;
+    if (!(params->hard_coef > 0.f)) r.target = nullptr;      // not read: its entries need not be valid
+    LossCall c;
+    memset(&c, 0, sizeof(c));
+    c.n_top = params->n_top; c.logits = params->teacher_mode == UNITY_TEACHER_LOGITS;
+    c.kd = params->kd_coef; c.hard = params->hard_coef; c.top_ids = top_ids; c.top_vals = top_vals;
+    c.norm = params->norm; c.tok_weight = tok_weight;
+    c.accumulate = params->accumulate_dW != 0; c.bf16_dw = params->dW_type == UNITY_BF16;
+    c.loss = loss; c.tok_loss = tok_loss; c.lse = lse; c.dHidden = dHidden; c.dW = dW;
+    return token_loss(ctx, &r, c);
 }
 
 }  // extern "C"
