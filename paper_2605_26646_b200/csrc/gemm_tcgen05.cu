@@ -66,6 +66,7 @@ __host__ __device__ constexpr bool is_grad(int epi) { return epi == kEpiLogitGra
 
 struct Unit {
     int m_tile, n_begin, n_end, split;
+    int k_begin, k_end;   // K slabs of 64 the unit contracts over
     bool rev;     // walk the unit's column tiles from n_end - 1 down to n_begin
 };
 
@@ -92,6 +93,8 @@ __device__ __forceinline__ bool in_rounds(const GemmArgs& g) {
 template <int EPI>
 __device__ __forceinline__ bool next_unit(const GemmArgs& g, int it, int pair, int n_pairs, int gm, Unit& t, bool& valid) {
     t.rev = false;
+    t.k_begin = 0;
+    t.k_end = g.k_iters;
     if (in_rounds<EPI>(g)) {
         const int m0 = it * gm;
         if (m0 >= g.m_tiles) return false;
@@ -114,7 +117,16 @@ __device__ __forceinline__ bool next_unit(const GemmArgs& g, int it, int pair, i
         // workers that hold the same run of columns sweep its W tiles in step
         const int tpu = stride_unit_tiles<EPI>(g);
         const int ncu = (g.n_tiles + tpu - 1) / tpu;
-        const int u = pair + it * n_pairs;
+        int u = pair + it * n_pairs;
+        t.split = 0;
+        if (EPI == kEpiAccumF32 && g.k_splits > 1) {   // the contraction cut into k_splits parts, one after the other
+            const int per_split = g.m_tiles * ncu;
+            if (u >= per_split * g.k_splits) return false;
+            t.split = u / per_split;
+            u -= t.split * per_split;
+            t.k_begin = t.split * g.k_per_split;
+            t.k_end = min(t.k_begin + g.k_per_split, g.k_iters);
+        }
         if (u >= g.m_tiles * ncu) return false;
         const int per_group = gm * ncu;
         const int grp = u / per_group, r = u - grp * per_group;
@@ -122,7 +134,6 @@ __device__ __forceinline__ bool next_unit(const GemmArgs& g, int it, int pair, i
         const int gm_here = min(gm, g.m_tiles - m0);
         const int q = r / gm_here;
         t.m_tile = m0 + (r - q * gm_here);
-        t.split = 0;
         if (tpu == 1) {
             // odd groups walk the columns backwards: the B tiles a group ends with are the ones the next group starts
             // with, while they are still in L2
@@ -195,11 +206,114 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     } else if (in.span_mode == kSpanRowsM) {
         g.m_rows = n_rows;
         g.m_tiles = n_rows / TILE_ROWS;
+        if (in.k_splits != 0) {
+            const SplitShape sp = split_shape(in.k_splits, g.m_tiles, g.n_tiles, g.k_iters, in.fwd.n_pairs);
+            g.k_splits = sp.splits; g.k_per_split = sp.per_split;
+            g.c_split = static_cast<long long>(n_rows) * in.ldc;
+        }
     } else if (in.span_mode == kSpanRowsK) {
         g.k_iters = n_rows / kTileK;
         g.b_k0 = in.b_k0 + slot0;
     }
     return g;
+}
+
+// Where a row stands in its ascending list of entries.
+struct TopCursor {
+    int next, pos, cnt;   // next vocabulary index (INT_MAX: none left)
+    long long base;
+};
+
+// Token losses, forward: one 256-column accumulator tile of one row (thread = row).  Two passes over tensor memory: the
+// tile's maximum first, so that the running sum is rescaled once per tile and everything below is relative to one
+// reference m (the row's running maximum including this tile):
+//   s += sum 2^((z - m) c2), z += sum z, the target's logit, the listed entries' logits, and, for a backward pass that does
+//   not recompute the logits, (m - z) in steps of 2^-10 octaves as 16-bit integers.
+// The integer costs as much memory as bf16 but is off by at most half a step whatever its size: p is off by a factor of
+// 2^(2^-11), 3.4e-4, where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries further than 64
+// octaves below m count as 64 (a probability below 2^-64 of the largest).  Sums of 32 columns are formed apart and then
+// added: V additions one after the other would cost log s three digits.
+__device__ __forceinline__ void loss_stats_tile(const GemmArgs& g, uint32_t taddr, int col0, int nt, int row, bool row_ok,
+                                                int tgt, float c2, float& run_m, uint64_t& run_s2, uint64_t& run_z2,
+                                                float& z_tgt, TopCursor& top) {
+    const int n_tile = min(kTileN, g.n_cols - col0);
+    float tm = kNegBig;
+#pragma unroll 1
+    for (int c = 0; c * 32 < n_tile; ++c) {
+        uint32_t rr[32];
+        ptx::tmem_ld_32x32(taddr + c * 32, rr);
+        ptx::tmem_ld_wait();
+        const int n_here = n_tile - c * 32;
+        float v[32];
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = j < n_here ? __uint_as_float(rr[j]) : kNegBig;
+        float cm = ptx::max3(v[0], v[1], v[2]);
+#pragma unroll
+        for (int j = 3; j < 31; j += 2) cm = ptx::max3(cm, v[j], v[j + 1]);
+        tm = ptx::max3(tm, cm, v[31]);
+    }
+    const float m = fmaxf(run_m, tm);
+    const float resc = ptx::ex2((run_m - m) * c2);
+    run_s2 = ptx::mul2(run_s2, ptx::pack2(resc, resc));
+    run_m = m;
+    if (g.tile_max != nullptr && row_ok) g.tile_max[static_cast<long long>(row) * g.n_tiles + nt] = m;
+    const uint64_t m2 = ptx::pack2(-m, -m), c22 = ptx::pack2(c2, c2);
+    const float steps = -c2 * kStashSteps;
+    const uint64_t steps2 = ptx::pack2(steps, steps), magic2 = ptx::pack2(8388608.f, 8388608.f);
+#pragma unroll 1
+    for (int c = 0; c * 32 < n_tile; ++c) {
+        const int cbase = col0 + c * 32, n_here = n_tile - c * 32;
+        uint32_t rr[32];
+        ptx::tmem_ld_32x32(taddr + c * 32, rr);
+        ptx::tmem_ld_wait();
+        uint64_t s2 = 0ull, z2 = 0ull;
+        unsigned packed[16];
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+            if (j < n_here) {                                  // V is a multiple of 8: whole pairs
+                const uint64_t x = ptx::pack2(__uint_as_float(rr[j]), __uint_as_float(rr[j + 1]));
+                const uint64_t d = ptx::add2(x, m2);
+                float a0, a1, t0, t1;
+                ptx::unpack2(ptx::mul2(d, c22), a0, a1);
+                s2 = ptx::add2(s2, ptx::pack2(ptx::ex2(a0), ptx::ex2(a1)));
+                z2 = ptx::add2(z2, x);
+                // adding 2^23 leaves the rounded integer in the low bits
+                ptx::unpack2(ptx::fma2(d, steps2, magic2), t0, t1);
+                packed[j >> 1] = __byte_perm(__float_as_uint(fminf(t0, 8388608.f + 65535.f)),
+                                             __float_as_uint(fminf(t1, 8388608.f + 65535.f)), 0x5410);
+            }
+        }
+        run_s2 = ptx::add2(run_s2, s2);
+        run_z2 = ptx::add2(run_z2, z2);
+        const int jt = tgt - cbase;
+        if (jt >= 0 && jt < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) if (j == jt) z_tgt = __uint_as_float(rr[j]);
+        }
+        while (top.next < cbase + 32) {                       // listed entries among these columns
+            const int jn = top.next - cbase;
+            float z = 0.f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) if (j == jn) z = __uint_as_float(rr[j]);
+            g.top_z[top.base + top.pos] = z;
+            ++top.pos;
+            top.next = top.pos < top.cnt ? g.top_ids[top.base + top.pos] : 0x7fffffff;
+        }
+        if (g.stash != nullptr && row_ok) {
+            uint16_t* dst = g.stash + static_cast<long long>(row) * g.ldz + cbase;      // pitch and base 32-byte aligned
+            if (n_here >= 32) {
+                ptx::st_global_v8(dst, packed[0], packed[1], packed[2], packed[3], packed[4], packed[5], packed[6], packed[7]);
+                ptx::st_global_v8(dst + 16, packed[8], packed[9], packed[10], packed[11], packed[12], packed[13], packed[14], packed[15]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (q * 8 < n_here)
+                        *reinterpret_cast<uint4*>(dst + q * 8) =
+                            make_uint4(packed[4 * q], packed[4 * q + 1], packed[4 * q + 2], packed[4 * q + 3]);
+                }
+            }
+        }
+    }
 }
 
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
@@ -278,7 +392,8 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     } else {
                         const long long before = static_cast<long long>(it) * n_pairs;      // units of earlier rounds
                         const int tpu = stride_unit_tiles<EPI>(g);
-                        const long long left = static_cast<long long>(g.m_tiles) * ((g.n_tiles + tpu - 1) / tpu) - before;
+                        const long long left = static_cast<long long>(g.m_tiles) * ((g.n_tiles + tpu - 1) / tpu) *
+                                               (EPI == kEpiAccumF32 && g.k_splits > 1 ? g.k_splits : 1) - before;
                         expect = static_cast<unsigned>(it / g.sync_period) * static_cast<unsigned>(n_pairs) +
                                  static_cast<unsigned>(left < n_pairs ? left : n_pairs);
                     }
@@ -295,7 +410,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     // MMA simply leaves their last columns unread
                     const int mma_n = EPI == kEpiAccumF32 ? g.mma_n : kTileN;
                     const int b_row = g.b_row0 + nt * (NB * mma_n) + static_cast<int>(cta_rank) * (mma_n / CTAS);
-                    for (int k = 0; k < g.k_iters; ++k) {
+                    for (int k = t.k_begin; k < t.k_end; ++k) {
                         if (!ptx::mbar_wait(&empty[stage], phase ^ 1, g.wait_budget) || *abort_flag) { ok = false; break; }
                         if (g.test_drop_slab && it == 0 && ni == t.n_begin && k == (g.k_iters > 1 ? 1 : 0)) {
                             // test hook: this slab never arrives; the MMA issuer's wait for it must run out
@@ -352,7 +467,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     if (!ptx::mbar_wait(&acc_empty[acc], acc_phase ^ 1, g.wait_budget) || *abort_flag) { ok = false; break; }
                     ptx::tc_fence_after();
                     const uint32_t d_tmem = tmem_base + acc * kTileCols;
-                    for (int k = 0; k < g.k_iters; ++k) {
+                    for (int k = t.k_begin; k < t.k_end; ++k) {
                         if (!ready && !ptx::mbar_wait(&full[stage], phase, g.wait_budget)) { ok = false; break; }
                         ptx::tc_fence_after();
                         const int next_stage = stage + 1 == kStages ? 0 : stage + 1;
@@ -373,7 +488,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                             for (int kk = 0; kk < kTileK / 16; ++kk)
                                 ptx::mma_bf16_ss_on<CTAS>(d_tmem + nb * kTileN, da + step_a * kk,
                                                           db + static_cast<uint64_t>(nb * (kBBytes >> 4)) + step_b * kk, idesc,
-                                                          (k | kk) != 0 ? 1u : 0u);
+                                                          ((k - t.k_begin) | kk) != 0 ? 1u : 0u);
                         }
                         ptx::tc_commit_on<CTAS>(&empty[stage]);
                         stage = next_stage;
@@ -440,19 +555,18 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 lt = g.target_g[g.a_row0 + row];
             }
             // ... the row's listed entries: the next one at or after this unit's first column
-            int top_next = 0x7fffffff, top_pos = 0, top_cnt = 0;
-            long long top_base = 0;
+            TopCursor top{0x7fffffff, 0, 0, 0};
             if (EPI == kEpiLossStats && g.top_ids != nullptr && row_ok) {
-                top_base = static_cast<long long>(g.a_row0 + row) * g.top_n;
-                top_cnt = g.top_cnt[g.a_row0 + row];
+                top.base = static_cast<long long>(g.a_row0 + row) * g.top_n;
+                top.cnt = g.top_cnt[g.a_row0 + row];
                 const int first = t.n_begin * kTileN;
-                int lo = 0, hi = top_cnt;
+                int lo = 0, hi = top.cnt;
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
-                    if (g.top_ids[top_base + mid] < first) lo = mid + 1; else hi = mid;
+                    if (g.top_ids[top.base + mid] < first) lo = mid + 1; else hi = mid;
                 }
-                top_pos = lo;
-                if (top_pos < top_cnt) top_next = g.top_ids[top_base + top_pos];
+                top.pos = lo;
+                if (top.pos < top.cnt) top.next = g.top_ids[top.base + top.pos];
             }
 
             for (int ni = t.n_begin; ni < t.n_end && ok; ++ni) {
@@ -463,8 +577,11 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 const int mma_n = EPI == kEpiAccumF32 ? g.mma_n : kTileN;     // columns per MMA block (<= 256)
                 const int col0 = nt * (NB * mma_n);
                 const int per_block = mma_n / 32;
+                if (EPI == kEpiLossStats) {
+                    loss_stats_tile(g, taddr, col0, nt, row, row_ok, tgt, c2, run_m, run_s2, run_t2, z_tgt, top);
+                }
 #pragma unroll 1
-                for (int c = 0; c < NB * per_block; ++c) {
+                for (int c = 0; c < (EPI == kEpiLossStats ? 0 : NB * per_block); ++c) {
                     const int cbase = col0 + c * 32;            // block nb of a two-block tile starts at col0 + nb * mma_n
                     if (cbase >= g.n_cols) break;               // uniform across the CTA
                     uint32_t rr[32];
@@ -529,47 +646,6 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                                             make_uint4(zp[4 * q], zp[4 * q + 1], zp[4 * q + 2], zp[4 * q + 3]);
                                 }
                             }
-                        }
-                    } else if (EPI == kEpiLossStats) {
-                        // the same online sums without the entropy's; sum z (label smoothing) in its place.  V is a multiple
-                        // of 8, so the last columns end on a pair.
-                        if (n_here < 32) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) if (j >= n_here) v[j] = kNegBig;
-                        }
-                        float cm = ptx::max3(v[0], v[1], v[2]);
-#pragma unroll
-                        for (int j = 3; j < 31; j += 2) cm = ptx::max3(cm, v[j], v[j + 1]);
-                        cm = fmaxf(cm, v[31]);
-                        const float new_m = fmaxf(run_m, cm);
-                        const float resc = ptx::ex2((run_m - new_m) * c2);
-                        run_s2 = ptx::mul2(run_s2, ptx::pack2(resc, resc));
-                        run_m = new_m;
-                        const float shift = -new_m * c2;
-                        const uint64_t shift2 = ptx::pack2(shift, shift), c22 = ptx::pack2(c2, c2);
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            if (j < n_here) {
-                                const uint64_t x = ptx::pack2(v[j], v[j + 1]);
-                                float a0, a1;
-                                ptx::unpack2(ptx::fma2(x, c22, shift2), a0, a1);
-                                run_s2 = ptx::add2(run_s2, ptx::pack2(ptx::ex2(a0), ptx::ex2(a1)));
-                                run_t2 = ptx::add2(run_t2, x);
-                            }
-                        }
-                        const int jt = tgt - cbase;
-                        if (jt >= 0 && jt < 32) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) if (j == jt) z_tgt = v[j];
-                        }
-                        while (top_next < cbase + 32) {           // listed entries among these columns
-                            const int jn = top_next - cbase;
-                            float z = 0.f;
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) if (j == jn) z = v[j];
-                            g.top_z[top_base + top_pos] = z;
-                            ++top_pos;
-                            top_next = top_pos < top_cnt ? g.top_ids[top_base + top_pos] : 0x7fffffff;
                         }
                     } else if (EPI == kEpiLossGrad) {
                         unsigned packed[16];
@@ -668,7 +744,35 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                         }
                     } else {
                         if (row_ok) {
-                            float* dst = g.C + static_cast<long long>(row) * g.ldc + cbase;
+                            if (g.C16 != nullptr) {
+                                // bf16 output: the fp32 accumulator (plus the old value) rounded once
+                                __nv_bfloat16* d16 = g.C16 + static_cast<long long>(row) * g.ldc + cbase;
+                                if (g.beta) {
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q) {
+                                        const uint4 old = *reinterpret_cast<const uint4*>(d16 + q * 8);
+                                        const unsigned ow[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+                                        for (int j = 0; j < 4; ++j) {
+                                            v[8 * q + 2 * j] += __uint_as_float(ow[j] << 16);
+                                            v[8 * q + 2 * j + 1] += __uint_as_float(ow[j] & 0xffff0000u);
+                                        }
+                                    }
+                                }
+                                unsigned o[16];
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) o[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+                                if (g.g_wide_store) {
+                                    ptx::st_global_v8(d16, o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]);
+                                    ptx::st_global_v8(d16 + 16, o[8], o[9], o[10], o[11], o[12], o[13], o[14], o[15]);
+                                } else {
+#pragma unroll
+                                    for (int q = 0; q < 4; ++q)
+                                        *reinterpret_cast<uint4*>(d16 + q * 8) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                                }
+                                continue;
+                            }
+                            float* dst = g.C + t.split * g.c_split + static_cast<long long>(row) * g.ldc + cbase;
 #pragma unroll
                             for (int q = 0; q < 8; ++q) {
                                 if (q * 4 < n_here) {

@@ -107,6 +107,29 @@ __host__ __device__ inline FwdShape forward_shape(const FwdPlanParams& p, int ro
     return best;
 }
 
+// Parts a contraction of k_iters slabs is cut into when its m_tiles x n_tiles outputs alone do not fill the workers (few
+// rows): the count with the least time, a worker's longest run of slabs plus, per part, the pipeline's fill and its
+// unoverlapped epilogue (kSplitOverhead slabs).  Computed alike by the GEMM, by the kernel that adds the parts up, and by
+// the host for the size of their buffer.
+constexpr int kSplitOverhead = 10;
+constexpr int kSplitWaves = 6;          // no more parts than make up 6 waves of workers: bounds their buffer
+struct SplitShape { int splits, per_split; };
+__host__ __device__ inline SplitShape split_shape(int most, int m_tiles, int n_tiles, int k_iters, int workers) {
+    SplitShape best{1, k_iters};
+    long long best_cost = -1;
+    const int cap = k_iters / 8 < most ? k_iters / 8 : most;      // a part has at least 8 slabs
+    for (int s = 1; s <= (cap > 1 ? cap : 1); ++s) {
+        if (s > 1 && static_cast<long long>(m_tiles) * n_tiles * s > static_cast<long long>(kSplitWaves) * workers) break;
+        const int per = (k_iters + s - 1) / s, n = per > 0 ? (k_iters + per - 1) / per : 1;
+        const long long waves = (static_cast<long long>(m_tiles) * n_tiles * n + workers - 1) / workers;
+        const long long cost = waves * (per + kSplitOverhead) + (s > 1 ? s : 0);
+        if (best_cost < 0 || cost < best_cost) { best_cost = cost; best.splits = n; best.per_split = per; }
+    }
+    return best;
+}
+constexpr int kMaxKSplits = 32;
+constexpr float kStashSteps = 1024.f;   // steps per octave of a kept logit (GemmArgs::stash)
+
 // ----------------------------------------------------------------------------------------------
 // GEMM  C[m, n] = sum_k A[m, k] * B[n, k]   (bf16 operands, K-major or MN-major, fp32 accumulation in TMEM)
 // ----------------------------------------------------------------------------------------------
@@ -164,6 +187,9 @@ struct GemmArgs {
     const int* top_cnt;       // [rows]
     float* top_z;             // out [rows, top_n]
     int top_n;
+    uint16_t* stash;          // optional, a block of rows: (running maximum - logit) in steps of 1 / kStashSteps octaves,
+                              // row pitch ldz ...
+    float* tile_max;          // ... and the running maximum each column tile refers to [rows, n_tiles], accumulator units
     // kEpiLossGrad: G = coef_p * p - coef_g * uniform, and target_g at the target (row_lse as above)
     const float* coef_p;      // [rows] dL/dz_v per unit of p_v, times scale
     const float* coef_g;      // [rows] scale * weight / M
@@ -171,7 +197,11 @@ struct GemmArgs {
     float uniform;            // label smoothing's share of every entry: eps / V
     // kEpiAccumF32
     float* C;
+    __nv_bfloat16* C16;       // not null: the output is bf16, here (row pitch ldc), and C is unused
     long long ldc;
+    int k_splits, k_per_split;   // the contraction is cut into k_splits parts of k_per_split slabs, each with an output of
+    long long c_split;           // its own, c_split values apart (0 or 1: not cut).  Before the kernel resolves its span (rows
+                                 // known on the device only), k_splits is the most parts split_shape may choose
     int beta;                 // 0: overwrite, 1: add to C
     int mma_n;                // columns per MMA block, a multiple of 32 up to 256 (a tile is 1 or 2 blocks wide); 256
                               // unless the output's width divides better (896 columns = 4 blocks of 224)
@@ -403,6 +433,29 @@ struct TeacherScatterArgs {
     long long ld;
 };
 cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream);
+// In place, the kept logits of a block of rows (GemmArgs::stash) become dL/dz in bf16: coef_p * p - coef_g * uniform, and
+// target_g at the target, with p = 2^(tile_max * c2 - lse log2(e) - u / kStashSteps).
+struct LossGradArgs {
+    uint16_t* Z;
+    long long ld;
+    RowSpan span;              // per-row vectors are indexed from its first slot
+    int cols, n_tiles;
+    const float* tile_max;     // [rows, n_tiles]
+    float c2;                  // inv_temperature * log2(e)
+    const int* target_p;
+    const float *row_lse, *coef_p, *coef_g, *target_g;
+    float uniform;
+};
+cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, cudaStream_t stream);
+// dHidden[token of slot r of the span] = bf16(sum of the row's k_splits parts), in the order of the parts
+struct StoreArgs {
+    const float* parts;        // [splits][rows of the span][H]
+    const int* slot_tok;
+    RowSpan span;
+    int H, most, n_tiles, k_iters, workers, tile_rows;   // what split_shape was given
+    __nv_bfloat16* dHidden;
+};
+cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream);
 // dst[0, n) = bf16(src) (+ dst when add); n a multiple of 8
 cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream);
 

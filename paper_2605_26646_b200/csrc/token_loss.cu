@@ -272,6 +272,76 @@ __global__ void __launch_bounds__(256) k_teacher_scatter(TeacherScatterArgs a) {
     }
 }
 
+// A block converts 8192 columns of a row: each thread issues four 128-bit loads 4 KiB apart, so a warp's access is the 256
+// columns of one tile of the forward GEMM and has one reference maximum.  2 B read and 2 B written per logit.
+constexpr int kGradVecs = 4;
+__global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
+    const int c_first = blockIdx.x * (256 * 8 * kGradVecs) + threadIdx.x * 8;
+    int row0, rows;
+    span_resolve(a.span, row0, rows);
+    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+        const int slot = row0 + r;
+        uint4* row = reinterpret_cast<uint4*>(a.Z + static_cast<long long>(r) * a.ld);
+        const float* tm = a.tile_max + static_cast<long long>(r) * a.n_tiles;
+        uint4 raw[kGradVecs];
+        float shift[kGradVecs];
+#pragma unroll
+        for (int u = 0; u < kGradVecs; ++u) {
+            const int c0 = c_first + u * 2048;
+            if (c0 < a.cols) { raw[u] = row[c0 >> 3]; shift[u] = tm[c0 / kTileN]; }
+        }
+        const float base = -a.row_lse[slot] * 1.4426950408889634f;
+        const float cp = a.coef_p[slot], cu = a.coef_g[slot] * a.uniform, gt = a.target_g[slot];
+        const int tgt = a.target_p[slot];
+#pragma unroll
+        for (int u = 0; u < kGradVecs; ++u) {
+            const int c0 = c_first + u * 2048;
+            if (c0 >= a.cols) continue;
+            const float sh = fmaf(shift[u], a.c2, base);
+            unsigned* w = reinterpret_cast<unsigned*>(&raw[u]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float u0 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7610)) - 8388608.f;
+                const float u1 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7632)) - 8388608.f;
+                float g0 = fmaf(cp, exp2f(fmaf(u0, -1.f / kStashSteps, sh)), -cu);
+                float g1 = fmaf(cp, exp2f(fmaf(u1, -1.f / kStashSteps, sh)), -cu);
+                if (c0 + 2 * j == tgt) g0 = gt;
+                if (c0 + 2 * j + 1 == tgt) g1 = gt;
+                const __nv_bfloat162 h = __floats2bfloat162_rn(g0, g1);
+                w[j] = *reinterpret_cast<const unsigned*>(&h);
+            }
+            row[c0 >> 3] = raw[u];
+        }
+    }
+}
+
+// One block per row: four columns per thread and step, the parts added in their order, one rounding to bf16.
+__global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
+    int slot0, rows;
+    span_resolve(a.span, slot0, rows);
+    const int r = blockIdx.x;
+    if (r >= rows) return;
+    const int tok = a.slot_tok[slot0 + r];
+    if (tok < 0) return;
+    __shared__ int sh_splits;
+    if (threadIdx.x == 0)
+        sh_splits = a.most != 0 ? split_shape(a.most, rows / a.tile_rows, a.n_tiles, a.k_iters, a.workers).splits : 1;
+    __syncthreads();
+    const int splits = sh_splits;
+    const long long stride = static_cast<long long>(rows) * a.H;
+    const float* src = a.parts + static_cast<long long>(r) * a.H;
+    __nv_bfloat16* dst = a.dHidden + static_cast<long long>(tok) * a.H;
+    for (int c = threadIdx.x * 4; c < a.H; c += 1024) {
+        float4 v = *reinterpret_cast<const float4*>(src + c);
+        for (int s = 1; s < splits; ++s) {
+            const float4 o = *reinterpret_cast<const float4*>(src + s * stride + c);
+            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+        }
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+        *reinterpret_cast<uint2*>(dst + c) = make_uint2(*reinterpret_cast<const unsigned*>(&lo), *reinterpret_cast<const unsigned*>(&hi));
+    }
+}
+
 // dst = bf16(src) (+ dst): one rounding of the fp32 sum over all row blocks.  Eight values per thread and step.
 __global__ void __launch_bounds__(256) k_cast_dw(const float4* __restrict__ src, uint4* __restrict__ dst, long long n8, int add) {
     const long long stride = static_cast<long long>(gridDim.x) * blockDim.x;
@@ -319,6 +389,19 @@ cudaError_t launch_loss_sum(const LossRowArgs& a, cudaStream_t stream) {
 
 cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream) {
     k_teacher_scatter<<<static_cast<unsigned>((a.span.row_cap + 7) / 8), 256, 0, stream>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, cudaStream_t stream) {
+    const int gx = (a.cols + 256 * 8 * kGradVecs - 1) / (256 * 8 * kGradVecs);
+    const int gy = a.span.row_cap < 32768 ? a.span.row_cap : 32768;
+    if (gy <= 0) return cudaSuccess;
+    k_loss_grad_inplace<<<dim3(gx, gy), 256, 0, stream>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {
+    k_store_parts<<<a.span.row_cap, 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
 

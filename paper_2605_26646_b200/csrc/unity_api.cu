@@ -67,6 +67,7 @@ constexpr int kDefaultChunkMult = 2;
 constexpr int kSyncCounters = 16384;       // rendezvous counters per call (4 bytes each)
 constexpr int kMinChunkRows = 1024;
 constexpr int kMinChunkVocab = 1024;
+constexpr int kMinKeepRows = 2048;         // token losses: least rows of a block whose logits are kept
 
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -437,21 +438,38 @@ struct LossLayout {
     __nv_bfloat16* hp; int* target_p; float4* stats; float* partial;
     int *ids_p, *cnt_p; float *q_p, *top_z;
     float *row_lse, *coef_p, *coef_g, *target_g;
-    __nv_bfloat16* G; float *dHc, *dWc;
+    __nv_bfloat16* G; float *tile_max, *parts, *dWc;
     long long max_slots;
-    int n_blocks, chunk_rows, chunk_vocab;
+    int n_blocks;
     size_t bytes;
 };
 
-// chunk_rows = 0: no gradient.  dw_scratch: fp32 copy of one dW, for sums over several row blocks rounded to bf16 once.
-LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int K, int n_top, int chunk_rows,
-                      int chunk_vocab, bool dw_scratch, bool* fits) {
+// How the backward walks the rows and the vocabulary: blocks of `rows` packed rows; `keep`: a block's logits are kept
+// (16 bits each, pitch `cols`) by its forward sweep and become dL/dz in place; otherwise pieces of `cols` vocabulary
+// entries are recomputed one after the other.  rows = 0: no gradient.
+struct LossBlocks {
+    int rows, cols;
+    bool keep, dw_scratch;       // dw_scratch: fp32 copy of one dW, for bf16 sums over several blocks that are rounded once
+};
+
+// Rows of the buffer that takes the parts of dHidden (split_shape): a block of rows, or the parts of fewer rows.
+// 160 bounds the SMs of the parts; on a larger device the contraction is not cut.
+constexpr int kMaxSms = 160;
+long long part_rows(int block_rows, int H, int V) {
+    const int wide = 2 * gemm_mma_n(H), n_tiles = H > kTileN ? (H + wide - 1) / wide : 1;
+    const long long splits = (V + kTileK - 1) / kTileK / 8;
+    const long long most = static_cast<long long>(block_rows) * (splits < 1 ? 1 : (splits < kMaxKSplits ? splits : kMaxKSplits));
+    const long long waves = static_cast<long long>(kSplitWaves) * kMaxSms * kCtaM / n_tiles;
+    const long long cut = most < waves ? most : waves;
+    return cut > block_rows ? cut : block_rows;
+}
+
+LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int K, int n_top, const LossBlocks& B, bool* fits) {
     LossLayout L;
     memset(&L, 0, sizeof(L));
     Bump b{base, 0, cap, true};
     L.max_slots = max_slots_of(n_tok, K);
     L.n_blocks = static_cast<int>((n_tok + kRouteBlock - 1) / kRouteBlock);
-    L.chunk_rows = chunk_rows; L.chunk_vocab = chunk_vocab;
     const size_t ms = static_cast<size_t>(L.max_slots);
     L.tok_slot = b.take<int>(n_tok);
     L.slot_tok = b.take<int>(ms);
@@ -469,18 +487,26 @@ LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int
         L.q_p = b.take<float>(ms * n_top);
         L.top_z = b.take<float>(ms * n_top);
     }
-    if (chunk_rows > 0) {
+    if (B.rows > 0) {
         L.row_lse = b.take<float>(ms);
         L.coef_p = b.take<float>(ms);
         L.coef_g = b.take<float>(ms);
         L.target_g = b.take<float>(ms);
-        L.G = b.take<__nv_bfloat16>(static_cast<size_t>(chunk_rows) * chunk_vocab);
-        L.dHc = b.take<float>(static_cast<size_t>(chunk_rows) * H);
-        if (dw_scratch) L.dWc = b.take<float>(static_cast<size_t>(V) * H);
+        L.G = b.take<__nv_bfloat16>(static_cast<size_t>(B.rows) * B.cols);
+        if (B.keep) L.tile_max = b.take<float>(static_cast<size_t>(B.rows) * (B.cols / kTileN));
+        L.parts = b.take<float>(static_cast<size_t>(part_rows(B.rows, H, V)) * H);
+        if (B.dw_scratch) L.dWc = b.take<float>(static_cast<size_t>(V) * H);
     }
     L.bytes = up(b.off, kAlign);
     if (fits) *fits = b.ok;
     return L;
+}
+
+// Blocks of equal size, at most kStashRows rows each.
+LossBlocks keep_blocks(long long n_tok, int V, bool dw_sums, int most) {
+    const long long bound = static_cast<long long>(up(n_tok, kTileM)), n = (bound + most - 1) / most;
+    const int rows = static_cast<int>(up((bound + n - 1) / (n > 0 ? n : 1), kTileM));
+    return LossBlocks{rows, static_cast<int>(up(V, kTileN)), true, dw_sums && bound > rows};
 }
 
 int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
@@ -503,18 +529,29 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         return UNITY_OK;
     }
 
-    int cr = want ? wanted_chunk_rows(r->n_tok, K, ctx->chunk_rows_mult) : 0;
-    int cv = want ? wanted_chunk_vocab(V, ctx->chunk_vocab_mult) : 0;
+    // the largest blocks that fit: with kept logits down to kMinKeepRows rows (smaller ones read and write dW too often),
+    // then pieces of recomputed ones
+    const long long rows_bound = static_cast<long long>(up(r->n_tok, kTileM));
+    LossBlocks B{0, 0, false, false};
     LossLayout L;
-    for (;;) {
-        bool fits = false;
-        L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, cr, cv, want_w && c.bf16_dw, &fits);
-        if (fits) break;
-        if (cr > kMinChunkRows && cr >= cv) cr = static_cast<int>(up(cr / 2, kTileM));
-        else if (cv > kMinChunkVocab) cv = static_cast<int>(up(cv / 2, kTileN));
-        else if (cr > kMinChunkRows) cr = static_cast<int>(up(cr / 2, kTileM));
-        else return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: need at least %zu bytes, have %zu", L.bytes, ctx->ws_bytes);
+    bool fits = false;
+    if (!want) L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, B, &fits);
+    for (int most = kStashRows; want && !fits && most >= kMinKeepRows; most /= 2) {
+        B = keep_blocks(r->n_tok, V, want_w && c.bf16_dw, most);
+        L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, B, &fits);
     }
+    if (want && !fits) {
+        int cr = static_cast<int>(rows_bound < kChunkRows ? rows_bound : kChunkRows), cv = wanted_chunk_vocab(V);
+        for (;;) {
+            B = LossBlocks{cr, cv, false, want_w && c.bf16_dw && rows_bound > cr};
+            L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, B, &fits);
+            if (fits) break;
+            if (cr > kMinChunkRows && (cr >= cv || cv <= kMinChunkVocab)) cr = static_cast<int>(up(cr / 2, kTileM));
+            else if (cv > kMinChunkVocab) cv = static_cast<int>(up(cv / 2, kTileN));
+            else break;
+        }
+    }
+    if (!fits) return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: need at least %zu bytes, have %zu", L.bytes, ctx->ws_bytes);
     if (c.tok_loss) CUDA_TRY(ctx, cudaMemsetAsync(c.tok_loss, 0, sizeof(float) * r->n_tok, st));
     if (c.lse) CUDA_TRY(ctx, cudaMemsetAsync(c.lse, 0, sizeof(float) * r->n_tok, st));
 
@@ -522,7 +559,6 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     FwdPlanParams fwd = fwd_params(ctx, V, H);
     fwd.max_splits = fwd.n_pairs;
     SyncCounters counters{L.sync_counters, 0, kSyncCounters};
-    const long long rows_bound = static_cast<long long>(up(r->n_tok, kTileM));
     CUDA_TRY(ctx, cudaMemsetAsync(L.slot_tok, 0xff, sizeof(int) * L.max_slots, st));
     CUDA_TRY(ctx, cudaMemsetAsync(L.sync_counters, 0, sizeof(unsigned) * kSyncCounters, st));
     RouteArgs ra;
@@ -543,26 +579,24 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         nl += 1;
     }
 
-    // forward: statistics of every row of every model
     CUtensorMap tm_hp_k, tm_hp_mn;
     if ((rc = make_tmap(ctx, &tm_hp_k, L.hp, H, L.max_slots, static_cast<uint64_t>(H) * 2, kBoxRows))) return rc;
     if ((rc = make_tmap(ctx, &tm_hp_mn, L.hp, H, L.max_slots, static_cast<uint64_t>(H) * 2, kTileK))) return rc;
-    for (int k = 0; k < K; ++k) {
-        const int ctas = ctx->ctas[UNITY_PROF_FWD_GEMM];
-        CUtensorMap tmB;
-        if ((rc = make_tmap(ctx, &tmB, r->W[k], H, V, static_cast<uint64_t>(H) * 2, kTileN / ctas))) return rc;
+    // forward sweep over the vocabulary for the rows of `span`: statistics, the listed entries' logits, the kept logits
+    auto forward = [&](const RowSpan& span, bool whole, const CUtensorMap& tmB) {
         GemmArgs g;
         memset(&g, 0, sizeof(g));
-        g.span = RowSpan{L.plan, k, 0, 0x7fffff00}; g.span_mode = kSpanForward; g.stats_from_plan = 1; g.fwd = fwd;
+        g.span = span; g.span_mode = kSpanForward; g.stats_from_plan = whole ? 1 : 0; g.fwd = fwd;
         g.m_tiles = 1;                                   // set by the kernel
-        g.n_tiles = (V + kTileN - 1) / kTileN; g.k_iters = H / kTileK; g.n_cols = V;
+        g.n_tiles = fwd.n_tiles; g.k_iters = H / kTileK; g.n_cols = V;
         g.stats = L.stats; g.target_p = L.target_p; g.scale = r->inv_temperature;
         g.top_ids = L.ids_p; g.top_cnt = L.cnt_p; g.top_z = L.top_z; g.top_n = c.n_top;
+        if (!whole) { g.stash = reinterpret_cast<uint16_t*>(L.G); g.ldz = B.cols; g.tile_max = L.tile_max; }
         gemm_common(ctx, g, UNITY_PROF_FWD_GEMM, &counters, ctx->fwd_sync != 0);
         ProfScope ps(ctx, UNITY_PROF_FWD_GEMM);
-        CUDA_TRY(ctx, launch_gemm(kEpiLossStats, false, ctas, tm_hp_k, tmB, g, ctx->sm_count, st));
         nl += 1;
-    }
+        return launch_gemm(kEpiLossStats, false, ctx->ctas[UNITY_PROF_FWD_GEMM], tm_hp_k, tmB, g, ctx->sm_count, st);
+    };
     LossRowArgs la;
     memset(&la, 0, sizeof(la));
     la.block = RowSpan{L.plan, -1, 0, 0}; la.plan = L.plan; la.fwd = fwd; la.max_slots = L.max_slots; la.K = K; la.V = V;
@@ -573,103 +607,145 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     la.ids_p = L.ids_p; la.cnt_p = L.cnt_p; la.q_p = L.q_p; la.top_z = L.top_z; la.target_p = L.target_p;
     la.with_grad = want; la.row_lse = L.row_lse; la.coef_p = L.coef_p; la.coef_g = L.coef_g; la.target_g = L.target_g;
     la.tok_loss = c.tok_loss; la.lse = c.lse; la.partial = L.partial; la.loss = c.loss;
-    CUDA_TRY(ctx, launch_loss_rows(la, st));
-    CUDA_TRY(ctx, launch_loss_sum(la, st));
-    nl += 2;
-    if (!want) { ctx->launches += nl; return UNITY_OK; }
-
-    // backward: per model, block of rows and piece of the vocabulary: G = dL/dz in bf16, dHidden += G W, dW += G^T hidden
+    const int c_fwd = ctx->ctas[UNITY_PROF_FWD_GEMM], c_grad = ctx->ctas[UNITY_PROF_GRAD_GEMM],
+              c_dh = ctx->ctas[UNITY_PROF_DH_GEMM], c_dw = ctx->ctas[UNITY_PROF_DW_GEMM];
+    auto w_map = [&](CUtensorMap* tm, int k, int box) {
+        return make_tmap(ctx, tm, r->W[k], H, V, static_cast<uint64_t>(H) * 2, box);
+    };
+    if (!B.keep) {
+        for (int k = 0; k < K; ++k) {
+            CUtensorMap tmB;
+            if ((rc = w_map(&tmB, k, kTileN / c_fwd))) return rc;
+            CUDA_TRY(ctx, forward(RowSpan{L.plan, k, 0, 0x7fffff00}, true, tmB));
+        }
+        CUDA_TRY(ctx, launch_loss_rows(la, st));
+        nl += 1;
+    }
     __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
     if (want_h) { CUDA_TRY(ctx, launch_zero_masked_rows(L.tok_slot, r->n_tok, H, dH, st)); nl += 1; }
-    const int c_grad = ctx->ctas[UNITY_PROF_GRAD_GEMM], c_dh = ctx->ctas[UNITY_PROF_DH_GEMM], c_dw = ctx->ctas[UNITY_PROF_DW_GEMM];
+
+    // per model and block of rows: G = dL/dz in bf16, dHidden = G W, dW += G^T hidden
     const int mma_n = gemm_mma_n(H);
-    for (int k = 0; k < K; ++k) {
-        const __nv_bfloat16* Wk = static_cast<const __nv_bfloat16*>(r->W[k]);
-        float* dWk = want_w ? (c.bf16_dw ? L.dWc : static_cast<float*>(c.dW[k])) : nullptr;
-        const bool add_dw = c.accumulate && !c.bf16_dw;
+    const bool two_blocks = ctx->wide_acc && H > mma_n;
+    for (int k = 0; want && k < K; ++k) {
+        float* dWk = want_w ? (B.dw_scratch ? L.dWc : static_cast<float*>(c.dW[k])) : nullptr;
+        const bool out16 = c.bf16_dw && !B.dw_scratch, add_dw = c.accumulate && !B.dw_scratch;
         if (want_w && !add_dw) {   // a model without rows: its dW reads zero
-            CUDA_TRY(ctx, launch_zero_if_empty(dWk, static_cast<long long>(V) * H, L.plan, k, st));
+            CUDA_TRY(ctx, launch_zero_if_empty(dWk, static_cast<long long>(V) * H / (out16 ? 2 : 1), L.plan, k, st));
             nl += 1;
         }
-        CUtensorMap tm_W_k, tm_W_mn;
-        if ((rc = make_tmap(ctx, &tm_W_k, Wk, H, V, static_cast<uint64_t>(H) * 2, kTileN / c_grad))) return rc;
-        if ((rc = make_tmap(ctx, &tm_W_mn, Wk, H, V, static_cast<uint64_t>(H) * 2, kTileK))) return rc;
-        for (long long c0 = 0; c0 < rows_bound; c0 += cr) {
-            const int nc = static_cast<int>(rows_bound - c0 < cr ? rows_bound - c0 : cr);
+        CUtensorMap tm_W_f, tm_W_k, tm_W_mn;
+        if ((rc = w_map(&tm_W_f, k, kTileN / c_fwd)) || (rc = w_map(&tm_W_k, k, kTileN / c_grad)) || (rc = w_map(&tm_W_mn, k, kTileK))) return rc;
+        for (long long c0 = 0; c0 < rows_bound; c0 += B.rows) {
+            const int nc = static_cast<int>(rows_bound - c0 < B.rows ? rows_bound - c0 : B.rows);
             const RowSpan chunk{L.plan, k, static_cast<int>(c0), nc};
-            int base, n_pieces;
-            vocab_chunks(V, cv, &base, &n_pieces);
+            int base = V, n_pieces = 1;
+            if (B.keep) {
+                CUDA_TRY(ctx, forward(chunk, false, tm_W_f));
+                LossRowArgs lb = la;
+                lb.block = chunk;
+                CUDA_TRY(ctx, launch_loss_rows(lb, st));
+                const LossGradArgs lg{reinterpret_cast<uint16_t*>(L.G), B.cols, chunk, V, fwd.n_tiles, L.tile_max,
+                                      r->inv_temperature * 1.4426950408889634f, L.target_p, L.row_lse, L.coef_p, L.coef_g,
+                                      L.target_g, c.smoothing / static_cast<float>(V)};
+                ProfScope ps(ctx, UNITY_PROF_GRAD_GEMM);
+                CUDA_TRY(ctx, launch_loss_grad_inplace(lg, st));
+                nl += 2;
+            } else {
+                vocab_chunks(V, B.cols, &base, &n_pieces);
+            }
             for (int ci = 0; ci < n_pieces; ++ci) {
                 const int v0 = ci * base, vc = ci + 1 == n_pieces ? V - v0 : base;
-                GemmArgs g;
-                memset(&g, 0, sizeof(g));
-                g.span = chunk; g.span_mode = kSpanRowsA;
-                g.m_tiles = 1;                                   // set by the kernel
-                g.n_tiles = (vc + kTileN - 1) / kTileN; g.k_iters = H / kTileK; g.group_m = 1;
-                g.fwd.n_pairs = ctx->sm_count / c_grad; g.fwd.tile_rows = gemm_tile_rows(c_grad); g.fwd.n_tiles = g.n_tiles;
-                g.fwd.max_splits = g.fwd.n_pairs;
-                if (large_rounds_fit(ctx, H)) {
-                    g.fwd.gmax = ctx->sm_count / 2 / c_grad;
-                } else {   // runs of column tiles, as many row tiles in flight as a 45 MB share of L2 holds
-                    int runs = static_cast<int>((45ll << 20) / (128ll * H * 2));
-                    runs = runs < 8 ? 8 : (runs > ctx->sm_count / 2 ? ctx->sm_count / 2 : runs);
-                    g.plan_runs = 1;
-                    g.fwd.gmax = runs / c_grad > 0 ? runs / c_grad : 1;
-                }
-                g.b_row0 = v0; g.n_cols = vc; g.target_p = L.target_p; g.vocab0 = v0; g.scale = r->inv_temperature;
-                g.row_lse = L.row_lse; g.coef_p = L.coef_p; g.coef_g = L.coef_g; g.target_g = L.target_g;
-                g.uniform = c.smoothing / static_cast<float>(V);
-                g.G = L.G; g.ldg = cv; g.g_wide_store = (reinterpret_cast<uintptr_t>(L.G) % 32 == 0) && cv % 16 == 0;
-                gemm_common(ctx, g, UNITY_PROF_GRAD_GEMM, &counters, (ctx->chunk_sync & 1) != 0);
-                {
+                if (!B.keep) {
+                    GemmArgs g;
+                    memset(&g, 0, sizeof(g));
+                    g.span = chunk; g.span_mode = kSpanRowsA;
+                    g.m_tiles = 1;                                   // set by the kernel
+                    g.n_tiles = (vc + kTileN - 1) / kTileN; g.k_iters = H / kTileK; g.group_m = 1;
+                    g.fwd.n_pairs = ctx->sm_count / c_grad; g.fwd.tile_rows = gemm_tile_rows(c_grad); g.fwd.n_tiles = g.n_tiles;
+                    g.fwd.max_splits = g.fwd.n_pairs;
+                    if (large_rounds_fit(ctx, H)) {
+                        g.fwd.gmax = ctx->sm_count / 2 / c_grad;
+                    } else {   // runs of column tiles, as many row tiles in flight as a 45 MB share of L2 holds
+                        int runs = static_cast<int>((45ll << 20) / (128ll * H * 2));
+                        runs = runs < 8 ? 8 : (runs > ctx->sm_count / 2 ? ctx->sm_count / 2 : runs);
+                        g.plan_runs = 1;
+                        g.fwd.gmax = runs / c_grad > 0 ? runs / c_grad : 1;
+                    }
+                    g.b_row0 = v0; g.n_cols = vc; g.target_p = L.target_p; g.vocab0 = v0; g.scale = r->inv_temperature;
+                    g.row_lse = L.row_lse; g.coef_p = L.coef_p; g.coef_g = L.coef_g; g.target_g = L.target_g;
+                    g.uniform = c.smoothing / static_cast<float>(V);
+                    g.G = L.G; g.ldg = B.cols; g.g_wide_store = B.cols % 16 == 0;
+                    gemm_common(ctx, g, UNITY_PROF_GRAD_GEMM, &counters, (ctx->chunk_sync & 1) != 0);
                     ProfScope ps(ctx, UNITY_PROF_GRAD_GEMM);
                     CUDA_TRY(ctx, launch_gemm(kEpiLossGrad, false, c_grad, tm_hp_k, tm_W_k, g, ctx->sm_count, st));
                     nl += 1;
                 }
                 if (c.n_top > 0) {
-                    const TeacherScatterArgs ts{chunk, L.ids_p, L.cnt_p, L.top_z, c.n_top, v0, vc, L.G, cv};
+                    const TeacherScatterArgs ts{chunk, L.ids_p, L.cnt_p, L.top_z, c.n_top, v0, vc, L.G, B.cols};
                     CUDA_TRY(ctx, launch_teacher_scatter(ts, st));
                     nl += 1;
                 }
                 CUtensorMap tm_G_k, tm_G_mn;
-                if ((rc = make_tmap(ctx, &tm_G_k, L.G, vc, nc, static_cast<uint64_t>(cv) * 2, kBoxRows))) return rc;
-                if ((rc = make_tmap(ctx, &tm_G_mn, L.G, vc, nc, static_cast<uint64_t>(cv) * 2, kTileK))) return rc;
+                if ((rc = make_tmap(ctx, &tm_G_k, L.G, vc, nc, static_cast<uint64_t>(B.cols) * 2, kBoxRows))) return rc;
+                if ((rc = make_tmap(ctx, &tm_G_mn, L.G, vc, nc, static_cast<uint64_t>(B.cols) * 2, kTileK))) return rc;
                 if (want_h) {
                     GemmArgs h;
                     memset(&h, 0, sizeof(h));
+                    const bool wide = two_blocks && c_dh == 2;
+                    const int cols = (wide ? 2 : 1) * mma_n;
                     h.mma_n = mma_n;
                     h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1;
-                    h.n_tiles = (H + mma_n - 1) / mma_n; h.k_iters = (vc + kTileK - 1) / kTileK;
+                    h.n_tiles = (H + cols - 1) / cols; h.k_iters = (vc + kTileK - 1) / kTileK;
+                    h.k_splits = B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0;
+                    h.fwd.n_pairs = ctx->sm_count / c_dh;
                     h.group_m = ctx->chunk_group[1] / c_dh > 0 ? ctx->chunk_group[1] / c_dh : 1;
-                    h.b_k0 = v0; h.n_cols = H; h.C = L.dHc; h.ldc = H; h.beta = v0 > 0;
+                    h.b_k0 = v0; h.n_cols = H; h.C = L.parts; h.ldc = H; h.beta = v0 > 0;
                     gemm_common(ctx, h, UNITY_PROF_DH_GEMM, &counters, (ctx->chunk_sync & 2) != 0);
-                    ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
-                    CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, false, c_dh, tm_G_k, tm_W_mn, h, ctx->sm_count, st));
-                    nl += 1;
+                    {
+                        ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
+                        CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, false, c_dh, tm_G_k, tm_W_mn, h, ctx->sm_count, st, wide));
+                        nl += 1;
+                    }
+                    if (ci + 1 == n_pieces) {
+                        const StoreArgs sa{L.parts, L.slot_tok, chunk, H, h.k_splits, h.n_tiles, h.k_iters, h.fwd.n_pairs,
+                                           gemm_tile_rows(c_dh), dH};
+                        CUDA_TRY(ctx, launch_store_parts(sa, st));
+                        nl += 1;
+                    }
                 }
                 if (want_w) {
                     GemmArgs w;
                     memset(&w, 0, sizeof(w));
-                    const int tile_v = gemm_tile_rows(c_dw);
+                    // few rows: a tile's epilogue must overlap the next tile's products, which only the narrow form does
+                    const bool wide = two_blocks && c_dw == 2 && nc > 1024;
+                    const int tile_v = gemm_tile_rows(c_dw), cols = (wide ? 2 : 1) * mma_n;
                     w.mma_n = mma_n;
                     w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = (vc + tile_v - 1) / tile_v;
-                    w.n_tiles = (H + mma_n - 1) / mma_n; w.k_iters = 1;
+                    w.n_tiles = (H + cols - 1) / cols; w.k_iters = 1;
                     w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
-                    w.m_rows = vc; w.n_cols = H; w.C = dWk + static_cast<long long>(v0) * H; w.ldc = H;
+                    w.m_rows = vc; w.n_cols = H; w.ldc = H;
+                    if (out16) {
+                        w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + static_cast<long long>(v0) * H;
+                        w.g_wide_store = reinterpret_cast<uintptr_t>(w.C16) % 32 == 0;
+                    } else {
+                        w.C = dWk + static_cast<long long>(v0) * H;
+                    }
                     w.beta = (add_dw || c0 > 0) ? 1 : 0;
                     gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0);
                     ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
-                    CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st));
+                    CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide));
                     nl += 1;
                 }
             }
-            if (want_h) { CUDA_TRY(ctx, launch_store_dhidden(L.dHc, L.slot_tok, chunk, H, dH, st)); nl += 1; }
         }
-        if (want_w && c.bf16_dw) {
+        if (want_w && B.dw_scratch) {
             CUDA_TRY(ctx, launch_cast_dw(dWk, static_cast<__nv_bfloat16*>(c.dW[k]), static_cast<long long>(V) * H, c.accumulate != 0, st));
             nl += 1;
         }
     }
+    CUDA_TRY(ctx, launch_loss_sum(la, st));
+    nl += 1;
     ctx->launches += nl;
     return UNITY_OK;
 }
@@ -1412,8 +1488,8 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
 // ------------------------------------------------------------------------------------------------
 size_t unity_token_loss_workspace_bytes(int64_t n_tok, int32_t H, int32_t V, int32_t K, int32_t n_top, int32_t backward) {
     if (n_tok < 0 || n_tok > 0x7fffff00LL || H <= 0 || V <= 0 || K <= 0 || n_top < 0 || n_top > UNITY_MAX_TOP) return 0;
-    return carve_loss(nullptr, ~size_t(0), n_tok, H, V, K, n_top, backward ? wanted_chunk_rows(n_tok, K, kDefaultChunkMult) : 0,
-                      wanted_chunk_vocab(V, kDefaultChunkMult), backward != 0, nullptr).bytes;
+    const LossBlocks B = backward ? keep_blocks(n_tok, V, true, kStashRows) : LossBlocks{0, 0, false, false};
+    return carve_loss(nullptr, ~size_t(0), n_tok, H, V, K, n_top, B, nullptr).bytes;
 }
 
 int unity_cross_entropy_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_ce_params* params,
