@@ -218,102 +218,143 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     return g;
 }
 
-// Where a row stands in its ascending list of entries.
-struct TopCursor {
-    int next, pos, cnt;   // next vocabulary index (INT_MAX: none left)
+// Token losses, forward: what one thread (= one row) carries through a sweep of column tiles.
+//   s = sum 2^((z - ref) c2), z2 = sum z (both as even / odd halves), the target's logit, and where the row stands in its
+//   ascending list of entries (next vocabulary index, INT_MAX: none left).
+// ref need not be the maximum: it is the maximum of the first tile, and later a tile's that lies more than kRefRoom octaves
+// above it.  So a tile is read from tensor memory once (a maximum first and the sum after it would read it twice: 276
+// against 353 us at 801 x 896 x 151936, where the epilogue is the bound), no sum exceeds 2^kRefRoom * V, and for a backward
+// pass that does not recompute the logits (ref - z) + kRefRoom octaves is kept in steps of 2^-10 octaves, 16 bits.  The integer
+// costs as much memory as bf16 but is off by at most half a step whatever its size: p is off by a factor of 2^(2^-11), 3.4e-4,
+// where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 48 octaves or more below ref count as 48.
+struct LossRow {
+    float ref, z_tgt;
+    uint64_t s, z2;
+    int tgt;
+    int next, pos, cnt;
     long long base;
 };
+// Launch constants, in registers: the resolved GemmArgs live in local memory.
+struct LossConsts {
+    float c2;
+    int n_cols, n_tiles;
+    const int* top_ids;
+    float *top_z, *tile_max;
+    uint16_t* stash;
+    long long ldz;
+};
 
-// Token losses, forward: one 256-column accumulator tile of one row (thread = row).  Two passes over tensor memory: the
-// tile's maximum first, so that the running sum is rescaled once per tile and everything below is relative to one
-// reference m (the row's running maximum including this tile):
-//   s += sum 2^((z - m) c2), z += sum z, the target's logit, the listed entries' logits, and, for a backward pass that does
-//   not recompute the logits, (m - z) in steps of 2^-10 octaves as 16-bit integers.
-// The integer costs as much memory as bf16 but is off by at most half a step whatever its size: p is off by a factor of
-// 2^(2^-11), 3.4e-4, where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries further than 64
-// octaves below m count as 64 (a probability below 2^-64 of the largest).  Sums of 32 columns are formed apart and then
-// added: V additions one after the other would cost log s three digits.
-__device__ __forceinline__ void loss_stats_tile(const GemmArgs& g, uint32_t taddr, int col0, int nt, int row, bool row_ok,
-                                                int tgt, float c2, float& run_m, uint64_t& run_s2, uint64_t& run_z2,
-                                                float& z_tgt, TopCursor& top) {
-    const int n_tile = min(kTileN, g.n_cols - col0);
-    float tm = kNegBig;
-#pragma unroll 1
-    for (int c = 0; c * 32 < n_tile; ++c) {
-        uint32_t rr[32];
-        ptx::tmem_ld_32x32(taddr + c * 32, rr);
-        ptx::tmem_ld_wait();
-        const int n_here = n_tile - c * 32;
-        float v[32];
+// 32 columns; returns their maximum.  TAIL: the vocabulary ends inside (V is a multiple of 8: on a pair).
+template <bool STASH, bool TAIL>
+__device__ __forceinline__ float loss_chunk(const LossConsts& k, LossRow& w, const uint32_t (&rr)[32], int n_here,
+                                            uint64_t& s2, uint64_t& z2, unsigned (&packed)[16]) {
+    const uint64_t m2 = ptx::pack2(-w.ref, -w.ref), c22 = ptx::pack2(k.c2, k.c2);
+    const float steps = -k.c2 * kStashSteps;
+    // adding 2^23 leaves the rounded integer in the low bits
+    const uint64_t steps2 = ptx::pack2(steps, steps), magic2 = ptx::pack2(8388608.f + kRefRoom * kStashSteps, 8388608.f + kRefRoom * kStashSteps);
+    float cm = kNegBig;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = j < n_here ? __uint_as_float(rr[j]) : kNegBig;
-        float cm = ptx::max3(v[0], v[1], v[2]);
-#pragma unroll
-        for (int j = 3; j < 31; j += 2) cm = ptx::max3(cm, v[j], v[j + 1]);
-        tm = ptx::max3(tm, cm, v[31]);
-    }
-    const float m = fmaxf(run_m, tm);
-    const float resc = ptx::ex2((run_m - m) * c2);
-    run_s2 = ptx::mul2(run_s2, ptx::pack2(resc, resc));
-    run_m = m;
-    if (g.tile_max != nullptr && row_ok) g.tile_max[static_cast<long long>(row) * g.n_tiles + nt] = m;
-    const uint64_t m2 = ptx::pack2(-m, -m), c22 = ptx::pack2(c2, c2);
-    const float steps = -c2 * kStashSteps;
-    const uint64_t steps2 = ptx::pack2(steps, steps), magic2 = ptx::pack2(8388608.f, 8388608.f);
-#pragma unroll 1
-    for (int c = 0; c * 32 < n_tile; ++c) {
-        const int cbase = col0 + c * 32, n_here = n_tile - c * 32;
-        uint32_t rr[32];
-        ptx::tmem_ld_32x32(taddr + c * 32, rr);
-        ptx::tmem_ld_wait();
-        uint64_t s2 = 0ull, z2 = 0ull;
-        unsigned packed[16];
-#pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            if (j < n_here) {                                  // V is a multiple of 8: whole pairs
-                const uint64_t x = ptx::pack2(__uint_as_float(rr[j]), __uint_as_float(rr[j + 1]));
-                const uint64_t d = ptx::add2(x, m2);
-                float a0, a1, t0, t1;
-                ptx::unpack2(ptx::mul2(d, c22), a0, a1);
-                s2 = ptx::add2(s2, ptx::pack2(ptx::ex2(a0), ptx::ex2(a1)));
-                z2 = ptx::add2(z2, x);
-                // adding 2^23 leaves the rounded integer in the low bits
+    for (int j = 0; j < 32; j += 2) {
+        if (!TAIL || j < n_here) {
+            const float v0 = __uint_as_float(rr[j]), v1 = __uint_as_float(rr[j + 1]);
+            const uint64_t x = ptx::pack2(v0, v1);
+            const uint64_t d = ptx::add2(x, m2);
+            float a0, a1;
+            ptx::unpack2(ptx::mul2(d, c22), a0, a1);
+            cm = ptx::max3(cm, v0, v1);
+            s2 = ptx::add2(s2, ptx::pack2(ptx::ex2(a0), ptx::ex2(a1)));
+            z2 = ptx::add2(z2, x);
+            if (STASH) {
+                float t0, t1;
                 ptx::unpack2(ptx::fma2(d, steps2, magic2), t0, t1);
+                // (a logit above the room makes the tile start again, so only the far end is cut off)
                 packed[j >> 1] = __byte_perm(__float_as_uint(fminf(t0, 8388608.f + 65535.f)),
                                              __float_as_uint(fminf(t1, 8388608.f + 65535.f)), 0x5410);
             }
-        }
-        run_s2 = ptx::add2(run_s2, s2);
-        run_z2 = ptx::add2(run_z2, z2);
-        const int jt = tgt - cbase;
-        if (jt >= 0 && jt < 32) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) if (j == jt) z_tgt = __uint_as_float(rr[j]);
-        }
-        while (top.next < cbase + 32) {                       // listed entries among these columns
-            const int jn = top.next - cbase;
-            float z = 0.f;
-#pragma unroll
-            for (int j = 0; j < 32; ++j) if (j == jn) z = __uint_as_float(rr[j]);
-            g.top_z[top.base + top.pos] = z;
-            ++top.pos;
-            top.next = top.pos < top.cnt ? g.top_ids[top.base + top.pos] : 0x7fffffff;
-        }
-        if (g.stash != nullptr && row_ok) {
-            uint16_t* dst = g.stash + static_cast<long long>(row) * g.ldz + cbase;      // pitch and base 32-byte aligned
-            if (n_here >= 32) {
-                ptx::st_global_v8(dst, packed[0], packed[1], packed[2], packed[3], packed[4], packed[5], packed[6], packed[7]);
-                ptx::st_global_v8(dst + 16, packed[8], packed[9], packed[10], packed[11], packed[12], packed[13], packed[14], packed[15]);
-            } else {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (q * 8 < n_here)
-                        *reinterpret_cast<uint4*>(dst + q * 8) =
-                            make_uint4(packed[4 * q], packed[4 * q + 1], packed[4 * q + 2], packed[4 * q + 3]);
-                }
-            }
+        } else {
+            packed[j >> 1] = 0u;
         }
     }
+    return cm;
+}
+
+// One 256-column accumulator tile.  The loads of the next 32 columns are under way while these are worked on: one warp
+// per SM quarter has nothing else to hide their latency behind.
+template <bool STASH>
+__device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w, uint32_t taddr, int col0, int nt, int row,
+                                                bool row_ok) {
+    const int n_tile = min(kTileN, k.n_cols - col0);
+    for (int attempt = 0; ; ++attempt) {
+        uint64_t s2 = 0ull, z2 = 0ull;
+        float tm = kNegBig;
+        uint32_t ra[32], rb[32];
+        ptx::tmem_ld_32x32(taddr, ra);
+        auto work = [&](const uint32_t (&rr)[32], int c) {
+            const int cbase = col0 + c * 32, n_here = n_tile - c * 32;
+            unsigned packed[16];
+            // sums of 32 columns are formed apart and then added: V additions one after the other would cost log s digits
+            uint64_t cs = 0ull, cz = 0ull;
+            const float cm = n_here >= 32 ? loss_chunk<STASH, false>(k, w, rr, n_here, cs, cz, packed)
+                                          : loss_chunk<STASH, true>(k, w, rr, n_here, cs, cz, packed);
+            tm = fmaxf(tm, cm);
+            s2 = ptx::add2(s2, cs);
+            z2 = ptx::add2(z2, cz);
+            const int jt = w.tgt - cbase;
+            if (jt >= 0 && jt < 32) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) if (j == jt) w.z_tgt = __uint_as_float(rr[j]);
+            }
+            while (w.next < cbase + 32) {                     // listed entries among these columns
+                const int jn = w.next - cbase;
+                float z = 0.f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) if (j == jn) z = __uint_as_float(rr[j]);
+                k.top_z[w.base + w.pos] = z;
+                ++w.pos;
+                w.next = w.pos < w.cnt ? k.top_ids[w.base + w.pos] : 0x7fffffff;
+            }
+            if (STASH && row_ok) {
+                uint16_t* dst = k.stash + static_cast<long long>(row) * k.ldz + cbase;      // pitch and base 32-byte aligned
+                if (n_here >= 32) {
+                    ptx::st_global_v8(dst, packed[0], packed[1], packed[2], packed[3], packed[4], packed[5], packed[6], packed[7]);
+                    ptx::st_global_v8(dst + 16, packed[8], packed[9], packed[10], packed[11], packed[12], packed[13], packed[14], packed[15]);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (q * 8 < n_here)
+                            *reinterpret_cast<uint4*>(dst + q * 8) =
+                                make_uint4(packed[4 * q], packed[4 * q + 1], packed[4 * q + 2], packed[4 * q + 3]);
+                    }
+                }
+            }
+        };
+#pragma unroll 1
+        for (int c = 0; c * 32 < n_tile; c += 2) {
+            const bool more = (c + 1) * 32 < n_tile;
+            ptx::tmem_ld_wait_for(ra);
+            if (more) ptx::tmem_ld_32x32(taddr + (c + 1) * 32, rb);
+            work(ra, c);
+            if (!more) break;
+            ptx::tmem_ld_wait_for(rb);
+            if ((c + 2) * 32 < n_tile) ptx::tmem_ld_32x32(taddr + (c + 2) * 32, ra);
+            work(rb, c + 1);
+        }
+        // A row whose maximum rose past the room takes it as its new reference and its warp works through the tile again
+        // (the list cursor has moved on: its logits are written; the target's is the same).  A second time is enough.
+        const bool over = (tm - w.ref) * k.c2 > kRefRoom;
+        if (attempt == 0 && __any_sync(0xffffffffu, over)) {
+            if (over) {
+                const float resc = ptx::ex2((w.ref - tm) * k.c2);
+                w.s = ptx::mul2(w.s, ptx::pack2(resc, resc));
+                w.ref = tm;
+            }
+            continue;
+        }
+        w.s = ptx::add2(w.s, s2);
+        w.z2 = ptx::add2(w.z2, z2);
+        break;
+    }
+    if (STASH && row_ok) k.tile_max[static_cast<long long>(row) * k.n_tiles + nt] = w.ref;
 }
 
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
@@ -554,19 +595,20 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 lu = g.coef_g[g.a_row0 + row] * g.uniform;
                 lt = g.target_g[g.a_row0 + row];
             }
-            // ... the row's listed entries: the next one at or after this unit's first column
-            TopCursor top{0x7fffffff, 0, 0, 0};
+            // ... and the forward's row state: the reference starts below everything, the list at this unit's first column
+            const LossConsts lk{c2, g.n_cols, g.n_tiles, g.top_ids, g.top_z, g.tile_max, g.stash, g.ldz};
+            LossRow lr{kNegBig, kNegBig, 0ull, 0ull, tgt, 0x7fffffff, 0, 0, 0};
             if (EPI == kEpiLossStats && g.top_ids != nullptr && row_ok) {
-                top.base = static_cast<long long>(g.a_row0 + row) * g.top_n;
-                top.cnt = g.top_cnt[g.a_row0 + row];
+                lr.base = static_cast<long long>(g.a_row0 + row) * g.top_n;
+                lr.cnt = g.top_cnt[g.a_row0 + row];
                 const int first = t.n_begin * kTileN;
-                int lo = 0, hi = top.cnt;
+                int lo = 0, hi = lr.cnt;
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
-                    if (g.top_ids[top.base + mid] < first) lo = mid + 1; else hi = mid;
+                    if (g.top_ids[lr.base + mid] < first) lo = mid + 1; else hi = mid;
                 }
-                top.pos = lo;
-                if (top.pos < top.cnt) top.next = g.top_ids[top.base + top.pos];
+                lr.pos = lo;
+                if (lr.pos < lr.cnt) lr.next = g.top_ids[lr.base + lr.pos];
             }
 
             for (int ni = t.n_begin; ni < t.n_end && ok; ++ni) {
@@ -578,7 +620,8 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 const int col0 = nt * (NB * mma_n);
                 const int per_block = mma_n / 32;
                 if (EPI == kEpiLossStats) {
-                    loss_stats_tile(g, taddr, col0, nt, row, row_ok, tgt, c2, run_m, run_s2, run_t2, z_tgt, top);
+                    if (lk.stash != nullptr) loss_stats_tile<true>(lk, lr, taddr, col0, nt, row, row_ok);
+                    else loss_stats_tile<false>(lk, lr, taddr, col0, nt, row, row_ok);
                 }
 #pragma unroll 1
                 for (int c = 0; c < (EPI == kEpiLossStats ? 0 : NB * per_block); ++c) {
@@ -804,6 +847,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
             }
             if (is_stats(EPI) && ok && row_ok) {
                 float s0, s1, t0, t1;
+                if (EPI == kEpiLossStats) { run_m = lr.ref; run_s2 = lr.s; run_t2 = lr.z2; z_tgt = lr.z_tgt; }
                 ptx::unpack2(run_s2, s0, s1);
                 ptx::unpack2(run_t2, t0, t1);
                 const long long at = t.m_tile >= g.last_m0

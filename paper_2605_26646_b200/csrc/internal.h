@@ -128,7 +128,8 @@ __host__ __device__ inline SplitShape split_shape(int most, int m_tiles, int n_t
     return best;
 }
 constexpr int kMaxKSplits = 32;
-constexpr float kStashSteps = 1024.f;   // steps per octave of a kept logit (GemmArgs::stash)
+constexpr float kStashSteps = 1024.f;   // steps per octave of a kept logit (GemmArgs::stash) ...
+constexpr float kRefRoom = 16.f;        // ... counted down from this many octaves above its reference
 
 // ----------------------------------------------------------------------------------------------
 // GEMM  C[m, n] = sum_k A[m, k] * B[n, k]   (bf16 operands, K-major or MN-major, fp32 accumulation in TMEM)
@@ -187,9 +188,9 @@ struct GemmArgs {
     const int* top_cnt;       // [rows]
     float* top_z;             // out [rows, top_n]
     int top_n;
-    uint16_t* stash;          // optional, a block of rows: (running maximum - logit) in steps of 1 / kStashSteps octaves,
-                              // row pitch ldz ...
-    float* tile_max;          // ... and the running maximum each column tile refers to [rows, n_tiles], accumulator units
+    uint16_t* stash;          // optional, a block of rows: kRefRoom octaves above the reference, minus the logit, in steps of
+                              // 1 / kStashSteps octaves, row pitch ldz ...
+    float* tile_max;          // ... and the reference of each column tile [rows, n_tiles], accumulator units
     // kEpiLossGrad: G = coef_p * p - coef_g * uniform, and target_g at the target (row_lse as above)
     const float* coef_p;      // [rows] dL/dz_v per unit of p_v, times scale
     const float* coef_g;      // [rows] scale * weight / M
@@ -434,7 +435,7 @@ struct TeacherScatterArgs {
 };
 cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream);
 // In place, the kept logits of a block of rows (GemmArgs::stash) become dL/dz in bf16: coef_p * p - coef_g * uniform, and
-// target_g at the target, with p = 2^(tile_max * c2 - lse log2(e) - u / kStashSteps).
+// target_g at the target, with p = 2^(tile_max * c2 + kRefRoom - lse log2(e) - u / kStashSteps).
 struct LossGradArgs {
     uint16_t* Z;
     long long ld;

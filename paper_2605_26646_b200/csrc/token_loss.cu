@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(256) k_teacher_scatter(TeacherScatterArgs a) {
 }
 
 // A block converts 8192 columns of a row: each thread issues four 128-bit loads 4 KiB apart, so a warp's access is the 256
-// columns of one tile of the forward GEMM and has one reference maximum.  2 B read and 2 B written per logit.
+// columns of one tile of the forward GEMM and has one reference.  2 B read and 2 B written per logit.
 constexpr int kGradVecs = 4;
 __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
     const int c_first = blockIdx.x * (256 * 8 * kGradVecs) + threadIdx.x * 8;
@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
             const int c0 = c_first + u * 2048;
             if (c0 < a.cols) { raw[u] = row[c0 >> 3]; shift[u] = tm[c0 / kTileN]; }
         }
-        const float base = -a.row_lse[slot] * 1.4426950408889634f;
+        const float base = kRefRoom - a.row_lse[slot] * 1.4426950408889634f;
         const float cp = a.coef_p[slot], cu = a.coef_g[slot] * a.uniform, gt = a.target_g[slot];
         const int tgt = a.target_p[slot];
 #pragma unroll
