@@ -161,7 +161,8 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     int slot0, n_rows;
     span_resolve(in.span, slot0, n_rows);
     if (in.span_mode == kSpanForward) {
-        const FwdShape fs = forward_shape(in.fwd, n_rows);
+        const FwdShape fs = in.shapes ? in.shapes->fwd[in.span.model][n_rows == in.span.row_cap ? 0 : 1]
+                                      : forward_shape(in.fwd, n_rows);
         g.a_row0 = slot0;
         g.m_rows = n_rows;
         g.m_tiles = n_rows / TILE_ROWS;
@@ -206,8 +207,8 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     } else if (in.span_mode == kSpanRowsM) {
         g.m_rows = n_rows;
         g.m_tiles = n_rows / TILE_ROWS;
-        if (in.k_splits != 0) {
-            const SplitShape sp = split_shape(in.k_splits, g.m_tiles, g.n_tiles, g.k_iters, in.fwd.n_pairs);
+        if (in.shapes) {
+            const SplitShape sp = in.shapes->dh[in.span.model][n_rows == in.span.row_cap ? 0 : 1];
             g.k_splits = sp.splits; g.k_per_split = sp.per_split;
             g.c_split = static_cast<long long>(n_rows) * in.ldc;
         }
@@ -364,6 +365,13 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     // The row extent of a launch may be known on the device only: derive it from the plan before anything else.  Every
     // thread of both CTAs reads the same plan, so a launch whose span is empty is left by all of them, here.
     const GemmArgs g = resolve_span<C::kTileRows>(g_in);
+    if (EPI == kEpiAccumF32 && g.zero_if_empty && g.k_iters <= 0) {
+        const long long n16 = static_cast<long long>(g.m_rows) * g.ldc / (g.C16 ? 8 : 4);      // 16-byte units, whole ones
+        uint4* out = g.C16 ? reinterpret_cast<uint4*>(g.C16) : reinterpret_cast<uint4*>(g.C);
+        for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < n16; i += static_cast<long long>(gridDim.x) * kThreads)
+            out[i] = make_uint4(0, 0, 0, 0);
+        return;
+    }
     if (g.m_tiles <= 0 || g.n_tiles <= 0 || g.k_iters <= 0) return;
     if (g.n_active > 0 && (CTAS == 2 ? blockIdx.x >> 1 : blockIdx.x) >= g.n_active) return;   // never holds a unit
     constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes, kABytes = C::kABytes, kBBytes = C::kBBytes;

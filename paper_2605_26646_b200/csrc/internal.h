@@ -63,71 +63,81 @@ struct FwdPlanParams {
     int n_tiles;     // vocabulary tiles of 256
     int max_splits;  // most vocabulary splits of a round (32 for stages 2 and 3; the token losses let few rows use all workers)
 };
+// One candidate: rounds of `cand` row tiles.  Returns its cost, work per worker in vocabulary tiles: tiles per split, summed
+// over the rounds, the last of which may hold fewer row tiles and then cuts the vocabulary into more splits (a batch whose
+// row tiles do not divide well would otherwise idle part of the machine in its last round).
+__host__ __device__ inline long long forward_candidate(const FwdPlanParams& p, int m_tiles, int cand, FwdShape& f) {
+    const int c = cand < m_tiles ? cand : (m_tiles > 0 ? m_tiles : 1);
+    int sp = p.n_pairs / c;
+    sp = sp > p.max_splits ? p.max_splits : sp;
+    sp = sp > p.n_tiles ? p.n_tiles : sp;
+    sp = sp < 1 ? 1 : sp;
+    // several rounds: at most 4 splits, which bounds the statistics a launch writes by 4 per row (plus the short last
+    // round's, at most one per worker and tile row); only a round size far below the default runs into this
+    if (c < m_tiles && sp > 4) sp = 4;
+    const int full_rounds = m_tiles / c, rest = m_tiles - full_rounds * c;
+    int sp_last = sp;
+    if (rest > 0) {
+        sp_last = p.n_pairs / rest;
+        sp_last = sp_last > p.max_splits ? p.max_splits : sp_last;
+        sp_last = sp_last > p.n_tiles ? p.n_tiles : sp_last;
+        sp_last = sp_last < 1 ? 1 : sp_last;
+    }
+    f.gm = c;
+    f.tps = (p.n_tiles + sp - 1) / sp;
+    f.splits = (p.n_tiles + f.tps - 1) / f.tps;
+    f.last_m0 = rest > 0 && sp_last != sp ? full_rounds * c : m_tiles;
+    f.last_tps = (p.n_tiles + sp_last - 1) / sp_last;
+    f.last_splits = (p.n_tiles + f.last_tps - 1) / f.last_tps;
+    return static_cast<long long>(full_rounds) * f.tps + (rest > 0 ? f.last_tps : 0);
+}
+__host__ __device__ inline int forward_cand_min(const FwdPlanParams& p, int m_tiles) {
+    return m_tiles <= p.gmax ? 1 : (2 * p.gmax + 2) / 3;      // few row tiles: any round size is L2-safe
+}
+__host__ __device__ inline void forward_finish(const FwdPlanParams& p, int rows, int m_tiles, FwdShape& f) {
+    const long long last_rows = static_cast<long long>(m_tiles - f.last_m0) * p.tile_rows;
+    f.stats_rows = static_cast<long long>(f.splits) * rows + f.last_splits * last_rows;
+}
 __host__ __device__ inline FwdShape forward_shape(const FwdPlanParams& p, int rows) {
     const int m_tiles = rows / p.tile_rows;
-    // Among round sizes from two thirds of gmax up to gmax, take the one with the least work per worker: vocabulary
-    // tiles per split, summed over the rounds, the last of which may hold fewer row tiles and then cuts the vocabulary
-    // into more splits (a batch whose row tiles do not divide well would otherwise idle part of the machine in its
-    // last round); ties go to the larger round, which streams W less often.
-    FwdShape best;
+    // Among round sizes from two thirds of gmax up to gmax, take the cheapest; ties go to the larger round, which streams
+    // W less often.
+    FwdShape best, f;
     best.gm = 1; best.splits = 1; best.tps = p.n_tiles; best.last_m0 = m_tiles; best.last_splits = 1; best.last_tps = p.n_tiles;
     long long best_cost = -1;
-    const int cand_min = m_tiles <= p.gmax ? 1 : (2 * p.gmax + 2) / 3;      // few row tiles: any round size is L2-safe
-    for (int cand = p.gmax; cand >= cand_min; --cand) {
-        const int c = cand < m_tiles ? cand : (m_tiles > 0 ? m_tiles : 1);
-        int sp = p.n_pairs / c;
-        sp = sp > p.max_splits ? p.max_splits : sp;
-        sp = sp > p.n_tiles ? p.n_tiles : sp;
-        sp = sp < 1 ? 1 : sp;
-        // several rounds: at most 4 splits, which bounds the statistics a launch writes by 4 per row (plus the short last
-        // round's, at most one per worker and tile row); only a round size far below the default runs into this
-        if (c < m_tiles && sp > 4) sp = 4;
-        const int full_rounds = m_tiles / c, rest = m_tiles - full_rounds * c;
-        int sp_last = sp;
-        if (rest > 0) {
-            sp_last = p.n_pairs / rest;
-            sp_last = sp_last > p.max_splits ? p.max_splits : sp_last;
-            sp_last = sp_last > p.n_tiles ? p.n_tiles : sp_last;
-            sp_last = sp_last < 1 ? 1 : sp_last;
-        }
-        const long long cost = static_cast<long long>(full_rounds) * ((p.n_tiles + sp - 1) / sp) +
-                               (rest > 0 ? (p.n_tiles + sp_last - 1) / sp_last : 0);
-        if (best_cost < 0 || cost < best_cost) {
-            best_cost = cost;
-            best.gm = c;
-            best.tps = (p.n_tiles + sp - 1) / sp;
-            best.splits = (p.n_tiles + best.tps - 1) / best.tps;
-            best.last_m0 = rest > 0 && sp_last != sp ? full_rounds * c : m_tiles;
-            best.last_tps = (p.n_tiles + sp_last - 1) / sp_last;
-            best.last_splits = (p.n_tiles + best.last_tps - 1) / best.last_tps;
-        }
+    for (int cand = p.gmax; cand >= forward_cand_min(p, m_tiles); --cand) {
+        const long long cost = forward_candidate(p, m_tiles, cand, f);
+        if (best_cost < 0 || cost < best_cost) { best_cost = cost; best = f; }
     }
-    const long long last_rows = static_cast<long long>(m_tiles - best.last_m0) * p.tile_rows;
-    best.stats_rows = static_cast<long long>(best.splits) * rows + best.last_splits * last_rows;
+    forward_finish(p, rows, m_tiles, best);
     return best;
 }
 
 // Parts a contraction of k_iters slabs is cut into when its m_tiles x n_tiles outputs alone do not fill the workers (few
 // rows): the count with the least time, a worker's longest run of slabs plus, per part, the pipeline's fill and its
-// unoverlapped epilogue (kSplitOverhead slabs).  Computed alike by the GEMM, by the kernel that adds the parts up, and by
-// the host for the size of their buffer.
+// unoverlapped epilogue (kSplitOverhead slabs).
 constexpr int kSplitOverhead = 10;
 constexpr int kSplitWaves = 6;          // no more parts than make up 6 waves of workers: bounds their buffer
 struct SplitShape { int splits, per_split; };
-__host__ __device__ inline SplitShape split_shape(int most, int m_tiles, int n_tiles, int k_iters, int workers) {
-    SplitShape best{1, k_iters};
-    long long best_cost = -1;
-    const int cap = k_iters / 8 < most ? k_iters / 8 : most;      // a part has at least 8 slabs
-    for (int s = 1; s <= (cap > 1 ? cap : 1); ++s) {
-        if (s > 1 && static_cast<long long>(m_tiles) * n_tiles * s > static_cast<long long>(kSplitWaves) * workers) break;
-        const int per = (k_iters + s - 1) / s, n = per > 0 ? (k_iters + per - 1) / per : 1;
-        const long long waves = (static_cast<long long>(m_tiles) * n_tiles * n + workers - 1) / workers;
-        const long long cost = waves * (per + kSplitOverhead) + (s > 1 ? s : 0);
-        if (best_cost < 0 || cost < best_cost) { best_cost = cost; best.splits = n; best.per_split = per; }
-    }
-    return best;
+struct SplitParams { int most, n_tiles, k_iters, workers, tile_rows; };   // most = 0: never cut
+__host__ __device__ inline long long split_candidate(const SplitParams& p, int m_tiles, int s, SplitShape& f) {
+    f.per_split = (p.k_iters + s - 1) / s;
+    f.splits = (p.k_iters + f.per_split - 1) / f.per_split;
+    const long long units = static_cast<long long>(m_tiles) * p.n_tiles * f.splits, waves = (units + p.workers - 1) / p.workers;
+    return waves * (f.per_split + kSplitOverhead) + (s > 1 ? s : 0);
+}
+__host__ __device__ inline bool split_allowed(const SplitParams& p, int m_tiles, int s) {   // a part has at least 8 slabs
+    return s == 1 || (s <= p.most && s <= p.k_iters / 8 && static_cast<long long>(m_tiles) * p.n_tiles * s <= kSplitWaves * p.workers);
 }
 constexpr int kMaxKSplits = 32;
+
+// The schedules of a token loss, per model: [0] of a full block of rows (RowSpan::row_cap of them), [1] of the model's last
+// one.  Written once per call by the kernel that counts the rows (a warp weighs the candidates side by side; evaluated where
+// they are used they cost every launch several microseconds).
+struct LossShapes {
+    FwdShape fwd[UNITY_MAX_MODELS][2];
+    SplitShape dh[UNITY_MAX_MODELS][2];
+};
 constexpr float kStashSteps = 1024.f;   // steps per octave of a kept logit (GemmArgs::stash) ...
 constexpr float kRefRoom = 16.f;        // ... counted down from this many octaves above its reference
 
@@ -201,8 +211,8 @@ struct GemmArgs {
     __nv_bfloat16* C16;       // not null: the output is bf16, here (row pitch ldc), and C is unused
     long long ldc;
     int k_splits, k_per_split;   // the contraction is cut into k_splits parts of k_per_split slabs, each with an output of
-    long long c_split;           // its own, c_split values apart (0 or 1: not cut).  Before the kernel resolves its span (rows
-                                 // known on the device only), k_splits is the most parts split_shape may choose
+    long long c_split;           // its own, c_split values apart (0 or 1: not cut)
+    int zero_if_empty;           // a launch whose contraction has no rows writes zeros to its m_rows x ldc outputs
     int beta;                 // 0: overwrite, 1: add to C
     int mma_n;                // columns per MMA block, a multiple of 32 up to 256 (a tile is 1 or 2 blocks wide); 256
                               // unless the output's width divides better (896 columns = 4 blocks of 224)
@@ -218,6 +228,7 @@ struct GemmArgs {
     int span_mode;
     int stats_from_plan;
     FwdPlanParams fwd;
+    const LossShapes* shapes; // token losses: schedules written by the counting kernel (null: worked out here)
     long long wait_budget;    // SM clocks after which an mbarrier wait gives up (kStatusTimeout)
     int test_drop_slab;       // test hook: the TMA producer of every worker leaves out one K slab of its first tile
                               // (neither the expected-bytes arrival nor the loads), so the waits behind it run out
@@ -383,11 +394,33 @@ cudaError_t launch_value_loss(const ValueArgs& a, cudaStream_t stream, int* n_la
 // ----------------------------------------------------------------------------------------------
 // token losses (token_loss.cu)
 // ----------------------------------------------------------------------------------------------
-struct TeacherArgs {
+// Routing of a token loss with everything the later launches need: tokens to packed slots, the plan, the schedules, zeros for
+// masked tokens' outputs and for the call's counters.  Up to kLossRouteTokens tokens it is one launch of one block.
+constexpr int kLossRouteTokens = 8192;
+constexpr int kLossCounters = 1024;
+struct LossRouteArgs {
+    RouteArgs route;           // fwd: the forward planner's inputs
+    SplitParams split;         // of dHidden's GEMM
+    int block_rows;            // rows of a full block (at least a batch's rows: one block)
+    long long max_slots;
+    LossShapes* shapes;
+    unsigned* counters;        // [kLossCounters]
+    float *tok_loss, *lse;     // caller order, nullable
+};
+cudaError_t launch_loss_route(const LossRouteArgs& a, cudaStream_t stream, int* n_launches);
+
+// Packs the hidden rows and targets, turns the teacher's lists into ascending distinct entries with their probabilities and
+// zeroes the masked tokens' rows of dHidden.
+struct LossGatherArgs {
     const DevPlan* plan;
-    const int* slot_tok;
-    int K, V, n_top;
-    int logits;                // 1: softmax of the listed logits (times scale); 0: exp of listed log-probabilities
+    const int *slot_tok, *tok_slot;
+    int K, V, H;
+    long long n_tok, max_slots;
+    const __nv_bfloat16* hidden;
+    const int* target;         // nullable
+    __nv_bfloat16 *hp, *dHidden;   // dHidden nullable
+    int* target_p;
+    int n_top, logits;         // logits 1: softmax of the listed logits (times scale); 0: exp of listed log-probabilities
     float scale;
     const int* top_ids;        // caller order [n_tok, n_top]
     const float* top_vals;
@@ -395,12 +428,14 @@ struct TeacherArgs {
     float* q_p;                // packed [slots, n_top]
     int* status;
 };
-cudaError_t launch_teacher_lists(const TeacherArgs& a, long long max_slots, cudaStream_t stream);
+cudaError_t launch_loss_gather(const LossGatherArgs& a, cudaStream_t stream);
 
 struct LossRowArgs {
-    RowSpan block;             // as in TokenArgs: one block of one model's rows, or (block.model < 0) every packed row
+    RowSpan block;             // one block of one model's rows, or (block.model < 0) up to row_cap rows of every model
     const DevPlan* plan;
-    FwdPlanParams fwd;
+    const LossShapes* shapes;
+    int tile_rows;             // of the forward GEMM
+    unsigned* ticket;          // this launch's counter, zero before it
     long long max_slots;
     int K, V;
     const float4* stats;       // (max, sum exp, sum z, target logit) per split, accumulator units
@@ -423,7 +458,6 @@ struct LossRowArgs {
     float* loss;               // [K]
 };
 cudaError_t launch_loss_rows(const LossRowArgs& a, cudaStream_t stream);
-cudaError_t launch_loss_sum(const LossRowArgs& a, cudaStream_t stream);
 
 struct TeacherScatterArgs {
     RowSpan span;
@@ -446,14 +480,18 @@ struct LossGradArgs {
     const int* target_p;
     const float *row_lse, *coef_p, *coef_g, *target_g;
     float uniform;
+    int n_top;                 // the listed entries' gradients go in last (0: none)
+    const int *ids_p, *cnt_p;
+    const float* top_g;
 };
-cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, cudaStream_t stream);
-// dHidden[token of slot r of the span] = bf16(sum of the row's k_splits parts), in the order of the parts
+cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream);
+// dHidden[token of slot r of the span] = bf16(sum of the row's parts), in the order of the parts
 struct StoreArgs {
-    const float* parts;        // [splits][rows of the span][H]
+    const float* parts;        // [parts][rows of the span][H]
     const int* slot_tok;
     RowSpan span;
-    int H, most, n_tiles, k_iters, workers, tile_rows;   // what split_shape was given
+    int H;
+    const LossShapes* shapes;  // null: one part
     __nv_bfloat16* dHidden;
 };
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream);

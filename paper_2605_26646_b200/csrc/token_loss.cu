@@ -1,5 +1,6 @@
-// Streaming kernels of the token losses (unity_cross_entropy_fwd_bwd, unity_distill_fwd_bwd): the teacher's lists, the
-// per-row losses and gradient coefficients, the loss sums, the listed entries' gradients and the cast of dW.
+// Streaming kernels of the token losses (unity_cross_entropy_fwd_bwd, unity_distill_fwd_bwd): routing, packing with the
+// teacher's lists, the per-row losses and gradient coefficients with their sums, the kept logits' conversion to gradients,
+// and the outputs' last sums and roundings.
 // Every sum has a fixed order and every output one writer: results are bitwise reproducible.
 #include "internal.h"
 
@@ -22,21 +23,177 @@ __device__ __forceinline__ float warp_max(float v) {
     return v;
 }
 
-// One warp per packed row: the row's listed entries become ascending, distinct vocabulary indexes with their teacher
-// probabilities q.  Entries with a negative id are empty places, an id >= V is reported and counts as one, and so do
-// entries of probability zero (a logit of -inf); equal ids add up in list order.  With at most 128 entries a rank by
-// counting (each entry is compared with all others, which sit in shared memory) needs no sorting network.
-__global__ void __launch_bounds__(256) k_teacher_lists(TeacherArgs a) {
-    __shared__ int sh_id[8][kMaxTop];
-    __shared__ float sh_q[8][kMaxTop];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long long slot = static_cast<long long>(blockIdx.x) * 8 + warp;
-    if (slot >= a.plan->off[a.K]) return;                       // whole warps leave: only warp-wide barriers below
-    const int tok = a.slot_tok[slot];
-    if (tok < 0) {
-        if (lane == 0) a.cnt_p[slot] = 0;
-        return;
+__device__ __forceinline__ long long warp_min64(long long v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const long long u = __shfl_xor_sync(kFull, v, o);
+        v = u < v ? u : v;
     }
+    return v;
+}
+
+// One warp: the forward schedule and dHidden's parts for `rows` rows, lanes weighing candidates side by side (the same
+// choice as forward_shape's).
+__device__ __forceinline__ void warp_shapes(const LossRouteArgs& a, int rows, FwdShape* fwd, SplitShape* dh) {
+    const int lane = threadIdx.x & 31;
+    const FwdPlanParams& p = a.route.fwd;
+    FwdShape f;
+    SplitShape s;
+    const int m = rows / p.tile_rows, cand_min = forward_cand_min(p, m);
+    long long best = 0x7fffffffffffffffll;
+    for (int cand = p.gmax - lane; cand >= cand_min; cand -= 32) {
+        const long long key = forward_candidate(p, m, cand, f) * 4096 + (p.gmax - cand);
+        best = key < best ? key : best;
+    }
+    best = warp_min64(best);
+    if (lane == 0) {
+        forward_candidate(p, m, p.gmax - static_cast<int>(best & 4095), f);
+        forward_finish(p, rows, m, f);
+        *fwd = f;
+    }
+    const int md = rows / a.split.tile_rows;
+    best = 0x7fffffffffffffffll;
+    for (int c = lane + 1; c <= kMaxKSplits; c += 32) {
+        if (!split_allowed(a.split, md, c)) continue;
+        const long long key = split_candidate(a.split, md, c, s) * 64 + c;
+        best = key < best ? key : best;
+    }
+    best = warp_min64(best);
+    if (lane == 0) {
+        split_candidate(a.split, md, static_cast<int>(best & 63), s);
+        *dh = s;
+    }
+}
+
+// 32 warps: model w / 2, its full block or its last one; then the models' statistics bases.
+__device__ __forceinline__ void write_shapes(const LossRouteArgs& a) {
+    const int w = threadIdx.x >> 5, k = w >> 1;
+    if (k < a.route.K) {
+        const int rows = a.route.plan->off[k + 1] - a.route.plan->off[k];
+        const int here = (w & 1) ? rows % a.block_rows : a.block_rows;
+        warp_shapes(a, here, &a.shapes->fwd[k][w & 1], &a.shapes->dh[k][w & 1]);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        long long base = 0;
+        for (int j = 0; j < a.route.K; ++j) {
+            a.route.plan->stats_base[j] = base;
+            // (read only where a model is one block)
+            const int rows = a.route.plan->off[j + 1] - a.route.plan->off[j];
+            base += rows == 0 ? 0 : a.shapes->fwd[j][rows >= a.block_rows ? 0 : 1].stats_rows;
+        }
+    }
+}
+__global__ void __launch_bounds__(1024) k_loss_shapes(LossRouteArgs a) { write_shapes(a); }
+
+// One block routes a whole small batch: thread t takes the tokens [t*per, t*per + per), counts them by model, and one scan
+// over the warps gives every token its slot, models one after the other and tokens in order.  Replaces four memsets and the
+// three routing launches: at 64 tokens the call takes 45 instead of 77 us.
+__global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
+    constexpr int kPer = kLossRouteTokens / 1024, kCu = 2048;
+    __shared__ int sh_cu[kCu];
+    __shared__ int sh_cnt[UNITY_MAX_MODELS][32];
+    __shared__ int sh_off[UNITY_MAX_MODELS + 1], sh_tot[UNITY_MAX_MODELS];
+    const RouteArgs& r = a.route;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = static_cast<int>(r.n_tok);
+    const int per = (n + 1023) / 1024, i0 = tid * per;
+    const bool staged = r.n_inv < kCu;
+    if (staged) for (int s = tid; s <= r.n_inv; s += 1024) sh_cu[s] = static_cast<int>(r.cu_seqlens[s]);
+    a.counters[tid] = 0u;
+    bool on[kPer];
+    int tgt[kPer], model[kPer];
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const bool in = j < per && i0 + j < n;
+        on[j] = in && (r.tok_mask ? r.tok_mask[i0 + j] != 0 : true);
+        tgt[j] = on[j] && r.target ? r.target[i0 + j] : 0;
+        model[j] = -1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (!on[j]) continue;
+        int lo = 0, hi = r.n_inv;                             // entries cu[1 .. n_inv] that are <= the token
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            const long long c = staged ? sh_cu[mid + 1] : r.cu_seqlens[mid + 1];
+            if (c <= i0 + j) lo = mid + 1; else hi = mid;
+        }
+        const int role = r.inv_role[min(lo, r.n_inv - 1)];
+        if (role >= 0 && role < r.n_roles && tgt[j] >= 0 && tgt[j] < r.V) model[j] = r.role_model[role];
+        else atomicOr(r.status, kStatusBadIndex);
+    }
+    for (int k = 0; k < r.K; ++k) {
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) c += model[j] == k;
+        c = __reduce_add_sync(kFull, c);
+        if (lane == 0) sh_cnt[k][warp] = c;
+    }
+    __syncthreads();
+    if (warp < r.K) {
+        const int c = sh_cnt[warp][lane];
+        int incl = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(kFull, incl, o);
+            if (lane >= o) incl += u;
+        }
+        sh_cnt[warp][lane] = incl - c;
+        if (lane == 31) sh_tot[warp] = incl;
+    }
+    __syncthreads();
+    if (tid == 0) {
+        int off = 0;
+        for (int k = 0; k < r.K; ++k) {
+            sh_off[k] = off;
+            r.plan->counts[k] = sh_tot[k];
+            r.plan->off[k] = off;
+            off += (sh_tot[k] + kTileM - 1) / kTileM * kTileM;
+        }
+        sh_off[r.K] = off;
+        r.plan->off[r.K] = off;
+    }
+    __syncthreads();
+    for (int k = 0; k < r.K; ++k) {
+        int c = 0;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) c += model[j] == k;
+        int incl = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(kFull, incl, o);
+            if (lane >= o) incl += u;
+        }
+        int slot = sh_off[k] + sh_cnt[k][warp] + incl - c;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if (model[j] != k) continue;
+            r.tok_slot[i0 + j] = slot;
+            r.slot_tok[slot] = i0 + j;
+            ++slot;
+        }
+        for (int s = sh_off[k] + sh_tot[k] + tid; s < sh_off[k + 1]; s += 1024) r.slot_tok[s] = -1;
+    }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (j >= per || i0 + j >= n) continue;
+        r.tok_model[i0 + j] = static_cast<int8_t>(model[j]);
+        if (model[j] >= 0) continue;
+        r.tok_slot[i0 + j] = -1;
+        if (a.tok_loss) a.tok_loss[i0 + j] = 0.f;
+        if (a.lse) a.lse[i0 + j] = 0.f;
+    }
+    __syncthreads();
+    write_shapes(a);
+}
+
+// One warp's list: ascending, distinct vocabulary indexes with their teacher probabilities q.  Entries with a negative id are
+// empty places, an id >= V is reported and counts as one, and so do entries of probability zero (a logit of -inf); equal ids
+// add up in list order.  With at most 128 entries a rank by counting (each entry is compared with all others, which sit in
+// shared memory) needs no sorting network.
+__device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slot, int tok, int (*sh_id)[kMaxTop], float (*sh_q)[kMaxTop]) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int* ids = a.top_ids + static_cast<long long>(tok) * a.n_top;
     const float* vals = a.top_vals + static_cast<long long>(tok) * a.n_top;
     int id[kMaxTop / 32];
@@ -116,6 +273,34 @@ __global__ void __launch_bounds__(256) k_teacher_lists(TeacherArgs a) {
     if (lane == 0) a.cnt_p[slot] = n;
 }
 
+// One warp per packed row and per token: 128-bit copies of the hidden row (zeros for padding slots) with its target and list,
+// and zeros for a masked token's gradient row.
+__global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
+    __shared__ int sh_id[8][kMaxTop];
+    __shared__ float sh_q[8][kMaxTop];
+    const long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31, n16 = a.H >> 3;
+    if (a.dHidden != nullptr && w < a.n_tok && a.tok_slot[w] < 0) {
+        uint4* dst = reinterpret_cast<uint4*>(a.dHidden + w * a.H);
+        for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
+    }
+    if (w >= a.plan->off[a.K]) return;                        // whole warps leave: only warp-wide barriers below
+    const int tok = a.slot_tok[w];
+    uint4* dst = reinterpret_cast<uint4*>(a.hp + w * a.H);
+    if (tok < 0) {
+        for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
+        if (lane == 0) {
+            a.target_p[w] = 0;
+            if (a.n_top > 0) a.cnt_p[w] = 0;
+        }
+        return;
+    }
+    const uint4* src = reinterpret_cast<const uint4*>(a.hidden + static_cast<long long>(tok) * a.H);
+    for (int j = lane; j < n16; j += 32) dst[j] = src[j];
+    if (lane == 0) a.target_p[w] = a.target ? a.target[tok] : -1;
+    if (a.n_top > 0) warp_list(a, w, tok, sh_id, sh_q);
+}
+
 // One warp per packed row: merge the vocabulary splits' statistics (one lane per split), then the row's loss and what
 // its gradient needs.  With d_v = lse - z_v (taken as scale*(max - acc_v) + log s, which keeps the digits of a sure
 // token's small loss):
@@ -124,50 +309,37 @@ __global__ void __launch_bounds__(256) k_teacher_lists(TeacherArgs a) {
 // A block's eight losses times their weights are one entry of `partial`; a model's rows start at a multiple of 256, so
 // no entry mixes two models.
 __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
-    __shared__ FwdShape sh_shape[UNITY_MAX_MODELS];
-    __shared__ int sh_first[UNITY_MAX_MODELS], sh_rows[UNITY_MAX_MODELS];
-    __shared__ long long sh_base[UNITY_MAX_MODELS];
-    __shared__ int sh_lo, sh_hi;
     __shared__ float sh_wl[8];
-    if (threadIdx.x < UNITY_MAX_MODELS) {
+    __shared__ double sh_sum[256];
+    __shared__ bool sh_last;
+    const bool whole = a.block.model < 0;
+    int lo = 0, n_rows = 0;
+    if (whole) n_rows = a.plan->off[a.K];
+    else span_resolve(a.block, lo, n_rows);
+    if (blockIdx.x == 0 && threadIdx.x < a.K) {               // models without a row (of a block: without a first one)
         const int k = threadIdx.x;
-        int first = 0, rows = 0;
-        long long base = 0;
-        if (k < a.K) {
-            if (a.block.model >= 0) {
-                if (k == a.block.model) span_resolve(a.block, first, rows);
-            } else {
-                first = a.plan->off[k];
-                rows = a.plan->off[k + 1] - first;
-                base = a.plan->stats_base[k];
-            }
-        }
-        sh_first[k] = first; sh_rows[k] = rows; sh_base[k] = base;
-        if (rows > 0) sh_shape[k] = forward_shape(a.fwd, rows);
-        if (k == 0) {
-            if (a.block.model >= 0) { int f, r; span_resolve(a.block, f, r); sh_lo = f; sh_hi = f + r; }
-            else { sh_lo = 0; sh_hi = a.plan->off[a.K]; }
-        }
+        if (a.plan->counts[k] == 0 && (whole || k == a.block.model)) a.loss[k] = 0.f;
     }
-    __syncthreads();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long idx = static_cast<long long>(blockIdx.x) * 8 + warp;
-    if (static_cast<long long>(blockIdx.x) * 8 >= sh_hi - sh_lo) return;      // the whole block: spans are multiples of 128
-    const int slot = sh_lo + static_cast<int>(idx);
+    if (static_cast<long long>(blockIdx.x) * 8 >= n_rows) return;             // the whole block: spans are multiples of 128
+    const int slot = lo + static_cast<int>(idx);
     const int tok = a.slot_tok[slot];
     float wl = 0.f;
     if (tok < 0) {
         if (lane == 0 && a.with_grad) { a.row_lse[slot] = 0.f; a.coef_p[slot] = 0.f; a.coef_g[slot] = 0.f; a.target_g[slot] = 0.f; }
     } else {
         const int k = a.tok_model[tok];
-        const FwdShape& fs = sh_shape[k];
-        long long pitch = sh_rows[k];
-        const int r = slot - sh_first[k];
-        const float4* st = a.stats + sh_base[k] + r;
+        const int first = whole ? a.plan->off[k] : lo;
+        const int span = min(whole ? a.plan->off[k + 1] - first : n_rows, a.block.row_cap);   // rows of the forward launch
+        const FwdShape& fs = a.shapes->fwd[k][span == a.block.row_cap ? 0 : 1];
+        long long pitch = span;
+        const int r = slot - first;
+        const float4* st = a.stats + (whole ? a.plan->stats_base[k] : 0) + r;
         int n_splits = fs.splits;
-        const long long last_row0 = static_cast<long long>(fs.last_m0) * a.fwd.tile_rows;
+        const long long last_row0 = static_cast<long long>(fs.last_m0) * a.tile_rows;
         if (r >= last_row0) {                                 // swept in the launch's short last round
-            st = a.stats + sh_base[k] + static_cast<long long>(fs.splits) * pitch + (r - last_row0);
+            st += static_cast<long long>(fs.splits) * pitch - last_row0;
             pitch -= last_row0;
             n_splits = fs.last_splits;
         }
@@ -235,24 +407,27 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) s += sh_wl[j];
         a.partial[slot >> 3] = s;
+        __threadfence();
+        sh_last = atomicAdd(a.ticket, 1u) + 1u == static_cast<unsigned>((n_rows + 7) / 8);
     }
-}
-
-// One block per model: its entries of `partial` in a fixed order.
-__global__ void __launch_bounds__(256) k_loss_sum(LossRowArgs a) {
-    __shared__ double sh[256];
-    const int k = blockIdx.x;
-    double s = 0.0;
-    for (int j = (a.plan->off[k] >> 3) + threadIdx.x; j < (a.plan->off[k + 1] >> 3); j += 256) s += a.partial[j];
-    sh[threadIdx.x] = s;
     __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-        if (threadIdx.x < o) sh[threadIdx.x] += sh[threadIdx.x + o];
+    if (!sh_last) return;
+    // The block that finishes last adds up the entries of its models, in a fixed order: of a block's model, those of the
+    // blocks before it too, so that the last block's launch leaves the whole sum.
+    __threadfence();
+    for (int k = whole ? 0 : a.block.model; k < (whole ? a.K : a.block.model + 1); ++k) {
+        const int j0 = a.plan->off[k] >> 3, j1 = (whole ? a.plan->off[k + 1] : lo + n_rows) >> 3;
+        if (a.plan->counts[k] == 0) continue;
+        double s = 0.0;
+        for (int j = j0 + threadIdx.x; j < j1; j += 256) s += __ldcg(a.partial + j);
+        sh_sum[threadIdx.x] = s;
         __syncthreads();
-    }
-    if (threadIdx.x == 0) {
-        const float M = a.has_norm ? a.norm[k] : fmaxf(static_cast<float>(a.plan->counts[k]), 1.f);
-        a.loss[k] = static_cast<float>(sh[0] / M);
+        for (int o = 128; o > 0; o >>= 1) {
+            if (threadIdx.x < o) sh_sum[threadIdx.x] += sh_sum[threadIdx.x + o];
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) a.loss[k] = static_cast<float>(sh_sum[0] / (a.has_norm ? a.norm[k] : fmaxf(static_cast<float>(a.plan->counts[k]), 1.f)));
+        __syncthreads();
     }
 }
 
@@ -272,14 +447,22 @@ __global__ void __launch_bounds__(256) k_teacher_scatter(TeacherScatterArgs a) {
     }
 }
 
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // A block converts 8192 columns of a row: each thread issues four 128-bit loads 4 KiB apart, so a warp's access is the 256
 // columns of one tile of the forward GEMM and has one reference.  2 B read and 2 B written per logit.
 constexpr int kGradVecs = 4;
+constexpr int kGradCols = 256 * 8 * kGradVecs;
 __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
-    const int c_first = blockIdx.x * (256 * 8 * kGradVecs) + threadIdx.x * 8;
     int row0, rows;
     span_resolve(a.span, row0, rows);
-    for (int r = blockIdx.y; r < rows; r += gridDim.y) {
+    const int per_row = (a.cols + kGradCols - 1) / kGradCols;
+    for (int item = blockIdx.x; item < rows * per_row; item += gridDim.x) {      // at most 18432 rows of 2^18 columns
+        const int r = item / per_row, c_lo = (item - r * per_row) * kGradCols, c_first = c_lo + threadIdx.x * 8;
         const int slot = row0 + r;
         uint4* row = reinterpret_cast<uint4*>(a.Z + static_cast<long long>(r) * a.ld);
         const float* tm = a.tile_max + static_cast<long long>(r) * a.n_tiles;
@@ -303,14 +486,30 @@ __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
             for (int j = 0; j < 4; ++j) {
                 const float u0 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7610)) - 8388608.f;
                 const float u1 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7632)) - 8388608.f;
-                float g0 = fmaf(cp, exp2f(fmaf(u0, -1.f / kStashSteps, sh)), -cu);
-                float g1 = fmaf(cp, exp2f(fmaf(u1, -1.f / kStashSteps, sh)), -cu);
-                if (c0 + 2 * j == tgt) g0 = gt;
-                if (c0 + 2 * j + 1 == tgt) g1 = gt;
+                const float g0 = fmaf(cp, ex2(fmaf(u0, -1.f / kStashSteps, sh)), -cu);
+                const float g1 = fmaf(cp, ex2(fmaf(u1, -1.f / kStashSteps, sh)), -cu);
                 const __nv_bfloat162 h = __floats2bfloat162_rn(g0, g1);
                 w[j] = *reinterpret_cast<const unsigned*>(&h);
             }
+            if (static_cast<unsigned>(tgt - c0) < 8u) {        // the target is among this thread's eight
+                const unsigned bits = __bfloat16_as_ushort(__float2bfloat16_rn(gt));
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (tgt - c0 == 2 * j) w[j] = (w[j] & 0xffff0000u) | bits;
+                    if (tgt - c0 == 2 * j + 1) w[j] = (w[j] & 0x0000ffffu) | (bits << 16);
+                }
+            }
             row[c0 >> 3] = raw[u];
+        }
+        if (a.n_top > 0) {                                     // the row's listed entries among this block's columns
+            __syncthreads();
+            const long long at = static_cast<long long>(slot) * a.n_top;
+            const int cnt = a.cnt_p[slot];
+            for (int j = threadIdx.x; j < cnt; j += 256) {
+                const int c = a.ids_p[at + j] - c_lo;
+                if (c >= 0 && c < kGradCols)
+                    reinterpret_cast<__nv_bfloat16*>(row)[c_lo + c] = __float2bfloat16_rn(a.top_g[at + j]);
+            }
         }
     }
 }
@@ -323,11 +522,7 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
     if (r >= rows) return;
     const int tok = a.slot_tok[slot0 + r];
     if (tok < 0) return;
-    __shared__ int sh_splits;
-    if (threadIdx.x == 0)
-        sh_splits = a.most != 0 ? split_shape(a.most, rows / a.tile_rows, a.n_tiles, a.k_iters, a.workers).splits : 1;
-    __syncthreads();
-    const int splits = sh_splits;
+    const int splits = a.shapes ? a.shapes->dh[a.span.model][rows == a.span.row_cap ? 0 : 1].splits : 1;
     const long long stride = static_cast<long long>(rows) * a.H;
     const float* src = a.parts + static_cast<long long>(r) * a.H;
     __nv_bfloat16* dst = a.dHidden + static_cast<long long>(tok) * a.H;
@@ -370,8 +565,27 @@ __global__ void __launch_bounds__(256) k_cast_dw(const float4* __restrict__ src,
 
 }  // namespace
 
-cudaError_t launch_teacher_lists(const TeacherArgs& a, long long max_slots, cudaStream_t stream) {
-    k_teacher_lists<<<static_cast<unsigned>((max_slots + 7) / 8), 256, 0, stream>>>(a);
+cudaError_t launch_loss_route(const LossRouteArgs& a, cudaStream_t stream, int* n_launches) {
+    cudaError_t e;
+    if (a.route.n_tok <= kLossRouteTokens) {
+        k_loss_route<<<1, 1024, 0, stream>>>(a);
+        *n_launches += 1;
+        return cudaGetLastError();
+    }
+    const size_t n = static_cast<size_t>(a.route.n_tok);
+    if (a.tok_loss && (e = cudaMemsetAsync(a.tok_loss, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
+    if (a.lse && (e = cudaMemsetAsync(a.lse, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
+    if ((e = cudaMemsetAsync(a.route.slot_tok, 0xff, sizeof(int) * a.max_slots, stream)) != cudaSuccess) return e;
+    if ((e = cudaMemsetAsync(a.counters, 0, sizeof(unsigned) * kLossCounters, stream)) != cudaSuccess) return e;
+    if ((e = launch_route(a.route, stream, n_launches)) != cudaSuccess) return e;
+    k_loss_shapes<<<1, 1024, 0, stream>>>(a);
+    *n_launches += 1;
+    return cudaGetLastError();
+}
+
+cudaError_t launch_loss_gather(const LossGatherArgs& a, cudaStream_t stream) {
+    const long long n = a.max_slots > a.n_tok ? a.max_slots : a.n_tok;
+    k_loss_gather<<<static_cast<unsigned>((n + 7) / 8), 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -382,21 +596,15 @@ cudaError_t launch_loss_rows(const LossRowArgs& a, cudaStream_t stream) {
     return cudaGetLastError();
 }
 
-cudaError_t launch_loss_sum(const LossRowArgs& a, cudaStream_t stream) {
-    k_loss_sum<<<a.K, 256, 0, stream>>>(a);
-    return cudaGetLastError();
-}
-
 cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream) {
     k_teacher_scatter<<<static_cast<unsigned>((a.span.row_cap + 7) / 8), 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
 
-cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, cudaStream_t stream) {
-    const int gx = (a.cols + 256 * 8 * kGradVecs - 1) / (256 * 8 * kGradVecs);
-    const int gy = a.span.row_cap < 32768 ? a.span.row_cap : 32768;
-    if (gy <= 0) return cudaSuccess;
-    k_loss_grad_inplace<<<dim3(gx, gy), 256, 0, stream>>>(a);
+cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream) {
+    const long long items = static_cast<long long>(a.span.row_cap) * ((a.cols + kGradCols - 1) / kGradCols);
+    const long long blocks = 6ll * sm_count;                  // as many as are resident (40 registers, 256 threads)
+    k_loss_grad_inplace<<<static_cast<unsigned>(items < blocks ? items : blocks), 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
 

@@ -436,7 +436,7 @@ struct LossCall {
 struct LossLayout {
     int* tok_slot; int* slot_tok; int8_t* tok_model; int* blk_cnt; DevPlan* plan; unsigned* sync_counters;
     __nv_bfloat16* hp; int* target_p; float4* stats; float* partial;
-    int *ids_p, *cnt_p; float *q_p, *top_z;
+    LossShapes* shapes; int *ids_p, *cnt_p; float *q_p, *top_z;
     float *row_lse, *coef_p, *coef_g, *target_g;
     __nv_bfloat16* G; float *tile_max, *parts, *dWc;
     long long max_slots;
@@ -476,7 +476,8 @@ LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int
     L.tok_model = b.take<int8_t>(n_tok);
     L.blk_cnt = b.take<int>(static_cast<size_t>(L.n_blocks) * K + 1);
     L.plan = b.take<DevPlan>(1);
-    L.sync_counters = b.take<unsigned>(kSyncCounters);
+    L.shapes = b.take<LossShapes>(1);
+    L.sync_counters = b.take<unsigned>(kLossCounters);
     L.hp = b.take<__nv_bfloat16>(ms * H);
     L.target_p = b.take<int>(ms);
     L.stats = b.take<float4>(4 * ms + 94720ull * K);
@@ -552,32 +553,47 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         }
     }
     if (!fits) return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: need at least %zu bytes, have %zu", L.bytes, ctx->ws_bytes);
-    if (c.tok_loss) CUDA_TRY(ctx, cudaMemsetAsync(c.tok_loss, 0, sizeof(float) * r->n_tok, st));
-    if (c.lse) CUDA_TRY(ctx, cudaMemsetAsync(c.lse, 0, sizeof(float) * r->n_tok, st));
-
     int nl = 0, rc;
+    // At most 128 rows: one row tile of a single CTA instead of a half empty one of a CTA pair, for every GEMM whose rows they
+    // are (with 87 rows at H = 3584 the products then take less time than the heads' bytes)
+    const bool few = r->n_tok <= kCtaM;
+    const int c_fwd = few ? 1 : ctx->ctas[UNITY_PROF_FWD_GEMM], c_grad = few ? 1 : ctx->ctas[UNITY_PROF_GRAD_GEMM],
+              c_dh = few ? 1 : ctx->ctas[UNITY_PROF_DH_GEMM], c_dw = ctx->ctas[UNITY_PROF_DW_GEMM];
+    const int cap_all = few ? kCtaM : 0x7fffff00;            // rows of a span that covers a model
+    const int mma_n = gemm_mma_n(H);
+    const bool two_blocks = ctx->wide_acc && H > mma_n, wide_dh = two_blocks && c_dh == 2;
+    const int cols_dh = (wide_dh ? 2 : 1) * mma_n;
     FwdPlanParams fwd = fwd_params(ctx, V, H);
+    fwd.n_pairs = ctx->sm_count / c_fwd;
+    fwd.tile_rows = gemm_tile_rows(c_fwd);
+    if (fwd.gmax > fwd.n_pairs) fwd.gmax = fwd.n_pairs;
     fwd.max_splits = fwd.n_pairs;
-    SyncCounters counters{L.sync_counters, 0, kSyncCounters};
-    CUDA_TRY(ctx, cudaMemsetAsync(L.slot_tok, 0xff, sizeof(int) * L.max_slots, st));
-    CUDA_TRY(ctx, cudaMemsetAsync(L.sync_counters, 0, sizeof(unsigned) * kSyncCounters, st));
-    RouteArgs ra;
-    memset(&ra, 0, sizeof(ra));
+    SyncCounters counters{L.sync_counters, 0, kLossCounters};
+    // loss_rows needs its counter: the rendezvous of the GEMMs may go without, so theirs come second
+    unsigned* tickets = counters.base;
+    const long long n_tickets = B.keep ? K * ((rows_bound + B.rows - 1) / B.rows) : 1;
+    if (n_tickets > kLossCounters) return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: %lld blocks of rows", n_tickets);
+    counters.used = static_cast<int>(n_tickets);
+
+    LossRouteArgs lr;
+    memset(&lr, 0, sizeof(lr));
+    RouteArgs& ra = lr.route;
     ra.n_tok = r->n_tok; ra.n_inv = r->n_inv; ra.n_roles = r->n_roles; ra.K = K; ra.V = V;
     ra.cu_seqlens = r->cu_seqlens; ra.inv_role = r->inv_role; ra.target = r->target; ra.tok_mask = r->tok_mask;
     for (int v = 0; v < r->n_roles; ++v) ra.role_model[v] = r->role_model[v];
     ra.n_blocks = L.n_blocks; ra.blk_cnt = L.blk_cnt; ra.plan = L.plan; ra.fwd = fwd;
     ra.tok_slot = L.tok_slot; ra.slot_tok = L.slot_tok; ra.tok_model = L.tok_model; ra.status = ctx->d_status;
-    CUDA_TRY(ctx, launch_route(ra, st, &nl));
-    CUDA_TRY(ctx, launch_gather_rows(static_cast<const __nv_bfloat16*>(r->hidden), r->target, L.slot_tok, L.plan, K,
-                                     L.max_slots, H, L.hp, L.target_p, st));
+    lr.split = SplitParams{B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0, (H + cols_dh - 1) / cols_dh,
+                           (V + kTileK - 1) / kTileK, ctx->sm_count / c_dh, gemm_tile_rows(c_dh)};
+    lr.block_rows = B.keep && !few ? B.rows : cap_all;
+    lr.max_slots = L.max_slots; lr.shapes = L.shapes; lr.counters = L.sync_counters; lr.tok_loss = c.tok_loss; lr.lse = c.lse;
+    CUDA_TRY(ctx, launch_loss_route(lr, st, &nl));
+    __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
+    const LossGatherArgs ga{L.plan, L.slot_tok, L.tok_slot, K, V, H, r->n_tok, L.max_slots,
+                            static_cast<const __nv_bfloat16*>(r->hidden), r->target, L.hp, dH, L.target_p, c.n_top, c.logits,
+                            r->inv_temperature, c.top_ids, c.top_vals, L.ids_p, L.cnt_p, L.q_p, ctx->d_status};
+    CUDA_TRY(ctx, launch_loss_gather(ga, st));
     nl += 1;
-    if (c.n_top > 0) {
-        const TeacherArgs ta{L.plan, L.slot_tok, K, V, c.n_top, c.logits, r->inv_temperature, c.top_ids, c.top_vals,
-                             L.ids_p, L.cnt_p, L.q_p, ctx->d_status};
-        CUDA_TRY(ctx, launch_teacher_lists(ta, L.max_slots, st));
-        nl += 1;
-    }
 
     CUtensorMap tm_hp_k, tm_hp_mn;
     if ((rc = make_tmap(ctx, &tm_hp_k, L.hp, H, L.max_slots, static_cast<uint64_t>(H) * 2, kBoxRows))) return rc;
@@ -586,7 +602,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     auto forward = [&](const RowSpan& span, bool whole, const CUtensorMap& tmB) {
         GemmArgs g;
         memset(&g, 0, sizeof(g));
-        g.span = span; g.span_mode = kSpanForward; g.stats_from_plan = whole ? 1 : 0; g.fwd = fwd;
+        g.span = span; g.span_mode = kSpanForward; g.stats_from_plan = whole ? 1 : 0; g.fwd = fwd; g.shapes = L.shapes;
         g.m_tiles = 1;                                   // set by the kernel
         g.n_tiles = fwd.n_tiles; g.k_iters = H / kTileK; g.n_cols = V;
         g.stats = L.stats; g.target_p = L.target_p; g.scale = r->inv_temperature;
@@ -595,11 +611,12 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         gemm_common(ctx, g, UNITY_PROF_FWD_GEMM, &counters, ctx->fwd_sync != 0);
         ProfScope ps(ctx, UNITY_PROF_FWD_GEMM);
         nl += 1;
-        return launch_gemm(kEpiLossStats, false, ctx->ctas[UNITY_PROF_FWD_GEMM], tm_hp_k, tmB, g, ctx->sm_count, st);
+        return launch_gemm(kEpiLossStats, false, c_fwd, tm_hp_k, tmB, g, ctx->sm_count, st);
     };
     LossRowArgs la;
     memset(&la, 0, sizeof(la));
-    la.block = RowSpan{L.plan, -1, 0, 0}; la.plan = L.plan; la.fwd = fwd; la.max_slots = L.max_slots; la.K = K; la.V = V;
+    la.block = RowSpan{L.plan, -1, 0, cap_all}; la.plan = L.plan; la.shapes = L.shapes; la.tile_rows = fwd.tile_rows;
+    la.ticket = tickets++; la.max_slots = L.max_slots; la.K = K; la.V = V;
     la.stats = L.stats; la.slot_tok = L.slot_tok; la.tok_model = L.tok_model; la.scale = r->inv_temperature;
     la.tok_weight = c.tok_weight; la.has_norm = c.norm != nullptr;
     for (int k = 0; k < K && c.norm; ++k) la.norm[k] = c.norm[k];
@@ -607,8 +624,6 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     la.ids_p = L.ids_p; la.cnt_p = L.cnt_p; la.q_p = L.q_p; la.top_z = L.top_z; la.target_p = L.target_p;
     la.with_grad = want; la.row_lse = L.row_lse; la.coef_p = L.coef_p; la.coef_g = L.coef_g; la.target_g = L.target_g;
     la.tok_loss = c.tok_loss; la.lse = c.lse; la.partial = L.partial; la.loss = c.loss;
-    const int c_fwd = ctx->ctas[UNITY_PROF_FWD_GEMM], c_grad = ctx->ctas[UNITY_PROF_GRAD_GEMM],
-              c_dh = ctx->ctas[UNITY_PROF_DH_GEMM], c_dw = ctx->ctas[UNITY_PROF_DW_GEMM];
     auto w_map = [&](CUtensorMap* tm, int k, int box) {
         return make_tmap(ctx, tm, r->W[k], H, V, static_cast<uint64_t>(H) * 2, box);
     };
@@ -616,40 +631,33 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         for (int k = 0; k < K; ++k) {
             CUtensorMap tmB;
             if ((rc = w_map(&tmB, k, kTileN / c_fwd))) return rc;
-            CUDA_TRY(ctx, forward(RowSpan{L.plan, k, 0, 0x7fffff00}, true, tmB));
+            CUDA_TRY(ctx, forward(RowSpan{L.plan, k, 0, cap_all}, true, tmB));
         }
         CUDA_TRY(ctx, launch_loss_rows(la, st));
         nl += 1;
     }
-    __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
-    if (want_h) { CUDA_TRY(ctx, launch_zero_masked_rows(L.tok_slot, r->n_tok, H, dH, st)); nl += 1; }
-
     // per model and block of rows: G = dL/dz in bf16, dHidden = G W, dW += G^T hidden
-    const int mma_n = gemm_mma_n(H);
-    const bool two_blocks = ctx->wide_acc && H > mma_n;
     for (int k = 0; want && k < K; ++k) {
         float* dWk = want_w ? (B.dw_scratch ? L.dWc : static_cast<float*>(c.dW[k])) : nullptr;
         const bool out16 = c.bf16_dw && !B.dw_scratch, add_dw = c.accumulate && !B.dw_scratch;
-        if (want_w && !add_dw) {   // a model without rows: its dW reads zero
-            CUDA_TRY(ctx, launch_zero_if_empty(dWk, static_cast<long long>(V) * H / (out16 ? 2 : 1), L.plan, k, st));
-            nl += 1;
-        }
         CUtensorMap tm_W_f, tm_W_k, tm_W_mn;
         if ((rc = w_map(&tm_W_f, k, kTileN / c_fwd)) || (rc = w_map(&tm_W_k, k, kTileN / c_grad)) || (rc = w_map(&tm_W_mn, k, kTileK))) return rc;
         for (long long c0 = 0; c0 < rows_bound; c0 += B.rows) {
-            const int nc = static_cast<int>(rows_bound - c0 < B.rows ? rows_bound - c0 : B.rows);
+            // (a full block's span has block_rows as its bound even where fewer rows are left: the schedules go by it)
+            const int nc = few ? kCtaM : B.rows;
             const RowSpan chunk{L.plan, k, static_cast<int>(c0), nc};
             int base = V, n_pieces = 1;
             if (B.keep) {
                 CUDA_TRY(ctx, forward(chunk, false, tm_W_f));
                 LossRowArgs lb = la;
                 lb.block = chunk;
+                if (k > 0 || c0 > 0) lb.ticket = tickets++;
                 CUDA_TRY(ctx, launch_loss_rows(lb, st));
                 const LossGradArgs lg{reinterpret_cast<uint16_t*>(L.G), B.cols, chunk, V, fwd.n_tiles, L.tile_max,
                                       r->inv_temperature * 1.4426950408889634f, L.target_p, L.row_lse, L.coef_p, L.coef_g,
-                                      L.target_g, c.smoothing / static_cast<float>(V)};
+                                      L.target_g, c.smoothing / static_cast<float>(V), c.n_top, L.ids_p, L.cnt_p, L.top_z};
                 ProfScope ps(ctx, UNITY_PROF_GRAD_GEMM);
-                CUDA_TRY(ctx, launch_loss_grad_inplace(lg, st));
+                CUDA_TRY(ctx, launch_loss_grad_inplace(lg, ctx->sm_count, st));
                 nl += 2;
             } else {
                 vocab_chunks(V, B.cols, &base, &n_pieces);
@@ -681,7 +689,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     CUDA_TRY(ctx, launch_gemm(kEpiLossGrad, false, c_grad, tm_hp_k, tm_W_k, g, ctx->sm_count, st));
                     nl += 1;
                 }
-                if (c.n_top > 0) {
+                if (c.n_top > 0 && !B.keep) {
                     const TeacherScatterArgs ts{chunk, L.ids_p, L.cnt_p, L.top_z, c.n_top, v0, vc, L.G, B.cols};
                     CUDA_TRY(ctx, launch_teacher_scatter(ts, st));
                     nl += 1;
@@ -692,24 +700,19 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                 if (want_h) {
                     GemmArgs h;
                     memset(&h, 0, sizeof(h));
-                    const bool wide = two_blocks && c_dh == 2;
-                    const int cols = (wide ? 2 : 1) * mma_n;
                     h.mma_n = mma_n;
-                    h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1;
-                    h.n_tiles = (H + cols - 1) / cols; h.k_iters = (vc + kTileK - 1) / kTileK;
-                    h.k_splits = B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0;
-                    h.fwd.n_pairs = ctx->sm_count / c_dh;
+                    h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1; h.shapes = B.keep ? L.shapes : nullptr;
+                    h.n_tiles = lr.split.n_tiles; h.k_iters = (vc + kTileK - 1) / kTileK;
                     h.group_m = ctx->chunk_group[1] / c_dh > 0 ? ctx->chunk_group[1] / c_dh : 1;
                     h.b_k0 = v0; h.n_cols = H; h.C = L.parts; h.ldc = H; h.beta = v0 > 0;
                     gemm_common(ctx, h, UNITY_PROF_DH_GEMM, &counters, (ctx->chunk_sync & 2) != 0);
                     {
                         ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
-                        CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, false, c_dh, tm_G_k, tm_W_mn, h, ctx->sm_count, st, wide));
+                        CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, false, c_dh, tm_G_k, tm_W_mn, h, ctx->sm_count, st, wide_dh));
                         nl += 1;
                     }
                     if (ci + 1 == n_pieces) {
-                        const StoreArgs sa{L.parts, L.slot_tok, chunk, H, h.k_splits, h.n_tiles, h.k_iters, h.fwd.n_pairs,
-                                           gemm_tile_rows(c_dh), dH};
+                        const StoreArgs sa{L.parts, L.slot_tok, chunk, H, h.shapes, dH};
                         CUDA_TRY(ctx, launch_store_parts(sa, st));
                         nl += 1;
                     }
@@ -732,6 +735,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         w.C = dWk + static_cast<long long>(v0) * H;
                     }
                     w.beta = (add_dw || c0 > 0) ? 1 : 0;
+                    w.zero_if_empty = !w.beta;               // a model without rows: its dW reads zero
                     gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0);
                     ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
                     CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide));
@@ -744,8 +748,6 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
             nl += 1;
         }
     }
-    CUDA_TRY(ctx, launch_loss_sum(la, st));
-    nl += 1;
     ctx->launches += nl;
     return UNITY_OK;
 }
