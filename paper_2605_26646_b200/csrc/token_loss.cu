@@ -66,12 +66,22 @@ __device__ __forceinline__ void warp_shapes(const LossRouteArgs& a, int rows, Fw
 }
 
 // 32 warps: model w / 2, its full block or its last one; then the models' statistics bases.
-__device__ __forceinline__ void write_shapes(const LossRouteArgs& a) {
+__device__ __forceinline__ void write_shapes(const LossRouteArgs& a, const int* off) {
+    __shared__ long long sh_stats[UNITY_MAX_MODELS][2];
     const int w = threadIdx.x >> 5, k = w >> 1;
     if (k < a.route.K) {
-        const int rows = a.route.plan->off[k + 1] - a.route.plan->off[k];
-        const int here = (w & 1) ? rows % a.block_rows : a.block_rows;
-        warp_shapes(a, here, &a.shapes->fwd[k][w & 1], &a.shapes->dh[k][w & 1]);
+        const int rows = off[k + 1] - off[k];
+        const bool full = (w & 1) == 0;
+        if (!full || rows >= a.block_rows) {                   // (no full block, no schedule of one)
+            FwdShape f;
+            SplitShape s;
+            warp_shapes(a, full ? a.block_rows : rows % a.block_rows, &f, &s);
+            if ((threadIdx.x & 31) == 0) {
+                a.shapes->fwd[k][w & 1] = f;
+                a.shapes->dh[k][w & 1] = s;
+                sh_stats[k][w & 1] = f.stats_rows;
+            }
+        }
     }
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -79,12 +89,12 @@ __device__ __forceinline__ void write_shapes(const LossRouteArgs& a) {
         for (int j = 0; j < a.route.K; ++j) {
             a.route.plan->stats_base[j] = base;
             // (read only where a model is one block)
-            const int rows = a.route.plan->off[j + 1] - a.route.plan->off[j];
-            base += rows == 0 ? 0 : a.shapes->fwd[j][rows >= a.block_rows ? 0 : 1].stats_rows;
+            const int rows = off[j + 1] - off[j];
+            base += rows == 0 ? 0 : sh_stats[j][rows >= a.block_rows ? 0 : 1];
         }
     }
 }
-__global__ void __launch_bounds__(1024) k_loss_shapes(LossRouteArgs a) { write_shapes(a); }
+__global__ void __launch_bounds__(1024) k_loss_shapes(LossRouteArgs a) { write_shapes(a, a.route.plan->off); }
 
 // One block routes a whole small batch: thread t takes the tokens [t*per, t*per + per), counts them by model, and one scan
 // over the warps gives every token its slot, models one after the other and tokens in order.  Replaces four memsets and the
@@ -184,8 +194,7 @@ __global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
         if (a.tok_loss) a.tok_loss[i0 + j] = 0.f;
         if (a.lse) a.lse[i0 + j] = 0.f;
     }
-    __syncthreads();
-    write_shapes(a);
+    write_shapes(a, sh_off);
 }
 
 // One warp's list: ascending, distinct vocabulary indexes with their teacher probabilities q.  Entries with a negative id are
@@ -273,32 +282,43 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
     if (lane == 0) a.cnt_p[slot] = n;
 }
 
-// One warp per packed row and per token: 128-bit copies of the hidden row (zeros for padding slots) with its target and list,
-// and zeros for a masked token's gradient row.
+// One warp per packed row and per token: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
+// zeros for a masked token's gradient row; with teacher's lists, every second warp takes a row's list.
 __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
     __shared__ int sh_id[8][kMaxTop];
     __shared__ float sh_q[8][kMaxTop];
-    const long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31, n16 = a.H >> 3;
+    const bool list = a.n_top > 0 && (w & 1);
+    if (a.n_top > 0) w >>= 1;
+    const int n_slots = a.plan->off[a.K];
+    const int tok = w < a.max_slots ? a.slot_tok[w] : -1;      // (not written beyond off[K]: not used there)
+    if (list) {
+        if (w >= n_slots) return;                              // whole warps leave: only warp-wide barriers below
+        if (tok < 0) { if (lane == 0) a.cnt_p[w] = 0; return; }
+        warp_list(a, w, tok, sh_id, sh_q);
+        return;
+    }
     if (a.dHidden != nullptr && w < a.n_tok && a.tok_slot[w] < 0) {
         uint4* dst = reinterpret_cast<uint4*>(a.dHidden + w * a.H);
         for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
     }
-    if (w >= a.plan->off[a.K]) return;                        // whole warps leave: only warp-wide barriers below
-    const int tok = a.slot_tok[w];
+    if (w >= n_slots) return;
     uint4* dst = reinterpret_cast<uint4*>(a.hp + w * a.H);
     if (tok < 0) {
         for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
-        if (lane == 0) {
-            a.target_p[w] = 0;
-            if (a.n_top > 0) a.cnt_p[w] = 0;
-        }
+        if (lane == 0) a.target_p[w] = 0;
         return;
     }
     const uint4* src = reinterpret_cast<const uint4*>(a.hidden + static_cast<long long>(tok) * a.H);
-    for (int j = lane; j < n16; j += 32) dst[j] = src[j];
+    for (int j0 = lane; j0 < n16; j0 += 256) {                 // eight loads in flight
+        uint4 v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) if (j0 + 32 * u < n16) v[u] = src[j0 + 32 * u];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) if (j0 + 32 * u < n16) dst[j0 + 32 * u] = v[u];
+    }
     if (lane == 0) a.target_p[w] = a.target ? a.target[tok] : -1;
-    if (a.n_top > 0) warp_list(a, w, tok, sh_id, sh_q);
 }
 
 // One warp per packed row: merge the vocabulary splits' statistics (one lane per split), then the row's loss and what
@@ -310,7 +330,7 @@ __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
 // no entry mixes two models.
 __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
     __shared__ float sh_wl[8];
-    __shared__ double sh_sum[256];
+    __shared__ double sh_sum[8];
     __shared__ bool sh_last;
     const bool whole = a.block.model < 0;
     int lo = 0, n_rows = 0;
@@ -325,11 +345,12 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
     if (static_cast<long long>(blockIdx.x) * 8 >= n_rows) return;             // the whole block: spans are multiples of 128
     const int slot = lo + static_cast<int>(idx);
     const int tok = a.slot_tok[slot];
+    int k = whole ? 0 : a.block.model;
+    while (whole && k + 1 < a.K && slot >= a.plan->off[k + 1]) ++k;
     float wl = 0.f;
     if (tok < 0) {
         if (lane == 0 && a.with_grad) { a.row_lse[slot] = 0.f; a.coef_p[slot] = 0.f; a.coef_g[slot] = 0.f; a.target_g[slot] = 0.f; }
     } else {
-        const int k = a.tok_model[tok];
         const int first = whole ? a.plan->off[k] : lo;
         const int span = min(whole ? a.plan->off[k + 1] - first : n_rows, a.block.row_cap);   // rows of the forward launch
         const FwdShape& fs = a.shapes->fwd[k][span == a.block.row_cap ? 0 : 1];
@@ -420,13 +441,13 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
         if (a.plan->counts[k] == 0) continue;
         double s = 0.0;
         for (int j = j0 + threadIdx.x; j < j1; j += 256) s += __ldcg(a.partial + j);
-        sh_sum[threadIdx.x] = s;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
+        if (lane == 0) sh_sum[warp] = s;
         __syncthreads();
-        for (int o = 128; o > 0; o >>= 1) {
-            if (threadIdx.x < o) sh_sum[threadIdx.x] += sh_sum[threadIdx.x + o];
-            __syncthreads();
-        }
-        if (threadIdx.x == 0) a.loss[k] = static_cast<float>(sh_sum[0] / (a.has_norm ? a.norm[k] : fmaxf(static_cast<float>(a.plan->counts[k]), 1.f)));
+        s = 0.0;
+        for (int j = 0; j < 8; ++j) s += sh_sum[j];
+        if (threadIdx.x == 0) a.loss[k] = static_cast<float>(s / (a.has_norm ? a.norm[k] : fmaxf(static_cast<float>(a.plan->counts[k]), 1.f)));
         __syncthreads();
     }
 }
@@ -514,27 +535,33 @@ __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
     }
 }
 
-// One block per row: four columns per thread and step, the parts added in their order, one rounding to bf16.
+// One block per row and 1024 columns: four columns per thread, the parts added in their order, one rounding to bf16.
 __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
     int slot0, rows;
     span_resolve(a.span, slot0, rows);
-    const int r = blockIdx.x;
-    if (r >= rows) return;
+    const int r = blockIdx.x, c = (blockIdx.y * 256 + threadIdx.x) * 4;
+    if (r >= rows || c >= a.H) return;
     const int tok = a.slot_tok[slot0 + r];
-    if (tok < 0) return;
     const int splits = a.shapes ? a.shapes->dh[a.span.model][rows == a.span.row_cap ? 0 : 1].splits : 1;
+    if (tok < 0) return;
     const long long stride = static_cast<long long>(rows) * a.H;
-    const float* src = a.parts + static_cast<long long>(r) * a.H;
-    __nv_bfloat16* dst = a.dHidden + static_cast<long long>(tok) * a.H;
-    for (int c = threadIdx.x * 4; c < a.H; c += 1024) {
-        float4 v = *reinterpret_cast<const float4*>(src + c);
-        for (int s = 1; s < splits; ++s) {
-            const float4 o = *reinterpret_cast<const float4*>(src + s * stride + c);
-            v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
-        }
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
-        *reinterpret_cast<uint2*>(dst + c) = make_uint2(*reinterpret_cast<const unsigned*>(&lo), *reinterpret_cast<const unsigned*>(&hi));
+    const float* src = a.parts + static_cast<long long>(r) * a.H + c;
+    float4 v = *reinterpret_cast<const float4*>(src);
+    int s = 1;
+    for (; s + 4 <= splits; s += 4) {                          // four loads in flight
+        float4 o[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) o[u] = *reinterpret_cast<const float4*>(src + (s + u) * stride);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { v.x += o[u].x; v.y += o[u].y; v.z += o[u].z; v.w += o[u].w; }
     }
+    for (; s < splits; ++s) {
+        const float4 o = *reinterpret_cast<const float4*>(src + s * stride);
+        v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+    }
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2*>(a.dHidden + static_cast<long long>(tok) * a.H + c) =
+        make_uint2(*reinterpret_cast<const unsigned*>(&lo), *reinterpret_cast<const unsigned*>(&hi));
 }
 
 // dst = bf16(src) (+ dst): one rounding of the fp32 sum over all row blocks.  Eight values per thread and step.
@@ -584,7 +611,7 @@ cudaError_t launch_loss_route(const LossRouteArgs& a, cudaStream_t stream, int* 
 }
 
 cudaError_t launch_loss_gather(const LossGatherArgs& a, cudaStream_t stream) {
-    const long long n = a.max_slots > a.n_tok ? a.max_slots : a.n_tok;
+    const long long n = (a.max_slots > a.n_tok ? a.max_slots : a.n_tok) * (a.n_top > 0 ? 2 : 1);
     k_loss_gather<<<static_cast<unsigned>((n + 7) / 8), 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
@@ -609,7 +636,7 @@ cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaSt
 }
 
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {
-    k_store_parts<<<a.span.row_cap, 256, 0, stream>>>(a);
+    k_store_parts<<<dim3(a.span.row_cap, (a.H + 1023) / 1024), 256, 0, stream>>>(a);
     return cudaGetLastError();
 }
 

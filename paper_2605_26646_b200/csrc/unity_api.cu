@@ -67,6 +67,7 @@ constexpr int kDefaultChunkMult = 2;
 constexpr int kSyncCounters = 16384;       // rendezvous counters per call (4 bytes each)
 constexpr int kMinChunkRows = 1024;
 constexpr int kMinChunkVocab = 1024;
+constexpr int kShortRows = 2048;           // ... up to which the backward GEMMs' workers do not meet at every tile
 constexpr int kMinKeepRows = 2048;         // token losses: least rows of a block whose logits are kept
 
 inline size_t up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -608,7 +609,9 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         g.stats = L.stats; g.target_p = L.target_p; g.scale = r->inv_temperature;
         g.top_ids = L.ids_p; g.top_cnt = L.cnt_p; g.top_z = L.top_z; g.top_n = c.n_top;
         if (!whole) { g.stash = reinterpret_cast<uint16_t*>(L.G); g.ldz = B.cols; g.tile_max = L.tile_max; }
-        gemm_common(ctx, g, UNITY_PROF_FWD_GEMM, &counters, ctx->fwd_sync != 0);
+        // (rows of a single round start together anyway: the rendezvous would only cost its round trip)
+        const long long rows = rows_bound < span.row_cap ? rows_bound : span.row_cap;
+        gemm_common(ctx, g, UNITY_PROF_FWD_GEMM, &counters, ctx->fwd_sync != 0 && rows > static_cast<long long>(fwd.gmax) * fwd.tile_rows);
         ProfScope ps(ctx, UNITY_PROF_FWD_GEMM);
         nl += 1;
         return launch_gemm(kEpiLossStats, false, c_fwd, tm_hp_k, tmB, g, ctx->sm_count, st);
@@ -646,6 +649,8 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
             // (a full block's span has block_rows as its bound even where fewer rows are left: the schedules go by it)
             const int nc = few ? kCtaM : B.rows;
             const RowSpan chunk{L.plan, k, static_cast<int>(c0), nc};
+            // a rendezvous per tile (about 2 us of the producer's time) costs more than it saves where a dW tile has few slabs
+            const bool short_k = nc <= kShortRows;
             int base = V, n_pieces = 1;
             if (B.keep) {
                 CUDA_TRY(ctx, forward(chunk, false, tm_W_f));
@@ -705,7 +710,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     h.n_tiles = lr.split.n_tiles; h.k_iters = (vc + kTileK - 1) / kTileK;
                     h.group_m = ctx->chunk_group[1] / c_dh > 0 ? ctx->chunk_group[1] / c_dh : 1;
                     h.b_k0 = v0; h.n_cols = H; h.C = L.parts; h.ldc = H; h.beta = v0 > 0;
-                    gemm_common(ctx, h, UNITY_PROF_DH_GEMM, &counters, (ctx->chunk_sync & 2) != 0);
+                    gemm_common(ctx, h, UNITY_PROF_DH_GEMM, &counters, (ctx->chunk_sync & 2) != 0 && !short_k);
                     {
                         ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
                         CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, false, c_dh, tm_G_k, tm_W_mn, h, ctx->sm_count, st, wide_dh));
@@ -736,7 +741,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     }
                     w.beta = (add_dw || c0 > 0) ? 1 : 0;
                     w.zero_if_empty = !w.beta;               // a model without rows: its dW reads zero
-                    gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0);
+                    gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0 && !short_k);
                     ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
                     CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide));
                     nl += 1;
