@@ -47,7 +47,9 @@ constexpr float kNegBig = -3.0e38f;
 // MN-major operands: a stage holds boxes of 64 rows x 64 K (8 KiB), one after the other.
 constexpr int kMnBoxBytes = 64 * kTileK * 2;
 
-template <int CTAS, int NB = 1>
+constexpr int kOutWarpBytes = 32 * 128;   // 32 rows x 64 bf16 columns
+
+template <int CTAS, int NB = 1, int EPI = kEpiAccumF32>
 struct Cfg {
     static constexpr int kTileRows = kCtaM * CTAS;               // rows of one output tile (128 or 256)
     static constexpr int kTileCols = kTileN * NB;                // columns of one output tile (256 or 512)
@@ -56,12 +58,14 @@ struct Cfg {
     static constexpr int kABytes = kCtaM * kTileK * 2;           // 16 KiB
     static constexpr int kBBytes = kBRows * kTileK * 2;          // 32 or 16 KiB per 256-column block
     static constexpr int kStageBytes = kABytes + NB * kBBytes;   // 48 or 32 KiB
-    static constexpr int kStages = (CTAS == 1 || NB == 2) ? 4 : 7;
-    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kBarBytes;
+    static constexpr int kStageOut = EPI == kEpiAccumB16 ? 4 * kOutWarpBytes : 0;   // the epilogue warps' staging
+    static constexpr int kStages = (CTAS == 1 || NB == 2) ? 4 : (EPI == kEpiAccumB16 ? 6 : 7);
+    static constexpr int kSmemBytes = 1024 + kStages * kStageBytes + kStageOut + kBarBytes;
 };
 
 // The token losses' epilogues run on the schedules of the policy update's.
 __host__ __device__ constexpr bool is_stats(int epi) { return epi == kEpiSoftmaxStats || epi == kEpiLossStats; }
+__host__ __device__ constexpr bool is_accum(int epi) { return epi == kEpiAccumF32 || epi == kEpiAccumB16; }
 __host__ __device__ constexpr bool is_grad(int epi) { return epi == kEpiLogitGrad || epi == kEpiLossGrad; }
 
 struct Unit {
@@ -119,7 +123,7 @@ __device__ __forceinline__ bool next_unit(const GemmArgs& g, int it, int pair, i
         const int ncu = (g.n_tiles + tpu - 1) / tpu;
         int u = pair + it * n_pairs;
         t.split = 0;
-        if (EPI == kEpiAccumF32 && g.k_splits > 1) {   // the contraction cut into k_splits parts, one after the other
+        if (is_accum(EPI) && g.k_splits > 1) {   // the contraction cut into k_splits parts, one after the other
             const int per_split = g.m_tiles * ncu;
             if (u >= per_split * g.k_splits) return false;
             t.split = u / per_split;
@@ -219,21 +223,88 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     return g;
 }
 
+// One warp's 32 rows of a block of `cols` (a multiple of 32, at most 256) accumulator columns, rounded once to bf16.  A thread
+// holds a row, but a store of 32 rows at a time touches 32 cache lines per instruction and the write of dW is what bounds the
+// GEMM of few rows (96 x 3584 x 152064: 277 us so): 64 columns go through shared memory (16-byte units exchanged by row, no
+// bank conflicts) and leave as four whole lines per instruction.  The next 32 columns' loads from tensor memory are under way
+// meanwhile.  With `add` the old values are added before the rounding, row by row.
+__device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ldc, int add, uint8_t* out, uint32_t taddr, int row0,
+                                                int m_rows, int col0, int cols) {
+    const int lane = threadIdx.x & 31;
+    if (cols <= 0) return;
+    uint32_t ra[32], rb[32];
+    auto load = [&](uint32_t (&rr)[32], int c) { ptx::tmem_ld_32x32(taddr + c * 32, rr); };
+    const bool row_ok = row0 + lane < m_rows;
+    auto pack = [&](const uint32_t (&rr)[32], int c, int half) {
+        unsigned o[16];
+        if (add) {
+            __nv_bfloat16* d = C16 + static_cast<long long>(row0 + lane) * ldc + col0 + c * 32;
+            if (!row_ok) return;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint4 old = *reinterpret_cast<const uint4*>(d + q * 8);
+                const unsigned ow[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    o[4 * q + j] = pack_bf16(__uint_as_float(rr[8 * q + 2 * j]) + __uint_as_float(ow[j] << 16),
+                                             __uint_as_float(rr[8 * q + 2 * j + 1]) + __uint_as_float(ow[j] & 0xffff0000u));
+                *reinterpret_cast<uint4*>(d + q * 8) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+            }
+            return;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[j] = pack_bf16(__uint_as_float(rr[2 * j]), __uint_as_float(rr[2 * j + 1]));
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<uint4*>(out + lane * 128 + (((half * 4 + q) ^ (lane & 7)) << 4)) =
+                make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+    };
+    const int n = cols / 32;
+    load(ra, 0);
+#pragma unroll 1
+    for (int c = 0; c < n; c += 2) {
+        const bool two = c + 1 < n;
+        ptx::tmem_ld_wait_for(ra);
+        if (two) load(rb, c + 1);
+        pack(ra, c, 0);
+        if (two) {
+            ptx::tmem_ld_wait_for(rb);
+            if (c + 2 < n) load(ra, c + 2);
+            pack(rb, c + 1, 1);
+        }
+        if (add) continue;
+        __syncwarp();
+        const int unit = lane & 7;
+        if (two || unit < 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = i * 4 + (lane >> 3);
+                const uint4 v = *reinterpret_cast<const uint4*>(out + r * 128 + ((unit ^ (r & 7)) << 4));
+                if (row0 + r < m_rows)
+                    *reinterpret_cast<uint4*>(C16 + static_cast<long long>(row0 + r) * ldc + col0 + c * 32 + unit * 8) = v;
+            }
+        }
+        __syncwarp();
+    }
+}
+
 // Token losses, forward: what one thread (= one row) carries through a sweep of column tiles.
 //   s = sum 2^((z - ref) c2), z2 = sum z (both as even / odd halves), the target's logit, and where the row stands in its
 //   ascending list of entries (next vocabulary index, INT_MAX: none left).
-// ref need not be the maximum: it is the maximum of the first tile, and later a tile's that lies more than kRefRoom octaves
-// above it.  So a tile is read from tensor memory once (a maximum first and the sum after it would read it twice: 276
+// ref need not be the maximum: it is 0 where the first tile's maximum lies within kRefBelow octaves below and kRefRoom above
+// that, else that maximum, and later a tile's maximum more than kRefRoom octaves above it.  So a tile is read from tensor memory once (a maximum first and the sum after it would read it twice: 276
 // against 353 us at 801 x 896 x 151936, where the epilogue is the bound), no sum exceeds 2^kRefRoom * V, and for a backward
 // pass that does not recompute the logits (ref - z) + kRefRoom octaves is kept in steps of 2^-10 octaves, 16 bits.  The integer
 // costs as much memory as bf16 but is off by at most half a step whatever its size: p is off by a factor of 2^(2^-11), 3.4e-4,
-// where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 48 octaves or more below ref count as 48.
+// where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 48 octaves or more below ref, 40 below the row's
+// maximum, count as 48.
 struct LossRow {
     float ref, z_tgt;
     uint64_t s, z2;
     int tgt;
     int next, pos, cnt;
     long long base;
+    bool first;     // no tile yet
 };
 // Launch constants, in registers: the resolved GemmArgs live in local memory.
 struct LossConsts {
@@ -342,11 +413,12 @@ __device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w,
         }
         // A row whose maximum rose past the room takes it as its new reference and its warp works through the tile again
         // (the list cursor has moved on: its logits are written; the target's is the same).  A second time is enough.
-        const bool over = (tm - w.ref) * k.c2 > kRefRoom;
+        const bool over = (tm - w.ref) * k.c2 > kRefRoom || (w.first && (tm - w.ref) * k.c2 < -kRefBelow);
+        w.first = false;
         if (attempt == 0 && __any_sync(0xffffffffu, over)) {
             if (over) {
-                const float resc = ptx::ex2((w.ref - tm) * k.c2);
-                w.s = ptx::mul2(w.s, ptx::pack2(resc, resc));
+                const float resc = ptx::ex2((w.ref - tm) * k.c2);       // (of a first tile: the sum is 0)
+                w.s = w.s == 0ull ? 0ull : ptx::mul2(w.s, ptx::pack2(resc, resc));
                 w.ref = tm;
             }
             continue;
@@ -361,13 +433,17 @@ __device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w,
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
 __global__ void __launch_bounds__(kThreads, 1)
 k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmArgs g_in) {
-    using C = Cfg<CTAS, NB>;
+    using C = Cfg<CTAS, NB, EPI>;
+    // Under programmatic stream serialisation the launch may overlap the end of the one before it: nothing is read or written
+    // in global memory before that one is complete (no-ops otherwise).
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
     // The row extent of a launch may be known on the device only: derive it from the plan before anything else.  Every
     // thread of both CTAs reads the same plan, so a launch whose span is empty is left by all of them, here.
     const GemmArgs g = resolve_span<C::kTileRows>(g_in);
-    if (EPI == kEpiAccumF32 && g.zero_if_empty && g.k_iters <= 0) {
-        const long long n16 = static_cast<long long>(g.m_rows) * g.ldc / (g.C16 ? 8 : 4);      // 16-byte units, whole ones
-        uint4* out = g.C16 ? reinterpret_cast<uint4*>(g.C16) : reinterpret_cast<uint4*>(g.C);
+    if (is_accum(EPI) && g.zero_if_empty && g.k_iters <= 0) {
+        const long long n16 = static_cast<long long>(g.m_rows) * g.ldc / (EPI == kEpiAccumB16 ? 8 : 4);      // 16-byte units, whole ones
+        uint4* out = EPI == kEpiAccumB16 ? reinterpret_cast<uint4*>(g.C16) : reinterpret_cast<uint4*>(g.C);
         for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < n16; i += static_cast<long long>(gridDim.x) * kThreads)
             out[i] = make_uint4(0, 0, 0, 0);
         return;
@@ -376,11 +452,11 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     if (g.n_active > 0 && (CTAS == 2 ? blockIdx.x >> 1 : blockIdx.x) >= g.n_active) return;   // never holds a unit
     constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes, kABytes = C::kABytes, kBBytes = C::kBBytes;
     constexpr int kAccStages = C::kAccStages, kTileCols = C::kTileCols;
-    static_assert(NB == 1 || (EPI == kEpiAccumF32 && CTAS == 2), "two-block tiles: fp32-accumulate epilogue, CTA pairs");
+    static_assert(NB == 1 || (is_accum(EPI) && CTAS == 2), "two-block tiles: fp32-accumulate epilogue, CTA pairs");
     extern __shared__ uint8_t smem_raw[];
     // the dynamic shared-memory window starts at the same offset in both CTAs of a pair, so all offsets below match
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStageBytes + C::kStageOut);
     uint64_t* full = bars;                       // [kStages]  (even CTA) bytes of both CTAs landed
     uint64_t* empty = bars + kStages;            // [kStages]  MMAs that read the stage have completed
     uint64_t* acc_full = bars + 2 * kStages;     // [2]        accumulator stage complete
@@ -442,7 +518,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                         const long long before = static_cast<long long>(it) * n_pairs;      // units of earlier rounds
                         const int tpu = stride_unit_tiles<EPI>(g);
                         const long long left = static_cast<long long>(g.m_tiles) * ((g.n_tiles + tpu - 1) / tpu) *
-                                               (EPI == kEpiAccumF32 && g.k_splits > 1 ? g.k_splits : 1) - before;
+                                               (is_accum(EPI) && g.k_splits > 1 ? g.k_splits : 1) - before;
                         expect = static_cast<unsigned>(it / g.sync_period) * static_cast<unsigned>(n_pairs) +
                                  static_cast<unsigned>(left < n_pairs ? left : n_pairs);
                     }
@@ -457,7 +533,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     const int nt = t.rev ? t.n_begin + t.n_end - 1 - ni : ni;
                     // fp32-accumulate tiles may be narrower than 256 columns per MMA (mma_n); the B boxes keep their size, the
                     // MMA simply leaves their last columns unread
-                    const int mma_n = EPI == kEpiAccumF32 ? g.mma_n : kTileN;
+                    const int mma_n = is_accum(EPI) ? g.mma_n : kTileN;
                     const int b_row = g.b_row0 + nt * (NB * mma_n) + static_cast<int>(cta_rank) * (mma_n / CTAS);
                     for (int k = t.k_begin; k < t.k_end; ++k) {
                         if (!ptx::mbar_wait(&empty[stage], phase ^ 1, g.wait_budget) || *abort_flag) { ok = false; break; }
@@ -498,7 +574,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer (even CTA only)
         if (lane == 0 && cta_rank == 0) {
-            const uint32_t idesc = ptx::idesc_bf16_f32(C::kTileRows, EPI == kEpiAccumF32 ? g.mma_n : kTileN) |
+            const uint32_t idesc = ptx::idesc_bf16_f32(C::kTileRows, is_accum(EPI) ? g.mma_n : kTileN) |
                                    (A_MN ? (1u << 15) : 0u) | (B_MN ? (1u << 16) : 0u);
             int stage = 0, acc = 0;
             uint32_t phase = 0, acc_phase = 0;
@@ -571,7 +647,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
             uint64_t run_s2 = 0ull, run_t2 = 0ull;           // (even, odd) partial sums of e and e*v
             int tgt = -1;
             float ca = 0.f, cb = 0.f, lse = 0.f, ent = 0.f;
-            if (EPI != kEpiAccumF32) {
+            if (!is_accum(EPI)) {
                 if (row_ok) tgt = g.target_p[g.a_row0 + row] - g.vocab0;     // column index relative to b_row0
             }
             if (EPI == kEpiLogitGrad && row_ok) {
@@ -603,9 +679,9 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 lu = g.coef_g[g.a_row0 + row] * g.uniform;
                 lt = g.target_g[g.a_row0 + row];
             }
-            // ... and the forward's row state: the reference starts below everything, the list at this unit's first column
+            // ... and the forward's row state, its list at this unit's first column
             const LossConsts lk{c2, g.n_cols, g.n_tiles, g.top_ids, g.top_z, g.tile_max, g.stash, g.ldz};
-            LossRow lr{kNegBig, kNegBig, 0ull, 0ull, tgt, 0x7fffffff, 0, 0, 0};
+            LossRow lr{0.f, kNegBig, 0ull, 0ull, tgt, 0x7fffffff, 0, 0, 0, true};
             if (EPI == kEpiLossStats && g.top_ids != nullptr && row_ok) {
                 lr.base = static_cast<long long>(g.a_row0 + row) * g.top_n;
                 lr.cnt = g.top_cnt[g.a_row0 + row];
@@ -624,15 +700,23 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                 if (!ptx::mbar_wait(&acc_full[acc], acc_phase, g.wait_budget) || *abort_flag) { ok = false; break; }
                 ptx::tc_fence_after();
                 const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + acc * kTileCols;
-                const int mma_n = EPI == kEpiAccumF32 ? g.mma_n : kTileN;     // columns per MMA block (<= 256)
+                const int mma_n = is_accum(EPI) ? g.mma_n : kTileN;     // columns per MMA block (<= 256)
                 const int col0 = nt * (NB * mma_n);
                 const int per_block = mma_n / 32;
+                if (EPI == kEpiAccumB16) {
+                    uint8_t* out = smem + kStages * kStageBytes + (warp & 3) * kOutWarpBytes;
+                    const int row0 = t.m_tile * C::kTileRows + static_cast<int>(cta_rank) * kCtaM + quarter * 32;
+#pragma unroll 1
+                    for (int nb = 0; nb < NB; ++nb)
+                        store_b16_block(g.C16, g.ldc, g.beta, out, taddr + nb * kTileN, row0, g.m_rows, col0 + nb * mma_n,
+                                        min(mma_n, g.n_cols - col0 - nb * mma_n));
+                }
                 if (EPI == kEpiLossStats) {
                     if (lk.stash != nullptr) loss_stats_tile<true>(lk, lr, taddr, col0, nt, row, row_ok);
                     else loss_stats_tile<false>(lk, lr, taddr, col0, nt, row, row_ok);
                 }
 #pragma unroll 1
-                for (int c = 0; c < (EPI == kEpiLossStats ? 0 : NB * per_block); ++c) {
+                for (int c = 0; c < (EPI == kEpiLossStats || EPI == kEpiAccumB16 ? 0 : NB * per_block); ++c) {
                     const int cbase = col0 + c * 32;            // block nb of a two-block tile starts at col0 + nb * mma_n
                     if (cbase >= g.n_cols) break;               // uniform across the CTA
                     uint32_t rr[32];
@@ -795,34 +879,6 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                         }
                     } else {
                         if (row_ok) {
-                            if (g.C16 != nullptr) {
-                                // bf16 output: the fp32 accumulator (plus the old value) rounded once
-                                __nv_bfloat16* d16 = g.C16 + static_cast<long long>(row) * g.ldc + cbase;
-                                if (g.beta) {
-#pragma unroll
-                                    for (int q = 0; q < 4; ++q) {
-                                        const uint4 old = *reinterpret_cast<const uint4*>(d16 + q * 8);
-                                        const unsigned ow[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-                                        for (int j = 0; j < 4; ++j) {
-                                            v[8 * q + 2 * j] += __uint_as_float(ow[j] << 16);
-                                            v[8 * q + 2 * j + 1] += __uint_as_float(ow[j] & 0xffff0000u);
-                                        }
-                                    }
-                                }
-                                unsigned o[16];
-#pragma unroll
-                                for (int j = 0; j < 16; ++j) o[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-                                if (g.g_wide_store) {
-                                    ptx::st_global_v8(d16, o[0], o[1], o[2], o[3], o[4], o[5], o[6], o[7]);
-                                    ptx::st_global_v8(d16 + 16, o[8], o[9], o[10], o[11], o[12], o[13], o[14], o[15]);
-                                } else {
-#pragma unroll
-                                    for (int q = 0; q < 4; ++q)
-                                        *reinterpret_cast<uint4*>(d16 + q * 8) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-                                }
-                                continue;
-                            }
                             float* dst = g.C + t.split * g.c_split + static_cast<long long>(row) * g.ldc + cbase;
 #pragma unroll
                             for (int q = 0; q < 8; ++q) {
@@ -888,7 +944,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
 cudaError_t set_attr() {
     return cudaFuncSetAttribute(k_gemm<EPI, A_MN, B_MN, CTAS, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                Cfg<CTAS, NB>::kSmemBytes);
+                                Cfg<CTAS, NB, EPI>::kSmemBytes);
 }
 
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
@@ -897,15 +953,17 @@ cudaError_t launch(const CUtensorMap& tmA, const CUtensorMap& tmB, const GemmArg
     memset(&cfg, 0, sizeof(cfg));
     cfg.gridDim = dim3(workers * CTAS, 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = Cfg<CTAS, NB>::kSmemBytes;
+    cfg.dynamicSmemBytes = Cfg<CTAS, NB, EPI>::kSmemBytes;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = CTAS;
     attr[0].val.clusterDim.y = 1;
     attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = args.pdl ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, k_gemm<EPI, A_MN, B_MN, CTAS, NB>, tmA, tmB, args);
 }
 
@@ -926,6 +984,9 @@ cudaError_t gemm_set_attributes() {
     if ((e = set_attr<kEpiAccumF32, true, true, 1>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiAccumF32, true, true, 2>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiAccumF32, false, true, 2, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr<kEpiAccumB16, true, true, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr<kEpiAccumB16, true, true, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr<kEpiAccumB16, true, true, 2, 2>()) != cudaSuccess) return e;
     return set_attr<kEpiAccumF32, true, true, 2, 2>();
 }
 
@@ -949,7 +1010,7 @@ cudaError_t launch_gemm(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap
         if (units <= 0 || args.m_tiles <= 0 || args.k_iters <= 0) return cudaSuccess;
         workers = static_cast<int>(units < max_workers ? units : max_workers);
     }
-    if (epi == kEpiAccumF32 && (args.mma_n < 32 || args.mma_n > kTileN || args.mma_n % 32 != 0)) return cudaErrorInvalidValue;
+    if (is_accum(epi) && (args.mma_n < 32 || args.mma_n > kTileN || args.mma_n % 32 != 0)) return cudaErrorInvalidValue;
     const bool two = ctas == 2;
     switch (epi) {
         case kEpiSoftmaxStats:
@@ -964,6 +1025,10 @@ cudaError_t launch_gemm(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap
         case kEpiLossGrad:
             return two ? launch<kEpiLossGrad, false, false, 2>(tmA, tmB, args, workers, stream)
                        : launch<kEpiLossGrad, false, false, 1>(tmA, tmB, args, workers, stream);
+        case kEpiAccumB16:   // as the fp32 form below, A always MN-major
+            if (wide && two) return launch<kEpiAccumB16, true, true, 2, 2>(tmA, tmB, args, workers, stream);
+            return two ? launch<kEpiAccumB16, true, true, 2>(tmA, tmB, args, workers, stream)
+                       : launch<kEpiAccumB16, true, true, 1>(tmA, tmB, args, workers, stream);
         default:   // fp32 accumulate: B is always MN-major (W or hidden read in place), A is G either way round
             if (wide && two)
                 return a_mn ? launch<kEpiAccumF32, true, true, 2, 2>(tmA, tmB, args, workers, stream)

@@ -140,6 +140,7 @@ struct LossShapes {
 };
 constexpr float kStashSteps = 1024.f;   // steps per octave of a kept logit (GemmArgs::stash) ...
 constexpr float kRefRoom = 16.f;        // ... counted down from this many octaves above its reference
+constexpr float kRefBelow = 8.f;        // a row whose first columns stay within this many octaves below 0 takes 0 as reference
 
 // ----------------------------------------------------------------------------------------------
 // GEMM  C[m, n] = sum_k A[m, k] * B[n, k]   (bf16 operands, K-major or MN-major, fp32 accumulation in TMEM)
@@ -150,7 +151,8 @@ enum GemmEpilogue : int {
     kEpiLogitGrad = 1,      // dL/dz in bf16 for a bounded (rows x vocab) chunk
     kEpiAccumF32 = 2,       // C (+)= acc, fp32, row-major
     kEpiLossStats = 3,      // token losses: online (max, sum exp, sum z, target logit) per row, the logits of listed entries
-    kEpiLossGrad = 4        // token losses: dL/dz in bf16 for a bounded (rows x vocab) chunk
+    kEpiLossGrad = 4,       // token losses: dL/dz in bf16 for a bounded (rows x vocab) chunk
+    kEpiAccumB16 = 5        // C (+)= acc rounded to bf16, row-major (token losses' dW)
 };
 
 struct GemmArgs {
@@ -208,7 +210,7 @@ struct GemmArgs {
     float uniform;            // label smoothing's share of every entry: eps / V
     // kEpiAccumF32
     float* C;
-    __nv_bfloat16* C16;       // not null: the output is bf16, here (row pitch ldc), and C is unused
+    __nv_bfloat16* C16;       // kEpiAccumB16's output, row pitch ldc (C is unused)
     long long ldc;
     int k_splits, k_per_split;   // the contraction is cut into k_splits parts of k_per_split slabs, each with an output of
     long long c_split;           // its own, c_split values apart (0 or 1: not cut)
@@ -230,6 +232,7 @@ struct GemmArgs {
     FwdPlanParams fwd;
     const LossShapes* shapes; // token losses: schedules written by the counting kernel (null: worked out here)
     long long wait_budget;    // SM clocks after which an mbarrier wait gives up (kStatusTimeout)
+    int pdl;                  // launch with programmatic stream serialisation (see launch_gemm)
     int test_drop_slab;       // test hook: the TMA producer of every worker leaves out one K slab of its first tile
                               // (neither the expected-bytes arrival nor the loads), so the waits behind it run out
 };

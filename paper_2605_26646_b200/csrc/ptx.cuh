@@ -166,6 +166,10 @@ __device__ __forceinline__ void tmem_ld_32x32(uint32_t taddr, uint32_t (&r)[32])
         : "r"(taddr)
         : "memory");
 }
+// Programmatic dependent launch: the next launch of the stream may start its blocks; wait for the launches before this one to
+// complete and their writes to be visible.  Both do nothing in a launch without the attribute.
+__device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Waits for all tcgen05.ld of this thread; the loaded registers pass through, so no use of them moves ahead of the wait.
 __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"

@@ -3,6 +3,7 @@
 // and the outputs' last sums and roundings.
 // Every sum has a fixed order and every output one writer: results are bitwise reproducible.
 #include "internal.h"
+#include "ptx.cuh"
 
 namespace unity {
 
@@ -11,6 +12,27 @@ namespace {
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kMaxTop = UNITY_MAX_TOP;
 constexpr int kNone = 0x7fffffff;
+
+// Every launch of a token loss may overlap the end of the one before it (programmatic stream serialisation): its blocks are
+// in place when that one ends.  So every kernel here begins with this, before any access to global memory; since each waits
+// for its predecessor to complete, order is that of the stream.
+__device__ __forceinline__ void begin() {
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
+}
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, cudaStream_t stream, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -94,12 +116,16 @@ __device__ __forceinline__ void write_shapes(const LossRouteArgs& a, const int* 
         }
     }
 }
-__global__ void __launch_bounds__(1024) k_loss_shapes(LossRouteArgs a) { write_shapes(a, a.route.plan->off); }
+__global__ void __launch_bounds__(1024) k_loss_shapes(LossRouteArgs a) {
+    begin();
+    write_shapes(a, a.route.plan->off);
+}
 
 // One block routes a whole small batch: thread t takes the tokens [t*per, t*per + per), counts them by model, and one scan
 // over the warps gives every token its slot, models one after the other and tokens in order.  Replaces four memsets and the
 // three routing launches: at 64 tokens the call takes 45 instead of 77 us.
 __global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
+    begin();
     constexpr int kPer = kLossRouteTokens / 1024, kCu = 2048;
     __shared__ int sh_cu[kCu];
     __shared__ int sh_cnt[UNITY_MAX_MODELS][32];
@@ -285,6 +311,7 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
 // One warp per packed row and per token: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
 // zeros for a masked token's gradient row; with teacher's lists, every second warp takes a row's list.
 __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
+    begin();
     __shared__ int sh_id[8][kMaxTop];
     __shared__ float sh_q[8][kMaxTop];
     long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
@@ -329,6 +356,7 @@ __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
 // A block's eight losses times their weights are one entry of `partial`; a model's rows start at a multiple of 256, so
 // no entry mixes two models.
 __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
+    begin();
     __shared__ float sh_wl[8];
     __shared__ double sh_sum[8];
     __shared__ bool sh_last;
@@ -455,6 +483,7 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
 // One warp per row of the span: the gradients of its listed entries among columns [v0, v0 + cols) replace what the dense
 // pass wrote there (which left out the teacher's part).
 __global__ void __launch_bounds__(256) k_teacher_scatter(TeacherScatterArgs a) {
+    begin();
     const int lane = threadIdx.x & 31;
     int slot0, rows;
     span_resolve(a.span, slot0, rows);
@@ -468,17 +497,12 @@ __global__ void __launch_bounds__(256) k_teacher_scatter(TeacherScatterArgs a) {
     }
 }
 
-__device__ __forceinline__ float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
 // A block converts 8192 columns of a row: each thread issues four 128-bit loads 4 KiB apart, so a warp's access is the 256
 // columns of one tile of the forward GEMM and has one reference.  2 B read and 2 B written per logit.
 constexpr int kGradVecs = 4;
 constexpr int kGradCols = 256 * 8 * kGradVecs;
 __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
+    begin();
     int row0, rows;
     span_resolve(a.span, row0, rows);
     const int per_row = (a.cols + kGradCols - 1) / kGradCols;
@@ -507,8 +531,8 @@ __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
             for (int j = 0; j < 4; ++j) {
                 const float u0 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7610)) - 8388608.f;
                 const float u1 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7632)) - 8388608.f;
-                const float g0 = fmaf(cp, ex2(fmaf(u0, -1.f / kStashSteps, sh)), -cu);
-                const float g1 = fmaf(cp, ex2(fmaf(u1, -1.f / kStashSteps, sh)), -cu);
+                const float g0 = fmaf(cp, ptx::ex2(fmaf(u0, -1.f / kStashSteps, sh)), -cu);
+                const float g1 = fmaf(cp, ptx::ex2(fmaf(u1, -1.f / kStashSteps, sh)), -cu);
                 const __nv_bfloat162 h = __floats2bfloat162_rn(g0, g1);
                 w[j] = *reinterpret_cast<const unsigned*>(&h);
             }
@@ -537,6 +561,7 @@ __global__ void __launch_bounds__(256) k_loss_grad_inplace(LossGradArgs a) {
 
 // One block per row and 1024 columns: four columns per thread, the parts added in their order, one rounding to bf16.
 __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
+    begin();
     int slot0, rows;
     span_resolve(a.span, slot0, rows);
     const int r = blockIdx.x, c = (blockIdx.y * 256 + threadIdx.x) * 4;
@@ -566,6 +591,7 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
 
 // dst = bf16(src) (+ dst): one rounding of the fp32 sum over all row blocks.  Eight values per thread and step.
 __global__ void __launch_bounds__(256) k_cast_dw(const float4* __restrict__ src, uint4* __restrict__ dst, long long n8, int add) {
+    begin();
     const long long stride = static_cast<long long>(gridDim.x) * blockDim.x;
     for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < n8; i += stride) {
         const float4 a = src[2 * i], b = src[2 * i + 1];
@@ -595,9 +621,8 @@ __global__ void __launch_bounds__(256) k_cast_dw(const float4* __restrict__ src,
 cudaError_t launch_loss_route(const LossRouteArgs& a, cudaStream_t stream, int* n_launches) {
     cudaError_t e;
     if (a.route.n_tok <= kLossRouteTokens) {
-        k_loss_route<<<1, 1024, 0, stream>>>(a);
         *n_launches += 1;
-        return cudaGetLastError();
+        return launch(k_loss_route, dim3(1), 1024, stream, a);
     }
     const size_t n = static_cast<size_t>(a.route.n_tok);
     if (a.tok_loss && (e = cudaMemsetAsync(a.tok_loss, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
@@ -605,44 +630,37 @@ cudaError_t launch_loss_route(const LossRouteArgs& a, cudaStream_t stream, int* 
     if ((e = cudaMemsetAsync(a.route.slot_tok, 0xff, sizeof(int) * a.max_slots, stream)) != cudaSuccess) return e;
     if ((e = cudaMemsetAsync(a.counters, 0, sizeof(unsigned) * kLossCounters, stream)) != cudaSuccess) return e;
     if ((e = launch_route(a.route, stream, n_launches)) != cudaSuccess) return e;
-    k_loss_shapes<<<1, 1024, 0, stream>>>(a);
     *n_launches += 1;
-    return cudaGetLastError();
+    return launch(k_loss_shapes, dim3(1), 1024, stream, a);
 }
 
 cudaError_t launch_loss_gather(const LossGatherArgs& a, cudaStream_t stream) {
     const long long n = (a.max_slots > a.n_tok ? a.max_slots : a.n_tok) * (a.n_top > 0 ? 2 : 1);
-    k_loss_gather<<<static_cast<unsigned>((n + 7) / 8), 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch(k_loss_gather, dim3(static_cast<unsigned>((n + 7) / 8)), 256, stream, a);
 }
 
 cudaError_t launch_loss_rows(const LossRowArgs& a, cudaStream_t stream) {
     const long long n = a.block.model >= 0 ? a.block.row_cap : a.max_slots;
     if (n <= 0) return cudaSuccess;
-    k_loss_rows<<<static_cast<unsigned>((n + 7) / 8), 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch(k_loss_rows, dim3(static_cast<unsigned>((n + 7) / 8)), 256, stream, a);
 }
 
 cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream) {
-    k_teacher_scatter<<<static_cast<unsigned>((a.span.row_cap + 7) / 8), 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch(k_teacher_scatter, dim3(static_cast<unsigned>((a.span.row_cap + 7) / 8)), 256, stream, a);
 }
 
 cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream) {
     const long long items = static_cast<long long>(a.span.row_cap) * ((a.cols + kGradCols - 1) / kGradCols);
     const long long blocks = 6ll * sm_count;                  // as many as are resident (40 registers, 256 threads)
-    k_loss_grad_inplace<<<static_cast<unsigned>(items < blocks ? items : blocks), 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch(k_loss_grad_inplace, dim3(static_cast<unsigned>(items < blocks ? items : blocks)), 256, stream, a);
 }
 
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {
-    k_store_parts<<<dim3(a.span.row_cap, (a.H + 1023) / 1024), 256, 0, stream>>>(a);
-    return cudaGetLastError();
+    return launch(k_store_parts, dim3(a.span.row_cap, (a.H + 1023) / 1024), 256, stream, a);
 }
 
 cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream) {
-    k_cast_dw<<<1184, 256, 0, stream>>>(reinterpret_cast<const float4*>(src), reinterpret_cast<uint4*>(dst), n >> 3, add ? 1 : 0);
-    return cudaGetLastError();
+    return launch(k_cast_dw, dim3(1184), 256, stream, reinterpret_cast<const float4*>(src), reinterpret_cast<uint4*>(dst), n >> 3, add ? 1 : 0);
 }
 
 }  // namespace unity

@@ -603,6 +603,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     auto forward = [&](const RowSpan& span, bool whole, const CUtensorMap& tmB) {
         GemmArgs g;
         memset(&g, 0, sizeof(g));
+        g.pdl = 1;
         g.span = span; g.span_mode = kSpanForward; g.stats_from_plan = whole ? 1 : 0; g.fwd = fwd; g.shapes = L.shapes;
         g.m_tiles = 1;                                   // set by the kernel
         g.n_tiles = fwd.n_tiles; g.k_iters = H / kTileK; g.n_cols = V;
@@ -672,6 +673,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                 if (!B.keep) {
                     GemmArgs g;
                     memset(&g, 0, sizeof(g));
+                    g.pdl = 1;
                     g.span = chunk; g.span_mode = kSpanRowsA;
                     g.m_tiles = 1;                                   // set by the kernel
                     g.n_tiles = (vc + kTileN - 1) / kTileN; g.k_iters = H / kTileK; g.group_m = 1;
@@ -705,6 +707,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                 if (want_h) {
                     GemmArgs h;
                     memset(&h, 0, sizeof(h));
+                    h.pdl = 1;
                     h.mma_n = mma_n;
                     h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1; h.shapes = B.keep ? L.shapes : nullptr;
                     h.n_tiles = lr.split.n_tiles; h.k_iters = (vc + kTileK - 1) / kTileK;
@@ -725,6 +728,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                 if (want_w) {
                     GemmArgs w;
                     memset(&w, 0, sizeof(w));
+                    w.pdl = 1;
                     // few rows: a tile's epilogue must overlap the next tile's products, which only the narrow form does
                     const bool wide = two_blocks && c_dw == 2 && nc > 1024;
                     const int tile_v = gemm_tile_rows(c_dw), cols = (wide ? 2 : 1) * mma_n;
@@ -733,17 +737,13 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     w.n_tiles = (H + cols - 1) / cols; w.k_iters = 1;
                     w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
                     w.m_rows = vc; w.n_cols = H; w.ldc = H;
-                    if (out16) {
-                        w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + static_cast<long long>(v0) * H;
-                        w.g_wide_store = reinterpret_cast<uintptr_t>(w.C16) % 32 == 0;
-                    } else {
-                        w.C = dWk + static_cast<long long>(v0) * H;
-                    }
+                    if (out16) w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + static_cast<long long>(v0) * H;
+                    else w.C = dWk + static_cast<long long>(v0) * H;
                     w.beta = (add_dw || c0 > 0) ? 1 : 0;
                     w.zero_if_empty = !w.beta;               // a model without rows: its dW reads zero
                     gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0 && !short_k);
                     ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
-                    CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide));
+                    CUDA_TRY(ctx, launch_gemm(out16 ? kEpiAccumB16 : kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide));
                     nl += 1;
                 }
             }
