@@ -275,14 +275,18 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
         if (add) continue;
         __syncwarp();
         const int unit = lane & 7;
+        // (all eight reads before the first write: the compiler keeps their order, and each would wait for its latency)
+        uint4 v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = i * 4 + (lane >> 3);
+            v[i] = *reinterpret_cast<const uint4*>(out + r * 128 + ((unit ^ (r & 7)) << 4));
+        }
+        __nv_bfloat16* dst = C16 + static_cast<long long>(row0 + (lane >> 3)) * ldc + col0 + c * 32 + unit * 8;
         if (two || unit < 4) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int r = i * 4 + (lane >> 3);
-                const uint4 v = *reinterpret_cast<const uint4*>(out + r * 128 + ((unit ^ (r & 7)) << 4));
-                if (row0 + r < m_rows)
-                    *reinterpret_cast<uint4*>(C16 + static_cast<long long>(row0 + r) * ldc + col0 + c * 32 + unit * 8) = v;
-            }
+            for (int i = 0; i < 8; ++i)
+                if (row0 + i * 4 + (lane >> 3) < m_rows) *reinterpret_cast<uint4*>(dst + i * 4 * ldc) = v[i];
         }
         __syncwarp();
     }
