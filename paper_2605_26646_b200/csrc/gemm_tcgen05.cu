@@ -438,22 +438,6 @@ template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
 __global__ void __launch_bounds__(kThreads, 1)
 k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmArgs g_in) {
     using C = Cfg<CTAS, NB, EPI>;
-    // Under programmatic stream serialisation the launch may overlap the end of the one before it: nothing is read or written
-    // in global memory before that one is complete (no-ops otherwise).
-    ptx::grid_launch_dependents();
-    ptx::grid_wait();
-    // The row extent of a launch may be known on the device only: derive it from the plan before anything else.  Every
-    // thread of both CTAs reads the same plan, so a launch whose span is empty is left by all of them, here.
-    const GemmArgs g = resolve_span<C::kTileRows>(g_in);
-    if (is_accum(EPI) && g.zero_if_empty && g.k_iters <= 0) {
-        const long long n16 = static_cast<long long>(g.m_rows) * g.ldc / (EPI == kEpiAccumB16 ? 8 : 4);      // 16-byte units, whole ones
-        uint4* out = EPI == kEpiAccumB16 ? reinterpret_cast<uint4*>(g.C16) : reinterpret_cast<uint4*>(g.C);
-        for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < n16; i += static_cast<long long>(gridDim.x) * kThreads)
-            out[i] = make_uint4(0, 0, 0, 0);
-        return;
-    }
-    if (g.m_tiles <= 0 || g.n_tiles <= 0 || g.k_iters <= 0) return;
-    if (g.n_active > 0 && (CTAS == 2 ? blockIdx.x >> 1 : blockIdx.x) >= g.n_active) return;   // never holds a unit
     constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes, kABytes = C::kABytes, kBBytes = C::kBBytes;
     constexpr int kAccStages = C::kAccStages, kTileCols = C::kTileCols;
     static_assert(NB == 1 || (is_accum(EPI) && CTAS == 2), "two-block tiles: fp32-accumulate epilogue, CTA pairs");
@@ -471,30 +455,56 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t cta_rank = CTAS == 2 ? ptx::cluster_ctarank() : 0u;     // 0: issues the MMAs, 1: its peer
     const int pair = CTAS == 2 ? blockIdx.x >> 1 : blockIdx.x;              // index of this worker (CTA or CTA pair)
+    auto setup = [&] {
+        if (threadIdx.x == 0) {
+            for (int s = 0; s < kStages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
+            for (int s = 0; s < kAccStages; ++s) { ptx::mbar_init(&acc_full[s], 1); ptx::mbar_init(&acc_empty[s], 4 * CTAS); }
+            *abort_flag = 0;
+            ptx::fence_barrier_init();
+            ptx::prefetch_tensormap(&tmA);
+            ptx::prefetch_tensormap(&tmB);
+        }
+        if (warp == 1) {
+            if (CTAS == 2) { ptx::tmem_alloc_pair(tmem_slot, kTmemCols); ptx::tmem_relinquish_pair(); }
+            else { ptx::tmem_alloc(tmem_slot, kTmemCols); ptx::tmem_relinquish(); }
+        }
+        ptx::tc_fence_before();
+        if (CTAS == 2) ptx::cluster_sync_all();   // barriers of both CTAs are initialised before anyone signals across
+        else __syncthreads();
+        ptx::tc_fence_after();
+    };
+    // Under programmatic stream serialisation the launch may overlap the end of the one before it: barriers and tensor memory
+    // are set up meanwhile, and nothing is read or written in global memory before that one is complete.
+    const bool pdl = g_in.pdl != 0;
+    if (pdl) {
+        setup();
+        ptx::grid_launch_dependents();
+        ptx::grid_wait();
+    }
+    // The row extent of a launch may be known on the device only: derive it from the plan.  Every thread of both CTAs reads the
+    // same plan, so a launch whose span is empty is left by all of them, here (at the end, once tensor memory is held).
+    const GemmArgs g = resolve_span<C::kTileRows>(g_in);
+    if (is_accum(EPI) && g.zero_if_empty && g.k_iters <= 0) {
+        const long long n16 = static_cast<long long>(g.m_rows) * g.ldc / (EPI == kEpiAccumB16 ? 8 : 4);      // 16-byte units, whole ones
+        uint4* out = EPI == kEpiAccumB16 ? reinterpret_cast<uint4*>(g.C16) : reinterpret_cast<uint4*>(g.C);
+        for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < n16; i += static_cast<long long>(gridDim.x) * kThreads)
+            out[i] = make_uint4(0, 0, 0, 0);
+    }
+    const bool idle = g.m_tiles <= 0 || g.n_tiles <= 0 || g.k_iters <= 0 ||
+                      (g.n_active > 0 && (CTAS == 2 ? blockIdx.x >> 1 : blockIdx.x) >= g.n_active);   // never holds a unit
+    if (!pdl) {
+        if (idle) return;
+        setup();
+    }
     const int n_launched = CTAS == 2 ? gridDim.x >> 1 : gridDim.x;
     const int n_pairs = g.n_active > 0 && g.n_active < n_launched ? g.n_active : n_launched;   // workers at work
-
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
-        for (int s = 0; s < kAccStages; ++s) { ptx::mbar_init(&acc_full[s], 1); ptx::mbar_init(&acc_empty[s], 4 * CTAS); }
-        *abort_flag = 0;
-        ptx::fence_barrier_init();
-        ptx::prefetch_tensormap(&tmA);
-        ptx::prefetch_tensormap(&tmB);
-    }
-    if (warp == 1) {
-        if (CTAS == 2) { ptx::tmem_alloc_pair(tmem_slot, kTmemCols); ptx::tmem_relinquish_pair(); }
-        else { ptx::tmem_alloc(tmem_slot, kTmemCols); ptx::tmem_relinquish(); }
-    }
-    ptx::tc_fence_before();
-    if (CTAS == 2) ptx::cluster_sync_all();   // barriers of both CTAs are initialised before anyone signals across
-    else __syncthreads();
-    ptx::tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
     const int gm = max(1, g.group_m);
 
-    if (warp == 0) {
+    if (idle) {
+        // nothing to do but to give the tensor memory back
+    } else if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer (both CTAs)
         if (lane == 0) {
             int stage = 0;
@@ -884,6 +894,15 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
                     } else {
                         if (row_ok) {
                             float* dst = g.C + t.split * g.c_split + static_cast<long long>(row) * g.ldc + cbase;
+                            if (g.g_wide_store && !g.beta) {        // whole 32-byte sectors per thread
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    if (q * 8 < n_here)
+                                        ptx::st_global_v8(dst + q * 8, rr[8 * q], rr[8 * q + 1], rr[8 * q + 2], rr[8 * q + 3], rr[8 * q + 4],
+                                                          rr[8 * q + 5], rr[8 * q + 6], rr[8 * q + 7]);
+                                }
+                                continue;
+                            }
 #pragma unroll
                             for (int q = 0; q < 8; ++q) {
                                 if (q * 4 < n_here) {

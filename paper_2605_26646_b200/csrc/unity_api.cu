@@ -712,7 +712,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1; h.shapes = B.keep ? L.shapes : nullptr;
                     h.n_tiles = lr.split.n_tiles; h.k_iters = (vc + kTileK - 1) / kTileK;
                     h.group_m = ctx->chunk_group[1] / c_dh > 0 ? ctx->chunk_group[1] / c_dh : 1;
-                    h.b_k0 = v0; h.n_cols = H; h.C = L.parts; h.ldc = H; h.beta = v0 > 0;
+                    h.b_k0 = v0; h.n_cols = H; h.C = L.parts; h.ldc = H; h.beta = v0 > 0; h.g_wide_store = 1;
                     gemm_common(ctx, h, UNITY_PROF_DH_GEMM, &counters, (ctx->chunk_sync & 2) != 0 && !short_k);
                     {
                         ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
