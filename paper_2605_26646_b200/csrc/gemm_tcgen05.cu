@@ -217,7 +217,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
             g.c_split = static_cast<long long>(n_rows) * in.ldc;
         }
     } else if (in.span_mode == kSpanRowsK) {
-        g.k_iters = n_rows / kTileK;
+        g.k_iters = (in.shapes ? span_slab_rows(in.span, n_rows) : n_rows) / kTileK;
         g.b_k0 = in.b_k0 + slot0;
     }
     return g;

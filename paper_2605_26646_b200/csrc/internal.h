@@ -45,6 +45,12 @@ __device__ __forceinline__ void span_resolve(const RowSpan& s, int& slot0, int& 
     slot0 = first + s.row_begin;
 }
 
+// The span's rows that hold tokens, rounded up to whole slabs of the contraction over rows (`n_rows`: its padded rows).
+__device__ __forceinline__ int span_slab_rows(const RowSpan& s, int n_rows) {
+    const int valid = s.plan->counts[s.model] - s.row_begin, slab = (valid + kTileK - 1) / kTileK * kTileK;
+    return slab < 0 ? 0 : (slab < n_rows ? slab : n_rows);
+}
+
 // Shape of one forward launch over `rows` packed rows (a multiple of the row tile): row tiles per round and
 // vocabulary splits.  One round of the persistent kernel = gm row tiles x splits vocabulary splits <= number of
 // workers (CTAs or CTA pairs): gm bounds the hidden rows that must stay L2 resident (48 tiles of 128 rows by default:
@@ -230,7 +236,8 @@ struct GemmArgs {
     int span_mode;
     int stats_from_plan;
     FwdPlanParams fwd;
-    const LossShapes* shapes; // token losses: schedules written by the counting kernel (null: worked out here)
+    const LossShapes* shapes; // token losses: schedules written by the counting kernel (null: worked out here); a contraction
+                              // over rows ends with the last slab that holds a token
     long long wait_budget;    // SM clocks after which an mbarrier wait gives up (kStatusTimeout)
     int pdl;                  // launch with programmatic stream serialisation (see launch_gemm)
     int test_drop_slab;       // test hook: the TMA producer of every worker leaves out one K slab of its first tile

@@ -726,25 +726,38 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     }
                 }
                 if (want_w) {
-                    GemmArgs w;
-                    memset(&w, 0, sizeof(w));
-                    w.pdl = 1;
                     // few rows: a tile's epilogue must overlap the next tile's products, which only the narrow form does
                     const bool wide = two_blocks && c_dw == 2 && nc > 1024;
-                    const int tile_v = gemm_tile_rows(c_dw), cols = (wide ? 2 : 1) * mma_n;
-                    w.mma_n = mma_n;
-                    w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = (vc + tile_v - 1) / tile_v;
-                    w.n_tiles = (H + cols - 1) / cols; w.k_iters = 1;
-                    w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
-                    w.m_rows = vc; w.n_cols = H; w.ldc = H;
-                    if (out16) w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + static_cast<long long>(v0) * H;
-                    else w.C = dWk + static_cast<long long>(v0) * H;
-                    w.beta = (add_dw || c0 > 0) ? 1 : 0;
-                    w.zero_if_empty = !w.beta;               // a model without rows: its dW reads zero
-                    gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0 && !short_k);
-                    ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
-                    CUDA_TRY(ctx, launch_gemm(out16 ? kEpiAccumB16 : kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide));
-                    nl += 1;
+                    const int tile_v = gemm_tile_rows(c_dw), vt = (vc + tile_v - 1) / tile_v, cols = (wide ? 2 : 1) * mma_n;
+                    // the last few vocabulary tiles as a launch of narrow ones where they would open one more wave (as in
+                    // the policy update: V = 151936 is eight waves of 74 tiles and two more) and that wave is longer than a launch
+                    const int workers = ctx->sm_count / c_dw, nt = (H + cols - 1) / cols, rem = vt % workers;
+                    int narrow_n = 0;
+                    if (ctx->dw_tail && c_dw == 2 && !short_k && vt > workers && rem > 0 && 2 * rem * nt < workers)
+                        for (int cand = 64; cand <= kTileN && narrow_n == 0; cand += 32)
+                            if (static_cast<long long>(rem) * ((H + cand - 1) / cand) <= workers) narrow_n = cand;
+                    for (int part = 0; part < (narrow_n > 0 ? 2 : 1); ++part) {
+                        const int t0 = part == 0 ? 0 : vt - rem, t1 = part == 0 && narrow_n > 0 ? vt - rem : vt;
+                        const int row0 = t0 * tile_v, n_here = (t1 * tile_v < vc ? t1 * tile_v : vc) - row0;
+                        const bool wide_here = wide && part == 0;
+                        GemmArgs w;
+                        memset(&w, 0, sizeof(w));
+                        w.pdl = 1;
+                        w.mma_n = part == 0 ? mma_n : narrow_n;
+                        w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = t1 - t0; w.shapes = L.shapes;
+                        w.n_tiles = (H + (wide_here ? 2 : 1) * w.mma_n - 1) / ((wide_here ? 2 : 1) * w.mma_n); w.k_iters = 1;
+                        w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
+                        w.a_row0 = row0; w.m_rows = n_here; w.n_cols = H; w.ldc = H;
+                        const long long at = static_cast<long long>(v0 + row0) * H;
+                        if (out16) w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + at;
+                        else w.C = dWk + at;
+                        w.beta = (add_dw || c0 > 0) ? 1 : 0;
+                        w.zero_if_empty = !w.beta;               // a model without rows: its dW reads zero
+                        gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0 && !short_k);
+                        ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
+                        CUDA_TRY(ctx, launch_gemm(out16 ? kEpiAccumB16 : kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide_here));
+                        nl += 1;
+                    }
                 }
             }
         }
