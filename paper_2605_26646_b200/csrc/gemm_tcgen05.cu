@@ -179,6 +179,10 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
             const int full = min(g.m_tiles, fs.gm) * fs.splits, last = (g.m_tiles - fs.last_m0) * fs.last_splits;
             g.n_active = max(full, last);
         }
+        if (in.stash_by_slot) {
+            g.stash = in.stash + static_cast<long long>(slot0) * in.ldz;
+            g.tile_max = in.tile_max + static_cast<long long>(slot0) * in.n_tiles;
+        }
         if (in.stats_from_plan) g.stats = in.stats + in.span.plan->stats_base[in.span.model];
     } else if (in.span_mode == kSpanRowsA) {
         g.a_row0 = in.a_row0 + slot0;
@@ -211,6 +215,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     } else if (in.span_mode == kSpanRowsM) {
         g.m_rows = n_rows;
         g.m_tiles = n_rows / TILE_ROWS;
+        if (in.stash_by_slot) g.a_row0 = slot0;
         if (in.shapes) {
             const SplitShape sp = in.shapes->dh[in.span.model][n_rows == in.span.row_cap ? 0 : 1];
             g.k_splits = sp.splits; g.k_per_split = sp.per_split;
@@ -219,6 +224,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     } else if (in.span_mode == kSpanRowsK) {
         g.k_iters = (in.shapes ? span_slab_rows(in.span, n_rows) : n_rows) / kTileK;
         g.b_k0 = in.b_k0 + slot0;
+        if (in.stash_by_slot) g.a_k0 = slot0;
     }
     return g;
 }

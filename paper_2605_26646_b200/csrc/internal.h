@@ -208,7 +208,8 @@ struct GemmArgs {
     int top_n;
     uint16_t* stash;          // optional, a block of rows: kRefRoom octaves above the reference, minus the logit, in steps of
                               // 1 / kStashSteps octaves, row pitch ldz ...
-    float* tile_max;          // ... and the reference of each column tile [rows, n_tiles], accumulator units
+    float* tile_max;          // ... and the reference of each column tile [rows, n_tiles], accumulator units;
+    int stash_by_slot;        // both (and G of a GEMM that reads it) hold every packed row, not the span's alone
     // kEpiLossGrad: G = coef_p * p - coef_g * uniform, and target_g at the target (row_lse as above)
     const float* coef_p;      // [rows] dL/dz_v per unit of p_v, times scale
     const float* coef_g;      // [rows] scale * weight / M
@@ -405,7 +406,7 @@ cudaError_t launch_value_loss(const ValueArgs& a, cudaStream_t stream, int* n_la
 // token losses (token_loss.cu)
 // ----------------------------------------------------------------------------------------------
 // Routing of a token loss with everything the later launches need: tokens to packed slots, the plan, the schedules, zeros for
-// masked tokens' outputs and for the call's counters.  Up to kLossRouteTokens tokens it is one launch of one block.
+// masked tokens' outputs and for the call's counters.
 constexpr int kLossRouteTokens = 8192;
 constexpr int kLossCounters = 1024;
 struct LossRouteArgs {
@@ -417,7 +418,6 @@ struct LossRouteArgs {
     unsigned* counters;        // [kLossCounters]
     float *tok_loss, *lse;     // caller order, nullable
 };
-cudaError_t launch_loss_route(const LossRouteArgs& a, cudaStream_t stream, int* n_launches);
 
 // Packs the hidden rows and targets, turns the teacher's lists into ascending distinct entries with their probabilities and
 // zeroes the masked tokens' rows of dHidden.
@@ -438,7 +438,8 @@ struct LossGatherArgs {
     float* q_p;                // packed [slots, n_top]
     int* status;
 };
-cudaError_t launch_loss_gather(const LossGatherArgs& a, cudaStream_t stream);
+// Both of the above: one launch up to 1024 tokens, two up to kLossRouteTokens, else memsets and six.
+cudaError_t launch_loss_pack(const LossRouteArgs& a, const LossGatherArgs& g, cudaStream_t stream, int* n_launches);
 
 struct LossRowArgs {
     RowSpan block;             // one block of one model's rows, or (block.model < 0) up to row_cap rows of every model
@@ -483,8 +484,8 @@ cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t str
 struct LossGradArgs {
     uint16_t* Z;
     long long ld;
-    RowSpan span;              // per-row vectors are indexed from its first slot
-    int cols, n_tiles;
+    RowSpan span;              // a block (per-row vectors are indexed from its first slot), or (model < 0) every packed row
+    int K, cols, n_tiles;
     const float* tile_max;     // [rows, n_tiles]
     float c2;                  // inv_temperature * log2(e)
     const int* target_p;
@@ -502,6 +503,7 @@ struct StoreArgs {
     RowSpan span;
     int H;
     const LossShapes* shapes;  // null: one part
+    int bound;                 // rows the span can have at most
     __nv_bfloat16* dHidden;
 };
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream);

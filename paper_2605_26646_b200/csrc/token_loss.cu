@@ -87,22 +87,20 @@ __device__ __forceinline__ void warp_shapes(const LossRouteArgs& a, int rows, Fw
     }
 }
 
-// 32 warps: model w / 2, its full block or its last one; then the models' statistics bases.
+// Model w / 2, its full block or its last one, for w over the block's warps; then the models' statistics bases.
 __device__ __forceinline__ void write_shapes(const LossRouteArgs& a, const int* off) {
     __shared__ long long sh_stats[UNITY_MAX_MODELS][2];
-    const int w = threadIdx.x >> 5, k = w >> 1;
-    if (k < a.route.K) {
-        const int rows = off[k + 1] - off[k];
+    for (int w = threadIdx.x >> 5; w < 2 * a.route.K; w += blockDim.x >> 5) {
+        const int k = w >> 1, rows = off[k + 1] - off[k];
         const bool full = (w & 1) == 0;
-        if (!full || rows >= a.block_rows) {                   // (no full block, no schedule of one)
-            FwdShape f;
-            SplitShape s;
-            warp_shapes(a, full ? a.block_rows : rows % a.block_rows, &f, &s);
-            if ((threadIdx.x & 31) == 0) {
-                a.shapes->fwd[k][w & 1] = f;
-                a.shapes->dh[k][w & 1] = s;
-                sh_stats[k][w & 1] = f.stats_rows;
-            }
+        if (full && rows < a.block_rows) continue;             // no full block, no schedule of one
+        FwdShape f;
+        SplitShape s;
+        warp_shapes(a, full ? a.block_rows : rows % a.block_rows, &f, &s);
+        if ((threadIdx.x & 31) == 0) {
+            a.shapes->fwd[k][w & 1] = f;
+            a.shapes->dh[k][w & 1] = s;
+            sh_stats[k][w & 1] = f.stats_rows;
         }
     }
     __syncthreads();
@@ -121,29 +119,33 @@ __global__ void __launch_bounds__(1024) k_loss_shapes(LossRouteArgs a) {
     write_shapes(a, a.route.plan->off);
 }
 
-// One block routes a whole small batch: thread t takes the tokens [t*per, t*per + per), counts them by model, and one scan
-// over the warps gives every token its slot, models one after the other and tokens in order.  Replaces four memsets and the
-// three routing launches: at 64 tokens the call takes 45 instead of 77 us.
-__global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
-    begin();
-    constexpr int kPer = kLossRouteTokens / 1024, kCu = 2048;
-    __shared__ int sh_cu[kCu];
-    __shared__ int sh_cnt[UNITY_MAX_MODELS][32];
-    __shared__ int sh_off[UNITY_MAX_MODELS + 1], sh_tot[UNITY_MAX_MODELS];
-    const RouteArgs& r = a.route;
+// Routing of all tokens by one block: thread t takes the tokens [t*per, t*per + per), counts them by model, and a scan over
+// the warps gives every token its rank within its model, tokens in order.
+template <int kThreads>
+struct RouteShared {
+    static constexpr int kCu = 1024;
+    int cu[kCu];
+    int cnt[UNITY_MAX_MODELS][kThreads / 32];
+    int off[UNITY_MAX_MODELS + 1];     // first slot of each model
+    int tot[UNITY_MAX_MODELS];         // its tokens
+};
+template <int kThreads, int kPer>
+__device__ __forceinline__ void route_tokens(const RouteArgs& r, bool report, RouteShared<kThreads>& sh, int (&model)[kPer],
+                                             int (&rank)[kPer]) {
+    constexpr int kCu = RouteShared<kThreads>::kCu, kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = static_cast<int>(r.n_tok);
-    const int per = (n + 1023) / 1024, i0 = tid * per;
+    const int per = (n + kThreads - 1) / kThreads, i0 = tid * per;
     const bool staged = r.n_inv < kCu;
-    if (staged) for (int s = tid; s <= r.n_inv; s += 1024) sh_cu[s] = static_cast<int>(r.cu_seqlens[s]);
-    a.counters[tid] = 0u;
+    if (staged) for (int s = tid; s <= r.n_inv; s += kThreads) sh.cu[s] = static_cast<int>(r.cu_seqlens[s]);
     bool on[kPer];
-    int tgt[kPer], model[kPer];
+    int tgt[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         const bool in = j < per && i0 + j < n;
         on[j] = in && (r.tok_mask ? r.tok_mask[i0 + j] != 0 : true);
-        tgt[j] = on[j] && r.target ? r.target[i0 + j] : 0;
+        tgt[j] = in && r.target ? r.target[i0 + j] : 0;
         model[j] = -1;
+        rank[j] = 0;
     }
     __syncthreads();
 #pragma unroll
@@ -152,75 +154,84 @@ __global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
         int lo = 0, hi = r.n_inv;                             // entries cu[1 .. n_inv] that are <= the token
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            const long long c = staged ? sh_cu[mid + 1] : r.cu_seqlens[mid + 1];
+            const long long c = staged ? sh.cu[mid + 1] : r.cu_seqlens[mid + 1];
             if (c <= i0 + j) lo = mid + 1; else hi = mid;
         }
         const int role = r.inv_role[min(lo, r.n_inv - 1)];
         if (role >= 0 && role < r.n_roles && tgt[j] >= 0 && tgt[j] < r.V) model[j] = r.role_model[role];
-        else atomicOr(r.status, kStatusBadIndex);
+        else if (report) atomicOr(r.status, kStatusBadIndex);
     }
     for (int k = 0; k < r.K; ++k) {
         int c = 0;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) c += model[j] == k;
-        c = __reduce_add_sync(kFull, c);
-        if (lane == 0) sh_cnt[k][warp] = c;
-    }
-    __syncthreads();
-    if (warp < r.K) {
-        const int c = sh_cnt[warp][lane];
         int incl = c;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int u = __shfl_up_sync(kFull, incl, o);
             if (lane >= o) incl += u;
         }
-        sh_cnt[warp][lane] = incl - c;
-        if (lane == 31) sh_tot[warp] = incl;
+        int at = incl - c;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) if (model[j] == k) rank[j] = at++;
+        if (lane == 31) sh.cnt[k][warp] = incl;
     }
     __syncthreads();
-    if (tid == 0) {
+    for (int k = warp; k < r.K; k += kWarps) {
+        const int c = lane < kWarps ? sh.cnt[k][lane] : 0;
+        int incl = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(kFull, incl, o);
+            if (lane >= o) incl += u;
+        }
+        if (lane < kWarps) sh.cnt[k][lane] = incl - c;
+        if (lane == 31) sh.tot[k] = incl;
+    }
+    __syncthreads();
+    if (tid <= r.K) {
         int off = 0;
-        for (int k = 0; k < r.K; ++k) {
-            sh_off[k] = off;
-            r.plan->counts[k] = sh_tot[k];
-            r.plan->off[k] = off;
-            off += (sh_tot[k] + kTileM - 1) / kTileM * kTileM;
-        }
-        sh_off[r.K] = off;
-        r.plan->off[r.K] = off;
+        for (int k = 0; k < tid; ++k) off += (sh.tot[k] + kTileM - 1) / kTileM * kTileM;
+        sh.off[tid] = off;
     }
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) if (model[j] >= 0) rank[j] += sh.cnt[model[j]][warp];
     __syncthreads();
-    for (int k = 0; k < r.K; ++k) {
-        int c = 0;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) c += model[j] == k;
-        int incl = c;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(kFull, incl, o);
-            if (lane >= o) incl += u;
-        }
-        int slot = sh_off[k] + sh_cnt[k][warp] + incl - c;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            if (model[j] != k) continue;
-            r.tok_slot[i0 + j] = slot;
-            r.slot_tok[slot] = i0 + j;
-            ++slot;
-        }
-        for (int s = sh_off[k] + sh_tot[k] + tid; s < sh_off[k + 1]; s += 1024) r.slot_tok[s] = -1;
+}
+
+// ... and its result for the later launches.
+template <int kThreads, int kPer>
+__device__ __forceinline__ void write_routes(const LossRouteArgs& a, const RouteShared<kThreads>& sh, const int (&model)[kPer],
+                                             const int (&rank)[kPer]) {
+    const RouteArgs& r = a.route;
+    const int tid = threadIdx.x, n = static_cast<int>(r.n_tok), per = (n + kThreads - 1) / kThreads, i0 = tid * per;
+    for (int j = tid; j < kLossCounters; j += kThreads) a.counters[j] = 0u;
+    if (tid <= r.K) {
+        r.plan->off[tid] = sh.off[tid];
+        if (tid < r.K) r.plan->counts[tid] = sh.tot[tid];
     }
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         if (j >= per || i0 + j >= n) continue;
+        const int slot = model[j] >= 0 ? sh.off[model[j]] + rank[j] : -1;
         r.tok_model[i0 + j] = static_cast<int8_t>(model[j]);
-        if (model[j] >= 0) continue;
-        r.tok_slot[i0 + j] = -1;
+        r.tok_slot[i0 + j] = slot;
+        if (slot >= 0) { r.slot_tok[slot] = i0 + j; continue; }
         if (a.tok_loss) a.tok_loss[i0 + j] = 0.f;
         if (a.lse) a.lse[i0 + j] = 0.f;
     }
-    write_shapes(a, sh_off);
+    for (int k = 0; k < r.K; ++k)
+        for (int s = sh.off[k] + sh.tot[k] + tid; s < sh.off[k + 1]; s += kThreads) r.slot_tok[s] = -1;
+    write_shapes(a, sh.off);
+}
+
+// One block routes a whole batch of up to kLossRouteTokens tokens, in place of four memsets and three routing launches.
+__global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
+    begin();
+    __shared__ RouteShared<1024> sh;
+    int model[kLossRouteTokens / 1024], rank[kLossRouteTokens / 1024];
+    route_tokens(a.route, true, sh, model, rank);
+    write_routes(a, sh, model, rank);
 }
 
 // One warp's list: ascending, distinct vocabulary indexes with their teacher probabilities q.  Entries with a negative id are
@@ -308,25 +319,18 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
     if (lane == 0) a.cnt_p[slot] = n;
 }
 
-// One warp per packed row and per token: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
+// One warp per packed row and per token, w: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
 // zeros for a masked token's gradient row; with teacher's lists, every second warp takes a row's list.
-__global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
-    begin();
-    __shared__ int sh_id[8][kMaxTop];
-    __shared__ float sh_q[8][kMaxTop];
-    long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+__device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w, bool list, int n_slots, int tok, bool masked,
+                                           int (*sh_id)[kMaxTop], float (*sh_q)[kMaxTop]) {
     const int lane = threadIdx.x & 31, n16 = a.H >> 3;
-    const bool list = a.n_top > 0 && (w & 1);
-    if (a.n_top > 0) w >>= 1;
-    const int n_slots = a.plan->off[a.K];
-    const int tok = w < a.max_slots ? a.slot_tok[w] : -1;      // (not written beyond off[K]: not used there)
     if (list) {
         if (w >= n_slots) return;                              // whole warps leave: only warp-wide barriers below
         if (tok < 0) { if (lane == 0) a.cnt_p[w] = 0; return; }
         warp_list(a, w, tok, sh_id, sh_q);
         return;
     }
-    if (a.dHidden != nullptr && w < a.n_tok && a.tok_slot[w] < 0) {
+    if (a.dHidden != nullptr && masked) {
         uint4* dst = reinterpret_cast<uint4*>(a.dHidden + w * a.H);
         for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
     }
@@ -346,6 +350,54 @@ __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
         for (int u = 0; u < 8; ++u) if (j0 + 32 * u < n16) dst[j0 + 32 * u] = v[u];
     }
     if (lane == 0) a.target_p[w] = a.target ? a.target[tok] : -1;
+}
+
+__global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
+    begin();
+    __shared__ int sh_id[8][kMaxTop];
+    __shared__ float sh_q[8][kMaxTop];
+    long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+    const bool list = a.n_top > 0 && (w & 1);
+    if (a.n_top > 0) w >>= 1;
+    const int tok = w < a.max_slots ? a.slot_tok[w] : -1;      // (not written beyond off[K]: not used there)
+    const bool masked = a.dHidden != nullptr && w < a.n_tok && a.tok_slot[w] < 0;
+    gather_row(a, w, list, a.plan->off[a.K], tok, masked, sh_id, sh_q);
+}
+
+// Up to kLossPackTokens tokens: routing and packing in one launch.  Every block routes all tokens for itself (a few memory
+// latencies, no waiting for another block); block 0 writes the result down and weighs the schedules while the others pack.
+constexpr int kLossPackTokens = 1024;
+__global__ void __launch_bounds__(256) k_loss_pack(LossRouteArgs r, LossGatherArgs a) {
+    begin();
+    __shared__ RouteShared<256> sh;
+    __shared__ short sh_tok[kLossPackTokens];                  // tokens by model and rank
+    __shared__ signed char sh_model[kLossPackTokens];
+    __shared__ int sh_id[8][kMaxTop];
+    __shared__ float sh_q[8][kMaxTop];
+    constexpr int kPer = kLossPackTokens / 256;
+    int model[kPer], rank[kPer];
+    route_tokens(r.route, blockIdx.x == 0, sh, model, rank);
+    if (blockIdx.x == 0) { write_routes(r, sh, model, rank); return; }
+    const int n = static_cast<int>(r.route.n_tok), per = (n + 255) / 256, i0 = threadIdx.x * per;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        if (j >= per || i0 + j >= n) continue;
+        sh_model[i0 + j] = static_cast<signed char>(model[j]);
+        if (model[j] < 0) continue;
+        int first = 0;
+        for (int k = 0; k < model[j]; ++k) first += sh.tot[k];
+        sh_tok[first + rank[j]] = static_cast<short>(i0 + j);
+    }
+    __syncthreads();
+    long long w = static_cast<long long>(blockIdx.x - 1) * 8 + (threadIdx.x >> 5);
+    const bool list = a.n_top > 0 && (w & 1);
+    if (a.n_top > 0) w >>= 1;
+    int tok = -1, first = 0;
+    for (int k = 0; k < r.route.K; ++k) {
+        if (w >= sh.off[k] && w < sh.off[k] + sh.tot[k]) tok = sh_tok[first + static_cast<int>(w) - sh.off[k]];
+        first += sh.tot[k];
+    }
+    gather_row(a, w, list, sh.off[r.route.K], tok, w < n && sh_model[w] < 0, sh_id, sh_q);
 }
 
 // One warp per packed row: merge the vocabulary splits' statistics (one lane per split), then the row's loss and what
@@ -504,13 +556,23 @@ constexpr int kGradVecs = 4;
 constexpr int kGradCols = 256 * 8 * kGradVecs;
 __global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
     begin();
-    int row0, rows;
-    span_resolve(a.span, row0, rows);
-    rows = span_slab_rows(a.span, rows);                       // padding rows beyond the last slab are read by nobody's sums
+    int row0 = 0, rows;
+    const bool joint = a.span.model < 0;
+    if (joint) {
+        rows = a.span.plan->off[a.K];
+    } else {
+        span_resolve(a.span, row0, rows);
+        rows = span_slab_rows(a.span, rows);                   // padding rows beyond the last slab are read by nobody's sums
+    }
     const int per_row = (a.cols + kGradCols - 1) / kGradCols;
     for (int item = blockIdx.x; item < rows * per_row; item += gridDim.x) {      // at most 18432 rows of 2^18 columns
         const int r = item / per_row, c_lo = (item - r * per_row) * kGradCols, c_first = c_lo + threadIdx.x * 8;
         const int slot = row0 + r;
+        if (joint) {
+            int k = 0;
+            while (k + 1 < a.K && slot >= a.span.plan->off[k + 1]) ++k;
+            if (slot - a.span.plan->off[k] >= (a.span.plan->counts[k] + kTileK - 1) / kTileK * kTileK) continue;
+        }
         uint4* row = reinterpret_cast<uint4*>(a.Z + static_cast<long long>(r) * a.ld);
         const float* tm = a.tile_max + static_cast<long long>(r) * a.n_tiles;
         uint4 raw[kGradVecs];
@@ -620,25 +682,26 @@ __global__ void __launch_bounds__(256) k_cast_dw(const float4* __restrict__ src,
 
 }  // namespace
 
-cudaError_t launch_loss_route(const LossRouteArgs& a, cudaStream_t stream, int* n_launches) {
-    cudaError_t e;
-    if (a.route.n_tok <= kLossRouteTokens) {
-        *n_launches += 1;
-        return launch(k_loss_route, dim3(1), 1024, stream, a);
-    }
-    const size_t n = static_cast<size_t>(a.route.n_tok);
-    if (a.tok_loss && (e = cudaMemsetAsync(a.tok_loss, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
-    if (a.lse && (e = cudaMemsetAsync(a.lse, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
-    if ((e = cudaMemsetAsync(a.route.slot_tok, 0xff, sizeof(int) * a.max_slots, stream)) != cudaSuccess) return e;
-    if ((e = cudaMemsetAsync(a.counters, 0, sizeof(unsigned) * kLossCounters, stream)) != cudaSuccess) return e;
-    if ((e = launch_route(a.route, stream, n_launches)) != cudaSuccess) return e;
+cudaError_t launch_loss_pack(const LossRouteArgs& a, const LossGatherArgs& g, cudaStream_t stream, int* n_launches) {
+    const long long work = (g.max_slots > g.n_tok ? g.max_slots : g.n_tok) * (g.n_top > 0 ? 2 : 1);
+    const unsigned blocks = static_cast<unsigned>((work + 7) / 8);
     *n_launches += 1;
-    return launch(k_loss_shapes, dim3(1), 1024, stream, a);
-}
-
-cudaError_t launch_loss_gather(const LossGatherArgs& a, cudaStream_t stream) {
-    const long long n = (a.max_slots > a.n_tok ? a.max_slots : a.n_tok) * (a.n_top > 0 ? 2 : 1);
-    return launch(k_loss_gather, dim3(static_cast<unsigned>((n + 7) / 8)), 256, stream, a);
+    if (g.n_tok <= kLossPackTokens) return launch(k_loss_pack, dim3(blocks + 1), 256, stream, a, g);
+    cudaError_t e;
+    if (g.n_tok <= kLossRouteTokens) {
+        e = launch(k_loss_route, dim3(1), 1024, stream, a);
+    } else {
+        const size_t n = static_cast<size_t>(g.n_tok);
+        if (a.tok_loss && (e = cudaMemsetAsync(a.tok_loss, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
+        if (a.lse && (e = cudaMemsetAsync(a.lse, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
+        if ((e = cudaMemsetAsync(a.route.slot_tok, 0xff, sizeof(int) * a.max_slots, stream)) != cudaSuccess) return e;
+        if ((e = cudaMemsetAsync(a.counters, 0, sizeof(unsigned) * kLossCounters, stream)) != cudaSuccess) return e;
+        if ((e = launch_route(a.route, stream, n_launches)) != cudaSuccess) return e;
+        e = launch(k_loss_shapes, dim3(1), 1024, stream, a);
+    }
+    if (e != cudaSuccess) return e;
+    *n_launches += 1;
+    return launch(k_loss_gather, dim3(blocks), 256, stream, g);
 }
 
 cudaError_t launch_loss_rows(const LossRowArgs& a, cudaStream_t stream) {
@@ -658,7 +721,7 @@ cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaSt
 }
 
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {
-    return launch(k_store_parts, dim3(a.span.row_cap, (a.H + 1023) / 1024), 256, stream, a);
+    return launch(k_store_parts, dim3(a.bound, (a.H + 1023) / 1024), 256, stream, a);
 }
 
 cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream) {

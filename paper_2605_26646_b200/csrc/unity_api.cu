@@ -450,7 +450,9 @@ struct LossLayout {
 // entries are recomputed one after the other.  rows = 0: no gradient.
 struct LossBlocks {
     int rows, cols;
-    bool keep, dw_scratch;       // dw_scratch: fp32 copy of one dW, for bf16 sums over several blocks that are rounded once
+    bool keep;
+    bool joint;                  // one block holds the packed rows of every model
+    bool dw_scratch;             // fp32 copy of one dW, for bf16 sums over several blocks that are rounded once
 };
 
 // Rows of the buffer that takes the parts of dHidden (split_shape): a block of rows, or the parts of fewer rows.
@@ -504,11 +506,13 @@ LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int
     return L;
 }
 
-// Blocks of equal size, at most kStashRows rows each.
-LossBlocks keep_blocks(long long n_tok, int V, bool dw_sums, int most) {
+// Blocks of equal size, at most `most` rows each; all models' rows in one where they fit.
+LossBlocks keep_blocks(long long n_tok, int V, int K, bool dw_sums, int most) {
+    const int cols = static_cast<int>(up(V, kTileN));
+    if (max_slots_of(n_tok, K) <= most) return LossBlocks{static_cast<int>(max_slots_of(n_tok, K)), cols, true, true, false};
     const long long bound = static_cast<long long>(up(n_tok, kTileM)), n = (bound + most - 1) / most;
     const int rows = static_cast<int>(up((bound + n - 1) / (n > 0 ? n : 1), kTileM));
-    return LossBlocks{rows, static_cast<int>(up(V, kTileN)), true, dw_sums && bound > rows};
+    return LossBlocks{rows, cols, true, false, dw_sums && bound > rows};
 }
 
 int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
@@ -534,18 +538,18 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     // the largest blocks that fit: with kept logits down to kMinKeepRows rows (smaller ones read and write dW too often),
     // then pieces of recomputed ones
     const long long rows_bound = static_cast<long long>(up(r->n_tok, kTileM));
-    LossBlocks B{0, 0, false, false};
+    LossBlocks B{0, 0, false, false, false};
     LossLayout L;
     bool fits = false;
     if (!want) L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, B, &fits);
     for (int most = kStashRows; want && !fits && most >= kMinKeepRows; most /= 2) {
-        B = keep_blocks(r->n_tok, V, want_w && c.bf16_dw, most);
+        B = keep_blocks(r->n_tok, V, K, want_w && c.bf16_dw, most);
         L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, B, &fits);
     }
     if (want && !fits) {
         int cr = static_cast<int>(rows_bound < kChunkRows ? rows_bound : kChunkRows), cv = wanted_chunk_vocab(V);
         for (;;) {
-            B = LossBlocks{cr, cv, false, want_w && c.bf16_dw && rows_bound > cr};
+            B = LossBlocks{cr, cv, false, false, want_w && c.bf16_dw && rows_bound > cr};
             L = carve_loss(ctx->ws, ctx->ws_bytes, r->n_tok, H, V, K, c.n_top, B, &fits);
             if (fits) break;
             if (cr > kMinChunkRows && (cr >= cv || cv <= kMinChunkVocab)) cr = static_cast<int>(up(cr / 2, kTileM));
@@ -572,7 +576,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     SyncCounters counters{L.sync_counters, 0, kLossCounters};
     // loss_rows needs its counter: the rendezvous of the GEMMs may go without, so theirs come second
     unsigned* tickets = counters.base;
-    const long long n_tickets = B.keep ? K * ((rows_bound + B.rows - 1) / B.rows) : 1;
+    const long long n_tickets = B.keep && !B.joint ? K * ((rows_bound + B.rows - 1) / B.rows) : 1;
     if (n_tickets > kLossCounters) return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: %lld blocks of rows", n_tickets);
     counters.used = static_cast<int>(n_tickets);
 
@@ -586,15 +590,13 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     ra.tok_slot = L.tok_slot; ra.slot_tok = L.slot_tok; ra.tok_model = L.tok_model; ra.status = ctx->d_status;
     lr.split = SplitParams{B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0, (H + cols_dh - 1) / cols_dh,
                            (V + kTileK - 1) / kTileK, ctx->sm_count / c_dh, gemm_tile_rows(c_dh)};
-    lr.block_rows = B.keep && !few ? B.rows : cap_all;
+    lr.block_rows = B.keep && !B.joint ? B.rows : cap_all;
     lr.max_slots = L.max_slots; lr.shapes = L.shapes; lr.counters = L.sync_counters; lr.tok_loss = c.tok_loss; lr.lse = c.lse;
-    CUDA_TRY(ctx, launch_loss_route(lr, st, &nl));
     __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
     const LossGatherArgs ga{L.plan, L.slot_tok, L.tok_slot, K, V, H, r->n_tok, L.max_slots,
                             static_cast<const __nv_bfloat16*>(r->hidden), r->target, L.hp, dH, L.target_p, c.n_top, c.logits,
                             r->inv_temperature, c.top_ids, c.top_vals, L.ids_p, L.cnt_p, L.q_p, ctx->d_status};
-    CUDA_TRY(ctx, launch_loss_gather(ga, st));
-    nl += 1;
+    CUDA_TRY(ctx, launch_loss_pack(lr, ga, st, &nl));
 
     CUtensorMap tm_hp_k, tm_hp_mn;
     if ((rc = make_tmap(ctx, &tm_hp_k, L.hp, H, L.max_slots, static_cast<uint64_t>(H) * 2, kBoxRows))) return rc;
@@ -609,7 +611,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         g.n_tiles = fwd.n_tiles; g.k_iters = H / kTileK; g.n_cols = V;
         g.stats = L.stats; g.target_p = L.target_p; g.scale = r->inv_temperature;
         g.top_ids = L.ids_p; g.top_cnt = L.cnt_p; g.top_z = L.top_z; g.top_n = c.n_top;
-        if (!whole) { g.stash = reinterpret_cast<uint16_t*>(L.G); g.ldz = B.cols; g.tile_max = L.tile_max; }
+        if (B.keep) { g.stash = reinterpret_cast<uint16_t*>(L.G); g.ldz = B.cols; g.tile_max = L.tile_max; g.stash_by_slot = B.joint; }
         // (rows of a single round start together anyway: the rendezvous would only cost its round trip)
         const long long rows = rows_bound < span.row_cap ? rows_bound : span.row_cap;
         gemm_common(ctx, g, UNITY_PROF_FWD_GEMM, &counters, ctx->fwd_sync != 0 && rows > static_cast<long long>(fwd.gmax) * fwd.tile_rows);
@@ -631,7 +633,20 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     auto w_map = [&](CUtensorMap* tm, int k, int box) {
         return make_tmap(ctx, tm, r->W[k], H, V, static_cast<uint64_t>(H) * 2, box);
     };
-    if (!B.keep) {
+    LossGradArgs lg;
+    memset(&lg, 0, sizeof(lg));
+    lg.Z = reinterpret_cast<uint16_t*>(L.G); lg.ld = B.cols; lg.span = RowSpan{L.plan, -1, 0, B.rows}; lg.K = K; lg.cols = V;
+    lg.n_tiles = fwd.n_tiles; lg.tile_max = L.tile_max; lg.c2 = r->inv_temperature * 1.4426950408889634f;
+    lg.target_p = L.target_p; lg.row_lse = L.row_lse; lg.coef_p = L.coef_p; lg.coef_g = L.coef_g; lg.target_g = L.target_g;
+    lg.uniform = c.smoothing / static_cast<float>(V);
+    lg.n_top = c.n_top; lg.ids_p = L.ids_p; lg.cnt_p = L.cnt_p; lg.top_g = L.top_z;
+    auto convert = [&](const RowSpan& span) {
+        lg.span = span;
+        ProfScope ps(ctx, UNITY_PROF_GRAD_GEMM);
+        nl += 1;
+        return launch_loss_grad_inplace(lg, ctx->sm_count, st);
+    };
+    if (!B.keep || B.joint) {
         for (int k = 0; k < K; ++k) {
             CUtensorMap tmB;
             if ((rc = w_map(&tmB, k, kTileN / c_fwd))) return rc;
@@ -639,6 +654,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         }
         CUDA_TRY(ctx, launch_loss_rows(la, st));
         nl += 1;
+        if (B.joint) CUDA_TRY(ctx, convert(lg.span));
     }
     // per model and block of rows: G = dL/dz in bf16, dHidden = G W, dW += G^T hidden
     for (int k = 0; want && k < K; ++k) {
@@ -648,23 +664,21 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         if ((rc = w_map(&tm_W_f, k, kTileN / c_fwd)) || (rc = w_map(&tm_W_k, k, kTileN / c_grad)) || (rc = w_map(&tm_W_mn, k, kTileK))) return rc;
         for (long long c0 = 0; c0 < rows_bound; c0 += B.rows) {
             // (a full block's span has block_rows as its bound even where fewer rows are left: the schedules go by it)
-            const int nc = few ? kCtaM : B.rows;
-            const RowSpan chunk{L.plan, k, static_cast<int>(c0), nc};
+            const int bound = static_cast<int>(rows_bound < B.rows ? rows_bound : B.rows);    // rows a model can have in it
+            const RowSpan chunk{L.plan, k, static_cast<int>(c0), few ? kCtaM : (B.joint ? cap_all : B.rows)};
             // a rendezvous per tile (about 2 us of the producer's time) costs more than it saves where a dW tile has few slabs
-            const bool short_k = nc <= kShortRows;
+            const bool short_k = bound <= kShortRows;
             int base = V, n_pieces = 1;
-            if (B.keep) {
+            if (B.joint) {
+                // the forward has run for all models
+            } else if (B.keep) {
                 CUDA_TRY(ctx, forward(chunk, false, tm_W_f));
                 LossRowArgs lb = la;
                 lb.block = chunk;
                 if (k > 0 || c0 > 0) lb.ticket = tickets++;
                 CUDA_TRY(ctx, launch_loss_rows(lb, st));
-                const LossGradArgs lg{reinterpret_cast<uint16_t*>(L.G), B.cols, chunk, V, fwd.n_tiles, L.tile_max,
-                                      r->inv_temperature * 1.4426950408889634f, L.target_p, L.row_lse, L.coef_p, L.coef_g,
-                                      L.target_g, c.smoothing / static_cast<float>(V), c.n_top, L.ids_p, L.cnt_p, L.top_z};
-                ProfScope ps(ctx, UNITY_PROF_GRAD_GEMM);
-                CUDA_TRY(ctx, launch_loss_grad_inplace(lg, ctx->sm_count, st));
-                nl += 2;
+                CUDA_TRY(ctx, convert(chunk));
+                nl += 1;
             } else {
                 vocab_chunks(V, B.cols, &base, &n_pieces);
             }
@@ -702,14 +716,14 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     nl += 1;
                 }
                 CUtensorMap tm_G_k, tm_G_mn;
-                if ((rc = make_tmap(ctx, &tm_G_k, L.G, vc, nc, static_cast<uint64_t>(B.cols) * 2, kBoxRows))) return rc;
-                if ((rc = make_tmap(ctx, &tm_G_mn, L.G, vc, nc, static_cast<uint64_t>(B.cols) * 2, kTileK))) return rc;
+                if ((rc = make_tmap(ctx, &tm_G_k, L.G, vc, B.rows, static_cast<uint64_t>(B.cols) * 2, kBoxRows))) return rc;
+                if ((rc = make_tmap(ctx, &tm_G_mn, L.G, vc, B.rows, static_cast<uint64_t>(B.cols) * 2, kTileK))) return rc;
                 if (want_h) {
                     GemmArgs h;
                     memset(&h, 0, sizeof(h));
                     h.pdl = 1;
                     h.mma_n = mma_n;
-                    h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1; h.shapes = B.keep ? L.shapes : nullptr;
+                    h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1; h.shapes = B.keep ? L.shapes : nullptr; h.stash_by_slot = B.joint;
                     h.n_tiles = lr.split.n_tiles; h.k_iters = (vc + kTileK - 1) / kTileK;
                     h.group_m = ctx->chunk_group[1] / c_dh > 0 ? ctx->chunk_group[1] / c_dh : 1;
                     h.b_k0 = v0; h.n_cols = H; h.C = L.parts; h.ldc = H; h.beta = v0 > 0; h.g_wide_store = 1;
@@ -720,14 +734,14 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         nl += 1;
                     }
                     if (ci + 1 == n_pieces) {
-                        const StoreArgs sa{L.parts, L.slot_tok, chunk, H, h.shapes, dH};
+                        StoreArgs sa{L.parts, L.slot_tok, chunk, H, h.shapes, bound, dH};
                         CUDA_TRY(ctx, launch_store_parts(sa, st));
                         nl += 1;
                     }
                 }
                 if (want_w) {
                     // few rows: a tile's epilogue must overlap the next tile's products, which only the narrow form does
-                    const bool wide = two_blocks && c_dw == 2 && nc > 1024;
+                    const bool wide = two_blocks && c_dw == 2 && bound > 1024;
                     const int tile_v = gemm_tile_rows(c_dw), vt = (vc + tile_v - 1) / tile_v, cols = (wide ? 2 : 1) * mma_n;
                     // the last few vocabulary tiles as a launch of narrow ones where they would open one more wave (as in
                     // the policy update: V = 151936 is eight waves of 74 tiles and two more) and that wave is longer than a launch
@@ -744,7 +758,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         memset(&w, 0, sizeof(w));
                         w.pdl = 1;
                         w.mma_n = part == 0 ? mma_n : narrow_n;
-                        w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = t1 - t0; w.shapes = L.shapes;
+                        w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = t1 - t0; w.shapes = L.shapes; w.stash_by_slot = B.joint;
                         w.n_tiles = (H + (wide_here ? 2 : 1) * w.mma_n - 1) / ((wide_here ? 2 : 1) * w.mma_n); w.k_iters = 1;
                         w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
                         w.a_row0 = row0; w.m_rows = n_here; w.n_cols = H; w.ldc = H;
@@ -1508,7 +1522,7 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
 // ------------------------------------------------------------------------------------------------
 size_t unity_token_loss_workspace_bytes(int64_t n_tok, int32_t H, int32_t V, int32_t K, int32_t n_top, int32_t backward) {
     if (n_tok < 0 || n_tok > 0x7fffff00LL || H <= 0 || V <= 0 || K <= 0 || n_top < 0 || n_top > UNITY_MAX_TOP) return 0;
-    const LossBlocks B = backward ? keep_blocks(n_tok, V, true, kStashRows) : LossBlocks{0, 0, false, false};
+    const LossBlocks B = backward ? keep_blocks(n_tok, V, K, true, kStashRows) : LossBlocks{0, 0, false, false, false};
     return carve_loss(nullptr, ~size_t(0), n_tok, H, V, K, n_top, B, nullptr).bytes;
 }
 
