@@ -163,10 +163,20 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     GemmArgs g = in;
     if (in.span.plan == nullptr) return g;
     int slot0, n_rows;
+    // token losses: both schedules are read beside the plan, not after it (a memory latency less in every launch)
+    const int k = in.span.model;
+    union { int4 v[2]; FwdShape f; } full, last;
+    int4 split = make_int4(0, 0, 0, 0);
+    long long stats_base = 0;
+    if (in.shapes != nullptr && in.span_mode == kSpanForward) {
+        const int4* f = reinterpret_cast<const int4*>(in.shapes->fwd[k]);
+        full.v[0] = f[0]; full.v[1] = f[1]; last.v[0] = f[2]; last.v[1] = f[3];
+        stats_base = in.span.plan->stats_base[k];
+    }
+    if (in.shapes != nullptr && in.span_mode == kSpanRowsM) split = *reinterpret_cast<const int4*>(in.shapes->dh[k]);
     span_resolve(in.span, slot0, n_rows);
     if (in.span_mode == kSpanForward) {
-        const FwdShape fs = in.shapes ? in.shapes->fwd[in.span.model][n_rows == in.span.row_cap ? 0 : 1]
-                                      : forward_shape(in.fwd, n_rows);
+        const FwdShape fs = in.shapes == nullptr ? forward_shape(in.fwd, n_rows) : (n_rows == in.span.row_cap ? full.f : last.f);
         g.a_row0 = slot0;
         g.m_rows = n_rows;
         g.m_tiles = n_rows / TILE_ROWS;
@@ -183,7 +193,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
             g.stash = in.stash + static_cast<long long>(slot0) * in.ldz;
             g.tile_max = in.tile_max + static_cast<long long>(slot0) * in.n_tiles;
         }
-        if (in.stats_from_plan) g.stats = in.stats + in.span.plan->stats_base[in.span.model];
+        if (in.stats_from_plan) g.stats = in.stats + (in.shapes ? stats_base : in.span.plan->stats_base[k]);
     } else if (in.span_mode == kSpanRowsA) {
         g.a_row0 = in.a_row0 + slot0;
         g.m_rows = n_rows;
@@ -217,8 +227,8 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
         g.m_tiles = n_rows / TILE_ROWS;
         if (in.stash_by_slot) g.a_row0 = slot0;
         if (in.shapes) {
-            const SplitShape sp = in.shapes->dh[in.span.model][n_rows == in.span.row_cap ? 0 : 1];
-            g.k_splits = sp.splits; g.k_per_split = sp.per_split;
+            const bool whole = n_rows == in.span.row_cap;
+            g.k_splits = whole ? split.x : split.z; g.k_per_split = whole ? split.y : split.w;
             g.c_split = static_cast<long long>(n_rows) * in.ldc;
         }
     } else if (in.span_mode == kSpanRowsK) {
@@ -304,10 +314,10 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
 // ref need not be the maximum: it is 0 where the first tile's maximum lies within kRefBelow octaves below and kRefRoom above
 // that, else that maximum, and later a tile's maximum more than kRefRoom octaves above it.  So a tile is read from tensor memory once (a maximum first and the sum after it would read it twice: 276
 // against 353 us at 801 x 896 x 151936, where the epilogue is the bound), no sum exceeds 2^kRefRoom * V, and for a backward
-// pass that does not recompute the logits (ref - z) + kRefRoom octaves is kept in steps of 2^-10 octaves, 16 bits.  The integer
-// costs as much memory as bf16 but is off by at most half a step whatever its size: p is off by a factor of 2^(2^-11), 3.4e-4,
-// where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 48 octaves or more below ref, 40 below the row's
-// maximum, count as 48.
+// pass that does not recompute the logits (ref - z) + kRefRoom octaves is kept in steps of 2^-9 octaves, 16 bits.  The integer
+// costs as much memory as bf16 but is off by at most half a step whatever its size: p is off by a factor of 2^(2^-10), 6.8e-4,
+// where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 96 octaves or more below ref, 64 below the row's
+// maximum, count as 96.
 struct LossRow {
     float ref, z_tgt;
     uint64_t s, z2;
@@ -410,16 +420,17 @@ __device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w,
                 }
             }
         };
+        // (one copy of the body, its registers moved on: two copies cost a launch of few tiles more in instruction fetches)
+        ptx::tmem_ld_wait_for(ra);
 #pragma unroll 1
-        for (int c = 0; c * 32 < n_tile; c += 2) {
+        for (int c = 0; c * 32 < n_tile; ++c) {
             const bool more = (c + 1) * 32 < n_tile;
-            ptx::tmem_ld_wait_for(ra);
             if (more) ptx::tmem_ld_32x32(taddr + (c + 1) * 32, rb);
             work(ra, c);
             if (!more) break;
             ptx::tmem_ld_wait_for(rb);
-            if ((c + 2) * 32 < n_tile) ptx::tmem_ld_32x32(taddr + (c + 2) * 32, ra);
-            work(rb, c + 1);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) ra[j] = rb[j];
         }
         // A row whose maximum rose past the room takes it as its new reference and its warp works through the tile again
         // (the list cursor has moved on: its logits are written; the target's is the same).  A second time is enough.

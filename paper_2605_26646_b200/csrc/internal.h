@@ -140,13 +140,14 @@ constexpr int kMaxKSplits = 32;
 // The schedules of a token loss, per model: [0] of a full block of rows (RowSpan::row_cap of them), [1] of the model's last
 // one.  Written once per call by the kernel that counts the rows (a warp weighs the candidates side by side; evaluated where
 // they are used they cost every launch several microseconds).
-struct LossShapes {
+struct __align__(16) LossShapes {
     FwdShape fwd[UNITY_MAX_MODELS][2];
     SplitShape dh[UNITY_MAX_MODELS][2];
 };
-constexpr float kStashSteps = 1024.f;   // steps per octave of a kept logit (GemmArgs::stash) ...
-constexpr float kRefRoom = 16.f;        // ... counted down from this many octaves above its reference
-constexpr float kRefBelow = 8.f;        // a row whose first columns stay within this many octaves below 0 takes 0 as reference
+static_assert(sizeof(FwdShape) == 32 && sizeof(SplitShape) == 8, "read as 16-byte and 8-byte vectors");
+constexpr float kStashSteps = 512.f;   // steps per octave of a kept logit (GemmArgs::stash) ...
+constexpr float kRefRoom = 32.f;        // ... counted down from this many octaves above its reference
+constexpr float kRefBelow = 32.f;       // a row whose first columns stay within this many octaves below 0 takes 0 as reference
 
 // ----------------------------------------------------------------------------------------------
 // GEMM  C[m, n] = sum_k A[m, k] * B[n, k]   (bf16 operands, K-major or MN-major, fp32 accumulation in TMEM)

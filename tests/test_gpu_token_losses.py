@@ -6,9 +6,9 @@ Tolerances, derived.  u = 2^-24 and b = 2^-8 are the largest relative errors of 
   lse        ez, plus V additions in chunks and exponentials of relative error 2^-21: 2^-17 in all on log s, plus 2u |lse|
   l          as many times the sum of its terms' weights as it has lse and z: 2 (ez + 2^-17) * mass, plus u times the terms
   G = dL/dz  p is off by a factor of e^(2 ez + 2^-17); G is written in bf16 (b), a block that was kept between the two sweeps
-             in steps of 2^-10 octaves (half a step: ln2 2^-11): relative to the terms that make G up,
-             eg = b + 2^-11 + 2 ez + 2^-16, and a kept logit 40 octaves or more below the row's maximum may count as
-             40: at most 2^-40 of the row's coefficient
+             in steps of 2^-9 octaves (half a step: ln2 2^-10): relative to the terms that make G up,
+             eg = b + 2^-10 + 2 ez + 2^-16, and a kept logit 64 octaves or more below the row's maximum may count as
+             64: at most 2^-64 of the row's coefficient
   dHidden    eg sum_v |G||W|, plus fp32 sums and the output's rounding: b |dHidden|
   dW         eg sum_i |G||h|, the same; f32: without the output's rounding
 The fp32 sums of the products are covered by 2^-12 of the sums of magnitudes (V/16 steps of 2u).
@@ -111,12 +111,12 @@ def oracle(p, op, weight=True, norm=None, tau=1.0, smoothing=0.0, z_loss=0.0, mo
                 own[np.arange(i.size), p.target.numpy()[i]] += hard
             mass[i] = cp
         terms[i] = np.abs(c)[:, None] * (cp[:, None] * P + own)
-        o.setdefault("floor", np.zeros(N))[i] = np.abs(c) * cp * 2.0 ** -40
+        o.setdefault("floor", np.zeros(N))[i] = np.abs(c) * cp * 2.0 ** -64
     big = np.abs(o["lse"]) + np.abs(o["tok_loss"])
     o["tol_lse"] = ez + 2.0 ** -17 + 2 * U * np.abs(o["lse"])
     o["tol_l"] = (2 * ez + 2.0 ** -16) * mass + 8 * U * (1 + big * (1 + mass) + (z_loss * o["lse"] ** 2 if q is None else 0))
     # a sure row's G is a small difference of p and its target: p's own error counts, not G's
-    eg = 2.0 ** -11 + 2 * ez[:, None] + 2.0 ** -16
+    eg = 2.0 ** -10 + 2 * ez[:, None] + 2.0 ** -16
     o["dG"] = B * np.abs(o["G"]) * (1 + B) + eg * terms + (o["floor"][:, None] if "floor" in o else 0)
     return o
 
