@@ -515,6 +515,14 @@ LossBlocks keep_blocks(long long n_tok, int V, int K, bool dw_sums, int most) {
     return LossBlocks{rows, cols, true, false, dw_sums && bound > rows};
 }
 
+// The tensor core's accumulation cuts where fp32 addition would round: a sum of H products loses on average 1.6e-8 of its
+// size per step of 16 (measured: 3.0e-7, 9.7e-7, 1.58e-6, 3.62e-6 at H = 256, 896, 1536, 3584, whatever the sign), because a
+// step cuts in proportion to the partial sum, which on average has grown half way.  The logits' scale takes that mean back,
+// which leaves the cuts' random part: a per-token loss at H = 3584 is then off by 5e-7 of its size and not by 2.5e-6.
+float accumulator_scale(float inv_temperature, int H) {
+    return static_cast<float>(inv_temperature * (1.0 + 1.6e-8 * (H / 16) + 4e-8));
+}
+
 int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     const int K = r->K, H = r->H, V = r->V;
     const bool want_h = c.dHidden != nullptr, want_w = c.dW != nullptr, want = want_h || want_w;
@@ -528,6 +536,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     const DeviceGuard dev(ctx->device);
     if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
     cudaStream_t st = ctx->stream;
+    const float scale = accumulator_scale(r->inv_temperature, r->H);
     const size_t dw_bytes = static_cast<size_t>(V) * H * (c.bf16_dw ? 2 : 4);
     if (r->n_tok == 0) {
         CUDA_TRY(ctx, cudaMemsetAsync(c.loss, 0, sizeof(float) * K, st));
@@ -609,7 +618,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         g.span = span; g.span_mode = kSpanForward; g.stats_from_plan = whole ? 1 : 0; g.fwd = fwd; g.shapes = L.shapes;
         g.m_tiles = 1;                                   // set by the kernel
         g.n_tiles = fwd.n_tiles; g.k_iters = H / kTileK; g.n_cols = V;
-        g.stats = L.stats; g.target_p = L.target_p; g.scale = r->inv_temperature;
+        g.stats = L.stats; g.target_p = L.target_p; g.scale = scale;
         g.top_ids = L.ids_p; g.top_cnt = L.cnt_p; g.top_z = L.top_z; g.top_n = c.n_top;
         if (B.keep) { g.stash = reinterpret_cast<uint16_t*>(L.G); g.ldz = B.cols; g.tile_max = L.tile_max; g.stash_by_slot = B.joint; }
         // (rows of a single round start together anyway: the rendezvous would only cost its round trip)
@@ -623,7 +632,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     memset(&la, 0, sizeof(la));
     la.block = RowSpan{L.plan, -1, 0, cap_all}; la.plan = L.plan; la.shapes = L.shapes; la.tile_rows = fwd.tile_rows;
     la.ticket = tickets++; la.max_slots = L.max_slots; la.K = K; la.V = V;
-    la.stats = L.stats; la.slot_tok = L.slot_tok; la.tok_model = L.tok_model; la.scale = r->inv_temperature;
+    la.stats = L.stats; la.slot_tok = L.slot_tok; la.tok_model = L.tok_model; la.scale = scale;
     la.tok_weight = c.tok_weight; la.has_norm = c.norm != nullptr;
     for (int k = 0; k < K && c.norm; ++k) la.norm[k] = c.norm[k];
     la.smoothing = c.smoothing; la.z_loss = c.z_loss; la.n_top = c.n_top; la.kd = c.kd; la.hard = c.hard;
@@ -636,7 +645,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     LossGradArgs lg;
     memset(&lg, 0, sizeof(lg));
     lg.Z = reinterpret_cast<uint16_t*>(L.G); lg.ld = B.cols; lg.span = RowSpan{L.plan, -1, 0, B.rows}; lg.K = K; lg.cols = V;
-    lg.n_tiles = fwd.n_tiles; lg.tile_max = L.tile_max; lg.c2 = r->inv_temperature * 1.4426950408889634f;
+    lg.n_tiles = fwd.n_tiles; lg.tile_max = L.tile_max; lg.c2 = scale * 1.4426950408889634f;
     lg.target_p = L.target_p; lg.row_lse = L.row_lse; lg.coef_p = L.coef_p; lg.coef_g = L.coef_g; lg.target_g = L.target_g;
     lg.uniform = c.smoothing / static_cast<float>(V);
     lg.n_top = c.n_top; lg.ids_p = L.ids_p; lg.cnt_p = L.cnt_p; lg.top_g = L.top_z;
@@ -701,7 +710,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         g.plan_runs = 1;
                         g.fwd.gmax = runs / c_grad > 0 ? runs / c_grad : 1;
                     }
-                    g.b_row0 = v0; g.n_cols = vc; g.target_p = L.target_p; g.vocab0 = v0; g.scale = r->inv_temperature;
+                    g.b_row0 = v0; g.n_cols = vc; g.target_p = L.target_p; g.vocab0 = v0; g.scale = scale;
                     g.row_lse = L.row_lse; g.coef_p = L.coef_p; g.coef_g = L.coef_g; g.target_g = L.target_g;
                     g.uniform = c.smoothing / static_cast<float>(V);
                     g.G = L.G; g.ldg = B.cols; g.g_wide_store = B.cols % 16 == 0;
