@@ -589,8 +589,14 @@ class Context:
     def ppo_loss_fwd_bwd(self, *a, **kw):
         return unity_ppo_loss_fwd_bwd(self.ctx, *a, **kw)
 
-    def cross_entropy_fwd_bwd(self, *a, **kw):
-        return unity_cross_entropy_fwd_bwd(self.ctx, *a, **kw)
+    def _on_device(self, hidden):
+        if hidden.is_cuda and hidden.device.index != self.device:
+            raise ValueError(f"hidden is on {hidden.device}, the context on cuda:{self.device}")
 
-    def distill_fwd_bwd(self, *a, **kw):
-        return unity_distill_fwd_bwd(self.ctx, *a, **kw)
+    def cross_entropy_fwd_bwd(self, hidden, *a, **kw):
+        self._on_device(hidden)
+        return unity_cross_entropy_fwd_bwd(self.ctx, hidden, *a, **kw)
+
+    def distill_fwd_bwd(self, hidden, *a, **kw):
+        self._on_device(hidden)
+        return unity_distill_fwd_bwd(self.ctx, hidden, *a, **kw)

@@ -416,7 +416,8 @@ struct LossRouteArgs {
     int block_rows;            // rows of a full block (at least a batch's rows: one block)
     long long max_slots;
     LossShapes* shapes;
-    unsigned* counters;        // [kLossCounters]
+    unsigned* counters;        // [n_counters]
+    int n_counters;
     float *tok_loss, *lse;     // caller order, nullable
 };
 

@@ -205,7 +205,7 @@ __device__ __forceinline__ void write_routes(const LossRouteArgs& a, const Route
                                              const int (&rank)[kPer]) {
     const RouteArgs& r = a.route;
     const int tid = threadIdx.x, n = static_cast<int>(r.n_tok), per = (n + kThreads - 1) / kThreads, i0 = tid * per;
-    for (int j = tid; j < kLossCounters; j += kThreads) a.counters[j] = 0u;
+    for (int j = tid; j < a.n_counters; j += kThreads) a.counters[j] = 0u;
     if (tid <= r.K) {
         r.plan->off[tid] = sh.off[tid];
         if (tid < r.K) r.plan->counts[tid] = sh.tot[tid];
@@ -695,7 +695,7 @@ cudaError_t launch_loss_pack(const LossRouteArgs& a, const LossGatherArgs& g, cu
         if (a.tok_loss && (e = cudaMemsetAsync(a.tok_loss, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
         if (a.lse && (e = cudaMemsetAsync(a.lse, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
         if ((e = cudaMemsetAsync(a.route.slot_tok, 0xff, sizeof(int) * a.max_slots, stream)) != cudaSuccess) return e;
-        if ((e = cudaMemsetAsync(a.counters, 0, sizeof(unsigned) * kLossCounters, stream)) != cudaSuccess) return e;
+        if ((e = cudaMemsetAsync(a.counters, 0, sizeof(unsigned) * a.n_counters, stream)) != cudaSuccess) return e;
         if ((e = launch_route(a.route, stream, n_launches)) != cudaSuccess) return e;
         e = launch(k_loss_shapes, dim3(1), 1024, stream, a);
     }

@@ -441,7 +441,7 @@ struct LossLayout {
     float *row_lse, *coef_p, *coef_g, *target_g;
     __nv_bfloat16* G; float *tile_max, *parts, *dWc;
     long long max_slots;
-    int n_blocks;
+    int n_blocks, n_counters;
     size_t bytes;
 };
 
@@ -480,7 +480,9 @@ LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int
     L.blk_cnt = b.take<int>(static_cast<size_t>(L.n_blocks) * K + 1);
     L.plan = b.take<DevPlan>(1);
     L.shapes = b.take<LossShapes>(1);
-    L.sync_counters = b.take<unsigned>(kLossCounters);
+    // one arrival counter per launch of the rows kernel, the others for the GEMMs' rendezvous (which go without if they run out)
+    L.n_counters = kLossCounters + (B.keep && !B.joint ? static_cast<int>(K * ((n_tok + B.rows - 1) / B.rows)) : 0);
+    L.sync_counters = b.take<unsigned>(L.n_counters);
     L.hp = b.take<__nv_bfloat16>(ms * H);
     L.target_p = b.take<int>(ms);
     L.stats = b.take<float4>(4 * ms + 94720ull * K);
@@ -498,7 +500,7 @@ LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int
         L.target_g = b.take<float>(ms);
         L.G = b.take<__nv_bfloat16>(static_cast<size_t>(B.rows) * B.cols);
         if (B.keep) L.tile_max = b.take<float>(static_cast<size_t>(B.rows) * (B.cols / kTileN));
-        L.parts = b.take<float>(static_cast<size_t>(part_rows(B.rows, H, V)) * H);
+        L.parts = b.take<float>(static_cast<size_t>(B.keep ? part_rows(B.rows, H, V) : B.rows) * H);
         if (B.dw_scratch) L.dWc = b.take<float>(static_cast<size_t>(V) * H);
     }
     L.bytes = up(b.off, kAlign);
@@ -582,12 +584,8 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     fwd.tile_rows = gemm_tile_rows(c_fwd);
     if (fwd.gmax > fwd.n_pairs) fwd.gmax = fwd.n_pairs;
     fwd.max_splits = fwd.n_pairs;
-    SyncCounters counters{L.sync_counters, 0, kLossCounters};
-    // loss_rows needs its counter: the rendezvous of the GEMMs may go without, so theirs come second
+    SyncCounters counters{L.sync_counters, L.n_counters - kLossCounters + 1, L.n_counters};
     unsigned* tickets = counters.base;
-    const long long n_tickets = B.keep && !B.joint ? K * ((rows_bound + B.rows - 1) / B.rows) : 1;
-    if (n_tickets > kLossCounters) return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: %lld blocks of rows", n_tickets);
-    counters.used = static_cast<int>(n_tickets);
 
     LossRouteArgs lr;
     memset(&lr, 0, sizeof(lr));
@@ -600,7 +598,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     lr.split = SplitParams{B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0, (H + cols_dh - 1) / cols_dh,
                            (V + kTileK - 1) / kTileK, ctx->sm_count / c_dh, gemm_tile_rows(c_dh)};
     lr.block_rows = B.keep && !B.joint ? B.rows : cap_all;
-    lr.max_slots = L.max_slots; lr.shapes = L.shapes; lr.counters = L.sync_counters; lr.tok_loss = c.tok_loss; lr.lse = c.lse;
+    lr.max_slots = L.max_slots; lr.shapes = L.shapes; lr.counters = L.sync_counters; lr.n_counters = L.n_counters; lr.tok_loss = c.tok_loss; lr.lse = c.lse;
     __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
     const LossGatherArgs ga{L.plan, L.slot_tok, L.tok_slot, K, V, H, r->n_tok, L.max_slots,
                             static_cast<const __nv_bfloat16*>(r->hidden), r->target, L.hp, dH, L.target_p, c.n_top, c.logits,

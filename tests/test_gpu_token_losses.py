@@ -217,26 +217,76 @@ def test_accumulation_and_norm(op, dw):
 
 @pytest.mark.parametrize("op", ["ce", "kd"])
 def test_every_workspace_down_to_the_least_gives_the_same_answer(op):
-    """Smaller workspaces take smaller blocks of rows and pieces of the vocabulary."""
-    p = Problem(2100, 64, 3000, 1, 1, n_top=6, seed=9, n_inv=3).gpu()
+    """Smaller workspaces take smaller blocks of rows, then pieces of the vocabulary whose logits are recomputed."""
+    p = Problem(4500, 64, 6000, 1, 1, n_top=6, seed=9, n_inv=3).gpu()
     o = oracle(p, op)
-    full = ub.unity_token_loss_workspace_bytes(p.N, p.H, p.V, p.K, p.n_top if op == "kd" else 0)
-    sizes, failed = [full, full * 3 // 4, full // 2, full // 3, full // 4, full // 6, full // 8], 0
-    for size in sizes:
-        for dw in (torch.bfloat16, torch.float32):
-            ctx = ub.Context(0, size)
+    size = ub.unity_token_loss_workspace_bytes(p.N, p.H, p.V, p.K, p.n_top if op == "kd" else 0)
+    for dw in (torch.bfloat16, torch.float32):
+        now, ways = size, set()
+        while True:
+            ctx = ub.Context(0, now)
             try:
                 g = call(ctx, p, op, dw=dw)
             except ub.UnityError as e:
                 assert e.code == -4
-                failed += 1
-                continue
-            finally:
-                torch.cuda.synchronize()
+                ctx.close()
+                break
             ctx.check_status()
+            ways.add(ctx.launch_count)
             check(p, g, o)
             ctx.close()
-    assert failed < len(sizes)
+            now = now * 4 // 5 // 256 * 256
+        # one block, blocks of kept logits, and the least: pieces of 1024 entries for blocks of at most 1024 rows
+        assert len(ways) >= 4 and max(ways) > 60 and now < size // 4, (ways, now, size)
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("N,H,V,K,n_inv", [
+    (127, 320, 248, 3, 5), (128, 64, 256, 2, 5), (129, 64, 512, 2, 5),        # one row tile of one CTA, and just more
+    (1024, 64, 136, 2, 3000), (1025, 64, 136, 3, 900),                        # routed with the packing or by a block of its own,
+    (8192, 64, 72, 1, 1500), (8193, 64, 72, 2, 40),                           # or by several; boundaries staged or searched
+    (10, 128, 20000, 1, 3), (40, 1344, 6000, 2, 4),                           # few rows: a contraction in many parts
+    (700, 896, 3000, 1, 9), (2600, 192, 1000, 2, 6)])
+def test_sizes_where_the_way_of_working_changes(N, H, V, K, n_inv, op):
+    p = Problem(N, H, V, K, K, n_inv=n_inv, n_top=7, seed=N + H).gpu()
+    ctx = context(p, op)
+    g = call(ctx, p, op, tau=0.9)
+    ctx.check_status()
+    check(p, g, oracle(p, op, tau=0.9))
+    ctx.close()
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("dw", [torch.bfloat16, torch.float32])
+def test_more_rows_than_one_block(op, dw):
+    """Over 18432 rows per model: several blocks, whose dW adds up in fp32."""
+    p = Problem(24000, 64, 200, 2, 2, n_inv=50, n_top=5, seed=6, mask=0.1)
+    p.inv_role[:] = 0
+    p.inv_role[7] = 1
+    p.gpu()
+    ctx = context(p, op)
+    torch.manual_seed(2)
+    old = [torch.randn(p.V, p.H, device="cuda").to(dw) * 0.01 for _ in range(p.K)]
+    base = [x.double().cpu().numpy() for x in old]
+    o = oracle(p, op)
+    check(p, call(ctx, p, op, dw=dw), o)
+    check(p, call(ctx, p, op, accumulate=True, dW=old), o, base=base)
+    ctx.check_status()
+    ctx.close()
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("options", [[(0, 1), (1, 1), (2, 1), (3, 1)], [(11, 0)], [(9, 0), (10, 0)], [(29, 0)]])
+def test_options_of_the_gemms(op, options):
+    """CTAs per tile, tiles one block wide, no rendezvous, no tail launch."""
+    p = Problem(2300, 640, 1400, 1, 1, n_top=9, seed=12).gpu()
+    ctx = context(p, op)
+    for option, value in options:
+        ctx.set_option(option, value)
+    g = call(ctx, p, op)
+    ctx.check_status()
+    check(p, g, oracle(p, op))
+    ctx.close()
 
 
 @pytest.mark.parametrize("op", ["ce", "kd"])
@@ -443,6 +493,52 @@ def test_step_of_both_losses_and_the_policy_update_on_one_context():
     check(p, {**ce, "dW": None}, o)
     check(p, {**kd, "dW": None}, k)
     ctx.close()
+
+
+def test_outputs_between_guards():
+    """Rows before the first and behind the last token, and entries before and behind the heads' gradients, stay as they were."""
+    p = Problem(77, 64, 264, 1, 1, n_top=6, seed=14).gpu()
+    ctx = context(p, "kd")
+    for op in ("ce", "kd"):
+        o = oracle(p, op)
+        dH = torch.full((p.N + 16, p.H), 5.0, dtype=torch.bfloat16, device="cuda")
+        per = {k: torch.full((p.N + 8,), 5.0, device="cuda") for k in ("tok_loss", "lse")}
+        dW = torch.full((p.V + 16, p.H), 5.0, dtype=torch.bfloat16, device="cuda")
+        loss = torch.full((5,), 5.0, device="cuda")
+        head = (p.d_hidden, p.d_W, p.d_cu, p.d_inv_role, p.role_model, p.d_target, p.d_mask, 1.0)
+        outs = (None, False, p.d_weight, loss[2:3], per["tok_loss"][4:-4], per["lse"][4:-4], dH[8:-8], [dW[8:-8]])
+        if op == "ce":
+            ctx.cross_entropy_fwd_bwd(*head, 0.0, 0.0, *outs)
+        else:
+            ctx.distill_fwd_bwd(*head, p.d_top_ids, p.d_top_vals, ub.TEACHER_LOGITS, 1.0, 0.0, *outs)
+        ctx.check_status()
+        check(p, dict(loss=outs[3], tok_loss=outs[4], lse=outs[5], dHidden=outs[6], dW=outs[7]), o)
+        for t, w in ((dH, 8), (dW, 8), (per["tok_loss"], 4), (per["lse"], 4), (loss, 2)):
+            assert torch.all(t[:w] == 5.0) and torch.all(t[-w:] == 5.0)
+    ctx.close()
+
+
+def test_two_contexts_at_once():
+    """Calls on two streams, each with its own context and workspace, overlap without touching one another."""
+    p, q = Problem(300, 128, 3000, 1, 1, n_top=6, seed=1).gpu(), Problem(90, 192, 2000, 2, 2, n_top=6, seed=2).gpu()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    ctxs, got = [], [[], []]
+    for s, x in zip(streams, (p, q)):
+        with torch.cuda.stream(s):
+            ctxs.append(ub.Context(0, ub.unity_token_loss_workspace_bytes(x.N, x.H, x.V, x.K, x.n_top), s))
+    for _ in range(4):
+        for i, x in enumerate((p, q)):
+            with torch.cuda.stream(streams[i]):
+                got[i] += [call(ctxs[i], x, "ce"), call(ctxs[i], x, "kd")]
+    torch.cuda.synchronize()
+    for i, x in enumerate((p, q)):
+        ctxs[i].check_status()
+        want = [oracle(x, "ce"), oracle(x, "kd")]
+        for j, g in enumerate(got[i]):
+            check(x, g, want[j % 2])
+            assert torch.equal(g["dHidden"], got[i][j % 2]["dHidden"])
+        ctxs[i].close()
 
 
 def test_current_device_and_default_arguments_stay():
