@@ -174,6 +174,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
         stats_base = in.span.plan->stats_base[k];
     }
     if (in.shapes != nullptr && in.span_mode == kSpanRowsM) split = *reinterpret_cast<const int4*>(in.shapes->dh[k]);
+    if (in.split_rows) split = *reinterpret_cast<const int4*>(in.shapes->dw[k]);
     span_resolve(in.span, slot0, n_rows);
     if (in.span_mode == kSpanForward) {
         const FwdShape fs = in.shapes == nullptr ? forward_shape(in.fwd, n_rows) : (n_rows == in.span.row_cap ? full.f : last.f);
@@ -235,6 +236,11 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
         g.k_iters = (in.shapes ? span_slab_rows(in.span, n_rows) : n_rows) / kTileK;
         g.b_k0 = in.b_k0 + slot0;
         if (in.stash_by_slot) g.a_k0 = slot0;
+        if (in.split_rows) {
+            const bool whole = n_rows == in.span.row_cap;
+            g.k_splits = whole ? split.x : split.z; g.k_per_split = whole ? split.y : split.w;
+            g.c_split = static_cast<long long>(in.m_rows) * in.ldc;
+        }
     }
     return g;
 }

@@ -123,9 +123,10 @@ __host__ __device__ inline FwdShape forward_shape(const FwdPlanParams& p, int ro
 // rows): the count with the least time, a worker's longest run of slabs plus, per part, the pipeline's fill and its
 // unoverlapped epilogue (kSplitOverhead slabs).
 constexpr int kSplitOverhead = 10;
-constexpr int kSplitWaves = 6;          // no more parts than make up 6 waves of workers: bounds their buffer
+constexpr int kSplitWaves = 6;          // dHidden: no more parts than make up 6 waves of workers, which bounds their buffer
+constexpr int kSplitWavesDw = 2;        // dW (heads of few tiles): 2 waves
 struct SplitShape { int splits, per_split; };
-struct SplitParams { int most, n_tiles, k_iters, workers, tile_rows; };   // most = 0: never cut
+struct SplitParams { int most, n_tiles, k_iters, workers, tile_rows, waves; };   // most = 0: never cut; waves: bounds the parts
 __host__ __device__ inline long long split_candidate(const SplitParams& p, int m_tiles, int s, SplitShape& f) {
     f.per_split = (p.k_iters + s - 1) / s;
     f.splits = (p.k_iters + f.per_split - 1) / f.per_split;
@@ -133,7 +134,7 @@ __host__ __device__ inline long long split_candidate(const SplitParams& p, int m
     return waves * (f.per_split + kSplitOverhead) + (s > 1 ? s : 0);
 }
 __host__ __device__ inline bool split_allowed(const SplitParams& p, int m_tiles, int s) {   // a part has at least 8 slabs
-    return s == 1 || (s <= p.most && s <= p.k_iters / 8 && static_cast<long long>(m_tiles) * p.n_tiles * s <= kSplitWaves * p.workers);
+    return s == 1 || (s <= p.most && s <= p.k_iters / 8 && static_cast<long long>(m_tiles) * p.n_tiles * s <= static_cast<long long>(p.waves) * p.workers);
 }
 constexpr int kMaxKSplits = 32;
 
@@ -143,6 +144,7 @@ constexpr int kMaxKSplits = 32;
 struct __align__(16) LossShapes {
     FwdShape fwd[UNITY_MAX_MODELS][2];
     SplitShape dh[UNITY_MAX_MODELS][2];
+    SplitShape dw[UNITY_MAX_MODELS][2];
 };
 static_assert(sizeof(FwdShape) == 32 && sizeof(SplitShape) == 8, "read as 16-byte and 8-byte vectors");
 constexpr float kStashSteps = 512.f;   // steps per octave of a kept logit (GemmArgs::stash) ...
@@ -222,6 +224,7 @@ struct GemmArgs {
     long long ldc;
     int k_splits, k_per_split;   // the contraction is cut into k_splits parts of k_per_split slabs, each with an output of
     long long c_split;           // its own, c_split values apart (0 or 1: not cut)
+    int split_rows;              // kSpanRowsK: the contraction over rows is cut as LossShapes::dw says
     int zero_if_empty;           // a launch whose contraction has no rows writes zeros to its m_rows x ldc outputs
     int beta;                 // 0: overwrite, 1: add to C
     int mma_n;                // columns per MMA block, a multiple of 32 up to 256 (a tile is 1 or 2 blocks wide); 256
@@ -413,6 +416,7 @@ constexpr int kLossCounters = 1024;
 struct LossRouteArgs {
     RouteArgs route;           // fwd: the forward planner's inputs
     SplitParams split;         // of dHidden's GEMM
+    SplitParams split_dw;      // of dW's: n_tiles = all its tiles, k_iters from the rows
     int block_rows;            // rows of a full block (at least a batch's rows: one block)
     long long max_slots;
     LossShapes* shapes;
@@ -509,6 +513,17 @@ struct StoreArgs {
     __nv_bfloat16* dHidden;
 };
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream);
+// One model's dW [n values] = the parts of its GEMM (+ its old value when add), fp32 or (out16 not null) rounded to bf16 once
+struct SumDwArgs {
+    const float* parts;        // [parts][n]
+    RowSpan span;
+    const LossShapes* shapes;
+    long long n;               // a multiple of 4
+    int add;
+    float* out;
+    __nv_bfloat16* out16;
+};
+cudaError_t launch_sum_dw(const SumDwArgs& a, cudaStream_t stream);
 // dst[0, n) = bf16(src) (+ dst when add); n a multiple of 8
 cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream);
 

@@ -56,11 +56,21 @@ __device__ __forceinline__ long long warp_min64(long long v) {
 
 // One warp: the forward schedule and dHidden's parts for `rows` rows, lanes weighing candidates side by side (the same
 // choice as forward_shape's).
-__device__ __forceinline__ void warp_shapes(const LossRouteArgs& a, int rows, FwdShape* fwd, SplitShape* dh) {
+__device__ __forceinline__ SplitShape warp_split(const SplitParams& p, int m_tiles) {
+    SplitShape s;
+    long long best = 0x7fffffffffffffffll;
+    const int c = (threadIdx.x & 31) + 1;
+    static_assert(kMaxKSplits <= 32, "one candidate per lane");
+    if (split_allowed(p, m_tiles, c)) best = split_candidate(p, m_tiles, c, s) * 64 + c;
+    best = warp_min64(best);
+    split_candidate(p, m_tiles, static_cast<int>(best & 63), s);
+    return s;
+}
+// `valid`: the rows that hold tokens
+__device__ __forceinline__ void warp_shapes(const LossRouteArgs& a, int rows, int valid, FwdShape* fwd, SplitShape* dh, SplitShape* dw) {
     const int lane = threadIdx.x & 31;
     const FwdPlanParams& p = a.route.fwd;
     FwdShape f;
-    SplitShape s;
     const int m = rows / p.tile_rows, cand_min = forward_cand_min(p, m);
     long long best = 0x7fffffffffffffffll;
     for (int cand = p.gmax - lane; cand >= cand_min; cand -= 32) {
@@ -73,33 +83,28 @@ __device__ __forceinline__ void warp_shapes(const LossRouteArgs& a, int rows, Fw
         forward_finish(p, rows, m, f);
         *fwd = f;
     }
-    const int md = rows / a.split.tile_rows;
-    best = 0x7fffffffffffffffll;
-    for (int c = lane + 1; c <= kMaxKSplits; c += 32) {
-        if (!split_allowed(a.split, md, c)) continue;
-        const long long key = split_candidate(a.split, md, c, s) * 64 + c;
-        best = key < best ? key : best;
-    }
-    best = warp_min64(best);
-    if (lane == 0) {
-        split_candidate(a.split, md, static_cast<int>(best & 63), s);
-        *dh = s;
-    }
+    const SplitShape h = warp_split(a.split, rows / a.split.tile_rows);
+    SplitParams pw = a.split_dw;
+    pw.k_iters = (valid + kTileK - 1) / kTileK;
+    const SplitShape w = warp_split(pw, 1);
+    if (lane == 0) { *dh = h; *dw = w; }
 }
 
 // Model w / 2, its full block or its last one, for w over the block's warps; then the models' statistics bases.
-__device__ __forceinline__ void write_shapes(const LossRouteArgs& a, const int* off) {
+__device__ __forceinline__ void write_shapes(const LossRouteArgs& a, const int* off, const int* counts) {
     __shared__ long long sh_stats[UNITY_MAX_MODELS][2];
     for (int w = threadIdx.x >> 5; w < 2 * a.route.K; w += blockDim.x >> 5) {
         const int k = w >> 1, rows = off[k + 1] - off[k];
         const bool full = (w & 1) == 0;
         if (full && rows < a.block_rows) continue;             // no full block, no schedule of one
         FwdShape f;
-        SplitShape s;
-        warp_shapes(a, full ? a.block_rows : rows % a.block_rows, &f, &s);
+        SplitShape h, d;
+        const int here = full ? a.block_rows : rows % a.block_rows, valid = full ? here : counts[k] - (rows - here);
+        warp_shapes(a, here, valid < here ? valid : here, &f, &h, &d);
         if ((threadIdx.x & 31) == 0) {
             a.shapes->fwd[k][w & 1] = f;
-            a.shapes->dh[k][w & 1] = s;
+            a.shapes->dh[k][w & 1] = h;
+            a.shapes->dw[k][w & 1] = d;
             sh_stats[k][w & 1] = f.stats_rows;
         }
     }
@@ -116,7 +121,7 @@ __device__ __forceinline__ void write_shapes(const LossRouteArgs& a, const int* 
 }
 __global__ void __launch_bounds__(1024) k_loss_shapes(LossRouteArgs a) {
     begin();
-    write_shapes(a, a.route.plan->off);
+    write_shapes(a, a.route.plan->off, a.route.plan->counts);
 }
 
 // Routing of all tokens by one block: thread t takes the tokens [t*per, t*per + per), counts them by model, and a scan over
@@ -222,7 +227,7 @@ __device__ __forceinline__ void write_routes(const LossRouteArgs& a, const Route
     }
     for (int k = 0; k < r.K; ++k)
         for (int s = sh.off[k] + sh.tot[k] + tid; s < sh.off[k + 1]; s += kThreads) r.slot_tok[s] = -1;
-    write_shapes(a, sh.off);
+    write_shapes(a, sh.off, sh.tot);
 }
 
 // One block routes a whole batch of up to kLossRouteTokens tokens, in place of four memsets and three routing launches.
@@ -236,27 +241,34 @@ __global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
 
 // One warp's list: ascending, distinct vocabulary indexes with their teacher probabilities q.  Entries with a negative id are
 // empty places, an id >= V is reported and counts as one, and so do entries of probability zero (a logit of -inf); equal ids
-// add up in list order.  With at most 128 entries a rank by counting (each entry is compared with all others, which sit in
-// shared memory) needs no sorting network.
-__device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slot, int tok, int (*sh_id)[kMaxTop], float (*sh_q)[kMaxTop]) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// add up in list order.  With at most 128 entries, four to a lane, a rank by counting (each entry is compared with all others,
+// which sit in shared memory and are read four at a time) needs no sorting network.
+__device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slot, int tok, int (*sh_ids)[kMaxTop], float (*sh_qs)[kMaxTop]) {
+    constexpr int kPer = kMaxTop / 32;
+    const int lane = threadIdx.x & 31;
+    int* sh_id = sh_ids[threadIdx.x >> 5];
+    float* sh_q = sh_qs[threadIdx.x >> 5];
     const int* ids = a.top_ids + static_cast<long long>(tok) * a.n_top;
     const float* vals = a.top_vals + static_cast<long long>(tok) * a.n_top;
-    int id[kMaxTop / 32];
-    float x[kMaxTop / 32];
+    int id[kPer];
+    float x[kPer];
     float m = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kMaxTop / 32; ++u) {
+    for (int u = 0; u < kPer; ++u) {
         const int j = lane + 32 * u;
         id[u] = -1;
         x[u] = 0.f;
         if (j < a.n_top) {
             id[u] = ids[j];
-            if (id[u] >= a.V) { atomicOr(a.status, kStatusBadIndex); id[u] = -1; }
-            if (id[u] >= 0) {
-                x[u] = a.logits ? vals[j] * a.scale : vals[j];
-                m = fmaxf(m, x[u]);
-            }
+            x[u] = vals[j];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        if (id[u] >= a.V) { atomicOr(a.status, kStatusBadIndex); id[u] = -1; }
+        if (id[u] >= 0) {
+            if (a.logits) x[u] *= a.scale;
+            m = fmaxf(m, x[u]);
         }
     }
     float sum = 1.f;
@@ -264,59 +276,59 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
         m = warp_max(m);
         float s = 0.f;
 #pragma unroll
-        for (int u = 0; u < kMaxTop / 32; ++u) {
-            // a list without a finite or infinite-above entry (m = -inf) has no probabilities: its row is empty
+        for (int u = 0; u < kPer; ++u) {
+            // a list without an entry above -inf has no probabilities: its row is empty
             x[u] = id[u] >= 0 ? (x[u] == -INFINITY ? 0.f : expf(x[u] - m)) : 0.f;
             s += x[u];
         }
         sum = warp_sum(s);
     } else {
 #pragma unroll
-        for (int u = 0; u < kMaxTop / 32; ++u) x[u] = id[u] >= 0 ? expf(x[u]) : 0.f;
+        for (int u = 0; u < kPer; ++u) x[u] = id[u] >= 0 ? expf(x[u]) : 0.f;
     }
+    int n = 0;
 #pragma unroll
-    for (int u = 0; u < kMaxTop / 32; ++u) {
-        const int j = lane + 32 * u;
-        const float q = x[u] == 0.f ? 0.f : x[u] / sum;
-        if (id[u] < 0 || q == 0.f) id[u] = kNone;
-        if (j < a.n_top) { sh_id[warp][j] = id[u]; sh_q[warp][j] = q; }
+    for (int u = 0; u < kPer; ++u) {
+        x[u] = x[u] == 0.f ? 0.f : x[u] / sum;
+        if (id[u] < 0 || x[u] == 0.f) id[u] = kNone;
+        sh_id[lane + 32 * u] = id[u];
+        n += __popc(__ballot_sync(kFull, id[u] != kNone));
     }
     __syncwarp();
-    // pass 1: the first of several equal ids takes their sum
-    bool lead[kMaxTop / 32];
-    float q[kMaxTop / 32];
+    int rank[kPer] = {};
+    for (int i = 0; i < a.n_top; i += 4) {
+        const int4 v = *reinterpret_cast<const int4*>(sh_id + i);
 #pragma unroll
-    for (int u = 0; u < kMaxTop / 32; ++u) {
-        const int j = lane + 32 * u;
-        lead[u] = j < a.n_top && id[u] != kNone;
-        q[u] = 0.f;
-        if (lead[u]) {
-            for (int i = 0; i < a.n_top; ++i) {
-                if (sh_id[warp][i] != id[u]) continue;
-                if (i < j) { lead[u] = false; break; }
-                q[u] += sh_q[warp][i];
-            }
+        for (int u = 0; u < kPer; ++u) {
+            if (32 * u >= a.n_top) break;
+            const int j = lane + 32 * u;
+            rank[u] += (v.x < id[u] || (v.x == id[u] && i < j)) + (v.y < id[u] || (v.y == id[u] && i + 1 < j)) +
+                       (v.z < id[u] || (v.z == id[u] && i + 2 < j)) + (v.w < id[u] || (v.w == id[u] && i + 3 < j));
         }
     }
     __syncwarp();
 #pragma unroll
-    for (int u = 0; u < kMaxTop / 32; ++u) {
-        const int j = lane + 32 * u;
-        if (j < a.n_top && !lead[u]) sh_id[warp][j] = kNone;
-    }
+    for (int u = 0; u < kPer; ++u)
+        if (id[u] != kNone) { sh_id[rank[u]] = id[u]; sh_q[rank[u]] = x[u]; }
     __syncwarp();
-    // pass 2: rank among the first ones
-    int n = 0;
+    // sorted: the first of several equal ids takes their sum
+    int kept = 0;
 #pragma unroll
-    for (int u = 0; u < kMaxTop / 32; ++u) {
-        n += __popc(__ballot_sync(kFull, lead[u]));
-        if (!lead[u]) continue;
-        int rank = 0;
-        for (int i = 0; i < a.n_top; ++i) rank += sh_id[warp][i] < id[u];
-        a.ids_p[slot * a.n_top + rank] = id[u];
-        a.q_p[slot * a.n_top + rank] = q[u];
+    for (int u = 0; u < kPer; ++u) {
+        const int r = lane + 32 * u;
+        const int mine = r < n ? sh_id[r] : kNone;
+        const bool lead = r < n && (r == 0 || sh_id[r - 1] != mine);
+        const unsigned leads = __ballot_sync(kFull, lead);
+        if (lead) {
+            float q = sh_q[r];
+            for (int i = r + 1; i < n && sh_id[i] == mine; ++i) q += sh_q[i];
+            const long long at = slot * a.n_top + kept + __popc(leads & ((1u << lane) - 1u));
+            a.ids_p[at] = mine;
+            a.q_p[at] = q;
+        }
+        kept += __popc(leads);
     }
-    if (lane == 0) a.cnt_p[slot] = n;
+    if (lane == 0) a.cnt_p[slot] = kept;
 }
 
 // One warp per packed row and per token, w: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
@@ -354,7 +366,7 @@ __device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w,
 
 __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
     begin();
-    __shared__ int sh_id[8][kMaxTop];
+    __shared__ __align__(16) int sh_id[8][kMaxTop];
     __shared__ float sh_q[8][kMaxTop];
     long long w = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
     const bool list = a.n_top > 0 && (w & 1);
@@ -372,7 +384,7 @@ __global__ void __launch_bounds__(256) k_loss_pack(LossRouteArgs r, LossGatherAr
     __shared__ RouteShared<256> sh;
     __shared__ short sh_tok[kLossPackTokens];                  // tokens by model and rank
     __shared__ signed char sh_model[kLossPackTokens];
-    __shared__ int sh_id[8][kMaxTop];
+    __shared__ __align__(16) int sh_id[8][kMaxTop];
     __shared__ float sh_q[8][kMaxTop];
     constexpr int kPer = kLossPackTokens / 256;
     int model[kPer], rank[kPer];
@@ -556,23 +568,32 @@ constexpr int kGradVecs = 4;
 constexpr int kGradCols = 256 * 8 * kGradVecs;
 __global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
     begin();
-    int row0 = 0, rows;
+    // the rows that the contractions read: of a block, or of every model (their slabs end with the last token)
+    __shared__ int sh_off[UNITY_MAX_MODELS], sh_rows[UNITY_MAX_MODELS];
     const bool joint = a.span.model < 0;
+    int row0 = 0, rows = 0;
     if (joint) {
-        rows = a.span.plan->off[a.K];
+        if (threadIdx.x < a.K) {
+            const int k = threadIdx.x;
+            sh_off[k] = a.span.plan->off[k];
+            sh_rows[k] = (a.span.plan->counts[k] + kTileK - 1) / kTileK * kTileK;
+        }
+        __syncthreads();
+        for (int k = 0; k < a.K; ++k) rows += sh_rows[k];
     } else {
         span_resolve(a.span, row0, rows);
-        rows = span_slab_rows(a.span, rows);                   // padding rows beyond the last slab are read by nobody's sums
+        rows = span_slab_rows(a.span, rows);
     }
     const int per_row = (a.cols + kGradCols - 1) / kGradCols;
     for (int item = blockIdx.x; item < rows * per_row; item += gridDim.x) {      // at most 18432 rows of 2^18 columns
-        const int r = item / per_row, c_lo = (item - r * per_row) * kGradCols, c_first = c_lo + threadIdx.x * 8;
-        const int slot = row0 + r;
+        int r = item / per_row;
+        const int c_lo = (item - r * per_row) * kGradCols, c_first = c_lo + threadIdx.x * 8;
         if (joint) {
             int k = 0;
-            while (k + 1 < a.K && slot >= a.span.plan->off[k + 1]) ++k;
-            if (slot - a.span.plan->off[k] >= (a.span.plan->counts[k] + kTileK - 1) / kTileK * kTileK) continue;
+            while (r >= sh_rows[k]) r -= sh_rows[k++];
+            r += sh_off[k];
         }
+        const int slot = row0 + r;
         uint4* row = reinterpret_cast<uint4*>(a.Z + static_cast<long long>(r) * a.ld);
         const float* tm = a.tile_max + static_cast<long long>(r) * a.n_tiles;
         uint4 raw[kGradVecs];
@@ -623,18 +644,7 @@ __global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
     }
 }
 
-// One block per row and 1024 columns: four columns per thread, the parts added in their order, one rounding to bf16.
-__global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
-    begin();
-    int slot0, rows;
-    span_resolve(a.span, slot0, rows);
-    const int r = blockIdx.x, c = (blockIdx.y * 256 + threadIdx.x) * 4;
-    if (r >= rows || c >= a.H) return;
-    const int tok = a.slot_tok[slot0 + r];
-    const int splits = a.shapes ? a.shapes->dh[a.span.model][rows == a.span.row_cap ? 0 : 1].splits : 1;
-    if (tok < 0) return;
-    const long long stride = static_cast<long long>(rows) * a.H;
-    const float* src = a.parts + static_cast<long long>(r) * a.H + c;
+__device__ __forceinline__ float4 sum_parts(const float* src, int splits, long long stride) {
     float4 v = *reinterpret_cast<const float4*>(src);
     int s = 1;
     for (; s + 4 <= splits; s += 4) {                          // four loads in flight
@@ -648,9 +658,52 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
         const float4 o = *reinterpret_cast<const float4*>(src + s * stride);
         v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
     }
+    return v;
+}
+__device__ __forceinline__ uint2 pack4(float4 v) {
     const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x, v.y), hi = __floats2bfloat162_rn(v.z, v.w);
-    *reinterpret_cast<uint2*>(a.dHidden + static_cast<long long>(tok) * a.H + c) =
-        make_uint2(*reinterpret_cast<const unsigned*>(&lo), *reinterpret_cast<const unsigned*>(&hi));
+    return make_uint2(*reinterpret_cast<const unsigned*>(&lo), *reinterpret_cast<const unsigned*>(&hi));
+}
+
+// Four columns per thread: the parts added in their order, one rounding to bf16.
+__global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
+    begin();
+    int slot0, rows;
+    span_resolve(a.span, slot0, rows);
+    const int per_row = a.H >> 2;
+    const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
+    const int r = static_cast<int>(i / per_row), c = static_cast<int>(i - static_cast<long long>(r) * per_row) * 4;
+    if (r >= rows) return;
+    const int tok = a.slot_tok[slot0 + r];
+    const int splits = a.shapes ? a.shapes->dh[a.span.model][rows == a.span.row_cap ? 0 : 1].splits : 1;
+    if (tok < 0) return;
+    const float4 v = sum_parts(a.parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
+    *reinterpret_cast<uint2*>(a.dHidden + static_cast<long long>(tok) * a.H + c) = pack4(v);
+}
+
+// The same for dW, four values per thread, plus the old value where it accumulates; zeros where the span has no token.
+__global__ void __launch_bounds__(256) k_sum_dw(SumDwArgs a) {
+    begin();
+    const long long i = (static_cast<long long>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (i >= a.n) return;
+    int slot0, rows;
+    span_resolve(a.span, slot0, rows);
+    if (rows <= 0 && a.add) return;
+    const int splits = a.shapes->dw[a.span.model][rows == a.span.row_cap ? 0 : 1].splits;
+    float4 v = rows > 0 ? sum_parts(a.parts + i, splits, a.n) : make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.out16 != nullptr) {
+        uint2* out = reinterpret_cast<uint2*>(a.out16 + i);
+        if (a.add) {
+            const uint2 old = *out;
+            v.x += __uint_as_float(old.x << 16); v.y += __uint_as_float(old.x & 0xffff0000u);
+            v.z += __uint_as_float(old.y << 16); v.w += __uint_as_float(old.y & 0xffff0000u);
+        }
+        *out = pack4(v);
+    } else {
+        float4* out = reinterpret_cast<float4*>(a.out + i);
+        if (a.add) { const float4 old = *out; v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w; }
+        *out = v;
+    }
 }
 
 // dst = bf16(src) (+ dst): one rounding of the fp32 sum over all row blocks.  Eight values per thread and step.
@@ -696,7 +749,9 @@ cudaError_t launch_loss_pack(const LossRouteArgs& a, const LossGatherArgs& g, cu
         if (a.lse && (e = cudaMemsetAsync(a.lse, 0, sizeof(float) * n, stream)) != cudaSuccess) return e;
         if ((e = cudaMemsetAsync(a.route.slot_tok, 0xff, sizeof(int) * a.max_slots, stream)) != cudaSuccess) return e;
         if ((e = cudaMemsetAsync(a.counters, 0, sizeof(unsigned) * a.n_counters, stream)) != cudaSuccess) return e;
-        if ((e = launch_route(a.route, stream, n_launches)) != cudaSuccess) return e;
+        RouteArgs r = a.route;                                 // (its statistics bases are written again below: the cheapest plan)
+        r.fwd.gmax = 1;
+        if ((e = launch_route(r, stream, n_launches)) != cudaSuccess) return e;
         e = launch(k_loss_shapes, dim3(1), 1024, stream, a);
     }
     if (e != cudaSuccess) return e;
@@ -721,7 +776,11 @@ cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaSt
 }
 
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {
-    return launch(k_store_parts, dim3(a.bound, (a.H + 1023) / 1024), 256, stream, a);
+    return launch(k_store_parts, dim3(static_cast<unsigned>((static_cast<long long>(a.bound) * (a.H >> 2) + 255) / 256)), 256, stream, a);
+}
+
+cudaError_t launch_sum_dw(const SumDwArgs& a, cudaStream_t stream) {
+    return launch(k_sum_dw, dim3(static_cast<unsigned>((a.n / 4 + 255) / 256)), 256, stream, a);
 }
 
 cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream) {

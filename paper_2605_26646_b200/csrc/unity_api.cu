@@ -458,13 +458,25 @@ struct LossBlocks {
 // Rows of the buffer that takes the parts of dHidden (split_shape): a block of rows, or the parts of fewer rows.
 // 160 bounds the SMs of the parts; on a larger device the contraction is not cut.
 constexpr int kMaxSms = 160;
-long long part_rows(int block_rows, int H, int V) {
+long long part_rows_dh(int block_rows, int H, int V) {
     const int wide = 2 * gemm_mma_n(H), n_tiles = H > kTileN ? (H + wide - 1) / wide : 1;
     const long long splits = (V + kTileK - 1) / kTileK / 8;
     const long long most = static_cast<long long>(block_rows) * (splits < 1 ? 1 : (splits < kMaxKSplits ? splits : kMaxKSplits));
     const long long waves = static_cast<long long>(kSplitWaves) * kMaxSms * kCtaM / n_tiles;
     const long long cut = most < waves ? most : waves;
     return cut > block_rows ? cut : block_rows;
+}
+// dW's contraction over the rows is cut where its tiles alone leave more than half of the workers idle.
+long long dw_tiles(int H, int V, bool wide, int tile_v) {
+    const int cols = (wide ? 2 : 1) * gemm_mma_n(H);
+    return static_cast<long long>((V + tile_v - 1) / tile_v) * ((H + cols - 1) / cols);
+}
+// Rows of H values that both buffers of parts need (they are used one after the other).
+long long part_rows(int block_rows, int H, int V) {
+    const long long dh = part_rows_dh(block_rows, H, V), tiles = dw_tiles(H, V, H > gemm_mma_n(H), kTileM);
+    if (2 * tiles > kMaxSms / 2) return dh;
+    const long long parts = kSplitWavesDw * (kMaxSms / 2) / tiles, dw = V * (parts < kMaxKSplits ? parts : kMaxKSplits);
+    return dh > dw ? dh : dw;
 }
 
 LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int K, int n_top, const LossBlocks& B, bool* fits) {
@@ -596,7 +608,12 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     ra.n_blocks = L.n_blocks; ra.blk_cnt = L.blk_cnt; ra.plan = L.plan; ra.fwd = fwd;
     ra.tok_slot = L.tok_slot; ra.slot_tok = L.slot_tok; ra.tok_model = L.tok_model; ra.status = ctx->d_status;
     lr.split = SplitParams{B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0, (H + cols_dh - 1) / cols_dh,
-                           (V + kTileK - 1) / kTileK, ctx->sm_count / c_dh, gemm_tile_rows(c_dh)};
+                           (V + kTileK - 1) / kTileK, ctx->sm_count / c_dh, gemm_tile_rows(c_dh), kSplitWaves};
+    // few rows: a dW tile's epilogue must overlap the next tile's products, which only the narrow form does, and is not cut
+    const bool long_k = (rows_bound < B.rows ? rows_bound : B.rows) > 1024, wide_dw = two_blocks && c_dw == 2 && long_k;
+    const long long tiles_dw = dw_tiles(H, V, wide_dw, gemm_tile_rows(c_dw));
+    const bool split_dw = want_w && B.keep && long_k && ctx->sm_count <= kMaxSms && c_dw == 2 && 2 * tiles_dw <= ctx->sm_count / c_dw;
+    lr.split_dw = SplitParams{split_dw ? kMaxKSplits : 0, static_cast<int>(tiles_dw), 0, ctx->sm_count / c_dw, kTileM, kSplitWavesDw};
     lr.block_rows = B.keep && !B.joint ? B.rows : cap_all;
     lr.max_slots = L.max_slots; lr.shapes = L.shapes; lr.counters = L.sync_counters; lr.n_counters = L.n_counters; lr.tok_loss = c.tok_loss; lr.lse = c.lse;
     __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
@@ -747,8 +764,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     }
                 }
                 if (want_w) {
-                    // few rows: a tile's epilogue must overlap the next tile's products, which only the narrow form does
-                    const bool wide = two_blocks && c_dw == 2 && bound > 1024;
+                    const bool wide = wide_dw;
                     const int tile_v = gemm_tile_rows(c_dw), vt = (vc + tile_v - 1) / tile_v, cols = (wide ? 2 : 1) * mma_n;
                     // the last few vocabulary tiles as a launch of narrow ones where they would open one more wave (as in
                     // the policy update: V = 151936 is eight waves of 74 tiles and two more) and that wave is longer than a launch
@@ -770,14 +786,22 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
                         w.a_row0 = row0; w.m_rows = n_here; w.n_cols = H; w.ldc = H;
                         const long long at = static_cast<long long>(v0 + row0) * H;
-                        if (out16) w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + at;
+                        const bool add = add_dw || c0 > 0;
+                        if (split_dw) { w.C = L.parts; w.split_rows = 1; w.g_wide_store = 1; }
+                        else if (out16) w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + at;
                         else w.C = dWk + at;
-                        w.beta = (add_dw || c0 > 0) ? 1 : 0;
-                        w.zero_if_empty = !w.beta;               // a model without rows: its dW reads zero
+                        w.beta = add && !split_dw ? 1 : 0;
+                        w.zero_if_empty = !add && !split_dw;     // a model without rows: its dW reads zero
                         gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0 && !short_k);
                         ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
-                        CUDA_TRY(ctx, launch_gemm(out16 ? kEpiAccumB16 : kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide_here));
+                        CUDA_TRY(ctx, launch_gemm(out16 && !split_dw ? kEpiAccumB16 : kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide_here));
                         nl += 1;
+                        if (split_dw) {
+                            const SumDwArgs sd{L.parts, chunk, L.shapes, static_cast<long long>(V) * H, add, dWk,
+                                               out16 ? static_cast<__nv_bfloat16*>(c.dW[k]) : nullptr};
+                            CUDA_TRY(ctx, launch_sum_dw(sd, st));
+                            nl += 1;
+                        }
                     }
                 }
             }

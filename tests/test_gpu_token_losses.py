@@ -203,8 +203,9 @@ def test_forms_agree_with_the_whole_call(op, grads):
 
 @pytest.mark.parametrize("op", ["ce", "kd"])
 @pytest.mark.parametrize("dw", [torch.bfloat16, torch.float32])
-def test_accumulation_and_norm(op, dw):
-    p = Problem(200, 64, 520, 2, 2, n_top=9, seed=5).gpu()
+@pytest.mark.parametrize("N", [200, 3000])
+def test_accumulation_and_norm(N, op, dw):
+    p = Problem(N, 64, 520, 2, 2, n_top=9, seed=5).gpu()
     ctx = context(p, op)
     torch.manual_seed(1)
     old = [torch.randn(p.V, p.H, device="cuda").to(dw) * 0.01 for _ in range(p.K)]
@@ -246,7 +247,8 @@ def test_every_workspace_down_to_the_least_gives_the_same_answer(op):
     (1024, 64, 136, 2, 3000), (1025, 64, 136, 3, 900),                        # routed with the packing or by a block of its own,
     (8192, 64, 72, 1, 1500), (8193, 64, 72, 2, 40),                           # or by several; boundaries staged or searched
     (10, 128, 20000, 1, 3), (40, 1344, 6000, 2, 4),                           # few rows: a contraction in many parts
-    (700, 896, 3000, 1, 9), (2600, 192, 1000, 2, 6)])
+    (700, 896, 3000, 1, 9), (2600, 192, 1000, 2, 6),
+    (6000, 256, 1024, 1, 9), (5000, 576, 600, 3, 9)])                         # many rows of a small head: dW in parts
 def test_sizes_where_the_way_of_working_changes(N, H, V, K, n_inv, op):
     p = Problem(N, H, V, K, K, n_inv=n_inv, n_top=7, seed=N + H).gpu()
     ctx = context(p, op)
