@@ -67,6 +67,7 @@ constexpr int kDefaultChunkMult = 2;
 constexpr int kSyncCounters = 16384;       // rendezvous counters per call (4 bytes each)
 constexpr int kMinChunkRows = 1024;
 constexpr int kMinChunkVocab = 1024;
+constexpr int kLongRows = 1024;            // token losses: rows above which dW's tiles are two blocks wide and may be cut into parts
 constexpr int kShortRows = 2048;           // ... up to which the backward GEMMs' workers do not meet at every tile
 constexpr int kMinKeepRows = 2048;         // token losses: least rows of a block whose logits are kept
 
@@ -474,7 +475,7 @@ long long dw_tiles(int H, int V, bool wide, int tile_v) {
 // Rows of H values that both buffers of parts need (they are used one after the other).
 long long part_rows(int block_rows, int H, int V) {
     const long long dh = part_rows_dh(block_rows, H, V), tiles = dw_tiles(H, V, H > gemm_mma_n(H), kTileM);
-    if (2 * tiles > kMaxSms / 2) return dh;
+    if (block_rows <= kLongRows || 2 * tiles > kMaxSms / 2) return dh;
     const long long parts = kSplitWavesDw * (kMaxSms / 2) / tiles, dw = V * (parts < kMaxKSplits ? parts : kMaxKSplits);
     return dh > dw ? dh : dw;
 }
@@ -610,7 +611,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     lr.split = SplitParams{B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0, (H + cols_dh - 1) / cols_dh,
                            (V + kTileK - 1) / kTileK, ctx->sm_count / c_dh, gemm_tile_rows(c_dh), kSplitWaves};
     // few rows: a dW tile's epilogue must overlap the next tile's products, which only the narrow form does, and is not cut
-    const bool long_k = (rows_bound < B.rows ? rows_bound : B.rows) > 1024, wide_dw = two_blocks && c_dw == 2 && long_k;
+    const bool long_k = (rows_bound < B.rows ? rows_bound : B.rows) > kLongRows, wide_dw = two_blocks && c_dw == 2 && long_k;
     const long long tiles_dw = dw_tiles(H, V, wide_dw, gemm_tile_rows(c_dw));
     const bool split_dw = want_w && B.keep && long_k && ctx->sm_count <= kMaxSms && c_dw == 2 && 2 * tiles_dw <= ctx->sm_count / c_dw;
     lr.split_dw = SplitParams{split_dw ? kMaxKSplits : 0, static_cast<int>(tiles_dw), 0, ctx->sm_count / c_dw, kTileM, kSplitWavesDw};
@@ -825,9 +826,14 @@ int unity_create(unity_ctx** out, int device, void* cuda_stream, void* workspace
     *out = nullptr;
     if (workspace_bytes > 0 && !workspace) return UNITY_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign) return UNITY_ERR_ALIGNMENT;
-    cudaDeviceProp prop;
-    if (cudaGetDeviceProperties(&prop, device) != cudaSuccess) { cudaGetLastError(); return UNITY_ERR_CUDA; }
-    if (prop.major != 10) return UNITY_ERR_UNSUPPORTED_ARCH;
+    // (two attributes take microseconds, cudaGetDeviceProperties 2.4 ms)
+    int major = 0, sms = 0;
+    if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) != cudaSuccess) {
+        cudaGetLastError();
+        return UNITY_ERR_CUDA;
+    }
+    if (major != 10) return UNITY_ERR_UNSUPPORTED_ARCH;
     if (cudaSetDevice(device) != cudaSuccess) return UNITY_ERR_CUDA;
     unity_ctx* c = new (std::nothrow) unity_ctx();
     if (!c) return UNITY_ERR_CUDA;
@@ -836,7 +842,7 @@ int unity_create(unity_ctx** out, int device, void* cuda_stream, void* workspace
     c->stream = static_cast<cudaStream_t>(cuda_stream);
     c->ws = static_cast<char*>(workspace);
     c->ws_bytes = workspace_bytes;
-    c->sm_count = prop.multiProcessorCount;
+    c->sm_count = sms;
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || !fn ||
