@@ -157,14 +157,15 @@ __device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
     return *reinterpret_cast<unsigned*>(&v);
 }
 
-// The launch's arguments with everything that depends on the number of rows filled in from the device plan.
+// The launch's arguments with everything that depends on the number of rows of model k filled in from the device plan.
 template <int TILE_ROWS>
-__device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
+__device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in, int k) {
     GemmArgs g = in;
     if (in.span.plan == nullptr) return g;
+    RowSpan span = in.span;
+    span.model = k;
     int slot0, n_rows;
     // token losses: both schedules are read beside the plan, not after it (a memory latency less in every launch)
-    const int k = in.span.model;
     union { int4 v[2]; FwdShape f; } full, last;
     int4 split = make_int4(0, 0, 0, 0);
     long long stats_base = 0;
@@ -175,7 +176,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
     }
     if (in.shapes != nullptr && in.span_mode == kSpanRowsM) split = *reinterpret_cast<const int4*>(in.shapes->dh[k]);
     if (in.split_rows) split = *reinterpret_cast<const int4*>(in.shapes->dw[k]);
-    span_resolve(in.span, slot0, n_rows);
+    span_resolve(span, slot0, n_rows);
     if (in.span_mode == kSpanForward) {
         const FwdShape fs = in.shapes == nullptr ? forward_shape(in.fwd, n_rows) : (n_rows == in.span.row_cap ? full.f : last.f);
         g.a_row0 = slot0;
@@ -233,7 +234,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in) {
             g.c_split = static_cast<long long>(n_rows) * in.ldc;
         }
     } else if (in.span_mode == kSpanRowsK) {
-        g.k_iters = (in.shapes ? span_slab_rows(in.span, n_rows) : n_rows) / kTileK;
+        g.k_iters = (in.shapes ? span_slab_rows(span, n_rows) : n_rows) / kTileK;
         g.b_k0 = in.b_k0 + slot0;
         if (in.stash_by_slot) g.a_k0 = slot0;
         if (in.split_rows) {
@@ -457,9 +458,14 @@ __device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w,
     if (STASH && row_ok) k.tile_max[static_cast<long long>(row) * k.n_tiles + nt] = w.ref;
 }
 
-template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
-__global__ void __launch_bounds__(kThreads, 1)
-k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmArgs g_in) {
+// A worker (CTA or CTA pair) among those of its model.
+struct Worker {
+    int model, index, count;
+    void* out;               // replaces the arguments' output; null: they have it
+};
+
+template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB>
+__device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensorMap& tmB, const GemmArgs& g_in, const Worker& wk) {
     using C = Cfg<CTAS, NB, EPI>;
     constexpr int kStages = C::kStages, kStageBytes = C::kStageBytes, kABytes = C::kABytes, kBBytes = C::kBBytes;
     constexpr int kAccStages = C::kAccStages, kTileCols = C::kTileCols;
@@ -477,7 +483,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t cta_rank = CTAS == 2 ? ptx::cluster_ctarank() : 0u;     // 0: issues the MMAs, 1: its peer
-    const int pair = CTAS == 2 ? blockIdx.x >> 1 : blockIdx.x;              // index of this worker (CTA or CTA pair)
+    const int pair = wk.index;
     auto setup = [&] {
         if (threadIdx.x == 0) {
             for (int s = 0; s < kStages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); }
@@ -506,21 +512,23 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     }
     // The row extent of a launch may be known on the device only: derive it from the plan.  Every thread of both CTAs reads the
     // same plan, so a launch whose span is empty is left by all of them, here (at the end, once tensor memory is held).
-    const GemmArgs g = resolve_span<C::kTileRows>(g_in);
+    GemmArgs resolved = resolve_span<C::kTileRows>(g_in, wk.model);
+    if (wk.out != nullptr) { resolved.C = static_cast<float*>(wk.out); resolved.C16 = static_cast<__nv_bfloat16*>(wk.out); }
+    const GemmArgs& g = resolved;
     if (is_accum(EPI) && g.zero_if_empty && g.k_iters <= 0) {
         const long long n16 = static_cast<long long>(g.m_rows) * g.ldc / (EPI == kEpiAccumB16 ? 8 : 4);      // 16-byte units, whole ones
         uint4* out = EPI == kEpiAccumB16 ? reinterpret_cast<uint4*>(g.C16) : reinterpret_cast<uint4*>(g.C);
-        for (long long i = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x; i < n16; i += static_cast<long long>(gridDim.x) * kThreads)
+        for (long long i = (static_cast<long long>(pair) * CTAS + cta_rank) * kThreads + threadIdx.x; i < n16;
+             i += static_cast<long long>(wk.count) * CTAS * kThreads)
             out[i] = make_uint4(0, 0, 0, 0);
     }
     const bool idle = g.m_tiles <= 0 || g.n_tiles <= 0 || g.k_iters <= 0 ||
-                      (g.n_active > 0 && (CTAS == 2 ? blockIdx.x >> 1 : blockIdx.x) >= g.n_active);   // never holds a unit
+                      (g.n_active > 0 && pair >= g.n_active);   // never holds a unit
     if (!pdl) {
         if (idle) return;
         setup();
     }
-    const int n_launched = CTAS == 2 ? gridDim.x >> 1 : gridDim.x;
-    const int n_pairs = g.n_active > 0 && g.n_active < n_launched ? g.n_active : n_launched;   // workers at work
+    const int n_pairs = g.n_active > 0 && g.n_active < wk.count ? g.n_active : wk.count;   // workers at work
     const uint32_t tmem_base = *tmem_slot;
 
     const int gm = max(1, g.group_m);
@@ -986,31 +994,66 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
     }
 }
 
+template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
+__global__ void __launch_bounds__(kThreads, 1)
+k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const GemmArgs g_in) {
+    gemm_body<EPI, A_MN, B_MN, CTAS, NB>(tmA, tmB, g_in, Worker{g_in.span.model, static_cast<int>(blockIdx.x / CTAS),
+                                                                static_cast<int>(gridDim.x / CTAS), nullptr});
+}
+
+// The same for several models side by side, each on its share of the workers: a small problem's launch costs more than its
+// work (333 tokens of two models, 256 x 4096: 11 launches took 89 us, 7 take 57).
+template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
+__global__ void __launch_bounds__(kThreads, 1)
+k_gemm_models(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ ModelMaps maps, const GemmArgs g_in) {
+    const int w = blockIdx.x / CTAS, model = w % maps.n;
+    gemm_body<EPI, A_MN, B_MN, CTAS, NB>(tmA, maps.b[model], g_in, Worker{model, w / maps.n, static_cast<int>(gridDim.x / CTAS) / maps.n,
+                                                                          maps.out[model]});
+}
+
 
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
 cudaError_t set_attr() {
     return cudaFuncSetAttribute(k_gemm<EPI, A_MN, B_MN, CTAS, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 Cfg<CTAS, NB, EPI>::kSmemBytes);
 }
+template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
+cudaError_t set_attr_models() {
+    return cudaFuncSetAttribute(k_gemm_models<EPI, A_MN, B_MN, CTAS, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                Cfg<CTAS, NB, EPI>::kSmemBytes);
+}
+
+template <int EPI, int CTAS, int NB>
+struct LaunchConfig {
+    cudaLaunchConfig_t cfg;
+    cudaLaunchAttribute attr[2];
+    LaunchConfig(int workers, bool pdl, cudaStream_t stream) {
+        memset(&cfg, 0, sizeof(cfg));
+        cfg.gridDim = dim3(workers * CTAS, 1, 1);
+        cfg.blockDim = dim3(kThreads, 1, 1);
+        cfg.dynamicSmemBytes = Cfg<CTAS, NB, EPI>::kSmemBytes;
+        cfg.stream = stream;
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = CTAS;
+        attr[0].val.clusterDim.y = 1;
+        attr[0].val.clusterDim.z = 1;
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = pdl ? 2 : 1;
+    }
+};
 
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
 cudaError_t launch(const CUtensorMap& tmA, const CUtensorMap& tmB, const GemmArgs& args, int workers, cudaStream_t stream) {
-    cudaLaunchConfig_t cfg;
-    memset(&cfg, 0, sizeof(cfg));
-    cfg.gridDim = dim3(workers * CTAS, 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = Cfg<CTAS, NB, EPI>::kSmemBytes;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = CTAS;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = args.pdl ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_gemm<EPI, A_MN, B_MN, CTAS, NB>, tmA, tmB, args);
+    LaunchConfig<EPI, CTAS, NB> c(workers, args.pdl != 0, stream);
+    return cudaLaunchKernelEx(&c.cfg, k_gemm<EPI, A_MN, B_MN, CTAS, NB>, tmA, tmB, args);
+}
+
+template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
+cudaError_t launch_models(const CUtensorMap& tmA, const ModelMaps& maps, const GemmArgs& args, int workers, cudaStream_t stream) {
+    LaunchConfig<EPI, CTAS, NB> c(workers * maps.n, args.pdl != 0, stream);
+    return cudaLaunchKernelEx(&c.cfg, k_gemm_models<EPI, A_MN, B_MN, CTAS, NB>, tmA, maps, args);
 }
 
 }  // namespace
@@ -1033,7 +1076,37 @@ cudaError_t gemm_set_attributes() {
     if ((e = set_attr<kEpiAccumB16, true, true, 1>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiAccumB16, true, true, 2>()) != cudaSuccess) return e;
     if ((e = set_attr<kEpiAccumB16, true, true, 2, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiLossStats, false, false, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiLossStats, false, false, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiAccumF32, false, true, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiAccumF32, false, true, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiAccumF32, false, true, 2, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiAccumF32, true, true, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiAccumF32, true, true, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiAccumB16, true, true, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr_models<kEpiAccumB16, true, true, 2>()) != cudaSuccess) return e;
     return set_attr<kEpiAccumF32, true, true, 2, 2>();
+}
+
+cudaError_t launch_gemm_models(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap& tmA, const ModelMaps& maps,
+                               const GemmArgs& args, int sm_count, cudaStream_t stream, bool wide) {
+    const int workers = sm_count / ctas / maps.n;              // of each model
+    if (is_accum(epi) && (args.mma_n < 32 || args.mma_n > kTileN || args.mma_n % 32 != 0)) return cudaErrorInvalidValue;
+    const bool two = ctas == 2;
+    if (epi == kEpiLossStats)
+        return two ? launch_models<kEpiLossStats, false, false, 2>(tmA, maps, args, workers, stream)
+                   : launch_models<kEpiLossStats, false, false, 1>(tmA, maps, args, workers, stream);
+    if (epi == kEpiAccumB16 && a_mn && !wide)
+        return two ? launch_models<kEpiAccumB16, true, true, 2>(tmA, maps, args, workers, stream)
+                   : launch_models<kEpiAccumB16, true, true, 1>(tmA, maps, args, workers, stream);
+    if (epi == kEpiAccumF32 && a_mn && !wide)
+        return two ? launch_models<kEpiAccumF32, true, true, 2>(tmA, maps, args, workers, stream)
+                   : launch_models<kEpiAccumF32, true, true, 1>(tmA, maps, args, workers, stream);
+    if (epi == kEpiAccumF32 && !a_mn && wide && two) return launch_models<kEpiAccumF32, false, true, 2, 2>(tmA, maps, args, workers, stream);
+    if (epi == kEpiAccumF32 && !a_mn && !wide)
+        return two ? launch_models<kEpiAccumF32, false, true, 2>(tmA, maps, args, workers, stream)
+                   : launch_models<kEpiAccumF32, false, true, 1>(tmA, maps, args, workers, stream);
+    return cudaErrorInvalidValue;
 }
 
 int gemm_tile_rows(int ctas) { return kCtaM * ctas; }

@@ -259,6 +259,15 @@ struct GemmArgs {
 // (a worker without a unit leaves at once).
 cudaError_t launch_gemm(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap& tmA, const CUtensorMap& tmB,
                         const GemmArgs& args, int sm_count, cudaStream_t stream, bool wide = false, int workers = 0);
+// A launch for several models at once (token losses): worker w takes model w % n of the span's plan, its B operand and output.
+constexpr int kMaxGroup = 4;
+struct ModelMaps {
+    CUtensorMap b[kMaxGroup];
+    void* out[kMaxGroup];        // accumulating epilogues
+    int n;
+};
+cudaError_t launch_gemm_models(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap& tmA, const ModelMaps& maps,
+                               const GemmArgs& args, int sm_count, cudaStream_t stream, bool wide = false);
 int gemm_tile_rows(int ctas);
 int gemm_mma_n(int n_cols);   // block width for an fp32-accumulate GEMM with n_cols output columns
 cudaError_t gemm_set_attributes();
@@ -506,10 +515,11 @@ cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaSt
 struct StoreArgs {
     const float* parts;        // [parts][rows of the span][H]
     const int* slot_tok;
-    RowSpan span;
-    int H;
+    RowSpan span;              // (model < 0: up to row_cap rows of each of the K models, whose parts are part_stride apart)
+    int K, H;
+    long long part_stride;
     const LossShapes* shapes;  // null: one part
-    int bound;                 // rows the span can have at most
+    long long bound;           // rows of the launch at most
     __nv_bfloat16* dHidden;
 };
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream);

@@ -668,16 +668,28 @@ __device__ __forceinline__ uint2 pack4(float4 v) {
 // Four columns per thread: the parts added in their order, one rounding to bf16.
 __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
     begin();
-    int slot0, rows;
-    span_resolve(a.span, slot0, rows);
     const int per_row = a.H >> 2;
     const long long i = static_cast<long long>(blockIdx.x) * 256 + threadIdx.x;
-    const int r = static_cast<int>(i / per_row), c = static_cast<int>(i - static_cast<long long>(r) * per_row) * 4;
+    int r = static_cast<int>(i / per_row), model = a.span.model;
+    const int c = static_cast<int>(i - static_cast<long long>(r) * per_row) * 4;
+    int slot0 = 0, rows;
+    const float* parts = a.parts;
+    if (model < 0) {
+        if (r >= a.span.plan->off[a.K]) return;
+        model = 0;
+        while (r >= a.span.plan->off[model + 1]) ++model;
+        slot0 = a.span.plan->off[model];
+        rows = min(a.span.plan->off[model + 1] - slot0, a.span.row_cap);
+        r -= slot0;
+        parts += model * a.part_stride;
+    } else {
+        span_resolve(a.span, slot0, rows);
+    }
     if (r >= rows) return;
     const int tok = a.slot_tok[slot0 + r];
-    const int splits = a.shapes ? a.shapes->dh[a.span.model][rows == a.span.row_cap ? 0 : 1].splits : 1;
+    const int splits = a.shapes ? a.shapes->dh[model][rows == a.span.row_cap ? 0 : 1].splits : 1;
     if (tok < 0) return;
-    const float4 v = sum_parts(a.parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
+    const float4 v = sum_parts(parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
     *reinterpret_cast<uint2*>(a.dHidden + static_cast<long long>(tok) * a.H + c) = pack4(v);
 }
 
@@ -776,7 +788,7 @@ cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaSt
 }
 
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {
-    return launch(k_store_parts, dim3(static_cast<unsigned>((static_cast<long long>(a.bound) * (a.H >> 2) + 255) / 256)), 256, stream, a);
+    return launch(k_store_parts, dim3(static_cast<unsigned>((a.bound * (a.H >> 2) + 255) / 256)), 256, stream, a);
 }
 
 cudaError_t launch_sum_dw(const SumDwArgs& a, cudaStream_t stream) {

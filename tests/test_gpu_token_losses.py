@@ -248,6 +248,7 @@ def test_every_workspace_down_to_the_least_gives_the_same_answer(op):
     (8192, 64, 72, 1, 1500), (8193, 64, 72, 2, 40),                           # or by several; boundaries staged or searched
     (10, 128, 20000, 1, 3), (40, 1344, 6000, 2, 4),                           # few rows: a contraction in many parts
     (700, 896, 3000, 1, 9), (2600, 192, 1000, 2, 6),
+    (90, 64, 4104, 4, 9), (900, 640, 3000, 4, 9), (60, 64, 520, 5, 9),        # models side by side in a launch, and one too many
     (6000, 256, 1024, 1, 9), (5000, 576, 600, 3, 9)])                         # many rows of a small head: dW in parts
 def test_sizes_where_the_way_of_working_changes(N, H, V, K, n_inv, op):
     p = Problem(N, H, V, K, K, n_inv=n_inv, n_top=7, seed=N + H).gpu()
