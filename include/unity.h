@@ -409,14 +409,18 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
  * update - recorded answers (cross entropy) or a teacher's listed logits (distillation).  Rows, routing, masks and
  * limits are those of stages 2 and 3; with z = inv_temperature * W_{model(i)} h_i, p = softmax(z), lse = log sum exp z:
  *   loss[k] = (1/M_k) sum_{valid i of model k} tok_weight[i] * l_i ,  M_k = norm[k] if given else max(#valid rows, 1)
- * Forms: evaluation (dHidden and dW NULL: one sweep over the vocabulary), frozen head (dW NULL), training.  The logits
- * exist only in tensor memory; the backward works on bounded blocks of dL/dz.
+ * Forms: evaluation (dHidden and dW NULL: one sweep over the vocabulary), frozen head (dW NULL), training, head alone
+ * (dHidden NULL).  The n_tok x V logits are never kept: an evaluation has them in tensor memory only; the backward works on
+ * blocks of at most 18432 rows, whose logits the forward sweep leaves in the workspace in 16 bits each (about 6 GB at
+ * V = 152064 whatever the batch), where they become dL/dz.  A workspace without room for that takes smaller blocks, down to
+ * 2048 rows, and below that the logits are recomputed in pieces of the vocabulary (a third more work).
  *   tok_weight : f32 [n_tok] or NULL (= all 1), any sign; not read where tok_mask is 0
  *   loss       : out f32 [K];  tok_loss (l_i, without its weight), lse : out f32 [n_tok] or NULL, 0 on masked rows
  *   dHidden    : out bf16 [n_tok, H] or NULL (zeros on masked rows)
  *   dW         : (host) K device pointers or NULL, each f32 or bf16 [V, H] (dW_type).  bf16 is rounded once, from the fp32
  *                sum over all rows (plus the old value with accumulate_dW)
- * dL/dz is held in bf16 between the products, as in stage 3: a gradient entry is off by up to 2^-8 of the terms it sums.
+ * dL/dz is held in bf16 between the products, as in stage 3: a gradient entry is off by up to 2^-8 of the terms it sums (and
+ * a kept logit by up to 2^-10 octaves).
  * Deterministic: no floating-point atomics anywhere. */
 #define UNITY_F32 0
 #define UNITY_BF16 1
@@ -424,7 +428,8 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
 #define UNITY_TEACHER_LOGPROBS 1 /* q = exp(top_vals) as given; what the list leaves out is left out of the loss      */
 
 /* Scratch bytes with which the calls below run with full-size blocks (n_top = 0 for the cross entropy, backward = 0
- * for evaluation only). */
+ * for evaluation only).  A call with less takes smaller blocks; one that does not fit at all returns UNITY_ERR_WORKSPACE with
+ * the least number of bytes in unity_last_error().  bf16 dW over several blocks needs 4*V*H bytes of it. */
 size_t unity_token_loss_workspace_bytes(int64_t n_tok, int32_t H, int32_t V, int32_t K, int32_t n_top, int32_t backward);
 
 /* Cross entropy of the targets:

@@ -319,12 +319,14 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
 //   s = sum 2^((z - ref) c2), z2 = sum z (both as even / odd halves), the target's logit, and where the row stands in its
 //   ascending list of entries (next vocabulary index, INT_MAX: none left).
 // ref need not be the maximum: it is 0 where the first tile's maximum lies within kRefBelow octaves below and kRefRoom above
-// that, else that maximum, and later a tile's maximum more than kRefRoom octaves above it.  So a tile is read from tensor memory once (a maximum first and the sum after it would read it twice: 276
-// against 353 us at 801 x 896 x 151936, where the epilogue is the bound), no sum exceeds 2^kRefRoom * V, and for a backward
-// pass that does not recompute the logits (ref - z) + kRefRoom octaves is kept in steps of 2^-9 octaves, 16 bits.  The integer
-// costs as much memory as bf16 but is off by at most half a step whatever its size: p is off by a factor of 2^(2^-10), 6.8e-4,
-// where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 96 octaves or more below ref, 64 below the row's
-// maximum, count as 96.
+// that, else that maximum, and later a tile's maximum more than kRefRoom octaves above it.  So a tile is read from tensor
+// memory once (a maximum first and the sum after it read it twice: 252 against 353 us at 801 x 896 x 151936), no sum exceeds
+// 2^kRefRoom * V, and for a backward pass that does not recompute the logits (ref - z) + kRefRoom octaves is kept in steps of
+// 2^-9 octaves, 16 bits.  The integer costs as much memory as bf16 but is off by at most half a step whatever its size: p is
+// off by a factor of 2^(2^-10), 6.8e-4, where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 96
+// octaves or more below ref, and so 64 below the row's maximum, count as 96.
+// Bound: the MMAs and the 1 kW power cap (801 x 896 x 151936: 185 us, 1.5 PFLOP/s of the rows the tiles are padded to; without
+// this epilogue's arithmetic 172 us).
 struct LossRow {
     float ref, z_tgt;
     uint64_t s, z2;
@@ -432,15 +434,18 @@ __device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w,
 #pragma unroll 1
         for (int c = 0; c * 32 < n_tile; ++c) {
             const bool more = (c + 1) * 32 < n_tile;
+            __syncwarp();                                      // rows part ways at their targets and listed entries
             if (more) ptx::tmem_ld_32x32(taddr + (c + 1) * 32, rb);
             work(ra, c);
             if (!more) break;
+            __syncwarp();
             ptx::tmem_ld_wait_for(rb);
 #pragma unroll
             for (int j = 0; j < 32; ++j) ra[j] = rb[j];
         }
         // A row whose maximum rose past the room takes it as its new reference and its warp works through the tile again
         // (the list cursor has moved on: its logits are written; the target's is the same).  A second time is enough.
+        __syncwarp();
         const bool over = (tm - w.ref) * k.c2 > kRefRoom || (w.first && (tm - w.ref) * k.c2 < -kRefBelow);
         w.first = false;
         if (attempt == 0 && __any_sync(0xffffffffu, over)) {

@@ -54,8 +54,7 @@ __device__ __forceinline__ long long warp_min64(long long v) {
     return v;
 }
 
-// One warp: the forward schedule and dHidden's parts for `rows` rows, lanes weighing candidates side by side (the same
-// choice as forward_shape's).
+// One warp: the parts of a contraction, a candidate per lane.
 __device__ __forceinline__ SplitShape warp_split(const SplitParams& p, int m_tiles) {
     SplitShape s;
     long long best = 0x7fffffffffffffffll;
@@ -66,7 +65,7 @@ __device__ __forceinline__ SplitShape warp_split(const SplitParams& p, int m_til
     split_candidate(p, m_tiles, static_cast<int>(best & 63), s);
     return s;
 }
-// `valid`: the rows that hold tokens
+// ... and the schedules of `rows` packed rows, `valid` of which hold tokens (the forward's is forward_shape's choice).
 __device__ __forceinline__ void warp_shapes(const LossRouteArgs& a, int rows, int valid, FwdShape* fwd, SplitShape* dh, SplitShape* dw) {
     const int lane = threadIdx.x & 31;
     const FwdPlanParams& p = a.route.fwd;
@@ -497,12 +496,12 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
             Q = warp_sum(Q);
             l = a.kd * kl + (a.hard > 0.f ? a.hard * dy : 0.f);
             cp = a.kd * Q + a.hard;
-            gt = a.hard > 0.f ? cp * expf(-dy) - a.hard : 0.f;
+            gt = a.hard > 0.f ? a.kd * Q * expf(-dy) + a.hard * expm1f(-dy) : 0.f;
             if (a.with_grad) {
                 for (int j = lane; j < cnt; j += 32) {         // the logits give way to the entries' gradients
                     const float d = a.scale * (m - a.top_z[base + j]) + log_s;
-                    const float own = a.kd * a.q_p[base + j] + (a.ids_p[base + j] == tgt ? a.hard : 0.f);
-                    a.top_z[base + j] = cg * (cp * expf(-d) - own);
+                    const float p = expf(-d), hard = a.ids_p[base + j] == tgt ? expm1f(-d) : p;
+                    a.top_z[base + j] = cg * (a.kd * (Q * p - a.q_p[base + j]) + a.hard * hard);
                 }
             }
         }
