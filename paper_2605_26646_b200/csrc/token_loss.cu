@@ -332,8 +332,9 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
 
 // One warp per packed row and per token, w: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
 // zeros for a masked token's gradient row; with teacher's lists, every second warp takes a row's list.
+// `twice`: the row is packed kLowRows rows further on as well.
 __device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w, bool list, int n_slots, int tok, bool masked,
-                                           int (*sh_id)[kMaxTop], float (*sh_q)[kMaxTop]) {
+                                           bool twice, int (*sh_id)[kMaxTop], float (*sh_q)[kMaxTop]) {
     const int lane = threadIdx.x & 31, n16 = a.H >> 3;
     if (list) {
         if (w >= n_slots) return;                              // whole warps leave: only warp-wide barriers below
@@ -347,8 +348,12 @@ __device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w,
     }
     if (w >= n_slots) return;
     uint4* dst = reinterpret_cast<uint4*>(a.hp + w * a.H);
+    uint4* low = dst + static_cast<long long>(kLowRows) * n16;
     if (tok < 0) {
-        for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
+        for (int j = lane; j < n16; j += 32) {
+            dst[j] = make_uint4(0, 0, 0, 0);
+            if (twice) low[j] = make_uint4(0, 0, 0, 0);
+        }
         if (lane == 0) a.target_p[w] = 0;
         return;
     }
@@ -359,6 +364,10 @@ __device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w,
         for (int u = 0; u < 8; ++u) if (j0 + 32 * u < n16) v[u] = src[j0 + 32 * u];
 #pragma unroll
         for (int u = 0; u < 8; ++u) if (j0 + 32 * u < n16) dst[j0 + 32 * u] = v[u];
+        if (twice) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) if (j0 + 32 * u < n16) low[j0 + 32 * u] = v[u];
+        }
     }
     if (lane == 0) a.target_p[w] = a.target ? a.target[tok] : -1;
 }
@@ -372,7 +381,7 @@ __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
     if (a.n_top > 0) w >>= 1;
     const int tok = w < a.max_slots ? a.slot_tok[w] : -1;      // (not written beyond off[K]: not used there)
     const bool masked = a.dHidden != nullptr && w < a.n_tok && a.tok_slot[w] < 0;
-    gather_row(a, w, list, a.plan->off[a.K], tok, masked, sh_id, sh_q);
+    gather_row(a, w, list, a.plan->off[a.K], tok, masked, false, sh_id, sh_q);
 }
 
 // Up to kLossPackTokens tokens: routing and packing in one launch.  Every block routes all tokens for itself (a few memory
@@ -403,12 +412,18 @@ __global__ void __launch_bounds__(256) k_loss_pack(LossRouteArgs r, LossGatherAr
     long long w = static_cast<long long>(blockIdx.x - 1) * 8 + (threadIdx.x >> 5);
     const bool list = a.n_top > 0 && (w & 1);
     if (a.n_top > 0) w >>= 1;
-    int tok = -1, first = 0;
+    int tok = -1, first = 0, rel = 0;
     for (int k = 0; k < r.route.K; ++k) {
-        if (w >= sh.off[k] && w < sh.off[k] + sh.tot[k]) tok = sh_tok[first + static_cast<int>(w) - sh.off[k]];
+        if (w >= sh.off[k] && w < sh.off[k + 1]) {
+            rel = static_cast<int>(w) - sh.off[k];
+            if (rel < sh.tot[k]) tok = sh_tok[first + rel];
+        }
         first += sh.tot[k];
     }
-    gather_row(a, w, list, sh.off[r.route.K], tok, w < n && sh_model[w] < 0, sh_id, sh_q);
+    // (a row whose place the first rows' second copies take is left alone, but for its list and its token's zeros)
+    int n_slots = sh.off[r.route.K];
+    if (a.low_half && !list && rel >= kLowRows && rel < 2 * kLowRows) n_slots = 0;
+    gather_row(a, w, list, n_slots, tok, w < n && sh_model[w] < 0, a.low_half && rel < kLowRows, sh_id, sh_q);
 }
 
 // One warp per packed row: merge the vocabulary splits' statistics (one lane per split), then the row's loss and what
@@ -565,7 +580,8 @@ __global__ void __launch_bounds__(256) k_teacher_scatter(TeacherScatterArgs a) {
 // per SM walk the items (1200 rows x 151936: 138 us, 5.3 TB/s of the copy's 6.5; five blocks with more registers: 163 us).
 constexpr int kGradVecs = 4;
 constexpr int kGradCols = 256 * 8 * kGradVecs;
-__global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
+template <bool LOW>
+__global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGradArgs a) {
     begin();
     // the rows that the contractions read: of a block, or of every model (their slabs end with the last token)
     __shared__ int sh_off[UNITY_MAX_MODELS], sh_rows[UNITY_MAX_MODELS];
@@ -594,6 +610,7 @@ __global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
         }
         const int slot = row0 + r;
         uint4* row = reinterpret_cast<uint4*>(a.Z + static_cast<long long>(r) * a.ld);
+        uint4* low_row = LOW ? row + kLowRows * (a.ld >> 3) : nullptr;
         const float* tm = a.tile_max + static_cast<long long>(r) * a.n_tiles;
         uint4 raw[kGradVecs];
         float shift[kGradVecs];
@@ -611,6 +628,7 @@ __global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
             if (c0 >= a.cols) continue;
             const float sh = fmaf(shift[u], a.c2, base);
             unsigned* w = reinterpret_cast<unsigned*>(&raw[u]);
+            unsigned lw[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float u0 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7610)) - 8388608.f;
@@ -619,16 +637,24 @@ __global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
                 const float g1 = fmaf(cp, ptx::ex2(fmaf(u1, -1.f / kStashSteps, sh)), -cu);
                 const __nv_bfloat162 h = __floats2bfloat162_rn(g0, g1);
                 w[j] = *reinterpret_cast<const unsigned*>(&h);
+                if (LOW) {
+                    const float2 f = __bfloat1622float2(h);
+                    const __nv_bfloat162 l = __floats2bfloat162_rn(g0 - f.x, g1 - f.y);
+                    lw[j] = *reinterpret_cast<const unsigned*>(&l);
+                }
             }
             if (static_cast<unsigned>(tgt - c0) < 8u) {        // the target is among this thread's eight
-                const unsigned bits = __bfloat16_as_ushort(__float2bfloat16_rn(gt));
+                const __nv_bfloat16 hi = __float2bfloat16_rn(gt);
+                const unsigned bits = __bfloat16_as_ushort(hi);
+                const unsigned low = LOW ? __bfloat16_as_ushort(__float2bfloat16_rn(gt - __bfloat162float(hi))) : 0u;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    if (tgt - c0 == 2 * j) w[j] = (w[j] & 0xffff0000u) | bits;
-                    if (tgt - c0 == 2 * j + 1) w[j] = (w[j] & 0x0000ffffu) | (bits << 16);
+                    if (tgt - c0 == 2 * j) { w[j] = (w[j] & 0xffff0000u) | bits; if (LOW) lw[j] = (lw[j] & 0xffff0000u) | low; }
+                    if (tgt - c0 == 2 * j + 1) { w[j] = (w[j] & 0x0000ffffu) | (bits << 16); if (LOW) lw[j] = (lw[j] & 0x0000ffffu) | (low << 16); }
                 }
             }
             row[c0 >> 3] = raw[u];
+            if (LOW) low_row[c0 >> 3] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
         }
         if (a.n_top > 0) {                                     // the row's listed entries among this block's columns
             __syncthreads();
@@ -636,8 +662,11 @@ __global__ void __launch_bounds__(256, 8) k_loss_grad_inplace(LossGradArgs a) {
             const int cnt = a.cnt_p[slot];
             for (int j = threadIdx.x; j < cnt; j += 256) {
                 const int c = a.ids_p[at + j] - c_lo;
-                if (c >= 0 && c < kGradCols)
-                    reinterpret_cast<__nv_bfloat16*>(row)[c_lo + c] = __float2bfloat16_rn(a.top_g[at + j]);
+                if (c < 0 || c >= kGradCols) continue;
+                const float g = a.top_g[at + j];
+                const __nv_bfloat16 hi = __float2bfloat16_rn(g);
+                reinterpret_cast<__nv_bfloat16*>(row)[c_lo + c] = hi;
+                if (LOW) reinterpret_cast<__nv_bfloat16*>(low_row)[c_lo + c] = __float2bfloat16_rn(g - __bfloat162float(hi));
             }
         }
     }
@@ -688,7 +717,11 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
     const int tok = a.slot_tok[slot0 + r];
     const int splits = a.shapes ? a.shapes->dh[model][rows == a.span.row_cap ? 0 : 1].splits : 1;
     if (tok < 0) return;
-    const float4 v = sum_parts(parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
+    float4 v = sum_parts(parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
+    if (a.low_half) {
+        const float4 l = sum_parts(parts + static_cast<long long>(r + kLowRows) * a.H + c, splits, static_cast<long long>(rows) * a.H);
+        v.x += l.x; v.y += l.y; v.z += l.z; v.w += l.w;
+    }
     *reinterpret_cast<uint2*>(a.dHidden + static_cast<long long>(tok) * a.H + c) = pack4(v);
 }
 
@@ -783,7 +816,7 @@ cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t str
 cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream) {
     const long long items = static_cast<long long>(a.span.row_cap) * ((a.cols + kGradCols - 1) / kGradCols);
     const long long blocks = 8ll * sm_count;                  // as many as are resident
-    return launch(k_loss_grad_inplace, dim3(static_cast<unsigned>(items < blocks ? items : blocks)), 256, stream, a);
+    return launch(a.low_half ? k_loss_grad_inplace<true> : k_loss_grad_inplace<false>, dim3(static_cast<unsigned>(items < blocks ? items : blocks)), 256, stream, a);
 }
 
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {
