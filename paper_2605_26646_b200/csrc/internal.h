@@ -445,7 +445,7 @@ struct LossGatherArgs {
     const int* target;         // nullable
     __nv_bfloat16 *hp, *dHidden;   // dHidden nullable
     int* target_p;
-    int low_half;              // a model's first kLowRows rows are packed twice (see LossGradArgs); at most as many tokens
+    int low_rows;              // a model's first low_rows rows are packed twice (see LossGradArgs); 0: none
     int n_top, logits;         // logits 1: softmax of the listed logits (times scale); 0: exp of listed log-probabilities
     float scale;
     const int* top_ids;        // caller order [n_tok, n_top]
@@ -510,13 +510,13 @@ struct LossGradArgs {
     int n_top;                 // the listed entries' gradients go in last (0: none)
     const int *ids_p, *cnt_p;
     const float* top_g;
-    int low_half;              // row r + kLowRows of the model takes what rounding to bf16 cut from row r
+    int low_rows;              // > 0: row r + low_rows of the model takes what rounding to bf16 cut from row r
 };
-// Up to kLowRows tokens, half of the one 128-row tile is empty: it takes the gradients' low halves, and dHidden and dW come
-// from 16 bits of dL/dz at no cost.  (With few tokens a gradient row is hardly more than the target's entry times a row of W
-// or of hidden, and the rounding of that one entry does not average out: 2.8e-3 in the 2-norm where the output's own rounding
-// is 1.7e-3.)
-constexpr int kLowRows = 64;
+// Up to 64 tokens half of the one 128-row tile is empty: it takes the gradients' low halves, and dHidden and dW come from 16
+// bits of dL/dz, for 2 to 4 % of the time.  (With few tokens a gradient row is hardly more than the target's entry times a row of W or of hidden,
+// and the rounding of that one entry does not average out: up to 3e-3 in the 2-norm where the output's own rounding is 1.7e-3.
+// From 65 to 128 tokens it would take a tile of 256 rows and 18-24 % of the time.)
+constexpr int kLowTokens = 64;
 cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream);
 // dHidden[token of slot r of the span] = bf16(sum of the row's parts), in the order of the parts
 struct StoreArgs {
@@ -526,7 +526,7 @@ struct StoreArgs {
     int K, H;
     long long part_stride;
     const LossShapes* shapes;  // null: one part
-    int low_half;              // row r + kLowRows belongs to row r (see LossGradArgs)
+    int low_rows;              // > 0: row r + low_rows belongs to row r (see LossGradArgs)
     long long bound;           // rows of the launch at most
     __nv_bfloat16* dHidden;
 };

@@ -332,7 +332,7 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
 
 // One warp per packed row and per token, w: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
 // zeros for a masked token's gradient row; with teacher's lists, every second warp takes a row's list.
-// `twice`: the row is packed kLowRows rows further on as well.
+// `twice`: the row is packed low_rows rows further on as well.
 __device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w, bool list, int n_slots, int tok, bool masked,
                                            bool twice, int (*sh_id)[kMaxTop], float (*sh_q)[kMaxTop]) {
     const int lane = threadIdx.x & 31, n16 = a.H >> 3;
@@ -348,7 +348,7 @@ __device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w,
     }
     if (w >= n_slots) return;
     uint4* dst = reinterpret_cast<uint4*>(a.hp + w * a.H);
-    uint4* low = dst + static_cast<long long>(kLowRows) * n16;
+    uint4* low = dst + static_cast<long long>(a.low_rows) * n16;
     if (tok < 0) {
         for (int j = lane; j < n16; j += 32) {
             dst[j] = make_uint4(0, 0, 0, 0);
@@ -422,8 +422,8 @@ __global__ void __launch_bounds__(256) k_loss_pack(LossRouteArgs r, LossGatherAr
     }
     // (a row whose place the first rows' second copies take is left alone, but for its list and its token's zeros)
     int n_slots = sh.off[r.route.K];
-    if (a.low_half && !list && rel >= kLowRows && rel < 2 * kLowRows) n_slots = 0;
-    gather_row(a, w, list, n_slots, tok, w < n && sh_model[w] < 0, a.low_half && rel < kLowRows, sh_id, sh_q);
+    if (!list && rel >= a.low_rows && rel < 2 * a.low_rows) n_slots = 0;
+    gather_row(a, w, list, n_slots, tok, w < n && sh_model[w] < 0, rel < a.low_rows, sh_id, sh_q);
 }
 
 // One warp per packed row: merge the vocabulary splits' statistics (one lane per split), then the row's loss and what
@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
         }
         const int slot = row0 + r;
         uint4* row = reinterpret_cast<uint4*>(a.Z + static_cast<long long>(r) * a.ld);
-        uint4* low_row = LOW ? row + kLowRows * (a.ld >> 3) : nullptr;
+        uint4* low_row = LOW ? row + a.low_rows * (a.ld >> 3) : nullptr;
         const float* tm = a.tile_max + static_cast<long long>(r) * a.n_tiles;
         uint4 raw[kGradVecs];
         float shift[kGradVecs];
@@ -718,8 +718,8 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
     const int splits = a.shapes ? a.shapes->dh[model][rows == a.span.row_cap ? 0 : 1].splits : 1;
     if (tok < 0) return;
     float4 v = sum_parts(parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
-    if (a.low_half) {
-        const float4 l = sum_parts(parts + static_cast<long long>(r + kLowRows) * a.H + c, splits, static_cast<long long>(rows) * a.H);
+    if (a.low_rows > 0) {
+        const float4 l = sum_parts(parts + static_cast<long long>(r + a.low_rows) * a.H + c, splits, static_cast<long long>(rows) * a.H);
         v.x += l.x; v.y += l.y; v.z += l.z; v.w += l.w;
     }
     *reinterpret_cast<uint2*>(a.dHidden + static_cast<long long>(tok) * a.H + c) = pack4(v);
@@ -816,7 +816,7 @@ cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t str
 cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream) {
     const long long items = static_cast<long long>(a.span.row_cap) * ((a.cols + kGradCols - 1) / kGradCols);
     const long long blocks = 8ll * sm_count;                  // as many as are resident
-    return launch(a.low_half ? k_loss_grad_inplace<true> : k_loss_grad_inplace<false>, dim3(static_cast<unsigned>(items < blocks ? items : blocks)), 256, stream, a);
+    return launch(a.low_rows > 0 ? k_loss_grad_inplace<true> : k_loss_grad_inplace<false>, dim3(static_cast<unsigned>(items < blocks ? items : blocks)), 256, stream, a);
 }
 
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream) {

@@ -592,11 +592,12 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     int nl = 0, rc;
     // At most 128 rows: one row tile of a single CTA instead of a half empty one of a CTA pair, for every GEMM whose rows they
     // are (with 87 rows at H = 3584 the products then take less time than the heads' bytes)
+    // Up to 64 of them: a gradient's low halves take as many rows again (see LossGradArgs)
+    const int low_rows = B.joint && r->n_tok <= kLowTokens ? kLowTokens : 0;
     const bool few = r->n_tok <= kCtaM;
     const int c_fwd = few ? 1 : ctx->ctas[UNITY_PROF_FWD_GEMM], c_grad = few ? 1 : ctx->ctas[UNITY_PROF_GRAD_GEMM],
               c_dh = few ? 1 : ctx->ctas[UNITY_PROF_DH_GEMM], c_dw = ctx->ctas[UNITY_PROF_DW_GEMM];
     const int at_once = !want || B.joint ? models_at_once(r->n_tok, H, V, K) : 1;   // models that share a launch
-    const bool low_half = B.joint && r->n_tok <= kLowRows;
     const int cap_all = few ? kCtaM : 0x7fffff00;            // rows of a span that covers a model
     const int mma_n = gemm_mma_n(H);
     const bool two_blocks = ctx->wide_acc && H > mma_n, wide_dh = two_blocks && c_dh == 2;
@@ -628,7 +629,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     lr.max_slots = L.max_slots; lr.shapes = L.shapes; lr.counters = L.sync_counters; lr.n_counters = L.n_counters; lr.tok_loss = c.tok_loss; lr.lse = c.lse;
     __nv_bfloat16* dH = static_cast<__nv_bfloat16*>(c.dHidden);
     const LossGatherArgs ga{L.plan, L.slot_tok, L.tok_slot, K, V, H, r->n_tok, L.max_slots,
-                            static_cast<const __nv_bfloat16*>(r->hidden), r->target, L.hp, dH, L.target_p, low_half, c.n_top, c.logits,
+                            static_cast<const __nv_bfloat16*>(r->hidden), r->target, L.hp, dH, L.target_p, low_rows, c.n_top, c.logits,
                             r->inv_temperature, c.top_ids, c.top_vals, L.ids_p, L.cnt_p, L.q_p, ctx->d_status};
     CUDA_TRY(ctx, launch_loss_pack(lr, ga, st, &nl));
 
@@ -674,7 +675,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     lg.n_tiles = fwd.n_tiles; lg.tile_max = L.tile_max; lg.c2 = scale * 1.4426950408889634f;
     lg.target_p = L.target_p; lg.row_lse = L.row_lse; lg.coef_p = L.coef_p; lg.coef_g = L.coef_g; lg.target_g = L.target_g;
     lg.uniform = c.smoothing / static_cast<float>(V);
-    lg.n_top = c.n_top; lg.ids_p = L.ids_p; lg.cnt_p = L.cnt_p; lg.top_g = L.top_z; lg.low_half = low_half;
+    lg.n_top = c.n_top; lg.ids_p = L.ids_p; lg.cnt_p = L.cnt_p; lg.top_g = L.top_z; lg.low_rows = low_rows;
     auto convert = [&](const RowSpan& span) {
         lg.span = span;
         ProfScope ps(ctx, UNITY_PROF_GRAD_GEMM);
@@ -790,7 +791,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     if (ci + 1 == n_pieces) {
                         RowSpan stored = chunk;
                         if (at_once > 1) stored.model = -1;
-                        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, low_half,
+                        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, low_rows,
                                            at_once > 1 ? L.max_slots : bound, dH};
                         CUDA_TRY(ctx, launch_store_parts(sa, st));
                         nl += 1;
@@ -814,7 +815,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         memset(&w, 0, sizeof(w));
                         w.pdl = 1;
                         w.mma_n = part == 0 ? mma_n : narrow_n;
-                        w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = t1 - t0; w.shapes = low_half ? nullptr : L.shapes; w.stash_by_slot = B.joint;
+                        w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = t1 - t0; w.shapes = low_rows > 0 ? nullptr : L.shapes; w.stash_by_slot = B.joint;
                         w.n_tiles = (H + (wide_here ? 2 : 1) * w.mma_n - 1) / ((wide_here ? 2 : 1) * w.mma_n); w.k_iters = 1;
                         w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
                         w.a_row0 = row0; w.m_rows = n_here; w.n_cols = H; w.ldc = H;
