@@ -10,7 +10,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libunity.so")
 SOURCES = ["unity_api.cu", "stream_kernels.cu", "gemm_tcgen05.cu", "batch_kernels.cu",
-           "noalloc_advantage.cu", "token_loss.cu"]
+           "noalloc_advantage.cu", "token_loss.cu",
+           "few_rows_tcgen05.cu"]
 HEADERS = ["internal.h", "ptx.cuh", os.path.join("..", "..", "include", "unity.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math=false"]

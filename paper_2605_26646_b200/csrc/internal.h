@@ -525,12 +525,31 @@ struct StoreArgs {
     RowSpan span;              // (model < 0: up to row_cap rows of each of the K models, whose parts are part_stride apart)
     int K, H;
     long long part_stride;
-    const LossShapes* shapes;  // null: one part
+    const LossShapes* shapes;  // null: parts_n parts
+    int parts_n;
     int low_rows;              // > 0: row r + low_rows belongs to row r (see LossGradArgs)
     long long bound;           // rows of the launch at most
     __nv_bfloat16* dHidden;
 };
 cudaError_t launch_store_parts(const StoreArgs& a, cudaStream_t stream);
+// Backward of at most 128 rows (few_rows_tcgen05.cu): dHidden's parts [parts_n][128][H] and dW (overwritten) in one launch.
+// tmG: G [rows, V] and tmH: hidden [rows, H] in boxes of 64 columns x 128 rows; tmW: W [V, H] in boxes of 64 x 64.
+struct FewRowsArgs {
+    const DevPlan* plan;
+    int model, H, V;
+    int n_col_blocks, parts_n, per_part;    // column blocks of 128 x ranges of per_part vocabulary chunks (few_rows_plan)
+    int low_rows;                           // see LossGradArgs
+    int wide;                               // fp32 dW is 32-byte aligned
+    float* parts;
+    void* dW;
+    int* status;
+    long long wait_budget;
+};
+cudaError_t few_rows_set_attributes();
+void few_rows_plan(int H, int V, int sm_count, long long part_capacity, FewRowsArgs* a);
+// tmO: bf16 dW [V, H] in boxes of 64 columns x 128 rows; null: dW is fp32
+cudaError_t launch_few_rows_bwd(const CUtensorMap& tmG, const CUtensorMap& tmH, const CUtensorMap& tmW, const CUtensorMap* tmO,
+                                const FewRowsArgs& a, cudaStream_t stream);
 // One model's dW [n values] = the parts of its GEMM (+ its old value when add), fp32 or (out16 not null) rounded to bf16 once
 struct SumDwArgs {
     const float* parts;        // [parts][n]

@@ -268,6 +268,17 @@ __device__ __forceinline__ void tma_load_2d_hint_on(void* smem_dst, const void* 
     }
 }
 
+// 2-D tiled store from this CTA's shared memory (one thread; the bytes were written by ordinary stores, each writer having
+// passed fence_proxy_async), as a bulk group of its own; then the waits for that thread's groups: sources read, or complete.
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_2d(const void* tmap, const void* smem_src, int32_t x, int32_t y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(smem_u32(smem_src)), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // Forms selected by the number of CTAs that cooperate on a tile (1, or 2 = a CTA pair).
 template <int CTAS>
 __device__ __forceinline__ void mma_bf16_ss_on(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,

@@ -715,7 +715,7 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
     }
     if (r >= rows) return;
     const int tok = a.slot_tok[slot0 + r];
-    const int splits = a.shapes ? a.shapes->dh[model][rows == a.span.row_cap ? 0 : 1].splits : 1;
+    const int splits = a.shapes ? a.shapes->dh[model][rows == a.span.row_cap ? 0 : 1].splits : a.parts_n;
     if (tok < 0) return;
     float4 v = sum_parts(parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
     if (a.low_rows > 0) {

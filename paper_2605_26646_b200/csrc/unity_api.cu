@@ -2,6 +2,7 @@
 // All arithmetic of the path runs in the kernels of stream_kernels.cu and gemm_tcgen05.cu.
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -706,6 +707,9 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         nl += 1;
         if (B.joint) CUDA_TRY(ctx, convert(lg.span));
     }
+    // At most 128 rows of one model at a time: both products in one sweep over W (not where dW accumulates, nor under the
+    // test hook, which knows the GEMMs only)
+    const bool few_rows = few && want_h && want_w && B.joint && at_once == 1 && !c.accumulate && ctx->test_drop == 0 && !getenv("UT_NOFEW");
     // per model and block of rows: G = dL/dz in bf16, dHidden = G W, dW += G^T hidden
     for (int k = 0; want && k < K; k += at_once) {
         float* dWk = want_w ? (B.dw_scratch ? L.dWc : static_cast<float*>(c.dW[k])) : nullptr;
@@ -768,6 +772,24 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                 CUtensorMap tm_G_k, tm_G_mn;
                 if ((rc = make_tmap(ctx, &tm_G_k, L.G, vc, B.rows, static_cast<uint64_t>(B.cols) * 2, kBoxRows))) return rc;
                 if ((rc = make_tmap(ctx, &tm_G_mn, L.G, vc, B.rows, static_cast<uint64_t>(B.cols) * 2, kTileK))) return rc;
+                if (few_rows) {
+                    FewRowsArgs f;
+                    memset(&f, 0, sizeof(f));
+                    f.plan = L.plan; f.model = k; f.H = H; f.V = V; f.low_rows = low_rows; f.parts = L.parts; f.dW = c.dW[k];
+                    f.wide = reinterpret_cast<uintptr_t>(c.dW[k]) % 32 == 0;
+                    f.status = ctx->d_status; f.wait_budget = ctx->wait_budget;
+                    few_rows_plan(H, V, ctx->sm_count, L.part_stride, &f);
+                    CUtensorMap tm_O;
+                    if (out16 && (rc = make_tmap(ctx, &tm_O, c.dW[k], H, V, static_cast<uint64_t>(H) * 2, kBoxRows))) return rc;
+                    {
+                        ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
+                        CUDA_TRY(ctx, launch_few_rows_bwd(tm_G_k, tm_hp_k, tm_W_mn, out16 ? &tm_O : nullptr, f, st));
+                    }
+                    const StoreArgs sa{L.parts, L.slot_tok, chunk, K, H, 0, nullptr, f.parts_n, low_rows, bound, dH};
+                    CUDA_TRY(ctx, launch_store_parts(sa, st));
+                    nl += 2;
+                    continue;
+                }
                 if (want_h) {
                     GemmArgs h;
                     memset(&h, 0, sizeof(h));
@@ -791,7 +813,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     if (ci + 1 == n_pieces) {
                         RowSpan stored = chunk;
                         if (at_once > 1) stored.model = -1;
-                        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, low_rows,
+                        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, 1, low_rows,
                                            at_once > 1 ? L.max_slots : bound, dH};
                         CUDA_TRY(ctx, launch_store_parts(sa, st));
                         nl += 1;
@@ -921,7 +943,8 @@ int unity_create(unity_ctx** out, int device, void* cuda_stream, void* workspace
     c->ev_pool = new (std::nothrow) std::vector<cudaEvent_t>();
     c->ev_class = new (std::nothrow) std::vector<int>();
     if (cudaMalloc(&c->d_status, 256) != cudaSuccess || cudaMallocHost(&c->h_pinned, 4096) != cudaSuccess ||
-        cudaMemset(c->d_status, 0, 256) != cudaSuccess || gemm_set_attributes() != cudaSuccess) {
+        cudaMemset(c->d_status, 0, 256) != cudaSuccess || gemm_set_attributes() != cudaSuccess ||
+        few_rows_set_attributes() != cudaSuccess) {
         if (c->d_status) cudaFree(c->d_status);
         if (c->h_pinned) cudaFreeHost(c->h_pinned);
         delete c;
