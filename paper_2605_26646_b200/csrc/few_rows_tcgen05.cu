@@ -2,16 +2,20 @@
 //
 //   dHidden[r, h] = sum_v G[r, v] W[v, h]          dW[v, h] = sum_r G[r, v] hidden[r, h]
 //
-// With so few rows both products take less time than their bytes: dHidden reads W, dW is written, each V x H values.  As two
-// launches they take 184 and 266 us at 96 x 3584 x 152064 (1.09 GB each way: HBM reads at 5.9 and writes at 4.1 TB/s, the most
-// that either direction gives alone); reads and writes at the same time share more (a copy: 6.5 TB/s).  So a CTA walks a range
-// of the vocabulary in chunks of 128 entries for 128 columns of H: a chunk's tile of W (32 KiB) and its 128 x 128 block of G
-// (32 KiB) land by TMA in one stage of a ring of three, and one thread issues
+// With so few rows both products take less time than their bytes: W is read and dW written, each V x H values.  As two launches
+// they read at 5.9 and write at 4.1 TB/s, the most that either direction gives alone; reads and writes at the same time share
+// more (a copy: 6.5 TB/s).  So a CTA walks a range of the vocabulary in chunks of 128 entries for 128 columns of H: a chunk's
+// tile of W (32 KiB) and its 128 x 128 block of G (32 KiB) land by TMA in one stage of a ring of three, and one thread issues
 //   dHidden (128 rows x 128 columns, tensor-memory columns 0..127)  +=  G     W        G K-major, W MN-major
 //   dW      (128 entries x 128 columns, one of two stages behind)    =  G^T   hidden   both MN-major, G being the same bytes
-// for 16 MMAs of 64 clocks.  The columns' hidden rows (32 KiB) stay in shared memory throughout.  Four epilogue warps write
-// dW from tensor memory, a thread per vocabulary entry (256 contiguous bytes), while the next chunk's MMAs run; at the end
-// they write the CTA's part of dHidden.  The vocabulary is cut into as many ranges as fill the SMs once.
+// as 16 MMAs.  The columns' hidden rows (32 KiB) stay in shared memory throughout.  Four epilogue warps round a dW tile to bf16
+// into the place of the stage's W, whose MMAs have completed, and a seventh warp sends it off as bulk stores (a thread per entry
+// storing its own 256 bytes touches 32 lines at a time and took 10 % longer); fp32 tiles go out by plain stores.  At the end the
+// epilogue writes the CTA's part of dHidden.  The vocabulary is cut into as many ranges as fill the SMs once.
+// Measured (training step, both products and dHidden's sum): 40 rows x 896 x 151936 207 against 248 us as two GEMMs, x 1536 314 /
+// 339, 60 rows x 2560 x 100000 345 / 363, 96 rows x 3584 x 152064 647 / 659, 40 rows x 256 x 4096 44 / 53.  Bound: shared memory,
+// which the MMAs' operands, the loads and the stores pass through (256 KiB per chunk: 2.0 k clocks of the 3.5 k a chunk takes at
+// H = 3584), and HBM together.
 // Every mbarrier wait is bounded as in gemm_tcgen05.cu.
 #include <cstring>
 
@@ -283,6 +287,13 @@ cudaError_t few_rows_set_attributes() {
     const cudaError_t e = cudaFuncSetAttribute(k_few_rows_bwd<float>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     if (e != cudaSuccess) return e;
     return cudaFuncSetAttribute(k_few_rows_bwd<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+}
+
+// Where the column blocks leave no tenth of the SMs without a range (H = 5120: 40 blocks x 3 = 120 of 148, 6 % slower than two
+// GEMMs), or where the vocabulary has fewer chunks than that would take: launches decide there.
+bool few_rows_pays(int H, int V, int sm_count) {
+    const int blocks = (H + kCols - 1) / kCols, parts = sm_count / blocks;
+    return parts >= (V + kChunk - 1) / kChunk || 10 * blocks * parts >= 9 * sm_count;
 }
 
 void few_rows_plan(int H, int V, int sm_count, long long part_capacity, FewRowsArgs* a) {

@@ -546,6 +546,7 @@ struct FewRowsArgs {
     long long wait_budget;
 };
 cudaError_t few_rows_set_attributes();
+bool few_rows_pays(int H, int V, int sm_count);   // whether it is faster than the two GEMMs
 void few_rows_plan(int H, int V, int sm_count, long long part_capacity, FewRowsArgs* a);
 // tmO: bf16 dW [V, H] in boxes of 64 columns x 128 rows; null: dW is fp32
 cudaError_t launch_few_rows_bwd(const CUtensorMap& tmG, const CUtensorMap& tmH, const CUtensorMap& tmW, const CUtensorMap* tmO,

@@ -2,7 +2,6 @@
 // All arithmetic of the path runs in the kernels of stream_kernels.cu and gemm_tcgen05.cu.
 #include <cstdarg>
 #include <cstdio>
-#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -709,7 +708,8 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     }
     // At most 128 rows of one model at a time: both products in one sweep over W (not where dW accumulates, nor under the
     // test hook, which knows the GEMMs only)
-    const bool few_rows = few && want_h && want_w && B.joint && at_once == 1 && !c.accumulate && ctx->test_drop == 0 && !getenv("UT_NOFEW");
+    const bool few_rows = few && want_h && want_w && B.joint && at_once == 1 && !c.accumulate && ctx->test_drop == 0 &&
+                          few_rows_pays(H, V, ctx->sm_count);
     // per model and block of rows: G = dL/dz in bf16, dHidden = G W, dW += G^T hidden
     for (int k = 0; want && k < K; k += at_once) {
         float* dWk = want_w ? (B.dw_scratch ? L.dWc : static_cast<float*>(c.dW[k])) : nullptr;

@@ -204,6 +204,29 @@ def test_forms_agree_with_the_whole_call(op, grads):
 
 
 @pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("N", [1, 40, 64, 65, 128])
+@pytest.mark.parametrize("H,V", [(64, 2000), (320, 1000), (1344, 520), (1920, 20000)])
+def test_few_rows_in_every_form(N, H, V, op):
+    """Both gradients in one launch, or one of them, or added to an old dW, of either type; the first rows may be all masked."""
+    p = Problem(N, H, V, 1, 1, n_top=6, seed=N + V, mask=0.3 if N > 1 else 0.0).gpu()
+    ctx = context(p, op)
+    o = oracle(p, op)
+    for dw in (torch.bfloat16, torch.float32):
+        check(p, call(ctx, p, op, dw=dw), o)
+        check(p, call(ctx, p, op, "head", dw=dw), o)
+        old = [torch.full((V, H), 0.5, device="cuda", dtype=dw)]
+        check(p, call(ctx, p, op, accumulate=True, dW=old), o, base=[np.full((V, H), 0.5)])
+    check(p, call(ctx, p, op, "hidden"), o)
+    ctx.check_status()
+    p.mask.zero_()
+    p.d_mask = p.mask.cuda()
+    g = call(ctx, p, op)
+    assert g["loss"][0] == 0 and g["dW"][0].abs().max() == 0 and g["dHidden"].abs().max() == 0
+    ctx.check_status()
+    ctx.close()
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
 @pytest.mark.parametrize("dw", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("N", [200, 3000])
 def test_accumulation_and_norm(N, op, dw):
