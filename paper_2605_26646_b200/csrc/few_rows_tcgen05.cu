@@ -289,11 +289,12 @@ cudaError_t few_rows_set_attributes() {
     return cudaFuncSetAttribute(k_few_rows_bwd<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
 }
 
-// Where the column blocks leave no tenth of the SMs without a range (H = 5120: 40 blocks x 3 = 120 of 148, 6 % slower than two
-// GEMMs), or where the vocabulary has fewer chunks than that would take: launches decide there.
+// Where the ranges of all column blocks fill 85 % of the SMs, or the vocabulary has no more chunks than SMs to go round.  120
+// rows against two GEMMs: 4608 columns (97 % of the SMs) x 60000 356 / 385 us, 3328 (88 %) 271 / 287, 4096 (86 %) 326 / 332,
+// 8192 (86 %) x 40000 441 / 459; 40 rows x 5120 (81 %) x 152064 980 / 937.
 bool few_rows_pays(int H, int V, int sm_count) {
     const int blocks = (H + kCols - 1) / kCols, parts = sm_count / blocks;
-    return parts >= (V + kChunk - 1) / kChunk || 10 * blocks * parts >= 9 * sm_count;
+    return parts >= (V + kChunk - 1) / kChunk || 20 * blocks * parts >= 17 * sm_count;
 }
 
 void few_rows_plan(int H, int V, int sm_count, long long part_capacity, FewRowsArgs* a) {
