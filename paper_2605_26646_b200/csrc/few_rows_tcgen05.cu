@@ -33,9 +33,8 @@ constexpr int kRows = 128;
 constexpr int kBox = kRows * 128;                        // 64 bf16 columns x 128 rows
 constexpr int kHiddenBytes = 2 * kBox;
 constexpr int kGBytes = 2 * kBox, kWBytes = 2 * kBox;
-constexpr int kStageBytes = kGBytes + kWBytes;
-constexpr int kStages = 3;
-constexpr int kSmemBytes = 1024 + kHiddenBytes + kStages * kStageBytes + 256;
+constexpr int kGStages = 2, kWStages = 4;
+constexpr int kSmemBytes = 1024 + kHiddenBytes + kGStages * kGBytes + kWStages * kWBytes + 256;
 constexpr int kTmemCols = 512;                           // 128 + 2 x 128, rounded up to a power of two
 
 __device__ __forceinline__ void store_row(float* dst, const uint32_t (&r)[32], bool wide) {
@@ -57,20 +56,24 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
     constexpr bool kStaged = sizeof(T) == 2;     // bf16 dW leaves through shared memory
     extern __shared__ uint8_t smem_raw[];
     uint8_t* hidden = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* stages = hidden + kHiddenBytes;
-    uint64_t* full = reinterpret_cast<uint64_t*>(stages + kStages * kStageBytes);   // [kStages] a stage's bytes have landed
-    uint64_t* empty = full + kStages;            // [kStages] the MMAs that read it have completed
-    uint64_t* acc_full = empty + kStages;        // [2] a dW tile is complete
+    uint8_t* ring_g = hidden + kHiddenBytes;
+    uint8_t* ring_w = ring_g + kGStages * kGBytes;
+    uint64_t* g_full = reinterpret_cast<uint64_t*>(ring_w + kWStages * kWBytes);   // [kGStages] a stage's bytes have landed
+    uint64_t* g_empty = g_full + kGStages;       // [kGStages] the MMAs that read it have completed
+    uint64_t* w_full = g_empty + kGStages;       // [kWStages]
+    uint64_t* w_empty = w_full + kWStages;       // [kWStages] the MMAs that read it have completed; bf16 dW: its tile has left
+    uint64_t* staged = w_empty + kWStages;       // [kWStages] a bf16 dW tile lies where the stage's W was
+    uint64_t* acc_full = staged + kWStages;      // [2] a dW tile is complete
     uint64_t* acc_empty = acc_full + 2;          // [2] ... and drained
-    uint64_t* staged = acc_empty + 2;            // [kStages] a bf16 dW tile lies where the stage's W was
-    uint64_t* hid_full = staged + kStages;
+    uint64_t* hid_full = acc_empty + 2;
     uint64_t* dh_full = hid_full + 1;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(dh_full + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { ptx::mbar_init(&full[s], 1); ptx::mbar_init(&empty[s], 1); ptx::mbar_init(&staged[s], 4); }
+        for (int s = 0; s < kGStages; ++s) { ptx::mbar_init(&g_full[s], 1); ptx::mbar_init(&g_empty[s], 1); }
+        for (int s = 0; s < kWStages; ++s) { ptx::mbar_init(&w_full[s], 1); ptx::mbar_init(&w_empty[s], 1); ptx::mbar_init(&staged[s], 4); }
         for (int b = 0; b < 2; ++b) { ptx::mbar_init(&acc_full[b], 1); ptx::mbar_init(&acc_empty[b], 4); }
         ptx::mbar_init(hid_full, 1);
         ptx::mbar_init(dh_full, 1);
@@ -110,23 +113,28 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
             ptx::mbar_arrive_expect_tx(hid_full, kHiddenBytes);
             for (int j = 0; j < 2; ++j)
                 ptx::tma_load_2d_hint_on<1>(hidden + j * kBox, &tmH, ptx::smem_u32(hid_full), h0 + 64 * j, first, keep);
-            int s = 0;
-            uint32_t phase = 0;
+            int s = 0, t = 0;
+            uint32_t phase = 0, phase_w = 0;
             for (int c = c0; c < c1; ++c) {
-                if (!ptx::mbar_wait(&empty[s], phase ^ 1, a.wait_budget) || *abort_flag) {
+                bool ok = ptx::mbar_wait(&w_empty[t], phase_w ^ 1, a.wait_budget) && !*abort_flag;
+                if (ok) {
+                    const uint32_t bar = ptx::smem_u32(&w_full[t]);
+                    ptx::mbar_arrive_expect_tx(&w_full[t], kWBytes);
+                    for (int k = 0; k < 2; ++k)                      // 64 entries each: a box of 64 columns, then the next
+                        for (int j = 0; j < 2; ++j)
+                            ptx::tma_load_2d_hint_on<1>(ring_w + t * kWBytes + (2 * k + j) * (kBox / 2), &tmW, bar, h0 + 64 * j, c * kChunk + 64 * k, once);
+                    if (++t == kWStages) { t = 0; phase_w ^= 1; }
+                    ok = ptx::mbar_wait(&g_empty[s], phase ^ 1, a.wait_budget) && !*abort_flag;
+                }
+                if (!ok) {
                     *abort_flag = 1;
                     atomicOr(a.status, kStatusTimeout);
                     break;
                 }
-                uint8_t* g = stages + s * kStageBytes;
-                uint8_t* w = g + kGBytes;
-                const uint32_t bar = ptx::smem_u32(&full[s]);
-                ptx::mbar_arrive_expect_tx(&full[s], kStageBytes);
-                for (int j = 0; j < 2; ++j) ptx::tma_load_2d_hint_on<1>(g + j * kBox, &tmG, bar, c * kChunk + 64 * j, first, keep);
-                for (int k = 0; k < 2; ++k)                          // 64 entries each: a box of 64 columns, then the next
-                    for (int j = 0; j < 2; ++j)
-                        ptx::tma_load_2d_hint_on<1>(w + (2 * k + j) * (kBox / 2), &tmW, bar, h0 + 64 * j, c * kChunk + 64 * k, once);
-                if (++s == kStages) { s = 0; phase ^= 1; }
+                const uint32_t bar = ptx::smem_u32(&g_full[s]);
+                ptx::mbar_arrive_expect_tx(&g_full[s], kGBytes);
+                for (int j = 0; j < 2; ++j) ptx::tma_load_2d_hint_on<1>(ring_g + s * kGBytes + j * kBox, &tmG, bar, c * kChunk + 64 * j, first, keep);
+                if (++s == kGStages) { s = 0; phase ^= 1; }
             }
         }
     } else if (warp == 1) {
@@ -137,15 +145,16 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
             // rows that hold tokens, or (low halves) all 128, in steps of 16; the rows behind them are not gradients
             const int k_rows = a.low_rows > 0 ? kRows / 16 : (valid + kTileK - 1) / kTileK * (kTileK / 16);
             bool ok = ptx::mbar_wait(hid_full, 0, a.wait_budget);
-            int s = 0;
-            uint32_t phase = 0;
+            int s = 0, t = 0;
+            uint32_t phase = 0, phase_w = 0;
             for (int c = c0; ok && c < c1; ++c) {
                 const int b = (c - c0) & 1;
                 const uint32_t acc_phase = ((c - c0) >> 1) & 1;
-                ok = ptx::mbar_wait(&acc_empty[b], acc_phase ^ 1, a.wait_budget) && ptx::mbar_wait(&full[s], phase, a.wait_budget) && !*abort_flag;
+                ok = ptx::mbar_wait(&acc_empty[b], acc_phase ^ 1, a.wait_budget) && ptx::mbar_wait(&w_full[t], phase_w, a.wait_budget) &&
+                     ptx::mbar_wait(&g_full[s], phase, a.wait_budget) && !*abort_flag;
                 if (!ok) break;
                 ptx::tc_fence_after();
-                const uint32_t g = ptx::smem_u32(stages + s * kStageBytes), w = g + kGBytes;
+                const uint32_t g = ptx::smem_u32(ring_g + s * kGBytes), w = ptx::smem_u32(ring_w + t * kWBytes);
                 for (int k = 0; k < kChunk / 16; ++k) {              // 16 entries each: inside a swizzle row of G, 16 rows of W
                     const uint64_t da = ptx::smem_desc_k_sw128(g + (k >> 2) * kBox) + 2 * (k & 3);
                     const uint64_t db = ptx::smem_desc_mn_sw128(w + (k >> 2) * kBox, kBox / 2) + 128 * (k & 3);
@@ -153,9 +162,11 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
                 }
                 const uint64_t da = ptx::smem_desc_mn_sw128(g, kBox), db = ptx::smem_desc_mn_sw128(ptx::smem_u32(hidden), kBox);
                 for (int k = 0; k < k_rows; ++k) ptx::mma_bf16_ss(tmem + kCols * (1 + b), da + 128 * k, db + 128 * k, id_dw, k > 0 ? 1u : 0u);
-                if (!kStaged) ptx::tc_commit(&empty[s]);
+                ptx::tc_commit(&g_empty[s]);
+                if (!kStaged) ptx::tc_commit(&w_empty[t]);
                 ptx::tc_commit(&acc_full[b]);
-                if (++s == kStages) { s = 0; phase ^= 1; }
+                if (++s == kGStages) { s = 0; phase ^= 1; }
+                if (++t == kWStages) { t = 0; phase_w ^= 1; }
             }
             if (ok) ptx::tc_commit(dh_full);
             else { *abort_flag = 1; atomicOr(a.status, kStatusTimeout); }
@@ -172,11 +183,11 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
                     break;
                 }
                 for (int j = 0; 64 * j < n_cols; ++j)                // (rows behind the vocabulary are left out by the map)
-                    ptx::tma_store_2d(&tmO, stages + s * kStageBytes + kGBytes + j * kBox, h0 + 64 * j, c * kChunk);
+                    ptx::tma_store_2d(&tmO, ring_w + s * kWBytes + j * kBox, h0 + 64 * j, c * kChunk);
                 ptx::tma_store_commit();
                 ptx::tma_store_wait_read();
-                ptx::mbar_arrive(&empty[s]);
-                if (++s == kStages) { s = 0; phase ^= 1; }
+                ptx::mbar_arrive(&w_empty[s]);
+                if (++s == kWStages) { s = 0; phase ^= 1; }
             }
             ptx::tma_store_wait();
         }
@@ -196,7 +207,7 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
             const uint32_t acc = tmem + lanes + kCols * (1 + b);
             // the stage's MMAs have completed: its W gives way to the dW tile, in the layout of a store's boxes (rows of 128
             // bytes whose 16-byte units are exchanged by row, which also keeps these writes free of bank conflicts)
-            uint8_t* out = stages + s * kStageBytes + kGBytes + at * 128;
+            uint8_t* out = ring_w + s * kWBytes + at * 128;
             ptx::tmem_ld_32x32(acc, r);
             ptx::tmem_ld_wait_for(r);
 #pragma unroll 1
@@ -230,7 +241,7 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
                 if (kStaged) ptx::mbar_arrive(&staged[s]);
                 ptx::mbar_arrive(&acc_empty[b]);
             }
-            if (++s == kStages) s = 0;
+            if (++s == kWStages) s = 0;
         }
         if (ok) ok = ptx::mbar_wait(dh_full, 0, a.wait_budget) && !*abort_flag;
         if (ok) {
