@@ -5,17 +5,19 @@
 // With so few rows both products take less time than their bytes: W is read and dW written, each V x H values.  As two launches
 // they read at 5.9 and write at 4.1 TB/s, the most that either direction gives alone; reads and writes at the same time share
 // more (a copy: 6.5 TB/s).  So a CTA walks a range of the vocabulary in chunks of 128 entries for 128 columns of H: a chunk's
-// tile of W (32 KiB) and its 128 x 128 block of G (32 KiB) land by TMA in one stage of a ring of three, and one thread issues
+// tile of W and its 128 x 128 block of G (32 KiB each) land by TMA, and one thread issues
 //   dHidden (128 rows x 128 columns, tensor-memory columns 0..127)  +=  G     W        G K-major, W MN-major
 //   dW      (128 entries x 128 columns, one of two stages behind)    =  G^T   hidden   both MN-major, G being the same bytes
 // as 16 MMAs.  The columns' hidden rows (32 KiB) stay in shared memory throughout.  Four epilogue warps round a dW tile to bf16
-// into the place of the stage's W, whose MMAs have completed, and a seventh warp sends it off as bulk stores (a thread per entry
-// storing its own 256 bytes touches 32 lines at a time and took 10 % longer); fp32 tiles go out by plain stores.  At the end the
-// epilogue writes the CTA's part of dHidden.  The vocabulary is cut into as many ranges as fill the SMs once.
-// Measured (training step, both products and dHidden's sum): 40 rows x 896 x 151936 207 against 248 us as two GEMMs, x 1536 314 /
-// 339, 60 rows x 2560 x 100000 345 / 363, 96 rows x 3584 x 152064 647 / 659, 40 rows x 256 x 4096 44 / 53.  Bound: shared memory,
-// which the MMAs' operands, the loads and the stores pass through (256 KiB per chunk: 2.0 k clocks of the 3.5 k a chunk takes at
-// H = 3584), and HBM together.
+// into the place of the chunk's W, whose MMAs have completed, and a warp of its own sends it off as bulk stores (a thread per
+// entry storing its own 256 bytes touches 32 lines at a time and took 10 % longer); fp32 tiles go out by plain stores.  W comes
+// from HBM and its place is taken until the tile has left: a ring of four stages and a producer of its own.  G comes from L2 and
+// is done with after the MMAs: two stages.  (Three stages of both: 652 us for the step of 96 rows x 3584 x 152064, now 605.)
+// At the end the epilogue writes the CTA's part of dHidden.  The vocabulary is cut into as many ranges as fill the SMs once.
+// Measured (training step, this kernel against two GEMMs): 40 rows x 896 x 151936 204 / 248 us, x 1536 304 / 339, 60 rows x
+// 2560 x 100000 318 / 363, 96 rows x 3584 x 152064 610 / 659, 40 rows x 256 x 4096 44 / 53; the kernel alone moves W and dW
+// at 5.1 to 5.4 TB/s.  Bound: HBM, beside shared memory, which the MMAs' operands, the loads and the stores pass through
+// (256 KiB and 2.0 k clocks per chunk, of 3.2 k).
 // Every mbarrier wait is bounded as in gemm_tcgen05.cu.
 #include <cstring>
 
@@ -26,7 +28,7 @@ namespace unity {
 
 namespace {
 
-constexpr int kThreads = 224;
+constexpr int kThreads = 256;
 constexpr int kChunk = 128;                              // vocabulary entries per stage
 constexpr int kCols = 128;                               // columns of H per CTA
 constexpr int kRows = 128;
@@ -107,26 +109,36 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
             *reinterpret_cast<uint4*>(dW + static_cast<long long>(v) * a.H + h) = make_uint4(0, 0, 0, 0);
         }
     } else if (warp == 0) {
-        // ------------------------------------------------------------------ TMA producer
+        // ------------------------------------------------------------------ TMA producer of W, as far ahead as its ring allows
         if (lane == 0) {
-            const uint64_t once = ptx::l2_policy(1), keep = ptx::l2_policy(0);
+            const uint64_t once = ptx::l2_policy(1);
+            int s = 0;
+            uint32_t phase = 0;
+            for (int c = c0; c < c1; ++c) {
+                if (!ptx::mbar_wait(&w_empty[s], phase ^ 1, a.wait_budget) || *abort_flag) {
+                    *abort_flag = 1;
+                    atomicOr(a.status, kStatusTimeout);
+                    break;
+                }
+                const uint32_t bar = ptx::smem_u32(&w_full[s]);
+                ptx::mbar_arrive_expect_tx(&w_full[s], kWBytes);
+                for (int k = 0; k < 2; ++k)                          // 64 entries each: a box of 64 columns, then the next
+                    for (int j = 0; j < 2; ++j)
+                        ptx::tma_load_2d_hint_on<1>(ring_w + s * kWBytes + (2 * k + j) * (kBox / 2), &tmW, bar, h0 + 64 * j, c * kChunk + 64 * k, once);
+                if (++s == kWStages) { s = 0; phase ^= 1; }
+            }
+        }
+    } else if (warp == 7) {
+        // ------------------------------------------------------------------ ... of the hidden rows and G
+        if (lane == 0) {
+            const uint64_t keep = ptx::l2_policy(0);
             ptx::mbar_arrive_expect_tx(hid_full, kHiddenBytes);
             for (int j = 0; j < 2; ++j)
                 ptx::tma_load_2d_hint_on<1>(hidden + j * kBox, &tmH, ptx::smem_u32(hid_full), h0 + 64 * j, first, keep);
-            int s = 0, t = 0;
-            uint32_t phase = 0, phase_w = 0;
+            int s = 0;
+            uint32_t phase = 0;
             for (int c = c0; c < c1; ++c) {
-                bool ok = ptx::mbar_wait(&w_empty[t], phase_w ^ 1, a.wait_budget) && !*abort_flag;
-                if (ok) {
-                    const uint32_t bar = ptx::smem_u32(&w_full[t]);
-                    ptx::mbar_arrive_expect_tx(&w_full[t], kWBytes);
-                    for (int k = 0; k < 2; ++k)                      // 64 entries each: a box of 64 columns, then the next
-                        for (int j = 0; j < 2; ++j)
-                            ptx::tma_load_2d_hint_on<1>(ring_w + t * kWBytes + (2 * k + j) * (kBox / 2), &tmW, bar, h0 + 64 * j, c * kChunk + 64 * k, once);
-                    if (++t == kWStages) { t = 0; phase_w ^= 1; }
-                    ok = ptx::mbar_wait(&g_empty[s], phase ^ 1, a.wait_budget) && !*abort_flag;
-                }
-                if (!ok) {
+                if (!ptx::mbar_wait(&g_empty[s], phase ^ 1, a.wait_budget) || *abort_flag) {
                     *abort_flag = 1;
                     atomicOr(a.status, kStatusTimeout);
                     break;
@@ -300,12 +312,12 @@ cudaError_t few_rows_set_attributes() {
     return cudaFuncSetAttribute(k_few_rows_bwd<__nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
 }
 
-// Where the ranges of all column blocks fill 85 % of the SMs, or the vocabulary has no more chunks than SMs to go round.  120
-// rows against two GEMMs: 4608 columns (97 % of the SMs) x 60000 356 / 385 us, 3328 (88 %) 271 / 287, 4096 (86 %) 326 / 332,
-// 8192 (86 %) x 40000 441 / 459; 40 rows x 5120 (81 %) x 152064 980 / 937.
+// Where the ranges of all column blocks fill three quarters of the SMs, or the vocabulary has no more chunks than SMs to go
+// round.  A training step of 120 rows against two GEMMs: 4608 columns (97 % of the SMs) x 60000 330 / 385 us, 4096 (86 %)
+// 308 / 332, 5120 (81 %) x 152064 882 / 941, 7168 (76 %) x 60000 548 / 565; below that (9600: 51 %) the rest idles.
 bool few_rows_pays(int H, int V, int sm_count) {
     const int blocks = (H + kCols - 1) / kCols, parts = sm_count / blocks;
-    return parts >= (V + kChunk - 1) / kChunk || 20 * blocks * parts >= 17 * sm_count;
+    return parts >= (V + kChunk - 1) / kChunk || 4 * blocks * parts >= 3 * sm_count;
 }
 
 void few_rows_plan(int H, int V, int sm_count, long long part_capacity, FewRowsArgs* a) {
