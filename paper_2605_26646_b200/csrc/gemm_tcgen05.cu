@@ -1007,7 +1007,7 @@ k_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensor
 }
 
 // The same for several models side by side, each on its share of the workers: a small problem's launch costs more than its
-// work (333 tokens of two models, 256 x 4096: 11 launches took 89 us, 7 take 57).
+// work (333 tokens of two models, 256 x 4096: 11 launches took 89 us, 7 took 57).
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
 __global__ void __launch_bounds__(kThreads, 1)
 k_gemm_models(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ ModelMaps maps, const GemmArgs g_in) {
@@ -1016,6 +1016,18 @@ k_gemm_models(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ M
                                                                           maps.out[model]});
 }
 
+// dHidden's parts and dW of all models, neither of which waits for the other: the first `h_workers` CTA pairs of each model take
+// dHidden (A: G K-major, B: W), the others dW (A: G MN-major, B: the hidden rows).
+template <int EPI_W, int NB>
+__global__ void __launch_bounds__(kThreads, 1)
+k_gemm_grads(const __grid_constant__ CUtensorMap tmGk, const __grid_constant__ ModelMaps maps_h, const GemmArgs h, int h_workers,
+             const __grid_constant__ CUtensorMap tmGmn, const __grid_constant__ ModelMaps maps_w, const GemmArgs w) {
+    const int n = maps_h.n, worker = blockIdx.x / 2 / n, model = blockIdx.x / 2 % n, workers = gridDim.x / 2 / n;
+    if (worker < h_workers)
+        gemm_body<kEpiAccumF32, false, true, 2, NB>(tmGk, maps_h.b[model], h, Worker{model, worker, h_workers, maps_h.out[model]});
+    else
+        gemm_body<EPI_W, true, true, 2, 1>(tmGmn, maps_w.b[model], w, Worker{model, worker - h_workers, workers - h_workers, maps_w.out[model]});
+}
 
 template <int EPI, bool A_MN, bool B_MN, int CTAS, int NB = 1>
 cudaError_t set_attr() {
@@ -1061,7 +1073,36 @@ cudaError_t launch_models(const CUtensorMap& tmA, const ModelMaps& maps, const G
     return cudaLaunchKernelEx(&c.cfg, k_gemm_models<EPI, A_MN, B_MN, CTAS, NB>, tmA, maps, args);
 }
 
+template <int EPI_W, int NB>
+constexpr int grads_smem() {
+    return Cfg<2, NB, kEpiAccumF32>::kSmemBytes > Cfg<2, 1, EPI_W>::kSmemBytes ? Cfg<2, NB, kEpiAccumF32>::kSmemBytes : Cfg<2, 1, EPI_W>::kSmemBytes;
+}
+template <int EPI_W, int NB>
+cudaError_t set_attr_grads() {
+    return cudaFuncSetAttribute(k_gemm_grads<EPI_W, NB>, cudaFuncAttributeMaxDynamicSharedMemorySize, grads_smem<EPI_W, NB>());
+}
+template <int EPI_W, int NB>
+cudaError_t launch_grads(const CUtensorMap& tmGk, const ModelMaps& maps_h, const GemmArgs& h, int h_workers, const CUtensorMap& tmGmn,
+                         const ModelMaps& maps_w, const GemmArgs& w, int workers, cudaStream_t stream) {
+    LaunchConfig<EPI_W, 2, 1> c(workers * maps_h.n, true, stream);
+    c.cfg.dynamicSmemBytes = grads_smem<EPI_W, NB>();
+    return cudaLaunchKernelEx(&c.cfg, k_gemm_grads<EPI_W, NB>, tmGk, maps_h, h, h_workers, tmGmn, maps_w, w);
+}
+
 }  // namespace
+
+cudaError_t launch_gemm_grads(bool out16, const CUtensorMap& tmGk, const ModelMaps& maps_h, const GemmArgs& h, int h_workers,
+                              const CUtensorMap& tmGmn, const ModelMaps& maps_w, const GemmArgs& w, int sm_count, cudaStream_t stream,
+                              bool wide_h) {
+    const int workers = sm_count / 2 / maps_h.n;
+    if (h_workers < 1 || h_workers >= workers) return cudaErrorInvalidValue;
+    if (h.mma_n < 32 || h.mma_n > kTileN || h.mma_n % 32 != 0 || w.mma_n < 32 || w.mma_n > kTileN || w.mma_n % 32 != 0) return cudaErrorInvalidValue;
+    if (wide_h)
+        return out16 ? launch_grads<kEpiAccumB16, 2>(tmGk, maps_h, h, h_workers, tmGmn, maps_w, w, workers, stream)
+                     : launch_grads<kEpiAccumF32, 2>(tmGk, maps_h, h, h_workers, tmGmn, maps_w, w, workers, stream);
+    return out16 ? launch_grads<kEpiAccumB16, 1>(tmGk, maps_h, h, h_workers, tmGmn, maps_w, w, workers, stream)
+                 : launch_grads<kEpiAccumF32, 1>(tmGk, maps_h, h, h_workers, tmGmn, maps_w, w, workers, stream);
+}
 
 cudaError_t gemm_set_attributes() {
     cudaError_t e;
@@ -1090,6 +1131,10 @@ cudaError_t gemm_set_attributes() {
     if ((e = set_attr_models<kEpiAccumF32, true, true, 2>()) != cudaSuccess) return e;
     if ((e = set_attr_models<kEpiAccumB16, true, true, 1>()) != cudaSuccess) return e;
     if ((e = set_attr_models<kEpiAccumB16, true, true, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_grads<kEpiAccumB16, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr_grads<kEpiAccumB16, 2>()) != cudaSuccess) return e;
+    if ((e = set_attr_grads<kEpiAccumF32, 1>()) != cudaSuccess) return e;
+    if ((e = set_attr_grads<kEpiAccumF32, 2>()) != cudaSuccess) return e;
     return set_attr<kEpiAccumF32, true, true, 2, 2>();
 }
 

@@ -268,6 +268,10 @@ struct ModelMaps {
 };
 cudaError_t launch_gemm_models(GemmEpilogue epi, bool a_mn, int ctas, const CUtensorMap& tmA, const ModelMaps& maps,
                                const GemmArgs& args, int sm_count, cudaStream_t stream, bool wide = false);
+// Both gradient GEMMs of all models in one launch of CTA pairs, `h_workers` pairs per model on dHidden.
+cudaError_t launch_gemm_grads(bool out16, const CUtensorMap& tmGk, const ModelMaps& maps_h, const GemmArgs& h, int h_workers,
+                              const CUtensorMap& tmGmn, const ModelMaps& maps_w, const GemmArgs& w, int sm_count, cudaStream_t stream,
+                              bool wide_h);
 int gemm_tile_rows(int ctas);
 int gemm_mma_n(int n_cols);   // block width for an fp32-accumulate GEMM with n_cols output columns
 cudaError_t gemm_set_attributes();

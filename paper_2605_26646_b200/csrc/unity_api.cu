@@ -481,10 +481,11 @@ long long part_rows(int block_rows, int H, int V) {
 }
 
 // Models that share their launches: few tokens and heads whose work is less than the launches.  Measured at 333 tokens of two
-// models, 256 x 4096 (4 MB of heads): 57 us against 89.
-int models_at_once(long long n_tok, int H, int V, int K) {
-    return K > 1 && K <= kMaxGroup && n_tok <= 1024 && static_cast<long long>(K) * V * H * 2 <= 64ll << 20 ? K : 1;
+// models, 256 x 4096 (4 MB of heads): 57 us against 89, before the gradients shared a launch too.
+bool small_problem(long long n_tok, int H, int V, int K) {
+    return K <= kMaxGroup && n_tok <= 1024 && static_cast<long long>(K) * V * H * 2 <= 64ll << 20;
 }
+int models_at_once(long long n_tok, int H, int V, int K) { return small_problem(n_tok, H, V, K) ? K : 1; }
 
 LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int K, int n_top, const LossBlocks& B, bool* fits) {
     LossLayout L;
@@ -602,6 +603,14 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     const int mma_n = gemm_mma_n(H);
     const bool two_blocks = ctx->wide_acc && H > mma_n, wide_dh = two_blocks && c_dh == 2;
     const int cols_dh = (wide_dh ? 2 : 1) * mma_n;
+    // A small problem's gradients run side by side (dHidden and dW are as many products): half of the workers each, but no more
+    // for dW than it has tiles.  One after the other, each fills the machine for a moment only (1 model of 500 tokens, 256 x 4096:
+    // 52 us against 59, 512 x 30000 105 / 123; 2 models of 1000 in all, 512 x 30000 215 / 219, 1536 x 10000 196 / 201).
+    const int pairs = ctx->sm_count / 2 / at_once;
+    const long long w_tiles = dw_tiles(H, V, false, kTileM);
+    const int h_workers = pairs - static_cast<int>(w_tiles < pairs / 2 ? w_tiles : pairs / 2);
+    const bool both = want_h && want_w && B.joint && c_dh == 2 && c_dw == 2 && pairs >= 2 && ctx->test_drop == 0 &&
+                      small_problem(r->n_tok, H, V, K);
     FwdPlanParams fwd = fwd_params(ctx, V, H);
     fwd.n_pairs = ctx->sm_count / c_fwd / at_once;
     fwd.tile_rows = gemm_tile_rows(c_fwd);
@@ -619,7 +628,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     ra.n_blocks = L.n_blocks; ra.blk_cnt = L.blk_cnt; ra.plan = L.plan; ra.fwd = fwd;
     ra.tok_slot = L.tok_slot; ra.slot_tok = L.slot_tok; ra.tok_model = L.tok_model; ra.status = ctx->d_status;
     lr.split = SplitParams{B.keep && ctx->sm_count <= kMaxSms ? kMaxKSplits : 0, (H + cols_dh - 1) / cols_dh,
-                           (V + kTileK - 1) / kTileK, ctx->sm_count / c_dh / at_once, gemm_tile_rows(c_dh), kSplitWaves};
+                           (V + kTileK - 1) / kTileK, both ? h_workers : ctx->sm_count / c_dh / at_once, gemm_tile_rows(c_dh), kSplitWaves};
     // few rows: a dW tile's epilogue must overlap the next tile's products, which only the narrow form does, and is not cut
     const bool long_k = (rows_bound < B.rows ? rows_bound : B.rows) > kLongRows, wide_dw = two_blocks && c_dw == 2 && long_k;
     const long long tiles_dw = dw_tiles(H, V, wide_dw, gemm_tile_rows(c_dw));
@@ -706,6 +715,13 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
         nl += 1;
         if (B.joint) CUDA_TRY(ctx, convert(lg.span));
     }
+    auto store_dh = [&](const GemmArgs& h, const RowSpan& span, int bound) {
+        RowSpan stored = span;
+        if (at_once > 1) stored.model = -1;
+        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, 1, low_rows, at_once > 1 ? L.max_slots : bound, dH};
+        nl += 1;
+        return launch_store_parts(sa, st);
+    };
     // At most 128 rows of one model at a time: both products in one sweep over W (not where dW accumulates, nor under the
     // test hook, which knows the GEMMs only)
     const bool few_rows = few && want_h && want_w && B.joint && at_once == 1 && !c.accumulate && ctx->test_drop == 0 &&
@@ -790,9 +806,9 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     nl += 2;
                     continue;
                 }
+                GemmArgs h;
+                memset(&h, 0, sizeof(h));
                 if (want_h) {
-                    GemmArgs h;
-                    memset(&h, 0, sizeof(h));
                     h.pdl = 1;
                     h.mma_n = mma_n;
                     h.span = chunk; h.span_mode = kSpanRowsM; h.m_tiles = 1; h.shapes = B.keep ? L.shapes : nullptr; h.stash_by_slot = B.joint;
@@ -800,24 +816,21 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     h.group_m = ctx->chunk_group[1] / c_dh > 0 ? ctx->chunk_group[1] / c_dh : 1;
                     h.b_k0 = v0; h.n_cols = H; h.C = L.parts; h.ldc = H; h.beta = v0 > 0; h.g_wide_store = 1;
                     gemm_common(ctx, h, UNITY_PROF_DH_GEMM, &counters, (ctx->chunk_sync & 2) != 0 && !short_k);
-                    if (at_once > 1) {
+                    if (at_once > 1 || both) {
                         if ((rc = all_maps(kTileK))) return rc;
                         for (int m = 0; m < at_once; ++m) maps.out[m] = L.parts + m * L.part_stride;
+                    }
+                    if (both) {
+                        // below, with dW
+                    } else if (at_once > 1) {
                         ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
                         CUDA_TRY(ctx, launch_gemm_models(kEpiAccumF32, false, c_dh, tm_G_k, maps, h, ctx->sm_count, st, wide_dh));
                     } else {
                         ProfScope ps(ctx, UNITY_PROF_DH_GEMM);
                         CUDA_TRY(ctx, launch_gemm(kEpiAccumF32, false, c_dh, tm_G_k, tm_W_mn, h, ctx->sm_count, st, wide_dh));
                     }
-                    nl += 1;
-                    if (ci + 1 == n_pieces) {
-                        RowSpan stored = chunk;
-                        if (at_once > 1) stored.model = -1;
-                        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, 1, low_rows,
-                                           at_once > 1 ? L.max_slots : bound, dH};
-                        CUDA_TRY(ctx, launch_store_parts(sa, st));
-                        nl += 1;
-                    }
+                    nl += both ? 0 : 1;
+                    if (ci + 1 == n_pieces && !both) CUDA_TRY(ctx, store_dh(h, chunk, bound));
                 }
                 if (want_w) {
                     const bool wide = wide_dw;
@@ -826,7 +839,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     // the policy update: V = 151936 is eight waves of 74 tiles and two more) and that wave is longer than a launch
                     const int workers = ctx->sm_count / c_dw, nt = (H + cols - 1) / cols, rem = vt % workers;
                     int narrow_n = 0;
-                    if (ctx->dw_tail && c_dw == 2 && !short_k && vt > workers && rem > 0 && 2 * rem * nt < workers)
+                    if (ctx->dw_tail && c_dw == 2 && !short_k && !both && vt > workers && rem > 0 && 2 * rem * nt < workers)
                         for (int cand = 64; cand <= kTileN && narrow_n == 0; cand += 32)
                             if (static_cast<long long>(rem) * ((H + cand - 1) / cand) <= workers) narrow_n = cand;
                     for (int part = 0; part < (narrow_n > 0 ? 2 : 1); ++part) {
@@ -849,6 +862,18 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         w.beta = add && !split_dw ? 1 : 0;
                         w.zero_if_empty = !add && !split_dw;     // a model without rows: its dW reads zero
                         gemm_common(ctx, w, UNITY_PROF_DW_GEMM, &counters, (ctx->chunk_sync & 4) != 0 && !short_k);
+                        if (both) {
+                            ModelMaps maps_w;
+                            maps_w.n = at_once;
+                            for (int m = 0; m < at_once; ++m) { maps_w.b[m] = tm_hp_mn; maps_w.out[m] = c.dW[m]; }
+                            {
+                                ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
+                                CUDA_TRY(ctx, launch_gemm_grads(out16, tm_G_k, maps, h, h_workers, tm_G_mn, maps_w, w, ctx->sm_count, st, wide_dh));
+                            }
+                            nl += 1;
+                            CUDA_TRY(ctx, store_dh(h, chunk, bound));
+                            continue;
+                        }
                         ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
                         if (at_once > 1) {                       // (not split: at most 1024 rows; B is the hidden rows of all models)
                             for (int m = 0; m < at_once; ++m) { maps.b[m] = tm_hp_mn; maps.out[m] = c.dW[m]; }

@@ -227,6 +227,24 @@ def test_few_rows_in_every_form(N, H, V, op):
 
 
 @pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("N,H,V,K", [(129, 64, 264, 1), (300, 576, 3000, 1), (1024, 256, 1000, 4), (700, 1088, 2504, 3), (1024, 128, 60000, 1)])
+def test_small_problems_gradients_side_by_side(N, H, V, K, op):
+    """Both gradients of all models share a launch: each type of dW, added to or not, a model without rows among them."""
+    p = Problem(N, H, V, K, K, n_top=6, seed=N + V, mask=0.2).gpu()
+    ctx = context(p, op)
+    o = oracle(p, op)
+    for dw in (torch.bfloat16, torch.float32):
+        g = call(ctx, p, op, dw=dw)
+        check(p, g, o)
+        again = call(ctx, p, op, dw=dw)
+        assert torch.equal(g["dHidden"], again["dHidden"]) and all(torch.equal(a, b) for a, b in zip(g["dW"], again["dW"]))
+        old = [torch.full((V, H), 0.5, device="cuda", dtype=dw) for _ in range(K)]
+        check(p, call(ctx, p, op, accumulate=True, dW=old), o, base=[np.full((V, H), 0.5)] * K)
+    ctx.check_status()
+    ctx.close()
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
 @pytest.mark.parametrize("dw", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("N", [200, 3000])
 def test_accumulation_and_norm(N, op, dw):
