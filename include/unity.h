@@ -417,7 +417,7 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
  *   tok_weight : f32 [n_tok] or NULL (= all 1), any sign; not read where tok_mask is 0
  *   loss       : out f32 [K];  tok_loss (l_i, without its weight), lse : out f32 [n_tok] or NULL, 0 on masked rows
  *   dHidden    : out bf16 [n_tok, H] or NULL (zeros on masked rows)
- *   dW         : (host) K device pointers or NULL, each f32 or bf16 [V, H] (dW_type).  bf16 is rounded once, from the fp32
+ *   dW         : (host) K different device pointers or NULL, each f32 or bf16 [V, H] (dW_type).  bf16 is rounded once, from the fp32
  *                sum over all rows (plus the old value with accumulate_dW)
  * dL/dz is held in bf16 between the products, as in stage 3: a gradient entry is off by up to 2^-8 of the terms it sums (and
  * a kept logit by up to 2^-10 octaves).

@@ -553,6 +553,8 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     for (int k = 0; k < K; ++k) {
         if (want_w && !c.dW[k]) return fail(ctx, UNITY_ERR_INVALID_ARG, "dW[%d] is NULL", k);
         if (want_w && (reinterpret_cast<uintptr_t>(c.dW[k]) & 15)) return fail(ctx, UNITY_ERR_ALIGNMENT, "dW[%d] not 16-byte aligned", k);
+        for (int j = 0; want_w && j < k; ++j)        // (models of a small problem write theirs at the same time)
+            if (c.dW[j] == c.dW[k]) return fail(ctx, UNITY_ERR_INVALID_ARG, "dW[%d] and dW[%d] are the same", j, k);
         if (c.norm && !(c.norm[k] > 0.f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "norm[%d] must be > 0", k);
     }
     if (reinterpret_cast<uintptr_t>(c.dHidden) & 15) return fail(ctx, UNITY_ERR_ALIGNMENT, "dHidden not 16-byte aligned");

@@ -285,6 +285,28 @@ def test_every_workspace_down_to_the_least_gives_the_same_answer(op):
 
 
 @pytest.mark.parametrize("op", ["ce", "kd"])
+def test_few_rows_of_many_models_in_smaller_workspaces(op):
+    """Sixteen models' rows in one block, then a block of each in turn, then pieces of the vocabulary."""
+    p = Problem(100, 64, 4104, 16, 16, n_inv=40, n_top=6, seed=19).gpu()
+    o = oracle(p, op)
+    now, ways = ub.unity_token_loss_workspace_bytes(p.N, p.H, p.V, p.K, p.n_top if op == "kd" else 0), set()
+    while True:
+        ctx = ub.Context(0, now)
+        try:
+            g = call(ctx, p, op)
+        except ub.UnityError as e:
+            assert e.code == -4
+            ctx.close()
+            break
+        ctx.check_status()
+        ways.add(ctx.launch_count)
+        check(p, g, o)
+        ctx.close()
+        now = now * 3 // 4 // 256 * 256
+    assert len(ways) >= 3, ways
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
 @pytest.mark.parametrize("N,H,V,K,n_inv", [
     (64, 192, 2000, 3, 9), (63, 64, 264, 1, 2), (127, 320, 248, 3, 5), (128, 64, 256, 2, 5), (129, 64, 512, 2, 5),        # one row tile of one CTA, and just more
     (1024, 64, 136, 2, 3000), (1025, 64, 136, 3, 900),                        # routed with the packing or by a block of its own,
@@ -426,6 +448,12 @@ def test_refusals():
     with pytest.raises(ub.UnityError) as e:
         call(ctx, p, "ce", dW=[off])
     assert e.value.code == -3
+    two = Problem(40, 64, 104, 2, 2, n_top=3, seed=4).gpu()
+    same = torch.zeros(two.V, two.H, device="cuda")
+    for op in ("ce", "kd"):
+        with pytest.raises(ub.UnityError) as e:
+            call(ctx, two, op, accumulate=True, dW=[same, same])
+        assert e.value.code == -1 and "same" in str(e.value)
     small = ub.Context(0, 1 << 16)
     with pytest.raises(ub.UnityError) as e:
         call(small, p, "ce")
