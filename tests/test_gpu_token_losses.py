@@ -302,7 +302,7 @@ def test_few_rows_of_many_models_in_smaller_workspaces(op):
         ways.add(ctx.launch_count)
         check(p, g, o)
         ctx.close()
-        now = now * 3 // 4 // 256 * 256
+        now = now * 31 // 32 // 256 * 256      # (most of it is a buffer that all ways need)
     assert len(ways) >= 3, ways
 
 
