@@ -625,3 +625,55 @@ def test_current_device_and_default_arguments_stay():
     g["weight"] = False
     check(p, g, oracle(p, "ce", mask=False, weight=False))
     ctx.close()
+
+
+def test_offsets_beyond_32_bits():
+    """16500 rows of 152064 kept logits: more than 2^31 of them.  Reference: the formulas in 64 bits on the device, 500 rows at a
+    time; tolerances as in oracle(), with a bound of |h| |W| that holds for every entry."""
+    N, H, V = 16500, 64, 152064
+    g = torch.Generator(device="cuda").manual_seed(5)
+    W = (torch.randn(V, H, generator=g, device="cuda") / 8).to(torch.bfloat16)
+    h = torch.randn(N, H, generator=g, device="cuda").to(torch.bfloat16)
+    target = torch.randint(0, V, (N,), generator=g, device="cuda", dtype=torch.int32)
+    target[-1], target[-2] = V - 1, 0
+    mask = (torch.rand(N, generator=g, device="cuda") < 0.99).to(torch.uint8)
+    mask[-3:] = 1
+    cu = torch.tensor([0, N], device="cuda")
+    role = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ctx = ub.Context(0, ub.unity_token_loss_workspace_bytes(N, H, V, 1, 0))
+    loss, tl, lse = torch.empty(1, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, device="cuda")
+    dH = torch.empty_like(h)
+    dW = torch.empty(V, H, device="cuda")
+    ctx.cross_entropy_fwd_bwd(h, [W], cu, role, [0], target, mask, 1.0, 0.0, 0.0, None, False, None, loss, tl, lse, dH, [dW])
+    ctx.check_status()
+    on = mask.bool()
+    M, Wd = int(on.sum()), W.double()
+    want_W, tol_W = torch.zeros(V, H, device="cuda", dtype=torch.float64), torch.zeros(V, H, device="cuda", dtype=torch.float64)
+    total = 0.0
+    for i in range(0, N, 500):
+        rows, y = h[i:i + 500].double(), target[i:i + 500].long()
+        c = on[i:i + 500].double()[:, None] / M
+        z = rows @ Wd.T
+        want_lse = torch.logsumexp(z, 1)
+        at = torch.arange(rows.shape[0], device="cuda")
+        want_l = want_lse - z[at, y]
+        keep = on[i:i + 500]
+        ez = (H / 16 + 2) * 2 * U * rows.abs().sum(1) * Wd.abs().max()
+        assert torch.all(((lse[i:i + 500] - want_lse).abs() <= ez + 2.0 ** -17 + 2 * U * want_lse.abs())[keep])
+        assert torch.all(((tl[i:i + 500] - want_l).abs() <= 2 * ez + 2.0 ** -16 + 8 * U * (1 + 2 * (want_lse.abs() + want_l.abs())))[keep])
+        assert torch.all(tl[i:i + 500][~keep] == 0) and torch.all(dH[i:i + 500][~keep] == 0)
+        total += float((want_l * keep).sum())
+        P = torch.exp(z - want_lse[:, None])
+        terms = P.clone()
+        terms[at, y] += 1
+        P[at, y] -= 1
+        G = P * c
+        dG = B * (1 + B) * G.abs() + (2.0 ** -10 + 2 * ez[:, None] + 2.0 ** -16) * terms * c + c * 2.0 ** -64
+        dG += 2.0 ** -12 * G.abs()
+        want = G @ Wd
+        assert torch.all((dH[i:i + 500].double() - want).abs() <= dG @ Wd.abs() + B * (1 + B) * want.abs() + 1e-38), i
+        want_W += G.T @ rows
+        tol_W += dG.T @ rows.abs()
+    assert abs(float(loss) - total / M) <= 1e-5 * abs(total / M)
+    assert torch.all((dW.double() - want_W).abs() <= tol_W + 4 * U * want_W.abs() + 1e-38)
+    ctx.close()
