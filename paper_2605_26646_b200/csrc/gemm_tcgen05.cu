@@ -191,6 +191,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in, int k) {
             const int full = min(g.m_tiles, fs.gm) * fs.splits, last = (g.m_tiles - fs.last_m0) * fs.last_splits;
             g.n_active = max(full, last);
         }
+        if (in.shapes != nullptr) g.valid_rows = min(max(in.span.plan->counts[k] - in.span.row_begin, 0), n_rows);
         if (in.stash_by_slot) {
             g.stash = in.stash + static_cast<long long>(slot0) * in.ldz;
             g.tile_max = in.tile_max + static_cast<long long>(slot0) * in.n_tiles;
@@ -690,7 +691,7 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
             if (!next_unit<EPI>(g, it, pair, n_pairs, gm, t, valid)) break;
             if (!valid) continue;
             const int row = t.m_tile * C::kTileRows + row_in_tile;        // relative to a_row0
-            const bool row_ok = row < g.m_rows;
+            const bool row_ok = row < (EPI == kEpiLossStats ? g.valid_rows : g.m_rows);
 
             // per-row state
             float run_m = kNegBig, z_tgt = kNegBig;
@@ -761,7 +762,7 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
                         store_b16_block(g.C16, g.ldc, g.beta, out, taddr + nb * kTileN, row0, g.m_rows, col0 + nb * mma_n,
                                         min(mma_n, g.n_cols - col0 - nb * mma_n));
                 }
-                if (EPI == kEpiLossStats) {
+                if (EPI == kEpiLossStats && __any_sync(0xffffffffu, row_ok)) {
                     if (lk.stash != nullptr) loss_stats_tile<true>(lk, lr, taddr, col0, nt, row, row_ok);
                     else loss_stats_tile<false>(lk, lr, taddr, col0, nt, row, row_ok);
                 }

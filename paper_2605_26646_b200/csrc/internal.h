@@ -212,6 +212,7 @@ struct GemmArgs {
     uint16_t* stash;          // optional, a block of rows: kRefRoom octaves above the reference, minus the logit, in steps of
                               // 1 / kStashSteps octaves, row pitch ldz ...
     float* tile_max;          // ... and the reference of each column tile [rows, n_tiles], accumulator units;
+    int valid_rows;           // kEpiLossStats: rows that hold tokens; nothing is worked out or written for those behind them
     int stash_by_slot;        // both (and G of a GEMM that reads it) hold every packed row, not the span's alone
     // kEpiLossGrad: G = coef_p * p - coef_g * uniform, and target_g at the target (row_lse as above)
     const float* coef_p;      // [rows] dL/dz_v per unit of p_v, times scale
@@ -500,7 +501,7 @@ struct TeacherScatterArgs {
 };
 cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream);
 // In place, the kept logits of a block of rows (GemmArgs::stash) become dL/dz in bf16: coef_p * p - coef_g * uniform, and
-// target_g at the target, with p = 2^(tile_max * c2 + kRefRoom - lse log2(e) - u / kStashSteps).
+// target_g at the target (0 in rows without a token, whose logits nobody kept), with p = 2^(tile_max * c2 + kRefRoom - lse log2(e) - u / kStashSteps).
 struct LossGradArgs {
     uint16_t* Z;
     long long ld;

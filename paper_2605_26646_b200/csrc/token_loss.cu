@@ -584,20 +584,22 @@ template <bool LOW>
 __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGradArgs a) {
     begin();
     // the rows that the contractions read: of a block, or of every model (their slabs end with the last token)
-    __shared__ int sh_off[UNITY_MAX_MODELS], sh_rows[UNITY_MAX_MODELS];
+    __shared__ int sh_off[UNITY_MAX_MODELS], sh_rows[UNITY_MAX_MODELS], sh_valid[UNITY_MAX_MODELS];
     const bool joint = a.span.model < 0;
-    int row0 = 0, rows = 0;
+    int row0 = 0, rows = 0, valid = 0;
     if (joint) {
         if (threadIdx.x < a.K) {
             const int k = threadIdx.x;
             sh_off[k] = a.span.plan->off[k];
-            sh_rows[k] = (a.span.plan->counts[k] + kTileK - 1) / kTileK * kTileK;
+            sh_valid[k] = a.span.plan->counts[k];
+            sh_rows[k] = (sh_valid[k] + kTileK - 1) / kTileK * kTileK;
         }
         __syncthreads();
         for (int k = 0; k < a.K; ++k) rows += sh_rows[k];
     } else {
         span_resolve(a.span, row0, rows);
         rows = span_slab_rows(a.span, rows);
+        valid = a.span.plan->counts[a.span.model] - a.span.row_begin;
     }
     const int per_row = (a.cols + kGradCols - 1) / kGradCols;
     for (int item = blockIdx.x; item < rows * per_row; item += gridDim.x) {      // at most 18432 rows of 2^18 columns
@@ -606,11 +608,22 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
         if (joint) {
             int k = 0;
             while (r >= sh_rows[k]) r -= sh_rows[k++];
+            valid = sh_valid[k] + sh_off[k];
             r += sh_off[k];
         }
         const int slot = row0 + r;
         uint4* row = reinterpret_cast<uint4*>(a.Z + static_cast<long long>(r) * a.ld);
         uint4* low_row = LOW ? row + a.low_rows * (a.ld >> 3) : nullptr;
+        if (r >= valid) {                                      // no token: zeros, whatever lies there
+#pragma unroll
+            for (int u = 0; u < kGradVecs; ++u) {
+                const int c0 = c_first + u * 2048;
+                if (c0 >= a.cols) continue;
+                row[c0 >> 3] = make_uint4(0, 0, 0, 0);
+                if (LOW) low_row[c0 >> 3] = make_uint4(0, 0, 0, 0);
+            }
+            continue;
+        }
         const float* tm = a.tile_max + static_cast<long long>(r) * a.n_tiles;
         uint4 raw[kGradVecs];
         float shift[kGradVecs];
