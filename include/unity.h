@@ -419,8 +419,8 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
  *   dHidden    : out bf16 [n_tok, H] or NULL (zeros on masked rows)
  *   dW         : (host) K different device pointers or NULL, each f32 or bf16 [V, H] (dW_type).  bf16 is rounded once, from the fp32
  *                sum over all rows (plus the old value with accumulate_dW)
- * dL/dz is held in bf16 between the products, as in stage 3: a gradient entry is off by up to 2^-8 of the terms it sums (and
- * a kept logit by up to 2^-10 octaves).
+ * dL/dz is held in bf16 between the products, as in stage 3, but without its common factor inv_temperature / M_k: a gradient
+ * entry is off by up to 2^-8 of the terms it sums (and a kept logit by up to 2^-10 octaves).
  * Deterministic: no floating-point atomics anywhere. */
 #define UNITY_F32 0
 #define UNITY_BF16 1

@@ -207,6 +207,7 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
         // ------------------------------------------------------------------ epilogue: thread = one vocabulary entry, then one row
         const int quarter = warp & 3, at = quarter * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+        const float alpha = a.alpha[a.model];
         bool ok = true;
         uint32_t r[32], next[32];
         int s = 0;
@@ -226,6 +227,8 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
             for (int q = 0; q * 32 < n_cols; ++q) {
                 const bool more = (q + 1) * 32 < n_cols;
                 if (more) ptx::tmem_ld_32x32(acc + 32 * (q + 1), next);
+#pragma unroll
+                for (int j = 0; j < 32; ++j) r[j] = __float_as_uint(alpha * __uint_as_float(r[j]));
                 if (kStaged) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {

@@ -235,6 +235,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in, int k) {
             g.c_split = static_cast<long long>(n_rows) * in.ldc;
         }
     } else if (in.span_mode == kSpanRowsK) {
+        if (in.alpha != nullptr) g.alpha = in.alpha + k;
         g.k_iters = (in.shapes ? span_slab_rows(span, n_rows) : n_rows) / kTileK;
         g.b_k0 = in.b_k0 + slot0;
         if (in.stash_by_slot) g.a_k0 = slot0;
@@ -252,8 +253,8 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in, int k) {
 // GEMM of few rows (96 x 3584 x 152064: 277 us so): 64 columns go through shared memory (16-byte units exchanged by row, no
 // bank conflicts) and leave as four whole lines per instruction.  The next 32 columns' loads from tensor memory are under way
 // meanwhile.  With `add` the old values are added before the rounding, row by row.
-__device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ldc, int add, uint8_t* out, uint32_t taddr, int row0,
-                                                int m_rows, int col0, int cols) {
+__device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ldc, int add, float alpha, uint8_t* out, uint32_t taddr,
+                                                int row0, int m_rows, int col0, int cols) {
     const int lane = threadIdx.x & 31;
     if (cols <= 0) return;
     uint32_t ra[32], rb[32];
@@ -270,14 +271,14 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
                 const unsigned ow[4] = {old.x, old.y, old.z, old.w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    o[4 * q + j] = pack_bf16(__uint_as_float(rr[8 * q + 2 * j]) + __uint_as_float(ow[j] << 16),
-                                             __uint_as_float(rr[8 * q + 2 * j + 1]) + __uint_as_float(ow[j] & 0xffff0000u));
+                    o[4 * q + j] = pack_bf16(fmaf(alpha, __uint_as_float(rr[8 * q + 2 * j]), __uint_as_float(ow[j] << 16)),
+                                             fmaf(alpha, __uint_as_float(rr[8 * q + 2 * j + 1]), __uint_as_float(ow[j] & 0xffff0000u)));
                 *reinterpret_cast<uint4*>(d + q * 8) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
             }
             return;
         }
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[j] = pack_bf16(__uint_as_float(rr[2 * j]), __uint_as_float(rr[2 * j + 1]));
+        for (int j = 0; j < 16; ++j) o[j] = pack_bf16(alpha * __uint_as_float(rr[2 * j]), alpha * __uint_as_float(rr[2 * j + 1]));
 #pragma unroll
         for (int q = 0; q < 4; ++q)
             *reinterpret_cast<uint4*>(out + lane * 128 + (((half * 4 + q) ^ (lane & 7)) << 4)) =
@@ -708,6 +709,7 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
                 ent = g.row_ent[g.a_row0 + row];
             }
             const float c2 = g.scale * kLog2e;
+            const float alpha = is_accum(EPI) && A_MN && g.alpha != nullptr ? *g.alpha : 1.f;
             // per-row constants of the logit-gradient epilogue (see there)
             float gshift = 0.f, gA = 0.f, gB = 0.f;
             unsigned gsign = 0u;
@@ -759,7 +761,7 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
                     const int row0 = t.m_tile * C::kTileRows + static_cast<int>(cta_rank) * kCtaM + quarter * 32;
 #pragma unroll 1
                     for (int nb = 0; nb < NB; ++nb)
-                        store_b16_block(g.C16, g.ldc, g.beta, out, taddr + nb * kTileN, row0, g.m_rows, col0 + nb * mma_n,
+                        store_b16_block(g.C16, g.ldc, g.beta, alpha, out, taddr + nb * kTileN, row0, g.m_rows, col0 + nb * mma_n,
                                         min(mma_n, g.n_cols - col0 - nb * mma_n));
                 }
                 if (EPI == kEpiLossStats && __any_sync(0xffffffffu, row_ok)) {
@@ -774,6 +776,10 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
                     // ... and sits at tensor-memory column nb * 256 whatever mma_n is
                     ptx::tmem_ld_32x32(taddr + (NB == 1 ? c * 32 : (c / per_block) * kTileN + (c % per_block) * 32), rr);
                     ptx::tmem_ld_wait();
+                    if (EPI == kEpiAccumF32 && A_MN && g.alpha != nullptr) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) rr[j] = __float_as_uint(alpha * __uint_as_float(rr[j]));
+                    }
                     float v[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(rr[j]);

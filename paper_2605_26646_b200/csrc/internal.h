@@ -215,8 +215,8 @@ struct GemmArgs {
     int valid_rows;           // kEpiLossStats: rows that hold tokens; nothing is worked out or written for those behind them
     int stash_by_slot;        // both (and G of a GEMM that reads it) hold every packed row, not the span's alone
     // kEpiLossGrad: G = coef_p * p - coef_g * uniform, and target_g at the target (row_lse as above)
-    const float* coef_p;      // [rows] dL/dz_v per unit of p_v, times scale
-    const float* coef_g;      // [rows] scale * weight / M
+    const float* coef_p;      // [rows] dL/dz_v per unit of p_v (times weight, as everything here; without alpha)
+    const float* coef_g;      // [rows] weight
     const float* target_g;    // [rows] the whole gradient at the target
     float uniform;            // label smoothing's share of every entry: eps / V
     // kEpiAccumF32
@@ -226,6 +226,7 @@ struct GemmArgs {
     int k_splits, k_per_split;   // the contraction is cut into k_splits parts of k_per_split slabs, each with an output of
     long long c_split;           // its own, c_split values apart (0 or 1: not cut)
     int split_rows;              // kSpanRowsK: the contraction over rows is cut as LossShapes::dw says
+    const float* alpha;          // token losses' dW: each model's factor of its outputs (LossRowArgs::alpha); null: 1
     int zero_if_empty;           // a launch whose contraction has no rows writes zeros to its m_rows x ldc outputs
     int beta;                 // 0: overwrite, 1: add to C
     int mma_n;                // columns per MMA block, a multiple of 32 up to 256 (a tile is 1 or 2 blocks wide); 256
@@ -485,6 +486,10 @@ struct LossRowArgs {
     float* top_z;              // packed [slots, n_top]: logits in, gradients out (with_grad)
     int with_grad;
     float *row_lse, *coef_p, *coef_g, *target_g;   // packed [slots]
+    // inv_temperature / M of each model [K].  dL/dz is kept without this factor and dHidden and dW get it in fp32: without
+    // weights an unsure row's target entry is then near -1, which bf16 holds exactly, where -1/M would be off by the same share
+    // in every row (150 tokens, 256 x 4096: fp32 dW off by 2.6e-4 in norm, 1.8e-3 with the factor inside; 1536 x 20000 6e-5, 2.0e-3).
+    float* alpha;
     float *tok_loss, *lse;     // caller order, nullable
     float* partial;            // [slots / 8]
     float* loss;               // [K]
@@ -533,6 +538,7 @@ struct StoreArgs {
     const LossShapes* shapes;  // null: parts_n parts
     int parts_n;
     int low_rows;              // > 0: row r + low_rows belongs to row r (see LossGradArgs)
+    const float* alpha;        // [K]
     long long bound;           // rows of the launch at most
     __nv_bfloat16* dHidden;
 };
@@ -545,6 +551,7 @@ struct FewRowsArgs {
     int n_col_blocks, parts_n, per_part;    // column blocks of 128 x ranges of per_part vocabulary chunks (few_rows_plan)
     int low_rows;                           // see LossGradArgs
     int wide;                               // fp32 dW is 32-byte aligned
+    const float* alpha;                     // [K], of dW (the parts go without)
     float* parts;
     void* dW;
     int* status;
@@ -562,13 +569,14 @@ struct SumDwArgs {
     RowSpan span;
     const LossShapes* shapes;
     long long n;               // a multiple of 4
+    const float* alpha;        // [K]; null: 1 (a sum that is not the last)
     int add;
     float* out;
     __nv_bfloat16* out16;
 };
 cudaError_t launch_sum_dw(const SumDwArgs& a, cudaStream_t stream);
-// dst[0, n) = bf16(src) (+ dst when add); n a multiple of 8
-cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream);
+// dst[0, n) = bf16(*alpha * src (+ dst when add)); n a multiple of 8
+cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, const float* alpha, bool add, cudaStream_t stream);
 
 // ----------------------------------------------------------------------------------------------
 // ready-batch construction (batch_kernels.cu)

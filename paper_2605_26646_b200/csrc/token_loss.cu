@@ -445,6 +445,7 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
     if (blockIdx.x == 0 && threadIdx.x < a.K) {               // models without a row (of a block: without a first one)
         const int k = threadIdx.x;
         if (a.plan->counts[k] == 0 && (whole || k == a.block.model)) a.loss[k] = 0.f;
+        if (a.with_grad) a.alpha[k] = a.scale / (a.has_norm ? a.norm[k] : fmaxf(static_cast<float>(a.plan->counts[k]), 1.f));
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long long idx = static_cast<long long>(blockIdx.x) * 8 + warp;
@@ -489,8 +490,6 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
         const float lse = a.scale * m + log_s;
         const float dy = a.scale * (m - zy) + log_s;          // lse - z_y (unused without a target)
         const float w = a.tok_weight ? a.tok_weight[tok] : 1.f;
-        const float M = a.has_norm ? a.norm[k] : fmaxf(static_cast<float>(a.plan->counts[k]), 1.f);
-        const float cg = a.scale * (w / M);
         float l, cp, gt;
         if (a.n_top == 0) {
             l = dy + a.z_loss * lse * lse;
@@ -516,7 +515,7 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
                 for (int j = lane; j < cnt; j += 32) {         // the logits give way to the entries' gradients
                     const float d = a.scale * (m - a.top_z[base + j]) + log_s;
                     const float p = expf(-d), hard = a.ids_p[base + j] == tgt ? expm1f(-d) : p;
-                    a.top_z[base + j] = cg * (a.kd * (Q * p - a.q_p[base + j]) + a.hard * hard);
+                    a.top_z[base + j] = w * (a.kd * (Q * p - a.q_p[base + j]) + a.hard * hard);
                 }
             }
         }
@@ -524,7 +523,7 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
         if (lane == 0) {
             if (a.tok_loss) a.tok_loss[tok] = l;
             if (a.lse) a.lse[tok] = lse;
-            if (a.with_grad) { a.row_lse[slot] = lse; a.coef_p[slot] = cg * cp; a.coef_g[slot] = cg; a.target_g[slot] = cg * gt; }
+            if (a.with_grad) { a.row_lse[slot] = lse; a.coef_p[slot] = w * cp; a.coef_g[slot] = w; a.target_g[slot] = w * gt; }
         }
     }
     if (lane == 0) sh_wl[warp] = wl;
@@ -735,6 +734,8 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
         const float4 l = sum_parts(parts + static_cast<long long>(r + a.low_rows) * a.H + c, splits, static_cast<long long>(rows) * a.H);
         v.x += l.x; v.y += l.y; v.z += l.z; v.w += l.w;
     }
+    const float f = a.alpha[model];
+    v.x *= f; v.y *= f; v.z *= f; v.w *= f;
     *reinterpret_cast<uint2*>(a.dHidden + static_cast<long long>(tok) * a.H + c) = pack4(v);
 }
 
@@ -748,6 +749,8 @@ __global__ void __launch_bounds__(256) k_sum_dw(SumDwArgs a) {
     if (rows <= 0 && a.add) return;
     const int splits = a.shapes->dw[a.span.model][rows == a.span.row_cap ? 0 : 1].splits;
     float4 v = rows > 0 ? sum_parts(a.parts + i, splits, a.n) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float f = a.alpha ? a.alpha[a.span.model] : 1.f;
+    v.x *= f; v.y *= f; v.z *= f; v.w *= f;
     if (a.out16 != nullptr) {
         uint2* out = reinterpret_cast<uint2*>(a.out16 + i);
         if (a.add) {
@@ -763,13 +766,14 @@ __global__ void __launch_bounds__(256) k_sum_dw(SumDwArgs a) {
     }
 }
 
-// dst = bf16(src) (+ dst): one rounding of the fp32 sum over all row blocks.  Eight values per thread and step.
-__global__ void __launch_bounds__(256) k_cast_dw(const float4* __restrict__ src, uint4* __restrict__ dst, long long n8, int add) {
+// dst = bf16(*alpha * src (+ dst)): one rounding of the fp32 sum over all row blocks.  Eight values per thread and step.
+__global__ void __launch_bounds__(256) k_cast_dw(const float4* __restrict__ src, uint4* __restrict__ dst, long long n8, const float* alpha, int add) {
     begin();
+    const float f = *alpha;
     const long long stride = static_cast<long long>(gridDim.x) * blockDim.x;
     for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < n8; i += stride) {
         const float4 a = src[2 * i], b = src[2 * i + 1];
-        float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        float v[8] = {f * a.x, f * a.y, f * a.z, f * a.w, f * b.x, f * b.y, f * b.z, f * b.w};
         uint4 o;
         unsigned* ow = reinterpret_cast<unsigned*>(&o);
         if (add) {
@@ -840,8 +844,8 @@ cudaError_t launch_sum_dw(const SumDwArgs& a, cudaStream_t stream) {
     return launch(k_sum_dw, dim3(static_cast<unsigned>((a.n / 4 + 255) / 256)), 256, stream, a);
 }
 
-cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, bool add, cudaStream_t stream) {
-    return launch(k_cast_dw, dim3(1184), 256, stream, reinterpret_cast<const float4*>(src), reinterpret_cast<uint4*>(dst), n >> 3, add ? 1 : 0);
+cudaError_t launch_cast_dw(const float* src, __nv_bfloat16* dst, long long n, const float* alpha, bool add, cudaStream_t stream) {
+    return launch(k_cast_dw, dim3(1184), 256, stream, reinterpret_cast<const float4*>(src), reinterpret_cast<uint4*>(dst), n >> 3, alpha, add ? 1 : 0);
 }
 
 }  // namespace unity

@@ -439,7 +439,7 @@ struct LossLayout {
     int* tok_slot; int* slot_tok; int8_t* tok_model; int* blk_cnt; DevPlan* plan; unsigned* sync_counters;
     __nv_bfloat16* hp; int* target_p; float4* stats; float* partial;
     LossShapes* shapes; int *ids_p, *cnt_p; float *q_p, *top_z;
-    float *row_lse, *coef_p, *coef_g, *target_g;
+    float *row_lse, *coef_p, *coef_g, *target_g, *alpha;
     __nv_bfloat16* G; float *tile_max, *parts, *dWc;
     long long max_slots, part_stride;
     int n_blocks, n_counters;
@@ -518,6 +518,7 @@ LossLayout carve_loss(char* base, size_t cap, long long n_tok, int H, int V, int
         L.coef_p = b.take<float>(ms);
         L.coef_g = b.take<float>(ms);
         L.target_g = b.take<float>(ms);
+        L.alpha = b.take<float>(K);
         L.G = b.take<__nv_bfloat16>(static_cast<size_t>(B.rows) * B.cols);
         if (B.keep) L.tile_max = b.take<float>(static_cast<size_t>(B.rows) * (B.cols / kTileN));
         L.part_stride = static_cast<long long>(B.keep ? part_rows(B.rows, H, V) : B.rows) * H;
@@ -675,7 +676,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     for (int k = 0; k < K && c.norm; ++k) la.norm[k] = c.norm[k];
     la.smoothing = c.smoothing; la.z_loss = c.z_loss; la.n_top = c.n_top; la.kd = c.kd; la.hard = c.hard;
     la.ids_p = L.ids_p; la.cnt_p = L.cnt_p; la.q_p = L.q_p; la.top_z = L.top_z; la.target_p = L.target_p;
-    la.with_grad = want; la.row_lse = L.row_lse; la.coef_p = L.coef_p; la.coef_g = L.coef_g; la.target_g = L.target_g;
+    la.with_grad = want; la.row_lse = L.row_lse; la.coef_p = L.coef_p; la.coef_g = L.coef_g; la.target_g = L.target_g; la.alpha = L.alpha;
     la.tok_loss = c.tok_loss; la.lse = c.lse; la.partial = L.partial; la.loss = c.loss;
     auto w_map = [&](CUtensorMap* tm, int k, int box) {
         return make_tmap(ctx, tm, r->W[k], H, V, static_cast<uint64_t>(H) * 2, box);
@@ -720,7 +721,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     auto store_dh = [&](const GemmArgs& h, const RowSpan& span, int bound) {
         RowSpan stored = span;
         if (at_once > 1) stored.model = -1;
-        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, 1, low_rows, at_once > 1 ? L.max_slots : bound, dH};
+        const StoreArgs sa{L.parts, L.slot_tok, stored, K, H, L.part_stride, h.shapes, 1, low_rows, L.alpha, at_once > 1 ? L.max_slots : bound, dH};
         nl += 1;
         return launch_store_parts(sa, st);
     };
@@ -794,7 +795,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                     FewRowsArgs f;
                     memset(&f, 0, sizeof(f));
                     f.plan = L.plan; f.model = k; f.H = H; f.V = V; f.low_rows = low_rows; f.parts = L.parts; f.dW = c.dW[k];
-                    f.wide = reinterpret_cast<uintptr_t>(c.dW[k]) % 32 == 0;
+                    f.alpha = L.alpha; f.wide = reinterpret_cast<uintptr_t>(c.dW[k]) % 32 == 0;
                     f.status = ctx->d_status; f.wait_budget = ctx->wait_budget;
                     few_rows_plan(H, V, ctx->sm_count, L.part_stride, &f);
                     CUtensorMap tm_O;
@@ -803,7 +804,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         ProfScope ps(ctx, UNITY_PROF_DW_GEMM);
                         CUDA_TRY(ctx, launch_few_rows_bwd(tm_G_k, tm_hp_k, tm_W_mn, out16 ? &tm_O : nullptr, f, st));
                     }
-                    const StoreArgs sa{L.parts, L.slot_tok, chunk, K, H, 0, nullptr, f.parts_n, low_rows, bound, dH};
+                    const StoreArgs sa{L.parts, L.slot_tok, chunk, K, H, 0, nullptr, f.parts_n, low_rows, L.alpha, bound, dH};
                     CUDA_TRY(ctx, launch_store_parts(sa, st));
                     nl += 2;
                     continue;
@@ -858,6 +859,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         w.a_row0 = row0; w.m_rows = n_here; w.n_cols = H; w.ldc = H;
                         const long long at = static_cast<long long>(v0 + row0) * H;
                         const bool add = add_dw || c0 > 0;
+                        if (!split_dw && !B.dw_scratch) w.alpha = L.alpha;
                         if (split_dw) { w.C = L.parts; w.split_rows = 1; w.g_wide_store = 1; }
                         else if (out16) w.C16 = static_cast<__nv_bfloat16*>(c.dW[k]) + at;
                         else w.C = dWk + at;
@@ -886,7 +888,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         CUDA_TRY(ctx, launch_gemm(out16 && !split_dw ? kEpiAccumB16 : kEpiAccumF32, true, c_dw, tm_G_mn, tm_hp_mn, w, ctx->sm_count, st, wide_here));
                         nl += 1;
                         if (split_dw) {
-                            const SumDwArgs sd{L.parts, chunk, L.shapes, static_cast<long long>(V) * H, add, dWk,
+                            const SumDwArgs sd{L.parts, chunk, L.shapes, static_cast<long long>(V) * H, B.dw_scratch ? nullptr : L.alpha, add, dWk,
                                                out16 ? static_cast<__nv_bfloat16*>(c.dW[k]) : nullptr};
                             CUDA_TRY(ctx, launch_sum_dw(sd, st));
                             nl += 1;
@@ -896,7 +898,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
             }
         }
         if (want_w && B.dw_scratch) {
-            CUDA_TRY(ctx, launch_cast_dw(dWk, static_cast<__nv_bfloat16*>(c.dW[k]), static_cast<long long>(V) * H, c.accumulate != 0, st));
+            CUDA_TRY(ctx, launch_cast_dw(dWk, static_cast<__nv_bfloat16*>(c.dW[k]), static_cast<long long>(V) * H, L.alpha + k, c.accumulate != 0, st));
             nl += 1;
         }
     }

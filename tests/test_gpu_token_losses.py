@@ -627,6 +627,27 @@ def test_current_device_and_default_arguments_stay():
     ctx.close()
 
 
+@pytest.mark.parametrize("N", [87, 150, 333, 1500])
+def test_targets_of_unsure_rows_are_not_rounded_together(N):
+    """Without weights dL/dz / (tau/M) is p - 1 at the target: at most p away from -1, which bf16 holds.  tau/M itself, which it does
+    not hold, comes in fp32.  So the target's entry is off by at most p (and its own error), the others' p by b and eg of them."""
+    p = Problem(N, 64, 4096, 1, 1, seed=N, mask=0.0, spread=0.0).gpu()
+    ctx = context(p, "ce")
+    g = call(ctx, p, "ce", dw=torch.float32, weight=False)
+    ctx.check_status()
+    h, W, y, at = p.d_hidden.double(), p.d_W[0].double(), p.d_target.long(), torch.arange(N, device="cuda")
+    ez = (p.H / 16 + 2) * 2 * U * (h.abs() @ W.abs().T).max(1).values[:, None]
+    P = torch.softmax(h @ W.T, 1)
+    tol = (B * (1 + B) + 2.0 ** -10 + 2 * ez + 2.0 ** -16) * P
+    tol[at, y] = P[at, y] * (1 + 2 * ez[:, 0] + 2.0 ** -16) + 4 * U
+    G = P.clone()
+    G[at, y] -= 1
+    want = G.T @ h / N
+    sums = ((N / 16 + 2) * 2 * U * G.abs()).T @ h.abs()
+    assert torch.all((g["dW"][0].double() - want).abs() <= (tol.T @ h.abs() + sums) / N + 4 * U * want.abs())
+    ctx.close()
+
+
 def test_offsets_beyond_32_bits():
     """16500 rows of 152064 kept logits: more than 2^31 of them.  Reference: the formulas in 64 bits on the device, 500 rows at a
     time; tolerances as in oracle(), with a bound of |h| |W| that holds for every entry."""
