@@ -524,7 +524,7 @@ struct LossGradArgs {
 };
 // Up to 64 tokens half of the one 128-row tile is empty: it takes the gradients' low halves, and dHidden and dW come from 16
 // bits of dL/dz, for 2 to 4 % of the time.  (With few tokens a gradient row is hardly more than the target's entry times a row of W or of hidden,
-// and the rounding of that one entry does not average out: up to 3e-3 in the 2-norm where the output's own rounding is 1.7e-3.
+// and with token weights the rounding of that one entry does not average out: up to 3e-3 in the 2-norm where the output's own rounding is 1.7e-3.
 // From 65 to 128 tokens it would take a tile of 256 rows and 18-24 % of the time.)
 constexpr int kLowTokens = 64;
 cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream);
