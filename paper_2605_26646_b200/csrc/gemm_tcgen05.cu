@@ -318,8 +318,11 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
 }
 
 // Token losses, forward: what one thread (= one row) carries through a sweep of column tiles.
-//   s = sum 2^((z - ref) c2), z2 = sum z (both as even / odd halves), the target's logit, and where the row stands in its
-//   ascending list of entries (next vocabulary index, INT_MAX: none left).
+//   s = sum over all columns but the target's of 2^((z - ref) c2), z2 = sum z (both as even / odd halves), the target's logit,
+//   and where the row stands in its ascending list of entries (next vocabulary index, INT_MAX: none left).
+// The target's own term is left out of s: a sure token's loss is log(1 + s / 2^((z_target - ref) c2)), whose digits are those of
+// s, where lse - z_target is a difference of two numbers near 20 (z_target = 20 over a background of 4096 logits near 0: off by up
+// to 35 % so, by 1e-5 now).  A target that is infinite or NaN stays in s, which then says so.
 // ref need not be the maximum: it is 0 where the first tile's maximum lies within kRefBelow octaves below and kRefRoom above
 // that, else that maximum, and later a tile's maximum more than kRefRoom octaves above it.  So a tile is read from tensor
 // memory once (a maximum first and the sum after it read it twice: 252 against 353 us at 801 x 896 x 151936), no sum exceeds
@@ -392,27 +395,40 @@ __device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w,
         float tm = kNegBig;
         uint32_t ra[32], rb[32];
         ptx::tmem_ld_32x32(taddr, ra);
-        auto work = [&](const uint32_t (&rr)[32], int c) {
+        auto work = [&](uint32_t (&rr)[32], int c) {
             const int cbase = col0 + c * 32, n_here = n_tile - c * 32;
             unsigned packed[16];
             // sums of 32 columns are formed apart and then added: V additions one after the other would cost log s digits
             uint64_t cs = 0ull, cz = 0ull;
+            const int jt = w.tgt - cbase;
+            const bool mine = jt >= 0 && jt < 32;
+            float z_sum = 0.f;
+            if (mine) {                                        // (a target lies before n_here: columns behind the vocabulary are 0)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    z_sum += __uint_as_float(rr[j]);
+                    if (j == jt) w.z_tgt = __uint_as_float(rr[j]);
+                }
+                if (fabsf(w.z_tgt) < INFINITY) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) if (j == jt) rr[j] = __float_as_uint(kNegBig);
+                }
+            }
             const float cm = n_here >= 32 ? loss_chunk<STASH, false>(k, w, rr, n_here, cs, cz, packed)
                                           : loss_chunk<STASH, true>(k, w, rr, n_here, cs, cz, packed);
             tm = fmaxf(tm, cm);
+            if (mine) {
+                tm = fmaxf(tm, w.z_tgt);
+                cz = ptx::pack2(z_sum, 0.f);
+            }
             s2 = ptx::add2(s2, cs);
             z2 = ptx::add2(z2, cz);
-            const int jt = w.tgt - cbase;
-            if (jt >= 0 && jt < 32) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j) if (j == jt) w.z_tgt = __uint_as_float(rr[j]);
-            }
             while (w.next < cbase + 32) {                     // listed entries among these columns
                 const int jn = w.next - cbase;
                 float z = 0.f;
 #pragma unroll
                 for (int j = 0; j < 32; ++j) if (j == jn) z = __uint_as_float(rr[j]);
-                k.top_z[w.base + w.pos] = z;
+                k.top_z[w.base + w.pos] = jn == jt ? w.z_tgt : z;
                 ++w.pos;
                 w.next = w.pos < w.cnt ? k.top_ids[w.base + w.pos] : 0x7fffffff;
             }
@@ -734,7 +750,7 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
             }
             // ... and the forward's row state, its list at this unit's first column
             const LossConsts lk{c2, g.n_cols, g.n_tiles, g.top_ids, g.top_z, g.tile_max, g.stash, g.ldz};
-            LossRow lr{0.f, kNegBig, 0ull, 0ull, tgt, 0x7fffffff, 0, 0, 0, true};
+            LossRow lr{0.f, -INFINITY, 0ull, 0ull, tgt, 0x7fffffff, 0, 0, 0, true};
             if (EPI == kEpiLossStats && g.top_ids != nullptr && row_ok) {
                 lr.base = static_cast<long long>(g.a_row0 + row) * g.top_n;
                 lr.cnt = g.top_cnt[g.a_row0 + row];

@@ -159,7 +159,7 @@ enum GemmEpilogue : int {
     kEpiSoftmaxStats = 0,   // online (max, sum exp, sum exp*z, target logit) per row; nothing of size M x N stored
     kEpiLogitGrad = 1,      // dL/dz in bf16 for a bounded (rows x vocab) chunk
     kEpiAccumF32 = 2,       // C (+)= acc, fp32, row-major
-    kEpiLossStats = 3,      // token losses: online (max, sum exp, sum z, target logit) per row, the logits of listed entries
+    kEpiLossStats = 3,      // token losses: (reference, sum exp, sum z, target logit) per row, the logits of listed entries
     kEpiLossGrad = 4,       // token losses: dL/dz in bf16 for a bounded (rows x vocab) chunk
     kEpiAccumB16 = 5        // C (+)= acc rounded to bf16, row-major (token losses' dW)
 };
@@ -186,6 +186,7 @@ struct GemmArgs {
                               // from fwd.n_pairs (workers) and fwd.gmax (row tiles in flight that fit L2)
     int sync_period;          // epilogues other than softmax: rendezvous at every sync_period-th tile of a worker (>= 1)
     float4* stats;            // [n_splits][stats_pitch], row relative to a_row0: (max acc, sum e, sum e*acc, target acc)
+                              // (kEpiLossStats: (reference, sum e without the target's, sum acc, target acc or -inf))
     long long stats_pitch;
     const int* target_p;      // [rows] packed targets (global vocabulary index), indexed from a_row0 + row
     int vocab0;               // global vocabulary index of B row b_row0
@@ -450,7 +451,7 @@ struct LossGatherArgs {
     const __nv_bfloat16* hidden;
     const int* target;         // nullable
     __nv_bfloat16 *hp, *dHidden;   // dHidden nullable
-    int* target_p;
+    int* target_p;             // without targets: the list's likeliest entry, or -1
     int low_rows;              // a model's first low_rows rows are packed twice (see LossGradArgs); 0: none
     int n_top, logits;         // logits 1: softmax of the listed logits (times scale); 0: exp of listed log-probabilities
     float scale;
@@ -471,7 +472,7 @@ struct LossRowArgs {
     unsigned* ticket;          // this launch's counter, zero before it
     long long max_slots;
     int K, V;
-    const float4* stats;       // (max, sum exp, sum z, target logit) per split, accumulator units
+    const float4* stats;       // (reference, sum exp without the target's, sum z, target logit or -inf) per split, accumulator units
     const int* slot_tok;
     const int8_t* tok_model;
     float scale;

@@ -241,7 +241,8 @@ __global__ void __launch_bounds__(1024) k_loss_route(LossRouteArgs a) {
 // One warp's list: ascending, distinct vocabulary indexes with their teacher probabilities q.  Entries with a negative id are
 // empty places, an id >= V is reported and counts as one, and so do entries of probability zero (a logit of -inf); equal ids
 // add up in list order.  With at most 128 entries, four to a lane, a rank by counting (each entry is compared with all others,
-// which sit in shared memory and are read four at a time) needs no sorting network.
+// which sit in shared memory and are read four at a time) needs no sorting network.  Without targets the likeliest entry (the first
+// of equal ones) is the row's "target", the one that the forward sweep keeps apart: a model as sure as its teacher is sure of that.
 __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slot, int tok, int (*sh_ids)[kMaxTop], float (*sh_qs)[kMaxTop]) {
     constexpr int kPer = kMaxTop / 32;
     const int lane = threadIdx.x & 31;
@@ -311,7 +312,8 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
         if (id[u] != kNone) { sh_id[rank[u]] = id[u]; sh_q[rank[u]] = x[u]; }
     __syncwarp();
     // sorted: the first of several equal ids takes their sum
-    int kept = 0;
+    int kept = 0, best = kNone;
+    float best_q = 0.f;
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
         const int r = lane + 32 * u;
@@ -324,10 +326,15 @@ __device__ __forceinline__ void warp_list(const LossGatherArgs& a, long long slo
             const long long at = slot * a.n_top + kept + __popc(leads & ((1u << lane) - 1u));
             a.ids_p[at] = mine;
             a.q_p[at] = q;
+            if (q > best_q) { best_q = q; best = mine; }
         }
         kept += __popc(leads);
     }
     if (lane == 0) a.cnt_p[slot] = kept;
+    if (a.target == nullptr) {
+        best = __reduce_min_sync(kFull, best_q == warp_max(best_q) ? best : kNone);
+        if (lane == 0) a.target_p[slot] = best == kNone ? -1 : best;
+    }
 }
 
 // One warp per packed row and per token, w: 128-bit copies of the hidden row (zeros for padding slots) with its target, and
@@ -369,7 +376,7 @@ __device__ __forceinline__ void gather_row(const LossGatherArgs& a, long long w,
             for (int u = 0; u < 8; ++u) if (j0 + 32 * u < n16) low[j0 + 32 * u] = v[u];
         }
     }
-    if (lane == 0) a.target_p[w] = a.target ? a.target[tok] : -1;
+    if (lane == 0 && a.target != nullptr) a.target_p[w] = a.target[tok];
 }
 
 __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
@@ -427,8 +434,9 @@ __global__ void __launch_bounds__(256) k_loss_pack(LossRouteArgs r, LossGatherAr
 }
 
 // One warp per packed row: merge the vocabulary splits' statistics (one lane per split), then the row's loss and what
-// its gradient needs.  With d_v = lse - z_v (taken as scale*(max - acc_v) + log s, which keeps the digits of a sure
-// token's small loss):
+// its gradient needs.  With d_v = lse - z_v, which for the target is log(1 + s / e): e = exp(z_target - ref) and s the sum of all
+// other columns' terms, kept apart since the sweep (the digits of a sure token's small loss are those of s).  Where e is a small
+// share of the sum, and for the other listed entries, d_v = scale*(ref - acc_v) + log(s + e):
 //   cross entropy : l = (1-eps) d_y + eps (lse - mean z) + lam lse^2
 //   distillation  : l = kd sum_v q_v (log q_v + d_v) + hard d_y
 // A block's eight losses times their weights are one entry of `partial`; a model's rows start at a multiple of 256, so
@@ -472,7 +480,7 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
             n_splits = fs.last_splits;
         }
         const float c = a.scale * 1.4426950408889634f;
-        float m = -3.0e38f, s = 0.f, zsum = 0.f, zy = -3.0e38f;
+        float m = -3.0e38f, s = 0.f, zsum = 0.f, zy = -INFINITY;
         for (int j = lane; j < n_splits; j += 32) {
             const float4 p = st[j * pitch];
             const float mn = fmaxf(m, p.x);
@@ -486,9 +494,10 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
         m = m_all;
         zsum = warp_sum(zsum);
         zy = warp_max(zy);
-        const float log_s = logf(s);
+        const float e = exp2f((zy - m) * c);                  // 0 without a target
+        const float log_s = logf(s + e);
         const float lse = a.scale * m + log_s;
-        const float dy = a.scale * (m - zy) + log_s;          // lse - z_y (unused without a target)
+        const float dy = e >= s * 0x1p-10f ? log1pf(s / e) : a.scale * (m - zy) + log_s;      // lse - z_y (unused without a target)
         const float w = a.tok_weight ? a.tok_weight[tok] : 1.f;
         float l, cp, gt;
         if (a.n_top == 0) {
@@ -503,7 +512,7 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
             float kl = 0.f, Q = 0.f;
             for (int j = lane; j < cnt; j += 32) {
                 const float q = a.q_p[base + j];
-                kl += q * (logf(q) + (a.scale * (m - a.top_z[base + j]) + log_s));
+                kl += q * (logf(q) + (a.ids_p[base + j] == tgt ? dy : a.scale * (m - a.top_z[base + j]) + log_s));
                 Q += q;
             }
             kl = warp_sum(kl);
@@ -513,9 +522,11 @@ __global__ void __launch_bounds__(256) k_loss_rows(LossRowArgs a) {
             gt = a.hard > 0.f ? a.kd * Q * expf(-dy) + a.hard * expm1f(-dy) : 0.f;
             if (a.with_grad) {
                 for (int j = lane; j < cnt; j += 32) {         // the logits give way to the entries' gradients
-                    const float d = a.scale * (m - a.top_z[base + j]) + log_s;
-                    const float p = expf(-d), hard = a.ids_p[base + j] == tgt ? expm1f(-d) : p;
-                    a.top_z[base + j] = w * (a.kd * (Q * p - a.q_p[base + j]) + a.hard * hard);
+                    const bool at = a.ids_p[base + j] == tgt;
+                    const float d = at ? dy : a.scale * (m - a.top_z[base + j]) + log_s, q = a.q_p[base + j];
+                    // Q p - q, of the target as Q (p - 1) + (Q - q): both may be near 1
+                    const float p = at ? expm1f(-d) : expf(-d);
+                    a.top_z[base + j] = w * (a.kd * (at ? Q * p + (Q - q) : Q * p - q) + a.hard * p);
                 }
             }
         }
