@@ -213,7 +213,8 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
         int s = 0;
         for (int c = c0; c < c1; ++c) {
             const int b = (c - c0) & 1;
-            ok = ptx::mbar_wait(&acc_full[b], ((c - c0) >> 1) & 1, a.wait_budget) && !*abort_flag;
+            // (all lanes go on or none: the loads from tensor memory are the whole warp's)
+            ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[b], ((c - c0) >> 1) & 1, a.wait_budget) && !*abort_flag);
             if (!ok) break;
             ptx::tc_fence_after();
             const int v = c * kChunk + at;
@@ -258,7 +259,7 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
             }
             if (++s == kWStages) s = 0;
         }
-        if (ok) ok = ptx::mbar_wait(dh_full, 0, a.wait_budget) && !*abort_flag;
+        if (ok) ok = __all_sync(0xffffffffu, ptx::mbar_wait(dh_full, 0, a.wait_budget) && !*abort_flag);
         if (ok) {
             ptx::tc_fence_after();
             float* dst = a.parts + (static_cast<long long>(part) * kRows + at) * a.H + h0;

@@ -264,17 +264,19 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
         unsigned o[16];
         if (add) {
             __nv_bfloat16* d = C16 + static_cast<long long>(row0 + lane) * ldc + col0 + c * 32;
-            if (!row_ok) return;
+            if (row_ok) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint4 old = *reinterpret_cast<const uint4*>(d + q * 8);
-                const unsigned ow[4] = {old.x, old.y, old.z, old.w};
+                for (int q = 0; q < 4; ++q) {
+                    const uint4 old = *reinterpret_cast<const uint4*>(d + q * 8);
+                    const unsigned ow[4] = {old.x, old.y, old.z, old.w};
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    o[4 * q + j] = pack_bf16(fmaf(alpha, __uint_as_float(rr[8 * q + 2 * j]), __uint_as_float(ow[j] << 16)),
-                                             fmaf(alpha, __uint_as_float(rr[8 * q + 2 * j + 1]), __uint_as_float(ow[j] & 0xffff0000u)));
-                *reinterpret_cast<uint4*>(d + q * 8) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                    for (int j = 0; j < 4; ++j)
+                        o[4 * q + j] = pack_bf16(fmaf(alpha, __uint_as_float(rr[8 * q + 2 * j]), __uint_as_float(ow[j] << 16)),
+                                                 fmaf(alpha, __uint_as_float(rr[8 * q + 2 * j + 1]), __uint_as_float(ow[j] & 0xffff0000u)));
+                    *reinterpret_cast<uint4*>(d + q * 8) = make_uint4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                }
             }
+            __syncwarp();                                      // whole warps load from tensor memory and wait for it
             return;
         }
 #pragma unroll
@@ -394,6 +396,7 @@ __device__ __forceinline__ void loss_stats_tile(const LossConsts& k, LossRow& w,
         uint64_t s2 = 0ull, z2 = 0ull;
         float tm = kNegBig;
         uint32_t ra[32], rb[32];
+        __syncwarp();
         ptx::tmem_ld_32x32(taddr, ra);
         auto work = [&](uint32_t (&rr)[32], int c) {
             const int cbase = col0 + c * 32, n_here = n_tile - c * 32;
@@ -766,7 +769,9 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
 
             for (int ni = t.n_begin; ni < t.n_end && ok; ++ni) {
                 const int nt = t.rev ? t.n_begin + t.n_end - 1 - ni : ni;
-                if (!ptx::mbar_wait(&acc_full[acc], acc_phase, g.wait_budget) || *abort_flag) { ok = false; break; }
+                // (all lanes go on or none: the loads below are the whole warp's)
+                ok = __all_sync(0xffffffffu, ptx::mbar_wait(&acc_full[acc], acc_phase, g.wait_budget) && !*abort_flag);
+                if (!ok) break;
                 ptx::tc_fence_after();
                 const uint32_t taddr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + acc * kTileCols;
                 const int mma_n = is_accum(EPI) ? g.mma_n : kTileN;     // columns per MMA block (<= 256)
@@ -788,6 +793,7 @@ __device__ __forceinline__ void gemm_body(const CUtensorMap& tmA, const CUtensor
                 for (int c = 0; c < (EPI == kEpiLossStats || EPI == kEpiAccumB16 ? 0 : NB * per_block); ++c) {
                     const int cbase = col0 + c * 32;            // block nb of a two-block tile starts at col0 + nb * mma_n
                     if (cbase >= g.n_cols) break;               // uniform across the CTA
+                    __syncwarp();                               // rows part ways at their bounds and targets
                     uint32_t rr[32];
                     // ... and sits at tensor-memory column nb * 256 whatever mma_n is
                     ptx::tmem_ld_32x32(taddr + (NB == 1 ? c * 32 : (c / per_block) * kTileN + (c % per_block) * 32), rr);

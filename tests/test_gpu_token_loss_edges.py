@@ -1,0 +1,32 @@
+"""GPU: forms of the token losses at the edges - gradients of the head added to old values where a warp's rows end inside the
+vocabulary's last tile."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2605_26646_b200 import binding as ub
+from test_gpu_token_losses import B, Problem, call, check, context, oracle
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dw", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("N,H,V,K", [(50, 64, 8, 1), (100, 320, 1000, 1), (300, 192, 136, 2), (700, 1088, 2504, 1), (1500, 576, 4120, 1),
+                                     (1200, 128, 40000, 2)])
+def test_adding_to_the_heads_gradients_at_ragged_vocabularies(N, H, V, K, op, dw):
+    """V ends 8, 16 or 24 entries into a warp's 32 rows of dW: the others of the warp neither read nor write."""
+    p = Problem(N, H, V, K, K, n_top=5, seed=N + V).gpu()
+    ctx = context(p, op)
+    guard = 64
+    torch.manual_seed(V)
+    whole = [torch.randn((V + 2 * guard) * H, device="cuda").to(dw) * 0.01 for _ in range(K)]
+    before = [w.clone() for w in whole]
+    old = [w[guard * H:-guard * H].view(V, H) for w in whole]
+    base = [x.double().cpu().numpy() for x in old]
+    g = call(ctx, p, op, accumulate=True, dW=old)
+    ctx.check_status()
+    check(p, g, oracle(p, op), base=base)
+    for w, b in zip(whole, before):
+        assert torch.equal(w[:guard * H], b[:guard * H]) and torch.equal(w[-guard * H:], b[-guard * H:])
+    ctx.close()
