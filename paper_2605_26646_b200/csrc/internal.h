@@ -128,8 +128,9 @@ constexpr int kSplitWavesDw = 2;        // dW (heads of few tiles): 2 waves
 struct SplitShape { int splits, per_split; };
 struct SplitParams { int most, n_tiles, k_iters, workers, tile_rows, waves; };   // most = 0: never cut; waves: bounds the parts
 __host__ __device__ inline long long split_candidate(const SplitParams& p, int m_tiles, int s, SplitShape& f) {
-    f.per_split = (p.k_iters + s - 1) / s;
-    f.splits = (p.k_iters + f.per_split - 1) / f.per_split;
+    const int k = p.k_iters > 0 ? p.k_iters : 1;               // (dW of a block without a token: nobody reads its schedule)
+    f.per_split = (k + s - 1) / s;
+    f.splits = (k + f.per_split - 1) / f.per_split;
     const long long units = static_cast<long long>(m_tiles) * p.n_tiles * f.splits, waves = (units + p.workers - 1) / p.workers;
     return waves * (f.per_split + kSplitOverhead) + (s > 1 ? s : 0);
 }
