@@ -241,7 +241,8 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in, int k) {
         if (in.stash_by_slot) g.a_k0 = slot0;
         if (in.split_rows) {
             const bool whole = n_rows == in.span.row_cap;
-            g.k_splits = whole ? split.x : split.z; g.k_per_split = whole ? split.y : split.w;
+            g.k_per_split = whole ? split.y : split.w;
+            g.k_splits = g.k_iters > 0 ? parts_in_use(whole ? split.x : split.z, g.k_per_split, g.k_iters) : 0;
             g.c_split = static_cast<long long>(in.m_rows) * in.ldc;
         }
     }

@@ -138,6 +138,12 @@ __host__ __device__ inline bool split_allowed(const SplitParams& p, int m_tiles,
     return s == 1 || (s <= p.most && s <= p.k_iters / 8 && static_cast<long long>(m_tiles) * p.n_tiles * s <= static_cast<long long>(p.waves) * p.workers);
 }
 constexpr int kMaxKSplits = 32;
+// Parts of a contraction over the rows, planned for a whole block of them: the slabs end with the last one that holds a token, so
+// the plan may have parts behind them, whose outputs nobody would write.  The GEMM and the sum of the parts leave those out.
+__host__ __device__ inline int parts_in_use(int splits, int per_split, int k_iters) {
+    const int used = (k_iters + per_split - 1) / per_split;
+    return used < splits ? used : splits;
+}
 
 // The schedules of a token loss, per model: [0] of a full block of rows (RowSpan::row_cap of them), [1] of the model's last
 // one.  Written once per call by the kernel that counts the rows (a warp weighs the candidates side by side; evaluated where

@@ -758,7 +758,8 @@ __global__ void __launch_bounds__(256) k_sum_dw(SumDwArgs a) {
     int slot0, rows;
     span_resolve(a.span, slot0, rows);
     if (rows <= 0 && a.add) return;
-    const int splits = a.shapes->dw[a.span.model][rows == a.span.row_cap ? 0 : 1].splits;
+    const SplitShape& plan = a.shapes->dw[a.span.model][rows == a.span.row_cap ? 0 : 1];
+    const int splits = rows > 0 ? parts_in_use(plan.splits, plan.per_split, span_slab_rows(a.span, rows) / kTileK) : 0;
     float4 v = rows > 0 ? sum_parts(a.parts + i, splits, a.n) : make_float4(0.f, 0.f, 0.f, 0.f);
     const float f = a.alpha ? a.alpha[a.span.model] : 1.f;
     v.x *= f; v.y *= f; v.z *= f; v.w *= f;

@@ -36,6 +36,31 @@ int main(int argc, char** argv) {
         }
         return 0;
     }
+    if (argc > 1 && !strcmp(argv[1], "parts")) {
+        // dW of a full block whose last rows hold no token (rows are padded to 256): every part that is used has a slab, and
+        // the parts that are used hold all slabs.  Also for plans that this choice does not make: every allowed count of parts.
+        long long cases = 0;
+        for (int rows = kTileM; rows <= 18432; rows += kTileM)
+            for (int tiles = 1; tiles <= 74; ++tiles) {
+                const SplitParams p{kMaxKSplits, tiles, rows / kTileK, 74, kTileM, kSplitWavesDw};
+                const SplitShape chosen = choose(p, 1);
+                for (int c = 0; c <= kMaxKSplits; ++c) {
+                    SplitShape s = chosen;
+                    if (c > 0 && !split_allowed(p, 1, c)) continue;
+                    if (c > 0) split_candidate(p, 1, c, s);
+                    for (int valid = rows - kTileM + 1; valid <= rows; valid += 5) {
+                        const int slabs = (valid + kTileK - 1) / kTileK, n = parts_in_use(s.splits, s.per_split, slabs);
+                        ++cases;
+                        if (n < 1 || (n - 1) * s.per_split >= slabs || n * s.per_split < slabs) {
+                            printf("rows %d valid %d tiles %d: %d of %d parts of %d\n", rows, valid, tiles, n, s.splits, s.per_split);
+                            return 1;
+                        }
+                    }
+                }
+            }
+        printf("%lld\n", cases);
+        return 0;
+    }
     return 2;
 }
 """
@@ -56,3 +81,9 @@ def test_contractions_without_rows_have_one_part(program):
     """No division by a part's length of zero."""
     run = subprocess.run([program, "empty"], capture_output=True, text=True)
     assert run.returncode == 0, (run.returncode, run.stdout)
+
+
+def test_no_part_of_a_contraction_over_rows_is_empty(program):
+    run = subprocess.run([program, "parts"], capture_output=True, text=True)
+    assert run.returncode == 0, run.stdout
+    assert int(run.stdout) > 1_000_000
