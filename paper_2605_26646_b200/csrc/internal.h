@@ -481,7 +481,6 @@ struct LossRowArgs {
     int K, V;
     const float4* stats;       // (reference, sum exp without the target's, sum z, target logit or -inf) per split, accumulator units
     const int* slot_tok;
-    const int8_t* tok_model;
     float scale;
     const float* tok_weight;   // caller order, nullable
     int has_norm;

@@ -377,7 +377,7 @@ __global__ void k_gather_rows(const __nv_bfloat16* __restrict__ hidden, const in
     } else {
         for (int j = lane; j < n16; j += 32) dst[j] = make_uint4(0, 0, 0, 0);
     }
-    if (lane == 0) target_p[slot] = tok >= 0 ? (target ? target[tok] : -1) : 0;
+    if (lane == 0) target_p[slot] = tok >= 0 ? target[tok] : 0;
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -218,7 +218,6 @@ __device__ __forceinline__ void write_routes(const LossRouteArgs& a, const Route
     for (int j = 0; j < kPer; ++j) {
         if (j >= per || i0 + j >= n) continue;
         const int slot = model[j] >= 0 ? sh.off[model[j]] + rank[j] : -1;
-        r.tok_model[i0 + j] = static_cast<int8_t>(model[j]);
         r.tok_slot[i0 + j] = slot;
         if (slot >= 0) { r.slot_tok[slot] = i0 + j; continue; }
         if (a.tok_loss) a.tok_loss[i0 + j] = 0.f;

@@ -671,7 +671,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     memset(&la, 0, sizeof(la));
     la.block = RowSpan{L.plan, -1, 0, cap_all}; la.plan = L.plan; la.shapes = L.shapes; la.tile_rows = fwd.tile_rows;
     la.ticket = tickets++; la.max_slots = L.max_slots; la.K = K; la.V = V;
-    la.stats = L.stats; la.slot_tok = L.slot_tok; la.tok_model = L.tok_model; la.scale = scale;
+    la.stats = L.stats; la.slot_tok = L.slot_tok; la.scale = scale;
     la.tok_weight = c.tok_weight; la.has_norm = c.norm != nullptr;
     for (int k = 0; k < K && c.norm; ++k) la.norm[k] = c.norm[k];
     la.smoothing = c.smoothing; la.z_loss = c.z_loss; la.n_top = c.n_top; la.kd = c.kd; la.hard = c.hard;
