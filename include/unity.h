@@ -421,7 +421,9 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
  *                sum over all rows (plus the old value with accumulate_dW)
  * dL/dz is held in bf16 between the products, as in stage 3, but without its common factor inv_temperature / M_k: a gradient
  * entry is off by up to 2^-8 of the terms it sums (and a kept logit by up to 2^-10 octaves).
- * Deterministic: no floating-point atomics anywhere. */
+ * A workspace below unity_token_loss_workspace_bytes() may give other last digits, within the same bound: recomputed logits are
+ * not rounded to steps, and up to 64 tokens the full workspace also holds what rounding to bf16 cut from dL/dz.
+ * Deterministic: every sum has a fixed order. */
 #define UNITY_F32 0
 #define UNITY_BF16 1
 #define UNITY_TEACHER_LOGITS 0   /* q = softmax over the row's listed entries of inv_temperature * top_vals           */

@@ -533,6 +533,8 @@ struct LossGradArgs {
 // bits of dL/dz, for 2 to 4 % of the time.  (With few tokens a gradient row is hardly more than the target's entry times a row of W or of hidden,
 // and with token weights the rounding of that one entry does not average out: up to 3e-3 in the 2-norm where the output's own rounding is 1.7e-3.
 // From 65 to 128 tokens it would take a tile of 256 rows and 18-24 % of the time.)
+// Only where one block holds the rows and kept logits of all models: a workspace without room for that takes per-model blocks or
+// recomputed logits, whose dL/dz is single bf16.
 constexpr int kLowTokens = 64;
 cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream);
 // dHidden[token of slot r of the span] = bf16(sum of the row's parts), in the order of the parts
