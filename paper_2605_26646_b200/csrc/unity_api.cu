@@ -539,10 +539,12 @@ LossBlocks keep_blocks(long long n_tok, int V, int K, bool dw_sums, int most) {
     return LossBlocks{rows, cols, true, false, dw_sums && bound > rows};
 }
 
-// The tensor core's accumulation cuts where fp32 addition would round: a sum of H products loses on average 1.6e-8 of its
-// size per step of 16 (measured: 3.0e-7, 9.7e-7, 1.58e-6, 3.62e-6 at H = 256, 896, 1536, 3584, whatever the sign), because a
-// step cuts in proportion to the partial sum, which on average has grown half way.  The logits' scale takes that mean back,
-// which leaves the cuts' random part: a per-token loss at H = 3584 is then off by 5e-7 of its size and not by 2.5e-6.
+// The tensor core's accumulation cuts where fp32 addition would round.  A sum of H products of both signs, as hidden states times
+// heads are, loses 1.6e-8 of its size per step of 16 on average (3.0e-7, 9.7e-7, 1.58e-6, 3.62e-6 at H = 256, 896, 1536, 3584; on
+// rows with the product's noise between 1 and 8 times its mean 0.92 to 1.34 times that).  The logits' scale takes that mean back: a
+// per-token loss at H = 3584 is then off by 5e-7 of its size and not by 2.5e-6.  It is a mean and no bound: products of one sign
+// lose 0.4 (H = 256) to 2.8 times (5120) as much, a row whose product sits in few channels next to nothing, so that its logit comes
+// out too large by the mean.
 float accumulator_scale(float inv_temperature, int H) {
     return static_cast<float>(inv_temperature * (1.0 + 1.6e-8 * (H / 16) + 4e-8));
 }

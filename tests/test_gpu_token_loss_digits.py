@@ -91,3 +91,66 @@ def test_sure_tokens_keep_their_targets_gradient(N, V, form):
         # G's rounding to bf16, the fp32 sums over at most 300 rows
         assert abs(dW[y, t] - want) <= (B * (1 + B) + p.tol + (N / 16 + 8) * 2 * U) * abs(want), (y, dW[y, t] / want - 1)
     ctx.close()
+
+
+# ------------------------------------------------------------------------------------------------ the logits' scale
+def scale_excess(H):
+    """What the logits' scale adds to the temperature: the tensor core's mean cut on sums of products of both signs."""
+    return 1.6e-8 * (H // 16) + 4e-8
+
+
+def one_target(h, w, V=264, y=5):
+    """Rows `h` whose one large logit is h w at `y` (the others are 0), and what cross entropy's lse says of them, relative."""
+    N, H = h.shape
+    W = torch.zeros(V, H, dtype=torch.bfloat16)
+    W[y] = w
+    z = (h.double() @ W[y].double()).numpy()
+    cuda = dict(device="cuda")
+    ctx = ub.Context(0, ub.unity_token_loss_workspace_bytes(N, H, V, 1, 0, False))
+    loss, lse = torch.empty(1, **cuda), torch.empty(N, **cuda)
+    ctx.cross_entropy_fwd_bwd(h.cuda(), [W.cuda()], torch.tensor([0, N], **cuda), torch.zeros(1, dtype=torch.int32, **cuda), [0],
+                              torch.full((N,), y, dtype=torch.int32, **cuda), None, 1.0, 0.0, 0.0, None, False, None, loss, None, lse)
+    ctx.check_status()
+    ctx.close()
+    want = z + np.log1p((V - 1) * np.exp(-z))
+    return (lse.double().cpu().numpy() - want) / want
+
+
+@pytest.mark.parametrize("noise", [1, 3, 8])
+@pytest.mark.parametrize("H", [256, 896, 1536, 3584])
+def test_scale_takes_back_the_mean_cut_of_products_of_both_signs(H, noise):
+    """Left out or taken twice, the excess would leave a mean of about minus or plus itself; half of it is the bound (the cut was
+    measured between 0.92 and 1.34 of it on such rows).  Logits from 33 to 60: their row's reference is the logit itself, so lse has no
+    more roundings than scale, product and sum (3 u)."""
+    g = torch.Generator().manual_seed(100 * H + noise)
+    w = (torch.randn(H, generator=g) / H ** 0.5).to(torch.bfloat16)
+    h = 46 * w.float() + noise * torch.randn(400, H, generator=g)
+    h = (h * (torch.linspace(35, 58, 400) / (h.double() @ w.double()).float())[:, None]).to(torch.bfloat16)
+    err = one_target(h, w)
+    assert abs(err.mean()) <= scale_excess(H) / 2 + 3 * U, (err.mean(), scale_excess(H))
+
+
+@pytest.mark.parametrize("N", [100, 600])
+@pytest.mark.parametrize("H", [896, 1536, 3584])
+def test_scale_of_products_of_one_sign(H, N):
+    """No mean is taken back here: 16 products and the sum so far are cut to the largest one's grid, and products of one sign lose on the
+    same side (0.4 to 2.8 times the excess, the more the wider).  What holds is the accumulator's bound: a step cuts at most 2 u of the
+    sum so far, H/16 + 2 steps, all downwards, and then the excess and 3 u."""
+    g = torch.Generator().manual_seed(H + N)
+    w = (torch.rand(H, generator=g) + 0.5).to(torch.bfloat16)
+    h = torch.rand(N, H, generator=g) + 0.5
+    h = (h * (torch.linspace(34, 59, N) / (h.double() @ w.double()).float())[:, None]).to(torch.bfloat16)
+    err = one_target(h, w)
+    assert np.all(err <= scale_excess(H) + 3 * U) and np.all(err >= scale_excess(H) - (H / 16 + 2) * 2 * U - 3 * U), (err.min(), err.max())
+
+
+@pytest.mark.parametrize("where", [0, 17, -1])
+@pytest.mark.parametrize("H", [64, 896, 3584])
+def test_scale_of_rows_that_sit_in_one_channel(H, where):
+    """Their logits are exact in the tensor core, so the excess stands in lse as it is, to the roundings of scale, product and sum."""
+    h = torch.zeros(112, H, dtype=torch.bfloat16)
+    h[:, where] = torch.arange(112) / 4 + 33                   # up to 60.75: bf16 holds them
+    w = torch.zeros(H, dtype=torch.bfloat16)
+    w[where] = 1
+    err = one_target(h, w)
+    assert np.all(np.abs(err - scale_excess(H)) <= 3 * U), (err.min(), err.max(), scale_excess(H))
