@@ -331,8 +331,10 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
 // memory once (a maximum first and the sum after it read it twice: 252 against 353 us at 801 x 896 x 151936), no sum exceeds
 // 2^kRefRoom * V, and for a backward pass that does not recompute the logits (ref - z) + kRefRoom octaves is kept in steps of
 // 2^-9 octaves, 16 bits.  The integer costs as much memory as bf16 but is off by at most half a step whatever its size: p is
-// off by a factor of 2^(2^-10), 6.8e-4, where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  Entries 96
-// octaves or more below ref, and so 64 below the row's maximum, count as 96.
+// off by a factor of 2^(2^-10), 6.8e-4, where a bf16 probability would be off by 2^-8 and double dL/dz's rounding.  The last
+// step, entries 96 octaves or more below ref and so 64 below the row's maximum, means a probability of 0: a head may hold its type's
+// lowest value where it is masked, and 2^-96 of that is not nothing.  (The target's column, left out of the sum, has it too; its
+// gradient comes by itself.)
 // Bound: the MMAs and the 1 kW power cap (801 x 896 x 151936: 185 us, 1.5 PFLOP/s of the rows the tiles are padded to; without
 // this epilogue's arithmetic 172 us).
 struct LossRow {

@@ -513,7 +513,7 @@ struct TeacherScatterArgs {
 };
 cudaError_t launch_teacher_scatter(const TeacherScatterArgs& a, cudaStream_t stream);
 // In place, the kept logits of a block of rows (GemmArgs::stash) become dL/dz in bf16: coef_p * p - coef_g * uniform, and
-// target_g at the target (0 in rows without a token, whose logits nobody kept), with p = 2^(tile_max * c2 + kRefRoom - lse log2(e) - u / kStashSteps).
+// target_g at the target (0 in rows without a token, whose logits nobody kept), with p = 2^(tile_max * c2 + kRefRoom - lse log2(e) - u / kStashSteps), 0 at the last step.
 struct LossGradArgs {
     uint16_t* Z;
     long long ld;

@@ -650,7 +650,12 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
             if (c0 >= a.cols) continue;
             const float sh = fmaf(shift[u], a.c2, base);
             unsigned* w = reinterpret_cast<unsigned*>(&raw[u]);
-            unsigned lw[4];
+            unsigned lw[4], gone = 0u;
+            const unsigned last = __vmaxu2(__vimax3_u16x2(w[0], w[1], w[2]), w[3]);
+            if (last >= 0xffff0000u || (last & 0xffffu) == 0xffffu) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) gone |= (((w[j] & 0xffffu) == 0xffffu ? 1u : 0u) | (w[j] >= 0xffff0000u ? 2u : 0u)) << (2 * j);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float u0 = __uint_as_float(__byte_perm(w[j], 0x4b000000u, 0x7610)) - 8388608.f;
@@ -663,6 +668,18 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
                     const float2 f = __bfloat1622float2(h);
                     const __nv_bfloat162 l = __floats2bfloat162_rn(g0 - f.x, g1 - f.y);
                     lw[j] = *reinterpret_cast<const unsigned*>(&l);
+                }
+            }
+            if (gone != 0u) {                                  // entries beyond the steps' range: p = 0 (or NaN, as the whole row)
+                const float g = fmaf(0.f, base, -cu);
+                const __nv_bfloat16 hi = __float2bfloat16_rn(g);
+                const unsigned bits = __bfloat16_as_ushort(hi) * 0x10001u;
+                const unsigned low = LOW ? __bfloat16_as_ushort(__float2bfloat16_rn(g - __bfloat162float(hi))) * 0x10001u : 0u;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const unsigned m = ((gone >> (2 * j) & 1u) ? 0xffffu : 0u) | ((gone >> (2 * j) & 2u) ? 0xffff0000u : 0u);
+                    w[j] = (w[j] & ~m) | (bits & m);
+                    if (LOW) lw[j] = (lw[j] & ~m) | (low & m);
                 }
             }
             if (static_cast<unsigned>(tgt - c0) < 8u) {        // the target is among this thread's eight

@@ -1,5 +1,5 @@
 """GPU: forms of the token losses at the edges - gradients of the head added to old values where a warp's rows end inside the
-vocabulary's last tile."""
+vocabulary's last tile, few tokens in workspaces that do not hold all their logits, entries masked by the lowest value."""
 import numpy as np
 import pytest
 import torch
@@ -56,3 +56,40 @@ def test_up_to_64_tokens_in_smaller_workspaces(N, H, V, K, op):
         ctx.close()
         now = now * 15 // 16 // 256 * 256
     assert len(ways) >= 2, ways
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("first", [0, 300, 700])
+@pytest.mark.parametrize("N", [30, 100, 400])
+def test_entries_of_the_vocabulary_that_are_masked_by_the_lowest_value(N, first, op):
+    """Rows of the head at the type's lowest value (logits of -1e38 and less, to -inf), whole column tiles of them: they have probability 0,
+    and the others' losses and gradients are those of a head without them."""
+    H, V, n_off = 64, 1320, 600
+    p = Problem(N, H, V, 1, 1, n_top=6, seed=N + first, spread=1.0)
+    off = np.arange(first, first + n_off)
+    on = np.setdiff1d(np.arange(V), off)
+    rng = np.random.default_rng(N)
+    hidden = p.hidden.float()
+    hidden[:, 0] = torch.from_numpy(rng.random(N).astype(np.float32)) + 0.5
+    hidden[::3, 0] *= 2
+    W = p.W[0].clone()
+    W[:, 0] = 0
+    p.hidden, p.target = hidden.to(torch.bfloat16), torch.from_numpy(rng.choice(on, N).astype(np.int32))
+    p.top_ids = torch.from_numpy(np.where(p.top_ids.numpy() < 0, -1, rng.choice(on, p.top_ids.shape)).astype(np.int32))
+    q = Problem(N, H, V, 1, 1, n_top=6, seed=N + first, spread=1.0)      # the same rows over the entries that are left
+    where = np.full(V + 1, -1)
+    where[on] = np.arange(on.size)
+    q.hidden, q.V, q.W = p.hidden, on.size, [W[on]]
+    q.target = torch.from_numpy(where[p.target.numpy()].astype(np.int32))
+    q.top_ids = torch.from_numpy(where[p.top_ids.numpy()].astype(np.int32))
+    W[off] = 0
+    W[off, 0] = torch.finfo(torch.bfloat16).min
+    p.W = [W]
+    p.gpu()
+    ctx = context(p, op)
+    g = call(ctx, p, op)
+    ctx.check_status()
+    assert torch.all(g["dW"][0][torch.from_numpy(off).cuda()] == 0)
+    g["dW"] = [g["dW"][0][torch.from_numpy(on).cuda()]]
+    check(q, g, oracle(q, op))
+    ctx.close()
