@@ -426,6 +426,9 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
  * The tensor core's fp32 sums cut where they would round.  Logits are scaled up by 1e-9 H + 4e-8 of themselves, the mean of that
  * cut for products of both signs: a row's lse differs by that share (3.6e-6 at H = 3584) from the one of unity_logprob_fwd, which
  * leaves the cut in.  The worst case stays (H/16 + 2) 2^-23 of sum_j |h_j W_vj|.
+ * A valid row whose logits are not finite has NaN as its loss, lse and gradient, and so have its model's loss and dW; other rows and
+ * models are as without it.  A head entry may be masked by its type's lowest value: probability and gradient 0.  By -inf in an
+ * evaluation only (0 * inf in dHidden is NaN): no share in lse, a target there costs inf.
  * Deterministic: every sum has a fixed order. */
 #define UNITY_F32 0
 #define UNITY_BF16 1

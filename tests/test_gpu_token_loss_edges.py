@@ -1,11 +1,11 @@
 """GPU: forms of the token losses at the edges - gradients of the head added to old values where a warp's rows end inside the
-vocabulary's last tile, few tokens in workspaces that do not hold all their logits, entries masked by the lowest value."""
+vocabulary's last tile, few tokens in workspaces that do not hold all their logits, values that are not finite or stand for masks."""
 import numpy as np
 import pytest
 import torch
 
 from paper_2605_26646_b200 import binding as ub
-from test_gpu_token_losses import B, Problem, call, check, context, oracle
+from test_gpu_token_losses import B, U, Problem, call, check, context, oracle
 
 pytestmark = pytest.mark.gpu
 
@@ -58,6 +58,58 @@ def test_up_to_64_tokens_in_smaller_workspaces(N, H, V, K, op):
     assert len(ways) >= 2, ways
 
 
+def rows_of(p, k):
+    """The valid rows of model k."""
+    role = np.repeat(p.inv_role.numpy(), np.diff(p.cu.numpy()))
+    return np.nonzero((np.asarray(p.role_model)[role] == k) & (p.mask.numpy() != 0))[0]
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("N,H,V", [(40, 64, 520), (100, 320, 1000), (400, 64, 4104), (1600, 128, 1000)])
+def test_hidden_rows_that_are_not_finite_stay_by_themselves(N, H, V, bad, op):
+    """A valid row with a NaN or an infinity: its loss, lse and gradient are NaN (as its model's loss and dW, which sum over it); the
+    other rows and the other model come out bit for bit as they do without it."""
+    p = Problem(N, H, V, 2, 2, n_top=5, seed=N, short_lists=False).gpu()
+    ctx = context(p, op)
+    clean = call(ctx, p, op, dw=torch.float32)
+    own = rows_of(p, 0)
+    hit = own[[0, len(own) // 2, -1]]
+    p.d_hidden = p.d_hidden.clone()
+    p.d_hidden[torch.from_numpy(hit).cuda(), H // 2] = bad
+    g = call(ctx, p, op, dw=torch.float32)
+    ctx.check_status()
+    keep = torch.ones(N, dtype=torch.bool, device="cuda")
+    keep[torch.from_numpy(hit).cuda()] = False
+    for key in ("tok_loss", "lse", "dHidden"):
+        assert torch.all(torch.isnan(g[key][~keep])), key
+        assert torch.equal(g[key][keep], clean[key][keep]), key
+    assert torch.isnan(g["loss"][0]) and torch.equal(g["loss"][1], clean["loss"][1])
+    assert torch.all(torch.isnan(g["dW"][0])) and torch.equal(g["dW"][1], clean["dW"][1])
+    ctx.close()
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("N,H,V", [(40, 64, 520), (100, 320, 1000), (400, 64, 4104), (1600, 128, 1000)])
+def test_masked_rows_may_hold_anything(N, H, V, op):
+    """Hidden values, weights, targets and lists of masked tokens are not read."""
+    p = Problem(N, H, V, 2, 2, n_top=5, seed=N + 1).gpu()
+    ctx = context(p, op)
+    clean = call(ctx, p, op, hard=0.5) if op == "kd" else call(ctx, p, op)
+    off = p.d_mask == 0
+    assert int(off.sum()) > 2
+    for name, what in (("d_hidden", float("nan")), ("d_weight", float("inf")), ("d_target", V + 7), ("d_top_ids", V), ("d_top_vals", float("nan"))):
+        t = getattr(p, name).clone()
+        t[off] = what
+        setattr(p, name, t)
+    g = call(ctx, p, op, hard=0.5) if op == "kd" else call(ctx, p, op)
+    ctx.check_status()
+    for key in ("loss", "tok_loss", "lse", "dHidden"):
+        assert torch.equal(g[key], clean[key]), key
+    assert all(torch.equal(a, b) for a, b in zip(g["dW"], clean["dW"]))
+    ctx.close()
+
+
 @pytest.mark.parametrize("op", ["ce", "kd"])
 @pytest.mark.parametrize("first", [0, 300, 700])
 @pytest.mark.parametrize("N", [30, 100, 400])
@@ -92,4 +144,44 @@ def test_entries_of_the_vocabulary_that_are_masked_by_the_lowest_value(N, first,
     assert torch.all(g["dW"][0][torch.from_numpy(off).cuda()] == 0)
     g["dW"] = [g["dW"][0][torch.from_numpy(on).cuda()]]
     check(q, g, oracle(q, op))
+    ctx.close()
+
+
+@pytest.mark.parametrize("N", [20, 300])
+def test_logits_of_minus_infinity(N):
+    """Evaluation: an entry at -inf has no share in lse; a target at -inf costs inf; a row of nothing else has lse -inf and no loss."""
+    H, V = 64, 520
+    p = Problem(N, H, V, 1, 1, seed=N, mask=0.0)
+    h = p.hidden.float()
+    h[:, 0] = 0
+    h[1, 0], h[2, 0] = 1, 1
+    p.hidden = h.to(torch.bfloat16)
+    W = p.W[0].clone()
+    W[:, 0] = 0
+    p.W = [W]
+    p.gpu()
+    ctx = context(p, "ce")
+    base = call(ctx, p, "ce", grads="none")
+    # rows 1 and 2 see -inf at some entries (0 x inf would be NaN in the others, so they get a head of their own)
+    q = Problem(2, H, V, 1, 1, seed=N, mask=0.0)
+    q.hidden, q.target = p.hidden[1:3], torch.tensor([p.target[1], 11], dtype=torch.int32)
+    if int(q.target[0]) in (11, 300, 519):
+        q.target[0] = 12
+    q.weight = q.weight * 0 + 1
+    Wq = W.clone()
+    Wq[[11, 300, 519], 0] = float("-inf")
+    q.W = [Wq]
+    q.gpu()
+    g = call(ctx, q, "ce", grads="none")
+    ctx.check_status()
+    z = q.hidden.double() @ Wq.double().T
+    want = torch.logsumexp(z, 1)
+    got = g["lse"].double().cpu()
+    ez = (H / 16 + 2) * 2 * U * (q.hidden.double().abs() @ torch.where(torch.isinf(Wq), 0, Wq).double().abs().T).max(1).values
+    assert torch.all((got - want).abs() <= ez + 2.0 ** -17 + 2 * U * want.abs())
+    assert torch.isfinite(g["tok_loss"][0]) and float(g["tok_loss"][1]) == float("inf") and torch.all(torch.isfinite(base["lse"]))
+    q.d_W = [torch.where(torch.arange(H, device="cuda") == 0, float("-inf"), q.d_W[0].float()).to(torch.bfloat16)]
+    g = call(ctx, q, "ce", grads="none")
+    ctx.check_status()
+    assert torch.all(g["lse"] == float("-inf")) and torch.all(torch.isnan(g["tok_loss"])) and torch.all(torch.isnan(g["loss"]))
     ctx.close()
