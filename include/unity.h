@@ -422,7 +422,8 @@ int unity_ppo_loss_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_p
  * dL/dz is held in bf16 between the products, as in stage 3, but without its common factor inv_temperature / M_k: a gradient
  * entry is off by up to 2^-8 of the terms it sums (and a kept logit by up to 2^-10 octaves).
  * A workspace below unity_token_loss_workspace_bytes() may give other last digits, within the same bound: recomputed logits are
- * not rounded to steps, and up to 64 tokens the full workspace also holds what rounding to bf16 cut from dL/dz.
+ * not rounded to steps, and for up to 64 rows of a model, in a batch of up to 1024 tokens, the full workspace also holds what rounding
+ * to bf16 cut from dL/dz.
  * The tensor core's fp32 sums cut where they would round.  Logits are scaled up by 1e-9 H + 4e-8 of themselves, the mean of that
  * cut for products of both signs: a row's lse differs by that share (3.6e-6 at H = 3584) from the one of unity_logprob_fwd, which
  * leaves the cut in.  The worst case stays (H/16 + 2) 2^-23 of sum_j |h_j W_vj|.

@@ -155,7 +155,7 @@ k_few_rows_bwd(const __grid_constant__ CUtensorMap tmG, const __grid_constant__ 
             const uint32_t id_dh = ptx::idesc_bf16_f32(kRows, kCols) | (1u << 16);
             const uint32_t id_dw = ptx::idesc_bf16_f32(kChunk, kCols) | (1u << 15) | (1u << 16);
             // rows that hold tokens, or (low halves) all 128, in steps of 16; the rows behind them are not gradients
-            const int k_rows = a.low_rows > 0 ? kRows / 16 : (valid + kTileK - 1) / kTileK * (kTileK / 16);
+            const int k_rows = valid <= a.low_rows ? kRows / 16 : (valid + kTileK - 1) / kTileK * (kTileK / 16);
             bool ok = ptx::mbar_wait(hid_full, 0, a.wait_budget);
             int s = 0, t = 0;
             uint32_t phase = 0, phase_w = 0;

@@ -237,6 +237,7 @@ __device__ __noinline__ GemmArgs resolve_span(const GemmArgs& in, int k) {
     } else if (in.span_mode == kSpanRowsK) {
         if (in.alpha != nullptr) g.alpha = in.alpha + k;
         g.k_iters = (in.shapes ? span_slab_rows(span, n_rows) : n_rows) / kTileK;
+        if (in.low_rows > 0 && n_rows > 0 && in.span.plan->counts[k] <= in.low_rows) g.k_iters = 2 * in.low_rows / kTileK;
         g.b_k0 = in.b_k0 + slot0;
         if (in.stash_by_slot) g.a_k0 = slot0;
         if (in.split_rows) {

@@ -234,6 +234,7 @@ struct GemmArgs {
     int k_splits, k_per_split;   // the contraction is cut into k_splits parts of k_per_split slabs, each with an output of
     long long c_split;           // its own, c_split values apart (0 or 1: not cut)
     int split_rows;              // kSpanRowsK: the contraction over rows is cut as LossShapes::dw says
+    int low_rows;                // kSpanRowsK: of a model of at most low_rows tokens it takes 2 * low_rows rows (see LossGradArgs)
     const float* alpha;          // token losses' dW: each model's factor of its outputs (LossRowArgs::alpha); null: 1
     int zero_if_empty;           // a launch whose contraction has no rows writes zeros to its m_rows x ldc outputs
     int beta;                 // 0: overwrite, 1: add to C
@@ -435,6 +436,7 @@ cudaError_t launch_value_loss(const ValueArgs& a, cudaStream_t stream, int* n_la
 // Routing of a token loss with everything the later launches need: tokens to packed slots, the plan, the schedules, zeros for
 // masked tokens' outputs and for the call's counters.
 constexpr int kLossRouteTokens = 8192;
+constexpr int kLossPackTokens = 1024;    // ... in one launch with the packing
 constexpr int kLossCounters = 1024;
 struct LossRouteArgs {
     RouteArgs route;           // fwd: the forward planner's inputs
@@ -459,7 +461,7 @@ struct LossGatherArgs {
     const int* target;         // nullable
     __nv_bfloat16 *hp, *dHidden;   // dHidden nullable
     int* target_p;             // without targets: the list's likeliest entry, or -1
-    int low_rows;              // a model's first low_rows rows are packed twice (see LossGradArgs); 0: none
+    int low_rows;              // models of at most low_rows tokens have theirs packed twice, low_rows apart (see LossGradArgs); 0: none
     int n_top, logits;         // logits 1: softmax of the listed logits (times scale); 0: exp of listed log-probabilities
     float scale;
     const int* top_ids;        // caller order [n_tok, n_top]
@@ -527,14 +529,14 @@ struct LossGradArgs {
     int n_top;                 // the listed entries' gradients go in last (0: none)
     const int *ids_p, *cnt_p;
     const float* top_g;
-    int low_rows;              // > 0: row r + low_rows of the model takes what rounding to bf16 cut from row r
+    int low_rows;              // > 0: in models of at most low_rows tokens, row r + low_rows takes what rounding to bf16 cut from row r
 };
-// Up to 64 tokens half of the one 128-row tile is empty: it takes the gradients' low halves, and dHidden and dW come from 16
-// bits of dL/dz, for 2 to 4 % of the time.  (With few tokens a gradient row is hardly more than the target's entry times a row of W or of hidden,
-// and with token weights the rounding of that one entry does not average out: up to 3e-3 in the 2-norm where the output's own rounding is 1.7e-3.
-// From 65 to 128 tokens it would take a tile of 256 rows and 18-24 % of the time.)
-// Only where one block holds the rows and kept logits of all models: a workspace without room for that takes per-model blocks or
-// recomputed logits, whose dL/dz is single bf16.
+// Up to 64 tokens of a model leave half of a row tile empty: it takes the gradients' low halves, and the model's dHidden and dW come
+// from 16 bits of dL/dz, for 2 to 4 % of the time.  (With few tokens a gradient row is hardly more than the target's entry times a row of
+// W or of hidden, and with token weights the rounding of that one entry does not average out: up to 3.3e-3 in the 2-norm where the
+// output's own rounding is 1.7e-3.  From 65 tokens of a model on it would take a second row tile and 18-24 % of the time.)
+// Only where one block holds the rows and kept logits of all models, and only in batches that one launch routes and packs: a workspace
+// without room for that takes per-model blocks or recomputed logits, whose dL/dz is single bf16, and so do larger batches.
 constexpr int kLowTokens = 64;
 cudaError_t launch_loss_grad_inplace(const LossGradArgs& a, int sm_count, cudaStream_t stream);
 // dHidden[token of slot r of the span] = bf16(sum of the row's parts), in the order of the parts
@@ -546,7 +548,7 @@ struct StoreArgs {
     long long part_stride;
     const LossShapes* shapes;  // null: parts_n parts
     int parts_n;
-    int low_rows;              // > 0: row r + low_rows belongs to row r (see LossGradArgs)
+    int low_rows;              // > 0: in models of at most low_rows tokens, row r + low_rows belongs to row r (see LossGradArgs)
     const float* alpha;        // [K]
     long long bound;           // rows of the launch at most
     __nv_bfloat16* dHidden;

@@ -392,7 +392,6 @@ __global__ void __launch_bounds__(256) k_loss_gather(LossGatherArgs a) {
 
 // Up to kLossPackTokens tokens: routing and packing in one launch.  Every block routes all tokens for itself (a few memory
 // latencies, no waiting for another block); block 0 writes the result down and weighs the schedules while the others pack.
-constexpr int kLossPackTokens = 1024;
 __global__ void __launch_bounds__(256) k_loss_pack(LossRouteArgs r, LossGatherArgs a) {
     begin();
     __shared__ RouteShared<256> sh;
@@ -419,17 +418,19 @@ __global__ void __launch_bounds__(256) k_loss_pack(LossRouteArgs r, LossGatherAr
     const bool list = a.n_top > 0 && (w & 1);
     if (a.n_top > 0) w >>= 1;
     int tok = -1, first = 0, rel = 0;
+    bool low = false;                                          // the row's model has its rows twice
     for (int k = 0; k < r.route.K; ++k) {
         if (w >= sh.off[k] && w < sh.off[k + 1]) {
             rel = static_cast<int>(w) - sh.off[k];
             if (rel < sh.tot[k]) tok = sh_tok[first + rel];
+            low = sh.tot[k] <= a.low_rows;
         }
         first += sh.tot[k];
     }
     // (a row whose place the first rows' second copies take is left alone, but for its list and its token's zeros)
     int n_slots = sh.off[r.route.K];
-    if (!list && rel >= a.low_rows && rel < 2 * a.low_rows) n_slots = 0;
-    gather_row(a, w, list, n_slots, tok, w < n && sh_model[w] < 0, rel < a.low_rows, sh_id, sh_q);
+    if (!list && low && rel >= a.low_rows && rel < 2 * a.low_rows) n_slots = 0;
+    gather_row(a, w, list, n_slots, tok, w < n && sh_model[w] < 0, low && rel < a.low_rows, sh_id, sh_q);
 }
 
 // One warp per packed row: merge the vocabulary splits' statistics (one lane per split), then the row's loss and what
@@ -615,10 +616,12 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
     for (int item = blockIdx.x; item < rows * per_row; item += gridDim.x) {      // at most 18432 rows of 2^18 columns
         int r = item / per_row;
         const int c_lo = (item - r * per_row) * kGradCols, c_first = c_lo + threadIdx.x * 8;
+        bool low = false;                                      // the row's model has low halves
         if (joint) {
             int k = 0;
             while (r >= sh_rows[k]) r -= sh_rows[k++];
             valid = sh_valid[k] + sh_off[k];
+            low = LOW && sh_valid[k] <= a.low_rows;
             r += sh_off[k];
         }
         const int slot = row0 + r;
@@ -630,7 +633,7 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
                 const int c0 = c_first + u * 2048;
                 if (c0 >= a.cols) continue;
                 row[c0 >> 3] = make_uint4(0, 0, 0, 0);
-                if (LOW) low_row[c0 >> 3] = make_uint4(0, 0, 0, 0);
+                if (LOW && low) low_row[c0 >> 3] = make_uint4(0, 0, 0, 0);
             }
             continue;
         }
@@ -699,7 +702,7 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
                 }
             }
             row[c0 >> 3] = raw[u];
-            if (LOW) low_row[c0 >> 3] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+            if (LOW && low) low_row[c0 >> 3] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
         }
         if (a.n_top > 0) {                                     // the row's listed entries among this block's columns
             __syncthreads();
@@ -711,7 +714,7 @@ __global__ void __launch_bounds__(256, LOW ? 6 : 8) k_loss_grad_inplace(LossGrad
                 const float g = a.top_g[at + j];
                 const __nv_bfloat16 hi = __float2bfloat16_rn(g);
                 reinterpret_cast<__nv_bfloat16*>(row)[c_lo + c] = hi;
-                if (LOW) reinterpret_cast<__nv_bfloat16*>(low_row)[c_lo + c] = __float2bfloat16_rn(g - __bfloat162float(hi));
+                if (LOW && low) reinterpret_cast<__nv_bfloat16*>(low_row)[c_lo + c] = __float2bfloat16_rn(g - __bfloat162float(hi));
             }
         }
     }
@@ -763,7 +766,7 @@ __global__ void __launch_bounds__(256) k_store_parts(StoreArgs a) {
     const int splits = a.shapes ? a.shapes->dh[model][rows == a.span.row_cap ? 0 : 1].splits : a.parts_n;
     if (tok < 0) return;
     float4 v = sum_parts(parts + static_cast<long long>(r) * a.H + c, splits, static_cast<long long>(rows) * a.H);
-    if (a.low_rows > 0) {
+    if (a.low_rows > 0 && a.span.plan->counts[model] <= a.low_rows) {
         const float4 l = sum_parts(parts + static_cast<long long>(r + a.low_rows) * a.H + c, splits, static_cast<long long>(rows) * a.H);
         v.x += l.x; v.y += l.y; v.z += l.z; v.w += l.w;
     }

@@ -598,8 +598,8 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     int nl = 0, rc;
     // At most 128 rows: one row tile of a single CTA instead of a half empty one of a CTA pair, for every GEMM whose rows they
     // are (with 87 rows at H = 3584 the products then take less time than the heads' bytes)
-    // Up to 64 of them: a gradient's low halves take as many rows again (see LossGradArgs)
-    const int low_rows = B.joint && r->n_tok <= kLowTokens ? kLowTokens : 0;
+    // Up to 64 of a model: a gradient's low halves take as many rows again (see LossGradArgs)
+    const int low_rows = B.joint && r->n_tok <= kLossPackTokens ? kLowTokens : 0;
     const bool few = r->n_tok <= kCtaM;
     const int c_fwd = few ? 1 : ctx->ctas[UNITY_PROF_FWD_GEMM], c_grad = few ? 1 : ctx->ctas[UNITY_PROF_GRAD_GEMM],
               c_dh = few ? 1 : ctx->ctas[UNITY_PROF_DH_GEMM], c_dw = ctx->ctas[UNITY_PROF_DW_GEMM];
@@ -855,7 +855,7 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
                         memset(&w, 0, sizeof(w));
                         w.pdl = 1;
                         w.mma_n = part == 0 ? mma_n : narrow_n;
-                        w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = t1 - t0; w.shapes = low_rows > 0 ? nullptr : L.shapes; w.stash_by_slot = B.joint;
+                        w.span = chunk; w.span_mode = kSpanRowsK; w.m_tiles = t1 - t0; w.shapes = L.shapes; w.low_rows = low_rows; w.stash_by_slot = B.joint;
                         w.n_tiles = (H + (wide_here ? 2 : 1) * w.mma_n - 1) / ((wide_here ? 2 : 1) * w.mma_n); w.k_iters = 1;
                         w.group_m = ctx->chunk_group[2] / c_dw > 0 ? ctx->chunk_group[2] / c_dw : 1;
                         w.a_row0 = row0; w.m_rows = n_here; w.n_cols = H; w.ldc = H;

@@ -185,3 +185,47 @@ def test_logits_of_minus_infinity(N):
     ctx.check_status()
     assert torch.all(g["lse"] == float("-inf")) and torch.all(torch.isnan(g["tok_loss"])) and torch.all(torch.isnan(g["loss"]))
     ctx.close()
+
+
+@pytest.mark.parametrize("dw", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("H,V,cuts", [(64, 520, [30, 70]), (128, 264, [1, 64, 65]), (320, 2000, [10, 240, 50]), (1344, 20000, [5, 700]),
+                                      (64, 40000, [64, 200, 3]), (256, 1000, [2, 900, 40, 60, 0]), (576, 30000, [20, 100])])
+def test_models_of_few_rows_beside_others(H, V, cuts, op, dw):
+    """Up to 64 rows of a model take the low halves of dL/dz however many rows the other models have (in a batch of up to 1024): their
+    gradients are off by b^2 of G in place of b."""
+    N = sum(cuts)
+    p = Problem(N, H, V, len(cuts), len(cuts), n_inv=len(cuts), n_top=6, seed=N + V, mask=0.0)
+    p.cu = torch.from_numpy(np.concatenate([[0], np.cumsum(cuts)]))
+    p.inv_role = torch.arange(len(cuts), dtype=torch.int32)
+    p.gpu()
+    ctx = context(p, op)
+    o = oracle(p, op)
+    if N > 64:
+        few = np.asarray(cuts)[o["tok_model"]] <= 64
+        o["dG"][few] -= (B * (1 + B) - B * B) * np.abs(o["G"][few])
+    g = call(ctx, p, op, dw=dw)
+    ctx.check_status()
+    check(p, g, o)
+    again = call(ctx, p, op, dw=dw)
+    assert torch.equal(g["dHidden"], again["dHidden"]) and all(torch.equal(a, b) for a, b in zip(g["dW"], again["dW"]))
+    old = [torch.full((V, H), 0.5, device="cuda", dtype=dw) for _ in cuts]
+    check(p, call(ctx, p, op, accumulate=True, dW=old), o, base=[np.full((V, H), 0.5)] * len(cuts))
+    ctx.check_status()
+    ctx.close()
+
+
+@pytest.mark.parametrize("op", ["ce", "kd"])
+@pytest.mark.parametrize("N,H,V", [(100, 64, 520), (300, 1344, 30000), (1024, 128, 2000)])
+def test_batches_with_few_valid_rows(N, H, V, op):
+    """The same for a batch of which the mask leaves at most 64 rows."""
+    p = Problem(N, H, V, 1, 1, n_top=6, seed=N, mask=0.95)
+    assert 0 < int(p.mask.sum()) <= 64
+    p.gpu()
+    ctx = context(p, op)
+    o = oracle(p, op)
+    o["dG"] -= (B * (1 + B) - B * B) * np.abs(o["G"])
+    for dw in (torch.bfloat16, torch.float32):
+        check(p, call(ctx, p, op, dw=dw), o)
+    ctx.check_status()
+    ctx.close()
