@@ -325,8 +325,8 @@ __device__ __forceinline__ void store_b16_block(__nv_bfloat16* C16, long long ld
 //   s = sum over all columns but the target's of 2^((z - ref) c2), z2 = sum z (both as even / odd halves), the target's logit,
 //   and where the row stands in its ascending list of entries (next vocabulary index, INT_MAX: none left).
 // The target's own term is left out of s: a sure token's loss is log(1 + s / 2^((z_target - ref) c2)), whose digits are those of
-// s, where lse - z_target is a difference of two numbers near 20 (z_target = 20 over a background of 4096 logits near 0: off by up
-// to 35 % so, by 1e-5 now).  A target that is infinite or NaN stays in s, which then says so.
+// s, where lse - z_target is a difference of two numbers near 20 (z_target from 12 to 30 over 4104 logits within 2 of 0: off by
+// all of the loss at the upper end so, by less than 2.4e-5 of it everywhere now).  A target that is infinite or NaN stays in s, which then says so.
 // ref need not be the maximum: it is 0 where the first tile's maximum lies within kRefBelow octaves below and kRefRoom above
 // that, else that maximum, and later a tile's maximum more than kRefRoom octaves above it.  So a tile is read from tensor
 // memory once (a maximum first and the sum after it read it twice: 252 against 353 us at 801 x 896 x 151936), no sum exceeds
