@@ -189,7 +189,7 @@ def _prepare_clip(case, g, c):
     if own:
         from paper_2605_26646_b200 import binding as ub
         st["grads"] = ub.GradTensors(tensors, models, outs)
-        st["ctx"] = ub.Context(0, ub.unity_clip_grad_norm_workspace_bytes(K))
+        st["ctx"] = ub.Context(0, ub.unity_clip_grad_norm_workspace_bytes(len(tensors), K))
     return st
 
 
