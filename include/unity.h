@@ -477,6 +477,90 @@ int unity_distill_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_di
                           const int32_t* top_ids, const float* top_vals, const float* tok_weight, float* loss,
                           float* tok_loss, float* lse, void* dHidden, void* const* dW);
 
+/* ------------------------------------------------------------------------------------------------
+ * Around the update (no counterpart in the paper): the final norm that makes the hidden rows of stages 2 and 3 and takes their
+ * dHidden back, the clipping of a model's gradients, and the sampling of the answers whose log-probabilities stage 2 evaluates.
+ *
+ * RMS norm with the residual's addition.  Tokens are routed as in stages 2 and 3 (K final norms, one per model):
+ *   r_i = x_i + residual_i (fp32);  s_i = 1 / sqrt(mean_j r_ij^2 + eps);  y_ij = gamma_k[j] r_ij s_i
+ * and back, from dy (dHidden of the losses) and what else arrives on the residual stream (dres):
+ *   g = dy gamma_k;  dx = s g - r s^3 mean_j(g r) + dres;  dgamma_k = sum over the valid tokens of model k of dy r s
+ * dx is the gradient of x and of residual alike.  Sums are fp32, outputs are rounded once.  The backward takes r as it was kept.
+ *   x, y, dy   : bf16 [n_tok, H];  residual, res_out, res, dres, dx : bf16 or f32 [n_tok, H] (res_type for all of a call)
+ *   residual   : NULL: r = x (and res_out must be NULL);  res_out : out, r rounded to res_type, or NULL
+ *   res        : r, as res_out has it (or x, in bf16, where there was no residual);  dres : or NULL
+ *   dgamma     : (host) K different device pointers, each f32 [H], or NULL (a frozen norm); accumulate: 1 adds to them
+ * Limits: H % 64 == 0, 64 <= H <= UNITY_MAX_NORM_H; rows densely packed, every pointer 16-byte aligned.  y may be x, res_out may be
+ * residual, dx may be res, dres or (bf16) dy; other overlaps are not allowed.  The sum of a row's squares must lie within fp32.
+ * Rows with tok_mask == 0 are not read and have zeros in y, res_out and dx; an out-of-range role flags UNITY_ERR_BAD_INDEX and its
+ * tokens count as masked.  The forward needs no workspace, the backward with dgamma unity_rms_norm_workspace_bytes(), with less it
+ * runs on fewer blocks (other last digits of dgamma).  Deterministic: every sum has a fixed order. */
+#define UNITY_MAX_NORM_H 16384
+typedef struct {
+    int64_t n_tok;
+    int32_t H, K, n_inv, n_roles;
+    const int64_t* cu_seqlens;   /* int64 [n_inv+1]                                             */
+    const int32_t* inv_role;     /* int32 [n_inv]                                               */
+    const int32_t* role_model;   /* (host) int32 [n_roles], values in [0, K)                    */
+    const uint8_t* tok_mask;     /* u8 [n_tok] or NULL (= all 1)                                */
+    const void* const* gamma;    /* (host) K device pointers, each [H] of gamma_type            */
+    int gamma_type;              /* UNITY_F32 or UNITY_BF16                                     */
+    float eps;                   /* >= 0                                                        */
+} unity_norm_rows;
+size_t unity_rms_norm_workspace_bytes(int64_t n_tok, int32_t H, int32_t K);
+int unity_rms_norm_fwd(unity_ctx* ctx, const unity_norm_rows* rows, const void* x, const void* residual, int res_type,
+                       void* y, void* res_out);
+int unity_rms_norm_bwd(unity_ctx* ctx, const unity_norm_rows* rows, const void* res, int res_type, const void* dy,
+                       const void* dres, void* dx, float* const* dgamma, int accumulate);
+
+/* Global gradient norm of each model over a list of tensors, and clipping - each worker group updates its own model, so norms and
+ * bounds are per model:
+ *   norm[k] = sqrt(sum over the tensors of model k of their squares);  coef[k] = norm[k] <= max_norm[k] ? 1 : max_norm[k] / norm[k]
+ *   out = coef[k] * data, in place or to another tensor (dW in f32 to an optimizer's bf16, say)
+ *   tensors  : (host) [n_tensors]; any of them may be empty.  What is written may not overlap any other tensor of the list
+ *   max_norm : (host) f32 [K], >= 0, inf = no bound; NULL: norms only (out is not written)
+ *   norm     : out f32 [K] (0 for a model without tensors);  coef : out f32 [K] or NULL
+ * In place, a model within its bound is not written at all.  A norm that is not finite makes coef 0 or NaN and the outputs
+ * accordingly: a caller who skips such a step looks at norm first.  Squares are added in fp64 (in fp32 within eight elements where that
+ * loses nothing), in a fixed order: neither 1e-30 nor 1e30 underflows or overflows.
+ * Tensors need the alignment of their elements only.  Workspace: unity_clip_grad_norm_workspace_bytes(). */
+typedef struct {
+    void* data;
+    void* out;          /* NULL: in place */
+    int64_t n;          /* elements, >= 0 */
+    int32_t model;      /* 0 .. K-1 */
+    int16_t type;       /* of data: UNITY_F32 or UNITY_BF16 */
+    int16_t out_type;   /* of out (not read in place): that of data, or UNITY_BF16 */
+} unity_tensor;
+size_t unity_clip_grad_norm_workspace_bytes(int32_t n_tensors, int32_t K);
+int unity_clip_grad_norm(unity_ctx* ctx, int32_t n_tensors, const unity_tensor* tensors, int32_t K, const float* max_norm,
+                         float* norm, float* coef);
+
+/* Sampling of next tokens from logits, one row per running answer, with a rule per role and one uniform number per row.  The entries
+ * are ordered by falling logit, equal ones by rising index; with z / T as logits of the probabilities p, an entry is
+ *   allowed if it is above -inf, its rank is below top_k (top_k <= 0: off) and p >= min_p * max p (min_p = 0: off),
+ *   kept    if it is allowed and the allowed mass before it is < top_p * the whole allowed mass (top_p = 1: off).
+ * token = the first kept index, ascending, whose running kept mass is > u * the kept mass.  T = 0 keeps the largest logit alone.
+ *   logits   : f32 or bf16 [n_rows, V], row pitch ld >= V elements;  V <= UNITY_MAX_SAMPLE_V;  any alignment of the type
+ *   row_role : int32 [n_rows] or NULL (all role 0);  rules : (host) [n_roles];  row_mask : u8 [n_rows] or NULL
+ *   u        : f32 [n_rows] in [0, 1)
+ *   token    : out int32 [n_rows];  logp : log p of the token over all V entries at T (at T = 1 where T = 0), which is what
+ *              unity_logprob_fwd gives for inv_temperature = 1 / T;  logp_kept : the same among the kept entries
+ *   n_kept   : number of kept entries;  logp, logp_kept, n_kept may be NULL
+ * Rows with row_mask == 0 (answers that are finished) get token -1 and 0 elsewhere, and their logits are not read; so do rows with a
+ * role out of range or u outside [0, 1), which flag UNITY_ERR_BAD_INDEX.  Rows with a NaN or +inf, or with nothing above -inf, get
+ * token -1, n_kept 0 and NaN elsewhere.  Tokens and n_kept are those of 64-bit arithmetic; bitwise reproducible.  No workspace. */
+#define UNITY_MAX_SAMPLE_V 262144
+typedef struct {
+    float temperature;  /* 0, or 1e-6 .. 1e6 */
+    int32_t top_k;
+    float top_p;        /* (0, 1] */
+    float min_p;        /* [0, 1] */
+} unity_sampling_rule;
+int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, int logits_type, int64_t ld, int32_t n_roles,
+                 const int32_t* row_role, const unity_sampling_rule* rules, const uint8_t* row_mask, const float* u,
+                 int32_t* token, float* logp, float* logp_kept, int32_t* n_kept);
+
 #ifdef __cplusplus
 }
 #endif

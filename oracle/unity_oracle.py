@@ -602,3 +602,89 @@ def token_loss_fwd_bwd(hidden, W, cu_seqlens, inv_role, role_model, target, tok_
             loss[k] = (w[i] * l[i]).sum() / M[k]
         dW.append(G[i].T @ h)
     return dict(loss=loss, tok_loss=l, lse=lse, dHidden=dH, dW=dW, G=G, M=np.array(M), tok_model=tok_model, on=on)
+
+
+# ------------------------------------------------------------------------------------------------
+# Around the update: final norm, gradient clipping, sampling (definitions of include/unity.h, float64)
+# ------------------------------------------------------------------------------------------------
+def _norm_tokens(cu_seqlens, inv_role, role_model, tok_mask):
+    """(model of each token, whether it counts): a role out of range counts as masked."""
+    tok_inv = token_invocation(np.asarray(cu_seqlens, dtype=np.int64))
+    role = np.asarray(inv_role)[tok_inv]
+    known = (role >= 0) & (role < len(role_model))
+    model = np.asarray(role_model)[np.where(known, role, 0)]
+    on = known if tok_mask is None else known & (np.asarray(tok_mask) != 0)
+    return model, on
+
+
+def rms_norm_fwd(x, residual, gamma, cu_seqlens, inv_role, role_model, tok_mask=None, eps=1e-6):
+    """y and r [n_tok, H]; zeros on rows that do not count."""
+    model, on = _norm_tokens(cu_seqlens, inv_role, role_model, tok_mask)
+    r = to_f64(x) if residual is None else to_f64(x) + to_f64(residual)
+    r = np.where(on[:, None], r, 0.0)
+    y = np.zeros_like(r)
+    for i in np.nonzero(on)[0]:
+        y[i] = to_f64(gamma[model[i]]) * r[i] / np.sqrt(np.mean(r[i] ** 2) + eps)
+    return y, r
+
+
+def rms_norm_bwd(r, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps, dy, dres=None):
+    """dx [n_tok, H], dgamma [K, H], and the sums of magnitudes that bound a rounding's effect on either."""
+    model, on = _norm_tokens(cu_seqlens, inv_role, role_model, tok_mask)
+    r, dy = to_f64(r), to_f64(dy)
+    dx, dg = np.zeros_like(r), np.zeros((len(gamma), r.shape[1]))
+    mag_x, mag_g = np.zeros_like(r), np.zeros_like(dg)
+    for i in np.nonzero(on)[0]:
+        s = 1.0 / np.sqrt(np.mean(r[i] ** 2) + eps)
+        g = dy[i] * to_f64(gamma[model[i]])
+        dx[i] = s * g - r[i] * s ** 3 * np.mean(g * r[i])
+        mag_x[i] = np.abs(s * g) + np.abs(r[i]) * s ** 3 * np.mean(np.abs(g * r[i]))
+        if dres is not None:
+            dx[i] += to_f64(dres)[i]
+            mag_x[i] += np.abs(to_f64(dres)[i])
+        dg[model[i]] += dy[i] * r[i] * s
+        mag_g[model[i]] += np.abs(dy[i] * r[i] * s)
+    return dx, dg, mag_x, mag_g
+
+
+def clip_grad_norm(grads, models, K, max_norm=None):
+    """norm [K], coef [K] and the scaled gradients."""
+    sq = [0.0] * K
+    for g, k in zip(grads, models):
+        sq[k] += float(np.sum(to_f64(g).ravel() ** 2))
+    norm = np.sqrt(np.array(sq))
+    coef = np.ones(K)
+    if max_norm is not None:
+        for k in range(K):
+            if norm[k] > float(np.float32(max_norm[k])):
+                coef[k] = float(np.float32(max_norm[k])) / norm[k]
+    return norm, coef, [coef[k] * to_f64(g) for g, k in zip(grads, models)]
+
+
+def sample_row(z, temperature, top_k, top_p, min_p, u):
+    """(token, logp, logp among the kept, number kept) of one row of logits; the rule's numbers and u are taken as fp32."""
+    z = to_f64(z)
+    T, top_p, min_p, u = (float(np.float32(v)) for v in (temperature, top_p, min_p, u))
+    if np.isnan(z).any() or z.max() == np.inf or z.max() == -np.inf:
+        return -1, np.nan, np.nan, 0
+    x = (z - z.max()) / (T if T > 0 else 1.0)
+    e = np.exp(x)
+    order = np.argsort(-z, kind="stable")
+    order = order[z[order] > -np.inf]
+    if T == 0:
+        order = order[:1]
+    else:
+        if top_k > 0:
+            order = order[:top_k]
+        if min_p > 0:
+            order = order[x[order] >= np.log(min_p)]
+        if top_p < 1:
+            run = np.cumsum(e[order])
+            before = np.concatenate([[0.0], run[:-1]])
+            order = order[before < top_p * run[-1]]
+    kept = np.sort(order)
+    run = np.cumsum(e[kept])
+    past = np.nonzero(run > u * run[-1])[0]
+    j = int(past[0]) if past.size else int(np.nonzero(e[kept] > 0)[0][-1])
+    t = int(kept[j])
+    return t, x[t] - np.log(e.sum()), x[t] - np.log(run[-1]), int(kept.size)

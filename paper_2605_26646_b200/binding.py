@@ -30,7 +30,9 @@ EXPORTS = ["unity_create", "unity_destroy", "unity_workspace_hint", "unity_works
            "unity_ready_batch_plan", "unity_ready_batch_gather", "unity_align_rewards",
            "unity_role_advantage_noalloc",
            "unity_logprob_fwd", "unity_ppo_loss_fwd_bwd",
-           "unity_token_loss_workspace_bytes", "unity_cross_entropy_fwd_bwd", "unity_distill_fwd_bwd"]
+           "unity_token_loss_workspace_bytes", "unity_cross_entropy_fwd_bwd", "unity_distill_fwd_bwd",
+           "unity_rms_norm_workspace_bytes", "unity_rms_norm_fwd", "unity_rms_norm_bwd",
+           "unity_clip_grad_norm_workspace_bytes", "unity_clip_grad_norm", "unity_sample"]
 
 
 class UnityError(RuntimeError):
@@ -73,6 +75,21 @@ class unity_ce_params(C.Structure):
 class unity_distill_params(C.Structure):
     _fields_ = [("n_top", C.c_int32), ("teacher_mode", C.c_int), ("kd_coef", C.c_float), ("hard_coef", C.c_float),
                 ("norm", C.POINTER(C.c_float)), ("accumulate_dW", C.c_int), ("dW_type", C.c_int)]
+
+
+class unity_norm_rows(C.Structure):
+    _fields_ = [("n_tok", C.c_int64), ("H", C.c_int32), ("K", C.c_int32), ("n_inv", C.c_int32), ("n_roles", C.c_int32),
+                ("cu_seqlens", C.c_void_p), ("inv_role", C.c_void_p), ("role_model", C.POINTER(C.c_int32)),
+                ("tok_mask", C.c_void_p), ("gamma", C.POINTER(C.c_void_p)), ("gamma_type", C.c_int), ("eps", C.c_float)]
+
+
+class unity_tensor(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("model", C.c_int32), ("type", C.c_int16),
+                ("out_type", C.c_int16)]
+
+
+class unity_sampling_rule(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float)]
 
 
 _LIB = None
@@ -149,6 +166,19 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.unity_distill_fwd_bwd.argtypes = [vp, C.POINTER(unity_rows), C.POINTER(unity_distill_params), vp, vp, vp, vp, vp,
                                           vp, vp, C.POINTER(vp)]
     lib.unity_distill_fwd_bwd.restype = C.c_int
+    lib.unity_rms_norm_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.unity_rms_norm_workspace_bytes.restype = C.c_size_t
+    lib.unity_rms_norm_fwd.argtypes = [vp, C.POINTER(unity_norm_rows), vp, vp, C.c_int, vp, vp]
+    lib.unity_rms_norm_fwd.restype = C.c_int
+    lib.unity_rms_norm_bwd.argtypes = [vp, C.POINTER(unity_norm_rows), vp, C.c_int, vp, vp, vp, C.POINTER(vp), C.c_int]
+    lib.unity_rms_norm_bwd.restype = C.c_int
+    lib.unity_clip_grad_norm_workspace_bytes.argtypes = [i32, i32]
+    lib.unity_clip_grad_norm_workspace_bytes.restype = C.c_size_t
+    lib.unity_clip_grad_norm.argtypes = [vp, i32, C.POINTER(unity_tensor), i32, f32p, vp, vp]
+    lib.unity_clip_grad_norm.restype = C.c_int
+    lib.unity_sample.argtypes = [vp, i32, i32, vp, C.c_int, i64, i32, vp, C.POINTER(unity_sampling_rule), vp, vp, vp, vp, vp,
+                                 vp]
+    lib.unity_sample.restype = C.c_int
     if path == _build.LIB_PATH:
         _LIB = lib
     return lib
@@ -447,7 +477,7 @@ def _sized(t: Optional[torch.Tensor], shape, dtype, device, name) -> Optional[in
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
     if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, hidden on {device}")
+        raise ValueError(f"{name} is on {t.device}, the call on {device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
@@ -524,6 +554,133 @@ def unity_distill_fwd_bwd(ctx, hidden, W, cu_seqlens, inv_role, role_model, targ
 
 
 # ------------------------------------------------------------------------------------------------
+# around the update: final norm, gradient clipping, sampling
+# ------------------------------------------------------------------------------------------------
+def unity_rms_norm_workspace_bytes(n_tok: int, H: int, K: int) -> int:
+    return int(load_library().unity_rms_norm_workspace_bytes(n_tok, H, K))
+
+
+def unity_clip_grad_norm_workspace_bytes(n_tensors: int, K: int) -> int:
+    return int(load_library().unity_clip_grad_norm_workspace_bytes(n_tensors, K))
+
+
+_TYPES = {torch.float32: UNITY_F32, torch.bfloat16: UNITY_BF16}
+
+
+def _type_of(t: torch.Tensor, name) -> int:
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{name}: expected float32 or bfloat16, got {t.dtype}")
+    return _TYPES[t.dtype]
+
+
+def _norm_rows(x, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps):
+    if x.dim() != 2 or not gamma or inv_role.dim() != 1:
+        raise ValueError("token rows must be [n_tok, H], gamma a non-empty sequence of [H] and inv_role [n_inv]")
+    if not x.is_cuda:
+        raise ValueError("token rows must be a CUDA tensor")
+    n_tok, H = x.shape
+    dev, n_inv, kind = x.device, inv_role.shape[0], gamma[0].dtype
+    gtype = _type_of(gamma[0], "gamma")
+    gp = (C.c_void_p * len(gamma))(*[_sized(g, (H,), kind, dev, "gamma") for g in gamma])
+    rm = (C.c_int32 * len(role_model))(*[int(r) for r in role_model])
+    return unity_norm_rows(n_tok, H, len(gamma), n_inv, len(role_model),
+                           _sized(cu_seqlens, (n_inv + 1,), torch.int64, dev, "cu_seqlens"),
+                           _sized(inv_role, (n_inv,), torch.int32, dev, "inv_role"), rm,
+                           _sized(tok_mask, (n_tok,), torch.uint8, dev, "tok_mask"), gp, gtype, float(eps))
+
+
+def unity_rms_norm_fwd(ctx, x, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps: float, y, residual=None,
+                       res_out=None) -> None:
+    """x, y: bf16 [n_tok, H]; gamma: K tensors [H], all f32 or all bf16; residual, res_out: f32 or bf16 [n_tok, H]."""
+    rows = _norm_rows(x, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
+    b16, dev = torch.bfloat16, x.device
+    rtype = UNITY_BF16 if residual is None else _type_of(residual, "residual")
+    kind = b16 if residual is None else residual.dtype
+    if y is None:
+        raise ValueError("y is None")
+    _raise(ctx, load_library().unity_rms_norm_fwd(
+        ctx, C.byref(rows), _sized(x, x.shape, b16, dev, "x"), _sized(residual, x.shape, kind, dev, "residual"), rtype,
+        _sized(y, x.shape, b16, dev, "y"), _sized(res_out, x.shape, kind, dev, "res_out")))
+
+
+def unity_rms_norm_bwd(ctx, res, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps: float, dy, dx, dres=None,
+                       dgamma=None, accumulate_dgamma: bool = False) -> None:
+    """res, dres, dx: all f32 or all bf16 [n_tok, H]; dy: bf16; dgamma: K f32 tensors [H], or None for a frozen norm."""
+    rows = _norm_rows(res, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
+    dev, rtype = res.device, _type_of(res, "res")
+    if dy is None or dx is None:
+        raise ValueError("dy / dx is None")
+    dg = None
+    if dgamma is not None:
+        if len(dgamma) != len(gamma):
+            raise ValueError(f"dgamma: expected {len(gamma)} tensors, got {len(dgamma)}")
+        dg = (C.c_void_p * len(dgamma))(*[_sized(g, (res.shape[1],), torch.float32, dev, "dgamma") for g in dgamma])
+    _raise(ctx, load_library().unity_rms_norm_bwd(
+        ctx, C.byref(rows), _sized(res, res.shape, res.dtype, dev, "res"), rtype,
+        _sized(dy, res.shape, torch.bfloat16, dev, "dy"), _sized(dres, res.shape, res.dtype, dev, "dres"),
+        _sized(dx, res.shape, res.dtype, dev, "dx"), dg, 1 if accumulate_dgamma else 0))
+
+
+class GradTensors:
+    """The tensors of a clipping call, checked and laid out once: gradients usually stay where they are from step to step.
+
+    grads: contiguous f32 or bf16 CUDA tensors of any shape; models: the model of each; outs: tensors that take the scaled
+    gradients (of the same type or bf16, None for in place), or None for all in place.  Keeps the tensors alive."""
+
+    def __init__(self, grads: Sequence[torch.Tensor], models: Sequence[int], outs: Optional[Sequence[Optional[torch.Tensor]]] = None):
+        self.grads, self.outs = list(grads), [None] * len(grads) if outs is None else list(outs)
+        models = [int(m) for m in models]
+        if len(models) != len(self.grads) or len(self.outs) != len(self.grads):
+            raise ValueError("grads, models and outs must have the same length")
+        self.device = self.grads[0].device if self.grads else None
+        self.array = (unity_tensor * len(models))()
+        for e, g, o, m in zip(self.array, self.grads, self.outs, models):
+            e.type = _type_of(g, "grads")
+            e.data, e.n, e.model = _sized(g, g.shape, g.dtype, self.device, "grads"), g.numel(), m
+            if o is not None:
+                e.out_type = _type_of(o, "outs")
+                e.out = _sized(o, g.shape, o.dtype, self.device, "outs")
+            if not g.is_cuda:
+                raise ValueError("grads must be CUDA tensors")
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def unity_clip_grad_norm(ctx, tensors: GradTensors, max_norm: Optional[Sequence[float]], norm, coef=None) -> None:
+    """norm, coef: f32 CUDA tensors [K]; max_norm: K bounds (inf: none), or None to compute the norms only."""
+    K = norm.shape[0]
+    if max_norm is not None and len(max_norm) != K:
+        raise ValueError(f"max_norm: expected {K} values, got {len(max_norm)}")
+    bounds = None if max_norm is None else (C.c_float * K)(*[float(x) for x in max_norm])
+    dev = norm.device if tensors.device is None else tensors.device
+    if not norm.is_cuda:
+        raise ValueError("norm must be a CUDA tensor")
+    _raise(ctx, load_library().unity_clip_grad_norm(ctx, len(tensors), tensors.array, K, bounds,
+                                                    _sized(norm, (K,), torch.float32, dev, "norm"),
+                                                    _sized(coef, (K,), torch.float32, dev, "coef")))
+
+
+def unity_sample(ctx, logits, rules, u, token, row_role=None, row_mask=None, logp=None, logp_kept=None, n_kept=None) -> None:
+    """logits: f32 or bf16 [n_rows, V], rows of any pitch; rules: (temperature, top_k, top_p, min_p) of each role."""
+    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be [n_rows, V] with consecutive entries in a row")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a CUDA tensor")
+    if u is None or token is None:
+        raise ValueError("u / token is None")
+    n, V = logits.shape
+    ld = logits.stride(0) if n > 1 else V
+    dev, f32, i32, per = logits.device, torch.float32, torch.int32, (n,)
+    arr = (unity_sampling_rule * len(rules))(*[unity_sampling_rule(float(t), int(k), float(p), float(m)) for t, k, p, m in rules])
+    _raise(ctx, load_library().unity_sample(
+        ctx, n, V, logits.data_ptr(), _type_of(logits, "logits"), ld, len(rules), _sized(row_role, per, i32, dev, "row_role"),
+        arr, _sized(row_mask, per, torch.uint8, dev, "row_mask"), _sized(u, per, f32, dev, "u"),
+        _sized(token, per, i32, dev, "token"), _sized(logp, per, f32, dev, "logp"),
+        _sized(logp_kept, per, f32, dev, "logp_kept"), _sized(n_kept, per, i32, dev, "n_kept")))
+
+
+# ------------------------------------------------------------------------------------------------
 class Context:
     """Owns a workspace tensor and a unity_ctx bound to a torch stream."""
 
@@ -589,9 +746,9 @@ class Context:
     def ppo_loss_fwd_bwd(self, *a, **kw):
         return unity_ppo_loss_fwd_bwd(self.ctx, *a, **kw)
 
-    def _on_device(self, hidden):
+    def _on_device(self, hidden, name="hidden"):
         if hidden.is_cuda and hidden.device.index != self.device:
-            raise ValueError(f"hidden is on {hidden.device}, the context on cuda:{self.device}")
+            raise ValueError(f"{name} is on {hidden.device}, the context on cuda:{self.device}")
 
     def cross_entropy_fwd_bwd(self, hidden, *a, **kw):
         self._on_device(hidden)
@@ -600,3 +757,19 @@ class Context:
     def distill_fwd_bwd(self, hidden, *a, **kw):
         self._on_device(hidden)
         return unity_distill_fwd_bwd(self.ctx, hidden, *a, **kw)
+
+    def rms_norm_fwd(self, x, *a, **kw):
+        self._on_device(x, "x")
+        return unity_rms_norm_fwd(self.ctx, x, *a, **kw)
+
+    def rms_norm_bwd(self, res, *a, **kw):
+        self._on_device(res, "res")
+        return unity_rms_norm_bwd(self.ctx, res, *a, **kw)
+
+    def clip_grad_norm(self, tensors, max_norm, norm, *a, **kw):
+        self._on_device(norm, "norm")
+        return unity_clip_grad_norm(self.ctx, tensors, max_norm, norm, *a, **kw)
+
+    def sample(self, logits, *a, **kw):
+        self._on_device(logits, "logits")
+        return unity_sample(self.ctx, logits, *a, **kw)

@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libunity.so")
 SOURCES = ["unity_api.cu", "stream_kernels.cu", "gemm_tcgen05.cu", "batch_kernels.cu",
            "noalloc_advantage.cu", "token_loss.cu",
-           "few_rows_tcgen05.cu"]
+           "few_rows_tcgen05.cu", "norm.cu", "clip.cu", "sample.cu"]
 HEADERS = ["internal.h", "ptx.cuh", os.path.join("..", "..", "include", "unity.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "--use_fast_math=false"]

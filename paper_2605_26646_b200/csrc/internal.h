@@ -636,4 +636,84 @@ cudaError_t launch_batch_gather(const GatherArgs& g, cudaStream_t stream);
 cudaError_t launch_align_rewards(int n_inv, const int64_t* cu, const uint8_t* mask, const float* r_inv,
                                  float* tok_reward, cudaStream_t stream);
 
+// ----------------------------------------------------------------------------------------------
+// RMS norm of token rows (norm.cu)
+// ----------------------------------------------------------------------------------------------
+struct NormArgs {
+    long long n_tok;
+    int H, K, n_inv, n_roles;
+    const int64_t* cu_seqlens;
+    const int32_t* inv_role;
+    const uint8_t* tok_mask;
+    int role_model[UNITY_MAX_ROLES];
+    const void* gamma[UNITY_MAX_MODELS];
+    int gamma_bf16, res_bf16;
+    float eps;
+    const __nv_bfloat16* x;              // forward
+    const void* residual;                // null: r = x
+    __nv_bfloat16* y;
+    void* res_out;                       // nullable
+    const void* res;                     // backward
+    const __nv_bfloat16* dy;
+    const void* dres;                    // nullable
+    void* dx;
+    float* dgamma[UNITY_MAX_MODELS];
+    int accumulate;
+    float* parts;                        // [blocks][K][H], null without dgamma
+    unsigned* touched;                   // [blocks]: bit k: the block wrote its slice of model k
+    int* status;
+};
+cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t stream);
+int norm_bwd_blocks(long long n_tok);
+cudaError_t launch_norm_bwd(const NormArgs& a, int blocks, cudaStream_t stream, int* n_launches);
+
+// ----------------------------------------------------------------------------------------------
+// Gradient norm and clipping (clip.cu)
+// ----------------------------------------------------------------------------------------------
+struct ClipEntry {
+    const void* src;
+    void* dst;                           // = src where it is scaled in place
+    long long n;
+    long long chunk0;                    // chunks of the entries before it in the launch
+    int model;
+    short src_bf16, dst_bf16;
+};
+constexpr int kClipBlocks = 148 * 4;     // blocks of a launch at most: a double per model of each in the workspace
+constexpr int kClipEntries = 800;        // entries of a launch at most: 32 000 bytes of parameters
+long long clip_chunks(const ClipEntry& e);
+struct ClipArgs {
+    double* partial;                     // [launches][kClipBlocks][K]
+    int K, n_launches, write;            // write: there is something to scale
+    int has_max;
+    float max_norm[UNITY_MAX_MODELS];
+    float *norm, *coef;                  // coef nullable
+};
+// entries [n] with their chunk0 set; the launch's partial sums go to slot `launch`
+cudaError_t launch_grad_squares(const ClipArgs& a, const ClipEntry* entries, int n, long long chunks, int launch, cudaStream_t stream);
+cudaError_t launch_grad_scale(const ClipArgs& a, const ClipEntry* entries, int n, long long chunks, int launch, cudaStream_t stream);
+
+// ----------------------------------------------------------------------------------------------
+// Sampling (sample.cu)
+// ----------------------------------------------------------------------------------------------
+struct SampleRule {
+    float temperature;                   // 0: the largest logit
+    int top_k;                           // 0: off
+    double inv_t, log_min_p;             // -inf: off
+    double top_p;                        // >= 1: off
+};
+struct SampleArgs {
+    const void* logits;
+    long long ld;
+    int n_rows, V, n_roles;
+    const int32_t* row_role;
+    const uint8_t* row_mask;
+    const float* u;
+    int32_t* token;
+    float *logp, *logp_kept;
+    int32_t* n_kept;
+    int* status;
+    SampleRule rules[UNITY_MAX_ROLES];
+};
+cudaError_t launch_sample(const SampleArgs& a, bool bf16, cudaStream_t stream);
+
 }  // namespace unity

@@ -1,7 +1,10 @@
 // C ABI of libunity: argument validation, workspace carving and the launch sequence of each call.
 // All arithmetic of the path runs in the kernels of stream_kernels.cu and gemm_tcgen05.cu.
+#include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -908,6 +911,95 @@ int token_loss(unity_ctx* ctx, const unity_rows* r, const LossCall& c) {
     return UNITY_OK;
 }
 
+// ------------------------------------------------------------------------------------------------
+// RMS norm and clipping
+// ------------------------------------------------------------------------------------------------
+bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+
+struct NormLayout { float* parts; unsigned* touched; size_t bytes; };
+NormLayout carve_norm(char* base, size_t cap, int H, int K, int blocks, bool* fits) {
+    NormLayout L;
+    Bump b{base, 0, cap, true};
+    L.touched = b.take<unsigned>(blocks);
+    L.parts = b.take<float>(static_cast<size_t>(blocks) * K * H);
+    L.bytes = up(b.off, kAlign);
+    if (fits) *fits = b.ok;
+    return L;
+}
+
+// Checks of what both directions take, and the arguments that follow from it.
+int norm_args(unity_ctx* ctx, const unity_norm_rows* r, int res_type, NormArgs& a) {
+    if (!ctx) return UNITY_ERR_INVALID_ARG;
+    if (!r) return fail(ctx, UNITY_ERR_INVALID_ARG, "rows is NULL");
+    if (r->n_tok < 0 || r->n_inv < 0) return fail(ctx, UNITY_ERR_INVALID_ARG, "negative size");
+    if (r->n_tok > 0x7fffff00LL) return fail(ctx, UNITY_ERR_SHAPE, "n_tok too large");
+    if (r->K < 1 || r->K > UNITY_MAX_MODELS) return fail(ctx, UNITY_ERR_SHAPE, "K=%d outside [1,%d]", r->K, UNITY_MAX_MODELS);
+    if (r->n_roles < 1 || r->n_roles > UNITY_MAX_ROLES) return fail(ctx, UNITY_ERR_SHAPE, "n_roles=%d outside [1,%d]", r->n_roles, UNITY_MAX_ROLES);
+    if (r->H < 64 || r->H % 64 != 0 || r->H > UNITY_MAX_NORM_H)
+        return fail(ctx, UNITY_ERR_SHAPE, "H=%d must be a multiple of 64 in [64,%d]", r->H, UNITY_MAX_NORM_H);
+    if (!(r->eps >= 0.f && r->eps <= 3.0e38f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "eps must be >= 0 and finite");
+    if ((r->gamma_type != UNITY_F32 && r->gamma_type != UNITY_BF16) || (res_type != UNITY_F32 && res_type != UNITY_BF16))
+        return fail(ctx, UNITY_ERR_INVALID_ARG, "gamma_type and res_type must be UNITY_F32 or UNITY_BF16");
+    if (!r->gamma || !r->role_model) return fail(ctx, UNITY_ERR_INVALID_ARG, "gamma / role_model is NULL");
+    if (r->n_tok > 0 && (!r->cu_seqlens || !r->inv_role || r->n_inv < 1))
+        return fail(ctx, UNITY_ERR_INVALID_ARG, "cu_seqlens / inv_role is NULL or n_inv < 1");
+    memset(&a, 0, sizeof(a));
+    for (int k = 0; k < r->K; ++k) {
+        if (!r->gamma[k]) return fail(ctx, UNITY_ERR_INVALID_ARG, "gamma[%d] is NULL", k);
+        if (misaligned(r->gamma[k])) return fail(ctx, UNITY_ERR_ALIGNMENT, "gamma[%d] not 16-byte aligned", k);
+        a.gamma[k] = r->gamma[k];
+    }
+    for (int v = 0; v < r->n_roles; ++v) {
+        if (r->role_model[v] < 0 || r->role_model[v] >= r->K)
+            return fail(ctx, UNITY_ERR_INVALID_ARG, "role_model[%d]=%d outside [0,%d)", v, r->role_model[v], r->K);
+        a.role_model[v] = r->role_model[v];
+    }
+    a.n_tok = r->n_tok; a.H = r->H; a.K = r->K; a.n_inv = r->n_inv; a.n_roles = r->n_roles;
+    a.cu_seqlens = r->cu_seqlens; a.inv_role = r->inv_role; a.tok_mask = r->tok_mask;
+    a.gamma_bf16 = r->gamma_type == UNITY_BF16; a.res_bf16 = res_type == UNITY_BF16; a.eps = r->eps; a.status = ctx->d_status;
+    return UNITY_OK;
+}
+
+// Memory that a clipping call reads or writes; `w`: writes.
+struct ClipRange { uintptr_t from, to; int tensor; bool w; };
+int clip_check(unity_ctx* ctx, int n, const unity_tensor* t, int K, bool scale) {
+    int m = 0;
+    for (int i = 0; i < n; ++i) {
+        if (t[i].n < 0 || t[i].n > (1LL << 44)) return fail(ctx, UNITY_ERR_INVALID_ARG, "tensors[%d]: %lld elements", i, static_cast<long long>(t[i].n));
+        if (t[i].model < 0 || t[i].model >= K) return fail(ctx, UNITY_ERR_INVALID_ARG, "tensors[%d]: model %d outside [0,%d)", i, t[i].model, K);
+        if (t[i].type != UNITY_F32 && t[i].type != UNITY_BF16) return fail(ctx, UNITY_ERR_INVALID_ARG, "tensors[%d]: type must be UNITY_F32 or UNITY_BF16", i);
+        if (t[i].n > 0 && !t[i].data) return fail(ctx, UNITY_ERR_INVALID_ARG, "tensors[%d]: data is NULL", i);
+        if (t[i].out && t[i].out_type != t[i].type && t[i].out_type != UNITY_BF16)
+            return fail(ctx, UNITY_ERR_INVALID_ARG, "tensors[%d]: out_type must be that of data or UNITY_BF16", i);
+        if (reinterpret_cast<uintptr_t>(t[i].data) % (t[i].type == UNITY_BF16 ? 2 : 4) ||
+            (t[i].out && reinterpret_cast<uintptr_t>(t[i].out) % (t[i].out_type == UNITY_BF16 ? 2 : 4)))
+            return fail(ctx, UNITY_ERR_ALIGNMENT, "tensors[%d] not aligned to its type", i);
+        m += t[i].n > 0 ? 2 : 0;
+    }
+    if (!scale || m == 0) return UNITY_OK;
+    ClipRange* r = static_cast<ClipRange*>(malloc(sizeof(ClipRange) * m));
+    if (!r) return fail(ctx, UNITY_ERR_INVALID_ARG, "out of host memory");
+    m = 0;
+    for (int i = 0; i < n; ++i) {
+        if (t[i].n == 0) continue;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(t[i].data), b = reinterpret_cast<uintptr_t>(t[i].out);
+        const bool same = !t[i].out || (a == b && t[i].type == t[i].out_type);
+        r[m++] = ClipRange{a, a + t[i].n * (t[i].type == UNITY_BF16 ? 2 : 4), i, same};
+        if (!same) r[m++] = ClipRange{b, b + t[i].n * (t[i].out_type == UNITY_BF16 ? 2 : 4), i, true};
+    }
+    std::sort(r, r + m, [](const ClipRange& x, const ClipRange& y) { return x.from < y.from; });
+    // in ascending order: what is written must begin behind everything before it, and what follows behind everything written
+    uintptr_t end = 0, end_w = 0;
+    int bad = -1;
+    for (int i = 0; i < m && bad < 0; ++i) {
+        if (r[i].from < (r[i].w ? end : end_w)) bad = r[i].tensor;
+        if (r[i].to > end) end = r[i].to;
+        if (r[i].w && r[i].to > end_w) end_w = r[i].to;
+    }
+    free(r);
+    return bad < 0 ? UNITY_OK : fail(ctx, UNITY_ERR_INVALID_ARG, "tensors[%d] overlaps another one that is read or written", bad);
+}
+
 }  // namespace
 
 // ================================================================================================
@@ -1699,6 +1791,159 @@ int unity_distill_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_di
     c.accumulate = params->accumulate_dW != 0; c.bf16_dw = params->dW_type == UNITY_BF16;
     c.loss = loss; c.tok_loss = tok_loss; c.lse = lse; c.dHidden = dHidden; c.dW = dW;
     return token_loss(ctx, &r, c);
+}
+
+// ------------------------------------------------------------------------------------------------
+size_t unity_rms_norm_workspace_bytes(int64_t n_tok, int32_t H, int32_t K) {
+    if (n_tok < 0 || n_tok > 0x7fffff00LL || H < 64 || H > UNITY_MAX_NORM_H || K < 1 || K > UNITY_MAX_MODELS) return 0;
+    return carve_norm(nullptr, ~size_t(0), H, K, norm_bwd_blocks(n_tok), nullptr).bytes;
+}
+
+int unity_rms_norm_fwd(unity_ctx* ctx, const unity_norm_rows* rows, const void* x, const void* residual, int res_type,
+                       void* y, void* res_out) {
+    NormArgs a;
+    int rc = norm_args(ctx, rows, res_type, a);
+    if (rc) return rc;
+    if (res_out && !residual) return fail(ctx, UNITY_ERR_INVALID_ARG, "res_out without residual");
+    if (rows->n_tok == 0) return UNITY_OK;
+    if (!x || !y) return fail(ctx, UNITY_ERR_INVALID_ARG, "x / y is NULL");
+    if (misaligned(x) || misaligned(residual) || misaligned(y) || misaligned(res_out))
+        return fail(ctx, UNITY_ERR_ALIGNMENT, "x / residual / y / res_out not 16-byte aligned");
+    const DeviceGuard dev(ctx->device);
+    if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+    a.x = static_cast<const __nv_bfloat16*>(x); a.residual = residual;
+    a.y = static_cast<__nv_bfloat16*>(y); a.res_out = res_out;
+    CUDA_TRY(ctx, launch_norm_fwd(a, ctx->stream));
+    ctx->launches += 1;
+    return UNITY_OK;
+}
+
+int unity_rms_norm_bwd(unity_ctx* ctx, const unity_norm_rows* rows, const void* res, int res_type, const void* dy,
+                       const void* dres, void* dx, float* const* dgamma, int accumulate) {
+    NormArgs a;
+    int rc = norm_args(ctx, rows, res_type, a);
+    if (rc) return rc;
+    for (int k = 0; dgamma && k < rows->K; ++k) {
+        if (!dgamma[k]) return fail(ctx, UNITY_ERR_INVALID_ARG, "dgamma[%d] is NULL", k);
+        if (misaligned(dgamma[k])) return fail(ctx, UNITY_ERR_ALIGNMENT, "dgamma[%d] not 16-byte aligned", k);
+        for (int j = 0; j < k; ++j)
+            if (dgamma[j] == dgamma[k]) return fail(ctx, UNITY_ERR_INVALID_ARG, "dgamma[%d] and dgamma[%d] are the same", j, k);
+        a.dgamma[k] = dgamma[k];
+    }
+    if (rows->n_tok > 0 && (!res || !dy || !dx)) return fail(ctx, UNITY_ERR_INVALID_ARG, "res / dy / dx is NULL");
+    if (misaligned(res) || misaligned(dy) || misaligned(dres) || misaligned(dx))
+        return fail(ctx, UNITY_ERR_ALIGNMENT, "res / dy / dres / dx not 16-byte aligned");
+    const DeviceGuard dev(ctx->device);
+    if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+    if (rows->n_tok == 0) {
+        for (int k = 0; dgamma && !accumulate && k < rows->K; ++k) CUDA_TRY(ctx, cudaMemsetAsync(dgamma[k], 0, sizeof(float) * rows->H, ctx->stream));
+        return UNITY_OK;
+    }
+    int blocks = norm_bwd_blocks(rows->n_tok);
+    if (dgamma) {
+        bool fits = false;
+        NormLayout L;
+        for (; blocks >= 1 && !fits; blocks -= fits ? 0 : (blocks + 7) / 8) {   // (fewer blocks, fewer slices)
+            L = carve_norm(ctx->ws, ctx->ws_bytes, rows->H, rows->K, blocks, &fits);
+            if (fits) break;
+        }
+        if (!fits) return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: need at least %zu bytes, have %zu",
+                               carve_norm(nullptr, ~size_t(0), rows->H, rows->K, 1, nullptr).bytes, ctx->ws_bytes);
+        a.parts = L.parts;
+        a.touched = L.touched;
+    }
+    a.res = res; a.dy = static_cast<const __nv_bfloat16*>(dy); a.dres = dres; a.dx = dx; a.accumulate = accumulate != 0;
+    int nl = 0;
+    CUDA_TRY(ctx, launch_norm_bwd(a, blocks, ctx->stream, &nl));
+    ctx->launches += nl;
+    return UNITY_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+size_t unity_clip_grad_norm_workspace_bytes(int32_t n_tensors, int32_t K) {
+    if (n_tensors < 0 || K < 1 || K > UNITY_MAX_MODELS) return 0;
+    const size_t launches = n_tensors < 1 ? 1 : (static_cast<size_t>(n_tensors) + kClipEntries - 1) / kClipEntries;
+    return up(launches * kClipBlocks * K * sizeof(double), kAlign);
+}
+
+int unity_clip_grad_norm(unity_ctx* ctx, int32_t n_tensors, const unity_tensor* tensors, int32_t K, const float* max_norm,
+                         float* norm, float* coef) {
+    if (!ctx) return UNITY_ERR_INVALID_ARG;
+    if (n_tensors < 0) return fail(ctx, UNITY_ERR_INVALID_ARG, "negative size");
+    if (K < 1 || K > UNITY_MAX_MODELS) return fail(ctx, UNITY_ERR_SHAPE, "K=%d outside [1,%d]", K, UNITY_MAX_MODELS);
+    if (!norm || (n_tensors > 0 && !tensors)) return fail(ctx, UNITY_ERR_INVALID_ARG, "norm / tensors is NULL");
+    ClipArgs a;
+    memset(&a, 0, sizeof(a));
+    for (int k = 0; max_norm && k < K; ++k) {
+        if (!(max_norm[k] >= 0.f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "max_norm[%d] must be >= 0", k);
+        a.max_norm[k] = max_norm[k];
+    }
+    a.K = K; a.has_max = max_norm != nullptr; a.write = max_norm != nullptr && n_tensors > 0; a.norm = norm; a.coef = coef;
+    a.n_launches = n_tensors < 1 ? 1 : (n_tensors + kClipEntries - 1) / kClipEntries;
+    const size_t need = unity_clip_grad_norm_workspace_bytes(n_tensors, K);
+    if (need > ctx->ws_bytes) return fail(ctx, UNITY_ERR_WORKSPACE, "workspace too small: need %zu bytes, have %zu", need, ctx->ws_bytes);
+    a.partial = reinterpret_cast<double*>(ctx->ws);
+    int rc = clip_check(ctx, n_tensors, tensors, K, max_norm != nullptr);
+    if (rc) return rc;
+    const DeviceGuard dev(ctx->device);
+    if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+    for (int pass = 0; pass < 2; ++pass)
+        for (int l = 0; l < a.n_launches; ++l) {
+            ClipEntry e[kClipEntries];
+            long long chunks = 0;
+            const int i0 = l * kClipEntries, n = n_tensors - i0 < kClipEntries ? n_tensors - i0 : kClipEntries;
+            for (int i = 0; i < n; ++i) {
+                const unity_tensor& t = tensors[i0 + i];
+                e[i].src = t.data; e[i].dst = t.out ? t.out : t.data; e[i].n = t.n; e[i].model = t.model;
+                e[i].src_bf16 = t.type == UNITY_BF16; e[i].dst_bf16 = t.out ? t.out_type == UNITY_BF16 : e[i].src_bf16;
+                e[i].chunk0 = chunks;
+                chunks += clip_chunks(e[i]);
+            }
+            if (pass == 1 && l > 0 && !a.write) break;            // (the first launch also writes norm and coef)
+            CUDA_TRY(ctx, pass == 0 ? launch_grad_squares(a, e, n, chunks, l, ctx->stream) : launch_grad_scale(a, e, n, chunks, l, ctx->stream));
+            ctx->launches += 1;
+        }
+    return UNITY_OK;
+}
+
+// ------------------------------------------------------------------------------------------------
+int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, int logits_type, int64_t ld, int32_t n_roles,
+                 const int32_t* row_role, const unity_sampling_rule* rules, const uint8_t* row_mask, const float* u,
+                 int32_t* token, float* logp, float* logp_kept, int32_t* n_kept) {
+    if (!ctx) return UNITY_ERR_INVALID_ARG;
+    if (n_rows < 0) return fail(ctx, UNITY_ERR_INVALID_ARG, "negative size");
+    if (n_rows > 1 << 24) return fail(ctx, UNITY_ERR_SHAPE, "n_rows too large");
+    if (V < 1 || V > UNITY_MAX_SAMPLE_V) return fail(ctx, UNITY_ERR_SHAPE, "V=%d outside [1,%d]", V, UNITY_MAX_SAMPLE_V);
+    if (ld < V) return fail(ctx, UNITY_ERR_SHAPE, "ld=%lld below V=%d", static_cast<long long>(ld), V);
+    if (ld > (1LL << 38)) return fail(ctx, UNITY_ERR_SHAPE, "ld too large");
+    if (n_roles < 1 || n_roles > UNITY_MAX_ROLES) return fail(ctx, UNITY_ERR_SHAPE, "n_roles=%d outside [1,%d]", n_roles, UNITY_MAX_ROLES);
+    if (logits_type != UNITY_F32 && logits_type != UNITY_BF16) return fail(ctx, UNITY_ERR_INVALID_ARG, "logits_type must be UNITY_F32 or UNITY_BF16");
+    if (!rules || (n_rows > 0 && (!logits || !u || !token))) return fail(ctx, UNITY_ERR_INVALID_ARG, "rules / logits / u / token is NULL");
+    if (reinterpret_cast<uintptr_t>(logits) % (logits_type == UNITY_BF16 ? 2 : 4)) return fail(ctx, UNITY_ERR_ALIGNMENT, "logits not aligned to their type");
+    SampleArgs a;
+    memset(&a, 0, sizeof(a));
+    for (int v = 0; v < n_roles; ++v) {
+        const unity_sampling_rule& r = rules[v];
+        if (!(r.temperature == 0.f || (r.temperature >= 1e-6f && r.temperature <= 1e6f)))
+            return fail(ctx, UNITY_ERR_INVALID_ARG, "rules[%d]: temperature must be 0 or lie in [1e-6, 1e6]", v);
+        if (!(r.top_p > 0.f && r.top_p <= 1.f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "rules[%d]: top_p must lie in (0, 1]", v);
+        if (!(r.min_p >= 0.f && r.min_p <= 1.f)) return fail(ctx, UNITY_ERR_INVALID_ARG, "rules[%d]: min_p must lie in [0, 1]", v);
+        SampleRule& s = a.rules[v];
+        s.temperature = r.temperature;
+        s.inv_t = r.temperature > 0.f ? 1.0 / static_cast<double>(r.temperature) : 1.0;
+        s.top_k = r.top_k > 0 && r.top_k < V ? r.top_k : 0;
+        s.top_p = static_cast<double>(r.top_p);
+        s.log_min_p = r.min_p > 0.f ? log(static_cast<double>(r.min_p)) : -INFINITY;
+    }
+    if (n_rows == 0) return UNITY_OK;
+    a.logits = logits; a.ld = ld; a.n_rows = n_rows; a.V = V; a.n_roles = n_roles;
+    a.row_role = row_role; a.row_mask = row_mask; a.u = u;
+    a.token = token; a.logp = logp; a.logp_kept = logp_kept; a.n_kept = n_kept; a.status = ctx->d_status;
+    const DeviceGuard dev(ctx->device);
+    if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
+    CUDA_TRY(ctx, launch_sample(a, logits_type == UNITY_BF16, ctx->stream));
+    ctx->launches += 1;
+    return UNITY_OK;
 }
 
 }  // extern "C"
