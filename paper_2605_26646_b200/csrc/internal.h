@@ -700,6 +700,7 @@ struct SampleRule {
     int top_k;                           // 0: off
     double inv_t, log_min_p;             // -inf: off
     double top_p;                        // >= 1: off
+    float quantile;                      // of the normal distribution at top_p
 };
 struct SampleArgs {
     const void* logits;

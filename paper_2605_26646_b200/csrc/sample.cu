@@ -4,13 +4,14 @@
 // Thread order is index order (a thread owns `per` consecutive entries), so running masses are sums over threads.
 //
 // With x = (z - max z) / T and e = exp x, what is kept is a prefix of the entries in the order (logit falling, index rising),
-// described by its last entry (logit, index).  min-p and top-k give such a prefix at once or by counting; top-p by mass.
-// The prefix's end is searched by thresholds: a pass counts and weighs the entries at or above four of them, until at most
-// kList entries are left between two, which are then ranked against one another, or only entries of one value, which go by index.
+// described by its last entry (logit, index).  min-p gives such a prefix at once, top-k by counting, top-p by mass.  Its end is
+// enclosed by thresholds: a pass counts and weighs what is at or above two of them, and the next two come from the two before
+// (for top-k first from the threads' largest entries, for top-p from mean and variance of x).  Once at most kList entries are
+// left between two thresholds they are sorted; where a single value holds more, its entries go by index.
 //
-// A decision compares a sum of masses with a share of another.  Sums are taken in fp32 exponentials first, with a bound on
-// their error (kSlack); where a comparison is closer than that, the row is done again with fp64 exponentials, so the outcome is
-// that of 64-bit arithmetic either way.
+// A decision compares a sum of masses with a share of another.  Sums are taken of fp32 exponentials first, with a bound on
+// their error (kSlackFast); where a comparison is closer than that, the row is done again with fp64 exponentials, so the outcome
+// is that of 64-bit arithmetic either way.
 #include "internal.h"
 #include "ptx.cuh"
 
@@ -21,61 +22,94 @@ namespace {
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kList = kThreads;              // entries ranked at most, one per thread
-constexpr int kTau = 4;                      // thresholds of a pass
-// fp32: e = ex2(x log2 e) is off by 2^-22 of itself, and by the roundings of x (twice 2^-24 |x|, whose mean under the
-// distribution is at most 18 octaves at 2^18 entries: 1.5e-6); four values are added in fp32, the rest in fp64 (1.8e-7).  Both
-// sides of a comparison carry that: 2^-18 of the whole mass.  fp64: exp is off by 2^-52 and by 2^-53 |x|.
+constexpr int kList = 2 * kThreads;          // entries sorted at most, two per thread
+constexpr int kTau = 2;                      // thresholds of a pass
+constexpr float kLowest = -3.402823466e38f;
+// fp32: e = ex2(z c - max z c), c = log2(e) / T, is off by 2^-22 of itself and by two roundings of its argument, 2^-24 |x| each (that
+// of max z c is common to all entries and taken out of the sums), whose mean under the distribution is at most 18 octaves at
+// 2^18 entries: 1.5e-6; four values are added in fp32, the rest in fp64: 1.8e-7.  Both sides of a comparison carry that: 2^-18
+// of the whole mass.  fp64: 2^-48.
 constexpr double kSlackFast = 0x1p-18, kSlackExact = 0.0;
 
-template <int N>
-struct Sums {
-    double m[N];
-    int c[N];
+struct Tally {                               // of the entries: mass of all, mass and number at or above each threshold
+    double whole, m[kTau];
+    float mean, square;                      // sums of e x and e x^2 (octaves)
+    int c[kTau];
 };
+constexpr int kTallyWords = 2 + kTau + kTau / 2;
+static_assert(sizeof(Tally) == 8 * kTallyWords && kTau % 2 == 0, "sent word by word");
 
 struct Shared {
-    Sums<kTau + 1> warp[kWarps];
-    Sums<kTau + 1> cta[2][kMaxCluster];      // of every block of the cluster; two in turn: one cluster barrier per exchange
-    double2 region[kMaxCluster * kWarps];    // (kept mass, whole mass) of every warp of the cluster
-    int region_n[kMaxCluster * kWarps];
-    float best_z[2][kMaxCluster];
-    int best_i[2][kMaxCluster];
+    uint64_t bar;                            // the row's arrival
+    uint64_t mail[2];                        // the messages' arrival, of the even and of the odd exchanges
+    unsigned long long box[2][kMaxCluster * kWarps];   // messages of every block, or of every warp
+    Tally warp[kWarps];
     float warp_z[kWarps];
-    int warp_i[kWarps];
+    int warp_i[kWarps], warp_n[kWarps];
     int scan[kWarps];
-    int count[2][kMaxCluster];
+    double scan_m[kWarps];
     int found;
-    float list_z[kList];
-    int list_i[kList];
-    double list_e[kList];
-    float last_z;
-    int last_i;
+    double exp2_table[32];
+    unsigned long long list[kList];          // (falling logit, rising index) as one rising number
 };
 
-__device__ __forceinline__ void remote_f64(void* local, int rank, double v) {
-    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(ptx::mapa(ptx::smem_u32(local), rank)), "d"(v) : "memory");
+// Messages between the blocks of a cluster: 8 bytes into another block's shared memory, counted by a barrier there.  An exchange is a
+// set of messages with at least one from every block to every block, so no block is more than one exchange ahead of another: two
+// barriers and two boxes, used in turn, do.
+__device__ __forceinline__ void send(unsigned long long* slot, uint64_t* mail, int to, unsigned long long v) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];" ::"r"(ptx::mapa(ptx::smem_u32(slot), to)), "l"(v),
+                 "r"(ptx::mapa(ptx::smem_u32(mail), to)) : "memory");
 }
-__device__ __forceinline__ void remote_u32(void* local, int rank, unsigned v) {
-    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ptx::mapa(ptx::smem_u32(local), rank)), "r"(v) : "memory");
-}
-__device__ __forceinline__ void cluster_meet() {
-    __syncwarp();                            // (the barrier's instructions are for whole warps)
-    ptx::cluster_sync_all();
+__device__ __forceinline__ bool mail_arrived(uint64_t* mail, unsigned parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(ptx::smem_u32(mail)), "r"(parity) : "memory");
+    return ok != 0;
 }
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
     return v;
 }
-__device__ __forceinline__ float as_float(float v) { return v; }
-__device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-// Order-preserving integers of finite floats.
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    return v;
+}
+// Inclusive sum over the lanes.
+__device__ __forceinline__ double warp_scan(double v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double u = __shfl_up_sync(kFull, v, o);
+        if (lane >= o) v += u;
+    }
+    return v;
+}
+// The larger one, NaN if one is NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+// Two neighbouring entries.
+__device__ __forceinline__ float2 pair(const float* p) { return *reinterpret_cast<const float2*>(p); }
+__device__ __forceinline__ float2 pair(const __nv_bfloat16* p) {
+    const unsigned v = *reinterpret_cast<const unsigned*>(p);
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+}
+__device__ __forceinline__ float one(const float* p) { return *p; }
+__device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+// Order-preserving integers of floats, one for both zeros: neighbouring values have neighbouring integers.
 __device__ __forceinline__ unsigned key_of(float z) {
     const unsigned b = __float_as_uint(z);
-    return b >> 31 ? ~b : b | 0x80000000u;
+    return b >> 31 ? 0x80000000u - (b & 0x7fffffffu) : b + 0x80000000u;
 }
-__device__ __forceinline__ float value_of(unsigned k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ float value_of(unsigned k) {
+    return __uint_as_float(k >= 0x80000000u ? k - 0x80000000u : 0x80000000u | (0x80000000u - k));
+}
 
 // The kept entries end with (z, i).
 struct Cut {
@@ -87,334 +121,575 @@ struct Cut {
 template <typename T>
 struct Row {
     Shared& s;
-    const T* z;                              // the block's entries
-    int per, ctas, rank, first;              // entries of a thread; index of the thread's first entry in the row
-    int turn, n_turn;
+    T* z;                                    // the thread's entries
+    int per, ctas, rank, first;              // entries of a thread (even); index of the thread's first entry in the row
+    int* status;
+    int turn;                                // exchanges so far
+    int n_all, my_n;                         // entries above -inf, and the thread's own
     float top;                               // largest logit
-    double inv_t;
-    float c_hi, c_lo;                        // log2(e) / T in two parts
-    int V;
+    double inv_t, c64;                       // 1 / T, log2(e) / T
+    float c, top_c;                          // log2(e) / T and that times the largest logit, in fp32
+    double whole;                            // mass of all entries
+    // what is known about the end of the kept entries: it lies in [lo, hi); the thread's own mass and numbers there
+    float lo, hi;
+    int n_lo, n_hi, my_lo, my_hi;
+    double m_hi, my_m;
+    float list_lo, list_hi;                  // the list holds the sorted entries of this interval
+    bool cut_down;                           // entries were taken out of shared memory
 
-    __device__ __forceinline__ float at(int j) const { return as_float(z[threadIdx.x * per + j]) + 0.f; }   // (+ 0: -0 becomes 0)
-    // Weight of an entry: fp32 or fp64 exponential.  -inf has none.
+    __device__ __forceinline__ int lane() const { return threadIdx.x & 31; }
+    __device__ __forceinline__ int warp() const { return threadIdx.x >> 5; }
+
+    // Weight of an entry.  -inf has none.
+    __device__ __forceinline__ float octaves(float v) const { return fmaf(v, c, -top_c); }
+    __device__ __forceinline__ float fast(float v) const { return ptx::ex2(octaves(v)); }
+    // exp in fp64 by a table (2^(j/32)) and the exponential series on a 64th of an octave: 2^k 2^(j/32) (1 + p), off by 2^-48.
+    __device__ __forceinline__ double slow(float v) const {
+        const double d = static_cast<double>(v) - static_cast<double>(top), y = d * c64;   // (octaves; the largest logit's e is 1)
+        if (!(y > -1020.0)) return v == -INFINITY ? 0.0 : exp(d * inv_t);
+        constexpr double kShift = 0x1.8p52 / 32.0, kLn2 = 0.69314718055994531;  // the sum with kShift rounds to 32nds
+        const double t = y + kShift, r = y - (t - kShift);
+        const int n = __double2loint(t);                         // 32 k + j
+        const double p = r * (kLn2 + r * (kLn2 * kLn2 / 2 + r * (kLn2 * kLn2 * kLn2 / 6 +
+                              r * (kLn2 * kLn2 * kLn2 * kLn2 / 24 + r * (kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 120)))));
+        const double b = s.exp2_table[n & 31];
+        const double scaled = __hiloint2double(__double2hiint(b) + ((n >> 5) << 20), __double2loint(b));
+        return fma(scaled, p, scaled);
+    }
     template <bool EXACT>
-    __device__ __forceinline__ double weight(float v) const {
-        if (EXACT) return exp((static_cast<double>(v) - static_cast<double>(top)) * inv_t);
-        return static_cast<double>(fast(v));
+    __device__ __forceinline__ double weight(float v) const { return EXACT ? slow(v) : static_cast<double>(fast(v)); }
+
+    // One exchange: announce the bytes that will arrive here, send, wait.
+    __device__ __forceinline__ uint64_t* mail() const { return &s.mail[turn & 1]; }
+    __device__ __forceinline__ unsigned long long* box(int i) const { return &s.box[turn & 1][i]; }
+    __device__ __forceinline__ void expect(int words) const {
+        if (threadIdx.x == 0) ptx::mbar_arrive_expect_tx(mail(), 8 * words);
     }
-    __device__ __forceinline__ float fast(float v) const {
-        const float d = v - top;
-        return ptx::ex2(fmaxf(fmaf(d, c_hi, d * c_lo), -200.f));
+    __device__ __forceinline__ void receive() {
+        const unsigned parity = turn >> 1 & 1;
+        if (!mail_arrived(mail(), parity)) {
+            const long long t0 = clock64();
+            while (!mail_arrived(mail(), parity))
+                if (clock64() - t0 > kWaitBudgetCycles) { atomicOr(status, kStatusTimeout); break; }
+        }
+        ++turn;
+    }
+    // A word of every block to every block; returns the other side's place of it.  (Behind a barrier of the block.)
+    __device__ __forceinline__ const unsigned long long* all_to_all(unsigned long long v) {
+        const unsigned long long* got = box(0);
+        expect(ctas);
+        if (threadIdx.x < ctas) send(box(rank), mail(), threadIdx.x, v);
+        receive();
+        return got;
     }
 
-    __device__ __forceinline__ Sums<kTau + 1> exchange(Sums<kTau + 1> v) {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // Sums over the cluster, the same in every thread.
+    __device__ __forceinline__ void add_lanes(Tally& v) const {
+        v.whole = warp_sum(v.whole);
+        v.mean = warp_sum(v.mean);
+        v.square = warp_sum(v.square);
 #pragma unroll
-        for (int k = 0; k <= kTau; ++k) {
+        for (int k = 0; k < kTau; ++k) {
             v.m[k] = warp_sum(v.m[k]);
             v.c[k] = __reduce_add_sync(kFull, v.c[k]);
         }
-        if (lane == 0) s.warp[warp] = v;
+    }
+    __device__ __forceinline__ Tally exchange(Tally v) {
+        expect(ctas * kTallyWords);
+        add_lanes(v);
+        if (lane() == 0) s.warp[warp()] = v;
         __syncthreads();
-        if (threadIdx.x <= kTau) {
-            const int k = threadIdx.x;
-            double m = 0.0;
-            int c = 0;
-            for (int w = 0; w < kWarps; ++w) { m += s.warp[w].m[k]; c += s.warp[w].c[k]; }
-            for (int r = 0; r < ctas; ++r) {
-                remote_f64(&s.cta[turn][rank].m[k], r, m);
-                remote_u32(&s.cta[turn][rank].c[k], r, c);
+        if (warp() == 0) {
+            if (lane() < kWarps) v = s.warp[lane()]; else v = Tally{};
+            add_lanes(v);
+            if (lane() < ctas) {
+                const unsigned long long* w = reinterpret_cast<const unsigned long long*>(&v);
+#pragma unroll
+                for (int i = 0; i < kTallyWords; ++i) send(box(rank * kTallyWords + i), mail(), lane(), w[i]);
             }
         }
-        cluster_meet();
-        v = s.cta[turn][0];
-        for (int r = 1; r < ctas; ++r)
+        const Tally* got = reinterpret_cast<const Tally*>(box(0));
+        receive();
+        v = got[0];
+        for (int r = 1; r < ctas; ++r) {
+            v.whole += got[r].whole;
+            v.mean += got[r].mean;
+            v.square += got[r].square;
 #pragma unroll
-            for (int k = 0; k <= kTau; ++k) { v.m[k] += s.cta[turn][r].m[k]; v.c[k] += s.cta[turn][r].c[k]; }
-        turn ^= 1;
+            for (int k = 0; k < kTau; ++k) { v.m[k] += got[r].m[k]; v.c[k] += got[r].c[k]; }
+        }
         return v;
     }
 
-    // Number and mass of the entries that `cut` keeps and that are >= tau[k]; the last place: all that it keeps.
-    template <bool EXACT>
-    __device__ __forceinline__ Sums<kTau + 1> tally(const Cut& cut, const float (&tau)[kTau]) {
-        Sums<kTau + 1> v = {};
-        for (int j0 = 0; j0 < per; j0 += 4) {
-            float part[kTau + 1] = {};
+    // One pass: mass of all entries, masses and numbers of those >= tau[k].  fp32: eight are added pairwise, their sums in two parts.
+    template <bool EXACT, bool TAU, bool MOMENTS>
+    __device__ __forceinline__ Tally weigh(const float (&tau)[kTau]) const {
+        Tally v = {};
+        float hi[kTau + 1] = {}, low[kTau + 1] = {};
+        for (int j0 = 0; j0 < per; j0 += 8) {
+            float x[8], e[8];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int j = j0 + q;
-                if (j >= per) break;
-                const float x = at(j);
-                if (!cut.keeps(x, first + j)) continue;
+            for (int q = 0; q < 8; q += 2) {
+                const float2 two = j0 + q < per ? pair(z + j0 + q) : make_float2(-INFINITY, -INFINITY);
+                x[q] = two.x;
+                x[q + 1] = two.y;
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                if (TAU)
+#pragma unroll
+                    for (int k = 0; k < kTau; ++k) v.c[k] += x[q] >= tau[k];
                 if (EXACT) {
-                    const double e = weight<true>(x);
-                    v.m[kTau] += e;
-                    v.c[kTau] += 1;
+                    const double e64 = slow(x[q]);
+                    v.whole += e64;
+                    if (TAU)
 #pragma unroll
-                    for (int k = 0; k < kTau; ++k)
-                        if (x >= tau[k]) { v.m[k] += e; v.c[k] += 1; }
+                        for (int k = 0; k < kTau; ++k)
+                            if (x[q] >= tau[k]) v.m[k] += e64;
                 } else {
-                    const float e = fast(x);
-                    part[kTau] += e;
-                    v.c[kTau] += 1;
-#pragma unroll
-                    for (int k = 0; k < kTau; ++k)
-                        if (x >= tau[k]) { part[k] += e; v.c[k] += 1; }
+                    const float o = octaves(x[q]);
+                    e[q] = ptx::ex2(o);
+                    if (MOMENTS) {
+                        const float eo = e[q] * fmaxf(o, -1e3f);
+                        v.mean += eo;
+                        v.square = fmaf(eo, fmaxf(o, -1e3f), v.square);
+                    }
                 }
             }
-            if (!EXACT)
+            if (!EXACT) {
 #pragma unroll
-                for (int k = 0; k <= kTau; ++k) v.m[k] += static_cast<double>(part[k]);
+                for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
+                    float f[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) f[q] = k == 0 || x[q] >= tau[k ? k - 1 : 0] ? e[q] : 0.f;
+                    const float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+                    const float next = hi[k] + sum, part = next - hi[k];
+                    low[k] += (hi[k] - (next - part)) + (sum - part);
+                    hi[k] = next;
+                }
+            }
         }
-        return exchange(v);
+        if (!EXACT) {
+            v.whole = static_cast<double>(hi[0]) + static_cast<double>(low[0]);
+#pragma unroll
+            for (int k = 0; k < kTau; ++k) v.m[k] = static_cast<double>(hi[k + 1]) + static_cast<double>(low[k + 1]);
+        }
+        return v;
     }
 
-    // Exclusive prefix of `n` over the cluster's threads in index order, and the total.
-    __device__ __forceinline__ int prefix(int n, int* total) {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    // A logit that about `want` entries or a few more reach: of every block its share of them is counted among its threads' largest
+    // entries, and the least such logit is taken (blocks of less than half a share say nothing).  `mine`: the thread's largest.
+    __device__ __forceinline__ float reached_by(int want, float mine, int valid, int V) {
+        unsigned least = 0xffffffffu;
+        if (2 * valid * ctas >= V) {
+            const int n = static_cast<int>((static_cast<long long>(valid) * want + V - 1) / V);
+            const unsigned key = mine > -INFINITY ? key_of(mine) : 0u;
+            least = 0;
+            for (int b = 31; b >= 14; --b) {                      // (the lower half of the digits says little)
+                const unsigned next = least | 1u << b;
+                if (__syncthreads_count(key >= next) >= n) least = next;
+            }
+        }
+        __syncthreads();
+        const unsigned long long* got = all_to_all(least);
+        for (int r = 0; r < ctas; ++r) least = min(least, static_cast<unsigned>(got[r]));
+        return least == 0u || least == 0xffffffffu ? -INFINITY : value_of(least);
+    }
+
+    // Exclusive prefix of `n` over the cluster's threads in index order.
+    __device__ __forceinline__ int prefix(int n) {
         int v = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int u = __shfl_up_sync(kFull, v, o);
-            if (lane >= o) v += u;
+            if (lane() >= o) v += u;
         }
+        if (lane() == 31) s.scan[warp()] = v;
         __syncthreads();
-        if (lane == 31) s.scan[warp] = v;
-        __syncthreads();
-        int before = v - n, mine = 0;
-        for (int w = 0; w < kWarps; ++w) { before += w < warp ? s.scan[w] : 0; mine += s.scan[w]; }
-        if (threadIdx.x < ctas) remote_u32(&s.count[n_turn][rank], threadIdx.x, mine);
-        cluster_meet();
-        int all = 0;
-        for (int r = 0; r < ctas; ++r) { before += r < rank ? s.count[n_turn][r] : 0; all += s.count[n_turn][r]; }
-        n_turn ^= 1;
-        *total = all;
+        const int w = lane() < kWarps ? s.scan[lane()] : 0;
+        int before = v - n + __reduce_add_sync(kFull, lane() < warp() ? w : 0);
+        const int block = __reduce_add_sync(kFull, w);
+        const unsigned long long* got = all_to_all(block);
+        for (int r = 0; r < rank; ++r) before += static_cast<int>(got[r]);
         return before;
     }
 
-    // Shortens `cut` to the first entries whose number reaches k (BY_MASS false) or whose mass reaches share * mass(cut).
-    // False: a comparison was too close for this arithmetic.  (Every thread of the cluster gets the same result.)
+    // Encloses the end of the first k_want entries (BY_MASS false) or of the first whose mass reaches share of the whole, until at
+    // most kList entries or one value are in [lo, hi).  `above`, `below`: first thresholds.  False: a comparison was too close for this
+    // arithmetic.  (Every thread of the cluster gets the same result.)
     template <bool EXACT, bool BY_MASS>
-    __device__ __forceinline__ bool shorten(Cut& cut, int k_want, double share) {
+    __device__ __forceinline__ bool enclose(int k_want, double share, float quantile, float above, float below, double* target, double* bound) {
         const double slack = EXACT ? kSlackExact : kSlackFast;
-        float lo = cut.z, hi = INFINITY;                         // the end lies in [lo, hi)
-        int n_lo = 0, n_hi = 0;
-        double m_hi = 0.0, target = 0.0, bound = 0.0;
+        const float octave = 0.69314718f / static_cast<float>(inv_t);
+        float tau[kTau] = {above, below};
+        double m_lo = 0.0;
+        float centre = 0.f, width = 0.f;
+        lo = kLowest;
         for (int round = 0;; ++round) {
-            float tau[kTau];
-            if (round == 0) {
-                // octaves below the largest logit
-                const float step = 0.69314718f / static_cast<float>(inv_t);
-#pragma unroll
-                for (int k = 0; k < kTau; ++k) tau[k] = top - step * (k == 0 ? 1.5f : k == 1 ? 5.f : k == 2 ? 9.f : 14.f);
-            } else {
-                // evenly between lo and hi, as values where they are close, else as order-preserving integers
+            if (round > 0) {
+                // between lo and hi: around the normal distribution's quantile, around the linear estimate, evenly; and evenly as
+                // order-preserving integers where all that took long or the interval is far longer than the distribution
+                const bool near = round < 10 && hi - lo < 256.f * octave;
+                float at = 0.5f * (lo + hi), wide = (hi - lo) * (1.f / 6);
+                if (BY_MASS && round == 1 && centre - width < hi && centre + width > lo) {
+                    at = centre;
+                    wide = width;
+                } else if (BY_MASS && round < 5) {
+                    at = hi - (hi - lo) * static_cast<float>((*target - m_hi) / (m_lo - m_hi));
+                    wide = (hi - lo) * (round == 2 ? 0.1f : 0.04f);
+                } else if (!BY_MASS && round < 5) {
+                    at = hi - (hi - lo) * (static_cast<float>(k_want - n_hi) / static_cast<float>(n_lo - n_hi));
+                    wide = (hi - lo) * 0.1f;
+                }
                 const unsigned a = key_of(lo), b = key_of(hi);
-                const bool near = round < 6 && hi - lo < 64.f / static_cast<float>(inv_t);
 #pragma unroll
                 for (int k = 0; k < kTau; ++k) {
                     const unsigned key = a + static_cast<unsigned>(static_cast<unsigned long long>(b - a) * (kTau - k) / (kTau + 1));
-                    tau[k] = near ? lo + (hi - lo) * (static_cast<float>(kTau - k) / (kTau + 1)) : value_of(key);
-                    if (!(tau[k] > lo && tau[k] < hi)) tau[k] = value_of(a + 1);
+                    tau[k] = near || (BY_MASS && round == 1 && wide == width) ? (k == 0 ? at + wide : at - wide) : value_of(key);
+                    if (!(tau[k] > lo && tau[k] < hi)) tau[k] = value_of(a + (b - a) / 2);
                 }
             }
-            const Sums<kTau + 1> v = tally<EXACT>(cut, tau);
+            const Tally mine = !EXACT && BY_MASS && round == 0 ? weigh<EXACT, true, true>(tau) : weigh<EXACT, true, false>(tau);
+            const Tally v = exchange(mine);
             if (round == 0) {
-                n_lo = v.c[kTau];
-                if (!BY_MASS && n_lo <= k_want) return true;      // nothing to cut off
-                target = share * v.m[kTau];
-                bound = slack * v.m[kTau];
+                whole = v.whole;
+                m_lo = v.whole;
+                n_lo = n_all;
+                my_lo = my_n;
                 hi = nextafterf(top, INFINITY);
-                if (!(lo > -INFINITY)) lo = -3.402823466e38f;
+                n_hi = my_hi = 0;
+                m_hi = my_m = 0.0;
+                *target = share * v.whole;
+                *bound = slack * v.whole;
+                const float mean = v.mean / static_cast<float>(v.whole);
+                const float sd = sqrtf(fmaxf(v.square / static_cast<float>(v.whole) - mean * mean, 0.f));
+                centre = top + octave * (mean - sd * quantile);
+                width = octave * (0.25f + 0.1f * sd);
             }
             bool moved = false;
 #pragma unroll
             for (int k = 0; k < kTau; ++k) {
                 if (!(tau[k] > lo && tau[k] < hi)) continue;
-                const bool enough = BY_MASS ? v.m[k] >= target + bound : v.c[k] >= k_want;
-                const bool little = BY_MASS ? v.m[k] < target - bound || (EXACT && v.m[k] < target) : v.c[k] < k_want;
-                if (little) { hi = tau[k]; n_hi = v.c[k]; m_hi = v.m[k]; moved = true; }
-                else if (enough) { lo = tau[k]; n_lo = v.c[k]; moved = true; }
+                const bool enough = BY_MASS ? v.m[k] >= *target + *bound : v.c[k] >= k_want;
+                const bool little = BY_MASS ? v.m[k] < *target - *bound : v.c[k] < k_want;
+                if (little) { hi = tau[k]; n_hi = v.c[k]; m_hi = v.m[k]; my_hi = mine.c[k]; my_m = mine.m[k]; moved = true; }
+                else if (enough) { lo = tau[k]; n_lo = v.c[k]; m_lo = v.m[k]; my_lo = mine.c[k]; moved = true; }
             }
-            if (n_lo - n_hi <= kList || key_of(hi) - key_of(lo) <= 1u) break;
+            if (n_lo - n_hi <= kList || key_of(hi) - key_of(lo) <= 1u) return true;
             if (!moved && round > 0) return false;
         }
-        if (n_lo - n_hi <= kList) {
-            // rank the entries in [lo, hi)
-            int n = 0, total;
-            for (int j = 0; j < per; ++j) {
-                const float x = at(j);
-                n += x >= lo && x < hi && cut.keeps(x, first + j);
-            }
-            int to = prefix(n, &total);
-            for (int j = 0; j < per && n > 0; ++j) {
-                const float x = at(j);
-                if (!(x >= lo && x < hi && cut.keeps(x, first + j))) continue;
-                const double e = BY_MASS ? weight<EXACT>(x) : 0.0;
-                for (int r = 0; r < ctas; ++r) {
-                    remote_u32(&s.list_z[to], r, __float_as_uint(x));
-                    remote_u32(&s.list_i[to], r, first + j);
-                    if (BY_MASS) remote_f64(&s.list_e[to], r, e);
-                }
-                ++to;
-                --n;
-            }
-            cluster_meet();
-            const int me = threadIdx.x;
-            int before = 0;
-            bool keep = false, close = false;
-            if (me < total) {
-                const float z0 = s.list_z[me];
-                double mass = m_hi;
-                for (int j = 0; j < total; ++j) {
-                    const float z1 = s.list_z[j];
-                    if (z1 > z0 || (z1 == z0 && j < me)) {        // (the list is in index order)
-                        ++before;
-                        if (BY_MASS) mass += s.list_e[j];
-                    }
-                }
-                keep = BY_MASS ? mass < target : n_hi + before < k_want;
-                close = BY_MASS && !EXACT && fabs(mass - target) <= bound;
-            }
-            const int kept = __syncthreads_count(keep);
-            const bool too_close = __syncthreads_or(close);
-            if (too_close) return false;
-            if (keep && before == kept - 1) { s.last_z = s.list_z[me]; s.last_i = s.list_i[me]; }
-            __syncthreads();
-            cut.z = s.last_z;
-            cut.i = s.last_i;
-        } else {
-            // entries of one value: so many of them by index
-            int want = k_want - n_hi;
-            if (BY_MASS) {
-                const double e = weight<EXACT>(lo), need = (target - m_hi) / e, whole = ceil(need);
-                if (!EXACT && !(fabs(need - rint(need)) * e > bound)) return false;
-                want = !(whole >= 1.0) ? 1 : whole > n_lo - n_hi ? n_lo - n_hi : static_cast<int>(whole);
-            }
-            int n = 0, total;
-            for (int j = 0; j < per; ++j) n += at(j) == lo && cut.keeps(lo, first + j);
-            const int before = prefix(n, &total);
-            if (before < want && want <= before + n) {
-                int left = want - before, found = first;
-                for (int j = 0; j < per; ++j)
-                    if (at(j) == lo && cut.keeps(lo, first + j) && --left == 0) { found = first + j; break; }
-                for (int r = 0; r < ctas; ++r) remote_u32(&s.found, r, found);
-            }
-            cluster_meet();
-            cut.z = lo;
-            cut.i = s.found;
+    }
+
+    // The entries in [lo, hi) in order: an entry's place is its rank behind the n_hi above.
+    __device__ __forceinline__ void sort_list(int total) {
+        if (list_lo == lo && list_hi == hi) return;
+        list_lo = lo;
+        list_hi = hi;
+        int n = my_lo - my_hi, to = prefix(n);
+        __syncthreads();                                          // (every warp has read its messages)
+        expect(total + ctas);
+        if (threadIdx.x < ctas) send(box(rank), mail(), threadIdx.x, 0);
+        for (int j = 0; n > 0 && j < per; ++j) {
+            const float x = one(z + j);
+            if (!(x >= lo && x < hi)) continue;
+            const unsigned long long item = static_cast<unsigned long long>(~key_of(x)) << 32 | static_cast<unsigned>(first + j);
+            for (int r = 0; r < ctas; ++r) send(&s.list[to], mail(), r, item);
+            ++to;
+            --n;
         }
+        int log_size = 6;
+        while (1 << log_size < total) ++log_size;
+        const int size = 1 << log_size;
+        for (int i = total + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
+        receive();
+        __syncthreads();
+        // bitonic: a thread compares one pair per step; up to 32 apart the pairs of a warp are the warp's own
+        for (int k = 1; k <= log_size; ++k)
+            for (int j = k - 1; j >= 0; --j) {
+                const int i = (threadIdx.x >> j << (j + 1)) | (threadIdx.x & ((1 << j) - 1));
+                if (i < size) {
+                    const unsigned long long a = s.list[i], b = s.list[i + (1 << j)];
+                    if ((a > b) == ((i >> k & 1) == 0)) { s.list[i] = b; s.list[i + (1 << j)] = a; }
+                }
+                if (j > 5 || (j > 0 ? j - 1 : k) > 5) __syncthreads(); else __syncwarp();
+            }
+        __syncthreads();
+    }
+
+    // Cuts the sorted entries: rank below k_want (behind the n_hi above) and, with BY_MASS, mass before them below the target.  With
+    // k_want and a share the target is that share of the first k_want's mass.
+    template <bool EXACT, bool BY_MASS>
+    __device__ __forceinline__ bool cut_list(int total, int k_want, double share, double target, double bound, Cut* cut, int* n_kept) {
+        const int i0 = 2 * threadIdx.x;
+        double e[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            e[h] = BY_MASS && i0 + h < total && n_hi + i0 + h < k_want ? weight<EXACT>(value_of(~static_cast<unsigned>(s.list[i0 + h] >> 32))) : 0.0;
+        double before = 0.0;
+        if (BY_MASS) {
+            const double run = warp_scan(e[0] + e[1], lane());
+            if (lane() == 31) s.scan_m[warp()] = run;
+            __syncthreads();
+            const double w = lane() < kWarps ? s.scan_m[lane()] : 0.0;
+            const double upto = warp_scan(w, lane());
+            before = __shfl_sync(kFull, upto, warp() ? warp() - 1 : 0);
+            before = (warp() ? before : 0.0) + (run - e[0] - e[1]);
+            if (share > 0.0) {
+                const double all = __shfl_sync(kFull, upto, kWarps - 1);
+                target = share * all;
+                bound = (EXACT ? kSlackExact : kSlackFast) * all;
+            }
+        }
+        int kept = 0;
+        bool close = false;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (i0 + h >= total || n_hi + i0 + h >= k_want) continue;
+            const double m = m_hi + before + (h ? e[0] : 0.0);
+            kept += !BY_MASS || m < target;
+            close |= BY_MASS && !EXACT && fabs(m - target) <= bound && i0 + h + n_hi > 0;
+        }
+        const int warp_kept = __reduce_add_sync(kFull, kept);
+        if (lane() == 0) s.scan[warp()] = warp_kept;
+        if (__syncthreads_or(close)) return false;
+        kept = __reduce_add_sync(kFull, lane() < kWarps ? s.scan[lane()] : 0);
+        kept = kept > 0 ? kept : 1;                              // (rounding does not take the first one)
+        const unsigned long long last = s.list[kept - 1];
+        cut->z = value_of(~static_cast<unsigned>(last >> 32));
+        cut->i = static_cast<int>(last & 0xffffffffu);
+        *n_kept = n_hi + kept;
         return true;
     }
 
-    // The first kept entry whose running mass is > u * mass(cut).  The thread that holds it writes the outputs.
+    // Cuts entries of one value, lo: so many of them by index.
+    template <bool EXACT, bool BY_MASS>
+    __device__ __forceinline__ bool cut_ties(int k_want, double target, double bound, Cut* cut, int* n_kept) {
+        int want = k_want - n_hi;
+        if (BY_MASS) {
+            const double e = weight<EXACT>(lo), need = (target - m_hi) / e, up = ceil(need);
+            if (!EXACT && !(fabs(need - rint(need)) * e > bound)) return false;
+            want = !(up >= 1.0) ? 1 : up > n_lo - n_hi ? n_lo - n_hi : static_cast<int>(up);
+        }
+        want = min(want, n_lo - n_hi);
+        const int n = my_lo - my_hi, before = prefix(n);
+        if (threadIdx.x == 0) s.found = -1;
+        __syncthreads();
+        if (before < want && want <= before + n) {
+            int left = want - before;
+            for (int j = 0; j < per; ++j)
+                if (one(z + j) == lo && --left == 0) { s.found = first + j; break; }
+        }
+        __syncthreads();
+        const unsigned long long* got = all_to_all(static_cast<unsigned>(s.found + 1));
+        int found = 0;
+        for (int r = 0; r < ctas; ++r) found += static_cast<int>(got[r]);
+        cut->z = lo;
+        cut->i = found - 1;
+        *n_kept = n_hi + want;
+        return true;
+    }
+
+    // The first kept entry whose running mass is > u times the kept mass: those >= hi, and those in [lo, hi) that `cut` keeps.  The
+    // warp that holds it writes the outputs.
     template <bool EXACT>
-    __device__ __forceinline__ bool pick(const SampleArgs& a, int row, const Cut& cut, float u) {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        double mine = 0.0, whole = 0.0;
-        int n = 0;
-        for (int j0 = 0; j0 < per; j0 += 4) {
-            float kept4 = 0.f, all4 = 0.f;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int j = j0 + q;
-                if (j >= per) break;
-                const float x = at(j);
-                const bool keep = cut.keeps(x, first + j);
-                n += keep;
-                if (EXACT) {
-                    const double e = weight<true>(x);
-                    whole += e;
-                    mine += keep ? e : 0.0;
-                } else {
-                    const float e = fast(x);
-                    all4 += e;
-                    kept4 += keep ? e : 0.f;
-                }
+    __device__ __forceinline__ bool pick(const SampleArgs& a, int row, const Cut& cut, int n_kept, float u) {
+        double mine = my_m;
+        if (my_lo > my_hi)
+            for (int j = 0; j < per; ++j) {
+                const float x = one(z + j);
+                if (x >= lo && x < hi && cut.keeps(x, first + j)) mine += weight<EXACT>(x);
             }
-            if (!EXACT) { whole += static_cast<double>(all4); mine += static_cast<double>(kept4); }
-        }
-        double run = mine;                                        // inclusive over the warp's lanes
+        const double run = warp_scan(mine, lane());               // inclusive over the warp's lanes
+        const double sum = __shfl_sync(kFull, run, 31);
+        expect(ctas * kWarps);
+        if (lane() < ctas) send(box(rank * kWarps + warp()), mail(), lane(), static_cast<unsigned long long>(__double_as_longlong(sum)));
+        const unsigned long long* region = box(0);
+        receive();
+        // Every warp looks for the warp whose range of running masses holds the target: the first that ends above it (u < 1, but
+        // rounding may leave none: then the last with any mass).  A lane has four neighbouring warps.
+        constexpr int kEach = kMaxCluster * kWarps / 32;
+        double part[kEach], four = 0.0;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const double v = __shfl_up_sync(kFull, run, o);
-            if (lane >= o) run += v;
+        for (int i = 0; i < kEach; ++i) {
+            const int w = lane() * kEach + i;
+            part[i] = w < ctas * kWarps ? __longlong_as_double(static_cast<long long>(region[w])) : 0.0;
+            four += part[i];
         }
-        whole = warp_sum(whole);
-        n = __reduce_add_sync(kFull, n);
-        if (lane == 31)
-            for (int r = 0; r < ctas; ++r) {
-                remote_f64(&s.region[rank * kWarps + warp].x, r, run);
-                remote_f64(&s.region[rank * kWarps + warp].y, r, whole);
-                remote_u32(&s.region_n[rank * kWarps + warp], r, n);
-            }
-        cluster_meet();
-        double before = 0.0, kept = 0.0;
-        whole = 0.0;
-        n = 0;
-        for (int w = 0; w < ctas * kWarps; ++w) {
-            if (w == rank * kWarps + warp) before = kept;
-            kept += s.region[w].x;
-            whole += s.region[w].y;
-            n += s.region_n[w];
-        }
-        // The warp whose range of running masses holds the target; in it the first lane whose own does (rounding may leave that to a
-        // lane without kept entries, or to none: then the next, or the last, with some).  u < 1, so the target is below kept.
+        const double upto = warp_scan(four, lane()), kept = __shfl_sync(kFull, upto, 31), prior = __shfl_up_sync(kFull, upto, 1);
         const double target = static_cast<double>(u) * kept, bound = EXACT ? kSlackExact : kSlackFast * kept;
-        const double prev = __shfl_up_sync(kFull, run, 1);
-        const double warp_end = before + __shfl_sync(kFull, run, 31);
+        double from = lane() ? prior : 0.0, start = 0.0, last_start = 0.0;
+        int hit = -1, last = -1;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const double to = from + part[i];
+            if (part[i] > 0.0) {
+                last = lane() * kEach + i;
+                last_start = from;
+                if (hit < 0 && to > target) { hit = last; start = from; }
+            }
+            from = to;
+        }
+        const unsigned hits = __ballot_sync(kFull, hit >= 0), lasts = __ballot_sync(kFull, last >= 0);
+        const int owner = hits ? __ffs(hits) - 1 : 31 - __clz(lasts);
+        const int home = __shfl_sync(kFull, hits ? hit : last, owner);
+        start = __shfl_sync(kFull, hits ? start : last_start, owner);
         bool close = false;
         int token = -1;
         float tz = 0.f;
-        if (before <= target && target < warp_end) {
-            const unsigned some = __ballot_sync(kFull, mine > 0.0), past = some & __ballot_sync(kFull, before + run > target);
-            if (lane == (past ? __ffs(past) - 1 : 31 - __clz(some))) {
-                double c = before + (lane ? prev : 0.0);
-                close = fabs(c - target) <= bound;
-                for (int j = 0; j < per; ++j) {
-                    const float x = at(j);
-                    if (!cut.keeps(x, first + j)) continue;
-                    const double e = weight<EXACT>(x);
-                    if (!(e > 0.0)) continue;
-                    token = first + j;
-                    tz = x;
-                    c += e;
-                    close |= fabs(c - target) <= bound;
-                    if (c > target) break;
+        if (home == rank * kWarps + warp()) {
+            // in the warp the first lane whose running mass is above the target, of those with any
+            const unsigned some = __ballot_sync(kFull, mine > 0.0), past = some & __ballot_sync(kFull, start + run > target);
+            const int holder = past ? __ffs(past) - 1 : 31 - __clz(some);
+            const double prev = __shfl_sync(kFull, run, holder ? holder - 1 : 0);
+            double at0 = start + (holder ? prev : 0.0);
+            close = fabs(at0 - target) <= bound;
+            // its entries, 32 at a time
+            const T* row_z = z + (holder - lane()) * per;
+            const int base = first + (holder - lane()) * per;
+            for (int j0 = 0; j0 < per; j0 += 32) {
+                const int j = j0 + lane();
+                float x = 0.f;
+                double e = 0.0;
+                if (j < per) {
+                    x = one(row_z + j);
+                    if (x >= hi || (x >= lo && cut.keeps(x, base + j))) e = weight<EXACT>(x);
                 }
+                const double at = at0 + warp_scan(e, lane());
+                const unsigned any = __ballot_sync(kFull, e > 0.0), above = any & __ballot_sync(kFull, at > target);
+                close |= __any_sync(kFull, e > 0.0 && fabs(at - target) <= bound);
+                const int l = above ? __ffs(above) - 1 : any ? 31 - __clz(any) : -1;
+                if (l >= 0) {
+                    token = base + j0 + l;                        // (rounding may leave the last one below the target)
+                    tz = __shfl_sync(kFull, x, l);
+                }
+                if (above) break;
+                at0 = __shfl_sync(kFull, at, 31);
             }
         }
         if (!EXACT) {
-            const bool any = __syncthreads_or(close);
-            // (every block decides for the cluster: one more exchange)
-            if (threadIdx.x < ctas) remote_u32(&s.count[n_turn][rank], threadIdx.x, any);
-            cluster_meet();
-            int sum = 0;
-            for (int r = 0; r < ctas; ++r) sum += s.count[n_turn][r];
-            n_turn ^= 1;
-            if (sum > 0) return false;
+            // (the block that holds the target decides for the cluster)
+            const unsigned long long* got = all_to_all(__syncthreads_or(close) != 0);
+            int sum_close = 0;
+            for (int r = 0; r < ctas; ++r) sum_close += static_cast<int>(got[r]);
+            if (sum_close > 0) return false;
         }
-        if (token >= 0) {
+        if (token >= 0 && lane() == 0) {
             const double x = (static_cast<double>(tz) - static_cast<double>(top)) * inv_t;
+            // fp32 weights have the largest logit's own in common, which rounding leaves next to 1
+            const double common = EXACT ? 0.0 : 0.69314718055994531 * static_cast<double>(octaves(top));
             a.token[row] = token;
-            if (a.logp) a.logp[row] = static_cast<float>(x - log(whole));
-            if (a.logp_kept) a.logp_kept[row] = static_cast<float>(x - log(kept));
-            if (a.n_kept) a.n_kept[row] = n;
+            if (a.logp) a.logp[row] = static_cast<float>(x + common - log(whole));
+            if (a.logp_kept) a.logp_kept[row] = static_cast<float>(x + common - log(kept));
+            if (a.n_kept) a.n_kept[row] = n_kept;
         }
         return true;
     }
 
+    // Takes out of shared memory what `keep` refuses; what remains goes by the rest.
+    template <typename F>
+    __device__ __forceinline__ void reduce_to(int n, F keep) {
+        my_n = 0;
+        for (int j = 0; j < per; ++j) {
+            const float x = one(z + j);
+            if (keep(x, first + j)) my_n += x > -INFINITY;
+            else z[j] = static_cast<T>(-INFINITY);
+        }
+        n_all = n;
+        cut_down = true;
+        list_lo = list_hi = 0.f;
+        __syncwarp();                                             // (pick reads the entries of its warp's other lanes)
+    }
+
+    // floor: entries below it are not allowed (min-p).
     template <bool EXACT>
-    __device__ __forceinline__ bool draw(const SampleArgs& a, int row, const SampleRule& rule, Cut cut, float u) {
-        if (rule.top_k > 0 && !shorten<EXACT, false>(cut, rule.top_k, 0.0)) return false;
-        if (rule.top_p < 1.0 && !shorten<EXACT, true>(cut, 0, rule.top_p)) return false;
-        return pick<EXACT>(a, row, cut, u);
+    __device__ __forceinline__ bool draw(const SampleArgs& a, int row, const SampleRule& rule, float floor, int top_i, float my_top, int valid, float u) {
+        const bool search = rule.top_k > 0 || rule.top_p < 1.0;
+        Cut cut{kLowest, 0x7fffffff};                             // (every entry in [lo, hi))
+        int n_kept = n_all;
+        double all = -1.0;
+        if (!search || floor > -INFINITY) {
+            // mass of all entries, and of those >= floor
+            const float at[kTau] = {floor, INFINITY};
+            const Tally mine = floor > -INFINITY ? weigh<EXACT, true, false>(at) : weigh<EXACT, false, false>(at);
+            const Tally v = exchange(mine);
+            whole = v.whole;
+            lo = hi = floor;
+            my_lo = my_hi = 0;
+            my_m = floor > -INFINITY ? mine.m[0] : mine.whole;
+            n_kept = floor > -INFINITY ? v.c[0] : n_all;
+            if (rule.temperature == 0.f) {
+                if (top_i >= first && top_i < first + per) {      // the one entry is known; its mass is what all have in common
+                    const double common = EXACT ? 0.0 : 0.69314718055994531 * static_cast<double>(octaves(top));
+                    a.token[row] = top_i;
+                    if (a.logp) a.logp[row] = static_cast<float>(common - log(whole));
+                    if (a.logp_kept) a.logp_kept[row] = 0.f;
+                    if (a.n_kept) a.n_kept[row] = 1;
+                }
+                return true;
+            }
+            if (!search) return pick<EXACT>(a, row, cut, n_kept, u);
+            all = whole;
+            reduce_to(n_kept, [&](float x, int) { return x >= floor; });
+        }
+        double target = 0.0, bound = 0.0;
+        bool done = false;
+        if (rule.top_k > 0) {
+            const bool again = EXACT && list_lo < list_hi;        // the interval that the fp32 pass has found
+            const float above = again ? list_hi : INFINITY, below = again ? list_lo : reached_by(rule.top_k, my_top, valid, a.V);
+            if (!enclose<EXACT, false>(rule.top_k, 0.0, 0.f, above, below, &target, &bound)) return false;
+            if (all < 0.0) all = whole;
+            const int total = n_lo - n_hi;
+            if (total <= kList) {
+                // where all of the first k are in the list, top-p is decided there too
+                sort_list(total);
+                done = rule.top_p < 1.0 && n_hi == 0;
+                if (done ? !cut_list<EXACT, true>(total, rule.top_k, rule.top_p, 0.0, 0.0, &cut, &n_kept)
+                         : !cut_list<EXACT, false>(total, rule.top_k, 0.0, 0.0, 0.0, &cut, &n_kept)) return false;
+            } else if (!cut_ties<EXACT, false>(rule.top_k, 0.0, 0.0, &cut, &n_kept)) return false;
+            if (rule.top_p < 1.0 && !done)
+                reduce_to(n_kept, [&](float x, int i) { return x >= hi || (x >= lo && cut.keeps(x, i)); });
+        }
+        if (rule.top_p < 1.0 && !done) {
+            const bool again = EXACT && list_lo < list_hi;
+            const float octave = 0.69314718f / static_cast<float>(inv_t);
+            const float above = again ? list_hi : top - 2.f * octave, below = again ? list_lo : top - 10.f * octave;
+            if (!enclose<EXACT, true>(0, rule.top_p, rule.quantile, above, below, &target, &bound)) return false;
+            const int total = n_lo - n_hi;
+            if (total <= kList) {
+                sort_list(total);
+                if (!cut_list<EXACT, true>(total, 0x7fffffff - kList, 0.0, target, bound, &cut, &n_kept)) return false;
+            } else if (!cut_ties<EXACT, true>(0, target, bound, &cut, &n_kept)) return false;
+        }
+        if (all >= 0.0) whole = all;
+        return pick<EXACT>(a, row, cut, n_kept, u);
     }
 };
 
+// The block's entries to shared memory: by one asynchronous copy where they begin at 16 bytes, -inf behind the row's end.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ SampleArgs a, int per, int ctas) {
+__device__ __forceinline__ void fetch(Shared& s, T* z, const T* src, int n, int share, const SampleArgs& a) {
+    const bool bulk = reinterpret_cast<uintptr_t>(src) % 16 == 0;
+    const int whole = bulk ? n * static_cast<int>(sizeof(T)) / 16 * 16 / static_cast<int>(sizeof(T)) : 0;
+    if (threadIdx.x == 0) {
+        if (whole > 0) {
+            ptx::mbar_arrive_expect_tx(&s.bar, whole * sizeof(T));
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_u32(z)),
+                         "l"(src), "r"(static_cast<uint32_t>(whole * sizeof(T))), "r"(ptx::smem_u32(&s.bar)) : "memory");
+        }
+    }
+    if (!bulk) {
+#pragma unroll 8
+        for (int i = threadIdx.x; i < n; i += kThreads) z[i] = src[i];
+    } else if (whole + static_cast<int>(threadIdx.x) < n) {
+        z[whole + threadIdx.x] = src[whole + threadIdx.x];       // at most seven
+    }
+    for (int i = n + threadIdx.x; i < share; i += kThreads) z[i] = static_cast<T>(-INFINITY);
+    __syncthreads();
+    if (whole > 0 && !ptx::mbar_wait(&s.bar, 0, kWaitBudgetCycles)) atomicOr(a.status, kStatusTimeout);
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ SampleArgs a, int per, int ctas) {
     __shared__ Shared s;
     extern __shared__ __align__(16) unsigned char raw[];
     T* z = reinterpret_cast<T*>(raw);
@@ -433,56 +708,71 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Sam
         }
         return;
     }
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // (the blocks of the cluster have begun: see below)
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(&s.bar, 1);
+        ptx::mbar_init(&s.mail[0], 1);
+        ptx::mbar_init(&s.mail[1], 1);
+        ptx::fence_barrier_init();
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // the block has begun and can take messages
     const SampleRule rule = a.rules[role];
     const int share = kThreads * per, begin = rank * share;
-    const T* src = static_cast<const T*>(a.logits) + row * a.ld + begin;
     const int n = a.V - begin < 0 ? 0 : a.V - begin < share ? a.V - begin : share;
-    for (int i = threadIdx.x; i < share; i += kThreads) z[i] = i < n ? src[i] : static_cast<T>(-INFINITY);
-    __syncthreads();
-    Row<T> r{s, z, per, ctas, rank, begin + static_cast<int>(threadIdx.x) * per, 0, 0, 0.f, 0.0, 0.f, 0.f, a.V};
+    fetch(s, z, static_cast<const T*>(a.logits) + row * a.ld + begin, n, share, a);
+    const int first = begin + static_cast<int>(threadIdx.x) * per;
+    Row<T> r{s, z + threadIdx.x * per, per, ctas, rank, first, a.status, 0};
 
-    // largest logit, the first of equal ones; a NaN makes it NaN
-    float top = -INFINITY;
-    int top_i = 0x7fffffff;
-    bool bad = false;
-    for (int j = 0; j < per; ++j) {
-        const float x = r.at(j);
-        bad |= !(x < INFINITY);
-        if (x > top) { top = x; top_i = r.first + j; }
+    // largest logit (NaN if one is NaN), and for T = 0 the first of equal ones; entries above -inf
+    float my_top = -INFINITY;
+    int finite = 0;
+    for (int j = 0; j < per; j += 2) {
+        const float2 v = pair(r.z + j);
+        my_top = max_nan(my_top, max_nan(v.x, v.y));
+        finite += (v.x > -INFINITY) + (v.y > -INFINITY);
     }
+    r.my_n = finite;
+    float top = my_top;
+    int top_i = 0x7fffffff;
+    if (rule.temperature == 0.f)
+        for (int j = per - 1; j >= 0; --j) top_i = one(r.z + j) == top ? first + j : top_i;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         const float v = __shfl_xor_sync(kFull, top, o);
         const int i = __shfl_xor_sync(kFull, top_i, o);
-        if (v > top || (v == top && i < top_i)) { top = v; top_i = i; }
+        top_i = v > top || (v == top && i < top_i) ? i : top_i;
+        top = max_nan(top, v);
     }
-    if (__any_sync(kFull, bad)) top = NAN;
-    if (lane == 0) { s.warp_z[warp] = top; s.warp_i[warp] = top_i; }
+    finite = __reduce_add_sync(kFull, finite);
+    if (lane == 0) { s.warp_z[warp] = top; s.warp_i[warp] = top_i; s.warp_n[warp] = finite; }
     __syncthreads();
     top = s.warp_z[0];
     top_i = s.warp_i[0];
-    bad = !(top == top);
+    finite = s.warp_n[0];
     for (int w = 1; w < kWarps; ++w) {
         const float v = s.warp_z[w];
-        bad |= !(v == v);
-        if (v > top) { top = v; top_i = s.warp_i[w]; }
+        top_i = v > top ? s.warp_i[w] : top_i;
+        top = max_nan(top, v);
+        finite += s.warp_n[w];
     }
     __syncwarp();
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");     // before the first write to another block
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");     // before the first message
+    r.expect(2 * ctas);
     if (threadIdx.x < ctas) {
-        remote_u32(&s.best_z[0][rank], threadIdx.x, __float_as_uint(bad ? NAN : top));
-        remote_u32(&s.best_i[0][rank], threadIdx.x, top_i);
+        send(r.box(2 * rank), r.mail(), threadIdx.x, static_cast<unsigned long long>(__float_as_uint(top)) << 32 | static_cast<unsigned>(top_i));
+        send(r.box(2 * rank + 1), r.mail(), threadIdx.x, static_cast<unsigned>(finite));
     }
-    cluster_meet();
+    const unsigned long long* got = r.box(0);
+    r.receive();
     top = -INFINITY;
-    bad = false;
+    r.n_all = 0;
     for (int q = 0; q < ctas; ++q) {
-        const float v = s.best_z[0][q];
-        bad |= !(v == v);
-        if (v > top) { top = v; top_i = s.best_i[0][q]; }
+        const float v = __uint_as_float(static_cast<unsigned>(got[2 * q] >> 32));
+        top_i = v > top ? static_cast<int>(got[2 * q] & 0xffffffffu) : top_i;
+        top = max_nan(top, v);
+        r.n_all += static_cast<int>(got[2 * q + 1]);
     }
-    if (bad || !(top > -INFINITY)) {                              // NaN, +inf or nothing but -inf
+    if (!(top > -INFINITY && top < INFINITY)) {                   // NaN, +inf or nothing but -inf
         if (rank == 0 && threadIdx.x == 0) {
             a.token[row] = -1;
             if (a.logp) a.logp[row] = NAN;
@@ -493,25 +783,40 @@ __global__ void __launch_bounds__(kThreads) k_sample(const __grid_constant__ Sam
     }
     r.top = top;
     r.inv_t = rule.inv_t;
-    const double c = 1.4426950408889634 * rule.inv_t;
-    r.c_hi = static_cast<float>(c);
-    r.c_lo = static_cast<float>(c - static_cast<double>(r.c_hi));
-    Cut cut{-INFINITY, -1};                                       // every entry above -inf
+    r.c64 = 1.4426950408889634 * rule.inv_t;
+    r.c = static_cast<float>(r.c64);
+    r.top_c = top * r.c;
+    r.list_lo = r.list_hi = 0.f;
+    r.cut_down = false;
+    const int n_all = r.n_all, my_n = r.my_n;
+    float floor = -INFINITY;
     SampleRule run = rule;
     if (rule.temperature == 0.f) {
-        cut = Cut{top, top_i};                                    // (one entry is kept)
         run.top_k = 0;
         run.top_p = 1.0;
     } else if (rule.log_min_p > -INFINITY) {
         // the lowest logit with x >= log min_p
-        double want = static_cast<double>(top) + rule.log_min_p / rule.inv_t;
-        float least = want > -3.4e38 ? static_cast<float>(want) : -3.402823466e38f;
+        const double want = static_cast<double>(top) + rule.log_min_p / rule.inv_t;
+        floor = want > -3.4e38 ? static_cast<float>(want) : kLowest;
         auto passes = [&](float v) { return (static_cast<double>(v) - static_cast<double>(top)) * rule.inv_t >= rule.log_min_p; };
-        for (int k = 0; k < 4 && least > -3.402823466e38f && passes(nextafterf(least, -INFINITY)); ++k) least = nextafterf(least, -INFINITY);
-        for (int k = 0; k < 4 && least < top && !passes(least); ++k) least = nextafterf(least, INFINITY);
-        cut = Cut{least + 0.f, 0x7fffffff};
+        for (int k = 0; k < 4 && floor > kLowest && passes(nextafterf(floor, -INFINITY)); ++k) floor = nextafterf(floor, -INFINITY);
+        for (int k = 0; k < 4 && floor < top && !passes(floor); ++k) floor = nextafterf(floor, INFINITY);
     }
-    if (!r.template draw<false>(a, row, run, cut, u)) r.template draw<true>(a, row, run, cut, u);
+    // (fp32 weights have 2^(rounding of top_c) in common, which has to stay near 1)
+    const bool fits = fabsf(r.top_c) <= 0x1p20f;
+    if (fits && r.template draw<false>(a, row, run, floor, top_i, my_top, n, u)) return;
+    __syncthreads();
+    if (threadIdx.x < 32) s.exp2_table[threadIdx.x] = exp2(threadIdx.x / 32.0);
+    if (r.cut_down) {
+        const T* src = static_cast<const T*>(a.logits) + row * a.ld + begin;
+        for (int i = threadIdx.x; i < n; i += kThreads) z[i] = src[i];
+        r.cut_down = false;
+        r.list_lo = r.list_hi = 0.f;
+        r.n_all = n_all;
+        r.my_n = my_n;
+    }
+    __syncthreads();
+    r.template draw<true>(a, row, run, floor, top_i, my_top, n, u);
 }
 
 }  // namespace
@@ -522,8 +827,8 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, cudaStream_t st) {
     int ctas = 1, per = 0;
     for (;; ctas *= 2) {
         per = (a.V + kThreads * ctas - 1) / (kThreads * ctas);
-        // a thread's entries begin at different banks: an odd number of words apart
-        per = bf16 ? ((per + 1) / 2 | 1) * 2 : per | 1;
+        // entries are read in pairs, and the threads' first ones lie an odd number of pairs apart: at different banks
+        per = ((per + 1) / 2 | 1) * 2;
         if (ctas == kMaxCluster || static_cast<long long>(per) * kThreads * width <= 80 * 1024) break;
     }
     const int bytes = per * kThreads * width;

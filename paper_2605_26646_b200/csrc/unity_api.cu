@@ -960,6 +960,16 @@ int norm_args(unity_ctx* ctx, const unity_norm_rows* r, int res_type, NormArgs& 
     return UNITY_OK;
 }
 
+// x with Phi(x) = p, for a first guess (bisection).
+float normal_quantile(double p) {
+    double lo = -6.0, hi = 6.0;
+    for (int i = 0; i < 30; ++i) {
+        const double mid = 0.5 * (lo + hi);
+        if (0.5 * erfc(-mid * 0.70710678118654752) < p) lo = mid; else hi = mid;
+    }
+    return static_cast<float>(lo);
+}
+
 // Memory that a clipping call reads or writes; `w`: writes.
 struct ClipRange { uintptr_t from, to; int tensor; bool w; };
 int clip_check(unity_ctx* ctx, int n, const unity_tensor* t, int K, bool scale) {
@@ -1933,6 +1943,7 @@ int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, 
         s.inv_t = r.temperature > 0.f ? 1.0 / static_cast<double>(r.temperature) : 1.0;
         s.top_k = r.top_k > 0 && r.top_k < V ? r.top_k : 0;
         s.top_p = static_cast<double>(r.top_p);
+        s.quantile = normal_quantile(s.top_p);
         s.log_min_p = r.min_p > 0.f ? log(static_cast<double>(r.min_p)) : -INFINITY;
     }
     if (n_rows == 0) return UNITY_OK;
