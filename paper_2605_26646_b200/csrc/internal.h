@@ -701,6 +701,7 @@ struct SampleRule {
     double inv_t, log_min_p;             // -inf: off
     double top_p;                        // >= 1: off
     float quantile;                      // of the normal distribution at top_p
+    int search;                          // the rule cuts entries off
 };
 struct SampleArgs {
     const void* logits;
@@ -715,6 +716,7 @@ struct SampleArgs {
     int* status;
     SampleRule rules[UNITY_MAX_ROLES];
 };
-cudaError_t launch_sample(const SampleArgs& a, bool bf16, cudaStream_t stream);
+// any_search, any_other: there are rules that cut entries off, and others
+cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_other, int sm_count, cudaStream_t stream, int* n_launches);
 
 }  // namespace unity

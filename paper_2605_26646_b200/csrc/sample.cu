@@ -1,6 +1,8 @@
 // Next tokens from logits and given uniform numbers (unity_sample): temperature, top-k, top-p and min-p by a rule per role.
 //
-// A cluster of blocks holds a row in shared memory: the logits cross HBM once and every further pass over them stays on chip.
+// Rows whose rule cuts nothing off take one pass over the logits (k_sample_stream, below); the others are searched (k_sample).
+//
+// k_sample: a cluster of blocks holds a row in shared memory: the logits cross HBM once and every further pass over them stays on chip.
 // Thread order is index order (a thread owns `per` consecutive entries), so running masses are sums over threads.
 //
 // With x = (z - max z) / T and e = exp x, what is kept is a prefix of the entries in the order (logit falling, index rising),
@@ -20,16 +22,16 @@ namespace unity {
 namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
-constexpr int kList = 2 * kThreads;          // entries sorted at most, two per thread
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 16;
+constexpr int kList = 1024;                  // entries sorted at most
 constexpr int kTau = 2;                      // thresholds of a pass
 constexpr float kLowest = -3.402823466e38f;
-// fp32: e = ex2(z c - max z c), c = log2(e) / T, is off by 2^-22 of itself and by two roundings of its argument, 2^-24 |x| each (that
-// of max z c is common to all entries and taken out of the sums), whose mean under the distribution is at most 18 octaves at
-// 2^18 entries: 1.5e-6; four values are added in fp32, the rest in fp64: 1.8e-7.  Both sides of a comparison carry that: 2^-18
-// of the whole mass.  fp64: 2^-48.
-constexpr double kSlackFast = 0x1p-18, kSlackExact = 0.0;
+// fp32: e = ex2(z c - r), c = log2(e) / T, is off by 2^-22 of itself and, but for what all entries have in common, by the rounding of
+// its argument and of c, 2^-24 |x| octaves each.  The mean of |x| under a distribution over 2^18 entries whose likeliest has p is at
+// most h(p) + 18 (1 - p) + log2 p < 14: 1.16e-6.  8 or 16 values are added pairwise in fp32, the rest in fp64 or two parts: 2.4e-7.
+// Both sides of a comparison carry that: 3.3e-6 of the whole mass.  fp64: 2^-48.
+constexpr double kSlackFast = 3.3e-6, kSlackExact = 0.0;
 
 struct Tally {                               // of the entries: mass of all, mass and number at or above each threshold
     double whole, m[kTau];
@@ -45,7 +47,7 @@ struct Shared {
     unsigned long long box[2][kMaxCluster * kWarps];   // messages of every block, or of every warp
     Tally warp[kWarps];
     float warp_z[kWarps];
-    int warp_i[kWarps], warp_n[kWarps];
+    int warp_n[kWarps];
     int scan[kWarps];
     double scan_m[kWarps];
     int found;
@@ -68,6 +70,12 @@ __device__ __forceinline__ bool mail_arrived(uint64_t* mail, unsigned parity) {
         "selp.b32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(ptx::smem_u32(mail)), "r"(parity) : "memory");
     return ok != 0;
+}
+__device__ __forceinline__ void wait_mail(uint64_t* mail, unsigned parity, int* status) {
+    if (mail_arrived(mail, parity)) return;
+    const long long t0 = clock64();
+    while (!mail_arrived(mail, parity))
+        if (clock64() - t0 > kWaitBudgetCycles) { atomicOr(status, kStatusTimeout); break; }
 }
 __device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
@@ -111,6 +119,44 @@ __device__ __forceinline__ float value_of(unsigned k) {
     return __uint_as_float(k >= 0x80000000u ? k - 0x80000000u : 0x80000000u | (0x80000000u - k));
 }
 
+// exp((v - top) / T) in fp64 by a table (2^(j/32)) and the exponential series on a 64th of an octave: 2^k 2^(j/32) (1 + p), off
+// by 2^-48; c64 = log2(e) / T.
+__device__ __forceinline__ double slow_weight(float v, float top, double c64, double inv_t, const double* table) {
+    const double d = static_cast<double>(v) - static_cast<double>(top), y = d * c64;    // (octaves; the largest logit's e is 1)
+    if (!(y > -1020.0)) return v == -INFINITY ? 0.0 : exp(d * inv_t);
+    constexpr double kShift = 0x1.8p52 / 32.0, kLn2 = 0.69314718055994531;              // the sum with kShift rounds to 32nds
+    const double t = y + kShift, r = y - (t - kShift);
+    const int n = __double2loint(t);                             // 32 k + j
+    const double p = r * (kLn2 + r * (kLn2 * kLn2 / 2 + r * (kLn2 * kLn2 * kLn2 / 6 +
+                          r * (kLn2 * kLn2 * kLn2 * kLn2 / 24 + r * (kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 120)))));
+    const double b = table[n & 31];
+    const double scaled = __hiloint2double(__double2hiint(b) + ((n >> 5) << 20), __double2loint(b));
+    return fma(scaled, p, scaled);
+}
+
+__device__ __forceinline__ void put_row(const SampleArgs& a, int row, int token, double logp, double logp_kept, int n_kept) {
+    a.token[row] = token;
+    if (a.logp) a.logp[row] = static_cast<float>(logp);
+    if (a.logp_kept) a.logp_kept[row] = static_cast<float>(logp_kept);
+    if (a.n_kept) a.n_kept[row] = n_kept;
+}
+__device__ __forceinline__ void no_distribution(const SampleArgs& a, int row) { put_row(a, row, -1, NAN, NAN, 0); }
+// The row's rule and number.  False: a row that is masked or has a bad role or number; its outputs are written here.
+__device__ __forceinline__ bool row_begins(const SampleArgs& a, int row, int rank, SampleRule& rule, float& u) {
+    const bool on = a.row_mask == nullptr || a.row_mask[row] != 0;
+    const int role = a.row_role ? a.row_role[row] : 0;
+    u = on ? a.u[row] : 0.f;
+    if (on && role >= 0 && role < a.n_roles && u >= 0.f && u < 1.f) {
+        rule = a.rules[role];
+        return true;
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+        put_row(a, row, -1, 0.0, 0.0, 0);
+        if (on) atomicOr(a.status, kStatusBadIndex);
+    }
+    return false;
+}
+
 // The kept entries end with (z, i).
 struct Cut {
     float z;
@@ -143,19 +189,7 @@ struct Row {
     // Weight of an entry.  -inf has none.
     __device__ __forceinline__ float octaves(float v) const { return fmaf(v, c, -top_c); }
     __device__ __forceinline__ float fast(float v) const { return ptx::ex2(octaves(v)); }
-    // exp in fp64 by a table (2^(j/32)) and the exponential series on a 64th of an octave: 2^k 2^(j/32) (1 + p), off by 2^-48.
-    __device__ __forceinline__ double slow(float v) const {
-        const double d = static_cast<double>(v) - static_cast<double>(top), y = d * c64;   // (octaves; the largest logit's e is 1)
-        if (!(y > -1020.0)) return v == -INFINITY ? 0.0 : exp(d * inv_t);
-        constexpr double kShift = 0x1.8p52 / 32.0, kLn2 = 0.69314718055994531;  // the sum with kShift rounds to 32nds
-        const double t = y + kShift, r = y - (t - kShift);
-        const int n = __double2loint(t);                         // 32 k + j
-        const double p = r * (kLn2 + r * (kLn2 * kLn2 / 2 + r * (kLn2 * kLn2 * kLn2 / 6 +
-                              r * (kLn2 * kLn2 * kLn2 * kLn2 / 24 + r * (kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 120)))));
-        const double b = s.exp2_table[n & 31];
-        const double scaled = __hiloint2double(__double2hiint(b) + ((n >> 5) << 20), __double2loint(b));
-        return fma(scaled, p, scaled);
-    }
+    __device__ __forceinline__ double slow(float v) const { return slow_weight(v, top, c64, inv_t, s.exp2_table); }
     template <bool EXACT>
     __device__ __forceinline__ double weight(float v) const { return EXACT ? slow(v) : static_cast<double>(fast(v)); }
 
@@ -165,15 +199,7 @@ struct Row {
     __device__ __forceinline__ void expect(int words) const {
         if (threadIdx.x == 0) ptx::mbar_arrive_expect_tx(mail(), 8 * words);
     }
-    __device__ __forceinline__ void receive() {
-        const unsigned parity = turn >> 1 & 1;
-        if (!mail_arrived(mail(), parity)) {
-            const long long t0 = clock64();
-            while (!mail_arrived(mail(), parity))
-                if (clock64() - t0 > kWaitBudgetCycles) { atomicOr(status, kStatusTimeout); break; }
-        }
-        ++turn;
-    }
+    __device__ __forceinline__ void receive() { wait_mail(mail(), turn >> 1 & 1, status); ++turn; }
     // A word of every block to every block; returns the other side's place of it.  (Behind a barrier of the block.)
     __device__ __forceinline__ const unsigned long long* all_to_all(unsigned long long v) {
         const unsigned long long* got = box(0);
@@ -403,11 +429,11 @@ struct Row {
         for (int i = total + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
         receive();
         __syncthreads();
-        // bitonic: a thread compares one pair per step; up to 32 apart the pairs of a warp are the warp's own
+        // bitonic: a thread compares up to two pairs per step; up to 32 apart the pairs of a warp are the warp's own
         for (int k = 1; k <= log_size; ++k)
             for (int j = k - 1; j >= 0; --j) {
-                const int i = (threadIdx.x >> j << (j + 1)) | (threadIdx.x & ((1 << j) - 1));
-                if (i < size) {
+                for (int t = threadIdx.x; t < size / 2; t += kThreads) {
+                    const int i = (t >> j << (j + 1)) | (t & ((1 << j) - 1));
                     const unsigned long long a = s.list[i], b = s.list[i + (1 << j)];
                     if ((a > b) == ((i >> k & 1) == 0)) { s.list[i] = b; s.list[i + (1 << j)] = a; }
                 }
@@ -420,20 +446,23 @@ struct Row {
     // k_want and a share the target is that share of the first k_want's mass.
     template <bool EXACT, bool BY_MASS>
     __device__ __forceinline__ bool cut_list(int total, int k_want, double share, double target, double bound, Cut* cut, int* n_kept) {
-        const int i0 = 2 * threadIdx.x;
-        double e[2];
+        constexpr int kEach = kList / kThreads;
+        const int i0 = kEach * threadIdx.x;
+        double e[kEach], sum = 0.0;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < kEach; ++h) {
             e[h] = BY_MASS && i0 + h < total && n_hi + i0 + h < k_want ? weight<EXACT>(value_of(~static_cast<unsigned>(s.list[i0 + h] >> 32))) : 0.0;
+            sum += e[h];
+        }
         double before = 0.0;
         if (BY_MASS) {
-            const double run = warp_scan(e[0] + e[1], lane());
+            const double run = warp_scan(sum, lane());
             if (lane() == 31) s.scan_m[warp()] = run;
             __syncthreads();
             const double w = lane() < kWarps ? s.scan_m[lane()] : 0.0;
             const double upto = warp_scan(w, lane());
             before = __shfl_sync(kFull, upto, warp() ? warp() - 1 : 0);
-            before = (warp() ? before : 0.0) + (run - e[0] - e[1]);
+            before = (warp() ? before : 0.0) + (run - sum);
             if (share > 0.0) {
                 const double all = __shfl_sync(kFull, upto, kWarps - 1);
                 target = share * all;
@@ -443,11 +472,12 @@ struct Row {
         int kept = 0;
         bool close = false;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kEach; ++h) {
             if (i0 + h >= total || n_hi + i0 + h >= k_want) continue;
-            const double m = m_hi + before + (h ? e[0] : 0.0);
+            const double m = m_hi + before;
             kept += !BY_MASS || m < target;
             close |= BY_MASS && !EXACT && fabs(m - target) <= bound && i0 + h + n_hi > 0;
+            before += e[h];
         }
         const int warp_kept = __reduce_add_sync(kFull, kept);
         if (lane() == 0) s.scan[warp()] = warp_kept;
@@ -577,10 +607,7 @@ struct Row {
             const double x = (static_cast<double>(tz) - static_cast<double>(top)) * inv_t;
             // fp32 weights have the largest logit's own in common, which rounding leaves next to 1
             const double common = EXACT ? 0.0 : 0.69314718055994531 * static_cast<double>(octaves(top));
-            a.token[row] = token;
-            if (a.logp) a.logp[row] = static_cast<float>(x + common - log(whole));
-            if (a.logp_kept) a.logp_kept[row] = static_cast<float>(x + common - log(kept));
-            if (a.n_kept) a.n_kept[row] = n_kept;
+            put_row(a, row, token, x + common - log(whole), x + common - log(kept), n_kept);
         }
         return true;
     }
@@ -602,31 +629,20 @@ struct Row {
 
     // floor: entries below it are not allowed (min-p).
     template <bool EXACT>
-    __device__ __forceinline__ bool draw(const SampleArgs& a, int row, const SampleRule& rule, float floor, int top_i, float my_top, int valid, float u) {
+    __device__ __forceinline__ bool draw(const SampleArgs& a, int row, const SampleRule& rule, float floor, float my_top, int valid, float u) {
         const bool search = rule.top_k > 0 || rule.top_p < 1.0;
         Cut cut{kLowest, 0x7fffffff};                             // (every entry in [lo, hi))
         int n_kept = n_all;
         double all = -1.0;
-        if (!search || floor > -INFINITY) {
+        if (floor > -INFINITY) {
             // mass of all entries, and of those >= floor
             const float at[kTau] = {floor, INFINITY};
-            const Tally mine = floor > -INFINITY ? weigh<EXACT, true, false>(at) : weigh<EXACT, false, false>(at);
-            const Tally v = exchange(mine);
+            const Tally mine = weigh<EXACT, true, false>(at), v = exchange(mine);
             whole = v.whole;
             lo = hi = floor;
             my_lo = my_hi = 0;
-            my_m = floor > -INFINITY ? mine.m[0] : mine.whole;
-            n_kept = floor > -INFINITY ? v.c[0] : n_all;
-            if (rule.temperature == 0.f) {
-                if (top_i >= first && top_i < first + per) {      // the one entry is known; its mass is what all have in common
-                    const double common = EXACT ? 0.0 : 0.69314718055994531 * static_cast<double>(octaves(top));
-                    a.token[row] = top_i;
-                    if (a.logp) a.logp[row] = static_cast<float>(common - log(whole));
-                    if (a.logp_kept) a.logp_kept[row] = 0.f;
-                    if (a.n_kept) a.n_kept[row] = 1;
-                }
-                return true;
-            }
+            my_m = mine.m[0];
+            n_kept = v.c[0];
             if (!search) return pick<EXACT>(a, row, cut, n_kept, u);
             all = whole;
             reduce_to(n_kept, [&](float x, int) { return x >= floor; });
@@ -689,25 +705,15 @@ __device__ __forceinline__ void fetch(Shared& s, T* z, const T* src, int n, int 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ SampleArgs a, int per, int ctas) {
+__global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ SampleArgs a, int per, int ctas) {
     __shared__ Shared s;
     extern __shared__ __align__(16) unsigned char raw[];
     T* z = reinterpret_cast<T*>(raw);
     const int rank = ctas > 1 ? ptx::cluster_ctarank() : 0, row = blockIdx.x / ctas;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const bool on = a.row_mask == nullptr || a.row_mask[row] != 0;
-    const int role = a.row_role ? a.row_role[row] : 0;
-    const float u = on ? a.u[row] : 0.f;
-    if (!on || role < 0 || role >= a.n_roles || !(u >= 0.f && u < 1.f)) {     // (the same in every block of the cluster)
-        if (rank == 0 && threadIdx.x == 0) {
-            a.token[row] = -1;
-            if (a.logp) a.logp[row] = 0.f;
-            if (a.logp_kept) a.logp_kept[row] = 0.f;
-            if (a.n_kept) a.n_kept[row] = 0;
-            if (on) atomicOr(a.status, kStatusBadIndex);
-        }
-        return;
-    }
+    SampleRule rule;
+    float u;
+    if (!row_begins(a, row, rank, rule, u) || !rule.search) return;           // (the same in every block of the cluster)
     if (threadIdx.x == 0) {
         ptx::mbar_init(&s.bar, 1);
         ptx::mbar_init(&s.mail[0], 1);
@@ -716,14 +722,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
     }
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");   // the block has begun and can take messages
-    const SampleRule rule = a.rules[role];
     const int share = kThreads * per, begin = rank * share;
     const int n = a.V - begin < 0 ? 0 : a.V - begin < share ? a.V - begin : share;
     fetch(s, z, static_cast<const T*>(a.logits) + row * a.ld + begin, n, share, a);
     const int first = begin + static_cast<int>(threadIdx.x) * per;
     Row<T> r{s, z + threadIdx.x * per, per, ctas, rank, first, a.status, 0};
 
-    // largest logit (NaN if one is NaN), and for T = 0 the first of equal ones; entries above -inf
+    // largest logit (NaN if one is NaN); entries above -inf
     float my_top = -INFINITY;
     int finite = 0;
     for (int j = 0; j < per; j += 2) {
@@ -733,52 +738,24 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
     }
     r.my_n = finite;
     float top = my_top;
-    int top_i = 0x7fffffff;
-    if (rule.temperature == 0.f)
-        for (int j = per - 1; j >= 0; --j) top_i = one(r.z + j) == top ? first + j : top_i;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const float v = __shfl_xor_sync(kFull, top, o);
-        const int i = __shfl_xor_sync(kFull, top_i, o);
-        top_i = v > top || (v == top && i < top_i) ? i : top_i;
-        top = max_nan(top, v);
-    }
+    for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
     finite = __reduce_add_sync(kFull, finite);
-    if (lane == 0) { s.warp_z[warp] = top; s.warp_i[warp] = top_i; s.warp_n[warp] = finite; }
+    if (lane == 0) { s.warp_z[warp] = top; s.warp_n[warp] = finite; }
     __syncthreads();
     top = s.warp_z[0];
-    top_i = s.warp_i[0];
     finite = s.warp_n[0];
-    for (int w = 1; w < kWarps; ++w) {
-        const float v = s.warp_z[w];
-        top_i = v > top ? s.warp_i[w] : top_i;
-        top = max_nan(top, v);
-        finite += s.warp_n[w];
-    }
+    for (int w = 1; w < kWarps; ++w) { top = max_nan(top, s.warp_z[w]); finite += s.warp_n[w]; }
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");     // before the first message
-    r.expect(2 * ctas);
-    if (threadIdx.x < ctas) {
-        send(r.box(2 * rank), r.mail(), threadIdx.x, static_cast<unsigned long long>(__float_as_uint(top)) << 32 | static_cast<unsigned>(top_i));
-        send(r.box(2 * rank + 1), r.mail(), threadIdx.x, static_cast<unsigned>(finite));
-    }
-    const unsigned long long* got = r.box(0);
-    r.receive();
-    top = -INFINITY;
+    const unsigned long long* got = r.all_to_all(static_cast<unsigned long long>(__float_as_uint(top)) << 32 | static_cast<unsigned>(finite));
     r.n_all = 0;
     for (int q = 0; q < ctas; ++q) {
-        const float v = __uint_as_float(static_cast<unsigned>(got[2 * q] >> 32));
-        top_i = v > top ? static_cast<int>(got[2 * q] & 0xffffffffu) : top_i;
-        top = max_nan(top, v);
-        r.n_all += static_cast<int>(got[2 * q + 1]);
+        top = max_nan(top, __uint_as_float(static_cast<unsigned>(got[q] >> 32)));
+        r.n_all += static_cast<int>(got[q] & 0xffffffffu);
     }
     if (!(top > -INFINITY && top < INFINITY)) {                   // NaN, +inf or nothing but -inf
-        if (rank == 0 && threadIdx.x == 0) {
-            a.token[row] = -1;
-            if (a.logp) a.logp[row] = NAN;
-            if (a.logp_kept) a.logp_kept[row] = NAN;
-            if (a.n_kept) a.n_kept[row] = 0;
-        }
+        if (rank == 0 && threadIdx.x == 0) no_distribution(a, row);
         return;
     }
     r.top = top;
@@ -790,11 +767,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
     r.cut_down = false;
     const int n_all = r.n_all, my_n = r.my_n;
     float floor = -INFINITY;
-    SampleRule run = rule;
-    if (rule.temperature == 0.f) {
-        run.top_k = 0;
-        run.top_p = 1.0;
-    } else if (rule.log_min_p > -INFINITY) {
+    if (rule.log_min_p > -INFINITY) {
         // the lowest logit with x >= log min_p
         const double want = static_cast<double>(top) + rule.log_min_p / rule.inv_t;
         floor = want > -3.4e38 ? static_cast<float>(want) : kLowest;
@@ -804,7 +777,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
     }
     // (fp32 weights have 2^(rounding of top_c) in common, which has to stay near 1)
     const bool fits = fabsf(r.top_c) <= 0x1p20f;
-    if (fits && r.template draw<false>(a, row, run, floor, top_i, my_top, n, u)) return;
+    if (fits && r.template draw<false>(a, row, rule, floor, my_top, n, u)) return;
     __syncthreads();
     if (threadIdx.x < 32) s.exp2_table[threadIdx.x] = exp2(threadIdx.x / 32.0);
     if (r.cut_down) {
@@ -816,27 +789,352 @@ __global__ void __launch_bounds__(kThreads, 2) k_sample(const __grid_constant__ 
         r.my_n = my_n;
     }
     __syncthreads();
-    r.template draw<true>(a, row, run, floor, top_i, my_top, n, u);
+    r.template draw<true>(a, row, rule, floor, my_top, n, u);
 }
 
-}  // namespace
+// ------------------------------------------------------------------------------------------------
+// Rows whose rule leaves every entry (no top-k, top-p or min-p) and rows that take the largest logit: one pass over the logits in
+// registers, no copy in shared memory, so that more rows are in flight.  Every warp of the cluster has a run of consecutive entries,
+// in tiles of 512; a tile's masses refer to a power of two of its own next to its largest entry.  The warp whose running mass holds
+// the target reads one of its tiles again.
+// ------------------------------------------------------------------------------------------------
+constexpr int kTileEntries = 512, kPerLane = kTileEntries / 32;
+constexpr int kMaxTiles = 5;                 // of a warp
+static_assert(kMaxTiles * kMaxCluster * kWarps * kTileEntries >= UNITY_MAX_SAMPLE_V, "enough for a row");
 
-cudaError_t launch_sample(const SampleArgs& a, bool bf16, cudaStream_t st) {
-    // the fewest blocks per row (1, 2, 4, 8) whose share takes at most 80 KB, so that two blocks fit an SM
-    const int width = bf16 ? 2 : 4;
-    int ctas = 1, per = 0;
-    for (;; ctas *= 2) {
-        per = (a.V + kThreads * ctas - 1) / (kThreads * ctas);
-        // entries are read in pairs, and the threads' first ones lie an odd number of pairs apart: at different banks
-        per = ((per + 1) / 2 | 1) * 2;
-        if (ctas == kMaxCluster || static_cast<long long>(per) * kThreads * width <= 80 * 1024) break;
+struct StreamShared {
+    uint64_t mail[2];
+    unsigned long long box[2][3 * kMaxCluster * kWarps];
+    double tile_m[kWarps][kMaxTiles];        // mass of a tile, in units of 2^tile_r
+    int tile_r[kWarps][kMaxTiles];
+    double exp2_table[32];
+};
+
+template <typename T>
+struct Tile {
+    static constexpr int kVec = 16 / sizeof(T), kVecs = kPerLane / kVec;
+    float v[kPerLane];
+    static __device__ __forceinline__ int index(int base, int i) {               // of the lane's i-th entry
+        return base + (i / kVec) * (32 * kVec) + (threadIdx.x & 31) * kVec + i % kVec;
     }
-    const int bytes = per * kThreads * width;
-    void (*kernel)(SampleArgs, int, int) = bf16 ? k_sample<__nv_bfloat16> : k_sample<float>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    __device__ __forceinline__ void load(const T* row, int base, int end, bool aligned) {
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+            const int at = index(base, k * kVec);
+            if (aligned && at + kVec <= end) {
+                const uint4 w = __ldg(reinterpret_cast<const uint4*>(row + at));
+                const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (sizeof(T) == 4) v[k * kVec + q] = __uint_as_float(u[q]);
+                    else {
+                        v[k * kVec + 2 * q] = __uint_as_float(u[q] << 16);
+                        v[k * kVec + (2 * q + 1) % kVec] = __uint_as_float(u[q] & 0xffff0000u);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kVec; ++q) v[k * kVec + q] = at + q < end ? one(row + at + q) : -INFINITY;
+            }
+        }
+    }
+    __device__ __forceinline__ float largest() const {                            // NaN if one is NaN
+        float m = v[0];
+#pragma unroll
+        for (int i = 1; i < kPerLane; ++i) m = max_nan(m, v[i]);
+        return m;
+    }
+};
+__device__ __forceinline__ double times_power(double m, int e) {                  // m 2^e, 0 far below
+    return e < -1000 ? 0.0 : m * __hiloint2double((1023 + e) << 20, 0);
+}
+
+template <typename T>
+struct Stream {
+    StreamShared& s;
+    const T* row;
+    int ctas, rank, home, begin, end;        // the warp's number in the cluster and its entries [begin, end)
+    bool aligned;
+    int* status;
+    int turn;
+    float c;
+    double c64, inv_t;
+    float top;
+
+    __device__ __forceinline__ int lane() const { return threadIdx.x & 31; }
+    __device__ __forceinline__ int warp() const { return threadIdx.x >> 5; }
+    __device__ __forceinline__ uint64_t* mail() const { return &s.mail[turn & 1]; }
+    __device__ __forceinline__ unsigned long long* box(int i) const { return &s.box[turn & 1][i]; }
+    __device__ __forceinline__ void expect(int words) const {
+        if (threadIdx.x == 0) ptx::mbar_arrive_expect_tx(mail(), 8 * words);
+    }
+    __device__ __forceinline__ void receive() { wait_mail(mail(), turn >> 1 & 1, status); ++turn; }
+
+    template <bool EXACT>
+    __device__ __forceinline__ double weight(float v, int r) const {
+        return EXACT ? slow_weight(v, top, c64, inv_t, s.exp2_table) : static_cast<double>(ptx::ex2(fmaf(v, c, -static_cast<float>(r))));
+    }
+
+    // Masses of the warp's tiles.
+    template <bool EXACT>
+    __device__ __forceinline__ void weigh_tile(const Tile<T>& t, int k, float most) {
+        // (no finite entry: any unit will do)
+        const int r = EXACT ? 0 : most > -INFINITY && most < INFINITY ? static_cast<int>(ceilf(fminf(fmaxf(most * c, -1e9f), 1e9f))) : 0;
+        double m = 0.0;
+        if (EXACT) {
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) m += weight<true>(t.v[i], 0);
+        } else {
+            const float rf = static_cast<float>(r);
+            float e[kPerLane];
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) e[i] = ptx::ex2(fmaf(t.v[i], c, -rf));
+#pragma unroll
+            for (int o = kPerLane / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < o; ++i) e[i] += e[i + o];
+            m = static_cast<double>(e[0]);
+        }
+        m = warp_sum(m);
+        if (lane() == 0) { s.tile_m[warp()][k] = m; s.tile_r[warp()][k] = r; }
+    }
+
+    // Sends the warp's mass, its unit, and two more numbers; finds the warp that holds the target and, there, the token.  `tz`: its
+    // logit.  close: a comparison was too close for this arithmetic (known in that warp).
+    struct Found { int token, n; float top, tz; int top_i, unit; double whole; bool close; };
+    template <bool EXACT>
+    __device__ __forceinline__ Found locate(int tiles, float my_top, int my_top_i, int my_n, float u) {
+        __syncwarp();
+        int r = -0x40000000;
+        for (int k = 0; k < tiles; ++k)
+            if (s.tile_m[warp()][k] > 0.0) r = max(r, s.tile_r[warp()][k]);
+        double m = 0.0;
+        for (int k = 0; k < tiles; ++k)
+            if (s.tile_m[warp()][k] > 0.0) m += times_power(s.tile_m[warp()][k], s.tile_r[warp()][k] - r);
+        const int warps = ctas * kWarps;
+        expect(3 * warps);
+        if (lane() < ctas) {
+            send(box(3 * home), mail(), lane(), static_cast<unsigned long long>(__double_as_longlong(m)));
+            send(box(3 * home + 1), mail(), lane(), static_cast<unsigned long long>(static_cast<unsigned>(r)) << 32 | static_cast<unsigned>(my_n));
+            send(box(3 * home + 2), mail(), lane(), static_cast<unsigned long long>(__float_as_uint(my_top)) << 32 | static_cast<unsigned>(my_top_i));
+        }
+        const unsigned long long* got = box(0);
+        receive();
+        constexpr int kEach = kMaxCluster * kWarps / 32;
+        Found f;
+        f.token = -1;
+        f.top = -INFINITY;
+        f.top_i = 0x7fffffff;
+        f.n = 0;
+        f.unit = -0x40000000;
+        f.close = false;
+        f.tz = 0.f;
+        double part[kEach], four = 0.0;
+        int unit[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int w = lane() * kEach + i;
+            part[i] = 0.0;
+            unit[i] = -0x40000000;
+            if (w < warps) {
+                part[i] = __longlong_as_double(static_cast<long long>(got[3 * w]));
+                unit[i] = static_cast<int>(got[3 * w + 1] >> 32);
+                f.n += static_cast<int>(got[3 * w + 1] & 0xffffffffu);
+                const float v = __uint_as_float(static_cast<unsigned>(got[3 * w + 2] >> 32));
+                f.top_i = v > f.top ? static_cast<int>(got[3 * w + 2] & 0xffffffffu) : f.top_i;
+                f.top = max_nan(f.top, v);
+                f.unit = max(f.unit, unit[i]);
+            }
+        }
+        f.unit = __reduce_max_sync(kFull, f.unit);
+        f.n = __reduce_add_sync(kFull, f.n);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {                        // (the first of equal ones: lanes are in index order)
+            const float v = __shfl_down_sync(kFull, f.top, o);
+            const int i = __shfl_down_sync(kFull, f.top_i, o);
+            if (lane() + o < 32) { f.top_i = v > f.top ? i : f.top_i; f.top = max_nan(f.top, v); }
+        }
+        f.top = __shfl_sync(kFull, f.top, 0);
+        f.top_i = __shfl_sync(kFull, f.top_i, 0);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            part[i] = times_power(part[i], unit[i] - f.unit);
+            four += part[i];
+        }
+        const double upto = warp_scan(four, lane()), prior = __shfl_up_sync(kFull, upto, 1);
+        f.whole = __shfl_sync(kFull, upto, 31);
+        const double target = static_cast<double>(u) * f.whole, bound = EXACT ? kSlackExact : kSlackFast * f.whole;
+        double from = lane() ? prior : 0.0, start = 0.0, last_start = 0.0;
+        int hit = -1, last = -1;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const double to = from + part[i];
+            if (part[i] > 0.0) {
+                last = lane() * kEach + i;
+                last_start = from;
+                if (hit < 0 && to > target) { hit = last; start = from; }
+            }
+            from = to;
+        }
+        const unsigned hits = __ballot_sync(kFull, hit >= 0), lasts = __ballot_sync(kFull, last >= 0);
+        if (lasts == 0) return f;                                 // (a row without a distribution)
+        const int owner = hits ? __ffs(hits) - 1 : 31 - __clz(lasts);
+        const int holder = __shfl_sync(kFull, hits ? hit : last, owner);
+        if (holder != home) return f;
+        start = __shfl_sync(kFull, hits ? start : last_start, owner);
+        // the tile: the first that ends above the target, or the last with any mass
+        int tile = 0;
+        double at0 = start;
+        for (int k = 0; k < tiles; ++k) {
+            const double mass = s.tile_m[warp()][k] > 0.0 ? times_power(s.tile_m[warp()][k], s.tile_r[warp()][k] - f.unit) : 0.0;
+            if (!(mass > 0.0)) continue;
+            tile = k;
+            at0 = start;
+            start += mass;
+            if (start > target) break;
+        }
+        Tile<T> t;
+        t.load(row, begin + tile * kTileEntries, end, aligned);
+        f.close = fabs(at0 - target) <= bound;
+        const int shift = s.tile_r[warp()][tile] - f.unit;
+        // index order: vectors of the tile, lanes, entries of a lane
+#pragma unroll
+        for (int k = 0; k < Tile<T>::kVecs; ++k) {
+            double e[Tile<T>::kVec], sum = 0.0;
+#pragma unroll
+            for (int q = 0; q < Tile<T>::kVec; ++q) {
+                e[q] = times_power(weight<EXACT>(t.v[k * Tile<T>::kVec + q], s.tile_r[warp()][tile]), shift);
+                sum += e[q];
+            }
+            double at = at0 + warp_scan(sum, lane()) - sum;       // before the lane's entries
+            int mine = -1;
+            float z = 0.f;
+            bool over = false;
+#pragma unroll
+            for (int q = 0; q < Tile<T>::kVec; ++q) {
+                at += e[q];
+                if (e[q] > 0.0) {
+                    f.close |= fabs(at - target) <= bound;
+                    if (!over) {
+                        mine = k * Tile<T>::kVec + q;
+                        z = t.v[k * Tile<T>::kVec + q];
+                        over = at > target;
+                    }
+                }
+            }
+            const unsigned any = __ballot_sync(kFull, mine >= 0), above = __ballot_sync(kFull, over);
+            const int l = above ? __ffs(above) - 1 : any ? 31 - __clz(any) : -1;
+            if (l >= 0) {
+                const int i = __shfl_sync(kFull, mine, l);
+                f.token = begin + tile * kTileEntries + (i / Tile<T>::kVec) * (32 * Tile<T>::kVec) + l * Tile<T>::kVec + i % Tile<T>::kVec;
+                f.tz = __shfl_sync(kFull, z, l);
+            }
+            if (above) break;
+            at0 = __shfl_sync(kFull, at, 31);
+        }
+        f.close = __any_sync(kFull, f.close);
+        return f;
+    }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads) k_sample_stream(const __grid_constant__ SampleArgs a, int run, int ctas) {
+    __shared__ StreamShared s;
+    const int rank = ctas > 1 ? ptx::cluster_ctarank() : 0, row = blockIdx.x / ctas;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    SampleRule rule;
+    float u;
+    if (!row_begins(a, row, rank, rule, u) || rule.search) return;            // (the same in every block of the cluster)
+    if (threadIdx.x == 0) {
+        ptx::mbar_init(&s.mail[0], 1);
+        ptx::mbar_init(&s.mail[1], 1);
+        ptx::fence_barrier_init();
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the block has begun and can take messages
+    const T* src = static_cast<const T*>(a.logits) + row * a.ld;
+    const int home = rank * kWarps + warp, begin = home * run, end = min(a.V, begin + run);
+    const int tiles = end > begin ? (end - begin + kTileEntries - 1) / kTileEntries : 0;
+    Stream<T> r{s, src, ctas, rank, home, begin, end, reinterpret_cast<uintptr_t>(src) % 16 == 0, a.status, 0};
+    r.inv_t = rule.inv_t;
+    r.c64 = 1.4426950408889634 * rule.inv_t;
+    r.c = static_cast<float>(r.c64);
+    float top = -INFINITY;
+    int top_i = 0x7fffffff, n = 0;
+    for (int k = 0; k < tiles; ++k) {
+        Tile<T> t;
+        t.load(src, begin + k * kTileEntries, end, r.aligned);
+        const float mine = t.largest();
+        float most = mine;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) most = max_nan(most, __shfl_xor_sync(kFull, most, o));
+        if (a.n_kept)
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) n += t.v[i] > -INFINITY;
+        if (rule.temperature == 0.f && most > top) {
+            int at = 0x7fffffff;
+#pragma unroll
+            for (int i = kPerLane - 1; i >= 0; --i) at = t.v[i] == most ? Tile<T>::index(begin + k * kTileEntries, i) : at;
+            top_i = __reduce_min_sync(kFull, at);
+        }
+        top = max_nan(top, most);
+        r.template weigh_tile<false>(t, k, most);
+    }
+    n = __reduce_add_sync(kFull, n);
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // before the first message
+    auto f = r.template locate<false>(tiles, top, top_i, n, u);
+    if (!(f.top > -INFINITY && f.top < INFINITY)) {                  // NaN, +inf or nothing but -inf
+        if (rank == 0 && threadIdx.x == 0) no_distribution(a, row);
+        return;
+    }
+    // log of the whole mass: its unit, and what the rounding of c adds to every exponent alike
+    const double shift = static_cast<double>(f.top) * (static_cast<double>(r.c) - r.c64);
+    if (rule.temperature == 0.f) {
+        if (rank == 0 && threadIdx.x == 0) {
+            const double lse = (log2(f.whole) + f.unit - shift) * 0.69314718055994531;
+            put_row(a, row, f.top_i, static_cast<double>(f.top) - lse, 0.0, 1);
+        }
+        return;
+    }
+    const bool fits = fabsf(f.top * r.c) <= 0x1p20f;                // (else a unit and c times a logit have no digits left to differ in)
+    r.expect(ctas);
+    const int close = __syncthreads_or(f.close || !fits);
+    if (threadIdx.x < ctas) send(r.box(rank), r.mail(), threadIdx.x, close != 0);
+    const unsigned long long* got = r.box(0);
+    r.receive();
+    int sum_close = 0;
+    for (int q = 0; q < ctas; ++q) sum_close += static_cast<int>(got[q]);
+    if (sum_close == 0) {
+        if (f.token >= 0 && lane == 0) {
+            const double logp = static_cast<double>(f.tz) * rule.inv_t - (log2(f.whole) + f.unit - shift) * 0.69314718055994531;
+            put_row(a, row, f.token, logp, logp, f.n);
+        }
+        return;
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) s.exp2_table[threadIdx.x] = exp2(threadIdx.x / 32.0);
+    __syncthreads();
+    r.top = f.top;
+    for (int k = 0; k < tiles; ++k) {
+        Tile<T> t;
+        t.load(src, begin + k * kTileEntries, end, r.aligned);
+        r.template weigh_tile<true>(t, k, 0.f);
+    }
+    f = r.template locate<true>(tiles, top, top_i, n, u);
+    if (f.token >= 0 && lane == 0) {
+        const double logp = (static_cast<double>(f.tz) - static_cast<double>(f.top)) * rule.inv_t - log(f.whole);
+        put_row(a, row, f.token, logp, logp, f.n);
+    }
+}
+
+template <typename... P, typename... A>
+cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes, cudaStream_t st, const A&... args) {
+    cudaError_t e = bytes > 0 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+    if (e == cudaSuccess && ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.n_rows) * ctas);
+    cfg.gridDim = dim3(static_cast<unsigned>(rows) * ctas);
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
@@ -846,7 +1144,39 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, cudaStream_t st) {
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, per, ctas);
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+}  // namespace
+
+cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_other, int sm_count, cudaStream_t st, int* n_launches) {
+    if (any_other) {
+        // a warp's run of entries: up to five tiles, and fewer while the rows leave SMs idle
+        int ctas = 1, run = 0;
+        for (;; ctas *= 2) {
+            run = ((a.V + kWarps * ctas - 1) / (kWarps * ctas) + 7) / 8 * 8;
+            if (ctas == kMaxCluster) break;
+            if (run <= kMaxTiles * kTileEntries && (run <= kTileEntries || static_cast<long long>(a.n_rows) * ctas >= sm_count)) break;
+        }
+        const cudaError_t e = launch_clusters(bf16 ? k_sample_stream<__nv_bfloat16> : k_sample_stream<float>, a.n_rows, ctas, 0, st, a, run, ctas);
+        if (e != cudaSuccess) return e;
+        *n_launches += 1;
+    }
+    if (any_search) {
+        // the fewest blocks per row (1 .. 16) whose share takes at most 40 KB, so that four blocks fit an SM
+        const int width = bf16 ? 2 : 4;
+        int ctas = 1, per = 0;
+        for (;; ctas *= 2) {
+            per = (a.V + kThreads * ctas - 1) / (kThreads * ctas);
+            // entries are read in pairs, and the threads' first ones lie an odd number of pairs apart: at different banks
+            per = ((per + 1) / 2 | 1) * 2;
+            if (ctas == kMaxCluster || static_cast<long long>(per) * kThreads * width <= 40 * 1024) break;
+        }
+        const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, ctas, per * kThreads * width, st, a, per, ctas);
+        if (e != cudaSuccess) return e;
+        *n_launches += 1;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace unity

@@ -1932,6 +1932,7 @@ int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, 
     if (reinterpret_cast<uintptr_t>(logits) % (logits_type == UNITY_BF16 ? 2 : 4)) return fail(ctx, UNITY_ERR_ALIGNMENT, "logits not aligned to their type");
     SampleArgs a;
     memset(&a, 0, sizeof(a));
+    bool any_search = false, any_other = false;
     for (int v = 0; v < n_roles; ++v) {
         const unity_sampling_rule& r = rules[v];
         if (!(r.temperature == 0.f || (r.temperature >= 1e-6f && r.temperature <= 1e6f)))
@@ -1945,6 +1946,8 @@ int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, 
         s.top_p = static_cast<double>(r.top_p);
         s.quantile = normal_quantile(s.top_p);
         s.log_min_p = r.min_p > 0.f ? log(static_cast<double>(r.min_p)) : -INFINITY;
+        s.search = r.temperature > 0.f && (s.top_k > 0 || r.top_p < 1.f || r.min_p > 0.f);
+        (s.search ? any_search : any_other) = true;
     }
     if (n_rows == 0) return UNITY_OK;
     a.logits = logits; a.ld = ld; a.n_rows = n_rows; a.V = V; a.n_roles = n_roles;
@@ -1952,8 +1955,9 @@ int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, 
     a.token = token; a.logp = logp; a.logp_kept = logp_kept; a.n_kept = n_kept; a.status = ctx->d_status;
     const DeviceGuard dev(ctx->device);
     if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
-    CUDA_TRY(ctx, launch_sample(a, logits_type == UNITY_BF16, ctx->stream));
-    ctx->launches += 1;
+    int nl = 0;
+    CUDA_TRY(ctx, launch_sample(a, logits_type == UNITY_BF16, any_search, any_other, ctx->sm_count, ctx->stream, &nl));
+    ctx->launches += nl;
     return UNITY_OK;
 }
 
