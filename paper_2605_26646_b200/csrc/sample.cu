@@ -52,6 +52,7 @@ struct Shared {
     double scan_m[kWarps];
     int found;
     double exp2_table[32];
+    uint16_t stage[kList];                   // the block's entries for the list, by their place in the block
     unsigned long long list[kList];          // (falling logit, rising index) as one rising number
 };
 
@@ -102,6 +103,17 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
+// The largest of three, NaN if one is NaN; the least of three.
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+    float y;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
 // Two neighbouring entries.
 __device__ __forceinline__ float2 pair(const float* p) { return *reinterpret_cast<const float2*>(p); }
 __device__ __forceinline__ float2 pair(const __nv_bfloat16* p) {
@@ -132,6 +144,11 @@ __device__ __forceinline__ double slow_weight(float v, float top, double c64, do
     const double b = table[n & 31];
     const double scaled = __hiloint2double(__double2hiint(b) + ((n >> 5) << 20), __double2loint(b));
     return fma(scaled, p, scaled);
+}
+
+// m 2^e for e <= 0, 0 far below.
+__device__ __forceinline__ double times_power(double m, int e) {                
+    return e < -1000 ? 0.0 : m * __hiloint2double((1023 + e) << 20, 0);
 }
 
 __device__ __forceinline__ void put_row(const SampleArgs& a, int row, int token, double logp, double logp_kept, int n_kept) {
@@ -171,16 +188,18 @@ struct Row {
     int per, ctas, rank, first;              // entries of a thread (even); index of the thread's first entry in the row
     int* status;
     int turn;                                // exchanges so far
-    int n_all, my_n;                         // entries above -inf, and the thread's own
+    int n_all;                               // entries above -inf
     float top;                               // largest logit
     double inv_t, c64;                       // 1 / T, log2(e) / T
     float c, top_c;                          // log2(e) / T and that times the largest logit, in fp32
     double whole;                            // mass of all entries
     // what is known about the end of the kept entries: it lies in [lo, hi); the thread's own mass and numbers there
     float lo, hi;
-    int n_lo, n_hi, my_lo, my_hi;
+    int n_lo, n_hi;
     double m_hi, my_m;
-    float list_lo, list_hi;                  // the list holds the sorted entries of this interval
+    unsigned long long marks[2];             // the thread's entries in [lo, hi)
+    float list_lo, list_hi;                  // the list holds the sorted entries of this interval, list_n of them
+    int list_n;
     bool cut_down;                           // entries were taken out of shared memory
 
     __device__ __forceinline__ int lane() const { return threadIdx.x & 31; }
@@ -322,8 +341,9 @@ struct Row {
         return least == 0u || least == 0xffffffffu ? -INFINITY : value_of(least);
     }
 
-    // Exclusive prefix of `n` over the cluster's threads in index order.
-    __device__ __forceinline__ int prefix(int n) {
+    // Exclusive prefix of `n` over the cluster's threads in index order, and over the block's; the block's and the cluster's sum.
+    struct Prefix { int cluster, block, block_n, n; };
+    __device__ __forceinline__ Prefix prefix(int n) {
         int v = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -333,11 +353,35 @@ struct Row {
         if (lane() == 31) s.scan[warp()] = v;
         __syncthreads();
         const int w = lane() < kWarps ? s.scan[lane()] : 0;
-        int before = v - n + __reduce_add_sync(kFull, lane() < warp() ? w : 0);
-        const int block = __reduce_add_sync(kFull, w);
-        const unsigned long long* got = all_to_all(block);
-        for (int r = 0; r < rank; ++r) before += static_cast<int>(got[r]);
-        return before;
+        Prefix p;
+        p.block = v - n + __reduce_add_sync(kFull, lane() < warp() ? w : 0);
+        p.block_n = __reduce_add_sync(kFull, w);
+        const unsigned long long* got = all_to_all(p.block_n);
+        const int theirs = lane() < ctas ? static_cast<int>(got[lane()]) : 0;
+        p.cluster = p.block + __reduce_add_sync(kFull, lane() < rank ? theirs : 0);
+        p.n = __reduce_add_sync(kFull, theirs);
+        return p;
+    }
+    // Which of the thread's entries are in [lo, hi) (at most 128 of them).
+    __device__ __forceinline__ int mark() {
+        marks[0] = marks[1] = 0;
+        for (int j0 = 0; j0 < per; j0 += 8) {
+            unsigned m = 0;
+#pragma unroll
+            for (int q = 0; q < 8; q += 2) {
+                const float2 two = j0 + q < per ? pair(z + j0 + q) : make_float2(-INFINITY, -INFINITY);
+                m |= (two.x >= lo && two.x < hi ? 1u << q : 0u) | (two.y >= lo && two.y < hi ? 2u << q : 0u);
+            }
+            if (j0 < 64) marks[0] |= static_cast<unsigned long long>(m) << j0;
+            else marks[1] |= static_cast<unsigned long long>(m) << (j0 - 64);
+        }
+        return __popcll(marks[0]) + __popcll(marks[1]);
+    }
+    template <typename F>
+    __device__ __forceinline__ void each_marked(F f) const {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            for (unsigned long long m = marks[h]; m; m &= m - 1) f(64 * h + __ffsll(m) - 1);
     }
 
     // Encloses the end of the first k_want entries (BY_MASS false) or of the first whose mass reaches share of the whole, until at
@@ -381,9 +425,8 @@ struct Row {
                 whole = v.whole;
                 m_lo = v.whole;
                 n_lo = n_all;
-                my_lo = my_n;
                 hi = nextafterf(top, INFINITY);
-                n_hi = my_hi = 0;
+                n_hi = 0;
                 m_hi = my_m = 0.0;
                 *target = share * v.whole;
                 *bound = slack * v.whole;
@@ -398,30 +441,34 @@ struct Row {
                 if (!(tau[k] > lo && tau[k] < hi)) continue;
                 const bool enough = BY_MASS ? v.m[k] >= *target + *bound : v.c[k] >= k_want;
                 const bool little = BY_MASS ? v.m[k] < *target - *bound : v.c[k] < k_want;
-                if (little) { hi = tau[k]; n_hi = v.c[k]; m_hi = v.m[k]; my_hi = mine.c[k]; my_m = mine.m[k]; moved = true; }
-                else if (enough) { lo = tau[k]; n_lo = v.c[k]; m_lo = v.m[k]; my_lo = mine.c[k]; moved = true; }
+                if (little) { hi = tau[k]; n_hi = v.c[k]; m_hi = v.m[k]; my_m = mine.m[k]; moved = true; }
+                else if (enough) { lo = tau[k]; n_lo = v.c[k]; m_lo = v.m[k]; moved = true; }
             }
             if (n_lo - n_hi <= kList || key_of(hi) - key_of(lo) <= 1u) return true;
             if (!moved && round > 0) return false;
         }
     }
 
-    // The entries in [lo, hi) in order: an entry's place is its rank behind the n_hi above.
-    __device__ __forceinline__ void sort_list(int total) {
-        if (list_lo == lo && list_hi == hi) return;
+    // The entries in [lo, hi) in order: an entry's place is its rank behind the n_hi above.  False: they are more than kList.
+    __device__ __forceinline__ bool sort_list() {
+        if (list_lo == lo && list_hi == hi) return true;
+        const Prefix p = prefix(mark());
+        if (p.n > kList) return false;
+        list_n = p.n;
         list_lo = lo;
         list_hi = hi;
-        int n = my_lo - my_hi, to = prefix(n);
-        __syncthreads();                                          // (every warp has read its messages)
+        const int total = p.n;
+        int to = p.block;
+        each_marked([&](int j) { s.stage[to++] = static_cast<uint16_t>(threadIdx.x * per + j); });
+        __syncthreads();                                          // (and every warp has read its messages)
         expect(total + ctas);
         if (threadIdx.x < ctas) send(box(rank), mail(), threadIdx.x, 0);
-        for (int j = 0; n > 0 && j < per; ++j) {
-            const float x = one(z + j);
-            if (!(x >= lo && x < hi)) continue;
-            const unsigned long long item = static_cast<unsigned long long>(~key_of(x)) << 32 | static_cast<unsigned>(first + j);
-            for (int r = 0; r < ctas; ++r) send(&s.list[to], mail(), r, item);
-            ++to;
-            --n;
+        const int base = p.cluster - p.block, log_ctas = 31 - __clz(ctas);
+        for (int i = threadIdx.x; i < p.block_n << log_ctas; i += kThreads) {
+            const int k = i >> log_ctas, at = s.stage[k];
+            const unsigned long long item = static_cast<unsigned long long>(~key_of(one(z - threadIdx.x * per + at))) << 32 |
+                                            static_cast<unsigned>(first - threadIdx.x * per + at);
+            send(&s.list[base + k], mail(), i & (ctas - 1), item);
         }
         int log_size = 6;
         while (1 << log_size < total) ++log_size;
@@ -429,7 +476,19 @@ struct Row {
         for (int i = total + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
         receive();
         __syncthreads();
-        // bitonic: a thread compares up to two pairs per step; up to 32 apart the pairs of a warp are the warp's own
+        if (total <= kThreads) {
+            // each counts the smaller ones
+            const unsigned long long mine = threadIdx.x < total ? s.list[threadIdx.x] : ~0ull;
+            int below = 0;
+            if (threadIdx.x < total)
+#pragma unroll 8
+                for (int i = 0; i < total; ++i) below += s.list[i] < mine;
+            __syncthreads();
+            if (threadIdx.x < total) s.list[below] = mine;
+            __syncthreads();
+            return true;
+        }
+        // bitonic: a thread compares two pairs per step; up to 32 apart the pairs of a warp are the warp's own
         for (int k = 1; k <= log_size; ++k)
             for (int j = k - 1; j >= 0; --j) {
                 for (int t = threadIdx.x; t < size / 2; t += kThreads) {
@@ -440,13 +499,16 @@ struct Row {
                 if (j > 5 || (j > 0 ? j - 1 : k) > 5) __syncthreads(); else __syncwarp();
             }
         __syncthreads();
+        return true;
     }
 
     // Cuts the sorted entries: rank below k_want (behind the n_hi above) and, with BY_MASS, mass before them below the target.  With
     // k_want and a share the target is that share of the first k_want's mass.
+    enum Outcome { kDone, kClose, kShort };  // kShort: the list's mass does not reach the target
     template <bool EXACT, bool BY_MASS>
-    __device__ __forceinline__ bool cut_list(int total, int k_want, double share, double target, double bound, Cut* cut, int* n_kept) {
+    __device__ __forceinline__ Outcome cut_list(int k_want, double share, double target, double bound, Cut* cut, int* n_kept) {
         constexpr int kEach = kList / kThreads;
+        const int total = list_n;
         const int i0 = kEach * threadIdx.x;
         double e[kEach], sum = 0.0;
 #pragma unroll
@@ -463,10 +525,12 @@ struct Row {
             const double upto = warp_scan(w, lane());
             before = __shfl_sync(kFull, upto, warp() ? warp() - 1 : 0);
             before = (warp() ? before : 0.0) + (run - sum);
+            const double all = __shfl_sync(kFull, upto, kWarps - 1);
             if (share > 0.0) {
-                const double all = __shfl_sync(kFull, upto, kWarps - 1);
                 target = share * all;
                 bound = (EXACT ? kSlackExact : kSlackFast) * all;
+            } else if (!(m_hi + all >= target + bound)) {
+                return kShort;
             }
         }
         int kept = 0;
@@ -481,14 +545,14 @@ struct Row {
         }
         const int warp_kept = __reduce_add_sync(kFull, kept);
         if (lane() == 0) s.scan[warp()] = warp_kept;
-        if (__syncthreads_or(close)) return false;
+        if (__syncthreads_or(close)) return kClose;
         kept = __reduce_add_sync(kFull, lane() < kWarps ? s.scan[lane()] : 0);
         kept = kept > 0 ? kept : 1;                              // (rounding does not take the first one)
         const unsigned long long last = s.list[kept - 1];
         cut->z = value_of(~static_cast<unsigned>(last >> 32));
         cut->i = static_cast<int>(last & 0xffffffffu);
         *n_kept = n_hi + kept;
-        return true;
+        return kDone;
     }
 
     // Cuts entries of one value, lo: so many of them by index.
@@ -501,13 +565,12 @@ struct Row {
             want = !(up >= 1.0) ? 1 : up > n_lo - n_hi ? n_lo - n_hi : static_cast<int>(up);
         }
         want = min(want, n_lo - n_hi);
-        const int n = my_lo - my_hi, before = prefix(n);
+        const int n = mark(), before = prefix(n).cluster;
         if (threadIdx.x == 0) s.found = -1;
         __syncthreads();
         if (before < want && want <= before + n) {
             int left = want - before;
-            for (int j = 0; j < per; ++j)
-                if (one(z + j) == lo && --left == 0) { s.found = first + j; break; }
+            each_marked([&](int j) { if (--left == 0) s.found = first + j; });
         }
         __syncthreads();
         const unsigned long long* got = all_to_all(static_cast<unsigned>(s.found + 1));
@@ -524,11 +587,10 @@ struct Row {
     template <bool EXACT>
     __device__ __forceinline__ bool pick(const SampleArgs& a, int row, const Cut& cut, int n_kept, float u) {
         double mine = my_m;
-        if (my_lo > my_hi)
-            for (int j = 0; j < per; ++j) {
-                const float x = one(z + j);
-                if (x >= lo && x < hi && cut.keeps(x, first + j)) mine += weight<EXACT>(x);
-            }
+        each_marked([&](int j) {
+            const float x = one(z + j);
+            if (cut.keeps(x, first + j)) mine += weight<EXACT>(x);
+        });
         const double run = warp_scan(mine, lane());               // inclusive over the warp's lanes
         const double sum = __shfl_sync(kFull, run, 31);
         expect(ctas * kWarps);
@@ -615,12 +677,8 @@ struct Row {
     // Takes out of shared memory what `keep` refuses; what remains goes by the rest.
     template <typename F>
     __device__ __forceinline__ void reduce_to(int n, F keep) {
-        my_n = 0;
-        for (int j = 0; j < per; ++j) {
-            const float x = one(z + j);
-            if (keep(x, first + j)) my_n += x > -INFINITY;
-            else z[j] = static_cast<T>(-INFINITY);
-        }
+        for (int j = 0; j < per; ++j)
+            if (!keep(one(z + j), first + j)) z[j] = static_cast<T>(-INFINITY);
         n_all = n;
         cut_down = true;
         list_lo = list_hi = 0.f;
@@ -640,43 +698,67 @@ struct Row {
             const Tally mine = weigh<EXACT, true, false>(at), v = exchange(mine);
             whole = v.whole;
             lo = hi = floor;
-            my_lo = my_hi = 0;
+            marks[0] = marks[1] = 0;
             my_m = mine.m[0];
             n_kept = v.c[0];
             if (!search) return pick<EXACT>(a, row, cut, n_kept, u);
             all = whole;
+            whole = v.m[0];
             reduce_to(n_kept, [&](float x, int) { return x >= floor; });
         }
-        double target = 0.0, bound = 0.0;
-        bool done = false;
-        if (rule.top_k > 0) {
-            const bool again = EXACT && list_lo < list_hi;        // the interval that the fp32 pass has found
-            const float above = again ? list_hi : INFINITY, below = again ? list_lo : reached_by(rule.top_k, my_top, valid, a.V);
-            if (!enclose<EXACT, false>(rule.top_k, 0.0, 0.f, above, below, &target, &bound)) return false;
-            if (all < 0.0) all = whole;
-            const int total = n_lo - n_hi;
-            if (total <= kList) {
-                // where all of the first k are in the list, top-p is decided there too
-                sort_list(total);
-                done = rule.top_p < 1.0 && n_hi == 0;
-                if (done ? !cut_list<EXACT, true>(total, rule.top_k, rule.top_p, 0.0, 0.0, &cut, &n_kept)
-                         : !cut_list<EXACT, false>(total, rule.top_k, 0.0, 0.0, 0.0, &cut, &n_kept)) return false;
-            } else if (!cut_ties<EXACT, false>(rule.top_k, 0.0, 0.0, &cut, &n_kept)) return false;
-            if (rule.top_p < 1.0 && !done)
-                reduce_to(n_kept, [&](float x, int i) { return x >= hi || (x >= lo && cut.keeps(x, i)); });
+        if (EXACT && all < 0.0) {
+            const float none[kTau] = {INFINITY, INFINITY};
+            whole = exchange(weigh<true, false, false>(none)).whole;
         }
-        if (rule.top_p < 1.0 && !done) {
-            const bool again = EXACT && list_lo < list_hi;
+        if (all < 0.0) all = whole;
+        // What is kept is mostly among the first few hundred: those are sorted, and if they hold the end everything is decided there
+        const bool again = EXACT && list_lo < list_hi;            // the interval that the fp32 pass has found
+        double target = rule.top_p * whole, bound = (EXACT ? kSlackExact : kSlackFast) * whole;
+        float below = -INFINITY;
+        bool done = false;
+        if (rule.top_k <= kList / 4 * 3) {
+            hi = nextafterf(top, INFINITY);
+            n_hi = 0;
+            m_hi = my_m = 0.0;
+            if (again) {
+                lo = list_lo;
+                done = list_hi == hi;
+            } else if (n_all <= kList) {
+                lo = kLowest;
+                done = true;
+            } else {
+                lo = below = reached_by(rule.top_k > 0 ? rule.top_k : kThreads / 2, my_top, valid, a.V);
+                done = below > -INFINITY;
+            }
+            done = done && sort_list() && (rule.top_k == 0 || list_n >= min(rule.top_k, n_all));
+            if (done) {
+                const Outcome o = rule.top_k == 0 ? cut_list<EXACT, true>(0x7fffffff, 0.0, target, bound, &cut, &n_kept)
+                                : rule.top_p < 1.0 ? cut_list<EXACT, true>(rule.top_k, rule.top_p, 0.0, 0.0, &cut, &n_kept)
+                                                   : cut_list<EXACT, false>(rule.top_k, 0.0, 0.0, 0.0, &cut, &n_kept);
+                if (o == kClose) return false;
+                done = o == kDone;
+            }
+        }
+        if (!done && rule.top_k > 0) {
+            if (!enclose<EXACT, false>(rule.top_k, 0.0, 0.f, again ? list_hi : INFINITY, again ? list_lo : below, &target, &bound)) return false;
+            if (n_lo - n_hi <= kList) {
+                sort_list();
+                cut_list<EXACT, false>(rule.top_k, 0.0, 0.0, 0.0, &cut, &n_kept);
+            } else {
+                cut_ties<EXACT, false>(rule.top_k, 0.0, 0.0, &cut, &n_kept);
+            }
+            if (rule.top_p < 1.0) reduce_to(n_kept, [&](float x, int i) { return x >= hi || (x >= lo && cut.keeps(x, i)); });
+        }
+        if (!done && rule.top_p < 1.0) {
             const float octave = 0.69314718f / static_cast<float>(inv_t);
-            const float above = again ? list_hi : top - 2.f * octave, below = again ? list_lo : top - 10.f * octave;
-            if (!enclose<EXACT, true>(0, rule.top_p, rule.quantile, above, below, &target, &bound)) return false;
-            const int total = n_lo - n_hi;
-            if (total <= kList) {
-                sort_list(total);
-                if (!cut_list<EXACT, true>(total, 0x7fffffff - kList, 0.0, target, bound, &cut, &n_kept)) return false;
+            const float above = again ? list_hi : top - 2.f * octave;
+            if (!enclose<EXACT, true>(0, rule.top_p, rule.quantile, above, again ? list_lo : top - 10.f * octave, &target, &bound)) return false;
+            if (n_lo - n_hi <= kList) {
+                sort_list();
+                if (cut_list<EXACT, true>(0x7fffffff, 0.0, target, EXACT ? -1.0 : bound, &cut, &n_kept) != kDone) return false;
             } else if (!cut_ties<EXACT, true>(0, target, bound, &cut, &n_kept)) return false;
         }
-        if (all >= 0.0) whole = all;
+        whole = all;
         return pick<EXACT>(a, row, cut, n_kept, u);
     }
 };
@@ -736,36 +818,62 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
         my_top = max_nan(my_top, max_nan(v.x, v.y));
         finite += (v.x > -INFINITY) + (v.y > -INFINITY);
     }
-    r.my_n = finite;
+    r.inv_t = rule.inv_t;
+    r.c64 = 1.4426950408889634 * rule.inv_t;
+    r.c = static_cast<float>(r.c64);
+    // the mass, in units of a power of two next to the thread's largest entry
+    int unit = my_top > -INFINITY && my_top < INFINITY ? static_cast<int>(ceilf(fminf(fmaxf(my_top * r.c, -1e9f), 1e9f))) : -1000000000;
+    double mass = 0.0;
+    if (rule.log_min_p == -INFINITY) {
+        const float none[kTau] = {INFINITY, INFINITY};
+        r.top_c = static_cast<float>(unit);
+        mass = r.template weigh<false, false, false>(none).whole;
+        const int most = __reduce_max_sync(kFull, unit);
+        mass = warp_sum(times_power(mass, unit - most));
+        unit = most;
+    }
     float top = my_top;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
     finite = __reduce_add_sync(kFull, finite);
-    if (lane == 0) { s.warp_z[warp] = top; s.warp_n[warp] = finite; }
+    if (lane == 0) { s.warp_z[warp] = top; s.warp_n[warp] = finite; s.scan_m[warp] = mass; s.scan[warp] = unit; }
     __syncthreads();
     top = s.warp_z[0];
     finite = s.warp_n[0];
-    for (int w = 1; w < kWarps; ++w) { top = max_nan(top, s.warp_z[w]); finite += s.warp_n[w]; }
+    unit = s.scan[0];
+    for (int w = 1; w < kWarps; ++w) { top = max_nan(top, s.warp_z[w]); finite += s.warp_n[w]; unit = max(unit, s.scan[w]); }
+    mass = 0.0;
+    for (int w = 0; w < kWarps; ++w) mass += times_power(s.scan_m[w], s.scan[w] - unit);
+    __syncthreads();
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");     // before the first message
-    const unsigned long long* got = r.all_to_all(static_cast<unsigned long long>(__float_as_uint(top)) << 32 | static_cast<unsigned>(finite));
+    r.expect(3 * ctas);
+    if (threadIdx.x < ctas) {
+        send(r.box(3 * rank), r.mail(), threadIdx.x, static_cast<unsigned long long>(__float_as_uint(top)) << 32 | static_cast<unsigned>(finite));
+        send(r.box(3 * rank + 1), r.mail(), threadIdx.x, static_cast<unsigned long long>(__double_as_longlong(mass)));
+        send(r.box(3 * rank + 2), r.mail(), threadIdx.x, static_cast<unsigned>(unit));
+    }
+    const unsigned long long* got = r.box(0);
+    r.receive();
     r.n_all = 0;
     for (int q = 0; q < ctas; ++q) {
-        top = max_nan(top, __uint_as_float(static_cast<unsigned>(got[q] >> 32)));
-        r.n_all += static_cast<int>(got[q] & 0xffffffffu);
+        top = max_nan(top, __uint_as_float(static_cast<unsigned>(got[3 * q] >> 32)));
+        r.n_all += static_cast<int>(got[3 * q] & 0xffffffffu);
+        unit = max(unit, static_cast<int>(got[3 * q + 2]));
     }
+    mass = 0.0;
+    for (int q = 0; q < ctas; ++q)
+        mass += times_power(__longlong_as_double(static_cast<long long>(got[3 * q + 1])), static_cast<int>(got[3 * q + 2]) - unit);
     if (!(top > -INFINITY && top < INFINITY)) {                   // NaN, +inf or nothing but -inf
         if (rank == 0 && threadIdx.x == 0) no_distribution(a, row);
         return;
     }
     r.top = top;
-    r.inv_t = rule.inv_t;
-    r.c64 = 1.4426950408889634 * rule.inv_t;
-    r.c = static_cast<float>(r.c64);
     r.top_c = top * r.c;
+    r.whole = mass * exp2(static_cast<double>(unit) - static_cast<double>(r.top_c));
     r.list_lo = r.list_hi = 0.f;
     r.cut_down = false;
-    const int n_all = r.n_all, my_n = r.my_n;
+    const int n_all = r.n_all;
     float floor = -INFINITY;
     if (rule.log_min_p > -INFINITY) {
         // the lowest logit with x >= log min_p
@@ -786,7 +894,6 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
         r.cut_down = false;
         r.list_lo = r.list_hi = 0.f;
         r.n_all = n_all;
-        r.my_n = my_n;
     }
     __syncthreads();
     r.template draw<true>(a, row, rule, floor, my_top, n, u);
@@ -795,65 +902,77 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
 // ------------------------------------------------------------------------------------------------
 // Rows whose rule leaves every entry (no top-k, top-p or min-p) and rows that take the largest logit: one pass over the logits in
 // registers, no copy in shared memory, so that more rows are in flight.  Every warp of the cluster has a run of consecutive entries,
-// in tiles of 512; a tile's masses refer to a power of two of its own next to its largest entry.  The warp whose running mass holds
-// the target reads one of its tiles again.
+// in tiles of 512; a lane's mass of a tile refers to a power of two next to the lane's largest entry there.  The warp whose running
+// mass holds the target reads one of its tiles again.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTileEntries = 512, kPerLane = kTileEntries / 32;
-constexpr int kMaxTiles = 5;                 // of a warp
+constexpr int kMaxTiles = 20;                // of a warp
 static_assert(kMaxTiles * kMaxCluster * kWarps * kTileEntries >= UNITY_MAX_SAMPLE_V, "enough for a row");
 
 struct StreamShared {
     uint64_t mail[2];
-    unsigned long long box[2][3 * kMaxCluster * kWarps];
-    double tile_m[kWarps][kMaxTiles];        // mass of a tile, in units of 2^tile_r
-    int tile_r[kWarps][kMaxTiles];
+    unsigned long long box[2][3 * kMaxCluster];
+    double warp_m[kWarps];                   // mass of a warp, in units of 2^warp_r
+    int warp_r[kWarps], warp_n[kWarps], warp_i[kWarps];
+    float warp_top[kWarps];
+    float top;                               // what the first warp found out for the others
+    int again;
+    union {                                  // a lane's mass of a tile
+        float2 lane_m[kMaxTiles][kThreads];  // x in units of 2^y
+        double lane_x[kMaxTiles][kThreads];  // from fp64 weights, in units of 1
+    };
     double exp2_table[32];
 };
 
 template <typename T>
 struct Tile {
     static constexpr int kVec = 16 / sizeof(T), kVecs = kPerLane / kVec;
-    float v[kPerLane];
+    uint4 raw[kVecs];
     static __device__ __forceinline__ int index(int base, int i) {               // of the lane's i-th entry
         return base + (i / kVec) * (32 * kVec) + (threadIdx.x & 31) * kVec + i % kVec;
     }
     __device__ __forceinline__ void load(const T* row, int base, int end, bool aligned) {
+        if (aligned && base + kTileEntries <= end) {
+            const uint4* p = reinterpret_cast<const uint4*>(row + base) + (threadIdx.x & 31);
+#pragma unroll
+            for (int k = 0; k < kVecs; ++k) raw[k] = __ldg(p + 32 * k);
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < kVecs; ++k) {
             const int at = index(base, k * kVec);
-            if (aligned && at + kVec <= end) {
-                const uint4 w = __ldg(reinterpret_cast<const uint4*>(row + at));
-                const unsigned u[4] = {w.x, w.y, w.z, w.w};
+            if (aligned && at + kVec <= end) raw[k] = __ldg(reinterpret_cast<const uint4*>(row + at));
+            else {
+                unsigned w[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    if (sizeof(T) == 4) v[k * kVec + q] = __uint_as_float(u[q]);
+                    if (sizeof(T) == 4) w[q] = at + q < end ? __float_as_uint(one(row + at + q)) : 0xff800000u;
                     else {
-                        v[k * kVec + 2 * q] = __uint_as_float(u[q] << 16);
-                        v[k * kVec + (2 * q + 1) % kVec] = __uint_as_float(u[q] & 0xffff0000u);
+                        const unsigned lo = at + 2 * q < end ? __float_as_uint(one(row + at + 2 * q)) : 0xff800000u;
+                        const unsigned hi = at + 2 * q + 1 < end ? __float_as_uint(one(row + at + 2 * q + 1)) : 0xff800000u;
+                        w[q] = lo >> 16 | (hi & 0xffff0000u);
                     }
                 }
-            } else {
-#pragma unroll
-                for (int q = 0; q < kVec; ++q) v[k * kVec + q] = at + q < end ? one(row + at + q) : -INFINITY;
+                raw[k] = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
     }
-    __device__ __forceinline__ float largest() const {                            // NaN if one is NaN
-        float m = v[0];
+    __device__ __forceinline__ void rotate() {                                    // the next vector becomes the first
 #pragma unroll
-        for (int i = 1; i < kPerLane; ++i) m = max_nan(m, v[i]);
-        return m;
+        for (int k = 0; k + 1 < kVecs; ++k) raw[k] = raw[k + 1];
+    }
+    __device__ __forceinline__ float value(int i) const {
+        const uint4& r = raw[i / kVec];
+        const int q = i % kVec * sizeof(T) / 4;
+        const unsigned w = q == 0 ? r.x : q == 1 ? r.y : q == 2 ? r.z : r.w;
+        return __uint_as_float(sizeof(T) == 4 ? w : i % 2 ? w & 0xffff0000u : w << 16);
     }
 };
-__device__ __forceinline__ double times_power(double m, int e) {                  // m 2^e, 0 far below
-    return e < -1000 ? 0.0 : m * __hiloint2double((1023 + e) << 20, 0);
-}
-
 template <typename T>
 struct Stream {
     StreamShared& s;
     const T* row;
-    int ctas, rank, home, begin, end;        // the warp's number in the cluster and its entries [begin, end)
+    int ctas, rank, run, V;                  // blocks of the cluster; entries of a warp
     bool aligned;
     int* status;
     int turn;
@@ -862,7 +981,11 @@ struct Stream {
     float top;
 
     __device__ __forceinline__ int lane() const { return threadIdx.x & 31; }
-    __device__ __forceinline__ int warp() const { return threadIdx.x >> 5; }
+    __device__ __forceinline__ int begin(int warp) const { return (rank * kWarps + warp) * run; }
+    __device__ __forceinline__ int tiles(int warp) const {
+        const int n = min(V, begin(warp) + run) - begin(warp);
+        return n > 0 ? (n + kTileEntries - 1) / kTileEntries : 0;
+    }
     __device__ __forceinline__ uint64_t* mail() const { return &s.mail[turn & 1]; }
     __device__ __forceinline__ unsigned long long* box(int i) const { return &s.box[turn & 1][i]; }
     __device__ __forceinline__ void expect(int words) const {
@@ -874,138 +997,120 @@ struct Stream {
     __device__ __forceinline__ double weight(float v, int r) const {
         return EXACT ? slow_weight(v, top, c64, inv_t, s.exp2_table) : static_cast<double>(ptx::ex2(fmaf(v, c, -static_cast<float>(r))));
     }
-
-    // Masses of the warp's tiles.
+    // Unit of a lane's mass: the power of two at or above its largest entry (any, if it has none).
+    __device__ __forceinline__ float unit_of(float most) const {
+        return most > -INFINITY && most < INFINITY ? ceilf(fminf(fmaxf(most * c, -1e9f), 1e9f)) : -1e9f;
+    }
+    // The mass of tile k in lane `t` of the block, in units of 2^unit.
     template <bool EXACT>
-    __device__ __forceinline__ void weigh_tile(const Tile<T>& t, int k, float most) {
-        // (no finite entry: any unit will do)
-        const int r = EXACT ? 0 : most > -INFINITY && most < INFINITY ? static_cast<int>(ceilf(fminf(fmaxf(most * c, -1e9f), 1e9f))) : 0;
-        double m = 0.0;
-        if (EXACT) {
-#pragma unroll
-            for (int i = 0; i < kPerLane; ++i) m += weight<true>(t.v[i], 0);
-        } else {
-            const float rf = static_cast<float>(r);
-            float e[kPerLane];
-#pragma unroll
-            for (int i = 0; i < kPerLane; ++i) e[i] = ptx::ex2(fmaf(t.v[i], c, -rf));
-#pragma unroll
-            for (int o = kPerLane / 2; o > 0; o >>= 1)
-#pragma unroll
-                for (int i = 0; i < o; ++i) e[i] += e[i + o];
-            m = static_cast<double>(e[0]);
-        }
-        m = warp_sum(m);
-        if (lane() == 0) { s.tile_m[warp()][k] = m; s.tile_r[warp()][k] = r; }
+    __device__ __forceinline__ double lane_mass(int k, int t, int unit) const {
+        if (EXACT) return s.lane_x[k][t];
+        const float2 m = s.lane_m[k][t];
+        return times_power(static_cast<double>(m.x), static_cast<int>(m.y) - unit);
     }
 
-    // Sends the warp's mass, its unit, and two more numbers; finds the warp that holds the target and, there, the token.  `tz`: its
-    // logit.  close: a comparison was too close for this arithmetic (known in that warp).
-    struct Found { int token, n; float top, tz; int top_i, unit; double whole; bool close; };
+    // Among lanes [0, n), which hold masses in index order: the first whose running mass is above the target, or the last with any; its
+    // `start`: the mass before it.  -1: no mass at all.
+    __device__ __forceinline__ int owner(double mass, double before_all, double target, double* start) const {
+        const double upto = warp_scan(mass, lane()), prior = __shfl_up_sync(kFull, upto, 1);
+        const double from = before_all + (lane() ? prior : 0.0);
+        const unsigned some = __ballot_sync(kFull, mass > 0.0), past = some & __ballot_sync(kFull, before_all + upto > target);
+        if (some == 0) return -1;
+        const int l = past ? __ffs(past) - 1 : 31 - __clz(some);
+        *start = __shfl_sync(kFull, from, l);
+        return l;
+    }
+
+    // One warp: the cluster's masses, and, in the block that holds the target, the token.  whole: in units of 2^unit; close: a
+    // comparison was too close for this arithmetic (known in that block).
+    struct Found { int token, n, top_i, unit; float top, tz; double whole; bool close; };
     template <bool EXACT>
-    __device__ __forceinline__ Found locate(int tiles, float my_top, int my_top_i, int my_n, float u) {
-        __syncwarp();
-        int r = -0x40000000;
-        for (int k = 0; k < tiles; ++k)
-            if (s.tile_m[warp()][k] > 0.0) r = max(r, s.tile_r[warp()][k]);
-        double m = 0.0;
-        for (int k = 0; k < tiles; ++k)
-            if (s.tile_m[warp()][k] > 0.0) m += times_power(s.tile_m[warp()][k], s.tile_r[warp()][k] - r);
-        const int warps = ctas * kWarps;
-        expect(3 * warps);
+    __device__ __forceinline__ Found locate(float u) {
+        Found f;
+        f.token = -1;
+        f.tz = 0.f;
+        f.close = false;
+        // the block's sums
+        const bool is_warp = lane() < kWarps;
+        double m = is_warp ? s.warp_m[lane()] : 0.0;
+        const int r = is_warp && m > 0.0 ? s.warp_r[lane()] : -0x40000000, block_r = __reduce_max_sync(kFull, r);
+        float most = is_warp ? s.warp_top[lane()] : -INFINITY;
+        int most_i = is_warp ? s.warp_i[lane()] : 0x7fffffff;
+#pragma unroll
+        for (int o = 1; o < kWarps; o <<= 1) {
+            const float v = __shfl_down_sync(kFull, most, o);
+            const int i = __shfl_down_sync(kFull, most_i, o);
+            most_i = v > most ? i : most_i;                       // (lanes are in index order)
+            most = max_nan(most, v);
+        }
+        most = __shfl_sync(kFull, most, 0);
+        most_i = __shfl_sync(kFull, most_i, 0);
+        const int n = __reduce_add_sync(kFull, is_warp ? s.warp_n[lane()] : 0);
+        m = times_power(m, r - block_r);
+        const double block_m = warp_sum(m);
+        expect(3 * ctas);
         if (lane() < ctas) {
-            send(box(3 * home), mail(), lane(), static_cast<unsigned long long>(__double_as_longlong(m)));
-            send(box(3 * home + 1), mail(), lane(), static_cast<unsigned long long>(static_cast<unsigned>(r)) << 32 | static_cast<unsigned>(my_n));
-            send(box(3 * home + 2), mail(), lane(), static_cast<unsigned long long>(__float_as_uint(my_top)) << 32 | static_cast<unsigned>(my_top_i));
+            send(box(3 * rank), mail(), lane(), static_cast<unsigned long long>(__double_as_longlong(block_m)));
+            send(box(3 * rank + 1), mail(), lane(), static_cast<unsigned long long>(static_cast<unsigned>(block_r)) << 32 | static_cast<unsigned>(n));
+            send(box(3 * rank + 2), mail(), lane(), static_cast<unsigned long long>(__float_as_uint(most)) << 32 | static_cast<unsigned>(most_i));
         }
         const unsigned long long* got = box(0);
         receive();
-        constexpr int kEach = kMaxCluster * kWarps / 32;
-        Found f;
-        f.token = -1;
-        f.top = -INFINITY;
-        f.top_i = 0x7fffffff;
-        f.n = 0;
-        f.unit = -0x40000000;
-        f.close = false;
-        f.tz = 0.f;
-        double part[kEach], four = 0.0;
-        int unit[kEach];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int w = lane() * kEach + i;
-            part[i] = 0.0;
-            unit[i] = -0x40000000;
-            if (w < warps) {
-                part[i] = __longlong_as_double(static_cast<long long>(got[3 * w]));
-                unit[i] = static_cast<int>(got[3 * w + 1] >> 32);
-                f.n += static_cast<int>(got[3 * w + 1] & 0xffffffffu);
-                const float v = __uint_as_float(static_cast<unsigned>(got[3 * w + 2] >> 32));
-                f.top_i = v > f.top ? static_cast<int>(got[3 * w + 2] & 0xffffffffu) : f.top_i;
-                f.top = max_nan(f.top, v);
-                f.unit = max(f.unit, unit[i]);
-            }
+        double mass = 0.0;
+        int unit = -0x40000000, count = 0;
+        most = -INFINITY;
+        most_i = 0x7fffffff;
+        if (lane() < ctas) {
+            mass = __longlong_as_double(static_cast<long long>(got[3 * lane()]));
+            unit = static_cast<int>(got[3 * lane() + 1] >> 32);
+            count = static_cast<int>(got[3 * lane() + 1] & 0xffffffffu);
+            most = __uint_as_float(static_cast<unsigned>(got[3 * lane() + 2] >> 32));
+            most_i = static_cast<int>(got[3 * lane() + 2] & 0xffffffffu);
         }
-        f.unit = __reduce_max_sync(kFull, f.unit);
-        f.n = __reduce_add_sync(kFull, f.n);
+        f.unit = __reduce_max_sync(kFull, unit);
+        f.n = __reduce_add_sync(kFull, count);
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {                        // (the first of equal ones: lanes are in index order)
-            const float v = __shfl_down_sync(kFull, f.top, o);
-            const int i = __shfl_down_sync(kFull, f.top_i, o);
-            if (lane() + o < 32) { f.top_i = v > f.top ? i : f.top_i; f.top = max_nan(f.top, v); }
+        for (int o = 1; o < kMaxCluster; o <<= 1) {
+            const float v = __shfl_down_sync(kFull, most, o);
+            const int i = __shfl_down_sync(kFull, most_i, o);
+            most_i = v > most ? i : most_i;
+            most = max_nan(most, v);
         }
-        f.top = __shfl_sync(kFull, f.top, 0);
-        f.top_i = __shfl_sync(kFull, f.top_i, 0);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            part[i] = times_power(part[i], unit[i] - f.unit);
-            four += part[i];
-        }
-        const double upto = warp_scan(four, lane()), prior = __shfl_up_sync(kFull, upto, 1);
-        f.whole = __shfl_sync(kFull, upto, 31);
+        f.top = __shfl_sync(kFull, most, 0);
+        f.top_i = __shfl_sync(kFull, most_i, 0);
+        mass = times_power(mass, unit - f.unit);
+        f.whole = warp_sum(mass);
         const double target = static_cast<double>(u) * f.whole, bound = EXACT ? kSlackExact : kSlackFast * f.whole;
-        double from = lane() ? prior : 0.0, start = 0.0, last_start = 0.0;
-        int hit = -1, last = -1;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const double to = from + part[i];
-            if (part[i] > 0.0) {
-                last = lane() * kEach + i;
-                last_start = from;
-                if (hit < 0 && to > target) { hit = last; start = from; }
-            }
-            from = to;
-        }
-        const unsigned hits = __ballot_sync(kFull, hit >= 0), lasts = __ballot_sync(kFull, last >= 0);
-        if (lasts == 0) return f;                                 // (a row without a distribution)
-        const int owner = hits ? __ffs(hits) - 1 : 31 - __clz(lasts);
-        const int holder = __shfl_sync(kFull, hits ? hit : last, owner);
-        if (holder != home) return f;
-        start = __shfl_sync(kFull, hits ? start : last_start, owner);
-        // the tile: the first that ends above the target, or the last with any mass
+        double start = 0.0;
+        if (owner(mass, 0.0, target, &start) != rank) return f;
+        const int home = owner(times_power(m, block_r - f.unit), start, target, &start);
         int tile = 0;
         double at0 = start;
-        for (int k = 0; k < tiles; ++k) {
-            const double mass = s.tile_m[warp()][k] > 0.0 ? times_power(s.tile_m[warp()][k], s.tile_r[warp()][k] - f.unit) : 0.0;
-            if (!(mass > 0.0)) continue;
+        for (int k = 0; k < tiles(home); ++k) {
+            const double sum = warp_sum(lane_mass<EXACT>(k, home * 32 + lane(), f.unit));
+            if (!(sum > 0.0)) continue;
             tile = k;
             at0 = start;
-            start += mass;
+            start += sum;
             if (start > target) break;
         }
         Tile<T> t;
-        t.load(row, begin + tile * kTileEntries, end, aligned);
+        const int base = begin(home) + tile * kTileEntries;
+        t.load(row, base, min(V, begin(home) + run), aligned);
         f.close = fabs(at0 - target) <= bound;
-        const int shift = s.tile_r[warp()][tile] - f.unit;
-        // index order: vectors of the tile, lanes, entries of a lane
-#pragma unroll
+        // the entries' weights as they were added up; index order: vectors of the tile, lanes, entries of a lane
+        const int own = EXACT ? 0 : static_cast<int>(s.lane_m[tile][home * 32 + lane()].y), shift = EXACT ? 0 : own - f.unit;
+#pragma unroll 1
         for (int k = 0; k < Tile<T>::kVecs; ++k) {
             double e[Tile<T>::kVec], sum = 0.0;
+            float v[Tile<T>::kVec];
 #pragma unroll
             for (int q = 0; q < Tile<T>::kVec; ++q) {
-                e[q] = times_power(weight<EXACT>(t.v[k * Tile<T>::kVec + q], s.tile_r[warp()][tile]), shift);
+                v[q] = t.value(q);
+                e[q] = times_power(weight<EXACT>(v[q], own), shift);
                 sum += e[q];
             }
+            t.rotate();
             double at = at0 + warp_scan(sum, lane()) - sum;       // before the lane's entries
             int mine = -1;
             float z = 0.f;
@@ -1016,8 +1121,8 @@ struct Stream {
                 if (e[q] > 0.0) {
                     f.close |= fabs(at - target) <= bound;
                     if (!over) {
-                        mine = k * Tile<T>::kVec + q;
-                        z = t.v[k * Tile<T>::kVec + q];
+                        mine = q;
+                        z = v[q];
                         over = at > target;
                     }
                 }
@@ -1025,8 +1130,7 @@ struct Stream {
             const unsigned any = __ballot_sync(kFull, mine >= 0), above = __ballot_sync(kFull, over);
             const int l = above ? __ffs(above) - 1 : any ? 31 - __clz(any) : -1;
             if (l >= 0) {
-                const int i = __shfl_sync(kFull, mine, l);
-                f.token = begin + tile * kTileEntries + (i / Tile<T>::kVec) * (32 * Tile<T>::kVec) + l * Tile<T>::kVec + i % Tile<T>::kVec;
+                f.token = base + (k * 32 + l) * Tile<T>::kVec + __shfl_sync(kFull, mine, l);
                 f.tz = __shfl_sync(kFull, z, l);
             }
             if (above) break;
@@ -1038,13 +1142,21 @@ struct Stream {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_sample_stream(const __grid_constant__ SampleArgs a, int run, int ctas) {
+__global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_constant__ SampleArgs a, int run, int ctas) {
     __shared__ StreamShared s;
     const int rank = ctas > 1 ? ptx::cluster_ctarank() : 0, row = blockIdx.x / ctas;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     SampleRule rule;
     float u;
     if (!row_begins(a, row, rank, rule, u) || rule.search) return;            // (the same in every block of the cluster)
+    const T* src = static_cast<const T*>(a.logits) + row * a.ld;
+    Stream<T> r{s, src, ctas, rank, run, a.V, reinterpret_cast<uintptr_t>(src) % 16 == 0, a.status, 0};
+    const int begin = r.begin(warp), end = min(a.V, begin + run), tiles = r.tiles(warp);
+    if (r.aligned && lane == 0 && end - begin >= 16) {
+        // the whole run to L2 at once: what the registers have in flight does not cover the way to HBM
+        const unsigned bytes = (end - begin) * sizeof(T) / 16 * 16;
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src + begin), "r"(bytes) : "memory");
+    }
     if (threadIdx.x == 0) {
         ptx::mbar_init(&s.mail[0], 1);
         ptx::mbar_init(&s.mail[1], 1);
@@ -1052,76 +1164,114 @@ __global__ void __launch_bounds__(kThreads) k_sample_stream(const __grid_constan
     }
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the block has begun and can take messages
-    const T* src = static_cast<const T*>(a.logits) + row * a.ld;
-    const int home = rank * kWarps + warp, begin = home * run, end = min(a.V, begin + run);
-    const int tiles = end > begin ? (end - begin + kTileEntries - 1) / kTileEntries : 0;
-    Stream<T> r{s, src, ctas, rank, home, begin, end, reinterpret_cast<uintptr_t>(src) % 16 == 0, a.status, 0};
+    const bool greedy = rule.temperature == 0.f;
     r.inv_t = rule.inv_t;
     r.c64 = 1.4426950408889634 * rule.inv_t;
     r.c = static_cast<float>(r.c64);
-    float top = -INFINITY;
-    int top_i = 0x7fffffff, n = 0;
+    // A lane's masses of its tiles, each in a unit of its own: nothing crosses lanes until all tiles are read.
+    float most = -INFINITY;
+    int n = 0, at_most = 0x7fffffff;
+    const uint64_t c2 = ptx::pack2(r.c, r.c);
     for (int k = 0; k < tiles; ++k) {
         Tile<T> t;
         t.load(src, begin + k * kTileEntries, end, r.aligned);
-        const float mine = t.largest();
-        float most = mine;
+        float m = max_nan(t.value(0), t.value(1)), least = fminf(t.value(0), t.value(1));
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) most = max_nan(most, __shfl_xor_sync(kFull, most, o));
-        if (a.n_kept)
-#pragma unroll
-            for (int i = 0; i < kPerLane; ++i) n += t.v[i] > -INFINITY;
-        if (rule.temperature == 0.f && most > top) {
-            int at = 0x7fffffff;
-#pragma unroll
-            for (int i = kPerLane - 1; i >= 0; --i) at = t.v[i] == most ? Tile<T>::index(begin + k * kTileEntries, i) : at;
-            top_i = __reduce_min_sync(kFull, at);
+        for (int i = 2; i < kPerLane; i += 2) {
+            m = max_nan(m, t.value(i), t.value(i + 1));
+            least = min3(least, t.value(i), t.value(i + 1));
         }
-        top = max_nan(top, most);
-        r.template weigh_tile<false>(t, k, most);
+        n += kPerLane;
+        if (least == -INFINITY)
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) n -= t.value(i) == -INFINITY;
+        if (greedy && m > most) {
+#pragma unroll
+            for (int i = kPerLane - 1; i >= 0; --i) at_most = t.value(i) == m ? Tile<T>::index(begin + k * kTileEntries, i) : at_most;
+        }
+        most = max_nan(most, m);
+        const float unit = r.unit_of(m);
+        const uint64_t u2 = ptx::pack2(-unit, -unit);
+        uint64_t e2[kPerLane / 2];
+#pragma unroll
+        for (int i = 0; i < kPerLane / 2; ++i) {
+            float x, y;
+            ptx::unpack2(ptx::fma2(ptx::pack2(t.value(2 * i), t.value(2 * i + 1)), c2, u2), x, y);
+            e2[i] = ptx::pack2(ptx::ex2(x), ptx::ex2(y));
+        }
+#pragma unroll
+        for (int o = kPerLane / 4; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < o; ++i) e2[i] = ptx::add2(e2[i], e2[i + o]);
+        float x, y;
+        ptx::unpack2(e2[0], x, y);
+        s.lane_m[k][threadIdx.x] = make_float2(x + y, unit);
     }
+    // the warp's mass, in a unit next to its largest entry
+    const int unit = __reduce_max_sync(kFull, static_cast<int>(r.unit_of(most)));
+    double mass = 0.0;
+    for (int k = 0; k < tiles; ++k) mass += r.template lane_mass<false>(k, threadIdx.x, unit);
+    mass = warp_sum(mass);
+    float top = most;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
+    const int top_i = greedy ? __reduce_min_sync(kFull, most == top ? at_most : 0x7fffffff) : 0;
     n = __reduce_add_sync(kFull, n);
+    if (lane == 0) {
+        s.warp_m[warp] = mass;
+        s.warp_r[warp] = unit;
+        s.warp_top[warp] = top;
+        s.warp_i[warp] = top_i;
+        s.warp_n[warp] = n;
+    }
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // before the first message
-    auto f = r.template locate<false>(tiles, top, top_i, n, u);
-    if (!(f.top > -INFINITY && f.top < INFINITY)) {                  // NaN, +inf or nothing but -inf
-        if (rank == 0 && threadIdx.x == 0) no_distribution(a, row);
-        return;
-    }
-    // log of the whole mass: its unit, and what the rounding of c adds to every exponent alike
-    const double shift = static_cast<double>(f.top) * (static_cast<double>(r.c) - r.c64);
-    if (rule.temperature == 0.f) {
-        if (rank == 0 && threadIdx.x == 0) {
-            const double lse = (log2(f.whole) + f.unit - shift) * 0.69314718055994531;
-            put_row(a, row, f.top_i, static_cast<double>(f.top) - lse, 0.0, 1);
+    __syncthreads();
+    if (warp == 0) {
+        const auto f = r.template locate<false>(u);
+        int again = 0;
+        if (!(f.top > -INFINITY && f.top < INFINITY)) {              // NaN, +inf or nothing but -inf
+            if (rank == 0 && lane == 0) no_distribution(a, row);
+        } else {
+            // log of the whole mass: its unit, less what the rounding of c adds to every exponent alike
+            const double lse = (log2(f.whole) + f.unit - static_cast<double>(f.top) * (static_cast<double>(r.c) - r.c64)) * 0.69314718055994531;
+            if (greedy) {
+                if (rank == 0 && lane == 0) put_row(a, row, f.top_i, static_cast<double>(f.top) - lse, 0.0, 1);
+            } else {
+                // (far from 0 a unit and c times a logit have no digits left to differ in)
+                r.expect(ctas);
+                if (lane < ctas) send(r.box(rank), r.mail(), lane, f.close || !(fabsf(f.top * r.c) <= 0x1p20f));
+                const unsigned long long* got = r.box(0);
+                r.receive();
+                again = __any_sync(kFull, lane < ctas && got[lane < ctas ? lane : 0] != 0);
+                if (!again && f.token >= 0 && lane == 0) {
+                    const double logp = static_cast<double>(f.tz) * rule.inv_t - lse;
+                    put_row(a, row, f.token, logp, logp, f.n);
+                }
+            }
         }
-        return;
-    }
-    const bool fits = fabsf(f.top * r.c) <= 0x1p20f;                // (else a unit and c times a logit have no digits left to differ in)
-    r.expect(ctas);
-    const int close = __syncthreads_or(f.close || !fits);
-    if (threadIdx.x < ctas) send(r.box(rank), r.mail(), threadIdx.x, close != 0);
-    const unsigned long long* got = r.box(0);
-    r.receive();
-    int sum_close = 0;
-    for (int q = 0; q < ctas; ++q) sum_close += static_cast<int>(got[q]);
-    if (sum_close == 0) {
-        if (f.token >= 0 && lane == 0) {
-            const double logp = static_cast<double>(f.tz) * rule.inv_t - (log2(f.whole) + f.unit - shift) * 0.69314718055994531;
-            put_row(a, row, f.token, logp, logp, f.n);
-        }
-        return;
+        if (lane == 0) { s.again = again; s.top = f.top; }
     }
     __syncthreads();
-    if (threadIdx.x < 32) s.exp2_table[threadIdx.x] = exp2(threadIdx.x / 32.0);
+    if (!s.again) return;
+    r.top = s.top;
+    if (warp == 0) s.exp2_table[lane] = exp2(lane / 32.0);
     __syncthreads();
-    r.top = f.top;
+    mass = 0.0;
     for (int k = 0; k < tiles; ++k) {
         Tile<T> t;
         t.load(src, begin + k * kTileEntries, end, r.aligned);
-        r.template weigh_tile<true>(t, k, 0.f);
+        double m = 0.0;
+#pragma unroll
+        for (int i = 0; i < kPerLane; ++i) m += r.template weight<true>(t.value(i), 0);
+        s.lane_x[k][threadIdx.x] = m;
+        mass += m;
     }
-    f = r.template locate<true>(tiles, top, top_i, n, u);
+    mass = warp_sum(mass);
+    if (lane == 0) { s.warp_m[warp] = mass; s.warp_r[warp] = 0; }
+    __syncthreads();
+    if (warp != 0) return;
+    const auto f = r.template locate<true>(u);
     if (f.token >= 0 && lane == 0) {
         const double logp = (static_cast<double>(f.tz) - static_cast<double>(f.top)) * rule.inv_t - log(f.whole);
         put_row(a, row, f.token, logp, logp, f.n);
@@ -1151,12 +1301,15 @@ cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes,
 
 cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_other, int sm_count, cudaStream_t st, int* n_launches) {
     if (any_other) {
-        // a warp's run of entries: up to five tiles, and fewer while the rows leave SMs idle
+        // A warp's run of entries: up to 20 tiles.  More blocks per row while a run is longer than a tile and the rows do not fill the
+        // machine several times over: a block ends with a phase of one warp, which others have to cover (512 rows of 151936, 2 / 4 / 8 / 16
+        // blocks per row: fp32 99 / 90 / 85 / 130 us, bf16 63 / 60 / 76 / 128 us).
+        const long long enough = (bf16 ? 8LL : 16LL) * sm_count;
         int ctas = 1, run = 0;
         for (;; ctas *= 2) {
             run = ((a.V + kWarps * ctas - 1) / (kWarps * ctas) + 7) / 8 * 8;
             if (ctas == kMaxCluster) break;
-            if (run <= kMaxTiles * kTileEntries && (run <= kTileEntries || static_cast<long long>(a.n_rows) * ctas >= sm_count)) break;
+            if (run <= kMaxTiles * kTileEntries && (run <= kTileEntries || static_cast<long long>(a.n_rows) * ctas >= enough)) break;
         }
         const cudaError_t e = launch_clusters(bf16 ? k_sample_stream<__nv_bfloat16> : k_sample_stream<float>, a.n_rows, ctas, 0, st, a, run, ctas);
         if (e != cudaSuccess) return e;
