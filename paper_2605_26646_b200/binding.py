@@ -565,60 +565,74 @@ def unity_clip_grad_norm_workspace_bytes(n_tensors: int, K: int) -> int:
 
 
 _TYPES = {torch.float32: UNITY_F32, torch.bfloat16: UNITY_BF16}
+_PTRS = [C.c_void_p * k for k in range(UNITY_MAX_MODELS + 1)]      # (making an array type costs as much as filling it)
+_INTS = [C.c_int32 * k for k in range(UNITY_MAX_ROLES + 1)]
+
+
+def _fit(t: Optional[torch.Tensor], shape, dtype, base, name) -> Optional[int]:
+    """_sized against the tensor `base`, with the fewest calls where all is well: these calls take microseconds themselves."""
+    if t is None:
+        return None
+    if t.shape == shape and t.dtype is dtype and t.get_device() == base.get_device() and t.is_contiguous():
+        return t.data_ptr()
+    return _sized(t, shape, dtype, base.device, name)
 
 
 def _type_of(t: torch.Tensor, name) -> int:
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise TypeError(f"{name}: expected float32 or bfloat16, got {t.dtype}")
-    return _TYPES[t.dtype]
+    return kind
 
 
-def _norm_rows(x, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps):
-    if x.dim() != 2 or not gamma or inv_role.dim() != 1:
+def _norm_rows(x, shape, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps):
+    if len(shape) != 2 or not gamma or inv_role.dim() != 1:
         raise ValueError("token rows must be [n_tok, H], gamma a non-empty sequence of [H] and inv_role [n_inv]")
     if not x.is_cuda:
         raise ValueError("token rows must be a CUDA tensor")
-    n_tok, H = x.shape
-    dev, n_inv, kind = x.device, inv_role.shape[0], gamma[0].dtype
-    gtype = _type_of(gamma[0], "gamma")
-    gp = (C.c_void_p * len(gamma))(*[_sized(g, (H,), kind, dev, "gamma") for g in gamma])
-    rm = (C.c_int32 * len(role_model))(*[int(r) for r in role_model])
-    return unity_norm_rows(n_tok, H, len(gamma), n_inv, len(role_model),
-                           _sized(cu_seqlens, (n_inv + 1,), torch.int64, dev, "cu_seqlens"),
-                           _sized(inv_role, (n_inv,), torch.int32, dev, "inv_role"), rm,
-                           _sized(tok_mask, (n_tok,), torch.uint8, dev, "tok_mask"), gp, gtype, float(eps))
+    K, R = len(gamma), len(role_model)
+    n_tok, H = shape
+    per_model, kind, n_inv = (H,), gamma[0].dtype, inv_role.shape[0]
+    if K > UNITY_MAX_MODELS or R > UNITY_MAX_ROLES:
+        raise ValueError(f"at most {UNITY_MAX_MODELS} models and {UNITY_MAX_ROLES} roles")
+    return unity_norm_rows(n_tok, H, K, n_inv, R, _fit(cu_seqlens, (n_inv + 1,), torch.int64, x, "cu_seqlens"),
+                           _fit(inv_role, (n_inv,), torch.int32, x, "inv_role"), _INTS[R](*role_model),
+                           _fit(tok_mask, (n_tok,), torch.uint8, x, "tok_mask"),
+                           _PTRS[K](*[_fit(g, per_model, kind, x, "gamma") for g in gamma]), _type_of(gamma[0], "gamma"), eps)
 
 
 def unity_rms_norm_fwd(ctx, x, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps: float, y, residual=None,
                        res_out=None) -> None:
     """x, y: bf16 [n_tok, H]; gamma: K tensors [H], all f32 or all bf16; residual, res_out: f32 or bf16 [n_tok, H]."""
-    rows = _norm_rows(x, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
-    b16, dev = torch.bfloat16, x.device
-    rtype = UNITY_BF16 if residual is None else _type_of(residual, "residual")
-    kind = b16 if residual is None else residual.dtype
+    shape, b16 = x.shape, torch.bfloat16
+    rows = _norm_rows(x, shape, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
+    rtype, kind = (UNITY_BF16, b16) if residual is None else (_type_of(residual, "residual"), residual.dtype)
     if y is None:
         raise ValueError("y is None")
-    _raise(ctx, load_library().unity_rms_norm_fwd(
-        ctx, C.byref(rows), _sized(x, x.shape, b16, dev, "x"), _sized(residual, x.shape, kind, dev, "residual"), rtype,
-        _sized(y, x.shape, b16, dev, "y"), _sized(res_out, x.shape, kind, dev, "res_out")))
+    code = load_library().unity_rms_norm_fwd(
+        ctx, rows, _fit(x, shape, b16, x, "x"), _fit(residual, shape, kind, x, "residual"), rtype, _fit(y, shape, b16, x, "y"),
+        _fit(res_out, shape, kind, x, "res_out"))
+    if code:
+        _raise(ctx, code)
 
 
 def unity_rms_norm_bwd(ctx, res, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps: float, dy, dx, dres=None,
                        dgamma=None, accumulate_dgamma: bool = False) -> None:
     """res, dres, dx: all f32 or all bf16 [n_tok, H]; dy: bf16; dgamma: K f32 tensors [H], or None for a frozen norm."""
-    rows = _norm_rows(res, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
-    dev, rtype = res.device, _type_of(res, "res")
+    shape, kind = res.shape, res.dtype
+    rows = _norm_rows(res, shape, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
     if dy is None or dx is None:
         raise ValueError("dy / dx is None")
     dg = None
     if dgamma is not None:
         if len(dgamma) != len(gamma):
             raise ValueError(f"dgamma: expected {len(gamma)} tensors, got {len(dgamma)}")
-        dg = (C.c_void_p * len(dgamma))(*[_sized(g, (res.shape[1],), torch.float32, dev, "dgamma") for g in dgamma])
-    _raise(ctx, load_library().unity_rms_norm_bwd(
-        ctx, C.byref(rows), _sized(res, res.shape, res.dtype, dev, "res"), rtype,
-        _sized(dy, res.shape, torch.bfloat16, dev, "dy"), _sized(dres, res.shape, res.dtype, dev, "dres"),
-        _sized(dx, res.shape, res.dtype, dev, "dx"), dg, 1 if accumulate_dgamma else 0))
+        dg = _PTRS[len(dgamma)](*[_fit(g, shape[1:], torch.float32, res, "dgamma") for g in dgamma])
+    code = load_library().unity_rms_norm_bwd(
+        ctx, rows, _fit(res, shape, kind, res, "res"), _type_of(res, "res"), _fit(dy, shape, torch.bfloat16, res, "dy"),
+        _fit(dres, shape, kind, res, "dres"), _fit(dx, shape, kind, res, "dx"), dg, 1 if accumulate_dgamma else 0)
+    if code:
+        _raise(ctx, code)
 
 
 class GradTensors:
@@ -652,32 +666,36 @@ def unity_clip_grad_norm(ctx, tensors: GradTensors, max_norm: Optional[Sequence[
     K = norm.shape[0]
     if max_norm is not None and len(max_norm) != K:
         raise ValueError(f"max_norm: expected {K} values, got {len(max_norm)}")
-    bounds = None if max_norm is None else (C.c_float * K)(*[float(x) for x in max_norm])
-    dev = norm.device if tensors.device is None else tensors.device
+    bounds = None if max_norm is None else (C.c_float * K)(*max_norm)
+    base = tensors.grads[0] if tensors.grads else norm
     if not norm.is_cuda:
         raise ValueError("norm must be a CUDA tensor")
-    _raise(ctx, load_library().unity_clip_grad_norm(ctx, len(tensors), tensors.array, K, bounds,
-                                                    _sized(norm, (K,), torch.float32, dev, "norm"),
-                                                    _sized(coef, (K,), torch.float32, dev, "coef")))
+    code = load_library().unity_clip_grad_norm(ctx, len(tensors.grads), tensors.array, K, bounds,
+                                               _fit(norm, (K,), torch.float32, base, "norm"),
+                                               _fit(coef, (K,), torch.float32, base, "coef"))
+    if code:
+        _raise(ctx, code)
 
 
 def unity_sample(ctx, logits, rules, u, token, row_role=None, row_mask=None, logp=None, logp_kept=None, n_kept=None) -> None:
     """logits: f32 or bf16 [n_rows, V], rows of any pitch; rules: (temperature, top_k, top_p, min_p) of each role."""
-    if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    shape = logits.shape
+    if len(shape) != 2 or (shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [n_rows, V] with consecutive entries in a row")
     if not logits.is_cuda:
         raise ValueError("logits must be a CUDA tensor")
     if u is None or token is None:
         raise ValueError("u / token is None")
-    n, V = logits.shape
-    ld = logits.stride(0) if n > 1 else V
-    dev, f32, i32, per = logits.device, torch.float32, torch.int32, (n,)
-    arr = (unity_sampling_rule * len(rules))(*[unity_sampling_rule(float(t), int(k), float(p), float(m)) for t, k, p, m in rules])
-    _raise(ctx, load_library().unity_sample(
-        ctx, n, V, logits.data_ptr(), _type_of(logits, "logits"), ld, len(rules), _sized(row_role, per, i32, dev, "row_role"),
-        arr, _sized(row_mask, per, torch.uint8, dev, "row_mask"), _sized(u, per, f32, dev, "u"),
-        _sized(token, per, i32, dev, "token"), _sized(logp, per, f32, dev, "logp"),
-        _sized(logp_kept, per, f32, dev, "logp_kept"), _sized(n_kept, per, i32, dev, "n_kept")))
+    n, V = shape
+    f32, i32, per = torch.float32, torch.int32, (n,)
+    arr = (unity_sampling_rule * len(rules))(*rules)
+    code = load_library().unity_sample(
+        ctx, n, V, logits.data_ptr(), _type_of(logits, "logits"), logits.stride(0) if n > 1 else V, len(rules),
+        _fit(row_role, per, i32, logits, "row_role"), arr, _fit(row_mask, per, torch.uint8, logits, "row_mask"),
+        _fit(u, per, f32, logits, "u"), _fit(token, per, i32, logits, "token"), _fit(logp, per, f32, logits, "logp"),
+        _fit(logp_kept, per, f32, logits, "logp_kept"), _fit(n_kept, per, i32, logits, "n_kept"))
+    if code:
+        _raise(ctx, code)
 
 
 # ------------------------------------------------------------------------------------------------

@@ -11,7 +11,16 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kThreads = 256;
-constexpr int kChunk = kThreads * 32;        // elements: four vectors of eight per thread
+// A chunk is 32 KB of what is read: 128 bytes in flight per thread, 128 KB on an SM with four blocks (half of that for bf16, as with
+// chunks of as many elements, left 40 % of the rate).
+__host__ __device__ constexpr int chunk_of(bool bf16) { return kThreads * 8 * (bf16 ? 8 : 4); }   // elements: vectors of eight
+
+// Both kernels begin with this, before any access to global memory: they may be in place when the kernel before them ends, and wait
+// for it to complete.
+__device__ __forceinline__ void begin() {
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
+}
 
 template <int N>
 struct ClipTable {
@@ -53,17 +62,15 @@ __device__ __forceinline__ void put(const ClipEntry& e, long long i, float v) {
     else static_cast<float*>(e.dst)[i] = v;
 }
 // Eight elements from an aligned place.
-__device__ __forceinline__ void load8(const ClipEntry& e, long long i, float (&f)[8]) {
-    if (e.src_bf16) {
-        const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(e.src) + i);
-        const unsigned w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&f)[8]) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { f[2 * k] = __uint_as_float(w[k] << 16); f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
-    } else {
-        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(e.src) + i);
-        const float4 a = p[0], b = p[1];
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    }
+    for (int k = 0; k < 4; ++k) { f[2 * k] = __uint_as_float(w[k] << 16); f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u); }
+}
+__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
 __device__ __forceinline__ void store8(const ClipEntry& e, long long i, const float (&f)[8], bool aligned) {
     if (!aligned) {
@@ -101,11 +108,11 @@ __device__ __forceinline__ double squares(const float (&f)[8]) {
 // The vectors of chunk `c` of the launch, which belongs to entry e: elements [i0, i1) of it, vectors in [v0, v1).
 struct Span { long long i0, i1, v0, v1; };
 __device__ __forceinline__ Span span_of(const ClipEntry& e, long long c) {
-    const long long h = head_of(e), local = c - e.chunk0;
+    const long long h = head_of(e), local = c - e.chunk0, chunk = chunk_of(e.src_bf16);
     Span s;
-    s.v0 = h + local * kChunk;
+    s.v0 = h + local * chunk;
     s.i0 = local == 0 ? 0 : s.v0;
-    s.i1 = s.v0 + kChunk < e.n ? s.v0 + kChunk : e.n;
+    s.i1 = s.v0 + chunk < e.n ? s.v0 + chunk : e.n;
     s.v1 = s.v0 + (s.i1 - s.v0) / 8 * 8;
     return s;
 }
@@ -119,8 +126,29 @@ __device__ __forceinline__ int entry_of(const ClipTable<N>& t, long long c) {
     return lo;
 }
 
+template <typename T>
+__device__ __forceinline__ double chunk_squares(const T* src, const Span& s) {
+    constexpr int kEach = 16 / sizeof(T);
+    double acc = 0.0;
+    float f[kEach][8];
+    if (s.v1 - s.v0 == kEach * kThreads * 8) {
+        const T* p = src + s.v0 + threadIdx.x * 8;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) load8(p + j * kThreads * 8, f[j]);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) acc += squares(f[j]);
+        return acc;
+    }
+    for (long long i = s.v0 + threadIdx.x * 8; i < s.v1; i += kThreads * 8) {
+        load8(src + i, f[0]);
+        acc += squares(f[0]);
+    }
+    return acc;
+}
+
 template <int N>
 __global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant__ ClipArgs a, const __grid_constant__ ClipTable<N> t) {
+    begin();
     __shared__ double slots[kThreads / 32], sums[UNITY_MAX_MODELS];
     const long long first = t.chunks * blockIdx.x / gridDim.x, last = t.chunks * (blockIdx.x + 1) / gridDim.x;
     if (threadIdx.x < UNITY_MAX_MODELS) sums[threadIdx.x] = 0.0;
@@ -136,15 +164,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant
             model = e.model;
         }
         const Span s = span_of(e, c);
-        float f[4][8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long i = s.v0 + (j * kThreads + threadIdx.x) * 8;
-            if (i < s.v1) load8(e, i, f[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (s.v0 + (j * kThreads + threadIdx.x) * 8 < s.v1) acc += squares(f[j]);
+        acc += e.src_bf16 ? chunk_squares(static_cast<const __nv_bfloat16*>(e.src), s) : chunk_squares(static_cast<const float*>(e.src), s);
         // up to seven elements before the vectors and seven behind them
         const long long i = s.i0 + threadIdx.x, tail = s.v1 + threadIdx.x;
         if (i < s.v0) { const double v = element(e, i); acc = fma(v, v, acc); }
@@ -161,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) k_grad_squares(const __grid_constant
 // Norm of a model in fp64: the partial sums of all launches' blocks, shared among the threads in a fixed way.
 __device__ __forceinline__ double model_norm(const ClipArgs& a, int model, double (&slots)[kThreads / 32]) {
     double s = 0.0;
-    const long long n = static_cast<long long>(a.n_launches) * kClipBlocks;
+    const long long n = a.n_launches == 1 ? a.blocks : static_cast<long long>(a.n_launches) * kClipBlocks;
     for (long long b = threadIdx.x; b < n; b += kThreads) s += a.partial[b * a.K + model];
     return sqrt(block_sum(s, slots));
 }
@@ -170,8 +190,34 @@ __device__ __forceinline__ float factor_of(const ClipArgs& a, int model, double 
     return !a.has_max || norm <= static_cast<double>(a.max_norm[model]) ? 1.f : static_cast<float>(static_cast<double>(a.max_norm[model]) / norm);
 }
 
+template <typename T>
+__device__ __forceinline__ void chunk_scale(const ClipEntry& e, const Span& s, float coef, bool aligned) {
+    constexpr int kEach = 16 / sizeof(T);
+    const T* src = static_cast<const T*>(e.src);
+    float f[kEach][8];
+    if (s.v1 - s.v0 == kEach * kThreads * 8) {
+        const long long i = s.v0 + threadIdx.x * 8;
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) load8(src + i + j * kThreads * 8, f[j]);
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[j][q] *= coef;
+            store8(e, i + j * kThreads * 8, f[j], aligned);
+        }
+        return;
+    }
+    for (long long i = s.v0 + threadIdx.x * 8; i < s.v1; i += kThreads * 8) {
+        load8(src + i, f[0]);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) f[0][q] *= coef;
+        store8(e, i, f[0], aligned);
+    }
+}
+
 template <int N>
 __global__ void __launch_bounds__(kThreads) k_grad_scale(const __grid_constant__ ClipArgs a, const __grid_constant__ ClipTable<N> t) {
+    begin();
     __shared__ double slots[kThreads / 32];
     if (t.launch == 0 && blockIdx.x == 0) {
         for (int m = 0; m < a.K; ++m) {
@@ -196,46 +242,40 @@ __global__ void __launch_bounds__(kThreads) k_grad_scale(const __grid_constant__
         if (e.src == e.dst && coef == 1.f) continue;
         const Span s = span_of(e, c);
         const bool aligned = (reinterpret_cast<uintptr_t>(e.dst) / (e.dst_bf16 ? 2 : 4) + s.v0) % 8 == 0;
-        float f[4][8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long i = s.v0 + (j * kThreads + threadIdx.x) * 8;
-            if (i < s.v1) load8(e, i, f[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const long long i = s.v0 + (j * kThreads + threadIdx.x) * 8;
-            if (i < s.v1) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q) f[j][q] *= coef;
-                store8(e, i, f[j], aligned);
-            }
-        }
+        if (e.src_bf16) chunk_scale<__nv_bfloat16>(e, s, coef, aligned);
+        else chunk_scale<float>(e, s, coef, aligned);
         const long long i = s.i0 + threadIdx.x, tail = s.v1 + threadIdx.x;
         if (i < s.v0) put(e, i, element(e, i) * coef);
         if (tail < s.i1) put(e, tail, element(e, tail) * coef);
     }
 }
 
-int blocks_of(long long chunks) { return static_cast<int>(chunks < 1 ? 1 : (chunks < kClipBlocks ? chunks : kClipBlocks)); }
-
 template <int N, bool SCALE>
 cudaError_t launch_table(const ClipArgs& a, const ClipEntry* entries, int n, long long chunks, int launch, cudaStream_t st) {
     ClipTable<N> t;
     t.n = n; t.launch = launch; t.chunks = chunks;
     for (int i = 0; i < n; ++i) t.e[i] = entries[i];
-    // the squares' blocks beyond the chunks still write their zeros: the sums are over all of them
-    if (SCALE) k_grad_scale<N><<<blocks_of(chunks), kThreads, 0, st>>>(a, t);
-    else k_grad_squares<N><<<kClipBlocks, kThreads, 0, st>>>(a, t);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    // (with several launches the sums are over all blocks that each might have: those without a chunk write their zeros)
+    cfg.gridDim = dim3(SCALE || a.n_launches == 1 ? clip_blocks(chunks) : kClipBlocks);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return SCALE ? cudaLaunchKernelEx(&cfg, k_grad_scale<N>, a, t) : cudaLaunchKernelEx(&cfg, k_grad_squares<N>, a, t);
 }
 
 }  // namespace
 
 long long clip_chunks(const ClipEntry& e) {
     const long long body = e.n - head_of(e);
-    return e.n == 0 ? 0 : (body <= kChunk ? 1 : (body + kChunk - 1) / kChunk);
+    const long long chunk = chunk_of(e.src_bf16);
+    return e.n == 0 ? 0 : (body <= chunk ? 1 : (body + chunk - 1) / chunk);
 }
+int clip_blocks(long long chunks) { return static_cast<int>(chunks < 1 ? 1 : (chunks < kClipBlocks ? chunks : kClipBlocks)); }
 
 // Few tensors go with a small table: a launch's parameters are copied with it.
 cudaError_t launch_grad_squares(const ClipArgs& a, const ClipEntry* entries, int n, long long chunks, int launch, cudaStream_t st) {

@@ -664,7 +664,7 @@ struct NormArgs {
     int* status;
 };
 cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t stream);
-int norm_bwd_blocks(long long n_tok);
+int norm_bwd_blocks(long long n_tok, int H);
 cudaError_t launch_norm_bwd(const NormArgs& a, int blocks, cudaStream_t stream, int* n_launches);
 
 // ----------------------------------------------------------------------------------------------
@@ -681,9 +681,11 @@ struct ClipEntry {
 constexpr int kClipBlocks = 148 * 4;     // blocks of a launch at most: a double per model of each in the workspace
 constexpr int kClipEntries = 800;        // entries of a launch at most: 32 000 bytes of parameters
 long long clip_chunks(const ClipEntry& e);
+int clip_blocks(long long chunks);       // of a launch over so many chunks
 struct ClipArgs {
     double* partial;                     // [launches][kClipBlocks][K]
     int K, n_launches, write;            // write: there is something to scale
+    int blocks;                          // of the only launch
     int has_max;
     float max_norm[UNITY_MAX_MODELS];
     float *norm, *coef;                  // coef nullable

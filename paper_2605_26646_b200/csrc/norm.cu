@@ -11,15 +11,22 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 
+// Every kernel here calls this before its first access to global memory: it may be in place when the kernel before it ends, and waits
+// for that one to complete.
+__device__ __forceinline__ void begin() {
+    ptx::grid_launch_dependents();
+    ptx::grid_wait();
+}
+
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
     return v;
 }
 
-// Model of token `tok` by the whole warp: 32 places of the offsets are looked at per step (a role in 8192 invocations takes
-// three dependent loads instead of thirteen).  -1: an id out of range, which is flagged.
-__device__ __forceinline__ int token_model(const NormArgs& a, long long tok, int lane) {
+// Invocation of token `tok` by the whole warp: 32 places of the offsets are looked at per step (one of 8192 invocations takes three
+// dependent loads instead of thirteen).
+__device__ __forceinline__ int token_invocation(const NormArgs& a, long long tok, int lane) {
     int lo = 0, hi = a.n_inv;                                   // the number of ends cu[1..n_inv] that are <= tok lies in [lo, hi]
     while (lo < hi) {
         const int step = (hi - lo + 31) / 32;
@@ -31,10 +38,12 @@ __device__ __forceinline__ int token_model(const NormArgs& a, long long tok, int
         hi = n == 32 ? hi : min(hi, next);
         lo = min(lo, hi);
     }
-    const int role = a.inv_role[min(lo, a.n_inv - 1)];
-    if (role >= 0 && role < a.n_roles) return a.role_model[role];
-    if (lane == 0) atomicOr(a.status, kStatusBadIndex);
-    return -1;
+    return min(lo, a.n_inv - 1);
+}
+// Its model, -1 for a role out of range.
+__device__ __forceinline__ int invocation_model(const NormArgs& a, int s) {
+    const int role = a.inv_role[s];
+    return role >= 0 && role < a.n_roles ? a.role_model[role] : -1;
 }
 
 // Eight consecutive elements.  Plain loads, not the read-only path: an output may be the input's own memory.
@@ -82,6 +91,12 @@ template <typename T> struct RawOf;
 template <> struct RawOf<__nv_bfloat16> { typedef Raw16 type; };
 template <> struct RawOf<float> { typedef Raw32 type; };
 
+// Copies to shared memory; both sides and the size in multiples of 16 bytes.
+__device__ __forceinline__ void bulk_load(void* to, const void* from, unsigned bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ptx::smem_u32(to)), "l"(from),
+                 "r"(bytes), "r"(ptx::smem_u32(bar)) : "memory");
+}
+
 // Sum of a pair over the WPR warps of a row; `slots` holds two of them in turn, so that one barrier per call is enough.
 template <int WPR>
 __device__ __forceinline__ float2 row_sum(float2 v, float2 (&slots)[2][WPR], int turn) {
@@ -104,6 +119,7 @@ __device__ __forceinline__ float2 row_sum(float2 v, float2 (&slots)[2][WPR], int
 constexpr int kFwdRowsOfWarps = 4;          // rows of a block whose rows belong to one warp each
 template <int WPR, int NV, typename R, bool HAS_R>
 __global__ void __launch_bounds__(WPR == 1 ? 32 * kFwdRowsOfWarps : 32 * WPR) k_norm_fwd(const __grid_constant__ NormArgs a) {
+    begin();
     __shared__ float2 slots[2][WPR];
     const int lane = threadIdx.x & 31;
     const int t = WPR == 1 ? lane : threadIdx.x;
@@ -111,7 +127,10 @@ __global__ void __launch_bounds__(WPR == 1 ? 32 * kFwdRowsOfWarps : 32 * WPR) k_
     if (row >= a.n_tok) return;                                  // (a whole warp, or a whole block)
     const int H = a.H;
     const long long base = row * H;
-    bool on = a.tok_mask == nullptr || a.tok_mask[row] != 0;
+    // (the search for the model needs nothing of the mask: the loads of both are on their way together)
+    const uint8_t mask = a.tok_mask == nullptr ? 1 : a.tok_mask[row];
+    const int inv = token_invocation(a, row, lane);
+    bool on = mask != 0;
     int model = -1;
     Raw16 x[NV];
     typename RawOf<R>::type res[NV];
@@ -124,8 +143,9 @@ __global__ void __launch_bounds__(WPR == 1 ? 32 * kFwdRowsOfWarps : 32 * WPR) k_
                 if (HAS_R) load8(static_cast<const R*>(a.residual) + base + col, res[j]);
             }
         }
-        model = token_model(a, row, lane);
+        model = invocation_model(a, inv);
         on = model >= 0;
+        if (!on && lane == 0) atomicOr(a.status, kStatusBadIndex);
     }
     if (!on) {                                                   // (the same for every warp of the row)
         const float zero[8] = {};
@@ -179,15 +199,57 @@ __global__ void __launch_bounds__(WPR == 1 ? 32 * kFwdRowsOfWarps : 32 * WPR) k_
 
 // ------------------------------------------------------------------------------------------------
 // dr = s g - r s^3 mean(g r) + dres with g = dy gamma; dgamma += dy r s.  A block takes a run of consecutive rows, so that its
-// dgamma stays in registers; where the model changes it goes to the block's slice of that model and the next one begins.
+// dgamma stays in registers; where the model changes it goes to the block's slice of that model and the next one begins.  The rows
+// come through a ring in shared memory, by asynchronous copies that run ahead of the row that is worked on: registers hold the
+// columns' sums and weights only, and HBM is asked for rows without a pause.
 // ------------------------------------------------------------------------------------------------
+constexpr int kMaxStages = 4;
 template <int WPR, int NV, typename R, bool DG>
-__global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ NormArgs a, int stages, int ring_dres) {
     __shared__ float2 slots[2][WPR];
-    const int lane = threadIdx.x & 31, t = threadIdx.x, H = a.H;
+    __shared__ uint64_t full[kMaxStages];
+    extern __shared__ __align__(16) unsigned char ring[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, t = threadIdx.x, H = a.H;
     const long long first = a.n_tok * blockIdx.x / gridDim.x, last = a.n_tok * (blockIdx.x + 1) / gridDim.x;
-    float acc[NV][8];
-    int model = -1, turn = 0;
+    const unsigned res_bytes = H * sizeof(R), dy_bytes = H * 2, stage_bytes = res_bytes + dy_bytes + (ring_dres ? res_bytes : 0);
+    if (t == 0) {
+        for (int i = 0; i < stages; ++i) ptx::mbar_init(&full[i], 1);
+        ptx::fence_barrier_init();
+    }
+    __syncthreads();
+    begin();
+    // mask bits of the 32 rows from `base`
+    auto bits_of = [&](long long base) {
+        return __ballot_sync(kFull, base + lane < last && (a.tok_mask == nullptr || a.tok_mask[base + lane] != 0));
+    };
+    // The first warp asks for the unmasked rows in order, `stages` of them ahead.
+    long long ask_base = first;
+    unsigned ask_bits = warp == 0 && first < last ? bits_of(first) : 0;
+    int asked = 0;
+    auto ask = [&]() {
+        while (ask_bits == 0) {
+            if (ask_base + 32 >= last) return;
+            ask_base += 32;
+            ask_bits = bits_of(ask_base);
+        }
+        const long long at = (ask_base + __ffs(ask_bits) - 1) * H;
+        ask_bits &= ask_bits - 1;
+        if (lane == 0) {
+            const int stage = asked % stages;
+            unsigned char* to = ring + static_cast<size_t>(stage) * stage_bytes;
+            ptx::mbar_arrive_expect_tx(&full[stage], stage_bytes);
+            bulk_load(to, static_cast<const R*>(a.res) + at, res_bytes, &full[stage]);
+            bulk_load(to + res_bytes, a.dy + at, dy_bytes, &full[stage]);
+            if (ring_dres) bulk_load(to + res_bytes + dy_bytes, static_cast<const R*>(a.dres) + at, res_bytes, &full[stage]);
+        }
+        ++asked;
+    };
+    if (warp == 0)
+        for (int i = 0; i < stages; ++i) ask();
+
+    float acc[NV][8], gamma[NV][8];
+    int model = -1, found = -1, done = 0;
+    long long found_end = first;
     unsigned touched = 0;
     auto flush = [&]() {
         if (!DG || model < 0) return;
@@ -209,13 +271,14 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
         }
         touched |= 1u << model;
     };
+    unsigned bits = 0;
     for (long long row = first; row < last; ++row) {
+        const int place = static_cast<int>(row - first) & 31;
+        if (place == 0) bits = bits_of(row);
         const long long base = row * H;
-        const bool on = a.tok_mask == nullptr || a.tok_mask[row] != 0;
-        const int m = on ? token_model(a, row, lane) : -1;
         R* dx = static_cast<R*>(a.dx) + base;
-        if (m < 0) {
-            const float zero[8] = {};
+        const float zero[8] = {};
+        if (!(bits >> place & 1)) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int col = (j * WPR * 32 + t) * 8;
@@ -223,65 +286,78 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
             }
             continue;
         }
-        if (m != model) {
+        if (row >= found_end) {
+            const int inv = token_invocation(a, row, lane);
+            found = invocation_model(a, inv);
+            found_end = a.cu_seqlens[inv + 1];
+            if (found < 0 && lane == 0) atomicOr(a.status, kStatusBadIndex);
+        }
+        const int m = found;
+        if (m >= 0 && m != model) {
             flush();
             model = m;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+            for (int j = 0; j < NV; ++j) {
+                const int col = (j * WPR * 32 + t) * 8;
+                if (col < H) load_gamma(a, m, col, gamma[j]);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) acc[j][i] = 0.f;
-        }
-        typename RawOf<R>::type res[NV];
-        Raw16 dy[NV];
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int col = (j * WPR * 32 + t) * 8;
-            if (col < H) {
-                load8(static_cast<const R*>(a.res) + base + col, res[j]);
-                load8(a.dy + base + col, dy[j]);
             }
         }
+        const int stage = done % stages;
+        const unsigned char* in = ring + static_cast<size_t>(stage) * stage_bytes;
+        const R* res = reinterpret_cast<const R*>(in);
+        const __nv_bfloat16* dy = reinterpret_cast<const __nv_bfloat16*>(in + res_bytes);
+        const R* dres = ring_dres ? reinterpret_cast<const R*>(in + res_bytes + dy_bytes) : a.dres ? static_cast<const R*>(a.dres) + base : nullptr;
+        if (!ptx::mbar_wait(&full[stage], done / stages & 1, kWaitBudgetCycles) && lane == 0) atomicOr(a.status, kStatusTimeout);
         float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = (j * WPR * 32 + t) * 8;
             if (col < H) {
-                float r[8], d[8], g[8];
-                widen(res[j], r);
-                widen(dy[j], d);
-                load_gamma(a, m, col, g);
+                typename RawOf<R>::type raw_r;
+                Raw16 raw_d;
+                float r[8], d[8];
+                load8(res + col, raw_r);
+                load8(dy + col, raw_d);
+                widen(raw_r, r);
+                widen(raw_d, d);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     sum.x = fmaf(r[i], r[i], sum.x);
-                    sum.y = fmaf(d[i] * g[i], r[i], sum.y);
+                    sum.y = fmaf(d[i] * gamma[j][i], r[i], sum.y);
                 }
             }
         }
-        sum = row_sum<WPR>(sum, slots, turn);
-        turn ^= 1;
+        // (a barrier: every warp is through with the row before, whose place in the ring takes the next one)
+        sum = row_sum<WPR>(sum, slots, done & 1);
+        if (warp == 0 && done > 0) ask();
+        ++done;
         const float s = 1.f / sqrtf(sum.x / static_cast<float>(H) + a.eps);
         const float c = s * s * s * (sum.y / static_cast<float>(H));
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = (j * WPR * 32 + t) * 8;
             if (col < H) {
+                typename RawOf<R>::type raw_r;
+                Raw16 raw_d;
                 float r[8], d[8], g[8];
-                widen(res[j], r);
-                widen(dy[j], d);
-                load_gamma(a, m, col, g);
+                load8(res + col, raw_r);
+                load8(dy + col, raw_d);
+                widen(raw_r, r);
+                widen(raw_d, d);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    g[i] = s * (d[i] * g[i]) - c * r[i];
-                    if (DG) acc[j][i] = fmaf(d[i], r[i] * s, acc[j][i]);
-                }
-                if (a.dres) {
-                    typename RawOf<R>::type more;
-                    load8(static_cast<const R*>(a.dres) + base + col, more);
-                    widen(more, r);
+                for (int i = 0; i < 8; ++i) g[i] = s * (d[i] * gamma[j][i]) - c * r[i];
+                if (DG && m >= 0)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[j][i] = fmaf(d[i], r[i] * s, acc[j][i]);
+                if (dres) {
+                    load8(dres + col, raw_r);
+                    widen(raw_r, r);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) g[i] += r[i];
                 }
-                store8(dx + col, g);
+                if (m >= 0) store8(dx + col, g); else store8(dx + col, zero);
             }
         }
     }
@@ -289,24 +365,34 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
     if (DG && t == 0) a.touched[blockIdx.x] = touched;
 }
 
-// dgamma of 128 columns of one model: the warps share the blocks' slices, each in ascending order, then warp by warp.
+// dgamma of 32 columns of one model: the block's 64 groups of eight lanes share the blocks' slices, each adds its own up in ascending
+// order, then the groups in a fixed tree.
 constexpr int kDgammaWarps = 16;
 __global__ void __launch_bounds__(32 * kDgammaWarps) k_norm_dgamma(const __grid_constant__ NormArgs a, int slices) {
-    __shared__ float4 part[kDgammaWarps][32];
+    begin();
+    __shared__ float4 part[kDgammaWarps][8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = blockIdx.y;
-    const int col = blockIdx.x * 128 + lane * 4;
+    const int col = blockIdx.x * 32 + (lane & 7) * 4, group = threadIdx.x >> 3;
+    const float* from = a.parts + static_cast<long long>(k) * a.H + col;
+    const long long pitch = static_cast<long long>(a.K) * a.H;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (col < a.H) {
 #pragma unroll 4
-        for (int b = warp; b < slices; b += kDgammaWarps) {
-            if (!(a.touched[b] >> k & 1)) continue;
-            const float4 v = *reinterpret_cast<const float4*>(a.parts + (static_cast<long long>(b) * a.K + k) * a.H + col);
+    for (int b = group; b < slices; b += 4 * kDgammaWarps)
+        if (a.touched[b] >> k & 1) {
+            const float4 v = *reinterpret_cast<const float4*>(from + b * pitch);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
+#pragma unroll
+    for (int o = 8; o < 32; o <<= 1) {
+        s.x += __shfl_xor_sync(kFull, s.x, o);
+        s.y += __shfl_xor_sync(kFull, s.y, o);
+        s.z += __shfl_xor_sync(kFull, s.z, o);
+        s.w += __shfl_xor_sync(kFull, s.w, o);
     }
-    part[warp][lane] = s;
+    if (lane < 8) part[warp][lane] = s;
     __syncthreads();
-    if (warp != 0 || col >= a.H) return;
+    if (threadIdx.x >= 8) return;
+    s = part[0][lane];
     for (int w = 1; w < kDgammaWarps; ++w) {
         const float4 v = part[w][lane];
         s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -319,25 +405,53 @@ __global__ void __launch_bounds__(32 * kDgammaWarps) k_norm_dgamma(const __grid_
     *out = s;
 }
 
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, int bytes, cudaStream_t stream, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
 template <int WPR, int NV>
 cudaError_t fwd_rows(const NormArgs& a, cudaStream_t st) {
     const int rows = WPR == 1 ? kFwdRowsOfWarps : 1, threads = 32 * WPR * rows;
     const unsigned grid = static_cast<unsigned>((a.n_tok + rows - 1) / rows);
-    if (a.residual == nullptr) k_norm_fwd<WPR, NV, __nv_bfloat16, false><<<grid, threads, 0, st>>>(a);
-    else if (a.res_bf16) k_norm_fwd<WPR, NV, __nv_bfloat16, true><<<grid, threads, 0, st>>>(a);
-    else k_norm_fwd<WPR, NV, float, true><<<grid, threads, 0, st>>>(a);
-    return cudaGetLastError();
+    if (a.residual == nullptr) return launch(k_norm_fwd<WPR, NV, __nv_bfloat16, false>, grid, threads, 0, st, a);
+    if (a.res_bf16) return launch(k_norm_fwd<WPR, NV, __nv_bfloat16, true>, grid, threads, 0, st, a);
+    return launch(k_norm_fwd<WPR, NV, float, true>, grid, threads, 0, st, a);
+}
+// The ring's depth and what it holds: as many rows as leave room for two blocks on an SM, or for one; a row's dres stays outside
+// where two rows with it do not fit.
+struct Ring { int stages, dres, bytes; };
+Ring ring_of(const NormArgs& a) {
+    const int width = a.res_bf16 ? 2 : 4;
+    Ring r;
+    r.dres = a.dres != nullptr && 2 * a.H * (2 * width + 2) <= 220 * 1024;
+    const int stage = a.H * (width + 2 + (r.dres ? width : 0));
+    r.stages = 110 * 1024 / stage;
+    r.stages = r.stages < 2 ? 2 : r.stages > kMaxStages ? kMaxStages : r.stages;
+    r.bytes = r.stages * stage;
+    return r;
+}
+template <int WPR, int NV, typename R, bool DG>
+cudaError_t bwd_launch(const NormArgs& a, int grid, cudaStream_t st) {
+    const Ring r = ring_of(a);
+    const cudaError_t e = cudaFuncSetAttribute(k_norm_bwd<WPR, NV, R, DG>, cudaFuncAttributeMaxDynamicSharedMemorySize, r.bytes);
+    if (e != cudaSuccess) return e;
+    return launch(k_norm_bwd<WPR, NV, R, DG>, grid, 32 * WPR, r.bytes, st, a, r.stages, r.dres);
 }
 template <int WPR, int NV>
 cudaError_t bwd_rows(const NormArgs& a, int grid, cudaStream_t st) {
-    if (a.res_bf16) {
-        if (a.parts) k_norm_bwd<WPR, NV, __nv_bfloat16, true><<<grid, 32 * WPR, 0, st>>>(a);
-        else k_norm_bwd<WPR, NV, __nv_bfloat16, false><<<grid, 32 * WPR, 0, st>>>(a);
-    } else {
-        if (a.parts) k_norm_bwd<WPR, NV, float, true><<<grid, 32 * WPR, 0, st>>>(a);
-        else k_norm_bwd<WPR, NV, float, false><<<grid, 32 * WPR, 0, st>>>(a);
-    }
-    return cudaGetLastError();
+    if (a.res_bf16) return a.parts ? bwd_launch<WPR, NV, __nv_bfloat16, true>(a, grid, st) : bwd_launch<WPR, NV, __nv_bfloat16, false>(a, grid, st);
+    return a.parts ? bwd_launch<WPR, NV, float, true>(a, grid, st) : bwd_launch<WPR, NV, float, false>(a, grid, st);
 }
 
 int vectors(int H, int wpr) { return (H / 8 + 32 * wpr - 1) / (32 * wpr); }   // of a lane
@@ -358,29 +472,33 @@ cudaError_t launch_norm_fwd(const NormArgs& a, cudaStream_t st) {
     return cudaErrorInvalidValue;
 }
 
-// Blocks of the backward, each with a slice of H floats per model for its share of dgamma.
-int norm_bwd_blocks(long long n_tok) {
-    const long long most = 148 * 4;
-    return static_cast<int>(n_tok < most ? n_tok : most);
+// Warps that share a row of the backward: the fewest with at most two vectors per lane.
+static int bwd_warps(int H) {
+    int wpr = 1;
+    while (vectors(H, wpr) > 2) wpr *= 2;
+    return wpr;
+}
+// Blocks of the backward, each with a slice of H floats per model for its share of dgamma: 16 warps on an SM, and four rows for a
+// block at least where there are enough.
+int norm_bwd_blocks(long long n_tok, int H) {
+    const int wpr = bwd_warps(H), per_sm = wpr >= 16 ? 1 : 16 / wpr;
+    const long long most = 148LL * per_sm, few = n_tok < 148 ? n_tok : n_tok < 4 * 148 ? 148 : (n_tok + 3) / 4;
+    return static_cast<int>(few < most ? few : most);
 }
 
 cudaError_t launch_norm_bwd(const NormArgs& a, int blocks, cudaStream_t st, int* n_launches) {
-    int wpr = 1;
-    while (vectors(a.H, wpr) > 4) wpr *= 2;
+    const int wpr = bwd_warps(a.H);
     cudaError_t e = cudaErrorInvalidValue;
     switch (wpr * 16 + vectors(a.H, wpr)) {
 #undef UNITY_ROWS
 #define UNITY_ROWS(W, N) case (W) * 16 + (N): e = bwd_rows<W, N>(a, blocks, st); break;
-        UNITY_ROWS(1, 1) UNITY_ROWS(1, 2) UNITY_ROWS(1, 3) UNITY_ROWS(1, 4)
-        UNITY_ROWS(2, 3) UNITY_ROWS(2, 4) UNITY_ROWS(4, 3) UNITY_ROWS(4, 4)
-        UNITY_ROWS(8, 3) UNITY_ROWS(8, 4) UNITY_ROWS(16, 3) UNITY_ROWS(16, 4)
+        UNITY_ROWS(1, 1) UNITY_ROWS(1, 2) UNITY_ROWS(2, 2) UNITY_ROWS(4, 2) UNITY_ROWS(8, 2) UNITY_ROWS(16, 2) UNITY_ROWS(32, 2)
     }
 #undef UNITY_ROWS
     *n_launches += 1;
     if (e != cudaSuccess || a.parts == nullptr) return e;
-    k_norm_dgamma<<<dim3((a.H + 127) / 128, a.K), 32 * kDgammaWarps, 0, st>>>(a, blocks);
     *n_launches += 1;
-    return cudaGetLastError();
+    return launch(k_norm_dgamma, dim3(a.H / 32, a.K), 32 * kDgammaWarps, 0, st, a, blocks);
 }
 
 }  // namespace unity

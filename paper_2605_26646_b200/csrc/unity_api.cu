@@ -1806,7 +1806,7 @@ int unity_distill_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_di
 // ------------------------------------------------------------------------------------------------
 size_t unity_rms_norm_workspace_bytes(int64_t n_tok, int32_t H, int32_t K) {
     if (n_tok < 0 || n_tok > 0x7fffff00LL || H < 64 || H > UNITY_MAX_NORM_H || K < 1 || K > UNITY_MAX_MODELS) return 0;
-    return carve_norm(nullptr, ~size_t(0), H, K, norm_bwd_blocks(n_tok), nullptr).bytes;
+    return carve_norm(nullptr, ~size_t(0), H, K, norm_bwd_blocks(n_tok, H), nullptr).bytes;
 }
 
 int unity_rms_norm_fwd(unity_ctx* ctx, const unity_norm_rows* rows, const void* x, const void* residual, int res_type,
@@ -1849,7 +1849,7 @@ int unity_rms_norm_bwd(unity_ctx* ctx, const unity_norm_rows* rows, const void* 
         for (int k = 0; dgamma && !accumulate && k < rows->K; ++k) CUDA_TRY(ctx, cudaMemsetAsync(dgamma[k], 0, sizeof(float) * rows->H, ctx->stream));
         return UNITY_OK;
     }
-    int blocks = norm_bwd_blocks(rows->n_tok);
+    int blocks = norm_bwd_blocks(rows->n_tok, rows->H);
     if (dgamma) {
         bool fits = false;
         NormLayout L;
@@ -1910,6 +1910,7 @@ int unity_clip_grad_norm(unity_ctx* ctx, int32_t n_tensors, const unity_tensor* 
                 chunks += clip_chunks(e[i]);
             }
             if (pass == 1 && l > 0 && !a.write) break;            // (the first launch also writes norm and coef)
+            a.blocks = clip_blocks(chunks);
             CUDA_TRY(ctx, pass == 0 ? launch_grad_squares(a, e, n, chunks, l, ctx->stream) : launch_grad_scale(a, e, n, chunks, l, ctx->stream));
             ctx->launches += 1;
         }
