@@ -35,21 +35,22 @@ constexpr double kSlackFast = 3.3e-6, kSlackExact = 0.0;
 
 struct Tally {                               // of the entries: mass of all, mass and number at or above each threshold
     double whole, m[kTau];
-    float mean, square;                      // sums of e x and e x^2 (octaves)
     int c[kTau];
 };
-constexpr int kTallyWords = 2 + kTau + kTau / 2;
+constexpr int kTallyWords = 1 + kTau + kTau / 2;
 static_assert(sizeof(Tally) == 8 * kTallyWords && kTau % 2 == 0, "sent word by word");
 
 struct Shared {
     uint64_t bar;                            // the row's arrival
     uint64_t mail[2];                        // the messages' arrival, of the even and of the odd exchanges
-    unsigned long long box[2][kMaxCluster * kWarps];   // messages of every block, or of every warp
+    unsigned long long box[2][kMaxCluster * kTallyWords];   // messages of every block
     Tally warp[kWarps];
+    unsigned keys[kThreads];
     float warp_z[kWarps];
     int warp_n[kWarps];
     int scan[kWarps];
     double scan_m[kWarps];
+    float2 moments[kWarps];
     int found;
     double exp2_table[32];
     uint16_t stage[kList];                   // the block's entries for the list, by their place in the block
@@ -133,9 +134,10 @@ __device__ __forceinline__ float value_of(unsigned k) {
 
 // exp((v - top) / T) in fp64 by a table (2^(j/32)) and the exponential series on a 64th of an octave: 2^k 2^(j/32) (1 + p), off
 // by 2^-48; c64 = log2(e) / T.
-__device__ __forceinline__ double slow_weight(float v, float top, double c64, double inv_t, const double* table) {
-    const double d = static_cast<double>(v) - static_cast<double>(top), y = d * c64;    // (octaves; the largest logit's e is 1)
-    if (!(y > -1020.0)) return v == -INFINITY ? 0.0 : exp(d * inv_t);
+__device__ __forceinline__ double slow_weight(float v, float top, double c64, const double* table) {
+    const double d = static_cast<double>(v) - static_cast<double>(top), x = d * c64;    // (octaves; the largest logit's e is 1)
+    // (no branch: neighbours are worked on together.  What lies between 2^-1075 and 2^-1020 is positive, all that is asked of it.)
+    const double y = fmax(x, -1020.0);
     constexpr double kShift = 0x1.8p52 / 32.0, kLn2 = 0.69314718055994531;              // the sum with kShift rounds to 32nds
     const double t = y + kShift, r = y - (t - kShift);
     const int n = __double2loint(t);                             // 32 k + j
@@ -143,12 +145,23 @@ __device__ __forceinline__ double slow_weight(float v, float top, double c64, do
                           r * (kLn2 * kLn2 * kLn2 * kLn2 / 24 + r * (kLn2 * kLn2 * kLn2 * kLn2 * kLn2 / 120)))));
     const double b = table[n & 31];
     const double scaled = __hiloint2double(__double2hiint(b) + ((n >> 5) << 20), __double2loint(b));
-    return fma(scaled, p, scaled);
+    return x < -1075.0 ? 0.0 : fma(scaled, p, scaled);
 }
 
 // m 2^e for e <= 0, 0 far below.
 __device__ __forceinline__ double times_power(double m, int e) {                
     return e < -1000 ? 0.0 : m * __hiloint2double((1023 + e) << 20, 0);
+}
+
+// Lanes hold masses in index order: the first lane whose running mass (behind `before`) is above the target, or, where rounding leaves
+// none, the last with any; its `start`: the mass before it.  -1: no mass at all.
+__device__ __forceinline__ int owner(double mass, double before, double target, int lane, double* start) {
+    const double upto = warp_scan(mass, lane), prior = __shfl_up_sync(kFull, upto, 1);
+    const unsigned some = __ballot_sync(kFull, mass > 0.0), past = some & __ballot_sync(kFull, before + upto > target);
+    if (some == 0) return -1;
+    const int l = past ? __ffs(past) - 1 : 31 - __clz(some);
+    *start = __shfl_sync(kFull, before + (lane ? prior : 0.0), l);
+    return l;
 }
 
 __device__ __forceinline__ void put_row(const SampleArgs& a, int row, int token, double logp, double logp_kept, int n_kept) {
@@ -208,7 +221,7 @@ struct Row {
     // Weight of an entry.  -inf has none.
     __device__ __forceinline__ float octaves(float v) const { return fmaf(v, c, -top_c); }
     __device__ __forceinline__ float fast(float v) const { return ptx::ex2(octaves(v)); }
-    __device__ __forceinline__ double slow(float v) const { return slow_weight(v, top, c64, inv_t, s.exp2_table); }
+    __device__ __forceinline__ double slow(float v) const { return slow_weight(v, top, c64, s.exp2_table); }
     template <bool EXACT>
     __device__ __forceinline__ double weight(float v) const { return EXACT ? slow(v) : static_cast<double>(fast(v)); }
 
@@ -231,8 +244,6 @@ struct Row {
     // Sums over the cluster, the same in every thread.
     __device__ __forceinline__ void add_lanes(Tally& v) const {
         v.whole = warp_sum(v.whole);
-        v.mean = warp_sum(v.mean);
-        v.square = warp_sum(v.square);
 #pragma unroll
         for (int k = 0; k < kTau; ++k) {
             v.m[k] = warp_sum(v.m[k]);
@@ -255,22 +266,20 @@ struct Row {
         }
         const Tally* got = reinterpret_cast<const Tally*>(box(0));
         receive();
-        v = got[0];
-        for (int r = 1; r < ctas; ++r) {
-            v.whole += got[r].whole;
-            v.mean += got[r].mean;
-            v.square += got[r].square;
-#pragma unroll
-            for (int k = 0; k < kTau; ++k) { v.m[k] += got[r].m[k]; v.c[k] += got[r].c[k]; }
-        }
+        if (lane() < ctas) v = got[lane()]; else v = Tally{};
+        add_lanes(v);
         return v;
     }
 
-    // One pass: mass of all entries, masses and numbers of those >= tau[k].  fp32: eight are added pairwise, their sums in two parts.
-    template <bool EXACT, bool TAU, bool MOMENTS>
-    __device__ __forceinline__ Tally weigh(const float (&tau)[kTau]) const {
+    // One pass: mass of all entries, masses and numbers of those >= tau[k].  fp32: two sums side by side (packed arithmetic), each of
+    // four entries added pairwise, those in two parts.
+    // `moments`: sums of e x and e x^2 (octaves).
+    template <bool EXACT, bool TAU, bool MOMENTS = false>
+    __device__ __forceinline__ Tally weigh(const float (&tau)[kTau], float2* moments = nullptr) const {
         Tally v = {};
-        float hi[kTau + 1] = {}, low[kTau + 1] = {};
+        float mean = 0.f, square = 0.f;
+        const uint64_t c2 = ptx::pack2(c, c), top2 = ptx::pack2(-top_c, -top_c), minus = ptx::pack2(-1.f, -1.f);
+        uint64_t hi[kTau + 1] = {}, low[kTau + 1] = {};
         for (int j0 = 0; j0 < per; j0 += 8) {
             float x[8], e[8];
 #pragma unroll
@@ -279,45 +288,65 @@ struct Row {
                 x[q] = two.x;
                 x[q + 1] = two.y;
             }
+            if constexpr (TAU) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
-                if (TAU)
+                for (int q = 0; q < 8; ++q)
 #pragma unroll
                     for (int k = 0; k < kTau; ++k) v.c[k] += x[q] >= tau[k];
-                if (EXACT) {
-                    const double e64 = slow(x[q]);
-                    v.whole += e64;
-                    if (TAU)
+            }
+            if constexpr (EXACT) {
+#pragma unroll
+                for (int h = 0; h < 8; h += 4) {
+                    double w[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) w[q] = slow(x[h + q]);
+                    v.whole += (w[0] + w[1]) + (w[2] + w[3]);
+                    if constexpr (TAU) {
 #pragma unroll
                         for (int k = 0; k < kTau; ++k)
-                            if (x[q] >= tau[k]) v.m[k] += e64;
-                } else {
-                    const float o = octaves(x[q]);
-                    e[q] = ptx::ex2(o);
-                    if (MOMENTS) {
-                        const float eo = e[q] * fmaxf(o, -1e3f);
-                        v.mean += eo;
-                        v.square = fmaf(eo, fmaxf(o, -1e3f), v.square);
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) v.m[k] += x[h + q] >= tau[k] ? w[q] : 0.0;
                     }
                 }
+                continue;
             }
-            if (!EXACT) {
 #pragma unroll
-                for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
-                    float f[8];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) f[q] = k == 0 || x[q] >= tau[k ? k - 1 : 0] ? e[q] : 0.f;
-                    const float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-                    const float next = hi[k] + sum, part = next - hi[k];
-                    low[k] += (hi[k] - (next - part)) + (sum - part);
-                    hi[k] = next;
+            for (int q = 0; q < 8; q += 2) {
+                float a, b;
+                ptx::unpack2(ptx::fma2(ptx::pack2(x[q], x[q + 1]), c2, top2), a, b);
+                e[q] = ptx::ex2(a);
+                e[q + 1] = ptx::ex2(b);
+                if (MOMENTS) {
+                    a = fmaxf(a, -1e3f);
+                    b = fmaxf(b, -1e3f);
+                    mean += e[q] * a + e[q + 1] * b;
+                    square += e[q] * a * a + e[q + 1] * b * b;
                 }
             }
-        }
-        if (!EXACT) {
-            v.whole = static_cast<double>(hi[0]) + static_cast<double>(low[0]);
 #pragma unroll
-            for (int k = 0; k < kTau; ++k) v.m[k] = static_cast<double>(hi[k + 1]) + static_cast<double>(low[k + 1]);
+            for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
+                uint64_t f[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float t = k ? tau[k - 1] : 0.f;
+                    f[q] = ptx::pack2(!k || x[2 * q] >= t ? e[2 * q] : 0.f, !k || x[2 * q + 1] >= t ? e[2 * q + 1] : 0.f);
+                }
+                const uint64_t sum = ptx::add2(ptx::add2(f[0], f[1]), ptx::add2(f[2], f[3])), next = ptx::add2(hi[k], sum);
+                const uint64_t part = ptx::fma2(hi[k], minus, next);                       // next - hi
+                const uint64_t lost = ptx::fma2(ptx::fma2(part, minus, next), minus, hi[k]);   // hi - (next - part)
+                low[k] = ptx::add2(low[k], ptx::add2(lost, ptx::fma2(part, minus, sum)));
+                hi[k] = next;
+            }
+        }
+        if (MOMENTS) *moments = make_float2(mean, square);
+        if (!EXACT) {
+#pragma unroll
+            for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
+                float a, b, d, f;
+                ptx::unpack2(hi[k], a, b);
+                ptx::unpack2(low[k], d, f);
+                (k ? v.m[k ? k - 1 : 0] : v.whole) = (static_cast<double>(a) + static_cast<double>(b)) + (static_cast<double>(d) + static_cast<double>(f));
+            }
         }
         return v;
     }
@@ -325,19 +354,30 @@ struct Row {
     // A logit that about `want` entries or a few more reach: of every block its share of them is counted among its threads' largest
     // entries, and the least such logit is taken (blocks of less than half a share say nothing).  `mine`: the thread's largest.
     __device__ __forceinline__ float reached_by(int want, float mine, int valid, int V) {
-        unsigned least = 0xffffffffu;
-        if (2 * valid * ctas >= V) {
-            const int n = static_cast<int>((static_cast<long long>(valid) * want + V - 1) / V);
-            const unsigned key = mine > -INFINITY ? key_of(mine) : 0u;
-            least = 0;
-            for (int b = 31; b >= 14; --b) {                      // (the lower half of the digits says little)
-                const unsigned next = least | 1u << b;
-                if (__syncthreads_count(key >= next) >= n) least = next;
-            }
-        }
+        s.keys[threadIdx.x] = mine > -INFINITY ? key_of(mine) : 0u;
         __syncthreads();
-        const unsigned long long* got = all_to_all(least);
-        for (int r = 0; r < ctas; ++r) least = min(least, static_cast<unsigned>(got[r]));
+        const unsigned long long* got = box(0);
+        expect(ctas);
+        if (warp() == 0) {
+            unsigned least = 0xffffffffu;
+            if (2 * valid * ctas >= V) {
+                const int n = static_cast<int>((static_cast<long long>(valid) * want + V - 1) / V);
+                unsigned key[kWarps];
+#pragma unroll
+                for (int i = 0; i < kWarps; ++i) key[i] = s.keys[32 * i + lane()];
+                least = 0;
+                for (int b = 31; b >= 14; --b) {                  // (the lower half of the digits says little)
+                    const unsigned next = least | 1u << b;
+                    int above = 0;
+#pragma unroll
+                    for (int i = 0; i < kWarps; ++i) above += key[i] >= next;
+                    if (__reduce_add_sync(kFull, above) >= n) least = next;
+                }
+            }
+            if (lane() < ctas) send(box(rank), mail(), lane(), least);
+        }
+        receive();
+        const unsigned least = __reduce_min_sync(kFull, lane() < ctas ? static_cast<unsigned>(got[lane()]) : 0xffffffffu);
         return least == 0u || least == 0xffffffffu ? -INFINITY : value_of(least);
     }
 
@@ -388,25 +428,21 @@ struct Row {
     // most kList entries or one value are in [lo, hi).  `above`, `below`: first thresholds.  False: a comparison was too close for this
     // arithmetic.  (Every thread of the cluster gets the same result.)
     template <bool EXACT, bool BY_MASS>
-    __device__ __forceinline__ bool enclose(int k_want, double share, float quantile, float above, float below, double* target, double* bound) {
+    __device__ __forceinline__ bool enclose(int k_want, double share, float above, float below, double* target, double* bound) {
         const double slack = EXACT ? kSlackExact : kSlackFast;
         const float octave = 0.69314718f / static_cast<float>(inv_t);
         float tau[kTau] = {above, below};
         double m_lo = 0.0;
-        float centre = 0.f, width = 0.f;
         lo = kLowest;
         for (int round = 0;; ++round) {
             if (round > 0) {
-                // between lo and hi: around the normal distribution's quantile, around the linear estimate, evenly; and evenly as
-                // order-preserving integers where all that took long or the interval is far longer than the distribution
+                // between lo and hi: around the linear estimate, evenly; and evenly as order-preserving integers where all that took long
+                // or the interval is far longer than the distribution
                 const bool near = round < 10 && hi - lo < 256.f * octave;
                 float at = 0.5f * (lo + hi), wide = (hi - lo) * (1.f / 6);
-                if (BY_MASS && round == 1 && centre - width < hi && centre + width > lo) {
-                    at = centre;
-                    wide = width;
-                } else if (BY_MASS && round < 5) {
+                if (BY_MASS && round < 5) {
                     at = hi - (hi - lo) * static_cast<float>((*target - m_hi) / (m_lo - m_hi));
-                    wide = (hi - lo) * (round == 2 ? 0.1f : 0.04f);
+                    wide = (hi - lo) * (round == 1 ? 0.1f : 0.04f);
                 } else if (!BY_MASS && round < 5) {
                     at = hi - (hi - lo) * (static_cast<float>(k_want - n_hi) / static_cast<float>(n_lo - n_hi));
                     wide = (hi - lo) * 0.1f;
@@ -415,11 +451,11 @@ struct Row {
 #pragma unroll
                 for (int k = 0; k < kTau; ++k) {
                     const unsigned key = a + static_cast<unsigned>(static_cast<unsigned long long>(b - a) * (kTau - k) / (kTau + 1));
-                    tau[k] = near || (BY_MASS && round == 1 && wide == width) ? (k == 0 ? at + wide : at - wide) : value_of(key);
+                    tau[k] = near ? (k == 0 ? at + wide : at - wide) : value_of(key);
                     if (!(tau[k] > lo && tau[k] < hi)) tau[k] = value_of(a + (b - a) / 2);
                 }
             }
-            const Tally mine = !EXACT && BY_MASS && round == 0 ? weigh<EXACT, true, true>(tau) : weigh<EXACT, true, false>(tau);
+            const Tally mine = weigh<EXACT, true>(tau);
             const Tally v = exchange(mine);
             if (round == 0) {
                 whole = v.whole;
@@ -430,10 +466,6 @@ struct Row {
                 m_hi = my_m = 0.0;
                 *target = share * v.whole;
                 *bound = slack * v.whole;
-                const float mean = v.mean / static_cast<float>(v.whole);
-                const float sd = sqrtf(fmaxf(v.square / static_cast<float>(v.whole) - mean * mean, 0.f));
-                centre = top + octave * (mean - sd * quantile);
-                width = octave * (0.25f + 0.1f * sd);
             }
             bool moved = false;
 #pragma unroll
@@ -592,49 +624,19 @@ struct Row {
             if (cut.keeps(x, first + j)) mine += weight<EXACT>(x);
         });
         const double run = warp_scan(mine, lane());               // inclusive over the warp's lanes
-        const double sum = __shfl_sync(kFull, run, 31);
-        expect(ctas * kWarps);
-        if (lane() < ctas) send(box(rank * kWarps + warp()), mail(), lane(), static_cast<unsigned long long>(__double_as_longlong(sum)));
-        const unsigned long long* region = box(0);
-        receive();
-        // Every warp looks for the warp whose range of running masses holds the target: the first that ends above it (u < 1, but
-        // rounding may leave none: then the last with any mass).  A lane has four neighbouring warps.
-        constexpr int kEach = kMaxCluster * kWarps / 32;
-        double part[kEach], four = 0.0;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int w = lane() * kEach + i;
-            part[i] = w < ctas * kWarps ? __longlong_as_double(static_cast<long long>(region[w])) : 0.0;
-            four += part[i];
-        }
-        const double upto = warp_scan(four, lane()), kept = __shfl_sync(kFull, upto, 31), prior = __shfl_up_sync(kFull, upto, 1);
+        if (lane() == 31) s.scan_m[warp()] = run;
+        __syncthreads();
+        const double of_warp = lane() < kWarps ? s.scan_m[lane()] : 0.0, of_block = warp_sum(of_warp);
+        const unsigned long long* got = all_to_all(static_cast<unsigned long long>(__double_as_longlong(of_block)));
+        const double block = lane() < ctas ? __longlong_as_double(static_cast<long long>(got[lane()])) : 0.0, kept = warp_sum(block);
         const double target = static_cast<double>(u) * kept, bound = EXACT ? kSlackExact : kSlackFast * kept;
-        double from = lane() ? prior : 0.0, start = 0.0, last_start = 0.0;
-        int hit = -1, last = -1;
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const double to = from + part[i];
-            if (part[i] > 0.0) {
-                last = lane() * kEach + i;
-                last_start = from;
-                if (hit < 0 && to > target) { hit = last; start = from; }
-            }
-            from = to;
-        }
-        const unsigned hits = __ballot_sync(kFull, hit >= 0), lasts = __ballot_sync(kFull, last >= 0);
-        const int owner = hits ? __ffs(hits) - 1 : 31 - __clz(lasts);
-        const int home = __shfl_sync(kFull, hits ? hit : last, owner);
-        start = __shfl_sync(kFull, hits ? start : last_start, owner);
         bool close = false;
         int token = -1;
         float tz = 0.f;
-        if (home == rank * kWarps + warp()) {
-            // in the warp the first lane whose running mass is above the target, of those with any
-            const unsigned some = __ballot_sync(kFull, mine > 0.0), past = some & __ballot_sync(kFull, start + run > target);
-            const int holder = past ? __ffs(past) - 1 : 31 - __clz(some);
-            const double prev = __shfl_sync(kFull, run, holder ? holder - 1 : 0);
-            double at0 = start + (holder ? prev : 0.0);
-            close = fabs(at0 - target) <= bound;
+        double start = 0.0;
+        if (owner(block, 0.0, target, lane(), &start) == rank && owner(of_warp, start, target, lane(), &start) == warp()) {
+            const int holder = owner(mine, start, target, lane(), &start);
+            close = fabs(start - target) <= bound;
             // its entries, 32 at a time
             const T* row_z = z + (holder - lane()) * per;
             const int base = first + (holder - lane()) * per;
@@ -646,7 +648,7 @@ struct Row {
                     x = one(row_z + j);
                     if (x >= hi || (x >= lo && cut.keeps(x, base + j))) e = weight<EXACT>(x);
                 }
-                const double at = at0 + warp_scan(e, lane());
+                const double at = start + warp_scan(e, lane());
                 const unsigned any = __ballot_sync(kFull, e > 0.0), above = any & __ballot_sync(kFull, at > target);
                 close |= __any_sync(kFull, e > 0.0 && fabs(at - target) <= bound);
                 const int l = above ? __ffs(above) - 1 : any ? 31 - __clz(any) : -1;
@@ -655,15 +657,13 @@ struct Row {
                     tz = __shfl_sync(kFull, x, l);
                 }
                 if (above) break;
-                at0 = __shfl_sync(kFull, at, 31);
+                start = __shfl_sync(kFull, at, 31);
             }
         }
         if (!EXACT) {
             // (the block that holds the target decides for the cluster)
-            const unsigned long long* got = all_to_all(__syncthreads_or(close) != 0);
-            int sum_close = 0;
-            for (int r = 0; r < ctas; ++r) sum_close += static_cast<int>(got[r]);
-            if (sum_close > 0) return false;
+            got = all_to_all(__syncthreads_or(close) != 0);
+            if (__any_sync(kFull, lane() < ctas && got[lane() < ctas ? lane() : 0] != 0)) return false;
         }
         if (token >= 0 && lane() == 0) {
             const double x = (static_cast<double>(tz) - static_cast<double>(top)) * inv_t;
@@ -687,7 +687,7 @@ struct Row {
 
     // floor: entries below it are not allowed (min-p).
     template <bool EXACT>
-    __device__ __forceinline__ bool draw(const SampleArgs& a, int row, const SampleRule& rule, float floor, float my_top, int valid, float u) {
+    __device__ __forceinline__ bool draw(const SampleArgs& a, int row, const SampleRule& rule, float floor, float my_top, int valid, float u, float centre, float width, bool spread) {
         const bool search = rule.top_k > 0 || rule.top_p < 1.0;
         Cut cut{kLowest, 0x7fffffff};                             // (every entry in [lo, hi))
         int n_kept = n_all;
@@ -695,7 +695,7 @@ struct Row {
         if (floor > -INFINITY) {
             // mass of all entries, and of those >= floor
             const float at[kTau] = {floor, INFINITY};
-            const Tally mine = weigh<EXACT, true, false>(at), v = exchange(mine);
+            const Tally mine = weigh<EXACT, true>(at), v = exchange(mine);
             whole = v.whole;
             lo = hi = floor;
             marks[0] = marks[1] = 0;
@@ -706,17 +706,19 @@ struct Row {
             whole = v.m[0];
             reduce_to(n_kept, [&](float x, int) { return x >= floor; });
         }
-        if (EXACT && all < 0.0) {
+        if (EXACT && all < 0.0 && !(list_lo < list_hi && list_hi <= top)) {       // (else with the thresholds' pass)
             const float none[kTau] = {INFINITY, INFINITY};
-            whole = exchange(weigh<true, false, false>(none)).whole;
+            whole = exchange(weigh<true, false>(none)).whole;
         }
-        if (all < 0.0) all = whole;
-        // What is kept is mostly among the first few hundred: those are sorted, and if they hold the end everything is decided there
+        const bool first_mass = all < 0.0;
+        if (first_mass) all = whole;
+        // What is kept is mostly among the first few hundred: those are sorted, and if they hold the end everything is decided there.
+        // (Not where the distribution's entropy says that it is spread over many more.)
         const bool again = EXACT && list_lo < list_hi;            // the interval that the fp32 pass has found
         double target = rule.top_p * whole, bound = (EXACT ? kSlackExact : kSlackFast) * whole;
         float below = -INFINITY;
         bool done = false;
-        if (rule.top_k <= kList / 4 * 3) {
+        if (rule.top_k <= kList / 4 * 3 && (rule.top_k > 0 || again || !spread)) {
             hi = nextafterf(top, INFINITY);
             n_hi = 0;
             m_hi = my_m = 0.0;
@@ -740,19 +742,19 @@ struct Row {
             }
         }
         if (!done && rule.top_k > 0) {
-            if (!enclose<EXACT, false>(rule.top_k, 0.0, 0.f, again ? list_hi : INFINITY, again ? list_lo : below, &target, &bound)) return false;
+            if (!enclose<EXACT, false>(rule.top_k, 0.0, again ? list_hi : INFINITY, again ? list_lo : below, &target, &bound)) return false;
             if (n_lo - n_hi <= kList) {
                 sort_list();
                 cut_list<EXACT, false>(rule.top_k, 0.0, 0.0, 0.0, &cut, &n_kept);
             } else {
                 cut_ties<EXACT, false>(rule.top_k, 0.0, 0.0, &cut, &n_kept);
             }
+            if (EXACT && first_mass) all = whole;
             if (rule.top_p < 1.0) reduce_to(n_kept, [&](float x, int i) { return x >= hi || (x >= lo && cut.keeps(x, i)); });
         }
         if (!done && rule.top_p < 1.0) {
-            const float octave = 0.69314718f / static_cast<float>(inv_t);
-            const float above = again ? list_hi : top - 2.f * octave;
-            if (!enclose<EXACT, true>(0, rule.top_p, rule.quantile, above, again ? list_lo : top - 10.f * octave, &target, &bound)) return false;
+            if (!enclose<EXACT, true>(0, rule.top_p, again ? list_hi : centre + width, again ? list_lo : centre - width, &target, &bound)) return false;
+            if (EXACT && first_mass && rule.top_k == 0) all = whole;
             if (n_lo - n_hi <= kList) {
                 sort_list();
                 if (cut_list<EXACT, true>(0x7fffffff, 0.0, target, EXACT ? -1.0 : bound, &cut, &n_kept) != kDone) return false;
@@ -824,46 +826,73 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     // the mass, in units of a power of two next to the thread's largest entry
     int unit = my_top > -INFINITY && my_top < INFINITY ? static_cast<int>(ceilf(fminf(fmaxf(my_top * r.c, -1e9f), 1e9f))) : -1000000000;
     double mass = 0.0;
+    float mean = 0.f, square = 0.f;
     if (rule.log_min_p == -INFINITY) {
         const float none[kTau] = {INFINITY, INFINITY};
         r.top_c = static_cast<float>(unit);
-        mass = r.template weigh<false, false, false>(none).whole;
-        const int most = __reduce_max_sync(kFull, unit);
-        mass = warp_sum(times_power(mass, unit - most));
-        unit = most;
+        float2 about = make_float2(0.f, 0.f);
+        mass = rule.top_p < 1.0 ? r.template weigh<false, false, true>(none, &about).whole : r.template weigh<false, false>(none).whole;
+        // (of the octaves themselves, no longer counted from the unit)
+        const float f = static_cast<float>(unit), w = static_cast<float>(mass);
+        mean = about.x + f * w;
+        square = about.y + f * (2.f * about.x + f * w);
     }
+    // Sums of masses in different units over the lanes of a warp.
+    auto add_units = [&]() {
+        const int most = __reduce_max_sync(kFull, unit), below = unit - most;
+        const float scale = below < -100 ? 0.f : ptx::ex2(static_cast<float>(below));
+        mass = warp_sum(times_power(mass, below));
+        mean = warp_sum(scale * mean);
+        square = warp_sum(scale * square);
+        unit = most;
+    };
+    add_units();
     float top = my_top;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
     finite = __reduce_add_sync(kFull, finite);
-    if (lane == 0) { s.warp_z[warp] = top; s.warp_n[warp] = finite; s.scan_m[warp] = mass; s.scan[warp] = unit; }
-    __syncthreads();
-    top = s.warp_z[0];
-    finite = s.warp_n[0];
-    unit = s.scan[0];
-    for (int w = 1; w < kWarps; ++w) { top = max_nan(top, s.warp_z[w]); finite += s.warp_n[w]; unit = max(unit, s.scan[w]); }
-    mass = 0.0;
-    for (int w = 0; w < kWarps; ++w) mass += times_power(s.scan_m[w], s.scan[w] - unit);
+    if (lane == 0) { s.warp_z[warp] = top; s.warp_n[warp] = finite; s.scan_m[warp] = mass; s.scan[warp] = unit; s.moments[warp] = make_float2(mean, square); }
     __syncthreads();
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");     // before the first message
-    r.expect(3 * ctas);
-    if (threadIdx.x < ctas) {
-        send(r.box(3 * rank), r.mail(), threadIdx.x, static_cast<unsigned long long>(__float_as_uint(top)) << 32 | static_cast<unsigned>(finite));
-        send(r.box(3 * rank + 1), r.mail(), threadIdx.x, static_cast<unsigned long long>(__double_as_longlong(mass)));
-        send(r.box(3 * rank + 2), r.mail(), threadIdx.x, static_cast<unsigned>(unit));
+    r.expect(4 * ctas);
+    if (warp == 0) {
+        const bool on = lane < kWarps;
+        top = on ? s.warp_z[lane] : -INFINITY;
+        finite = on ? s.warp_n[lane] : 0;
+        mass = on ? s.scan_m[lane] : 0.0;
+        unit = on ? s.scan[lane] : -1000000000;
+        mean = on ? s.moments[lane].x : 0.f;
+        square = on ? s.moments[lane].y : 0.f;
+        add_units();
+#pragma unroll
+        for (int o = kWarps / 2; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
+        top = __shfl_sync(kFull, top, 0);
+        finite = __reduce_add_sync(kFull, finite);
+        if (lane < ctas) {
+            send(r.box(4 * rank), r.mail(), lane, static_cast<unsigned long long>(__float_as_uint(top)) << 32 | static_cast<unsigned>(finite));
+            send(r.box(4 * rank + 1), r.mail(), lane, static_cast<unsigned long long>(__double_as_longlong(mass)));
+            send(r.box(4 * rank + 2), r.mail(), lane, static_cast<unsigned>(unit));
+            send(r.box(4 * rank + 3), r.mail(), lane, static_cast<unsigned long long>(__float_as_uint(mean)) << 32 | __float_as_uint(square));
+        }
     }
     const unsigned long long* got = r.box(0);
     r.receive();
-    r.n_all = 0;
-    for (int q = 0; q < ctas; ++q) {
-        top = max_nan(top, __uint_as_float(static_cast<unsigned>(got[3 * q] >> 32)));
-        r.n_all += static_cast<int>(got[3 * q] & 0xffffffffu);
-        unit = max(unit, static_cast<int>(got[3 * q + 2]));
+    {
+        const bool on = lane < ctas;
+        const unsigned long long* mine = got + 4 * (on ? lane : 0);
+        top = on ? __uint_as_float(static_cast<unsigned>(mine[0] >> 32)) : -INFINITY;
+        finite = on ? static_cast<int>(mine[0] & 0xffffffffu) : 0;
+        mass = on ? __longlong_as_double(static_cast<long long>(mine[1])) : 0.0;
+        unit = on ? static_cast<int>(mine[2]) : -1000000000;
+        mean = on ? __uint_as_float(static_cast<unsigned>(mine[3] >> 32)) : 0.f;
+        square = on ? __uint_as_float(static_cast<unsigned>(mine[3])) : 0.f;
+        add_units();
+#pragma unroll
+        for (int o = kMaxCluster / 2; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
+        top = __shfl_sync(kFull, top, 0);
+        r.n_all = __reduce_add_sync(kFull, finite);
     }
-    mass = 0.0;
-    for (int q = 0; q < ctas; ++q)
-        mass += times_power(__longlong_as_double(static_cast<long long>(got[3 * q + 1])), static_cast<int>(got[3 * q + 2]) - unit);
     if (!(top > -INFINITY && top < INFINITY)) {                   // NaN, +inf or nothing but -inf
         if (rank == 0 && threadIdx.x == 0) no_distribution(a, row);
         return;
@@ -871,6 +900,12 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     r.top = top;
     r.top_c = top * r.c;
     r.whole = mass * exp2(static_cast<double>(unit) - static_cast<double>(r.top_c));
+    // Where top-p ends in a normal distribution of the same mean and variance, and whether the entropy, log2 of the mass less the mean
+    // in octaves below the largest, is that of more than some four hundred entries.  (Guesses.)
+    mean /= static_cast<float>(mass);
+    const float sd = sqrtf(fmaxf(square / static_cast<float>(mass) - mean * mean, 0.f));
+    const float centre = (mean - sd * rule.quantile) / r.c, width = (0.25f + 0.1f * sd) / r.c;
+    const bool spread = log2f(static_cast<float>(mass)) + static_cast<float>(unit) - mean > 8.6f;
     r.list_lo = r.list_hi = 0.f;
     r.cut_down = false;
     const int n_all = r.n_all;
@@ -885,7 +920,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     }
     // (fp32 weights have 2^(rounding of top_c) in common, which has to stay near 1)
     const bool fits = fabsf(r.top_c) <= 0x1p20f;
-    if (fits && r.template draw<false>(a, row, rule, floor, my_top, n, u)) return;
+    if (fits && r.template draw<false>(a, row, rule, floor, my_top, n, u, centre, width, spread)) return;
+    // the row in 64 bits
     __syncthreads();
     if (threadIdx.x < 32) s.exp2_table[threadIdx.x] = exp2(threadIdx.x / 32.0);
     if (r.cut_down) {
@@ -896,7 +932,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
         r.n_all = n_all;
     }
     __syncthreads();
-    r.template draw<true>(a, row, rule, floor, my_top, n, u);
+    r.template draw<true>(a, row, rule, floor, my_top, n, u, centre, width, spread);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -995,7 +1031,7 @@ struct Stream {
 
     template <bool EXACT>
     __device__ __forceinline__ double weight(float v, int r) const {
-        return EXACT ? slow_weight(v, top, c64, inv_t, s.exp2_table) : static_cast<double>(ptx::ex2(fmaf(v, c, -static_cast<float>(r))));
+        return EXACT ? slow_weight(v, top, c64, s.exp2_table) : static_cast<double>(ptx::ex2(fmaf(v, c, -static_cast<float>(r))));
     }
     // Unit of a lane's mass: the power of two at or above its largest entry (any, if it has none).
     __device__ __forceinline__ float unit_of(float most) const {
@@ -1007,18 +1043,6 @@ struct Stream {
         if (EXACT) return s.lane_x[k][t];
         const float2 m = s.lane_m[k][t];
         return times_power(static_cast<double>(m.x), static_cast<int>(m.y) - unit);
-    }
-
-    // Among lanes [0, n), which hold masses in index order: the first whose running mass is above the target, or the last with any; its
-    // `start`: the mass before it.  -1: no mass at all.
-    __device__ __forceinline__ int owner(double mass, double before_all, double target, double* start) const {
-        const double upto = warp_scan(mass, lane()), prior = __shfl_up_sync(kFull, upto, 1);
-        const double from = before_all + (lane() ? prior : 0.0);
-        const unsigned some = __ballot_sync(kFull, mass > 0.0), past = some & __ballot_sync(kFull, before_all + upto > target);
-        if (some == 0) return -1;
-        const int l = past ? __ffs(past) - 1 : 31 - __clz(some);
-        *start = __shfl_sync(kFull, from, l);
-        return l;
     }
 
     // One warp: the cluster's masses, and, in the block that holds the target, the token.  whole: in units of 2^unit; close: a
@@ -1082,8 +1106,8 @@ struct Stream {
         f.whole = warp_sum(mass);
         const double target = static_cast<double>(u) * f.whole, bound = EXACT ? kSlackExact : kSlackFast * f.whole;
         double start = 0.0;
-        if (owner(mass, 0.0, target, &start) != rank) return f;
-        const int home = owner(times_power(m, block_r - f.unit), start, target, &start);
+        if (owner(mass, 0.0, target, lane(), &start) != rank) return f;
+        const int home = owner(times_power(m, block_r - f.unit), start, target, lane(), &start);
         int tile = 0;
         double at0 = start;
         for (int k = 0; k < tiles(home); ++k) {
@@ -1316,14 +1340,16 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool 
         *n_launches += 1;
     }
     if (any_search) {
-        // the fewest blocks per row (1 .. 16) whose share takes at most 40 KB, so that four blocks fit an SM
+        // the fewest blocks per row (1 .. 16) whose share takes at most 40 KB, so that four blocks fit an SM; more while the rows leave some
+        // without one
         const int width = bf16 ? 2 : 4;
         int ctas = 1, per = 0;
         for (;; ctas *= 2) {
             per = (a.V + kThreads * ctas - 1) / (kThreads * ctas);
             // entries are read in pairs, and the threads' first ones lie an odd number of pairs apart: at different banks
             per = ((per + 1) / 2 | 1) * 2;
-            if (ctas == kMaxCluster || static_cast<long long>(per) * kThreads * width <= 40 * 1024) break;
+            if (ctas == kMaxCluster) break;
+            if (static_cast<long long>(per) * kThreads * width <= 40 * 1024 && (per <= 16 || static_cast<long long>(a.n_rows) * ctas >= 4 * sm_count)) break;
         }
         const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, ctas, per * kThreads * width, st, a, per, ctas);
         if (e != cudaSuccess) return e;
