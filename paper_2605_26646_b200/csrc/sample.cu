@@ -231,7 +231,12 @@ struct Row {
     __device__ __forceinline__ void expect(int words) const {
         if (threadIdx.x == 0) ptx::mbar_arrive_expect_tx(mail(), 8 * words);
     }
-    __device__ __forceinline__ void receive() { wait_mail(mail(), turn >> 1 & 1, status); ++turn; }
+    // (One warp looks for the messages, the others wait at the block's barrier: looking takes issue slots.)
+    __device__ __forceinline__ void receive() {
+        if (warp() == 0) wait_mail(mail(), turn >> 1 & 1, status);
+        __syncthreads();
+        ++turn;
+    }
     // A word of every block to every block; returns the other side's place of it.  (Behind a barrier of the block.)
     __device__ __forceinline__ const unsigned long long* all_to_all(unsigned long long v) {
         const unsigned long long* got = box(0);
@@ -308,34 +313,34 @@ struct Row {
                             for (int q = 0; q < 4; ++q) v.m[k] += x[h + q] >= tau[k] ? w[q] : 0.0;
                     }
                 }
-                continue;
-            }
+            } else {
 #pragma unroll
-            for (int q = 0; q < 8; q += 2) {
-                float a, b;
-                ptx::unpack2(ptx::fma2(ptx::pack2(x[q], x[q + 1]), c2, top2), a, b);
-                e[q] = ptx::ex2(a);
-                e[q + 1] = ptx::ex2(b);
-                if (MOMENTS) {
-                    a = fmaxf(a, -1e3f);
-                    b = fmaxf(b, -1e3f);
-                    mean += e[q] * a + e[q + 1] * b;
-                    square += e[q] * a * a + e[q + 1] * b * b;
+                for (int q = 0; q < 8; q += 2) {
+                    float a, b;
+                    ptx::unpack2(ptx::fma2(ptx::pack2(x[q], x[q + 1]), c2, top2), a, b);
+                    e[q] = ptx::ex2(a);
+                    e[q + 1] = ptx::ex2(b);
+                    if (MOMENTS) {
+                        a = fmaxf(a, -1e3f);
+                        b = fmaxf(b, -1e3f);
+                        mean += e[q] * a + e[q + 1] * b;
+                        square += e[q] * a * a + e[q + 1] * b * b;
+                    }
                 }
-            }
 #pragma unroll
-            for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
-                uint64_t f[4];
+                for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
+                    uint64_t f[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float t = k ? tau[k - 1] : 0.f;
-                    f[q] = ptx::pack2(!k || x[2 * q] >= t ? e[2 * q] : 0.f, !k || x[2 * q + 1] >= t ? e[2 * q + 1] : 0.f);
+                    for (int q = 0; q < 4; ++q) {
+                        const float t = k ? tau[k - 1] : 0.f;
+                        f[q] = ptx::pack2(!k || x[2 * q] >= t ? e[2 * q] : 0.f, !k || x[2 * q + 1] >= t ? e[2 * q + 1] : 0.f);
+                    }
+                    const uint64_t sum = ptx::add2(ptx::add2(f[0], f[1]), ptx::add2(f[2], f[3])), next = ptx::add2(hi[k], sum);
+                    const uint64_t part = ptx::fma2(hi[k], minus, next);                       // next - hi
+                    const uint64_t lost = ptx::fma2(ptx::fma2(part, minus, next), minus, hi[k]);   // hi - (next - part)
+                    low[k] = ptx::add2(low[k], ptx::add2(lost, ptx::fma2(part, minus, sum)));
+                    hi[k] = next;
                 }
-                const uint64_t sum = ptx::add2(ptx::add2(f[0], f[1]), ptx::add2(f[2], f[3])), next = ptx::add2(hi[k], sum);
-                const uint64_t part = ptx::fma2(hi[k], minus, next);                       // next - hi
-                const uint64_t lost = ptx::fma2(ptx::fma2(part, minus, next), minus, hi[k]);   // hi - (next - part)
-                low[k] = ptx::add2(low[k], ptx::add2(lost, ptx::fma2(part, minus, sum)));
-                hi[k] = next;
             }
         }
         if (MOMENTS) *moments = make_float2(mean, square);
@@ -784,8 +789,8 @@ __device__ __forceinline__ void fetch(Shared& s, T* z, const T* src, int n, int 
         z[whole + threadIdx.x] = src[whole + threadIdx.x];       // at most seven
     }
     for (int i = n + threadIdx.x; i < share; i += kThreads) z[i] = static_cast<T>(-INFINITY);
+    if (threadIdx.x < 32 && whole > 0 && !ptx::mbar_wait(&s.bar, 0, kWaitBudgetCycles)) atomicOr(a.status, kStatusTimeout);
     __syncthreads();
-    if (whole > 0 && !ptx::mbar_wait(&s.bar, 0, kWaitBudgetCycles)) atomicOr(a.status, kStatusTimeout);
 }
 
 template <typename T>
