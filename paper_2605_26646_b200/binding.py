@@ -569,13 +569,13 @@ _PTRS = [C.c_void_p * k for k in range(UNITY_MAX_MODELS + 1)]      # (making an 
 _INTS = [C.c_int32 * k for k in range(UNITY_MAX_ROLES + 1)]
 
 
-def _fit(t: Optional[torch.Tensor], shape, dtype, base, name) -> Optional[int]:
-    """_sized against the tensor `base`, with the fewest calls where all is well: these calls take microseconds themselves."""
+def _fit(t: Optional[torch.Tensor], shape, dtype, device: int, name) -> Optional[int]:
+    """_sized on a CUDA device, with the fewest calls where all is well: these calls take microseconds themselves."""
     if t is None:
         return None
-    if t.shape == shape and t.dtype is dtype and t.get_device() == base.get_device() and t.is_contiguous():
+    if t.shape == shape and t.dtype is dtype and t.get_device() == device and t.is_contiguous():
         return t.data_ptr()
-    return _sized(t, shape, dtype, base.device, name)
+    return _sized(t, shape, dtype, torch.device("cuda", device), name)
 
 
 def _type_of(t: torch.Tensor, name) -> int:
@@ -588,30 +588,31 @@ def _type_of(t: torch.Tensor, name) -> int:
 def _norm_rows(x, shape, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps):
     if len(shape) != 2 or not gamma or inv_role.dim() != 1:
         raise ValueError("token rows must be [n_tok, H], gamma a non-empty sequence of [H] and inv_role [n_inv]")
-    if not x.is_cuda:
+    dev = x.get_device()
+    if dev < 0:
         raise ValueError("token rows must be a CUDA tensor")
     K, R = len(gamma), len(role_model)
     n_tok, H = shape
     per_model, kind, n_inv = (H,), gamma[0].dtype, inv_role.shape[0]
     if K > UNITY_MAX_MODELS or R > UNITY_MAX_ROLES:
         raise ValueError(f"at most {UNITY_MAX_MODELS} models and {UNITY_MAX_ROLES} roles")
-    return unity_norm_rows(n_tok, H, K, n_inv, R, _fit(cu_seqlens, (n_inv + 1,), torch.int64, x, "cu_seqlens"),
-                           _fit(inv_role, (n_inv,), torch.int32, x, "inv_role"), _INTS[R](*role_model),
-                           _fit(tok_mask, (n_tok,), torch.uint8, x, "tok_mask"),
-                           _PTRS[K](*[_fit(g, per_model, kind, x, "gamma") for g in gamma]), _type_of(gamma[0], "gamma"), eps)
+    return unity_norm_rows(n_tok, H, K, n_inv, R, _fit(cu_seqlens, (n_inv + 1,), torch.int64, dev, "cu_seqlens"),
+                           _fit(inv_role, (n_inv,), torch.int32, dev, "inv_role"), _INTS[R](*role_model),
+                           _fit(tok_mask, (n_tok,), torch.uint8, dev, "tok_mask"),
+                           _PTRS[K](*[_fit(g, per_model, kind, dev, "gamma") for g in gamma]), _type_of(gamma[0], "gamma"), eps)
 
 
 def unity_rms_norm_fwd(ctx, x, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps: float, y, residual=None,
                        res_out=None) -> None:
     """x, y: bf16 [n_tok, H]; gamma: K tensors [H], all f32 or all bf16; residual, res_out: f32 or bf16 [n_tok, H]."""
-    shape, b16 = x.shape, torch.bfloat16
+    shape, b16, dev = x.shape, torch.bfloat16, x.get_device()
     rows = _norm_rows(x, shape, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
     rtype, kind = (UNITY_BF16, b16) if residual is None else (_type_of(residual, "residual"), residual.dtype)
     if y is None:
         raise ValueError("y is None")
     code = load_library().unity_rms_norm_fwd(
-        ctx, rows, _fit(x, shape, b16, x, "x"), _fit(residual, shape, kind, x, "residual"), rtype, _fit(y, shape, b16, x, "y"),
-        _fit(res_out, shape, kind, x, "res_out"))
+        ctx, rows, _fit(x, shape, b16, dev, "x"), _fit(residual, shape, kind, dev, "residual"), rtype,
+        _fit(y, shape, b16, dev, "y"), _fit(res_out, shape, kind, dev, "res_out"))
     if code:
         _raise(ctx, code)
 
@@ -619,7 +620,7 @@ def unity_rms_norm_fwd(ctx, x, gamma, cu_seqlens, inv_role, role_model, tok_mask
 def unity_rms_norm_bwd(ctx, res, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps: float, dy, dx, dres=None,
                        dgamma=None, accumulate_dgamma: bool = False) -> None:
     """res, dres, dx: all f32 or all bf16 [n_tok, H]; dy: bf16; dgamma: K f32 tensors [H], or None for a frozen norm."""
-    shape, kind = res.shape, res.dtype
+    shape, kind, dev = res.shape, res.dtype, res.get_device()
     rows = _norm_rows(res, shape, gamma, cu_seqlens, inv_role, role_model, tok_mask, eps)
     if dy is None or dx is None:
         raise ValueError("dy / dx is None")
@@ -627,10 +628,10 @@ def unity_rms_norm_bwd(ctx, res, gamma, cu_seqlens, inv_role, role_model, tok_ma
     if dgamma is not None:
         if len(dgamma) != len(gamma):
             raise ValueError(f"dgamma: expected {len(gamma)} tensors, got {len(dgamma)}")
-        dg = _PTRS[len(dgamma)](*[_fit(g, shape[1:], torch.float32, res, "dgamma") for g in dgamma])
+        dg = _PTRS[len(dgamma)](*[_fit(g, shape[1:], torch.float32, dev, "dgamma") for g in dgamma])
     code = load_library().unity_rms_norm_bwd(
-        ctx, rows, _fit(res, shape, kind, res, "res"), _type_of(res, "res"), _fit(dy, shape, torch.bfloat16, res, "dy"),
-        _fit(dres, shape, kind, res, "dres"), _fit(dx, shape, kind, res, "dx"), dg, 1 if accumulate_dgamma else 0)
+        ctx, rows, _fit(res, shape, kind, dev, "res"), _type_of(res, "res"), _fit(dy, shape, torch.bfloat16, dev, "dy"),
+        _fit(dres, shape, kind, dev, "dres"), _fit(dx, shape, kind, dev, "dx"), dg, 1 if accumulate_dgamma else 0)
     if code:
         _raise(ctx, code)
 
@@ -667,12 +668,12 @@ def unity_clip_grad_norm(ctx, tensors: GradTensors, max_norm: Optional[Sequence[
     if max_norm is not None and len(max_norm) != K:
         raise ValueError(f"max_norm: expected {K} values, got {len(max_norm)}")
     bounds = None if max_norm is None else (C.c_float * K)(*max_norm)
-    base = tensors.grads[0] if tensors.grads else norm
-    if not norm.is_cuda:
-        raise ValueError("norm must be a CUDA tensor")
+    dev = norm.get_device()
+    if dev < 0 or (tensors.grads and tensors.grads[0].get_device() != dev):
+        raise ValueError("norm must be a CUDA tensor on the gradients' device")
     code = load_library().unity_clip_grad_norm(ctx, len(tensors.grads), tensors.array, K, bounds,
-                                               _fit(norm, (K,), torch.float32, base, "norm"),
-                                               _fit(coef, (K,), torch.float32, base, "coef"))
+                                               _fit(norm, (K,), torch.float32, dev, "norm"),
+                                               _fit(coef, (K,), torch.float32, dev, "coef"))
     if code:
         _raise(ctx, code)
 
@@ -682,7 +683,8 @@ def unity_sample(ctx, logits, rules, u, token, row_role=None, row_mask=None, log
     shape = logits.shape
     if len(shape) != 2 or (shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be [n_rows, V] with consecutive entries in a row")
-    if not logits.is_cuda:
+    dev = logits.get_device()
+    if dev < 0:
         raise ValueError("logits must be a CUDA tensor")
     if u is None or token is None:
         raise ValueError("u / token is None")
@@ -691,9 +693,9 @@ def unity_sample(ctx, logits, rules, u, token, row_role=None, row_mask=None, log
     arr = (unity_sampling_rule * len(rules))(*rules)
     code = load_library().unity_sample(
         ctx, n, V, logits.data_ptr(), _type_of(logits, "logits"), logits.stride(0) if n > 1 else V, len(rules),
-        _fit(row_role, per, i32, logits, "row_role"), arr, _fit(row_mask, per, torch.uint8, logits, "row_mask"),
-        _fit(u, per, f32, logits, "u"), _fit(token, per, i32, logits, "token"), _fit(logp, per, f32, logits, "logp"),
-        _fit(logp_kept, per, f32, logits, "logp_kept"), _fit(n_kept, per, i32, logits, "n_kept"))
+        _fit(row_role, per, i32, dev, "row_role"), arr, _fit(row_mask, per, torch.uint8, dev, "row_mask"),
+        _fit(u, per, f32, dev, "u"), _fit(token, per, i32, dev, "token"), _fit(logp, per, f32, dev, "logp"),
+        _fit(logp_kept, per, f32, dev, "logp_kept"), _fit(n_kept, per, i32, dev, "n_kept"))
     if code:
         _raise(ctx, code)
 
@@ -765,7 +767,7 @@ class Context:
         return unity_ppo_loss_fwd_bwd(self.ctx, *a, **kw)
 
     def _on_device(self, hidden, name="hidden"):
-        if hidden.is_cuda and hidden.device.index != self.device:
+        if hidden.get_device() not in (self.device, -1):
             raise ValueError(f"{name} is on {hidden.device}, the context on cuda:{self.device}")
 
     def cross_entropy_fwd_bwd(self, hidden, *a, **kw):

@@ -87,6 +87,17 @@ __device__ __forceinline__ void load_gamma(const NormArgs& a, int model, int col
     }
 }
 
+// The same as four packed pairs, for arithmetic on two lanes at once.
+typedef uint64_t Pairs[4];
+__device__ __forceinline__ void pairs_of(const float (&f)[8], Pairs& p) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = ptx::pack2(f[2 * i], f[2 * i + 1]);
+}
+__device__ __forceinline__ void floats_of(const Pairs& p, float (&f)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) ptx::unpack2(p[i], f[2 * i], f[2 * i + 1]);
+}
+
 template <typename T> struct RawOf;
 template <> struct RawOf<__nv_bfloat16> { typedef Raw16 type; };
 template <> struct RawOf<float> { typedef Raw32 type; };
@@ -247,7 +258,7 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
     if (warp == 0)
         for (int i = 0; i < stages; ++i) ask();
 
-    float acc[NV][8], gamma[NV][8];
+    Pairs acc[NV], gamma[NV];
     int model = -1, found = -1, done = 0;
     long long found_end = first;
     unsigned touched = 0;
@@ -258,15 +269,17 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
         for (int j = 0; j < NV; ++j) {
             const int col = (j * WPR * 32 + t) * 8;
             if (col < H) {
+                float f[8];
+                floats_of(acc[j], f);
                 if (touched >> model & 1) {
                     Raw32 r;
-                    float f[8];
+                    float old[8];
                     load8(slice + col, r);
-                    widen(r, f);
+                    widen(r, old);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[j][i] += f[i];
+                    for (int i = 0; i < 8; ++i) f[i] += old[i];
                 }
-                store8(slice + col, acc[j]);
+                store8(slice + col, f);
             }
         }
         touched |= 1u << model;
@@ -299,9 +312,13 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 const int col = (j * WPR * 32 + t) * 8;
-                if (col < H) load_gamma(a, m, col, gamma[j]);
+                if (col < H) {
+                    float g[8];
+                    load_gamma(a, m, col, g);
+                    pairs_of(g, gamma[j]);
+                }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[j][i] = 0.f;
+                for (int i = 0; i < 4; ++i) acc[j][i] = 0;
             }
         }
         const int stage = done % stages;
@@ -310,54 +327,66 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
         const __nv_bfloat16* dy = reinterpret_cast<const __nv_bfloat16*>(in + res_bytes);
         const R* dres = ring_dres ? reinterpret_cast<const R*>(in + res_bytes + dy_bytes) : a.dres ? static_cast<const R*>(a.dres) + base : nullptr;
         if (!ptx::mbar_wait(&full[stage], done / stages & 1, kWaitBudgetCycles) && lane == 0) atomicOr(a.status, kStatusTimeout);
-        float2 sum = make_float2(0.f, 0.f);
+        // r and dy stay in registers; sums of two columns side by side
+        Pairs r[NV], d[NV];
+        uint64_t squares = 0, dots = 0;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = (j * WPR * 32 + t) * 8;
             if (col < H) {
                 typename RawOf<R>::type raw_r;
                 Raw16 raw_d;
-                float r[8], d[8];
+                float f[8];
                 load8(res + col, raw_r);
                 load8(dy + col, raw_d);
-                widen(raw_r, r);
-                widen(raw_d, d);
+                widen(raw_r, f);
+                pairs_of(f, r[j]);
+                widen(raw_d, f);
+                pairs_of(f, d[j]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    sum.x = fmaf(r[i], r[i], sum.x);
-                    sum.y = fmaf(d[i] * gamma[j][i], r[i], sum.y);
+                for (int i = 0; i < 4; ++i) {
+                    squares = ptx::fma2(r[j][i], r[j][i], squares);
+                    dots = ptx::fma2(ptx::mul2(d[j][i], gamma[j][i]), r[j][i], dots);
                 }
             }
         }
+        float lo, hi;
+        float2 sum;
+        ptx::unpack2(squares, lo, hi);
+        sum.x = lo + hi;
+        ptx::unpack2(dots, lo, hi);
+        sum.y = lo + hi;
         // (a barrier: every warp is through with the row before, whose place in the ring takes the next one)
         sum = row_sum<WPR>(sum, slots, done & 1);
         if (warp == 0 && done > 0) ask();
         ++done;
         const float s = 1.f / sqrtf(sum.x / static_cast<float>(H) + a.eps);
-        const float c = s * s * s * (sum.y / static_cast<float>(H));
+        const float c = -s * s * s * (sum.y / static_cast<float>(H));
+        const uint64_t s2 = ptx::pack2(s, s), c2 = ptx::pack2(c, c);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int col = (j * WPR * 32 + t) * 8;
             if (col < H) {
-                typename RawOf<R>::type raw_r;
-                Raw16 raw_d;
-                float r[8], d[8], g[8];
-                load8(res + col, raw_r);
-                load8(dy + col, raw_d);
-                widen(raw_r, r);
-                widen(raw_d, d);
+                Pairs g;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[i] = s * (d[i] * gamma[j][i]) - c * r[i];
-                if (DG && m >= 0)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[j][i] = fmaf(d[i], r[i] * s, acc[j][i]);
-                if (dres) {
-                    load8(dres + col, raw_r);
-                    widen(raw_r, r);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) g[i] += r[i];
+                for (int i = 0; i < 4; ++i) {
+                    const uint64_t sd = ptx::mul2(d[j][i], s2);
+                    if (DG && m >= 0) acc[j][i] = ptx::fma2(sd, r[j][i], acc[j][i]);
+                    g[i] = ptx::fma2(r[j][i], c2, ptx::mul2(sd, gamma[j][i]));
                 }
-                if (m >= 0) store8(dx + col, g); else store8(dx + col, zero);
+                if (dres) {
+                    typename RawOf<R>::type more;
+                    float f[8];
+                    Pairs p;
+                    load8(dres + col, more);
+                    widen(more, f);
+                    pairs_of(f, p);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) g[i] = ptx::add2(g[i], p[i]);
+                }
+                float f[8];
+                floats_of(g, f);
+                if (m >= 0) store8(dx + col, f); else store8(dx + col, zero);
             }
         }
     }
@@ -444,8 +473,10 @@ Ring ring_of(const NormArgs& a) {
 template <int WPR, int NV, typename R, bool DG>
 cudaError_t bwd_launch(const NormArgs& a, int grid, cudaStream_t st) {
     const Ring r = ring_of(a);
-    const cudaError_t e = cudaFuncSetAttribute(k_norm_bwd<WPR, NV, R, DG>, cudaFuncAttributeMaxDynamicSharedMemorySize, r.bytes);
-    if (e != cudaSuccess) return e;
+    if (r.bytes > 47 * 1024) {                                    // (what a block has without asking)
+        const cudaError_t e = cudaFuncSetAttribute(k_norm_bwd<WPR, NV, R, DG>, cudaFuncAttributeMaxDynamicSharedMemorySize, r.bytes);
+        if (e != cudaSuccess) return e;
+    }
     return launch(k_norm_bwd<WPR, NV, R, DG>, grid, 32 * WPR, r.bytes, st, a, r.stages, r.dres);
 }
 template <int WPR, int NV>
