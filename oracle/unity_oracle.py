@@ -667,7 +667,8 @@ def sample_row(z, temperature, top_k, top_p, min_p, u):
     T, top_p, min_p, u = (float(np.float32(v)) for v in (temperature, top_p, min_p, u))
     if np.isnan(z).any() or z.max() == np.inf or z.max() == -np.inf:
         return -1, np.nan, np.nan, 0
-    x = (z - z.max()) / (T if T > 0 else 1.0)
+    # (running sums of many thousand entries next to a mass of 1: in extended precision)
+    x = (z - z.max()).astype(np.longdouble) / (T if T > 0 else 1.0)
     e = np.exp(x)
     order = np.argsort(-z, kind="stable")
     order = order[z[order] > -np.inf]
@@ -680,11 +681,10 @@ def sample_row(z, temperature, top_k, top_p, min_p, u):
             order = order[x[order] >= np.log(min_p)]
         if top_p < 1:
             run = np.cumsum(e[order])
-            before = np.concatenate([[0.0], run[:-1]])
-            order = order[before < top_p * run[-1]]
+            order = order[run - e[order] < top_p * run[-1]]
     kept = np.sort(order)
     run = np.cumsum(e[kept])
     past = np.nonzero(run > u * run[-1])[0]
     j = int(past[0]) if past.size else int(np.nonzero(e[kept] > 0)[0][-1])
     t = int(kept[j])
-    return t, x[t] - np.log(e.sum()), x[t] - np.log(run[-1]), int(kept.size)
+    return t, float(x[t] - np.log(e.sum())), float(x[t] - np.log(run[-1])), int(kept.size)

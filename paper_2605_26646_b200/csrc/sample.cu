@@ -206,6 +206,7 @@ struct Row {
     double inv_t, c64;                       // 1 / T, log2(e) / T
     float c, top_c;                          // log2(e) / T and that times the largest logit, in fp32
     double whole;                            // mass of all entries
+    double my_all;                           // fp32: the thread's share of the mass of all entries of the row
     // what is known about the end of the kept entries: it lies in [lo, hi); the thread's own mass and numbers there
     float lo, hi;
     int n_lo, n_hi;
@@ -638,7 +639,7 @@ struct Row {
         bool close = false;
         int token = -1;
         float tz = 0.f;
-        double start = 0.0;
+        double start = 0.0, logp = 0.0, logp_kept = 0.0;
         if (owner(block, 0.0, target, lane(), &start) == rank && owner(of_warp, start, target, lane(), &start) == warp()) {
             const int holder = owner(mine, start, target, lane(), &start);
             close = fabs(start - target) <= bound;
@@ -664,18 +665,36 @@ struct Row {
                 if (above) break;
                 start = __shfl_sync(kFull, at, 31);
             }
+            const double x = (static_cast<double>(tz) - static_cast<double>(top)) * inv_t;
+            // fp32 weights have the largest logit's own in common, which rounding leaves next to 1
+            const double common = EXACT ? 0.0 : 0.69314718055994531 * static_cast<double>(octaves(top));
+            logp = x + common - log(whole);
+            logp_kept = x + common - log(kept);
+            if (!EXACT && tz == top) {
+                // The likeliest entry may have nearly all of the mass: log p from what the others have, the sums without the thread's
+                // share, and its other entries on their own (a sum of small ones next to a large one loses their digits)
+                double others = 0.0, others_kept = 0.0;
+                const T* all_z = static_cast<const T*>(a.logits) + row * a.ld;
+                for (int j = lane(); j < per; j += 32) {
+                    const int i = base + j;
+                    if (i == token || i >= a.V) continue;
+                    others += static_cast<double>(fast(one(all_z + i)));
+                    const float v = one(row_z + j);
+                    if (v >= hi || (v >= lo && cut.keeps(v, i))) others_kept += static_cast<double>(fast(v));
+                }
+                others = warp_sum(others) + (whole - __shfl_sync(kFull, my_all, holder));
+                others_kept = warp_sum(others_kept) + (kept - __shfl_sync(kFull, mine, holder));
+                const double own = static_cast<double>(fast(top));
+                logp = 0.0 - log1p(fmax(others, 0.0) / own);
+                logp_kept = 0.0 - log1p(fmax(others_kept, 0.0) / own);
+            }
         }
         if (!EXACT) {
             // (the block that holds the target decides for the cluster)
             got = all_to_all(__syncthreads_or(close) != 0);
             if (__any_sync(kFull, lane() < ctas && got[lane() < ctas ? lane() : 0] != 0)) return false;
         }
-        if (token >= 0 && lane() == 0) {
-            const double x = (static_cast<double>(tz) - static_cast<double>(top)) * inv_t;
-            // fp32 weights have the largest logit's own in common, which rounding leaves next to 1
-            const double common = EXACT ? 0.0 : 0.69314718055994531 * static_cast<double>(octaves(top));
-            put_row(a, row, token, x + common - log(whole), x + common - log(kept), n_kept);
-        }
+        if (token >= 0 && lane() == 0) put_row(a, row, token, logp, logp_kept, n_kept);
         return true;
     }
 
@@ -702,6 +721,7 @@ struct Row {
             const float at[kTau] = {floor, INFINITY};
             const Tally mine = weigh<EXACT, true>(at), v = exchange(mine);
             whole = v.whole;
+            my_all = mine.whole;
             lo = hi = floor;
             marks[0] = marks[1] = 0;
             my_m = mine.m[0];
@@ -842,6 +862,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
         mean = about.x + f * w;
         square = about.y + f * (2.f * about.x + f * w);
     }
+    const double my_mass = mass;
+    const int my_unit = unit;
     // Sums of masses in different units over the lanes of a warp.
     auto add_units = [&]() {
         const int most = __reduce_max_sync(kFull, unit), below = unit - most;
@@ -904,7 +926,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     }
     r.top = top;
     r.top_c = top * r.c;
-    r.whole = mass * exp2(static_cast<double>(unit) - static_cast<double>(r.top_c));
+    const double to_top = exp2(static_cast<double>(unit) - static_cast<double>(r.top_c));
+    r.whole = mass * to_top;
+    r.my_all = times_power(my_mass, my_unit - unit) * to_top;
     // Where top-p ends in a normal distribution of the same mean and variance, and whether the entropy, log2 of the mass less the mean
     // in octaves below the largest, is that of more than some four hundred entries.  (Guesses.)
     mean /= static_cast<float>(mass);
@@ -1170,6 +1194,27 @@ struct Stream {
     }
 };
 
+// log p of the row's entry `token`, whose logit is the largest, in the block that has it, by its first warp: from what the others have
+// (see pick), their sums without the lane's tile, and the tile's other entries on their own.
+template <typename T>
+__device__ __forceinline__ double largest_logp(const Stream<T>& r, int token, double whole, int unit) {
+    const int lane = threadIdx.x & 31, warp = (token - r.begin(0)) / r.run, tile = (token - r.begin(warp)) / kTileEntries;
+    const int base = r.begin(warp) + tile * kTileEntries;
+    Tile<T> t;
+    t.load(r.row, base, min(r.V, r.begin(warp) + r.run), r.aligned);
+    const float2 m = r.s.lane_m[tile][warp * 32 + lane];
+    const int own = static_cast<int>(m.y), shift = own - unit;
+    double others = 0.0, mine = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) {
+        const double e = r.template weight<false>(t.value(i), own);
+        if (Tile<T>::index(base, i) == token) mine = e; else others += e;
+    }
+    others = times_power(others, shift) + (whole - times_power(static_cast<double>(m.x), shift));
+    const double logp = 0.0 - log1p(fmax(others, 0.0) / times_power(mine, shift));
+    return __shfl_sync(kFull, logp, __ffs(__ballot_sync(kFull, mine > 0.0)) - 1);
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_constant__ SampleArgs a, int run, int ctas) {
     __shared__ StreamShared s;
@@ -1264,18 +1309,21 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
         } else {
             // log of the whole mass: its unit, less what the rounding of c adds to every exponent alike
             const double lse = (log2(f.whole) + f.unit - static_cast<double>(f.top) * (static_cast<double>(r.c) - r.c64)) * 0.69314718055994531;
+            const bool fits = fabsf(f.top * r.c) <= 0x1p20f;          // (far from 0 a unit and c times a logit have no digits left to differ in)
             if (greedy) {
-                if (rank == 0 && lane == 0) put_row(a, row, f.top_i, static_cast<double>(f.top) - lse, 0.0, 1);
+                if (f.top_i / (kWarps * run) == rank) {
+                    const double logp = fits ? largest_logp(r, f.top_i, f.whole, f.unit) : static_cast<double>(f.top) - lse;
+                    if (lane == 0) put_row(a, row, f.top_i, logp, 0.0, 1);
+                }
             } else {
-                // (far from 0 a unit and c times a logit have no digits left to differ in)
                 r.expect(ctas);
-                if (lane < ctas) send(r.box(rank), r.mail(), lane, f.close || !(fabsf(f.top * r.c) <= 0x1p20f));
+                if (lane < ctas) send(r.box(rank), r.mail(), lane, f.close || !fits);
                 const unsigned long long* got = r.box(0);
                 r.receive();
                 again = __any_sync(kFull, lane < ctas && got[lane < ctas ? lane : 0] != 0);
-                if (!again && f.token >= 0 && lane == 0) {
-                    const double logp = static_cast<double>(f.tz) * rule.inv_t - lse;
-                    put_row(a, row, f.token, logp, logp, f.n);
+                if (!again && f.token >= 0) {
+                    const double logp = f.tz == f.top ? largest_logp(r, f.token, f.whole, f.unit) : static_cast<double>(f.tz) * rule.inv_t - lse;
+                    if (lane == 0) put_row(a, row, f.token, logp, logp, f.n);
                 }
             }
         }

@@ -115,6 +115,36 @@ def test_uniform_distribution_takes_64_bits():
     check(z, [(1.0, 0, 0.5, 0.0)], u, None, draw(z, [(1.0, 0, 0.5, 0.0)], u))
 
 
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("V", [300, 4096, 151936])
+@pytest.mark.parametrize("rule", [OFF, (0.0, 0, 1.0, 0.0), (1.0, 40, 1.0, 0.0), (1.0, 0, 0.9999999, 0.0), (1.0, 0, 1.0, 1e-9), (0.5, 200, 0.99, 0.0),
+                                  (1.0, 100000, 0.999999, 0.0)])
+def test_sure_tokens_keep_their_digits(V, dtype, rule):
+    """log p of an entry with nearly all of the mass is what the others have, relative to itself: each weight is off by 2^-22 and by two
+    roundings of an exponent of at most 40 octaves (2 * 40 * ln2 * 2^-24 = 3.3e-6), both sides of the quotient: 7.2e-6 and the output's
+    rounding.  The others' mass is a difference of fp64 sums of about 1 (5 + 3 + 4 lanes, warps and blocks, and the share that is taken
+    off: 13 additions of at most 2^-53): 2^-49 absolute.  One entry alone has log p = 0."""
+    n = 12
+    z = logits(n, V, "normal", dtype, V).float()
+    z[torch.arange(n), torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(V))] = torch.linspace(12, 27, n, device="cuda") + np.log(V) / 2
+    z = z.to(dtype)
+    u = torch.full((n,), 0.5, device="cuda")
+    got = draw(z, [rule], u)
+    check(z, [rule], u, None, got)
+    zs = z.double().cpu().numpy()
+    for i in range(n):
+        t, lp, lk, k = orc.sample_row(zs[i], *rule, 0.5)
+        T = float(np.float32(rule[0])) or 1.0
+        x = (zs[i] - zs[i].max()) / T
+        order = np.argsort(-zs[i], kind="stable")
+        if t != order[0]:
+            continue
+        rest = np.exp(np.delete(x, t)).sum()
+        rest_kept = np.exp(x[order[1:k]]).sum()
+        for v, w in ((got[1][i], -np.log1p(rest)), (got[2][i], -np.log1p(rest_kept))):
+            assert abs(v - w) <= 7.4e-6 * abs(w) + 2.0 ** -49, (i, v, w)
+
+
 def test_rows_without_a_distribution_and_masked_rows():
     z = logits(8, 3001, "peaked", F32, 1)
     z[1, 2000] = float("nan")
