@@ -125,7 +125,9 @@ __device__ __forceinline__ float2 row_sum(float2 v, float2 (&slots)[2][WPR], int
 
 // ------------------------------------------------------------------------------------------------
 // y = gamma r s, r = x + residual, s = 1 / sqrt(mean r^2 + eps).  A row belongs to WPR warps, each lane holding NV vectors of
-// eight columns, 256 WPR columns apart.  The norm is taken of the fp32 sum; r is rounded only where it is written.
+// eight columns, 256 WPR columns apart: at most eight, so that all of a row's loads are in flight at once and a dozen rows fit an SM.
+// The norm is taken of the fp32 sum; r is rounded only where it is written.  HBM bounds it (20001 x 3584 bf16 82 us, 98 % of the copy
+// rate; 32768 x 5120 with fp32 residual 291 us), one row takes 4.4 us from launch to launch.
 // ------------------------------------------------------------------------------------------------
 constexpr int kFwdRowsOfWarps = 4;          // rows of a block whose rows belong to one warp each
 template <int WPR, int NV, typename R, bool HAS_R>
@@ -212,7 +214,8 @@ __global__ void __launch_bounds__(WPR == 1 ? 32 * kFwdRowsOfWarps : 32 * WPR) k_
 // dr = s g - r s^3 mean(g r) + dres with g = dy gamma; dgamma += dy r s.  A block takes a run of consecutive rows, so that its
 // dgamma stays in registers; where the model changes it goes to the block's slice of that model and the next one begins.  The rows
 // come through a ring in shared memory, by asynchronous copies that run ahead of the row that is worked on: registers hold the
-// columns' sums and weights only, and HBM is asked for rows without a pause.
+// columns' sums and weights only, and HBM is asked for rows without a pause (40001 x 3584 fp32 with dres: 285 to 300 us, 0.9 of the
+// copy rate; rows in registers, without the ring, 378).  5000 x 1536 bf16: 22 us with the sums of the slices, most of it latency.
 // ------------------------------------------------------------------------------------------------
 constexpr int kMaxStages = 4;
 template <int WPR, int NV, typename R, bool DG>

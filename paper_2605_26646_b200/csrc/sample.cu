@@ -14,6 +14,9 @@
 // A decision compares a sum of masses with a share of another.  Sums are taken of fp32 exponentials first, with a bound on
 // their error (kSlackFast); where a comparison is closer than that, the row is done again with fp64 exponentials, so the outcome
 // is that of 64-bit arithmetic either way.
+//
+// What bounds it: latency for few rows (one of 152064: 14 us, some ten exchanges of about 1.2 thousand clocks), issue slots for many
+// (512 rows of 151936 fp32: top-k 322 us, min-p 224, top-p of a few tokens 370 to 570; the row's bytes would take 48).
 #include "internal.h"
 #include "ptx.cuh"
 
@@ -968,7 +971,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
 // Rows whose rule leaves every entry (no top-k, top-p or min-p) and rows that take the largest logit: one pass over the logits in
 // registers, no copy in shared memory, so that more rows are in flight.  Every warp of the cluster has a run of consecutive entries,
 // in tiles of 512; a lane's mass of a tile refers to a power of two next to the lane's largest entry there.  The warp whose running
-// mass holds the target reads one of its tiles again.
+// mass holds the target reads one of its tiles again.  512 rows of 151936: fp32 86 us (3.6 TB/s), bf16 61; each row ends with 6 to 8
+// thousand clocks in which one warp of a block is at work, and rows whose decision is close (a third of flat ones) are read again.
 // ------------------------------------------------------------------------------------------------
 constexpr int kTileEntries = 512, kPerLane = kTileEntries / 32;
 constexpr int kMaxTiles = 20;                // of a warp

@@ -96,3 +96,51 @@ def test_rollout_and_update_of_two_models(captured):
     assert np.all(np.abs(norm.cpu().numpy() - wn) <= pu.TOL_GRAD * wn) and wc[0] < 1 and wc[1] == 1 and coef[1].item() == 1
     for a, b in zip(out, wo):
         assert pu.rel_fro(a.float().cpu().numpy(), b) <= 2 * pu.TOL_GRAD
+
+
+def test_contexts_on_two_streams_at_once():
+    """The same three calls on two contexts whose kernels overlap give what each gives alone."""
+    work = []
+    for seed in (1, 2):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        st = torch.cuda.Stream()
+        n, H, V = 700, 1536, 33000
+        d = dict(st=st, x=torch.randn(n, H, generator=g, device="cuda").to(B16), gamma=[torch.randn(H, generator=g, device="cuda") for _ in range(2)],
+                 cu=torch.tensor([0, 300, n], device="cuda"), role=torch.tensor([0, 1], dtype=torch.int32, device="cuda"),
+                 z=torch.randn(300, V, generator=g, device="cuda") * 3, u=torch.rand(300, generator=g, device="cuda"),
+                 grads=[torch.randn(300001, generator=g, device="cuda"), torch.randn(4097, generator=g, device="cuda").to(B16)])
+        d["ctx"] = ub.Context(0, max(ub.unity_rms_norm_workspace_bytes(n, H, 2), ub.unity_clip_grad_norm_workspace_bytes(2, 2)), st)
+        d["o"] = lambda d=d, n=n, H=H: dict(
+            y=torch.zeros(n, H, dtype=B16, device="cuda"), dx=torch.zeros(n, H, dtype=B16, device="cuda"),
+            dg=[torch.zeros(H, device="cuda") for _ in range(2)], token=torch.zeros(300, dtype=torch.int32, device="cuda"),
+            logp=torch.zeros(300, device="cuda"), norm=torch.zeros(2, device="cuda"), out=[torch.zeros_like(t) for t in d["grads"]])
+        work.append(d)
+    torch.cuda.synchronize()
+
+    def go(d, o):
+        route = (d["cu"], d["role"], [0, 1], None, 1e-6)
+        d["ctx"].rms_norm_fwd(d["x"], d["gamma"], *route, o["y"])
+        d["ctx"].sample(d["z"], [(0.9, 30, 0.9, 0.0)], d["u"], o["token"], None, None, o["logp"])
+        d["ctx"].rms_norm_bwd(d["x"], d["gamma"], *route, o["y"], o["dx"], None, o["dg"])
+        d["ctx"].clip_grad_norm(ub.GradTensors(d["grads"], [0, 1], o["out"]), [1.0, 1e9], o["norm"])
+
+    def flat(o):
+        return [t for v in o.values() for t in (v if isinstance(v, list) else [v])]
+
+    alone = []
+    for d in work:
+        o = d["o"]()
+        torch.cuda.synchronize()
+        go(d, o)
+        torch.cuda.synchronize()
+        alone.append(flat(o))
+    for _ in range(5):
+        outs = [d["o"]() for d in work]
+        torch.cuda.synchronize()
+        for d, o in zip(work, outs):
+            go(d, o)
+        torch.cuda.synchronize()
+        for o, want in zip(outs, alone):
+            assert all(torch.equal(a, b) for a, b in zip(flat(o), want))
+    for d in work:
+        d["ctx"].check_status()
