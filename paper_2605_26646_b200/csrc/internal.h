@@ -697,6 +697,7 @@ cudaError_t launch_grad_scale(const ClipArgs& a, const ClipEntry* entries, int n
 // ----------------------------------------------------------------------------------------------
 // Sampling (sample.cu)
 // ----------------------------------------------------------------------------------------------
+constexpr int kSampleListK = 384;          // largest top-k that a short list serves
 struct SampleRule {
     float temperature;                   // 0: the largest logit
     int top_k;                           // 0: off
@@ -704,6 +705,7 @@ struct SampleRule {
     double top_p;                        // >= 1: off
     float quantile;                      // of the normal distribution at top_p
     int search;                          // the rule cuts entries off
+    int list;                            // mostly so many that a short list holds what is left
 };
 struct SampleArgs {
     const void* logits;
@@ -718,7 +720,7 @@ struct SampleArgs {
     int* status;
     SampleRule rules[UNITY_MAX_ROLES];
 };
-// any_search, any_other: there are rules that cut entries off, and others
-cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_other, int sm_count, cudaStream_t stream, int* n_launches);
+// any_search, any_list, any_other: there are rules that cut entries off, such as may leave few, and others
+cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_list, bool any_other, int sm_count, cudaStream_t stream, int* n_launches);
 
 }  // namespace unity

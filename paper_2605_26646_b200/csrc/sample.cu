@@ -1,6 +1,7 @@
 // Next tokens from logits and given uniform numbers (unity_sample): temperature, top-k, top-p and min-p by a rule per role.
 //
-// Rows whose rule cuts nothing off take one pass over the logits (k_sample_stream, below); the others are searched (k_sample).
+// Rows take one pass over the logits (k_sample_stream, below), at whose end a short list mostly decides where the rule cuts entries
+// off; those that it cannot decide (flat ones by top-p, large top-k, masses too close) are searched (k_sample).
 //
 // k_sample: a cluster of blocks holds a row in shared memory: the logits cross HBM once and every further pass over them stays on chip.
 // Thread order is index order (a thread owns `per` consecutive entries), so running masses are sums over threads.
@@ -16,7 +17,7 @@
 // is that of 64-bit arithmetic either way.
 //
 // What bounds it: latency for few rows (one of 152064: 14 us, some ten exchanges of about 1.2 thousand clocks), issue slots for many
-// (512 rows of 151936 fp32: top-k 322 us, min-p 224, top-p of a few tokens 370 to 570; the row's bytes would take 48).
+// (512 rows of 151936 fp32: top-p of ten thousand tokens 900 us; the row's bytes would take 48).
 #include "internal.h"
 #include "ptx.cuh"
 
@@ -27,6 +28,7 @@ namespace {
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 16;
+constexpr int kUnlisted = -2;                // a row's token between the two kernels: it is left to the search
 constexpr int kList = 1024;                  // entries sorted at most
 constexpr int kTau = 2;                      // thresholds of a pass
 constexpr float kLowest = -3.402823466e38f;
@@ -196,6 +198,47 @@ struct Cut {
     int i;
     __device__ __forceinline__ bool keeps(float v, int at) const { return v > z || (v == z && at <= i); }
 };
+
+// Sorts `total` numbers of a block's shared memory, room for kList of them: rising.
+__device__ __forceinline__ void sort_items(unsigned long long* list, int total) {
+    int log_size = 6;
+    while (1 << log_size < total) ++log_size;
+    const int size = 1 << log_size;
+    for (int i = total + threadIdx.x; i < size; i += kThreads) list[i] = ~0ull;
+    __syncthreads();
+    if (total <= kThreads) {
+        // each counts the smaller ones
+        const unsigned long long mine = threadIdx.x < total ? list[threadIdx.x] : ~0ull;
+        int below = 0;
+        if (threadIdx.x < total)
+#pragma unroll 8
+            for (int i = 0; i < total; ++i) below += list[i] < mine;
+        __syncthreads();
+        if (threadIdx.x < total) list[below] = mine;
+        __syncthreads();
+        return;
+    }
+    // bitonic: a thread compares two pairs per step; up to 32 apart the pairs of a warp are the warp's own
+    for (int k = 1; k <= log_size; ++k)
+        for (int j = k - 1; j >= 0; --j) {
+            for (int t = threadIdx.x; t < size / 2; t += kThreads) {
+                const int i = (t >> j << (j + 1)) | (t & ((1 << j) - 1));
+                const unsigned long long a = list[i], b = list[i + (1 << j)];
+                if ((a > b) == ((i >> k & 1) == 0)) { list[i] = b; list[i + (1 << j)] = a; }
+            }
+            if (j > 5 || (j > 0 ? j - 1 : k) > 5) __syncthreads(); else __syncwarp();
+        }
+    __syncthreads();
+}
+// The lowest logit that min-p leaves, next to the largest one: (z - top) / T >= log min_p.
+__device__ __forceinline__ float lowest_allowed(const SampleRule& rule, float top) {
+    const double want = static_cast<double>(top) + rule.log_min_p / rule.inv_t;
+    float floor = want > -3.4e38 ? static_cast<float>(want) : kLowest;
+    auto passes = [&](float v) { return (static_cast<double>(v) - static_cast<double>(top)) * rule.inv_t >= rule.log_min_p; };
+    for (int k = 0; k < 4 && floor > kLowest && passes(nextafterf(floor, -INFINITY)); ++k) floor = nextafterf(floor, -INFINITY);
+    for (int k = 0; k < 4 && floor < top && !passes(floor); ++k) floor = nextafterf(floor, INFINITY);
+    return floor;
+}
 
 template <typename T>
 struct Row {
@@ -511,35 +554,8 @@ struct Row {
                                             static_cast<unsigned>(first - threadIdx.x * per + at);
             send(&s.list[base + k], mail(), i & (ctas - 1), item);
         }
-        int log_size = 6;
-        while (1 << log_size < total) ++log_size;
-        const int size = 1 << log_size;
-        for (int i = total + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
         receive();
-        __syncthreads();
-        if (total <= kThreads) {
-            // each counts the smaller ones
-            const unsigned long long mine = threadIdx.x < total ? s.list[threadIdx.x] : ~0ull;
-            int below = 0;
-            if (threadIdx.x < total)
-#pragma unroll 8
-                for (int i = 0; i < total; ++i) below += s.list[i] < mine;
-            __syncthreads();
-            if (threadIdx.x < total) s.list[below] = mine;
-            __syncthreads();
-            return true;
-        }
-        // bitonic: a thread compares two pairs per step; up to 32 apart the pairs of a warp are the warp's own
-        for (int k = 1; k <= log_size; ++k)
-            for (int j = k - 1; j >= 0; --j) {
-                for (int t = threadIdx.x; t < size / 2; t += kThreads) {
-                    const int i = (t >> j << (j + 1)) | (t & ((1 << j) - 1));
-                    const unsigned long long a = s.list[i], b = s.list[i + (1 << j)];
-                    if ((a > b) == ((i >> k & 1) == 0)) { s.list[i] = b; s.list[i + (1 << j)] = a; }
-                }
-                if (j > 5 || (j > 0 ? j - 1 : k) > 5) __syncthreads(); else __syncwarp();
-            }
-        __syncthreads();
+        sort_items(s.list, total);
         return true;
     }
 
@@ -817,7 +833,7 @@ __device__ __forceinline__ void fetch(Shared& s, T* z, const T* src, int n, int 
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ SampleArgs a, int per, int ctas) {
+__global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ SampleArgs a, int per, int ctas, int listed) {
     __shared__ Shared s;
     extern __shared__ __align__(16) unsigned char raw[];
     T* z = reinterpret_cast<T*>(raw);
@@ -826,6 +842,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     SampleRule rule;
     float u;
     if (!row_begins(a, row, rank, rule, u) || !rule.search) return;           // (the same in every block of the cluster)
+    if (listed && rule.list && a.token[row] != kUnlisted) return;             // (nor does one write before it hears from all of them)
     if (threadIdx.x == 0) {
         ptx::mbar_init(&s.bar, 1);
         ptx::mbar_init(&s.mail[0], 1);
@@ -941,15 +958,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     r.list_lo = r.list_hi = 0.f;
     r.cut_down = false;
     const int n_all = r.n_all;
-    float floor = -INFINITY;
-    if (rule.log_min_p > -INFINITY) {
-        // the lowest logit with x >= log min_p
-        const double want = static_cast<double>(top) + rule.log_min_p / rule.inv_t;
-        floor = want > -3.4e38 ? static_cast<float>(want) : kLowest;
-        auto passes = [&](float v) { return (static_cast<double>(v) - static_cast<double>(top)) * rule.inv_t >= rule.log_min_p; };
-        for (int k = 0; k < 4 && floor > kLowest && passes(nextafterf(floor, -INFINITY)); ++k) floor = nextafterf(floor, -INFINITY);
-        for (int k = 0; k < 4 && floor < top && !passes(floor); ++k) floor = nextafterf(floor, INFINITY);
-    }
+    const float floor = rule.log_min_p > -INFINITY ? lowest_allowed(rule, top) : -INFINITY;
     // (fp32 weights have 2^(rounding of top_c) in common, which has to stay near 1)
     const bool fits = fabsf(r.top_c) <= 0x1p20f;
     if (fits && r.template draw<false>(a, row, rule, floor, my_top, n, u, centre, width, spread)) return;
@@ -978,17 +987,32 @@ constexpr int kTileEntries = 512, kPerLane = kTileEntries / 32;
 constexpr int kMaxTiles = 20;                // of a warp
 static_assert(kMaxTiles * kMaxCluster * kWarps * kTileEntries >= UNITY_MAX_SAMPLE_V, "enough for a row");
 
+constexpr int kBins = 128, kListP = 128;      // (kListP: entries of a list for top-p, about)
+struct ListState {                           // what a cluster's blocks know alike
+    float top, floor;
+    int unit, n_all, least, total, base;
+    double whole, rest;
+};
+struct ListSpace {
+    unsigned long long list[kList], stage[kList];
+    uint16_t queue[kList];
+};
 struct StreamShared {
     uint64_t mail[2];
-    unsigned long long box[2][3 * kMaxCluster];
+    unsigned long long box[2][4 * kMaxCluster];
     double warp_m[kWarps];                   // mass of a warp, in units of 2^warp_r
     int warp_r[kWarps], warp_n[kWarps], warp_i[kWarps];
     float warp_top[kWarps];
     float top;                               // what the first warp found out for the others
     int again;
+    ListState known;
+    int bins[kBins];                         // groups by their largest entry, in octaves below the block's largest
+    int n_listed;
+    double scan_a[kWarps], scan_b[kWarps];
     union {                                  // a lane's mass of a tile
         float2 lane_m[kMaxTiles][kThreads];  // x in units of 2^y
         double lane_x[kMaxTiles][kThreads];  // from fp64 weights, in units of 1
+        ListSpace space;                     // (when the masses are no longer needed)
     };
     double exp2_table[32];
 };
@@ -1219,14 +1243,278 @@ __device__ __forceinline__ double largest_logp(const Stream<T>& r, int token, do
     return __shfl_sync(kFull, logp, __ffs(__ballot_sync(kFull, mine > 0.0)) - 1);
 }
 
+// Rows whose rule cuts entries off.  A lane's tile is a group of 16 entries, and the pass has left the octave of its largest entry: an
+// index of the row.  Where at least k groups reach an octave, at least k entries do, and all that do are in those groups.  They are
+// read again, what reaches the octave goes to a list in the first block, and that block decides, with fp64 exponentials: of top-k
+// and min-p all that counts is in the list.  top-p needs the mass of the others too; where that is too close, or the list does not
+// reach it or has no room, the row is left to the search.  512 rows of 151936, with the launch of the search behind it: fp32 top-k 133
+// us (all of it by the search 338), min-p 123 (239); bf16 97 (184) and 91 (143).
 template <typename T>
+__device__ __forceinline__ void list_row(Stream<T>& r, const SampleArgs& a, int row, const SampleRule& rule, float u, int tiles) {
+    StreamShared& s = r.s;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tid = threadIdx.x;
+    constexpr int kNone = -0x40000000;
+    float block_top = s.warp_top[0];
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i) block_top = max_nan(block_top, s.warp_top[i]);
+    const int block_unit = static_cast<int>(r.unit_of(block_top));
+    for (int k = 0; k < tiles; ++k) {
+        const float2 m = s.lane_m[k][tid];
+        const unsigned below = static_cast<unsigned>(block_unit - static_cast<int>(m.y));   // (a block's NaN or inf has no unit: too large)
+        if (m.x > 0.f && below < kBins) atomicAdd(&s.bins[below], 1);
+    }
+    if (warp == 0) s.exp2_table[lane] = exp2(lane / 32.0);
+    __syncthreads();
+    if (warp == 0) {
+        // the octave that the block's share of the wanted number reaches
+        const int valid = max(min(a.V, r.begin(kWarps)) - r.begin(0), 0);
+        const int want = static_cast<int>((static_cast<long long>(valid) * (rule.top_k > 0 ? rule.top_k : kListP) + a.V - 1) / a.V);
+        int n[kBins / 32], sum = 0;
+#pragma unroll
+        for (int q = 0; q < kBins / 32; ++q) sum += n[q] = s.bins[lane * (kBins / 32) + q];
+        int upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(kFull, upto, o);
+            if (lane >= o) upto += v;
+        }
+        int least = -0x7fffffff, at = upto - sum;
+#pragma unroll
+        for (int q = 0; q < kBins / 32; ++q) {
+            at += n[q];
+            if (at >= want && least == -0x7fffffff) least = block_unit - (lane * (kBins / 32) + q);
+        }
+        least = __reduce_max_sync(kFull, least);
+        if (valid == 0 || least == -0x7fffffff) least = 0x7fffffff;   // (says nothing)
+        // masses of the blocks, in units next to the largest entry
+        double m = lane < kWarps ? s.warp_m[lane] : 0.0;
+        const int unit = lane < kWarps && m > 0.0 ? s.warp_r[lane] : kNone, most = __reduce_max_sync(kFull, unit);
+        m = warp_sum(times_power(m, unit - most));
+        const int count = __reduce_add_sync(kFull, lane < kWarps ? s.warp_n[lane] : 0);
+        r.expect(4 * r.ctas);
+        if (lane < r.ctas) {
+            send(r.box(4 * r.rank), r.mail(), lane, static_cast<unsigned long long>(__double_as_longlong(m)));
+            send(r.box(4 * r.rank + 1), r.mail(), lane, static_cast<unsigned long long>(static_cast<unsigned>(most)) << 32 | static_cast<unsigned>(count));
+            send(r.box(4 * r.rank + 2), r.mail(), lane, static_cast<unsigned long long>(__float_as_uint(block_top)) << 32 | static_cast<unsigned>(least));
+            send(r.box(4 * r.rank + 3), r.mail(), lane, 0);
+        }
+        const unsigned long long* got = r.box(0);
+        r.receive();
+        const bool on = lane < r.ctas;
+        got += 4 * (on ? lane : 0);
+        double mass = on ? __longlong_as_double(static_cast<long long>(got[0])) : 0.0;
+        const int their_unit = on ? static_cast<int>(got[1] >> 32) : kNone;
+        float top = on ? __uint_as_float(static_cast<unsigned>(got[2] >> 32)) : -INFINITY;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
+        ListState w = {};
+        w.top = top;
+        w.unit = __reduce_max_sync(kFull, their_unit);
+        w.whole = warp_sum(times_power(mass, their_unit - w.unit));
+        w.n_all = __reduce_add_sync(kFull, on ? static_cast<int>(got[1] & 0xffffffffu) : 0);
+        w.least = __reduce_min_sync(kFull, on ? static_cast<int>(got[2] & 0xffffffffu) : 0x7fffffff);
+        if (w.n_all <= kList) w.least = kNone;                    // all of them
+        w.floor = kLowest;
+        if (rule.log_min_p > -INFINITY && top > -INFINITY && top < INFINITY) {
+            w.floor = lowest_allowed(rule, top);
+            const int reached = static_cast<int>(r.unit_of(w.floor));
+            w.least = rule.top_k > 0 ? max(w.least, reached) : reached;
+        }
+        if (lane == 0) { s.known = w; s.n_listed = 0; }
+    }
+    __syncthreads();
+    const float top = s.known.top, floor = s.known.floor;
+    const int unit = s.known.unit, least = s.known.least;
+    if (!(top > -INFINITY && top < INFINITY)) {                   // NaN, +inf or nothing but -inf
+        if (r.rank == 0 && tid == 0) no_distribution(a, row);
+        return;
+    }
+    // the groups that reach it; mass of the others
+    unsigned marked = 0;
+    double rest = 0.0;
+    for (int k = 0; k < tiles; ++k) {
+        const float2 m = s.lane_m[k][tid];
+        if (m.x > 0.f && static_cast<int>(m.y) >= least) marked |= 1u << k;
+        else rest += r.template lane_mass<false>(k, tid, unit);
+    }
+    const int n_marked = __popc(marked);
+    int upto = n_marked;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) s.warp_n[warp] = upto;
+    __syncthreads();                                              // from here on the masses' memory is free
+    const int of_warp = lane < kWarps ? s.warp_n[lane] : 0, n_queue = __reduce_add_sync(kFull, of_warp);
+    int to = upto - n_marked + __reduce_add_sync(kFull, lane < warp ? of_warp : 0);
+    const bool room = n_queue <= kList && fabsf(top * r.c) <= 0x1p20f;   // (far from 0 a unit and c times a logit have no digits left to differ in)
+    ListSpace& sp = s.space;
+    if (room)
+        for (; marked; marked &= marked - 1) sp.queue[to++] = static_cast<uint16_t>((__ffs(marked) - 1) * kThreads + tid);
+    __syncthreads();
+    constexpr int kVec = Tile<T>::kVec, kVecs = Tile<T>::kVecs;
+    const float below = static_cast<float>(least) - 1.f;
+    if (room)
+        for (int i = tid; i < n_queue * kVecs; i += kThreads) {
+            const int g = sp.queue[i / kVecs], t = g % kThreads, begin = r.begin(t / 32), end = min(a.V, begin + r.run);
+            const int at = begin + g / kThreads * kTileEntries + i % kVecs * (32 * kVec) + t % 32 * kVec;
+            float x[kVec];
+            if (r.aligned && at + kVec <= end) {
+#pragma unroll
+                for (int q = 0; q < kVec; q += 2) { const float2 two = pair(r.row + at + q); x[q] = two.x; x[q + 1] = two.y; }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kVec; ++q) x[q] = at + q < end ? one(r.row + at + q) : -INFINITY;
+            }
+#pragma unroll
+            for (int q = 0; q < kVec; ++q) {
+                if (x[q] >= floor && fmaxf(x[q] * r.c, -1e9f) > below) {
+                    const int n = atomicAdd(&s.n_listed, 1);      // (any order: they are sorted)
+                    if (n < kList) sp.stage[n] = static_cast<unsigned long long>(~key_of(x[q])) << 32 | static_cast<unsigned>(at + q);
+                } else {
+                    rest += r.template weight<false>(x[q], unit);
+                }
+            }
+        }
+    rest = warp_sum(rest);
+    if (lane == 0) s.warp_m[warp] = rest;
+    __syncthreads();
+    const bool by_mass = rule.top_p < 1.0 && rule.top_k == 0 && rule.log_min_p == -INFINITY;
+    if (warp == 0) {
+        const int n = room && s.n_listed <= kList ? s.n_listed : 2 * kList;
+        rest = warp_sum(lane < kWarps ? s.warp_m[lane] : 0.0);
+        r.expect(2 * r.ctas);
+        if (lane < r.ctas) {
+            send(r.box(4 * r.rank), r.mail(), lane, static_cast<unsigned long long>(__double_as_longlong(rest)));
+            send(r.box(4 * r.rank + 1), r.mail(), lane, static_cast<unsigned>(n));
+        }
+        const unsigned long long* got = r.box(0);
+        r.receive();
+        const bool on = lane < r.ctas;
+        const int theirs = on ? static_cast<int>(got[4 * lane + 1]) : 0, total = __reduce_add_sync(kFull, theirs);
+        const int base = __reduce_add_sync(kFull, lane < r.rank ? theirs : 0);
+        rest = warp_sum(on ? __longlong_as_double(static_cast<long long>(got[4 * lane])) : 0.0);
+        if (lane == 0) {
+            const bool all_there = rule.top_k == 0 || total >= min(rule.top_k, s.known.n_all) ||
+                                   (rule.log_min_p > -INFINITY && least == static_cast<int>(r.unit_of(floor)));
+            s.again = total > kList || !all_there || (by_mass && s.known.whole - rest < rule.top_p * s.known.whole);
+            s.known.total = total;
+            s.known.base = base;
+            s.known.rest = rest;
+        }
+    }
+    __syncthreads();
+    r.turn = 2;
+    if (s.again) {
+        if (r.rank == 0 && tid == 0) a.token[row] = kUnlisted;
+        return;
+    }
+    const int total = s.known.total, n = s.n_listed;
+    if (r.rank == 0) r.expect(total);
+    for (int i = tid; i < n; i += kThreads) send(&sp.list[s.known.base + i], r.mail(), 0, sp.stage[i]);
+    if (r.rank != 0) return;
+    if (warp == 0) r.receive();
+    __syncthreads();
+    sort_items(sp.list, total);
+    constexpr int kEach = kList / kThreads;
+    // masses in units of the largest entry's
+    const double others = s.known.rest * exp2(static_cast<double>(unit) - static_cast<double>(top) * static_cast<double>(r.c));
+    const int limit = rule.top_k > 0 ? min(rule.top_k, total) : total, i0 = kEach * tid;
+    r.top = top;
+    // Sum over the threads before this one, and over all (`into`: a place for the warps' sums that no other sum uses).
+    auto prefix = [&](double v, double* into, double* all) {
+        const double run = warp_scan(v, lane);
+        if (lane == 31) into[warp] = run;
+        __syncthreads();
+        const double w = warp_scan(lane < kWarps ? into[lane] : 0.0, lane), before = __shfl_sync(kFull, w, warp ? warp - 1 : 0);
+        *all = __shfl_sync(kFull, w, kWarps - 1);
+        return (warp ? before : 0.0) + (run - v);
+    };
+    double e[kEach], sum = 0.0, all = 0.0, listed = 0.0;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) {
+        e[h] = i0 + h < total ? r.template weight<true>(value_of(~static_cast<unsigned>(sp.list[i0 + h] >> 32)), 0) : 0.0;
+        if (i0 + h > 0) listed += e[h];
+        if (i0 + h < limit) sum += e[h];
+    }
+    const double before = prefix(sum, s.scan_a, &all);
+    prefix(listed, s.scan_b, &listed);
+    int kept = 0;
+    bool close = false;
+    const double whole = by_mass ? 1.0 + (others + listed) : all, target = rule.top_p * whole, bound = by_mass ? kSlackFast * whole : 0.0;
+    double at = before;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) {
+        if (i0 + h >= limit) continue;
+        kept += rule.top_p >= 1.0 || at < target;
+        close |= by_mass && fabs(at - target) <= bound && i0 + h > 0;
+        at += e[h];
+    }
+    kept = __reduce_add_sync(kFull, kept);
+    if (lane == 0) s.warp_n[warp] = kept;
+    close |= by_mass && !(all >= target + bound);
+    if (__syncthreads_or(close)) {
+        if (tid == 0) a.token[row] = kUnlisted;
+        return;
+    }
+    kept = __reduce_add_sync(kFull, lane < kWarps ? s.warp_n[lane] : 0);
+    kept = kept > 0 ? kept : 1;                                   // (rounding does not take the first one)
+    // the kept ones by index
+    for (int i = tid; i < kept; i += kThreads) {
+        const unsigned long long item = sp.list[i];
+        sp.stage[i] = item << 32 | item >> 32;
+    }
+    double others_kept = 0.0;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h)
+        if (i0 + h > 0 && i0 + h < kept) others_kept += e[h];
+    prefix(others_kept, s.scan_a, &others_kept);
+    __syncthreads();
+    sort_items(sp.stage, kept);
+    sum = 0.0;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) {
+        e[h] = i0 + h < kept ? r.template weight<true>(value_of(~static_cast<unsigned>(sp.stage[i0 + h])), 0) : 0.0;
+        sum += e[h];
+    }
+    // the first one whose running mass is above the target, or, where rounding leaves none, the last with any
+    at = prefix(sum, s.scan_b, &all);
+    const double want = static_cast<double>(u) * all;
+    int mine = kList;
+    int last = -1;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) {
+        at += e[h];
+        if (e[h] > 0.0) {
+            last = i0 + h;
+            if (at > want && mine == kList) mine = i0 + h;
+        }
+    }
+    mine = __reduce_min_sync(kFull, mine);
+    last = __reduce_max_sync(kFull, last);
+    if (lane == 0) { s.warp_i[warp] = mine; s.warp_n[warp] = last; }
+    __syncthreads();
+    if (warp != 0) return;
+    mine = __reduce_min_sync(kFull, lane < kWarps ? s.warp_i[lane] : kList);
+    last = __reduce_max_sync(kFull, lane < kWarps ? s.warp_n[lane] : -1);
+    if (lane == 0) {
+        const unsigned long long item = sp.stage[mine < kList ? mine : last];
+        const float z = value_of(~static_cast<unsigned>(item));
+        const double x = (static_cast<double>(z) - static_cast<double>(top)) * r.inv_t;
+        put_row(a, row, static_cast<int>(item >> 32), x - log1p(others + listed), x - log1p(others_kept), kept);
+    }
+}
+
+// LIST: there are rules that cut entries off.
+template <typename T, bool LIST>
 __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_constant__ SampleArgs a, int run, int ctas) {
     __shared__ StreamShared s;
     const int rank = ctas > 1 ? ptx::cluster_ctarank() : 0, row = blockIdx.x / ctas;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     SampleRule rule;
     float u;
-    if (!row_begins(a, row, rank, rule, u) || rule.search) return;            // (the same in every block of the cluster)
+    if (!row_begins(a, row, rank, rule, u) || (LIST ? rule.search && !rule.list : rule.search)) return;   // (the same in every block of the cluster)
     const T* src = static_cast<const T*>(a.logits) + row * a.ld;
     Stream<T> r{s, src, ctas, rank, run, a.V, reinterpret_cast<uintptr_t>(src) % 16 == 0, a.status, 0};
     const int begin = r.begin(warp), end = min(a.V, begin + run), tiles = r.tiles(warp);
@@ -1240,6 +1528,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
         ptx::mbar_init(&s.mail[1], 1);
         ptx::fence_barrier_init();
     }
+    if (LIST && threadIdx.x < kBins) s.bins[threadIdx.x] = 0;
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // the block has begun and can take messages
     const bool greedy = rule.temperature == 0.f;
@@ -1305,6 +1594,12 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // before the first message
     __syncthreads();
+    if constexpr (LIST) {
+        if (rule.search) {
+            list_row(r, a, row, rule, u, tiles);
+            return;
+        }
+    }
     if (warp == 0) {
         const auto f = r.template locate<false>(u);
         int again = 0;
@@ -1380,8 +1675,11 @@ cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes,
 
 }  // namespace
 
-cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_other, int sm_count, cudaStream_t st, int* n_launches) {
-    if (any_other) {
+constexpr int kListRows = 1;
+
+cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_list, bool any_other, int sm_count, cudaStream_t st, int* n_launches) {
+    const bool list = any_list && a.n_rows >= kListRows;
+    if (list || any_other) {
         // A warp's run of entries: up to 20 tiles.  More blocks per row while a run is longer than a tile and the rows do not fill the
         // machine several times over: a block ends with a phase of one warp, which others have to cover (512 rows of 151936, 2 / 4 / 8 / 16
         // blocks per row: fp32 99 / 90 / 85 / 130 us, bf16 63 / 60 / 76 / 128 us).
@@ -1392,7 +1690,9 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool 
             if (ctas == kMaxCluster) break;
             if (run <= kMaxTiles * kTileEntries && (run <= kTileEntries || static_cast<long long>(a.n_rows) * ctas >= enough)) break;
         }
-        const cudaError_t e = launch_clusters(bf16 ? k_sample_stream<__nv_bfloat16> : k_sample_stream<float>, a.n_rows, ctas, 0, st, a, run, ctas);
+        const cudaError_t e = launch_clusters(list ? bf16 ? k_sample_stream<__nv_bfloat16, true> : k_sample_stream<float, true>
+                                                   : bf16 ? k_sample_stream<__nv_bfloat16, false> : k_sample_stream<float, false>,
+                                              a.n_rows, ctas, 0, st, a, run, ctas);
         if (e != cudaSuccess) return e;
         *n_launches += 1;
     }
@@ -1408,7 +1708,7 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool 
             if (ctas == kMaxCluster) break;
             if (static_cast<long long>(per) * kThreads * width <= 40 * 1024 && (per <= 16 || static_cast<long long>(a.n_rows) * ctas >= 4 * sm_count)) break;
         }
-        const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, ctas, per * kThreads * width, st, a, per, ctas);
+        const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, ctas, per * kThreads * width, st, a, per, ctas, list ? 1 : 0);
         if (e != cudaSuccess) return e;
         *n_launches += 1;
     }

@@ -1933,7 +1933,7 @@ int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, 
     if (reinterpret_cast<uintptr_t>(logits) % (logits_type == UNITY_BF16 ? 2 : 4)) return fail(ctx, UNITY_ERR_ALIGNMENT, "logits not aligned to their type");
     SampleArgs a;
     memset(&a, 0, sizeof(a));
-    bool any_search = false, any_other = false;
+    bool any_search = false, any_list = false, any_other = false;
     for (int v = 0; v < n_roles; ++v) {
         const unity_sampling_rule& r = rules[v];
         if (!(r.temperature == 0.f || (r.temperature >= 1e-6f && r.temperature <= 1e6f)))
@@ -1948,6 +1948,8 @@ int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, 
         s.quantile = normal_quantile(s.top_p);
         s.log_min_p = r.min_p > 0.f ? log(static_cast<double>(r.min_p)) : -INFINITY;
         s.search = r.temperature > 0.f && (s.top_k > 0 || r.top_p < 1.f || r.min_p > 0.f);
+        s.list = s.search && s.top_k <= kSampleListK;
+        any_list |= s.list != 0;
         (s.search ? any_search : any_other) = true;
     }
     if (n_rows == 0) return UNITY_OK;
@@ -1957,7 +1959,7 @@ int unity_sample(unity_ctx* ctx, int32_t n_rows, int32_t V, const void* logits, 
     const DeviceGuard dev(ctx->device);
     if (!dev.ok) return fail(ctx, UNITY_ERR_CUDA, "cudaSetDevice(%d) failed", ctx->device);
     int nl = 0;
-    CUDA_TRY(ctx, launch_sample(a, logits_type == UNITY_BF16, any_search, any_other, ctx->sm_count, ctx->stream, &nl));
+    CUDA_TRY(ctx, launch_sample(a, logits_type == UNITY_BF16, any_search, any_list, any_other, ctx->sm_count, ctx->stream, &nl));
     ctx->launches += nl;
     return UNITY_OK;
 }
