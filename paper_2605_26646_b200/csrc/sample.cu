@@ -240,6 +240,106 @@ __device__ __forceinline__ float lowest_allowed(const SampleRule& rule, float to
     return floor;
 }
 
+// One pass over a thread's entries: mass of all, and with TAU masses and numbers of those >= tau[k].  fp32: two sums side by side (packed
+// arithmetic), each of four entries added pairwise, those in two parts.  `moments`: sums of e x and e x^2 (octaves).
+template <typename T, bool TAU, bool MOMENTS>
+__device__ __forceinline__ Tally weigh_fast(const T* z, int per, float c, float top_c, float tau0, float tau1, float2* moments) {
+    Tally v = {};
+    float mean = 0.f, square = 0.f;
+    const float tau[kTau] = {tau0, tau1};
+    const uint64_t c2 = ptx::pack2(c, c), top2 = ptx::pack2(-top_c, -top_c), minus = ptx::pack2(-1.f, -1.f);
+    uint64_t hi[kTau + 1] = {}, low[kTau + 1] = {};
+    for (int j0 = 0; j0 < per; j0 += 8) {
+        float x[8], e[8];
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) {
+            const float2 two = j0 + q < per ? pair(z + j0 + q) : make_float2(-INFINITY, -INFINITY);
+            x[q] = two.x;
+            x[q + 1] = two.y;
+        }
+        if constexpr (TAU) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+#pragma unroll
+                for (int k = 0; k < kTau; ++k) v.c[k] += x[q] >= tau[k];
+        }
+#pragma unroll
+        for (int q = 0; q < 8; q += 2) {
+            float a, b;
+            ptx::unpack2(ptx::fma2(ptx::pack2(x[q], x[q + 1]), c2, top2), a, b);
+            e[q] = ptx::ex2(a);
+            e[q + 1] = ptx::ex2(b);
+            if (MOMENTS) {
+                a = fmaxf(a, -1e3f);
+                b = fmaxf(b, -1e3f);
+                mean += e[q] * a + e[q + 1] * b;
+                square += e[q] * a * a + e[q + 1] * b * b;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
+            uint64_t f[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float t = k ? tau[k - 1] : 0.f;
+                f[q] = ptx::pack2(!k || x[2 * q] >= t ? e[2 * q] : 0.f, !k || x[2 * q + 1] >= t ? e[2 * q + 1] : 0.f);
+            }
+            const uint64_t sum = ptx::add2(ptx::add2(f[0], f[1]), ptx::add2(f[2], f[3])), next = ptx::add2(hi[k], sum);
+            const uint64_t part = ptx::fma2(hi[k], minus, next);                           // next - hi
+            const uint64_t lost = ptx::fma2(ptx::fma2(part, minus, next), minus, hi[k]);   // hi - (next - part)
+            low[k] = ptx::add2(low[k], ptx::add2(lost, ptx::fma2(part, minus, sum)));
+            hi[k] = next;
+        }
+    }
+    if (MOMENTS) *moments = make_float2(mean, square);
+#pragma unroll
+    for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
+        float a, b, d, f;
+        ptx::unpack2(hi[k], a, b);
+        ptx::unpack2(low[k], d, f);
+        (k ? v.m[k ? k - 1 : 0] : v.whole) = (static_cast<double>(a) + static_cast<double>(b)) + (static_cast<double>(d) + static_cast<double>(f));
+    }
+    return v;
+}
+// The same in fp64.
+template <typename T, bool TAU>
+__device__ __forceinline__ Tally weigh_slow(const T* z, int per, float top, double c64, const double* table, float tau0, float tau1) {
+    Tally v = {};
+    const float tau[kTau] = {tau0, tau1};
+    for (int j0 = 0; j0 < per; j0 += 4) {
+        float x[4];
+        double w[4];
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+            const float2 two = j0 + q < per ? pair(z + j0 + q) : make_float2(-INFINITY, -INFINITY);
+            x[q] = two.x;
+            x[q + 1] = two.y;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) w[q] = slow_weight(x[q], top, c64, table);
+        v.whole += (w[0] + w[1]) + (w[2] + w[3]);
+        if constexpr (TAU) {
+#pragma unroll
+            for (int k = 0; k < kTau; ++k)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v.c[k] += x[q] >= tau[k];
+                    v.m[k] += x[q] >= tau[k] ? w[q] : 0.0;
+                }
+        }
+    }
+    return v;
+}
+// As functions of their own, where much else is live: what a caller holds is put away once, not in the loop.
+template <typename T>
+__device__ __noinline__ Tally weigh_fast_apart(const T* z, int per, float c, float top_c, float tau0, float tau1) {
+    return weigh_fast<T, true, false>(z, per, c, top_c, tau0, tau1, nullptr);
+}
+template <typename T, bool TAU>
+__device__ __noinline__ Tally weigh_slow_apart(const T* z, int per, float top, double c64, const double* table, float tau0, float tau1) {
+    return weigh_slow<T, TAU>(z, per, top, c64, table, tau0, tau1);
+}
+
 template <typename T>
 struct Row {
     Shared& s;
@@ -323,84 +423,11 @@ struct Row {
         return v;
     }
 
-    // One pass: mass of all entries, masses and numbers of those >= tau[k].  fp32: two sums side by side (packed arithmetic), each of
-    // four entries added pairwise, those in two parts.
-    // `moments`: sums of e x and e x^2 (octaves).
     template <bool EXACT, bool TAU, bool MOMENTS = false>
     __device__ __forceinline__ Tally weigh(const float (&tau)[kTau], float2* moments = nullptr) const {
-        Tally v = {};
-        float mean = 0.f, square = 0.f;
-        const uint64_t c2 = ptx::pack2(c, c), top2 = ptx::pack2(-top_c, -top_c), minus = ptx::pack2(-1.f, -1.f);
-        uint64_t hi[kTau + 1] = {}, low[kTau + 1] = {};
-        for (int j0 = 0; j0 < per; j0 += 8) {
-            float x[8], e[8];
-#pragma unroll
-            for (int q = 0; q < 8; q += 2) {
-                const float2 two = j0 + q < per ? pair(z + j0 + q) : make_float2(-INFINITY, -INFINITY);
-                x[q] = two.x;
-                x[q + 1] = two.y;
-            }
-            if constexpr (TAU) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-#pragma unroll
-                    for (int k = 0; k < kTau; ++k) v.c[k] += x[q] >= tau[k];
-            }
-            if constexpr (EXACT) {
-#pragma unroll
-                for (int h = 0; h < 8; h += 4) {
-                    double w[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) w[q] = slow(x[h + q]);
-                    v.whole += (w[0] + w[1]) + (w[2] + w[3]);
-                    if constexpr (TAU) {
-#pragma unroll
-                        for (int k = 0; k < kTau; ++k)
-#pragma unroll
-                            for (int q = 0; q < 4; ++q) v.m[k] += x[h + q] >= tau[k] ? w[q] : 0.0;
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < 8; q += 2) {
-                    float a, b;
-                    ptx::unpack2(ptx::fma2(ptx::pack2(x[q], x[q + 1]), c2, top2), a, b);
-                    e[q] = ptx::ex2(a);
-                    e[q + 1] = ptx::ex2(b);
-                    if (MOMENTS) {
-                        a = fmaxf(a, -1e3f);
-                        b = fmaxf(b, -1e3f);
-                        mean += e[q] * a + e[q + 1] * b;
-                        square += e[q] * a * a + e[q + 1] * b * b;
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
-                    uint64_t f[4];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float t = k ? tau[k - 1] : 0.f;
-                        f[q] = ptx::pack2(!k || x[2 * q] >= t ? e[2 * q] : 0.f, !k || x[2 * q + 1] >= t ? e[2 * q + 1] : 0.f);
-                    }
-                    const uint64_t sum = ptx::add2(ptx::add2(f[0], f[1]), ptx::add2(f[2], f[3])), next = ptx::add2(hi[k], sum);
-                    const uint64_t part = ptx::fma2(hi[k], minus, next);                       // next - hi
-                    const uint64_t lost = ptx::fma2(ptx::fma2(part, minus, next), minus, hi[k]);   // hi - (next - part)
-                    low[k] = ptx::add2(low[k], ptx::add2(lost, ptx::fma2(part, minus, sum)));
-                    hi[k] = next;
-                }
-            }
-        }
-        if (MOMENTS) *moments = make_float2(mean, square);
-        if (!EXACT) {
-#pragma unroll
-            for (int k = 0; k <= (TAU ? kTau : 0); ++k) {
-                float a, b, d, f;
-                ptx::unpack2(hi[k], a, b);
-                ptx::unpack2(low[k], d, f);
-                (k ? v.m[k ? k - 1 : 0] : v.whole) = (static_cast<double>(a) + static_cast<double>(b)) + (static_cast<double>(d) + static_cast<double>(f));
-            }
-        }
-        return v;
+        if constexpr (EXACT) return weigh_slow_apart<T, TAU>(z, per, top, c64, s.exp2_table, tau[0], tau[1]);
+        else if constexpr (TAU) return weigh_fast_apart<T>(z, per, c, top_c, tau[0], tau[1]);
+        else return weigh_fast<T, false, MOMENTS>(z, per, c, top_c, 0.f, 0.f, moments);
     }
 
     // A logit that about `want` entries or a few more reach: of every block its share of them is counted among its threads' largest
