@@ -18,6 +18,8 @@
 //
 // What bounds it: latency for few rows (one of 152064: 14 us, some ten exchanges of about 1.2 thousand clocks), issue slots for many
 // (512 rows of 151936 fp32: top-p of ten thousand tokens 900 us; the row's bytes would take 48).
+#include <algorithm>
+
 #include "internal.h"
 #include "ptx.cuh"
 
@@ -868,8 +870,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     SampleRule rule;
     float u;
+    if (listed && a.token[row] != kUnlisted) return;                          // (no block writes before it hears from all of the cluster)
     if (!row_begins(a, row, rank, rule, u) || !rule.search) return;           // (the same in every block of the cluster)
-    if (listed && rule.list && a.token[row] != kUnlisted) return;             // (nor does one write before it hears from all of them)
     if (threadIdx.x == 0) {
         ptx::mbar_init(&s.bar, 1);
         ptx::mbar_init(&s.mail[0], 1);
@@ -1290,7 +1292,7 @@ __device__ __forceinline__ void list_row(Stream<T>& r, const SampleArgs& a, int 
         const unsigned below = static_cast<unsigned>(block_unit - static_cast<int>(m.y));   // (a block's NaN or inf has no unit: too large)
         if (m.x > 0.f && below < kBins) atomicAdd(&s.bins[below], 1);
     }
-    if (warp == 0) s.exp2_table[lane] = exp2(lane / 32.0);
+    if (r.rank == 0 && warp == 1) s.exp2_table[lane] = exp2(lane / 32.0);
     __syncthreads();
     if (warp == 0) {
         // the octave that the block's share of the wanted number reaches
@@ -1443,11 +1445,10 @@ __device__ __forceinline__ void list_row(Stream<T>& r, const SampleArgs& a, int 
     if (r.rank != 0) return;
     if (warp == 0) r.receive();
     __syncthreads();
-    sort_items(sp.list, total);
-    constexpr int kEach = kList / kThreads;
     // masses in units of the largest entry's
     const double others = s.known.rest * exp2(static_cast<double>(unit) - static_cast<double>(top) * static_cast<double>(r.c));
-    const int limit = rule.top_k > 0 ? min(rule.top_k, total) : total, i0 = kEach * tid;
+    constexpr int kEach = kList / kThreads;
+    const int i0 = kEach * tid;
     r.top = top;
     // Sum over the threads before this one, and over all (`into`: a place for the warps' sums that no other sum uses).
     auto prefix = [&](double v, double* into, double* all) {
@@ -1459,54 +1460,69 @@ __device__ __forceinline__ void list_row(Stream<T>& r, const SampleArgs& a, int 
         return (warp ? before : 0.0) + (run - v);
     };
     double e[kEach], sum = 0.0, all = 0.0, listed = 0.0;
+    int kept = total;
+    if (rule.top_k > 0 || rule.top_p < 1.0) {
+        sort_items(sp.list, total);
+        const int limit = rule.top_k > 0 ? min(rule.top_k, total) : total;
 #pragma unroll
-    for (int h = 0; h < kEach; ++h) {
-        e[h] = i0 + h < total ? r.template weight<true>(value_of(~static_cast<unsigned>(sp.list[i0 + h] >> 32)), 0) : 0.0;
-        if (i0 + h > 0) listed += e[h];
-        if (i0 + h < limit) sum += e[h];
-    }
-    const double before = prefix(sum, s.scan_a, &all);
-    prefix(listed, s.scan_b, &listed);
-    int kept = 0;
-    bool close = false;
-    const double whole = by_mass ? 1.0 + (others + listed) : all, target = rule.top_p * whole, bound = by_mass ? kSlackFast * whole : 0.0;
-    double at = before;
+        for (int h = 0; h < kEach; ++h) {
+            e[h] = i0 + h < total ? r.template weight<true>(value_of(~static_cast<unsigned>(sp.list[i0 + h] >> 32)), 0) : 0.0;
+            if (i0 + h < limit) sum += e[h];
+        }
+        const double before = prefix(sum, s.scan_a, &all);
+        bool close = false;
+        const double whole = by_mass ? others + all : all, target = rule.top_p * whole, bound = by_mass ? kSlackFast * whole : 0.0;
+        double at = before;
+        kept = 0;
 #pragma unroll
-    for (int h = 0; h < kEach; ++h) {
-        if (i0 + h >= limit) continue;
-        kept += rule.top_p >= 1.0 || at < target;
-        close |= by_mass && fabs(at - target) <= bound && i0 + h > 0;
-        at += e[h];
+        for (int h = 0; h < kEach; ++h) {
+            if (i0 + h >= limit) continue;
+            const bool in = rule.top_p >= 1.0 || at < target || i0 + h == 0;      // (rounding does not take the first one)
+            kept += in;
+            close |= by_mass && fabs(at - target) <= bound && i0 + h > 0;
+            at += e[h];
+        }
+        kept = __reduce_add_sync(kFull, kept);
+        if (lane == 0) s.warp_n[warp] = kept;
+        close |= by_mass && !(all >= target + bound);
+        if (__syncthreads_or(close)) {
+            if (tid == 0) a.token[row] = kUnlisted;
+            return;
+        }
+        kept = __reduce_add_sync(kFull, lane < kWarps ? s.warp_n[lane] : 0);
+        // mass of the listed ones that are not kept
+#pragma unroll
+        for (int h = 0; h < kEach; ++h)
+            if (i0 + h >= kept) listed += e[h];
+        prefix(listed, s.scan_b, &listed);
     }
-    kept = __reduce_add_sync(kFull, kept);
-    if (lane == 0) s.warp_n[warp] = kept;
-    close |= by_mass && !(all >= target + bound);
-    if (__syncthreads_or(close)) {
-        if (tid == 0) a.token[row] = kUnlisted;
-        return;
-    }
-    kept = __reduce_add_sync(kFull, lane < kWarps ? s.warp_n[lane] : 0);
-    kept = kept > 0 ? kept : 1;                                   // (rounding does not take the first one)
     // the kept ones by index
     for (int i = tid; i < kept; i += kThreads) {
         const unsigned long long item = sp.list[i];
         sp.stage[i] = item << 32 | item >> 32;
     }
-    double others_kept = 0.0;
-#pragma unroll
-    for (int h = 0; h < kEach; ++h)
-        if (i0 + h > 0 && i0 + h < kept) others_kept += e[h];
-    prefix(others_kept, s.scan_a, &others_kept);
     __syncthreads();
     sort_items(sp.stage, kept);
+    // the largest entry stands apart: it may have nearly all of the mass
+    const unsigned most = ~key_of(top);
+    double others_kept = 0.0;
     sum = 0.0;
 #pragma unroll
     for (int h = 0; h < kEach; ++h) {
-        e[h] = i0 + h < kept ? r.template weight<true>(value_of(~static_cast<unsigned>(sp.stage[i0 + h])), 0) : 0.0;
+        const unsigned key = i0 + h < kept ? static_cast<unsigned>(sp.stage[i0 + h]) : 0u;
+        e[h] = i0 + h < kept ? r.template weight<true>(value_of(~key), 0) : 0.0;
         sum += e[h];
+        others_kept += key == most ? 0.0 : e[h];
     }
+    int tops = 0;
+#pragma unroll
+    for (int h = 0; h < kEach; ++h) tops += i0 + h < kept && static_cast<unsigned>(sp.stage[i0 + h]) == most;
+    tops = __reduce_add_sync(kFull, tops);
+    if (lane == 0) s.warp_n[warp] = tops;
+    prefix(others_kept, s.scan_a, &others_kept);
+    others_kept += __reduce_add_sync(kFull, lane < kWarps ? s.warp_n[lane] : 0) - 1;
     // the first one whose running mass is above the target, or, where rounding leaves none, the last with any
-    at = prefix(sum, s.scan_b, &all);
+    double at = prefix(sum, s.scan_b, &all);
     const double want = static_cast<double>(u) * all;
     int mine = kList;
     int last = -1;
@@ -1529,7 +1545,7 @@ __device__ __forceinline__ void list_row(Stream<T>& r, const SampleArgs& a, int 
         const unsigned long long item = sp.stage[mine < kList ? mine : last];
         const float z = value_of(~static_cast<unsigned>(item));
         const double x = (static_cast<double>(z) - static_cast<double>(top)) * r.inv_t;
-        put_row(a, row, static_cast<int>(item >> 32), x - log1p(others + listed), x - log1p(others_kept), kept);
+        put_row(a, row, static_cast<int>(item >> 32), x - log1p(others + listed + others_kept), x - log1p(others_kept), kept);
     }
 }
 
@@ -1541,7 +1557,15 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     SampleRule rule;
     float u;
-    if (!row_begins(a, row, rank, rule, u) || (LIST ? rule.search && !rule.list : rule.search)) return;   // (the same in every block of the cluster)
+    if (!row_begins(a, row, rank, rule, u)) return;                            // (the same in every block of the cluster)
+    if constexpr (LIST) {
+        if (rule.search && !rule.list) {
+            if (rank == 0 && threadIdx.x == 0) a.token[row] = kUnlisted;
+            return;
+        }
+    } else if (rule.search) {
+        return;
+    }
     const T* src = static_cast<const T*>(a.logits) + row * a.ld;
     Stream<T> r{s, src, ctas, rank, run, a.V, reinterpret_cast<uintptr_t>(src) % 16 == 0, a.status, 0};
     const int begin = r.begin(warp), end = min(a.V, begin + run), tiles = r.tiles(warp);
@@ -1609,7 +1633,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
     float top = most;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(kFull, top, o));
-    const int top_i = greedy ? __reduce_min_sync(kFull, most == top ? at_most : 0x7fffffff) : 0;
+    const int top_i = __reduce_min_sync(kFull, most == top ? at_most : 0x7fffffff);   // (greedy's)
     n = __reduce_add_sync(kFull, n);
     if (lane == 0) {
         s.warp_m[warp] = mass;
@@ -1702,20 +1726,34 @@ cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes,
 
 }  // namespace
 
-constexpr int kListRows = 1;
-
 cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool any_list, bool any_other, int sm_count, cudaStream_t st, int* n_launches) {
-    const bool list = any_list && a.n_rows >= kListRows;
+    // The search: the fewest blocks per row (1 .. 16) whose share takes at most 40 KB, so that four blocks fit an SM; more while the rows
+    // leave some without one.
+    const int width = bf16 ? 2 : 4;
+    int search_ctas = 1, per = 0;
+    for (;; search_ctas *= 2) {
+        per = (a.V + kThreads * search_ctas - 1) / (kThreads * search_ctas);
+        // entries are read in pairs, and the threads' first ones lie an odd number of pairs apart: at different banks
+        per = ((per + 1) / 2 | 1) * 2;
+        if (search_ctas == kMaxCluster) break;
+        if (static_cast<long long>(per) * kThreads * width <= 40 * 1024 && (per <= 16 || static_cast<long long>(a.n_rows) * search_ctas >= 4 * sm_count)) break;
+    }
+    // With room for all rows at once the search alone takes less than a pass and then the search's launch (top-k of 151936 fp32, 1 / 8
+    // / 32 / 64 rows: 15 / 19 / 33 / 52 us against 20 / 23 / 31 / 28).
+    const bool list = any_list && static_cast<long long>(a.n_rows) * search_ctas > 4 * sm_count;
     if (list || any_other) {
         // A warp's run of entries: up to 20 tiles.  More blocks per row while a run is longer than a tile and the rows do not fill the
         // machine several times over: a block ends with a phase of one warp, which others have to cover (512 rows of 151936, 2 / 4 / 8 / 16
         // blocks per row: fp32 99 / 90 / 85 / 130 us, bf16 63 / 60 / 76 / 128 us).
-        const long long enough = (bf16 ? 8LL : 16LL) * sm_count;
+        // With lists a row ends with more than that: runs of up to 20 KB, and two blocks per SM are enough (top-k with top-p,
+        // blocks per row: 512 rows fp32 122 / 110 / 118 us at 2 / 4 / 8, 128 rows fp32 43 / 47 / 60 at 4 / 8 / 16, bf16 35 / 42 / 61).
+        const long long enough = (list ? 2LL : bf16 ? 8LL : 16LL) * sm_count;
+        const int longest = list ? std::min(kMaxTiles * kTileEntries, 20 * 1024 / width) : kMaxTiles * kTileEntries;
         int ctas = 1, run = 0;
         for (;; ctas *= 2) {
             run = ((a.V + kWarps * ctas - 1) / (kWarps * ctas) + 7) / 8 * 8;
             if (ctas == kMaxCluster) break;
-            if (run <= kMaxTiles * kTileEntries && (run <= kTileEntries || static_cast<long long>(a.n_rows) * ctas >= enough)) break;
+            if (run <= longest && (run <= kTileEntries || static_cast<long long>(a.n_rows) * ctas >= enough)) break;
         }
         const cudaError_t e = launch_clusters(list ? bf16 ? k_sample_stream<__nv_bfloat16, true> : k_sample_stream<float, true>
                                                    : bf16 ? k_sample_stream<__nv_bfloat16, false> : k_sample_stream<float, false>,
@@ -1724,18 +1762,8 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool 
         *n_launches += 1;
     }
     if (any_search) {
-        // the fewest blocks per row (1 .. 16) whose share takes at most 40 KB, so that four blocks fit an SM; more while the rows leave some
-        // without one
-        const int width = bf16 ? 2 : 4;
-        int ctas = 1, per = 0;
-        for (;; ctas *= 2) {
-            per = (a.V + kThreads * ctas - 1) / (kThreads * ctas);
-            // entries are read in pairs, and the threads' first ones lie an odd number of pairs apart: at different banks
-            per = ((per + 1) / 2 | 1) * 2;
-            if (ctas == kMaxCluster) break;
-            if (static_cast<long long>(per) * kThreads * width <= 40 * 1024 && (per <= 16 || static_cast<long long>(a.n_rows) * ctas >= 4 * sm_count)) break;
-        }
-        const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, ctas, per * kThreads * width, st, a, per, ctas, list ? 1 : 0);
+        const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, search_ctas, per * kThreads * width, st, a, per,
+                                              search_ctas, list ? 1 : 0);
         if (e != cudaSuccess) return e;
         *n_launches += 1;
     }
