@@ -870,7 +870,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     SampleRule rule;
     float u;
-    if (listed && a.token[row] != kUnlisted) return;                          // (no block writes before it hears from all of the cluster)
+    if (listed) {
+        ptx::grid_wait();                                                     // the pass is over
+        if (a.token[row] != kUnlisted) return;                                // (no block writes before it hears from all of the cluster)
+    }
     if (!row_begins(a, row, rank, rule, u) || !rule.search) return;           // (the same in every block of the cluster)
     if (threadIdx.x == 0) {
         ptx::mbar_init(&s.bar, 1);
@@ -1557,6 +1560,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     SampleRule rule;
     float u;
+    if constexpr (LIST) ptx::grid_launch_dependents();                         // the search behind it waits for its end
     if (!row_begins(a, row, rank, rule, u)) return;                            // (the same in every block of the cluster)
     if constexpr (LIST) {
         if (rule.search && !rule.list) {
@@ -1706,7 +1710,7 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
 }
 
 template <typename... P, typename... A>
-cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes, cudaStream_t st, const A&... args) {
+cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes, bool early, cudaStream_t st, const A&... args) {
     cudaError_t e = bytes > 0 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
     if (e == cudaSuccess && ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
@@ -1715,12 +1719,14 @@ cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes,
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = early ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -1757,12 +1763,12 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool 
         }
         const cudaError_t e = launch_clusters(list ? bf16 ? k_sample_stream<__nv_bfloat16, true> : k_sample_stream<float, true>
                                                    : bf16 ? k_sample_stream<__nv_bfloat16, false> : k_sample_stream<float, false>,
-                                              a.n_rows, ctas, 0, st, a, run, ctas);
+                                              a.n_rows, ctas, 0, false, st, a, run, ctas);
         if (e != cudaSuccess) return e;
         *n_launches += 1;
     }
     if (any_search) {
-        const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, search_ctas, per * kThreads * width, st, a, per,
+        const cudaError_t e = launch_clusters(bf16 ? k_sample<__nv_bfloat16> : k_sample<float>, a.n_rows, search_ctas, per * kThreads * width, list, st, a, per,
                                               search_ctas, list ? 1 : 0);
         if (e != cudaSuccess) return e;
         *n_launches += 1;
