@@ -259,3 +259,106 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         check(z, rules, u, None, [t.cpu().numpy() for t in o])
+
+
+# Calls whose rows the machine does not hold at once take one pass over all rows first and search only what a short list leaves open.
+@pytest.mark.parametrize("V,n,kinds", [(513, 640, KINDS), (20481, 300, KINDS), (151936, 42, ["peaked", "wide", "ties", "masked"])])
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_every_rule_in_calls_of_many_rows(V, n, kinds, dtype):
+    for kind in kinds:
+        z = logits(n, V, kind, dtype, V)
+        role = torch.arange(n, dtype=torch.int32) % len(RULES)
+        u = torch.rand(n, generator=torch.Generator().manual_seed(V)).cuda()
+        check(z, RULES, u, role, draw(z, RULES, u, role.cuda()))
+
+
+@pytest.mark.parametrize("dtype", [F32, B16])
+@pytest.mark.parametrize("left", [1, 30, 1000, 1100, 10000])
+def test_many_rows_with_most_of_the_vocabulary_masked(left, dtype):
+    n, V = 300, 20481
+    z = logits(n, V, "normal", dtype, left)
+    z[:, left:] = -float("inf")
+    z[::2] = z[::2].flip(1)
+    rules = [(1.0, 40, 1.0, 0.0), (0.7, 0, 1.0, 0.1), (1.0, 0, 0.7, 0.0), (1.0, 30, 0.9, 0.01)]
+    role = torch.arange(n, dtype=torch.int32) % 4
+    u = torch.rand(n).cuda()
+    check(z, rules, u, role, draw(z, rules, u, role.cuda()))
+
+
+def test_list_sizes_of_many_rows():
+    n, V = 300, 20481
+    z = logits(n, V, "normal", F32, 77) * 2
+    rules = [(1.0, k, p, m) for k in (1, 2, 255, 256, 383, 384, 385, 1000) for p, m in ((1.0, 0.0), (0.8, 0.0), (1.0, 0.002))] + [(1.0, 0, 1.0, 1e-5)]
+    role = torch.arange(n, dtype=torch.int32) % len(rules)
+    u = torch.rand(n).cuda()
+    check(z, rules, u, role, draw(z, rules, u, role.cuda()))
+
+
+def test_many_rows_without_a_distribution_at_odd_pitches():
+    n, V = 640, 3001
+    for ld, off, dtype in ((3001, 0, F32), (3007, 3, B16)):
+        flat = torch.full((n * ld + off,), float("nan"), dtype=dtype, device="cuda")
+        z = torch.as_strided(flat, (n, V), (ld, 1), off)
+        z.copy_(logits(n, V, "peaked", dtype, ld))
+        for i, v in ((1, float("nan")), (2, float("inf")), (3, -float("inf"))):
+            z[i::9, i * 700] = v
+        z[5::9] = -float("inf")
+        z[6::9] = float("nan")
+        mask = torch.ones(n, dtype=torch.uint8)
+        mask[7::9] = 0
+        rules = [(1.0, 20, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (1.0, 0, 1.0, 0.05), (1.0, 700, 1.0, 0.0), OFF]
+        role = torch.arange(n, dtype=torch.int32) % 5
+        u = torch.rand(n).cuda()
+        ctx = ub.Context(0, 256)
+        got = draw(z, rules, u, role.cuda(), mask.cuda(), ctx)
+        on = mask.bool()
+        check(z[on.cuda()], rules, u[on.cuda()], role[on], [g[on.numpy()] for g in got])
+        assert all((g[7::9] == w).all() for g, w in zip(got, (-1, 0, 0, 0)))
+        ctx.check_status()
+
+
+@pytest.mark.parametrize("rule", [(1.0, 40, 1.0, 0.0), (1.0, 0, 0.99, 0.0), (1.0, 0, 1.0, 1e-9), (0.5, 200, 0.99, 0.0)])
+def test_sure_tokens_of_many_rows_keep_their_digits(rule):
+    """As in calls of few rows: 7.4e-6 relative and 2^-49; here the others' mass is added up by itself."""
+    n, V = 300, 20481
+    z = logits(n, V, "normal", F32, 5)
+    z[torch.arange(n), torch.randint(0, V, (n,), generator=torch.Generator().manual_seed(V))] = torch.linspace(12, 27, n, device="cuda") + np.log(V) / 2
+    u = torch.full((n,), 0.5, device="cuda")
+    got = draw(z, [rule], u)
+    check(z, [rule], u, None, got)
+    zs = z.double().cpu().numpy()
+    for i in range(n):
+        t, lp, lk, k = orc.sample_row(zs[i], *rule, 0.5)
+        x = (zs[i] - zs[i].max()) / rule[0]
+        order = np.argsort(-zs[i], kind="stable")
+        if t != order[0]:
+            continue
+        for v, rest in ((got[1][i], np.exp(np.delete(x, t)).sum()), (got[2][i], np.exp(x[order[1:k]]).sum())):
+            assert abs(v + np.log1p(rest)) <= 7.4e-6 * np.log1p(rest) + 2.0 ** -49, (i, v, rest)
+
+
+def test_many_rows_captured_and_replayed_give_the_same_twice():
+    n, V = 640, 4097
+    st = torch.cuda.Stream()
+    ctx = ub.Context(0, 256, st)
+    z, u = logits(n, V, "peaked", B16, 5), torch.rand(n).cuda()
+    o = [torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"),
+         torch.zeros(n, dtype=torch.int32, device="cuda")]
+    role = (torch.arange(n, dtype=torch.int32) % 6)
+    dev = role.cuda()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        ctx.sample(z, RULES[:6], u, o[0], dev, None, *o[1:])
+        ctx.sample(z, RULES[:6], u, o[0], dev, None, *o[1:])
+    for seed in (6, 7):
+        z.copy_(logits(n, V, "peaked", B16, seed))
+        u.uniform_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.cpu().numpy() for t in o]
+        check(z, RULES[:6], u, role, got)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(np.array_equal(a, t.cpu().numpy()) for a, t in zip(got, o))
