@@ -1279,8 +1279,10 @@ __device__ __forceinline__ double largest_logp(const Stream<T>& r, int token, do
 // index of the row.  Where at least k groups reach an octave, at least k entries do, and all that do are in those groups.  They are
 // read again, what reaches the octave goes to a list in the first block, and that block decides, with fp64 exponentials: of top-k
 // and min-p all that counts is in the list.  top-p needs the mass of the others too; where that is too close, or the list does not
-// reach it or has no room, the row is left to the search.  512 rows of 151936, with the launch of the search behind it: fp32 top-k 133
-// us (all of it by the search 338), min-p 123 (239); bf16 97 (184) and 91 (143).
+// reach it or has no room, the row is left to the search.  512 rows of 151936, with the launch of the search behind it: fp32 top-k 108
+// us (all of it by the search 338), min-p 105 (239), top-p of a few tokens 119 (570); bf16 89 (184), 81 (143) and 95 (371).  The pass
+// alone takes 87 and 62; the rest is two exchanges and the first block's end, 8 thousand clocks of a row, and blocks of the search that
+// look at a row and end.  Both lists are sorted, so their order in memory, which atomics decide, changes nothing.
 template <typename T>
 __device__ __forceinline__ void list_row(Stream<T>& r, const SampleArgs& a, int row, const SampleRule& rule, float u, int tiles) {
     StreamShared& s = r.s;
@@ -1745,7 +1747,7 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool 
         if (static_cast<long long>(per) * kThreads * width <= 40 * 1024 && (per <= 16 || static_cast<long long>(a.n_rows) * search_ctas >= 4 * sm_count)) break;
     }
     // With room for all rows at once the search alone takes less than a pass and then the search's launch (top-k of 151936 fp32, 1 / 8
-    // / 32 / 64 rows: 15 / 19 / 33 / 52 us against 20 / 23 / 31 / 28).
+    // / 32 / 64 rows: 15 / 19 / 33 / 52 us against 20 / 23 / 31 / 27).
     const bool list = any_list && static_cast<long long>(a.n_rows) * search_ctas > 4 * sm_count;
     if (list || any_other) {
         // A warp's run of entries: up to 20 tiles.  More blocks per row while a run is longer than a tile and the rows do not fill the
