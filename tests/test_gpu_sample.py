@@ -362,3 +362,12 @@ def test_many_rows_captured_and_replayed_give_the_same_twice():
         graph.replay()
         torch.cuda.synchronize()
         assert all(np.array_equal(a, t.cpu().numpy()) for a, t in zip(got, o))
+
+
+@pytest.mark.parametrize("V", [1, 2, 7, 64])
+def test_many_rows_of_short_vocabularies(V):
+    n = 40 * len(RULES) + 41
+    z = torch.cat([logits(n // 3, V, kind, F32, V) for kind in ("normal", "ties", "masked")])
+    role = torch.arange(len(z), dtype=torch.int32) % len(RULES)
+    u = torch.rand(len(z)).cuda()
+    check(z, RULES, u, role, draw(z, RULES, u, role.cuda()))
