@@ -17,7 +17,7 @@
 // is that of 64-bit arithmetic either way.
 //
 // What bounds it: latency for few rows (one of 152064: 14 us, some ten exchanges of about 1.2 thousand clocks), issue slots for many
-// (512 rows of 151936 fp32: top-p of ten thousand tokens 900 us; the row's bytes would take 48).
+// (512 rows of 151936 fp32: top-p of thirty thousand tokens 900 us; the row's bytes would take 48).
 #include <algorithm>
 
 #include "internal.h"
