@@ -1667,8 +1667,9 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
             const double lse = (log2(f.whole) + f.unit - static_cast<double>(f.top) * (static_cast<double>(r.c) - r.c64)) * 0.69314718055994531;
             const bool fits = fabsf(f.top * r.c) <= 0x1p20f;          // (far from 0 a unit and c times a logit have no digits left to differ in)
             if (greedy) {
-                if (f.top_i / (kWarps * run) == rank) {
-                    const double logp = fits ? largest_logp(r, f.top_i, f.whole, f.unit) : static_cast<double>(f.top) - lse;
+                again = !fits;                                       // (the same in every block)
+                if (fits && f.top_i / (kWarps * run) == rank) {
+                    const double logp = largest_logp(r, f.top_i, f.whole, f.unit);
                     if (lane == 0) put_row(a, row, f.top_i, logp, 0.0, 1);
                 }
             } else {
@@ -1705,7 +1706,9 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
     __syncthreads();
     if (warp != 0) return;
     const auto f = r.template locate<true>(u);
-    if (f.token >= 0 && lane == 0) {
+    if (greedy) {
+        if (f.top_i / (kWarps * run) == rank && lane == 0) put_row(a, row, f.top_i, 0.0 - log(f.whole), 0.0, 1);
+    } else if (f.token >= 0 && lane == 0) {
         const double logp = (static_cast<double>(f.tz) - static_cast<double>(f.top)) * rule.inv_t - log(f.whole);
         put_row(a, row, f.token, logp, logp, f.n);
     }

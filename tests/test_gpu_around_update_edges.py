@@ -1,0 +1,67 @@
+"""Calls at the ends of what the norm, the clipping and the sampling accept: rows far from zero, contexts of several host threads,
+captured calls of different sizes."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_sample as ts
+from paper_2605_26646_b200 import binding as ub
+
+pytestmark = pytest.mark.gpu
+
+F32, B16 = torch.float32, torch.bfloat16
+
+
+# ------------------------------------------------------------------------------------------------
+# Rows whose largest logit is so far from zero that its share of an octave has no digits left, or none of its octaves: a mask that refuses
+# everything leaves such a row.  Tokens, numbers of kept entries and log-probabilities (tolerance of test_gpu_sample.py).
+# ------------------------------------------------------------------------------------------------
+def far_rows(V, dtype, n):
+    """n rows, one kind after another."""
+    lowest, largest = torch.finfo(dtype).min, torch.finfo(dtype).max
+    g = torch.Generator(device="cuda").manual_seed(V)
+    rows = []
+    for i in range(n):
+        kind = i % 9
+        if kind < 5:
+            row = torch.full((V,), (-1e9, lowest, 1e9, largest, -1e30)[kind], device="cuda")
+        elif kind == 5:                                              # some entries are not allowed at all
+            row = torch.full((V,), lowest, device="cuda")
+            row[torch.rand(V, generator=g, device="cuda") < 0.3] = -float("inf")
+            row[V // 2] = lowest
+        elif kind == 6:                                              # the largest stands alone
+            row = torch.full((V,), -1e9, device="cuda")
+            row[V // 3] = 1e9
+        elif kind == 7:                                              # a few equal ones above ordinary logits
+            row = torch.randn(V, generator=g, device="cuda") * 3
+            row[::1 + V // 3] = 2e9
+        else:                                                        # neighbours of one another around 2^20 octaves
+            row = 726817.0 + torch.randn(V, generator=g, device="cuda").mul_(3).round_()
+        rows.append(row)
+    return torch.stack(rows).to(dtype)
+
+
+@pytest.mark.parametrize("V,n", [(1, 27), (7, 27), (64, 700), (513, 27), (20481, 18), (20481, 297), (151936, 9), (262144, 9), (151936, 45)])
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_greedy_rows_far_from_zero(V, n, dtype):
+    z = far_rows(V, dtype, n)
+    u = torch.rand(n, generator=torch.Generator().manual_seed(n)).cuda()
+    ctx = ub.Context(0, 256)
+    rule = (0.0, 0, 1.0, 0.0)
+    got = ts.draw(z, [rule], u, None, None, ctx)
+    assert np.all(got[2] == 0) and np.all(got[3] == 1)
+    ts.check(z, [rule], u, None, got)
+    ctx.check_status()
+
+
+@pytest.mark.parametrize("V,n", [(7, 72), (513, 72), (20481, 72), (20481, 297), (151936, 36)])
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_every_rule_on_rows_far_from_zero(V, n, dtype):
+    rules = [(0.0, 0, 1.0, 0.0), ts.OFF, (0.7, 20, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (1.3, 0, 1.0, 0.02), (1.0, 700, 0.5, 0.0), (1e-6, 0, 0.9, 0.0),
+             (1e6, 5, 1.0, 0.1)]
+    z = far_rows(V, dtype, n)
+    role = torch.arange(n, dtype=torch.int32) // 9 % len(rules)
+    u = torch.rand(n, generator=torch.Generator().manual_seed(n)).cuda()
+    ctx = ub.Context(0, 256)
+    ts.check(z, rules, u, role, ts.draw(z, rules, u, role.cuda(), None, ctx))
+    ctx.check_status()
