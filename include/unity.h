@@ -491,7 +491,8 @@ int unity_distill_fwd_bwd(unity_ctx* ctx, const unity_rows* rows, const unity_di
  *   res        : r, as res_out has it (or x, in bf16, where there was no residual);  dres : or NULL
  *   dgamma     : (host) K different device pointers, each f32 [H], or NULL (a frozen norm); accumulate: 1 adds to them
  * Limits: H % 64 == 0, 64 <= H <= UNITY_MAX_NORM_H; rows densely packed, every pointer 16-byte aligned.  y may be x, res_out may be
- * residual, dx may be res, dres or (bf16) dy; other overlaps are not allowed.  The sum of a row's squares must lie within fp32.
+ * residual, dx may be res, dres or (bf16) dy; other overlaps are not allowed.  The sum of a row's squares must lie within fp32, in the
+ * backward that of its g r too; their powers and products need not.
  * Rows with tok_mask == 0 are not read and have zeros in y, res_out and dx; an out-of-range role flags UNITY_ERR_BAD_INDEX and its
  * tokens count as masked.  The forward needs no workspace, the backward with dgamma unity_rms_norm_workspace_bytes(), with less it
  * runs on fewer blocks (other last digits of dgamma).  Deterministic: every sum has a fixed order. */

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import test_gpu_norm as tn
 import test_gpu_sample as ts
 from paper_2605_26646_b200 import binding as ub
 
@@ -64,4 +65,24 @@ def test_every_rule_on_rows_far_from_zero(V, n, dtype):
     u = torch.rand(n, generator=torch.Generator().manual_seed(n)).cuda()
     ctx = ub.Context(0, 256)
     ts.check(z, rules, u, role, ts.draw(z, rules, u, role.cuda(), None, ctx))
+    ctx.check_status()
+
+
+# ------------------------------------------------------------------------------------------------
+# Norm backward: s and its powers lie far from 1, all that the definition gives lies within fp32 (tolerances of test_gpu_norm.py).
+# ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("H", [64, 896, 3584])
+@pytest.mark.parametrize("res", [F32, B16])
+@pytest.mark.parametrize("x_scale,eps", [(2e16, 1e-6), (2e16, 0.0), (1e13, 1e-6), (1e8, 0.0), (1e-9, 0.0), (1e-14, 0.0), (1e-17, 0.0), (1e-14, 1e-30)])
+@pytest.mark.parametrize("dy_scale", [1.0, 1e-8])
+def test_backward_of_large_and_of_tiny_rows(H, res, x_scale, eps, dy_scale):
+    n = 40
+    p = tn.Rows(n, H, K=2, n_inv=5, res=res, gamma=F32, seed=H, x_scale=x_scale)
+    p.eps = eps
+    p.dy = (p.dy.float() * dy_scale).to(B16)
+    ctx = ub.Context(0, ub.unity_rms_norm_workspace_bytes(n, H, 2))
+    dx, dg = tn.junk((n, H), res), [tn.junk((H,), F32) for _ in range(2)]
+    ctx.rms_norm_bwd(p.res.cuda(), *p.head(), p.dy.cuda(), dx, None, dg)
+    assert torch.isfinite(dx.float()).all()
+    tn.check_bwd(p, p.res, dx, dg, False)
     ctx.check_status()
