@@ -464,11 +464,13 @@ cudaError_t fwd_rows(const NormArgs& a, cudaStream_t st) {
 }
 // The ring's depth and what it holds: as many rows as leave room for two blocks on an SM, or for one; a row's dres stays outside
 // where two rows with it do not fit.
+constexpr int kMaxRing = 220 * 1024;
+static_assert(2 * UNITY_MAX_NORM_H * (4 + 2) <= kMaxRing, "two rows without dres");
 struct Ring { int stages, dres, bytes; };
 Ring ring_of(const NormArgs& a) {
     const int width = a.res_bf16 ? 2 : 4;
     Ring r;
-    r.dres = a.dres != nullptr && 2 * a.H * (2 * width + 2) <= 220 * 1024;
+    r.dres = a.dres != nullptr && 2 * a.H * (2 * width + 2) <= kMaxRing;
     const int stage = a.H * (width + 2 + (r.dres ? width : 0));
     r.stages = 110 * 1024 / stage;
     r.stages = r.stages < 2 ? 2 : r.stages > kMaxStages ? kMaxStages : r.stages;
@@ -479,7 +481,9 @@ template <int WPR, int NV, typename R, bool DG>
 cudaError_t bwd_launch(const NormArgs& a, int grid, cudaStream_t st) {
     const Ring r = ring_of(a);
     if (r.bytes > 47 * 1024) {                                    // (what a block has without asking)
-        const cudaError_t e = cudaFuncSetAttribute(k_norm_bwd<WPR, NV, R, DG>, cudaFuncAttributeMaxDynamicSharedMemorySize, r.bytes);
+        // The limit belongs to the function, whichever contexts and host threads launch it: always that of the largest ring, so that no
+        // call takes away what another is about to use.
+        const cudaError_t e = cudaFuncSetAttribute(k_norm_bwd<WPR, NV, R, DG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing);
         if (e != cudaSuccess) return e;
     }
     return launch(k_norm_bwd<WPR, NV, R, DG>, grid, 32 * WPR, r.bytes, st, a, r.stages, r.dres);

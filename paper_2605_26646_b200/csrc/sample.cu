@@ -1714,9 +1714,18 @@ __global__ void __launch_bounds__(kThreads, 5) k_sample_stream(const __grid_cons
     }
 }
 
+// The search's entries of a thread with so many blocks per row.  They are read in pairs, and the threads' first ones lie an odd number of
+// pairs apart: at different banks.
+constexpr int entries_of_thread(int V, int ctas) { return (((V + kThreads * ctas - 1) / (kThreads * ctas) + 1) / 2 | 1) * 2; }
+constexpr int kSearchBytes = 40 * 1024;      // of a block where fewer than 16 share the row
+// The most that a block of the search asks for.
+constexpr int kMaxSearchBytes = std::max<int>(entries_of_thread(UNITY_MAX_SAMPLE_V, kMaxCluster) * kThreads * sizeof(float), kSearchBytes);
+
 template <typename... P, typename... A>
 cudaError_t launch_clusters(void (*kernel)(P...), int rows, int ctas, int bytes, bool early, cudaStream_t st, const A&... args) {
-    cudaError_t e = bytes > 0 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+    // The limit belongs to the function, whichever contexts and host threads launch it: always that of the largest call, so that no call
+    // takes away what another is about to use.
+    cudaError_t e = bytes > 0 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSearchBytes) : cudaSuccess;
     if (e == cudaSuccess && ctas > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -1743,11 +1752,9 @@ cudaError_t launch_sample(const SampleArgs& a, bool bf16, bool any_search, bool 
     const int width = bf16 ? 2 : 4;
     int search_ctas = 1, per = 0;
     for (;; search_ctas *= 2) {
-        per = (a.V + kThreads * search_ctas - 1) / (kThreads * search_ctas);
-        // entries are read in pairs, and the threads' first ones lie an odd number of pairs apart: at different banks
-        per = ((per + 1) / 2 | 1) * 2;
+        per = entries_of_thread(a.V, search_ctas);
         if (search_ctas == kMaxCluster) break;
-        if (static_cast<long long>(per) * kThreads * width <= 40 * 1024 && (per <= 16 || static_cast<long long>(a.n_rows) * search_ctas >= 4 * sm_count)) break;
+        if (static_cast<long long>(per) * kThreads * width <= kSearchBytes && (per <= 16 || static_cast<long long>(a.n_rows) * search_ctas >= 4 * sm_count)) break;
     }
     // With room for all rows at once the search alone takes less than a pass and then the search's launch (top-k of 151936 fp32, 1 / 8
     // / 32 / 64 rows: 15 / 19 / 33 / 52 us against 20 / 23 / 31 / 27).

@@ -1,5 +1,7 @@
 """Calls at the ends of what the norm, the clipping and the sampling accept: rows far from zero, contexts of several host threads,
 captured calls of different sizes."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -86,3 +88,109 @@ def test_backward_of_large_and_of_tiny_rows(H, res, x_scale, eps, dy_scale):
     assert torch.isfinite(dx.float()).all()
     tn.check_bwd(p, p.res, dx, dg, False)
     ctx.check_status()
+
+
+# ------------------------------------------------------------------------------------------------
+# Contexts of several host threads share nothing: calls of one size do not change what another's may ask for.
+# ------------------------------------------------------------------------------------------------
+def norm_bwd_call(n, H, res, dres, stream):
+    p = tn.Rows(n, H, K=2, n_inv=3, res=res, seed=n)
+    ctx = ub.Context(0, ub.unity_rms_norm_workspace_bytes(n, H, 2), stream)
+    r, head, dy, more = p.res.cuda(), p.head(), p.dy.cuda(), p.dres.cuda() if dres else None
+    dx, dg = tn.junk((n, H), res), [tn.junk((H,), F32) for _ in range(2)]
+    return ctx, lambda: ctx.rms_norm_bwd(r, *head, dy, dx, more, dg), [dx, *dg]
+
+
+def sample_call(n, V, stream):
+    ctx = ub.Context(0, 256, stream)
+    z, u = ts.logits(n, V, "peaked", F32, V), torch.rand(n, generator=torch.Generator().manual_seed(V)).cuda()
+    token, logp = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, device="cuda")
+    return ctx, lambda: ctx.sample(z, [(0.9, 40, 0.9, 0.0)], u, token, None, None, logp), [token, logp]
+
+
+PAIRS = {"norm": (lambda st: norm_bwd_call(8, 3584, F32, True, st), lambda st: norm_bwd_call(8, 3584, F32, False, st)),
+         "sample": (lambda st: sample_call(1, 152064, st), lambda st: sample_call(1, 4096, st))}
+
+
+class Tape:
+    """The library with its last call kept, so that a loop can make it again without the interpreter between two calls."""
+
+    def __init__(self, lib):
+        self.lib = lib
+
+    def __getattr__(self, name):
+        fn = getattr(self.lib, name)
+
+        def call(*args):
+            self.last = (fn, args)
+            return fn(*args)
+        return call
+
+
+@pytest.mark.parametrize("which", PAIRS)
+def test_host_threads_with_calls_of_different_sizes(which, monkeypatch):
+    """A thread's calls give the same whatever the other threads ask for, and none is refused."""
+    work, failed = [make(torch.cuda.Stream()) for make in 2 * PAIRS[which]], []
+    tape = Tape(ub.load_library())
+    monkeypatch.setattr(ub, "load_library", lambda: tape)
+    torch.cuda.synchronize()
+    want, calls = [], []
+    for _, call, out in work:
+        call()
+        torch.cuda.synchronize()
+        calls.append(tape.last)
+        want.append([t.clone() for t in out])
+        for t in out:
+            t.zero_()
+    torch.cuda.synchronize()
+    monkeypatch.undo()
+    start = threading.Barrier(len(work))
+
+    def loop(ctx, fn, args):                                         # (no interpreter in between: calls overlap)
+        start.wait(60)
+        for i in range(5000):
+            code = fn(*args)
+            if code:
+                failed.append((code, ub.load_library().unity_last_error(ctx.ctx).decode()))
+                return
+
+    threads = [threading.Thread(target=loop, args=(w[0], *c)) for w, c in zip(work, calls)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(120)
+    torch.cuda.synchronize()
+    assert not failed, failed
+    for (ctx, _, out), w in zip(work, want):
+        ctx.check_status()
+        assert all(torch.equal(a, b) for a, b in zip(out, w))
+
+
+@pytest.mark.parametrize("which", PAIRS)
+def test_a_large_call_is_captured_before_a_small_one(which):
+    st = torch.cuda.Stream()
+    work = [make(st) for make in PAIRS[which]]
+    torch.cuda.synchronize()
+    want = []
+    for _, call, out in work:
+        call()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in out])
+        for t in out:
+            t.zero_()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        for _, call, _ in work:
+            call()
+    work[1][1]()                                                     # (the smaller one comes last before the replay, too)
+    torch.cuda.synchronize()
+    for _, _, out in work:
+        for t in out:
+            t.zero_()
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    for (ctx, _, out), w in zip(work, want):
+        ctx.check_status()
+        assert all(torch.equal(a, b) for a, b in zip(out, w))
