@@ -108,12 +108,16 @@ __device__ __forceinline__ void bulk_load(void* to, const void* from, unsigned b
                  "r"(bytes), "r"(ptx::smem_u32(bar)) : "memory");
 }
 
-// Sum of a pair over the WPR warps of a row; `slots` holds two of them in turn, so that one barrier per call is enough.
+// Sum of a pair over the WPR warps of a row; `slots` holds two of them in turn, so that one barrier per call is enough.  What the row's
+// threads read of shared memory before it has been read behind it, for one warp too: shuffles alone do not order memory.
 template <int WPR>
 __device__ __forceinline__ float2 row_sum(float2 v, float2 (&slots)[2][WPR], int turn) {
     v.x = warp_sum(v.x);
     v.y = warp_sum(v.y);
-    if (WPR == 1) return v;
+    if (WPR == 1) {
+        __syncwarp();
+        return v;
+    }
     const int warp = threadIdx.x >> 5;
     if ((threadIdx.x & 31) == 0) slots[turn][warp] = v;
     __syncthreads();
@@ -359,7 +363,7 @@ __global__ void __launch_bounds__(32 * WPR) k_norm_bwd(const __grid_constant__ N
         sum.x = lo + hi;
         ptx::unpack2(dots, lo, hi);
         sum.y = lo + hi;
-        // (a barrier: every warp is through with the row before, whose place in the ring takes the next one)
+        // (a barrier: every thread is through with the row before, whose place in the ring takes the next one)
         sum = row_sum<WPR>(sum, slots, done & 1);
         if (warp == 0 && done > 0) ask();
         ++done;

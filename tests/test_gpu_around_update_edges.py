@@ -194,3 +194,37 @@ def test_a_large_call_is_captured_before_a_small_one(which):
     for (ctx, _, out), w in zip(work, want):
         ctx.check_status()
         assert all(torch.equal(a, b) for a, b in zip(out, w))
+
+
+@pytest.mark.parametrize("H", [64, 256, 448, 512])
+@pytest.mark.parametrize("res", [F32, B16])
+def test_rows_of_one_warp_take_their_places_in_the_ring_in_turn(H, res):
+    """Many rows per block, one warp each: the place of a row that was read takes the next one.  Of 12001 rows on all blocks dx against the
+    formula in 64 bits, with the tolerance of test_gpu_norm.py; 601 rows on a few blocks as there."""
+    n, K = 12001, 2
+    p = tn.Rows(n, H, K=K, n_inv=5, res=res, seed=H, mask=0.1)
+    ctx = ub.Context(0, ub.unity_rms_norm_workspace_bytes(n, H, K))
+    r, head, dy, more = p.res.cuda(), p.head(), p.dy.cuda(), p.dres.cuda()
+    dx, dg = tn.junk((n, H), res), [tn.junk((H,), F32) for _ in range(K)]
+    ctx.rms_norm_bwd(r, *head, dy, dx, more, dg)
+    role = torch.repeat_interleave(p.role.long(), p.cu[1:] - p.cu[:-1])
+    model = torch.tensor(p.role_model)[role].cuda()
+    x, g = r.double(), dy.double() * torch.stack(head[0]).double()[model]
+    s = 1 / torch.sqrt((x * x).mean(1, keepdim=True) + float(np.float32(p.eps)))
+    want = s * g - x * s ** 3 * (g * x).mean(1, keepdim=True) + more.double()
+    size = (s * g).abs() + x.abs() * s ** 3 * (g * x).abs().mean(1, keepdim=True) + more.double().abs()
+    on = (p.mask != 0).cuda().unsqueeze(1)
+    want, size = torch.where(on, want, 0.0), torch.where(on, size, 0.0)
+    tol = 256 * tn.U * size + (tn.B if res == B16 else tn.U) * want.abs() * (1 + 256 * tn.U) + 1e-38
+    assert ((dx.double() - want).abs() <= tol).all()
+    for _ in range(20):
+        dx2, dg2 = tn.junk((n, H), res), [tn.junk((H,), F32) for _ in range(K)]
+        ctx.rms_norm_bwd(r, *head, dy, dx2, more, dg2)
+        assert torch.equal(dx, dx2) and all(torch.equal(a, b) for a, b in zip(dg, dg2))
+    ctx.check_status()
+    p = tn.Rows(601, H, K=K, n_inv=5, res=res, seed=H, mask=0.1)
+    ctx = ub.Context(0, ub.unity_rms_norm_workspace_bytes(7, H, K))
+    dx = tn.junk((601, H), res)
+    ctx.rms_norm_bwd(p.res.cuda(), *p.head(), p.dy.cuda(), dx, p.dres.cuda(), dg)
+    tn.check_bwd(p, p.res, dx, None)
+    ctx.check_status()
