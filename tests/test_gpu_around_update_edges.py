@@ -228,3 +228,57 @@ def test_rows_of_one_warp_take_their_places_in_the_ring_in_turn(H, res):
     ctx.rms_norm_bwd(p.res.cuda(), *p.head(), p.dy.cuda(), dx, p.dres.cuda(), dg)
     tn.check_bwd(p, p.res, dx, None)
     ctx.check_status()
+
+
+def test_a_captured_update_writes_every_output_again():
+    """Norm, sampling, policy loss, norm backward and clipping of two models in one graph: before the replay every output holds something
+    else, behind it what the calls gave one by one."""
+    N, H, V, K, eps = 200, 256, 4096, 2, 1e-6
+    g = torch.Generator().manual_seed(9)
+    cu, role = torch.tensor([0, 60, 60, 140, 200]).cuda(), torch.tensor([0, 1, 2, 1], dtype=torch.int32).cuda()
+    role_model, T = [0, 1, 1], 0.8
+    tok_role = torch.repeat_interleave(role, cu[1:] - cu[:-1])
+    mask = (torch.rand(N, generator=g) < 0.85).to(torch.uint8).cuda()
+    x, residual = torch.randn(N, H, generator=g).to(B16).cuda(), (torch.randn(N, H, generator=g) * 3).cuda()
+    gamma = [(1 + 0.2 * torch.randn(H, generator=g)).to(B16).cuda() for _ in range(K)]
+    W = [(torch.randn(V, H, generator=g) * 0.15).to(B16).cuda() for _ in range(K)]
+    u, adv, z = torch.rand(N, generator=g).cuda(), torch.randn(N, generator=g).cuda(), (torch.randn(N, V, generator=g) * 3).cuda()
+    rules = [(T, 0, 1.0, 0.0), (T, 50, 0.95, 0.0), (0.0, 0, 1.0, 0.0)]
+    new = lambda *s, t=F32: torch.empty(s, dtype=t, device="cuda")
+    o = dict(y=new(N, H, t=B16), r=new(N, H), token=new(N, t=torch.int32), logp=new(N), logk=new(N), kept=new(N, t=torch.int32), old=new(N),
+             loss=new(K), dh=new(N, H, t=B16), dx=new(N, H), norm=new(K), coef=new(K))
+    lists = dict(dW=[new(V, H) for _ in range(K)], dg=[new(H) for _ in range(K)], out=[new(V, H, t=B16) for _ in range(K)] + [new(H) for _ in range(K)])
+    outputs = list(o.values()) + [t for v in lists.values() for t in v]
+    st = torch.cuda.Stream()
+    ctx = ub.Context(0, max(ub.unity_workspace_bytes(N, H, V, K, 4), ub.unity_rms_norm_workspace_bytes(N, H, K),
+                            ub.unity_clip_grad_norm_workspace_bytes(4, K)), st)
+    handle, route = ub.GradTensors(lists["dW"] + lists["dg"], [0, 1, 0, 1], lists["out"]), (cu, role, role_model)
+    target = torch.empty_like(o["token"])
+
+    def step():
+        ctx.rms_norm_fwd(x, gamma, *route, mask, eps, o["y"], residual, o["r"])
+        ctx.sample(z, rules, u, o["token"], tok_role, mask, o["logp"], o["logk"], o["kept"])
+        torch.clamp(o["token"], min=0, out=target)
+        ctx.logprob_fwd(o["y"], W, *route, target, mask, 1 / T, o["old"])
+        ctx.ppo_loss_fwd_bwd(o["y"], W, *route, target, mask, 1 / T, 0.2, 0.2, 0.01, 3, 0.0, None, False, o["old"], o["old"], adv, o["loss"],
+                             None, None, None, None, o["dh"], lists["dW"])
+        ctx.rms_norm_bwd(o["r"], gamma, *route, mask, eps, o["dh"], o["dx"], residual, lists["dg"])
+        ctx.clip_grad_norm(handle, [1e-3, 1e3], o["norm"], o["coef"])
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in outputs]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        step()
+    for _ in range(2):
+        for t in outputs:
+            t.fill_(5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t, w in zip(outputs, want):
+            assert torch.equal(t, w)
+        ctx.check_status()
