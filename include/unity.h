@@ -522,8 +522,9 @@ int unity_rms_norm_bwd(unity_ctx* ctx, const unity_norm_rows* rows, const void* 
  *   max_norm : (host) f32 [K], >= 0, inf = no bound; NULL: norms only (out is not written)
  *   norm     : out f32 [K] (0 for a model without tensors);  coef : out f32 [K] or NULL
  * In place, a model within its bound is not written at all.  A norm that is not finite makes coef 0 or NaN and the outputs
- * accordingly: a caller who skips such a step looks at norm first.  Squares are added in fp64 (in fp32 within eight elements where that
- * loses nothing), in a fixed order: neither 1e-30 nor 1e30 underflows or overflows.
+ * accordingly: a caller who skips such a step looks at norm first.  Squares are added in a fixed order: in fp32 within eight elements, which
+ * leaves a vector's sum within 8 * 2^-24 of itself (in fp64 where fp32 might underflow or overflow, so neither 1e-30 nor 1e30 does), all
+ * else in fp64; the norm is within 5 * 2^-24 of its value.
  * Tensors need the alignment of their elements only.  Workspace: unity_clip_grad_norm_workspace_bytes(). */
 typedef struct {
     void* data;
@@ -550,7 +551,8 @@ int unity_clip_grad_norm(unity_ctx* ctx, int32_t n_tensors, const unity_tensor* 
  *   n_kept   : number of kept entries;  logp, logp_kept, n_kept may be NULL
  * Rows with row_mask == 0 (answers that are finished) get token -1 and 0 elsewhere, and their logits are not read; so do rows with a
  * role out of range or u outside [0, 1), which flag UNITY_ERR_BAD_INDEX.  Rows with a NaN or +inf, or with nothing above -inf, get
- * token -1, n_kept 0 and NaN elsewhere.  Tokens and n_kept are those of 64-bit arithmetic; bitwise reproducible.  No workspace. */
+ * token -1, n_kept 0 and NaN elsewhere.  Tokens and n_kept are those of 64-bit arithmetic.  The same call gives the same bits; a row's
+ * logp and logp_kept may differ in their last digits between calls of few and of many rows, which take other ways.  No workspace. */
 #define UNITY_MAX_SAMPLE_V 262144
 typedef struct {
     float temperature;  /* 0, or 1e-6 .. 1e6 */

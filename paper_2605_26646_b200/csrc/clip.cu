@@ -97,8 +97,9 @@ __device__ __forceinline__ double squares_in_64(const float (&f)[8]) {
     for (int k = 0; k < 8; ++k) s = fma(static_cast<double>(f[k]), static_cast<double>(f[k]), s);
     return s;
 }
-// Eight squares are added in fp32 where that loses nothing: their sum lies far from both ends of the range (a square that
-// underflows is then below 2^-30 of it).  Tiny, huge and zero vectors take 64 bits.
+// Eight squares are added in fp32 where their sum lies far from both ends of the range (a square that underflows is then below 2^-30
+// of it): eight roundings of one addition each, at most 8 2^-24 of the sum, 4 2^-24 of the norm, and all of one sign at worst.  Tiny,
+// huge and zero vectors take 64 bits.
 __device__ __forceinline__ double squares(const float (&f)[8]) {
     float q = 0.f;
 #pragma unroll

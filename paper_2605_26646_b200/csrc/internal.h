@@ -678,7 +678,9 @@ struct ClipEntry {
     int model;
     short src_bf16, dst_bf16;
 };
-constexpr int kClipBlocks = 148 * 4;     // blocks of a launch at most: a double per model of each in the workspace
+// Blocks of a launch at most, a double per model of each in the workspace: four on each of a B200's 148 SMs (a constant, since the
+// workspace's size is asked for without a device; with fewer SMs the results are the same).
+constexpr int kClipBlocks = 148 * 4;
 constexpr int kClipEntries = 800;        // entries of a launch at most: 32 000 bytes of parameters
 long long clip_chunks(const ClipEntry& e);
 int clip_blocks(long long chunks);       // of a launch over so many chunks

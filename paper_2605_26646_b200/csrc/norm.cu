@@ -219,7 +219,9 @@ __global__ void __launch_bounds__(WPR == 1 ? 32 * kFwdRowsOfWarps : 32 * WPR) k_
 // dgamma stays in registers; where the model changes it goes to the block's slice of that model and the next one begins.  The rows
 // come through a ring in shared memory, by asynchronous copies that run ahead of the row that is worked on: registers hold the
 // columns' sums and weights only, and HBM is asked for rows without a pause (40001 x 3584 fp32 with dres: 285 to 300 us, 0.9 of the
-// copy rate; rows in registers, without the ring, 378).  5000 x 1536 bf16: 22 us with the sums of the slices, most of it latency.
+// copy rate; rows in registers, without the ring, 378).  5000 x 1536 bf16: 22 us with the sums of the slices, most of it latency.  A block of
+// 32 warps (H above 8192) has no registers for its row and its dgamma: they go to local memory (8000 x 16384 bf16 610 us with dgamma and
+// 231 without, where 8192 columns take 100 and 96).
 // ------------------------------------------------------------------------------------------------
 constexpr int kMaxStages = 4;
 template <int WPR, int NV, typename R, bool DG>
@@ -522,8 +524,8 @@ static int bwd_warps(int H) {
     while (vectors(H, wpr) > 2) wpr *= 2;
     return wpr;
 }
-// Blocks of the backward, each with a slice of H floats per model for its share of dgamma: 16 warps on an SM, and four rows for a
-// block at least where there are enough.
+// Blocks of the backward, each with a slice of H floats per model for its share of dgamma: 16 warps on each of a B200's 148 SMs (a
+// constant, since the workspace's size is asked for without a device), and four rows for a block at least where there are enough.
 int norm_bwd_blocks(long long n_tok, int H) {
     const int wpr = bwd_warps(H), per_sm = wpr >= 16 ? 1 : 16 / wpr;
     const long long most = 148LL * per_sm, few = n_tok < 148 ? n_tok : n_tok < 4 * 148 ? 148 : (n_tok + 3) / 4;

@@ -16,8 +16,11 @@
 // their error (kSlackFast); where a comparison is closer than that, the row is done again with fp64 exponentials, so the outcome
 // is that of 64-bit arithmetic either way.
 //
-// What bounds it: latency for few rows (one of 152064: 14 us, some ten exchanges of about 1.2 thousand clocks), issue slots for many
-// (512 rows of 151936 fp32: top-p of thirty thousand tokens 900 us; the row's bytes would take 48).
+// What bounds it: latency for few rows (one of 152064 with top-k and top-p: 14 us, six exchanges of about 1.2 thousand clocks where the
+// first list decides, among loads, a pass and a sort), issue slots for many (512 rows of 151936 fp32 with top-p of thirty thousand tokens:
+// 900 us by the search alone, 1010 behind the pass, which does not decide such rows; the rows' bytes would take 48).  Four blocks per SM leave a
+// thread 64 registers, so part of a row's state is in local memory (802 bytes of spill stores in the code for fp32, 878 for bf16); weighing
+// is a function of its own so that its loop has none of it.
 #include <algorithm>
 
 #include "internal.h"
@@ -1013,7 +1016,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_sample(const __grid_constant__ 
 // registers, no copy in shared memory, so that more rows are in flight.  Every warp of the cluster has a run of consecutive entries,
 // in tiles of 512; a lane's mass of a tile refers to a power of two next to the lane's largest entry there.  The warp whose running
 // mass holds the target reads one of its tiles again.  512 rows of 151936: fp32 86 us (3.6 TB/s), bf16 61; each row ends with 6 to 8
-// thousand clocks in which one warp of a block is at work, and rows whose decision is close (a third of flat ones) are read again.
+// thousand clocks in which one warp of a block is at work, and rows whose decision is close (a third of flat ones) or whose largest entry
+// lies so far from 0 that fp32 exponents have no digits left are read again.  Five blocks per SM leave a thread 48 registers (92 to 168
+// bytes of spill stores in the code).
 // ------------------------------------------------------------------------------------------------
 constexpr int kTileEntries = 512, kPerLane = kTileEntries / 32;
 constexpr int kMaxTiles = 20;                // of a warp
