@@ -640,7 +640,8 @@ class GradTensors:
     """The tensors of a clipping call, checked and laid out once: gradients usually stay where they are from step to step.
 
     grads: contiguous f32 or bf16 CUDA tensors of any shape; models: the model of each; outs: tensors that take the scaled
-    gradients (of the same type or bf16, None for in place), or None for all in place.  Keeps the tensors alive."""
+    gradients (of the same type or bf16, None for in place), or None for all in place.  Keeps the tensors and their memory alive; a
+    tensor that is given other memory later (set_, .data) is not followed there."""
 
     def __init__(self, grads: Sequence[torch.Tensor], models: Sequence[int], outs: Optional[Sequence[Optional[torch.Tensor]]] = None):
         self.grads, self.outs = list(grads), [None] * len(grads) if outs is None else list(outs)
@@ -657,6 +658,7 @@ class GradTensors:
                 e.out = _sized(o, g.shape, o.dtype, self.device, "outs")
             if not g.is_cuda:
                 raise ValueError("grads must be CUDA tensors")
+        self.memory = [t.untyped_storage() for t in (*self.grads, *self.outs) if t is not None]
 
     def __len__(self):
         return len(self.grads)

@@ -282,3 +282,23 @@ def test_a_captured_update_writes_every_output_again():
         for t, w in zip(outputs, want):
             assert torch.equal(t, w)
         ctx.check_status()
+
+
+def test_a_list_of_tensors_keeps_its_memory():
+    """A listed tensor that is given other memory: what was listed stays what it was, and nobody else's memory is written."""
+    n = 1 << 20
+    g = torch.full((n,), 2.0, device="cuda")
+    out = torch.empty(n, device="cuda")
+    handle = ub.GradTensors([g, torch.ones(5, device="cuda")], [0, 0], [None, None])
+    other = ub.GradTensors([torch.ones(n, device="cuda")], [0], [out])
+    ctx = ub.Context(0, 1 << 16)
+    norm = torch.zeros(1, device="cuda")
+    with torch.no_grad():
+        g.set_(torch.full((n,), 3.0, device="cuda"))
+        out.set_(torch.full((n,), 3.0, device="cuda"))
+    later = [torch.full((n,), 7.0, device="cuda") for _ in range(8)]
+    ctx.clip_grad_norm(handle, [1.0], norm)
+    assert abs(norm.item() - (4.0 * n + 5) ** 0.5) <= 5.1 * 2.0 ** -24 * (4.0 * n + 5) ** 0.5
+    ctx.clip_grad_norm(other, [1.0], norm)
+    ctx.check_status()
+    assert (g == 3).all() and (out == 3).all() and all((t == 7).all() for t in later)
