@@ -19,7 +19,8 @@
  * - Rows with tok_mask == 0 receive 0 in every per-token output and cost no tensor work.
  * - Limits: 1 <= K <= UNITY_MAX_MODELS, 1 <= n_roles <= UNITY_MAX_ROLES, H % 64 == 0, V % 8 == 0,
  *   hidden / W / dHidden / dW base addresses 16-byte aligned and densely packed (row pitch = H).
- * - One context per stream; a context is not re-entrant.
+ * - One context per stream; a context is not re-entrant.  Contexts of their own may be used from several host threads at once.
+ *   Calls can be captured into a graph; graphs of one context share its workspace, so they are replayed one after another.
  */
 #ifndef UNITY_H_
 #define UNITY_H_
